@@ -74,7 +74,10 @@ enum equarx_status {
     EQUARX_ERR_CUDA = 8,       /* a launch failed; see equarx_last_cuda_error()          */
     EQUARX_ERR_STATIC_LIMIT = 9, /* problem too large for the built-in workspace of
                                   equarx_allreduce_sim_static                            */
-    EQUARX_ERR_FLAVOUR = 10    /* flavour is not a combination of EQUARX_FLAVOUR_* bits  */
+    EQUARX_ERR_FLAVOUR = 10,   /* flavour is not a combination of EQUARX_FLAVOUR_* bits  */
+    EQUARX_ERR_FORMAT = 11,    /* an element type, 4-bit format or activation is not one of
+                                  those the feed-forward calls list                      */
+    EQUARX_ERR_TIMEOUT = 12    /* equarx_feedforward_check: a kernel gave up a wait      */
 };
 
 /*
@@ -403,6 +406,142 @@ int equarx_ring_allreduce(const void *const *in_bf16, void *const *out_bf16,
                           int rank_first, int ranks_here, int nranks, size_t count, int block,
                           void *const *mailboxes, uint32_t epoch, uint64_t timeout_ns,
                           uint32_t *status, equarx_stream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * The feed-forward block in front of the AllReduce.
+ *
+ * In a tensor-parallel layer every rank computes
+ *     h = act(x Wg^T) * (x Wu^T),   partial = h Wd^T
+ * with its own slices of the weights, and the AllReduce sums the partials (in the
+ * backward pass it sums dx).  These calls compute that block: with 16-bit weights
+ * and their gradients, and, for serving, with weights and activations in
+ * microscaled 4-bit floating point.  (The paper has no counterpart for them.)
+ *
+ * Conventions, in addition to those at the top of this file
+ *   - Matrices are row-major: element (r, c) of a matrix with row stride ld is at
+ *     index r * ld + c; ld counts elements and is at least the number of columns.
+ *     Bases are 16-byte aligned; row strides are free (a 16-bit operand whose row
+ *     stride is no multiple of 8 elements is first copied into the workspace).
+ *   - A dimension is at most 2^30.  Zero tokens are allowed (nothing is launched,
+ *     gradients of weights become zero); the other dimensions are at least 1.
+ *   - Element types: EQUARX_BF16, EQUARX_FP16 and, where a call says so,
+ *     EQUARX_FP32.  Products are summed in fp32 and rounded once to the output type.
+ *   - Infinities and NaN follow the arithmetic; nothing traps.  An element that is
+ *     not finite quantizes to a NaN scale of its block (MX) or row (NV).
+ *   - Outputs must not overlap inputs, the workspace or one another.
+ *   - Workspaces and 4-bit buffers are 16-byte aligned.
+ *   - The result does not depend on timing: sums are taken in a fixed order.
+ */
+#define EQUARX_BF16 0
+#define EQUARX_FP16 1
+#define EQUARX_FP32 2
+
+#define EQUARX_ACT_SILU 0        /* g / (1 + e^-g)                                          */
+#define EQUARX_ACT_GELU_TANH 1   /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2          */
+
+/*
+ * Microscaled 4-bit floating point.  An element is E2M1: 0, .5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives, rounded to nearest, ties to the even code, saturating at 6.
+ *   EQUARX_FP4_MX : 32 neighbouring elements of a row share a power of two,
+ *       e = max(floor(log2 amax) - 2, -127) stored as the byte e + 127;
+ *       code = rn(v / 2^e), value = code * 2^e.
+ *   EQUARX_FP4_NV : 16 neighbouring elements share an E4M3 scale s, and a row
+ *       shares one fp32 factor g.  With A the row's largest magnitude (IEEE fp32
+ *       throughout): g = A / 2688, s = e4m3_rn(min(amax * (448 / A), 448)), d = s * g,
+ *       code = rn(v * (1 / d)), 0 where s = 0; value = code * d.  A row with
+ *       A < 2^-100 becomes zero.  The factor is the row's own, so the result for a
+ *       token does not depend on the tokens beside it.
+ *
+ * A quantized matrix of rows x cols is three buffers:
+ *   codes      : rows x ceil(cols/32)*16 bytes, two codes a byte, the first in the
+ *                low half; codes past the last column are 0
+ *   scales     : in the order in which the tensor cores read them: the scale of
+ *                row r and block b is at byte
+ *                (r/128 * tiles + b/4) * 512 + (r%32) * 16 + (r%128/32) * 4 + b%4,
+ *                tiles = ceil(cols/256) * (MX: 2, NV: 4); blocks past the last
+ *                column have scale byte 0, rows past the last are not written
+ *   row_scales : NV: rows floats, 16-byte aligned; MX: unused, may be NULL
+ */
+#define EQUARX_FP4_MX 0
+#define EQUARX_FP4_NV 1
+size_t equarx_fp4_codes_bytes(size_t rows, size_t cols);
+size_t equarx_fp4_scales_bytes(size_t rows, size_t cols, int format);
+
+/* x (rows x cols; BF16, FP16 or FP32) -> the three buffers above. */
+int equarx_fp4_quantize(const void *x, int dtype, size_t rows, size_t cols, size_t ld, int format,
+                        uint8_t *codes, uint8_t *scales, float *row_scales, equarx_stream_t stream);
+
+/* The values that the codes stand for, rounded once to `dtype` (BF16, FP16 or FP32). */
+int equarx_fp4_dequantize(const uint8_t *codes, const uint8_t *scales, const float *row_scales,
+                          size_t rows, size_t cols, int format,
+                          void *out, int dtype, size_t ld, equarx_stream_t stream);
+
+/*
+ * out = a b^T for two quantized matrices of the same format: a is m x k, b is
+ * n x k, out is m x n (BF16, FP16 or FP32).
+ */
+int equarx_fp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const float *a_row_scales,
+                      const uint8_t *b_codes, const uint8_t *b_scales, const float *b_row_scales,
+                      size_t m, size_t n, size_t k, int format,
+                      void *out, int dtype, size_t ld, equarx_stream_t stream);
+
+/*
+ * out = x w^T, x (m x k, BF16 or FP16) quantized by this call, w (n x k) before:
+ * exactly equarx_fp4_quantize followed by equarx_fp4_matmul.  out has x's type.
+ */
+size_t equarx_fp4_linear_workspace_bytes(size_t m, size_t k, int format);
+int equarx_fp4_linear(const void *x, int dtype, size_t ldx,
+                      const uint8_t *w_codes, const uint8_t *w_scales, const float *w_row_scales,
+                      size_t m, size_t n, size_t k, int format, void *out, size_t ld,
+                      void *workspace, size_t workspace_bytes, equarx_stream_t stream);
+
+/*
+ * h = act(x Wg^T) * (x Wu^T) over 4-bit weights (both f x k): both projections, the
+ * activation and the product in one kernel, after x (m x k, BF16 or FP16) has been
+ * quantized by this call.  h is m x f and has x's type.  Workspace:
+ * equarx_fp4_linear_workspace_bytes(m, k, format).
+ */
+int equarx_fp4_gated(const void *x, int dtype, size_t ldx,
+                     const uint8_t *g_codes, const uint8_t *g_scales, const float *g_row_scales,
+                     const uint8_t *u_codes, const uint8_t *u_scales, const float *u_row_scales,
+                     size_t m, size_t f, size_t k, int format, int act, void *h, size_t ldh,
+                     void *workspace, size_t workspace_bytes, equarx_stream_t stream);
+
+/*
+ * h = act(x Wg^T) * (x Wu^T) over 16-bit weights, in one kernel: x is m x k, wg and wu
+ * are f x k, h is m x f, all of one type (BF16 or FP16).  g and u, both m x f with row
+ * stride ldgu, receive the projections x Wg^T and x Wu^T for the backward call; both
+ * are NULL when no gradient is wanted.  Workspace (the copies that row strides make
+ * necessary, often 0 bytes): equarx_gated_forward_workspace_bytes.
+ */
+size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu);
+int equarx_gated_forward(const void *x, size_t ldx, const void *wg, size_t ldwg, const void *wu, size_t ldwu,
+                         int dtype, size_t m, size_t f, size_t k, int act,
+                         void *h, size_t ldh, void *g, void *u, size_t ldgu,
+                         void *workspace, size_t workspace_bytes, equarx_stream_t stream);
+
+/*
+ * Gradients of equarx_gated_forward.  From dh (m x f) and the g and u it kept:
+ *     dU = dh act(g), dG = dh u act'(g), dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.
+ * dU and dG are computed in fp32 and rounded to the 16-bit type that the products read.
+ * dx is m x k, dwg and dwu are f x k, of the inputs' type.
+ */
+size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu);
+int equarx_gated_backward(const void *dh, size_t lddh, const void *x, size_t ldx,
+                          const void *wg, size_t ldwg, const void *wu, size_t ldwu,
+                          const void *g, const void *u, size_t ldgu,
+                          int dtype, size_t m, size_t f, size_t k, int act,
+                          void *dx, size_t lddx, void *dwg, size_t lddwg, void *dwu, size_t lddwu,
+                          void *workspace, size_t workspace_bytes, equarx_stream_t stream);
+
+/*
+ * The kernels of the feed-forward calls wait only for their own copies and products,
+ * and each wait has a limit: a kernel whose wait ran out leaves and its output is
+ * incomplete.  This call synchronises the current device and returns
+ * EQUARX_ERR_TIMEOUT if that has happened on it since the last check, else EQUARX_OK.
+ */
+int equarx_feedforward_check(void);
 
 /* Static, human-readable name of a status. */
 const char *equarx_status_string(int status);

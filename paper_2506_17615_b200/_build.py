@@ -5,13 +5,15 @@ import shutil
 import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(_HERE, "csrc", "equarx_host.cu")]
-DEPENDS = SOURCES + [os.path.join(_HERE, "csrc", "equarx_kernels.cuh"),
-                     os.path.join(os.path.dirname(_HERE), "include", "equarx.h")]
+_CSRC = os.path.join(_HERE, "csrc")
+SOURCES = [os.path.join(_CSRC, "equarx_host.cu"), os.path.join(_CSRC, "feedforward_host.cu")]
+DEPENDS = SOURCES + [os.path.join(_CSRC, name) for name in ("equarx_kernels.cuh", "equarx_internal.h", "tensor_ops.cuh",
+                                                            "feedforward_kernels.cuh")] + \
+    [os.path.join(os.path.dirname(_HERE), "include", "equarx.h")]
 LIB = os.path.join(_HERE, "libequarx.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 
 
 def find_nvcc():

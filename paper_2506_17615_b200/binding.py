@@ -11,8 +11,11 @@ from . import _build
 
 MAX_RANKS = 64
 (OK, ERR_NULL, ERR_NRANKS, ERR_BLOCK, ERR_COUNT, ERR_ALIGN, ERR_WORKSPACE, ERR_ALIAS, ERR_CUDA, ERR_STATIC_LIMIT,
- ERR_FLAVOUR) = range(11)
+ ERR_FLAVOUR, ERR_FORMAT, ERR_TIMEOUT) = range(13)
 FLAVOUR_SEMI_LOOP, FLAVOUR_QUANT_RS, FLAVOUR_QUANT_AG, FLAVOUR_E4M3, FLAVOUR_E5M2 = 1, 2, 4, 8, 16
+BF16, FP16, FP32 = range(3)
+FP4_MX, FP4_NV = range(2)
+ACT_SILU, ACT_GELU_TANH = range(2)
 FLAVOUR_FIFO_BYTES = 16 * 1024 * 1024
 STATIC_WORKSPACE_BYTES = 16 * 1024 * 1024
 
@@ -35,6 +38,19 @@ EXPORTS = (
     "equarx_allreduce_sim_static",
     "equarx_allreduce_sim_bf16_workspace_bytes",
     "equarx_allreduce_sim_bf16",
+    "equarx_fp4_codes_bytes",
+    "equarx_fp4_scales_bytes",
+    "equarx_fp4_quantize",
+    "equarx_fp4_dequantize",
+    "equarx_fp4_matmul",
+    "equarx_fp4_linear",
+    "equarx_fp4_linear_workspace_bytes",
+    "equarx_fp4_gated",
+    "equarx_gated_forward",
+    "equarx_gated_forward_workspace_bytes",
+    "equarx_gated_backward",
+    "equarx_gated_backward_workspace_bytes",
+    "equarx_feedforward_check",
     "equarx_status_string",
     "equarx_last_cuda_error",
 )
@@ -74,6 +90,23 @@ def _load():
     lib.equarx_allreduce_sim_bf16_workspace_bytes.argtypes = [ci, sz]
     lib.equarx_allreduce_sim_bf16_workspace_bytes.restype = sz
     lib.equarx_allreduce_sim_bf16.argtypes = [vp, vp, ci, sz, vp, sz, vp]
+    lib.equarx_fp4_codes_bytes.argtypes = [sz, sz]
+    lib.equarx_fp4_scales_bytes.argtypes = [sz, sz, ci]
+    lib.equarx_fp4_quantize.argtypes = [vp, ci, sz, sz, sz, ci, vp, vp, vp, vp]
+    lib.equarx_fp4_dequantize.argtypes = [vp, vp, vp, sz, sz, ci, vp, ci, sz, vp]
+    lib.equarx_fp4_matmul.argtypes = [vp] * 6 + [sz, sz, sz, ci, vp, ci, sz, vp]
+    lib.equarx_fp4_linear_workspace_bytes.argtypes = [sz, sz, ci]
+    lib.equarx_fp4_linear.argtypes = [vp, ci, sz, vp, vp, vp, sz, sz, sz, ci, vp, sz, vp, sz, vp]
+    lib.equarx_fp4_gated.argtypes = [vp, ci, sz] + [vp] * 6 + [sz, sz, sz, ci, ci, vp, sz, vp, sz, vp]
+    lib.equarx_gated_forward_workspace_bytes.argtypes = [sz] * 6
+    lib.equarx_gated_forward.argtypes = [vp, sz, vp, sz, vp, sz, ci, sz, sz, sz, ci, vp, sz, vp, vp, sz, vp, sz, vp]
+    lib.equarx_gated_backward_workspace_bytes.argtypes = [sz] * 6
+    lib.equarx_gated_backward.argtypes = [vp, sz, vp, sz, vp, sz, vp, sz, vp, vp, sz, ci, sz, sz, sz, ci, vp, sz, vp, sz,
+                                          vp, sz, vp, sz, vp]
+    for name in ("fp4_codes_bytes", "fp4_scales_bytes", "fp4_linear_workspace_bytes", "gated_forward_workspace_bytes",
+                 "gated_backward_workspace_bytes"):
+        getattr(lib, "equarx_" + name).restype = sz
+    lib.equarx_feedforward_check.argtypes = []
     lib.equarx_status_string.argtypes = [ci]
     lib.equarx_status_string.restype = ctypes.c_char_p
     lib.equarx_last_cuda_error.argtypes = []
@@ -220,6 +253,80 @@ def allreduce_sim_bf16(in_bf16, out_bf16, nranks, count, workspace, workspace_by
     _check(lib.equarx_allreduce_sim_bf16(_table(in_bf16), _table(out_bf16), nranks, count, _ptr(workspace),
                                          workspace_bytes, _ptr(stream)),
            "equarx_allreduce_sim_bf16")
+
+
+# ---- the feed-forward block (paper_2506_17615_b200.feedforward wraps these for torch tensors)
+
+def fp4_codes_bytes(rows, cols):
+    return lib.equarx_fp4_codes_bytes(rows, cols)
+
+
+def fp4_scales_bytes(rows, cols, format):
+    return lib.equarx_fp4_scales_bytes(rows, cols, format)
+
+
+def fp4_quantize(x, dtype, rows, cols, ld, format, codes, scales, row_scales, stream=0):
+    _check(lib.equarx_fp4_quantize(_ptr(x), dtype, rows, cols, ld, format, _ptr(codes), _ptr(scales), _ptr(row_scales),
+                                   _ptr(stream)),
+           "equarx_fp4_quantize")
+
+
+def fp4_dequantize(codes, scales, row_scales, rows, cols, format, out, dtype, ld, stream=0):
+    _check(lib.equarx_fp4_dequantize(_ptr(codes), _ptr(scales), _ptr(row_scales), rows, cols, format, _ptr(out), dtype, ld,
+                                     _ptr(stream)),
+           "equarx_fp4_dequantize")
+
+
+def fp4_matmul(a_codes, a_scales, a_row_scales, b_codes, b_scales, b_row_scales, m, n, k, format, out, dtype, ld, stream=0):
+    _check(lib.equarx_fp4_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(a_row_scales), _ptr(b_codes), _ptr(b_scales),
+                                 _ptr(b_row_scales), m, n, k, format, _ptr(out), dtype, ld, _ptr(stream)),
+           "equarx_fp4_matmul")
+
+
+def fp4_linear_workspace_bytes(m, k, format):
+    return lib.equarx_fp4_linear_workspace_bytes(m, k, format)
+
+
+def fp4_linear(x, dtype, ldx, w_codes, w_scales, w_row_scales, m, n, k, format, out, ld, workspace, workspace_bytes,
+               stream=0):
+    _check(lib.equarx_fp4_linear(_ptr(x), dtype, ldx, _ptr(w_codes), _ptr(w_scales), _ptr(w_row_scales), m, n, k, format,
+                                 _ptr(out), ld, _ptr(workspace), workspace_bytes, _ptr(stream)),
+           "equarx_fp4_linear")
+
+
+def fp4_gated(x, dtype, ldx, g_codes, g_scales, g_row_scales, u_codes, u_scales, u_row_scales, m, f, k, format, act, h, ldh,
+              workspace, workspace_bytes, stream=0):
+    _check(lib.equarx_fp4_gated(_ptr(x), dtype, ldx, _ptr(g_codes), _ptr(g_scales), _ptr(g_row_scales), _ptr(u_codes),
+                                _ptr(u_scales), _ptr(u_row_scales), m, f, k, format, act, _ptr(h), ldh, _ptr(workspace),
+                                workspace_bytes, _ptr(stream)),
+           "equarx_fp4_gated")
+
+
+def gated_forward_workspace_bytes(m, f, k, ldx, ldwg, ldwu):
+    return lib.equarx_gated_forward_workspace_bytes(m, f, k, ldx, ldwg, ldwu)
+
+
+def gated_forward(x, ldx, wg, ldwg, wu, ldwu, dtype, m, f, k, act, h, ldh, g, u, ldgu, workspace, workspace_bytes, stream=0):
+    _check(lib.equarx_gated_forward(_ptr(x), ldx, _ptr(wg), ldwg, _ptr(wu), ldwu, dtype, m, f, k, act, _ptr(h), ldh, _ptr(g),
+                                    _ptr(u), ldgu, _ptr(workspace), workspace_bytes, _ptr(stream)),
+           "equarx_gated_forward")
+
+
+def gated_backward_workspace_bytes(m, f, k, ldx, ldwg, ldwu):
+    return lib.equarx_gated_backward_workspace_bytes(m, f, k, ldx, ldwg, ldwu)
+
+
+def gated_backward(dh, lddh, x, ldx, wg, ldwg, wu, ldwu, g, u, ldgu, dtype, m, f, k, act, dx, lddx, dwg, lddwg, dwu, lddwu,
+                   workspace, workspace_bytes, stream=0):
+    _check(lib.equarx_gated_backward(_ptr(dh), lddh, _ptr(x), ldx, _ptr(wg), ldwg, _ptr(wu), ldwu, _ptr(g), _ptr(u), ldgu,
+                                     dtype, m, f, k, act, _ptr(dx), lddx, _ptr(dwg), lddwg, _ptr(dwu), lddwu,
+                                     _ptr(workspace), workspace_bytes, _ptr(stream)),
+           "equarx_gated_backward")
+
+
+def feedforward_check():
+    """Synchronises; raises if a feed-forward kernel gave up a wait since the last check."""
+    _check(lib.equarx_feedforward_check(), "equarx_feedforward_check")
 
 
 RECORD_BYTES, RECORD_HEADER, TILE_ELEMS = 544, 32, 512

@@ -12,6 +12,7 @@
 #include <cstring>
 
 #include "../../include/equarx.h"
+#include "equarx_internal.h"
 
 namespace {
 
@@ -268,11 +269,28 @@ const char* equarx_status_string(int status) {
         case EQUARX_ERR_FLAVOUR: return "EQUARX_ERR_FLAVOUR: flavour must be a combination of the EQUARX_FLAVOUR_* bits";
         case EQUARX_ERR_STATIC_LIMIT:
             return "EQUARX_ERR_STATIC_LIMIT: problem needs more than the 16 MiB built-in workspace";
+        case EQUARX_ERR_FORMAT: return "EQUARX_ERR_FORMAT: unknown element type, 4-bit format or activation";
+        case EQUARX_ERR_TIMEOUT: return "EQUARX_ERR_TIMEOUT: a feed-forward kernel gave up a wait; its output is incomplete";
         default: return "EQUARX: unknown status";
     }
 }
 
 int equarx_last_cuda_error(void) { return g_last_cuda_error; }
+
+}  // extern "C"
+
+namespace equarx {
+// the same launch policy and error record for the other translation unit of the library
+cudaError_t launch_error_to_inject() { return injected_launch_error(); }
+bool dependent_launches() { return use_pdl(); }
+int cuda_failure(cudaError_t e) {
+    g_last_cuda_error = int(e);
+    (void)cudaGetLastError();
+    return EQUARX_ERR_CUDA;
+}
+}  // namespace equarx
+
+extern "C" {
 
 int equarx_quantize_blocks(const void* x_bf16, size_t count, int block, int8_t* codes, float* scales,
                            equarx_stream_t stream) {

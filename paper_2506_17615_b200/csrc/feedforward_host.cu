@@ -1,0 +1,615 @@
+// C ABI of the feed-forward block (include/equarx.h): argument checks, tensor maps, launches.
+#include <algorithm>
+#include <mutex>
+#include <vector>
+
+#include "../../include/equarx.h"
+#include "equarx_internal.h"
+#include "feedforward_kernels.cuh"
+
+namespace {
+
+using namespace equarx;
+using namespace equarx::ff;
+
+constexpr size_t kMaxDim = size_t(1) << 30;
+constexpr size_t kBigSmem = 227 * 1024;
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
+inline size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------- checks
+struct Span {
+    const void* p;
+    size_t bytes;
+};
+// bytes of a rows x cols matrix from its first to its last element
+inline Span matrix(const void* p, size_t rows, size_t cols, size_t ld, size_t size) {
+    return Span{p, rows ? ((rows - 1) * ld + cols) * size : 0};
+}
+inline bool overlap(const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.bytes && b.bytes && a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+// no output may meet an input or another output
+int check_overlap(std::initializer_list<Span> in, std::initializer_list<Span> out) {
+    for (auto o = out.begin(); o != out.end(); ++o) {
+        for (const Span& i : in)
+            if (overlap(*o, i)) return EQUARX_ERR_ALIAS;
+        for (auto q = out.begin(); q != o; ++q)
+            if (overlap(*o, *q)) return EQUARX_ERR_ALIAS;
+    }
+    return EQUARX_OK;
+}
+inline bool bad_dim(size_t d) { return d == 0 || d > kMaxDim; }
+inline bool bad_ld(size_t ld, size_t cols) { return ld < cols || ld > kMaxDim; }
+inline bool is_16bit(int dtype) { return dtype == EQUARX_BF16 || dtype == EQUARX_FP16; }
+inline bool is_float(int dtype) { return is_16bit(dtype) || dtype == EQUARX_FP32; }
+inline bool is_format(int f) { return f == EQUARX_FP4_MX || f == EQUARX_FP4_NV; }
+inline bool is_act(int a) { return a == EQUARX_ACT_SILU || a == EQUARX_ACT_GELU_TANH; }
+inline size_t size_of(int dtype) { return dtype == EQUARX_FP32 ? 4 : 2; }
+
+// ---------------------------------------------------------------- device facts, constant for the process
+int current_device(int& sms) {
+    static std::mutex mu;
+    static std::vector<int> counts;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_failure(e);
+    std::lock_guard<std::mutex> lock(mu);
+    if (int(counts.size()) <= dev) counts.resize(dev + 1, 0);
+    if (!counts[dev]) {
+        e = cudaDeviceGetAttribute(&counts[dev], cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return cuda_failure(e);
+    }
+    sms = counts[dev];
+    return EQUARX_OK;
+}
+
+// kernels that need more than 48 KB of shared memory ask for it once per device
+cudaError_t allow_smem(const void* kernel) {
+    struct Entry {
+        int dev;
+        const void* kernel;
+    };
+    static std::mutex mu;
+    static std::vector<Entry> seen;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mu);
+    for (const Entry& en : seen)
+        if (en.dev == dev && en.kernel == kernel) return cudaSuccess;
+    cudaFuncAttributes fa;
+    e = cudaFuncGetAttributes(&fa, kernel);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kBigSmem - fa.sharedSizeBytes));
+    if (e == cudaSuccess) seen.push_back(Entry{dev, kernel});
+    return e;
+}
+
+template <typename Args>
+int launch(void (*kernel)(Args), dim3 grid, int threads, size_t smem, unsigned cluster, const Args& args,
+           cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    unsigned n = 0;
+    if (dependent_launches()) {      // every kernel waits for the stream's earlier work before it reads
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = cluster;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    cudaError_t e = launch_error_to_inject();
+    if (e == cudaSuccess && smem > 48 * 1024) e = allow_smem(reinterpret_cast<const void*>(kernel));
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, args);
+    return e == cudaSuccess ? EQUARX_OK : cuda_failure(e);
+}
+
+// ---------------------------------------------------------------- tensor maps
+// The driver's encoder is looked up through the runtime, so the library needs no link to the driver.
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {
+    static Encode fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<Encode>(p);
+    }();
+    return fn;
+}
+
+// rows x inner elements of 1 or 2 bytes, row stride in bytes; boxes of box_rows x 128 bytes, swizzled;
+// elements outside the matrix read as zero
+int make_map(CUtensorMap& map, const void* base, size_t elem, size_t inner, size_t rows, size_t stride, size_t box_rows) {
+    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {stride};
+    const cuuint32_t box[2] = {cuuint32_t(kRowBytes / elem), cuuint32_t(box_rows)}, steps[2] = {1, 1};
+    const Encode fn = encoder();
+    if (!fn) return cuda_failure(cudaErrorNotSupported);
+    const CUresult r = fn(&map, elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2,
+                          const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? EQUARX_OK : cuda_failure(cudaErrorInvalidValue);
+}
+
+#define TRY(call)                              \
+    do {                                       \
+        if (const int try_status = (call)) return try_status; \
+    } while (0)
+
+inline Out out_rows(void* p, size_t ld, int dtype) {
+    return Out{p, ld, dtype, int(aligned(p, 16) && ld * size_of(dtype) % 16 == 0)};
+}
+
+// ---------------------------------------------------------------- 4-bit matrices
+struct Fp4 {
+    const uint8_t *codes, *scales;
+    const float* row_scales;
+};
+inline size_t codes_stride(size_t cols) { return ceil_div(cols, 32) * 16; }
+inline size_t fp4_stages(size_t cols) { return ceil_div(cols, 256); }
+inline size_t scales_bytes(size_t rows, size_t cols, int format) {
+    return ceil_div(rows, 128) * fp4_stages(cols) * (format == EQUARX_FP4_MX ? kScaleBytes<kMx> : kScaleBytes<kNv>);
+}
+int check_fp4(const Fp4& q, int format) {
+    if (!q.codes || !q.scales || (format == EQUARX_FP4_NV && !q.row_scales)) return EQUARX_ERR_NULL;
+    if (!aligned(q.codes, 16) || !aligned(q.scales, 16) || (format == EQUARX_FP4_NV && !aligned(q.row_scales, 16)))
+        return EQUARX_ERR_ALIGN;
+    return EQUARX_OK;
+}
+inline Span codes_span(const Fp4& q, size_t rows, size_t cols) { return Span{q.codes, rows * codes_stride(cols)}; }
+inline Span scales_span(const Fp4& q, size_t rows, size_t cols, int format) {
+    return Span{q.scales, scales_bytes(rows, cols, format)};
+}
+inline Span rows_span(const Fp4& q, size_t rows, int format) {
+    return Span{format == EQUARX_FP4_NV ? q.row_scales : nullptr, rows * sizeof(float)};
+}
+
+template <bool MX>
+int launch_quantize(const QuantArgs& a, int sms, cudaStream_t stream) {
+    // A warp for each row once that gives every SM eight of them; below, a CTA for each row.
+    if (a.rows >= 8 * sms) return launch(fp4_quantize_kernel<MX, 1>, dim3(ceil_div(a.rows, 8)), 256, 0, 1, a, stream);
+    return launch(fp4_quantize_kernel<MX, 8>, dim3(a.rows), 256, 0, 1, a, stream);
+}
+int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int format, const Fp4& q, cudaStream_t stream) {
+    int sms;
+    TRY(current_device(sms));
+    QuantArgs a = {};
+    a.x = x;
+    a.codes = const_cast<uint8_t*>(q.codes);
+    a.scales = const_cast<uint8_t*>(q.scales);
+    a.row_scales = const_cast<float*>(q.row_scales);
+    a.ld = ld;
+    a.rows = int(rows);
+    a.cols = int(cols);
+    a.dtype = dtype;
+    a.vec = aligned(x, 16) && ld * size_of(dtype) % 16 == 0;
+    return format == EQUARX_FP4_MX ? launch_quantize<true>(a, sms, stream) : launch_quantize<false>(a, sms, stream);
+}
+
+// ---------------------------------------------------------------- launches of the products
+// Tokens up to which the transposed kernel is used.
+constexpr size_t kFewTokens = 128;
+
+template <int KIND, int MODE, bool A_MN, bool B_MN>
+int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
+    int sms;
+    TRY(current_device(sms));
+    a.m = int(m);
+    a.n = int(n);
+    const int half = MODE == kGated ? a.bn / 2 : a.bn;
+    a.tiles_m = int(ceil_div(m, kRowsM));
+    a.tiles_n = int(ceil_div(n, half));
+    a.group = 16;
+    const size_t tiles = size_t(a.tiles_m) * a.tiles_n * (MODE == kOut2 ? 2 : 1);
+    return launch(tile_kernel<KIND, MODE, A_MN, B_MN>, dim3(unsigned(std::min<size_t>(tiles, sms))), kTileThreads,
+                  kTileSmem<KIND>, 1, a, stream);
+}
+
+template <int KIND, int MODE, bool W_MN>
+int launch_split(SplitArgs& a, size_t features, size_t tokens, cudaStream_t stream) {
+    int sms;
+    TRY(current_device(sms));
+    a.features = int(features);
+    a.tokens = int(tokens);
+    const size_t tiles = ceil_div(features, kRowsM) * ceil_div(tokens, a.nt);
+    const int total = a.stages * (MODE == kSum2 ? 2 : 1);
+    // as many parts of the reduction axis as fill the SMs: at most 8, the portable cluster size
+    const int ranks = int(std::max<size_t>(1, std::min<size_t>({8, size_t(total), size_t(sms) / tiles})));
+    const int stage = split_stage_bytes<KIND, MODE>(a.nt);
+    const int partial = (MODE == kGated ? 2 : 1) * a.nt * 128 * 4;
+    a.pipe = std::min({kSplitMaxPipe, int(ceil_div(total, ranks)), (200 * 1024) / stage});
+    const size_t smem = std::max(a.pipe * stage, partial) + kSmemSlack;
+    const dim3 grid(ranks, unsigned(ceil_div(features, kRowsM)), unsigned(ceil_div(tokens, a.nt)));
+    return launch(split_kernel<KIND, MODE, W_MN>, grid, kSplitThreads, smem, ranks, a, stream);
+}
+
+inline int token_tile(size_t tokens) { return int(std::min<size_t>(128, up(tokens, 16))); }
+
+template <int KIND, int MODE>
+int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, cudaStream_t stream) {
+    const size_t stride = codes_stride(k);
+    constexpr int NW = MODE == kGated ? 2 : 1;
+    if (m <= kFewTokens) {
+        SplitArgs a = {};
+        a.nt = token_tile(m);
+        for (int i = 0; i < NW; ++i) {
+            TRY(make_map(a.w[i], w[i].codes, 1, stride, n, stride, kRowsM));
+            a.scales_w[i] = w[i].scales;
+            a.row_w[i] = w[i].row_scales;
+        }
+        TRY(make_map(a.x[0], x.codes, 1, stride, m, stride, a.nt));
+        a.scales_x = x.scales;
+        a.row_x = x.row_scales;
+        a.out[0] = out;
+        a.stages = int(fp4_stages(k));
+        a.act = act;
+        return launch_split<KIND, MODE, false>(a, n, m, stream);
+    }
+    TileArgs a = {};
+    a.bn = 256;
+    TRY(make_map(a.a[0], x.codes, 1, stride, m, stride, kRowsM));
+    for (int i = 0; i < NW; ++i) {
+        TRY(make_map(a.b[i], w[i].codes, 1, stride, n, stride, a.bn / NW));
+        a.scales_b[i] = w[i].scales;
+        a.row_b[i] = w[i].row_scales;
+    }
+    a.scales_a = x.scales;
+    a.row_a = x.row_scales;
+    a.out[0] = out;
+    a.stages = int(fp4_stages(k));
+    a.act = act;
+    return launch_tiles<KIND, MODE, false, false>(a, m, n, stream);
+}
+
+// the workspace of a quantized activation: scales, row factors, codes
+Fp4 carve(void* ws, size_t rows, size_t cols, int format) {
+    uint8_t* p = static_cast<uint8_t*>(ws);
+    Fp4 q;
+    q.scales = p;
+    p += up(scales_bytes(rows, cols, format), 256);
+    q.row_scales = reinterpret_cast<float*>(p);
+    p += up(rows * sizeof(float), 256);
+    q.codes = p;
+    return q;
+}
+inline size_t carved_bytes(size_t rows, size_t cols, int format) {
+    return up(scales_bytes(rows, cols, format), 256) + up(rows * sizeof(float), 256) + up(rows * codes_stride(cols), 256);
+}
+
+// ---------------------------------------------------------------- 16-bit operands
+// TMA reads rows whose stride is a multiple of 16 bytes; others are copied
+inline bool needs_copy(size_t ld) { return ld % 8 != 0; }
+inline size_t copy_bytes(size_t rows, size_t cols, size_t ld) { return needs_copy(ld) ? up(rows * up(cols, 8) * 2, 256) : 0; }
+
+struct Operand {
+    const void* p;
+    size_t ld;
+};
+int readable(Operand& o, size_t rows, size_t cols, uint8_t*& ws, cudaStream_t stream) {
+    if (!needs_copy(o.ld)) return EQUARX_OK;
+    PackArgs a = {};
+    a.src = static_cast<const uint16_t*>(o.p);
+    a.dst = reinterpret_cast<uint16_t*>(ws);
+    a.ld_src = o.ld;
+    a.ld_dst = up(cols, 8);
+    a.rows = int(rows);
+    a.cols = int(cols);
+    int sms;
+    TRY(current_device(sms));
+    const size_t groups = rows * (a.ld_dst / 8);
+    TRY(launch(pack_kernel, dim3(unsigned(std::min<size_t>(ceil_div(groups, 256), size_t(sms) * 8))), 256, 0, 1, a, stream));
+    ws += copy_bytes(rows, cols, o.ld);
+    o.p = a.dst;
+    o.ld = a.ld_dst;
+    return EQUARX_OK;
+}
+inline int map16(CUtensorMap& map, const Operand& o, size_t rows, size_t cols, size_t box_rows) {
+    return make_map(map, o.p, 2, cols, rows, o.ld * 2, box_rows);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t equarx_fp4_codes_bytes(size_t rows, size_t cols) {
+    return rows > kMaxDim || bad_dim(cols) ? 0 : rows * codes_stride(cols);
+}
+
+size_t equarx_fp4_scales_bytes(size_t rows, size_t cols, int format) {
+    return rows > kMaxDim || bad_dim(cols) || !is_format(format) ? 0 : scales_bytes(rows, cols, format);
+}
+
+int equarx_fp4_quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int format, uint8_t* codes,
+                        uint8_t* scales, float* row_scales, equarx_stream_t stream) {
+    if (!is_float(dtype) || !is_format(format)) return EQUARX_ERR_FORMAT;
+    if (rows > kMaxDim || bad_dim(cols) || bad_ld(ld, cols)) return EQUARX_ERR_COUNT;
+    if (rows == 0) return EQUARX_OK;
+    const Fp4 q{codes, scales, row_scales};
+    if (!x) return EQUARX_ERR_NULL;
+    TRY(check_fp4(q, format));
+    if (!aligned(x, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({matrix(x, rows, cols, ld, size_of(dtype))},
+                      {codes_span(q, rows, cols), scales_span(q, rows, cols, format), rows_span(q, rows, format)}));
+    return quantize(x, dtype, rows, cols, ld, format, q, stream);
+}
+
+int equarx_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, const float* row_scales, size_t rows, size_t cols,
+                          int format, void* out, int dtype, size_t ld, equarx_stream_t stream) {
+    if (!is_float(dtype) || !is_format(format)) return EQUARX_ERR_FORMAT;
+    if (rows > kMaxDim || bad_dim(cols) || bad_ld(ld, cols)) return EQUARX_ERR_COUNT;
+    if (rows == 0) return EQUARX_OK;
+    const Fp4 q{codes, scales, row_scales};
+    if (!out) return EQUARX_ERR_NULL;
+    TRY(check_fp4(q, format));
+    if (!aligned(out, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({codes_span(q, rows, cols), scales_span(q, rows, cols, format), rows_span(q, rows, format)},
+                      {matrix(out, rows, cols, ld, size_of(dtype))}));
+    int sms;
+    TRY(current_device(sms));
+    DequantArgs a = {};
+    a.codes = codes;
+    a.scales = scales;
+    a.row_scales = row_scales;
+    a.out = out;
+    a.ld = ld;
+    a.rows = int(rows);
+    a.cols = int(cols);
+    a.dtype = dtype;
+    a.vec = ld * size_of(dtype) % 16 == 0;
+    const size_t groups = rows * ceil_div(cols, 16);
+    const dim3 grid(unsigned(std::min<size_t>(ceil_div(groups, 256), size_t(sms) * 8)));
+    return format == EQUARX_FP4_MX ? launch(fp4_dequantize_kernel<true>, grid, 256, 0, 1, a, stream)
+                                   : launch(fp4_dequantize_kernel<false>, grid, 256, 0, 1, a, stream);
+}
+
+int equarx_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_row_scales, const uint8_t* b_codes,
+                      const uint8_t* b_scales, const float* b_row_scales, size_t m, size_t n, size_t k, int format, void* out,
+                      int dtype, size_t ld, equarx_stream_t stream) {
+    if (!is_float(dtype) || !is_format(format)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(n) || bad_dim(k) || bad_ld(ld, n)) return EQUARX_ERR_COUNT;
+    if (m == 0) return EQUARX_OK;
+    const Fp4 a{a_codes, a_scales, a_row_scales}, b{b_codes, b_scales, b_row_scales};
+    if (!out) return EQUARX_ERR_NULL;
+    TRY(check_fp4(a, format));
+    TRY(check_fp4(b, format));
+    if (!aligned(out, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({codes_span(a, m, k), scales_span(a, m, k, format), rows_span(a, m, format), codes_span(b, n, k),
+                       scales_span(b, n, k, format), rows_span(b, n, format)},
+                      {matrix(out, m, n, ld, size_of(dtype))}));
+    const Out o = out_rows(out, ld, dtype);
+    return format == EQUARX_FP4_MX ? fp4_product<kMx, kPlain>(a, &b, m, n, k, 0, o, stream)
+                                   : fp4_product<kNv, kPlain>(a, &b, m, n, k, 0, o, stream);
+}
+
+size_t equarx_fp4_linear_workspace_bytes(size_t m, size_t k, int format) {
+    return m > kMaxDim || bad_dim(k) || !is_format(format) ? 0 : carved_bytes(m, k, format);
+}
+
+int equarx_fp4_linear(const void* x, int dtype, size_t ldx, const uint8_t* w_codes, const uint8_t* w_scales,
+                      const float* w_row_scales, size_t m, size_t n, size_t k, int format, void* out, size_t ld,
+                      void* workspace, size_t workspace_bytes, equarx_stream_t stream) {
+    if (!is_16bit(dtype) || !is_format(format)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(n) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ld, n)) return EQUARX_ERR_COUNT;
+    if (m == 0) return EQUARX_OK;
+    const Fp4 w{w_codes, w_scales, w_row_scales};
+    if (!x || !out || !workspace) return EQUARX_ERR_NULL;
+    TRY(check_fp4(w, format));
+    if (workspace_bytes < carved_bytes(m, k, format)) return EQUARX_ERR_WORKSPACE;
+    if (!aligned(x, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({matrix(x, m, k, ldx, 2), codes_span(w, n, k), scales_span(w, n, k, format), rows_span(w, n, format)},
+                      {matrix(out, m, n, ld, 2), Span{workspace, workspace_bytes}}));
+    const Fp4 q = carve(workspace, m, k, format);
+    TRY(quantize(x, dtype, m, k, ldx, format, q, stream));
+    const Out o = out_rows(out, ld, dtype);
+    return format == EQUARX_FP4_MX ? fp4_product<kMx, kPlain>(q, &w, m, n, k, 0, o, stream)
+                                   : fp4_product<kNv, kPlain>(q, &w, m, n, k, 0, o, stream);
+}
+
+int equarx_fp4_gated(const void* x, int dtype, size_t ldx, const uint8_t* g_codes, const uint8_t* g_scales,
+                     const float* g_row_scales, const uint8_t* u_codes, const uint8_t* u_scales, const float* u_row_scales,
+                     size_t m, size_t f, size_t k, int format, int act, void* h, size_t ldh, void* workspace,
+                     size_t workspace_bytes, equarx_stream_t stream) {
+    if (!is_16bit(dtype) || !is_format(format) || !is_act(act)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldh, f)) return EQUARX_ERR_COUNT;
+    if (m == 0) return EQUARX_OK;
+    const Fp4 w[2] = {{g_codes, g_scales, g_row_scales}, {u_codes, u_scales, u_row_scales}};
+    if (!x || !h || !workspace) return EQUARX_ERR_NULL;
+    TRY(check_fp4(w[0], format));
+    TRY(check_fp4(w[1], format));
+    if (workspace_bytes < carved_bytes(m, k, format)) return EQUARX_ERR_WORKSPACE;
+    if (!aligned(x, 16) || !aligned(h, 16) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({matrix(x, m, k, ldx, 2), codes_span(w[0], f, k), scales_span(w[0], f, k, format),
+                       rows_span(w[0], f, format), codes_span(w[1], f, k), scales_span(w[1], f, k, format),
+                       rows_span(w[1], f, format)},
+                      {matrix(h, m, f, ldh, 2), Span{workspace, workspace_bytes}}));
+    const Fp4 q = carve(workspace, m, k, format);
+    TRY(quantize(x, dtype, m, k, ldx, format, q, stream));
+    const Out o = out_rows(h, ldh, dtype);
+    return format == EQUARX_FP4_MX ? fp4_product<kMx, kGated>(q, w, m, f, k, act, o, stream)
+                                   : fp4_product<kNv, kGated>(q, w, m, f, k, act, o, stream);
+}
+
+size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu) {
+    if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k)) return 0;
+    return copy_bytes(m, k, ldx) + copy_bytes(f, k, ldwg) + copy_bytes(f, k, ldwu);
+}
+
+int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg, const void* wu, size_t ldwu, int dtype,
+                         size_t m, size_t f, size_t k, int act, void* h, size_t ldh, void* g, void* u, size_t ldgu,
+                         void* workspace, size_t workspace_bytes, equarx_stream_t stream) {
+    if (!is_16bit(dtype) || !is_act(act)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k) || bad_ld(ldh, f))
+        return EQUARX_ERR_COUNT;
+    if (m == 0) return EQUARX_OK;
+    if (!x || !wg || !wu || !h || (!g) != (!u)) return EQUARX_ERR_NULL;
+    if (g && bad_ld(ldgu, f)) return EQUARX_ERR_COUNT;
+    const size_t need = equarx_gated_forward_workspace_bytes(m, f, k, ldx, ldwg, ldwu);
+    if (need && !workspace) return EQUARX_ERR_NULL;
+    if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
+    for (const void* p : {x, wg, wu, static_cast<const void*>(h), static_cast<const void*>(g), static_cast<const void*>(u),
+                          static_cast<const void*>(workspace)})
+        if (!aligned(p, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({matrix(x, m, k, ldx, 2), matrix(wg, f, k, ldwg, 2), matrix(wu, f, k, ldwu, 2)},
+                      {matrix(h, m, f, ldh, 2), matrix(g, m, f, ldgu, 2), matrix(u, m, f, ldgu, 2), Span{workspace, need}}));
+
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    Operand ox{x, ldx}, og{wg, ldwg}, ou{wu, ldwu};
+    TRY(readable(ox, m, k, ws, stream));
+    TRY(readable(og, f, k, ws, stream));
+    TRY(readable(ou, f, k, ws, stream));
+    const Out oh = out_rows(h, ldh, dtype), sg = out_rows(g, ldgu, dtype), su = out_rows(u, ldgu, dtype);
+    const int stages = int(ceil_div(k, 64));
+    if (m <= kFewTokens) {
+        SplitArgs a = {};
+        a.nt = token_tile(m);
+        TRY(map16(a.w[0], og, f, k, kRowsM));
+        TRY(map16(a.w[1], ou, f, k, kRowsM));
+        TRY(map16(a.x[0], ox, m, k, a.nt));
+        a.out[0] = oh;
+        a.out[1] = sg;
+        a.out[2] = su;
+        a.stages = stages;
+        a.act = act;
+        a.bf16 = dtype == EQUARX_BF16;
+        a.save = g != nullptr;
+        return launch_split<kHalf, kGated, false>(a, f, m, stream);
+    }
+    TileArgs a = {};
+    a.bn = 256;
+    TRY(map16(a.a[0], ox, m, k, kRowsM));
+    TRY(map16(a.b[0], og, f, k, a.bn / 2));
+    TRY(map16(a.b[1], ou, f, k, a.bn / 2));
+    a.out[0] = oh;
+    a.out[1] = sg;
+    a.out[2] = su;
+    a.stages = stages;
+    a.act = act;
+    a.bf16 = dtype == EQUARX_BF16;
+    a.save = g != nullptr;
+    return launch_tiles<kHalf, kGated, false, false>(a, m, f, stream);
+}
+
+size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu) {
+    if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k)) return 0;
+    return copy_bytes(m, k, ldx) + copy_bytes(f, k, ldwg) + copy_bytes(f, k, ldwu) + 2 * up(m * up(f, 8) * 2, 256);
+}
+
+int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx, const void* wg, size_t ldwg, const void* wu,
+                          size_t ldwu, const void* g, const void* u, size_t ldgu, int dtype, size_t m, size_t f, size_t k,
+                          int act, void* dx, size_t lddx, void* dwg, size_t lddwg, void* dwu, size_t lddwu, void* workspace,
+                          size_t workspace_bytes, equarx_stream_t stream) {
+    if (!is_16bit(dtype) || !is_act(act)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(lddh, f) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k) ||
+        bad_ld(ldgu, f) || bad_ld(lddx, k) || bad_ld(lddwg, k) || bad_ld(lddwu, k))
+        return EQUARX_ERR_COUNT;
+    if (!dwg || !dwu || (m && (!dh || !x || !wg || !wu || !g || !u || !dx || !workspace))) return EQUARX_ERR_NULL;
+    const size_t need = equarx_gated_backward_workspace_bytes(m, f, k, ldx, ldwg, ldwu);
+    if (m && workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
+    for (const void* p : {dh, x, wg, wu, g, u, static_cast<const void*>(dx), static_cast<const void*>(dwg),
+                          static_cast<const void*>(dwu), static_cast<const void*>(workspace)})
+        if (!aligned(p, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({matrix(dh, m, f, lddh, 2), matrix(x, m, k, ldx, 2), matrix(wg, f, k, ldwg, 2),
+                       matrix(wu, f, k, ldwu, 2), matrix(g, m, f, ldgu, 2), matrix(u, m, f, ldgu, 2)},
+                      {matrix(dx, m, k, lddx, 2), matrix(dwg, f, k, lddwg, 2), matrix(dwu, f, k, lddwu, 2),
+                       Span{workspace, m ? need : 0}}));
+    if (m == 0) {       // sums over no tokens
+        cudaError_t e = launch_error_to_inject();
+        if (e == cudaSuccess) e = cudaMemset2DAsync(dwg, lddwg * 2, 0, k * 2, f, stream);
+        if (e == cudaSuccess) e = cudaMemset2DAsync(dwu, lddwu * 2, 0, k * 2, f, stream);
+        return e == cudaSuccess ? EQUARX_OK : cuda_failure(e);
+    }
+
+    int sms;
+    TRY(current_device(sms));
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    Operand ox{x, ldx}, og{wg, ldwg}, ou{wu, ldwu};
+    TRY(readable(ox, m, k, ws, stream));
+    TRY(readable(og, f, k, ws, stream));
+    TRY(readable(ou, f, k, ws, stream));
+    const size_t ldd = up(f, 8);
+    Operand dg{ws, ldd}, du{ws + up(m * ldd * 2, 256), ldd};
+
+    GradArgs e = {};
+    e.dh = dh;
+    e.g = g;
+    e.u = u;
+    e.dg = const_cast<void*>(dg.p);
+    e.du = const_cast<void*>(du.p);
+    e.ld_dh = lddh;
+    e.ld_gu = ldgu;
+    e.ld_out = ldd;
+    e.rows = int(m);
+    e.cols = int(f);
+    e.act = act;
+    e.dtype = dtype;
+    e.vec = lddh % 8 == 0 && ldgu % 8 == 0;
+    TRY(launch(gate_grad_kernel, dim3(unsigned(std::min<size_t>(ceil_div(m * (ldd / 8), 256), size_t(sms) * 8))), 256, 0, 1, e,
+               stream));
+
+    // dx = dG Wg + dU Wu: the reduction runs over f, twice
+    if (m <= kFewTokens) {
+        SplitArgs a = {};
+        a.nt = token_tile(m);
+        TRY(map16(a.w[0], og, f, k, 64));
+        TRY(map16(a.w[1], ou, f, k, 64));
+        TRY(map16(a.x[0], dg, m, f, a.nt));
+        TRY(map16(a.x[1], du, m, f, a.nt));
+        a.out[0] = out_rows(dx, lddx, dtype);
+        a.stages = int(ceil_div(f, 64));
+        a.bf16 = dtype == EQUARX_BF16;
+        TRY((launch_split<kHalf, kSum2, true>(a, k, m, stream)));
+    } else {
+        TileArgs a = {};
+        a.bn = 256;
+        TRY(map16(a.a[0], dg, m, f, kRowsM));
+        TRY(map16(a.a[1], du, m, f, kRowsM));
+        TRY(map16(a.b[0], og, f, k, 64));
+        TRY(map16(a.b[1], ou, f, k, 64));
+        a.out[0] = out_rows(dx, lddx, dtype);
+        a.stages = int(ceil_div(f, 64));
+        a.bf16 = dtype == EQUARX_BF16;
+        TRY((launch_tiles<kHalf, kSum2, false, true>(a, m, k, stream)));
+    }
+    // dWg = dG^T x, dWu = dU^T x: the reduction runs over the tokens
+    TileArgs a = {};
+    a.bn = 256;
+    TRY(map16(a.a[0], dg, m, f, 64));
+    TRY(map16(a.a[1], du, m, f, 64));
+    TRY(map16(a.b[0], ox, m, k, 64));
+    a.out[0] = out_rows(dwg, lddwg, dtype);
+    a.out[1] = out_rows(dwu, lddwu, dtype);
+    a.stages = int(ceil_div(m, 64));
+    a.bf16 = dtype == EQUARX_BF16;
+    return launch_tiles<kHalf, kOut2, true, true>(a, f, k, stream);
+}
+
+int equarx_feedforward_check(void) {
+    uint32_t seen = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&seen, tc::g_gave_up, sizeof(seen));
+    const uint32_t zero = 0;
+    if (e == cudaSuccess && seen) e = cudaMemcpyToSymbol(tc::g_gave_up, &zero, sizeof(zero));
+    if (e != cudaSuccess) return cuda_failure(e);
+    return seen ? EQUARX_ERR_TIMEOUT : EQUARX_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,895 @@
+// Kernels of the tensor-parallel feed-forward block whose partial sums the AllReduce reduces:
+// products and gated products of 16-bit and of microscaled 4-bit operands, their gradients, and the
+// 4-bit quantiser.
+//
+//   tile_kernel       persistent 128 x bn output tiles on the tensor cores
+//   split_kernel      few tokens: weights on the 128-row side, the reduction split over a cluster
+//   gate_grad_kernel  gradients of the two projections from dh, g and u
+//   pack_kernel       rows that TMA cannot read (a stride that is no multiple of 16 bytes) -> rows it can
+//   fp4_quantize_kernel, fp4_dequantize_kernel
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "tensor_ops.cuh"
+
+namespace equarx {
+namespace ff {
+
+using namespace tc;
+
+enum Kind { kHalf = 0, kMx = 1, kNv = 2 };                 // 16-bit operands, 4-bit with either scale format
+enum Mode { kPlain = 0, kGated = 1, kSum2 = 2, kOut2 = 3 };
+enum DType { kBf16 = 0, kFp16 = 1, kFp32 = 2 };
+enum Act { kSilu = 0, kGeluTanh = 1 };
+
+constexpr int kRowsM = 128;               // rows of a tile: lanes of tensor memory
+constexpr int kRowBytes = 128;            // one stage of the reduction axis: 64 16-bit or 256 4-bit elements
+constexpr int kTileBytes = kRowsM * kRowBytes;
+constexpr int kChunkBytes = 64 * kRowBytes;   // MN-major operands: 64 elements x 64 steps of the reduction
+
+template <int KIND> constexpr int kStageElems = KIND == kHalf ? 64 : 256;
+// scales of 128 rows for one stage: 512-byte tiles of 128 rows x 4 scales
+template <int KIND> constexpr int kScaleTiles = KIND == kNv ? 4 : KIND == kMx ? 2 : 0;
+template <int KIND> constexpr int kScaleBytes = 512 * kScaleTiles<KIND>;
+
+// ---------------------------------------------------------------- element types
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, int dtype) {
+    uint32_t r;
+    if (dtype == kBf16)
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(uint32_t w, int dtype) {
+    if (dtype == kBf16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    __half2 h;
+    memcpy(&h, &w, 4);
+    return __half22float2(h);
+}
+__device__ __forceinline__ float load1(const void* p, size_t i, int dtype) {
+    if (dtype == kBf16) return __uint_as_float(uint32_t(static_cast<const uint16_t*>(p)[i]) << 16);
+    if (dtype == kFp16) return __half2float(static_cast<const __half*>(p)[i]);
+    return static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store1(void* p, size_t i, float v, int dtype) {
+    if (dtype == kFp32)
+        static_cast<float*>(p)[i] = v;
+    else
+        static_cast<uint16_t*>(p)[i] = uint16_t(pack2(v, v, dtype));
+}
+
+// ---------------------------------------------------------------- activation
+// silu(g) = g sigma(g);  gelu_tanh(g) = g sigma(z), z = 2 sqrt(2/pi) (g + 0.044715 g^3), which is
+// 0.5 g (1 + tanh(z/2)) without the cancellation of 1 + tanh.  sigma in fp32: e^-z overflows to inf
+// for z below -88, where 1 / (1 + inf) is the right 0.
+constexpr float kGeluC = 1.5957691216057308f, kGeluC3 = kGeluC * 0.044715f;
+
+__device__ __forceinline__ float sigma(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+
+__device__ __forceinline__ float act(float g, int kind) {
+    const float z = kind == kSilu ? g : g * (kGeluC + kGeluC3 * g * g);
+    return g * sigma(z);
+}
+// value and slope: (g s)' = s + g s (1 - s) z'
+__device__ __forceinline__ void act_grad(float g, int kind, float& value, float& slope) {
+    const float z = kind == kSilu ? g : g * (kGeluC + kGeluC3 * g * g);
+    const float dz = kind == kSilu ? 1.0f : kGeluC + 3.0f * kGeluC3 * g * g;
+    const float s = sigma(z);
+    value = g * s;
+    // s (1 - s) is 0 where s is 0 or 1, also where g dz overflows
+    const float t = s * (1.0f - s);
+    slope = s + (t == 0.0f ? 0.0f : g * dz * t);
+}
+
+// ---------------------------------------------------------------- output rows
+struct Out {
+    void* p;
+    size_t ld;
+    int dtype;
+    int vec;      // 1: base and row stride are multiples of 16 bytes
+};
+
+// 32 x 32 transpose inside a warp: lane t holds row t before and column t after
+__device__ __forceinline__ void transpose32(float (&v)[32]) {
+    const uint32_t lane = threadIdx.x & 31;
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) {
+        const bool up = lane & s;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            if (i & s) continue;
+            const float give = up ? v[i] : v[i + s];
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, give, s);
+            if (up) v[i] = got; else v[i + s] = got;
+        }
+    }
+}
+
+// A warp's 32 rows x 32 columns, lane t holding row t.  Aligned rows: each lane writes its own 64 (128)
+// bytes, whole sectors.  Otherwise the tile is transposed so that a row's columns are written by
+// neighbouring lanes together; writing them lane by lane would touch each sector sixteen times.
+__device__ __forceinline__ void store_tile(const Out& o, int row0, int col0, int rows, int cols, float (&v)[32]) {
+    const int lane = threadIdx.x & 31;
+    if (o.vec && col0 + 32 <= cols) {
+        if (row0 + lane >= rows) return;
+        if (o.dtype == kFp32) {
+            float4* q = reinterpret_cast<float4*>(static_cast<float*>(o.p) + size_t(row0 + lane) * o.ld + col0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {
+            uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(o.p) + size_t(row0 + lane) * o.ld + col0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                q[i] = make_uint4(pack2(v[8 * i], v[8 * i + 1], o.dtype), pack2(v[8 * i + 2], v[8 * i + 3], o.dtype),
+                                  pack2(v[8 * i + 4], v[8 * i + 5], o.dtype), pack2(v[8 * i + 6], v[8 * i + 7], o.dtype));
+        }
+        return;
+    }
+    if (col0 >= cols) return;
+    transpose32(v);
+    if (col0 + lane < cols) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (row0 + i < rows) store1(o.p, size_t(row0 + i) * o.ld + col0 + lane, v[i], o.dtype);
+    }
+}
+
+// ---------------------------------------------------------------- persistent tiles
+struct TileArgs {
+    CUtensorMap a[2], b[2];
+    const uint8_t* scales_a;
+    const uint8_t* scales_b[2];
+    const float* row_a;               // NV: one factor for each row of a and of b
+    const float* row_b[2];
+    Out out[3];                       // gated: h, g, u; two outputs: one each
+    int m, n;                         // rows and columns of an output
+    int stages;                       // stages of the reduction axis (of each of the two parts of kSum2)
+    int tiles_m, tiles_n, bn, group;
+    int act, bf16, save;
+};
+
+template <int KIND> constexpr int kPipe = 4;
+template <int KIND> constexpr int kStageBytes = kTileBytes + 2 * kTileBytes + 3 * kScaleBytes<KIND>;
+constexpr int kEpilogueWarps = 8;
+constexpr int kTileThreads = 32 * (kEpilogueWarps + 2);
+constexpr int kSmemSlack = 1024;      // 128-byte swizzle atoms start on multiples of 1024 bytes
+template <int KIND> constexpr int kTileSmem = kPipe<KIND> * kStageBytes<KIND> + kSmemSlack;
+
+// tile t in an order that walks `group` row tiles before the next column tile: the tiles that run at
+// one time share operands in L2
+__device__ __forceinline__ void tile_at(const TileArgs& p, int t, int& mt, int& nt) {
+    const int per = p.group * p.tiles_n, g = t / per, first = g * p.group;
+    const int gm = min(p.group, p.tiles_m - first), r = t - g * per;
+    mt = first + r % gm;
+    nt = r / gm;
+}
+
+// Output tiles of 128 x bn.  One thread starts TMA loads through a ring of stages, one thread issues
+// the products, eight warps move finished accumulators from tensor memory to the output; two
+// accumulators let the next tile's products run meanwhile.  4-bit operands: the scales need tensor
+// memory too, so the second accumulator begins 64 columns inside the first, and each is drained from
+// that end first.
+//
+// kGated: columns [0, bn/2) of the tile are x Wg^T and [bn/2, bn) the same columns of x Wu^T, so a
+// thread finds g and u of one element in its own row and writes act(g) u.
+// kSum2: out = a0 b0 + a1 b1.  kOut2: out0 = a0 b0, out1 = a1 b0, tiles of both in one launch.
+template <int KIND, int MODE, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ TileArgs p) {
+    constexpr bool FP4 = KIND != kHalf;
+    constexpr int PIPE = kPipe<KIND>, STAGE = kStageBytes<KIND>, SB = kScaleBytes<KIND>;
+    constexpr uint32_t kSecond = FP4 ? 192 : 256;       // first column of the second accumulator
+    constexpr uint32_t kScaleCol = 448;                 // scales of a, then of b
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * PIPE + 5];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile uint32_t abort;
+
+    const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * PIPE, ready = empty + 8 * PIPE, drained = ready + 16,
+                   drain = drained + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < PIPE; ++i) {
+            barrier_init(full + 8 * i, 1);
+            barrier_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(ready + 8 * i, 1);
+            barrier_init(drained + 8 * i, kEpilogueWarps);
+        }
+        barrier_init(drain, 1);
+        abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == kEpilogueWarps) tmem_alloc(smem_addr(&tmem_slot), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    const int tiles = p.tiles_m * p.tiles_n * (MODE == kOut2 ? 2 : 1);
+    const int stages = p.stages * (MODE == kSum2 ? 2 : 1);
+    const int half = MODE == kGated ? p.bn / 2 : p.bn;
+    grid_launch();
+    grid_wait();
+
+    if (warp == kEpilogueWarps + 1) {
+        if (lane == 0) {
+            // ------------------------------------------------ loads
+            uint32_t it = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+                const int which = MODE == kOut2 ? t >= p.tiles_m * p.tiles_n : 0;
+                int mt, nt;
+                tile_at(p, t - which * p.tiles_m * p.tiles_n, mt, nt);
+                const int m0 = mt * kRowsM, n0 = nt * half;
+                const int sn0 = n0 / 128, sn = FP4 ? min(half / 128, (p.n + 127) / 128 - sn0) : 0;
+                for (int s = 0; s < stages; ++s, ++it) {
+                    const uint32_t slot = it % PIPE;
+                    if (!(ok = barrier_wait(empty + 8 * slot, (it / PIPE & 1) ^ 1, &abort))) break;
+                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, bar = full + 8 * slot;
+                    const int part = MODE == kSum2 ? s >= p.stages : 0;
+                    const int ks = s - part * p.stages;
+                    const CUtensorMap* ma = &p.a[MODE == kOut2 ? which : part];
+                    uint32_t bytes = kTileBytes;
+                    if (B_MN) bytes += (p.bn + 63) / 64 * kChunkBytes; else bytes += p.bn * kRowBytes;
+                    if (FP4) bytes += SB * (1 + (MODE == kGated ? 2 : 1) * sn);
+                    barrier_expect(bar, bytes);
+                    const int kc = FP4 ? ks * kRowBytes : ks * 64;     // 4-bit codes travel as bytes
+                    if (A_MN) {
+                        tma_load_2d(sa, ma, m0, kc, bar);
+                        tma_load_2d(sa + kChunkBytes, ma, m0 + 64, kc, bar);
+                    } else {
+                        tma_load_2d(sa, ma, kc, m0, bar);
+                    }
+                    if (B_MN) {
+                        for (int c = 0; c < p.bn; c += 64)
+                            tma_load_2d(sb + c / 64 * kChunkBytes, &p.b[part], n0 + c, kc, bar);
+                    } else {
+                        tma_load_2d(sb, &p.b[part], kc, n0, bar);
+                        if (MODE == kGated) tma_load_2d(sb + half * kRowBytes, &p.b[1], kc, n0, bar);
+                    }
+                    if (FP4) {
+                        const uint32_t ss = sb + 2 * kTileBytes;
+                        bulk_load(ss, p.scales_a + (size_t(mt) * p.stages + ks) * SB, SB, bar);
+                        for (int q = 0; q < (MODE == kGated ? 2 : 1); ++q)
+                            for (int i = 0; i < sn; ++i)
+                                bulk_load(ss + SB * (1 + q + i), p.scales_b[q] + (size_t(sn0 + i) * p.stages + ks) * SB, SB,
+                                          bar);
+                    }
+                }
+            }
+            if (abort)          // what has been started lands before the shared memory goes away
+                for (uint32_t i = it > PIPE ? it - PIPE : 0; i < it; ++i) barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
+        }
+        __syncwarp();
+    } else if (warp == kEpilogueWarps) {
+        if (lane == 0) {
+            // ------------------------------------------------ products
+            const uint32_t ta = tmem + kScaleCol, tb = ta + 4 * kScaleTiles<KIND>;
+            uint32_t it = 0, local = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++local) {
+                const uint32_t buf = local & 1, d = tmem + buf * kSecond;
+                if (FP4) {
+                    // the tile before has given up the columns that both accumulators use
+                    if (local && !(ok = barrier_wait(drained, (local - 1) & 1, &abort))) break;
+                } else {
+                    if (local > 1 && !(ok = barrier_wait(drained + 8 * buf, (local / 2 - 1) & 1, &abort))) break;
+                }
+                fence_after();
+                for (int s = 0; s < stages; ++s, ++it) {
+                    const uint32_t slot = it % PIPE;
+                    if (!(ok = barrier_wait(full + 8 * slot, it / PIPE & 1, &abort))) break;
+                    fence_after();
+                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, ss = sb + 2 * kTileBytes;
+                    if (FP4) {
+#pragma unroll
+                        for (int j = 0; j < kScaleTiles<KIND>; ++j) {
+                            copy_scales(ta + 4 * j, ss + 512 * j);
+                            copy_scales(tb + 8 * j, ss + SB + 512 * j);
+                            if (p.bn > 128) copy_scales(tb + 8 * j + 4, ss + 2 * SB + 512 * j);
+                        }
+                    }
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) {
+                        const uint64_t da = A_MN ? swizzled_desc(sa + 2048 * kk, kChunkBytes, 1024)
+                                                 : swizzled_desc(sa + 32 * kk, 16, 1024);
+                        const uint64_t db = B_MN ? swizzled_desc(sb + 2048 * kk, kChunkBytes, 1024)
+                                                 : swizzled_desc(sb + 32 * kk, 16, 1024);
+                        if constexpr (FP4) {
+                            const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
+                            mma_fp4<KIND == kMx>(d, da, db, desc_fp4(KIND == kMx, p.bn, which), ta + 4 * j, tb + 8 * j,
+                                                 s | kk);
+                        } else {
+                            mma_16bit(d, da, db, desc_16bit(p.bf16, A_MN, B_MN, p.bn), s | kk);
+                        }
+                    }
+                    mma_commit(empty + 8 * slot);
+                }
+                if (ok) mma_commit(ready + 8 * buf);
+            }
+            if (abort) {        // products in flight read this shared memory
+                mma_commit(drain);
+                barrier_drain(drain, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------- outputs
+        const int quarter = warp & 3, side = warp >> 2;
+        const int units = half / 32;                       // blocks of 32 output columns
+        uint32_t local = 0;
+        for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++local) {
+            const int which = MODE == kOut2 ? t >= p.tiles_m * p.tiles_n : 0;
+            int mt, nt;
+            tile_at(p, t - which * p.tiles_m * p.tiles_n, mt, nt);
+            const int row0 = mt * kRowsM + quarter * 32, n0 = nt * half;
+            const uint32_t buf = local & 1, acc = tmem + buf * kSecond + (uint32_t(quarter * 32) << 16);
+            float ra = 1.0f;
+            if (KIND == kNv && row0 + lane < p.m) ra = p.row_a[row0 + lane];
+            if (!barrier_wait(ready + 8 * buf, local / 2 & 1, &abort)) break;
+            __syncwarp();
+            fence_after();
+            const int steps = (units + 1) / 2;
+            for (int i = 0; i < steps; ++i) {
+                __syncwarp();
+                // the shared columns are the last of the first accumulator and the first of the second
+                const int u = buf ? 2 * i + side : units - 1 - (2 * i + side);
+                const bool live = u >= 0 && u < units;
+                uint32_t r[32], q[32];
+                if (live) {
+                    tmem_load32(acc + 32 * u, r);
+                    if (MODE == kGated) tmem_load32(acc + half + 32 * u, q);
+                    tmem_wait_loads();
+                }
+                if (i == (FP4 ? 0 : steps - 1)) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive(FP4 ? drained : drained + 8 * buf);
+                }
+                if (!live) continue;
+                const int col0 = n0 + 32 * u;
+                float v[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+                if (KIND == kNv) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] *= ra;
+                    if (col0 + 32 <= p.n) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float4 b = reinterpret_cast<const float4*>(p.row_b[0] + col0)[j];
+                            v[4 * j] *= b.x; v[4 * j + 1] *= b.y; v[4 * j + 2] *= b.z; v[4 * j + 3] *= b.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col0 + j < p.n) v[j] *= p.row_b[0][col0 + j];
+                    }
+                }
+                if constexpr (MODE == kGated) {
+                    float w[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) w[j] = __uint_as_float(q[j]);
+                    if (KIND == kNv) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col0 + j < p.n) w[j] = w[j] * ra * p.row_b[1][col0 + j];
+                    }
+                    float h[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) h[j] = act(v[j], p.act) * w[j];
+                    store_tile(p.out[0], row0, col0, p.m, p.n, h);
+                    if (KIND == kHalf && p.save) {
+                        store_tile(p.out[1], row0, col0, p.m, p.n, v);
+                        store_tile(p.out[2], row0, col0, p.m, p.n, w);
+                    }
+                } else {
+                    store_tile(p.out[which], row0, col0, p.m, p.n, v);
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kEpilogueWarps) {
+        fence_after();
+        tmem_free(tmem, 512);
+    }
+}
+
+// ---------------------------------------------------------------- few tokens
+struct SplitArgs {
+    CUtensorMap w[2], x[2];
+    const uint8_t* scales_w[2];
+    const uint8_t* scales_x;
+    const float* row_w[2];
+    const float* row_x;
+    Out out[3];
+    int features, tokens;             // rows of w, rows of x
+    int stages;                       // stages of the reduction axis (of each part of kSum2)
+    int nt;                           // tokens of a tile: a multiple of 16, at most 128
+    int pipe;                         // stages in shared memory
+    int act, bf16, save;
+};
+constexpr int kSplitThreads = 192, kSplitMaxPipe = 12;
+template <int KIND, int MODE>
+__host__ __device__ constexpr int split_stage_bytes(int nt) {
+    return (MODE == kGated ? 2 : 1) * (kTileBytes + kScaleBytes<KIND>) + nt * kRowBytes + kScaleBytes<KIND>;
+}
+
+// The output transposed: 128 features x nt tokens, so that a single token costs one narrow product over
+// each weight tile instead of a 128-row one, and the weights, which are all the bytes there are, are
+// read once.  The reduction axis is split over the CTAs of a cluster (cluster dimension x) because
+// features / 128 tiles alone would leave most SMs without work; the parts are added through distributed
+// shared memory, in rank order, so the sum does not depend on timing.
+template <int KIND, int MODE, bool W_MN>
+__global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_constant__ SplitArgs p) {
+    constexpr bool FP4 = KIND != kHalf;
+    constexpr int SB = kScaleBytes<KIND>, NW = MODE == kGated ? 2 : 1;
+    constexpr uint32_t kScaleCol = 256;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * kSplitMaxPipe + 2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile uint32_t abort;
+
+    const uint32_t pad = (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u;
+    const uint32_t smem = smem_addr(smem_raw) + pad;
+    float* const part = reinterpret_cast<float*>(smem_raw + pad);          // [NW * nt][128], after the products
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kSplitMaxPipe, ready = empty + 8 * kSplitMaxPipe,
+                   drain = ready + 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t xb = p.nt * kRowBytes, STAGE = NW * (kTileBytes + SB) + xb + SB;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < p.pipe; ++i) {
+            barrier_init(full + 8 * i, 1);
+            barrier_init(empty + 8 * i, 1);
+        }
+        barrier_init(ready, 1);
+        barrier_init(drain, 1);
+        abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == 5) tmem_alloc(smem_addr(&tmem_slot), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    const int ranks = gridDim.x, rank = cluster_rank();
+    const int total = p.stages * (MODE == kSum2 ? 2 : 1);
+    const int s0 = int(int64_t(total) * rank / ranks), s1 = int(int64_t(total) * (rank + 1) / ranks);
+    const int f0 = blockIdx.y * kRowsM, t0 = blockIdx.z * p.nt;
+    grid_launch();
+    grid_wait();
+
+    if (warp == 4) {
+        if (lane == 0) {
+            bool ok = true;
+            int it = 0;
+            for (int s = s0; s < s1; ++s, ++it) {
+                const int slot = it % p.pipe;
+                if (!(ok = barrier_wait(empty + 8 * slot, (it / p.pipe & 1) ^ 1, &abort))) break;
+                const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb, bar = full + 8 * slot;
+                const int second = MODE == kSum2 ? s >= p.stages : 0, ks = s - second * p.stages;
+                const int kc = FP4 ? ks * kRowBytes : ks * 64;
+                barrier_expect(bar, NW * kTileBytes + xb + (FP4 ? (NW + 1) * SB : 0));
+                for (int q = 0; q < NW; ++q) {
+                    const CUtensorMap* mw = &p.w[MODE == kSum2 ? second : q];
+                    if (W_MN) {
+                        tma_load_2d(sw, mw, f0, kc, bar);
+                        tma_load_2d(sw + kChunkBytes, mw, f0 + 64, kc, bar);
+                    } else {
+                        tma_load_2d(sw + q * kTileBytes, mw, kc, f0, bar);
+                    }
+                    if (FP4) bulk_load(ss + SB * q, p.scales_w[q] + (size_t(f0 / 128) * p.stages + ks) * SB, SB, bar);
+                }
+                tma_load_2d(sx, &p.x[second], kc, t0, bar);
+                if (FP4) bulk_load(ss + SB * NW, p.scales_x + (size_t(t0 / 128) * p.stages + ks) * SB, SB, bar);
+            }
+            if (abort)
+                for (int i = it > p.pipe ? it - p.pipe : 0; i < it; ++i) barrier_drain(full + 8 * (i % p.pipe), i / p.pipe & 1);
+        }
+        __syncwarp();
+    } else if (warp == 5) {
+        if (lane == 0) {
+            const uint32_t tw = tmem + kScaleCol, tx = tw + NW * 4 * kScaleTiles<KIND>;
+            bool ok = true;
+            int it = 0;
+            for (int s = s0; s < s1; ++s, ++it) {
+                const int slot = it % p.pipe;
+                if (!(ok = barrier_wait(full + 8 * slot, it / p.pipe & 1, &abort))) break;
+                fence_after();
+                const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb;
+                if (FP4) {
+#pragma unroll
+                    for (int j = 0; j < kScaleTiles<KIND>; ++j) {
+#pragma unroll
+                        for (int q = 0; q < NW; ++q)
+                            copy_scales(tw + (q * kScaleTiles<KIND> + j) * 4, ss + SB * q + 512 * j);
+                        copy_scales(tx + 4 * j, ss + SB * NW + 512 * j);
+                    }
+                }
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) {
+                    const uint64_t dx = swizzled_desc(sx + 32 * kk, 16, 1024);
+#pragma unroll
+                    for (int q = 0; q < NW; ++q) {
+                        const uint32_t a = sw + q * kTileBytes;
+                        const uint64_t dw = W_MN ? swizzled_desc(a + 2048 * kk, kChunkBytes, 1024)
+                                                 : swizzled_desc(a + 32 * kk, 16, 1024);
+                        if constexpr (FP4) {
+                            const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
+                            mma_fp4<KIND == kMx>(tmem + q * p.nt, dw, dx, desc_fp4(KIND == kMx, p.nt, which),
+                                                 tw + (q * kScaleTiles<KIND> + j) * 4, tx + 4 * j, it | kk);
+                        } else {
+                            mma_16bit(tmem + q * p.nt, dw, dx, desc_16bit(p.bf16, W_MN, false, p.nt), it | kk);
+                        }
+                    }
+                }
+                mma_commit(empty + 8 * slot);
+            }
+            if (ok) mma_commit(ready);
+            if (abort) {
+                mma_commit(drain);
+                barrier_drain(drain, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        if (barrier_wait(ready, 0, &abort)) {
+            __syncwarp();
+            fence_after();
+            // every load has landed and every product has read it: the stages now hold the partial sums
+            for (int c = 0; c < NW * p.nt; c += 16) {
+                uint32_t r[16];
+                tmem_load16(tmem + c + (uint32_t(warp * 32) << 16), r);
+                tmem_wait_loads();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) part[(c + j) * 128 + warp * 32 + lane] = __uint_as_float(r[j]);
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 5) {
+        fence_after();
+        tmem_free(tmem, 512);
+    }
+    cluster_sync();
+
+    const int count = min(p.nt, p.tokens - t0) * 128;
+    const uint32_t base = smem_addr(part);
+    for (int e = rank * kSplitThreads + int(threadIdx.x); e < count; e += ranks * kSplitThreads) {
+        const int t = e >> 7, f = f0 + (e & 127);
+        if (f >= p.features) continue;
+        float v = 0.0f, w = 0.0f;
+        for (int r = 0; r < ranks; ++r) {
+            v += ld_cluster_f32(base + 4 * e, r);
+            if (MODE == kGated) w += ld_cluster_f32(base + 4 * (p.nt * 128 + e), r);
+        }
+        if (KIND == kNv) {
+            const float rx = p.row_x[t0 + t];
+            v = v * rx * p.row_w[0][f];
+            if (MODE == kGated) w = w * rx * p.row_w[1][f];
+        }
+        if (MODE == kGated) {
+            const size_t row = size_t(t0 + t);
+            store1(p.out[0].p, row * p.out[0].ld + f, act(v, p.act) * w, p.out[0].dtype);
+            if (KIND == kHalf && p.save) {
+                store1(p.out[1].p, row * p.out[1].ld + f, v, p.out[1].dtype);
+                store1(p.out[2].p, row * p.out[2].ld + f, w, p.out[2].dtype);
+            }
+        } else {
+            store1(p.out[0].p, size_t(t0 + t) * p.out[0].ld + f, v, p.out[0].dtype);
+        }
+    }
+    cluster_sync();       // nobody leaves while a neighbour may still read its partial sums
+}
+
+// ---------------------------------------------------------------- 16-bit rows, element by element
+// dU = dh act(g), dG = dh u act'(g) in fp32, rounded to the 16-bit type that the gradients' products
+// read (the tensor cores take 16-bit operands; the sums over them stay in fp32).
+struct GradArgs {
+    const void *dh, *g, *u;
+    void *dg, *du;
+    size_t ld_dh, ld_gu, ld_out;      // ld_out is a multiple of 8; columns [cols, ld_out) are not read
+    int rows, cols, act, dtype, vec;
+};
+__global__ void __launch_bounds__(256) gate_grad_kernel(const __grid_constant__ GradArgs p) {
+    grid_launch();
+    grid_wait();
+    const int per_row = (p.cols + 7) / 8;
+    const size_t total = size_t(p.rows) * per_row;
+    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += size_t(gridDim.x) * 256) {
+        const size_t row = i / per_row;
+        const int col = int(i % per_row) * 8, n = min(8, p.cols - col);
+        float dh[8], g[8], u[8], dg[8], du[8];
+        if (p.vec && n == 8) {
+            const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.dh) + row * p.ld_dh + col);
+            const uint4 b = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.g) + row * p.ld_gu + col);
+            const uint4 c = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.u) + row * p.ld_gu + col);
+            const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w}, wc[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 fa = unpack2(wa[j], p.dtype), fb = unpack2(wb[j], p.dtype), fc = unpack2(wc[j], p.dtype);
+                dh[2 * j] = fa.x; dh[2 * j + 1] = fa.y;
+                g[2 * j] = fb.x; g[2 * j + 1] = fb.y;
+                u[2 * j] = fc.x; u[2 * j + 1] = fc.y;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = j < n;
+                dh[j] = in ? load1(p.dh, row * p.ld_dh + col + j, p.dtype) : 0.0f;
+                g[j] = in ? load1(p.g, row * p.ld_gu + col + j, p.dtype) : 0.0f;
+                u[j] = in ? load1(p.u, row * p.ld_gu + col + j, p.dtype) : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float a, slope;
+            act_grad(g[j], p.act, a, slope);
+            du[j] = dh[j] * a;
+            dg[j] = dh[j] * u[j] * slope;
+        }
+        uint4 og, ou;
+        og = make_uint4(pack2(dg[0], dg[1], p.dtype), pack2(dg[2], dg[3], p.dtype), pack2(dg[4], dg[5], p.dtype),
+                        pack2(dg[6], dg[7], p.dtype));
+        ou = make_uint4(pack2(du[0], du[1], p.dtype), pack2(du[2], du[3], p.dtype), pack2(du[4], du[5], p.dtype),
+                        pack2(du[6], du[7], p.dtype));
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dg) + row * p.ld_out + col) = og;
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.du) + row * p.ld_out + col) = ou;
+    }
+}
+
+// rows x cols 16-bit words to rows whose stride is a multiple of 16 bytes
+struct PackArgs {
+    const uint16_t* src;
+    uint16_t* dst;
+    size_t ld_src, ld_dst;
+    int rows, cols;
+};
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs p) {
+    grid_launch();
+    grid_wait();
+    const int per_row = int(p.ld_dst) / 8;
+    const size_t total = size_t(p.rows) * per_row;
+    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += size_t(gridDim.x) * 256) {
+        const size_t row = i / per_row;
+        const int col = int(i % per_row) * 8;
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = col + j < p.cols ? p.src[row * p.ld_src + col + j] : 0;
+        *reinterpret_cast<uint4*>(p.dst + row * p.ld_dst + col) =
+            make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    }
+}
+
+// ---------------------------------------------------------------- microscaled 4-bit floating point
+// Scales are stored as the tensor cores take them: tiles of 128 rows x 4 scales, the scale of row r and
+// block b at byte (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of tile (r / 128, b / 4); the tiles of a
+// 128-row group are consecutive and cover a whole number of 256-element stages.
+template <bool MX>
+__host__ __device__ constexpr int blocks_per_stage() { return MX ? 8 : 16; }
+template <bool MX>
+__host__ __device__ inline size_t scale_offset(size_t row, size_t block, size_t stages) {
+    return (row / 128 * stages * (blocks_per_stage<MX>() / 4) + block / 4) * 512 + (row % 32) * 16 + (row % 128 / 32) * 4 +
+           block % 4;
+}
+
+struct QuantArgs {
+    const void* x;
+    uint8_t *codes, *scales;
+    float* row_scales;
+    size_t ld;
+    int rows, cols, dtype, vec;       // vec: base and row stride are multiples of 16 bytes
+};
+
+// eight codes, the first in the lowest nibble
+__device__ __forceinline__ uint32_t encode8(const float* v) {
+    uint32_t r;
+    asm("{\n .reg .b8 a, b, c, d;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+        " mov.b32 %0, {a, b, c, d};\n}"
+        : "=r"(r)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+__device__ __forceinline__ void decode8(uint32_t w, float* v) {
+    uint32_t h[4];
+    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n"
+        " cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+        " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2(h[i], kFp16);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ uint32_t to_e4m3(float v) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
+    return r & 0xFF;
+}
+__device__ __forceinline__ float from_e4m3(uint32_t b) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(uint16_t(b)));
+    return unpack2(h, kFp16).x;
+}
+// 2^(byte - 127); 255 is NaN
+__device__ __forceinline__ float from_e8m0(uint32_t b) {
+    if (b == 255) return __uint_as_float(0x7FFFFFFFu);
+    return b ? __uint_as_float(b << 23) : __uint_as_float(0x00400000u);
+}
+
+__device__ __forceinline__ void load16(const QuantArgs& p, size_t row, int col, float (&v)[16]) {
+    if (p.vec && col + 16 <= p.cols) {
+        if (p.dtype == kFp32) {
+            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + row * p.ld + col);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 f = q[i];
+                v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
+            }
+        } else {
+            const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.x) + row * p.ld + col);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint4 w = q[i];
+                float2 f;
+                f = unpack2(w.x, p.dtype); v[8 * i] = f.x; v[8 * i + 1] = f.y;
+                f = unpack2(w.y, p.dtype); v[8 * i + 2] = f.x; v[8 * i + 3] = f.y;
+                f = unpack2(w.z, p.dtype); v[8 * i + 4] = f.x; v[8 * i + 5] = f.y;
+                f = unpack2(w.w, p.dtype); v[8 * i + 6] = f.x; v[8 * i + 7] = f.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = col + i < p.cols ? load1(p.x, row * p.ld + col + i, p.dtype) : 0.0f;
+    }
+}
+
+// magnitudes compared as integers, so that NaN and infinity come out on top
+__device__ __forceinline__ uint32_t amax16(const float (&v)[16]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
+}
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// One lane takes 16 neighbouring elements; WARPS warps share a row.
+//   MX: 32 elements share e = max(floor(log2 amax) - 2, -127): the power of two that brings the largest
+//       element into [4, 8); code = rn(v / 2^e), above 6 it saturates.  Every step but the rounding is exact.
+//   NV: 16 elements share s = e4m3_rn(min(amax * (448 / A), 448)), A the row's amax; d = s * (A / 2688);
+//       code = rn(v * (1 / d)), all zero where s is.  A < 2^-100: the row is zero.
+// A value that is not finite makes its block's scale (MX) or its row's factor (NV) NaN.
+template <bool MX, int WARPS>
+__global__ void __launch_bounds__(256) fp4_quantize_kernel(const __grid_constant__ QuantArgs p) {
+    constexpr int ROWS = 8 / WARPS, LANES = 32 * WARPS;
+    const int lane = int(threadIdx.x) % LANES;
+    const size_t row = size_t(blockIdx.x) * ROWS + threadIdx.x / LANES;
+    const size_t stages = (size_t(p.cols) + 255) / 256;
+    const int padded = int(stages * 256);
+    const int stride = (p.cols + 31) / 32 * 16;            // bytes of a row of codes
+    grid_launch();
+    grid_wait();
+    const bool live = row < size_t(p.rows);
+
+    float up = 0.0f, g = 0.0f;
+    if (!MX) {
+        uint32_t m = 0;
+        if (live)
+            for (int col = lane * 16; col < p.cols; col += LANES * 16) {
+                float v[16];
+                load16(p, row, col, v);
+                m = max(m, amax16(v));
+            }
+        m = __reduce_max_sync(0xFFFFFFFFu, m);
+        if (WARPS > 1) {
+            __shared__ uint32_t top[8];
+            if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = m;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) m = max(m, top[threadIdx.x / LANES * WARPS + i]);
+        }
+        const float amax = __uint_as_float(m);
+        if (m >= kInfBits) {
+            g = __uint_as_float(0x7FFFFFFFu);
+        } else if (amax >= 0x1p-100f) {
+            g = __fdiv_rn(amax, 2688.0f);
+            up = __fdiv_rn(448.0f, amax);
+        }
+        if (live && lane == 0) p.row_scales[row] = g;
+    }
+    if (!live) return;                                     // whole warps leave
+
+    for (int col0 = 0; col0 < padded; col0 += LANES * 16) {
+        const int col = col0 + lane * 16;
+        float v[16];
+        load16(p, row, col, v);                            // zeros beyond the row
+        uint32_t m = amax16(v), byte;
+        float inv;
+        if (MX) {
+            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+            const int field = int(m >> 23);                // exponent + 127
+            const int e = max(field - 2, 0);               // the stored byte
+            byte = m >= kInfBits ? 255u : uint32_t(e);
+            inv = m >= kInfBits ? 0.0f : __uint_as_float(uint32_t(254 - e) << 23);
+        } else {
+            const float s = from_e4m3(byte = to_e4m3(fminf(__fmul_rn(__uint_as_float(m), up), 448.0f)));
+            inv = s > 0.0f && up > 0.0f ? __fdiv_rn(1.0f, __fmul_rn(s, g)) : 0.0f;
+            if (up == 0.0f) byte = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = inv == 0.0f ? 0.0f : __fmul_rn(v[i], inv);
+        const uint2 code = make_uint2(encode8(v), encode8(v + 8));
+        if (col / 2 + 8 <= stride) *reinterpret_cast<uint2*>(p.codes + row * size_t(stride) + col / 2) = code;
+        // four scales of a row are one 32-bit word
+        constexpr int PER = MX ? 2 : 1;                    // lanes of a block
+        uint32_t word = byte << (8 * (lane / PER % 4));
+        word |= __shfl_xor_sync(0xFFFFFFFFu, word, PER);
+        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2 * PER);
+        if (lane % (4 * PER) == 0 && col < padded)
+            *reinterpret_cast<uint32_t*>(p.scales + scale_offset<MX>(row, size_t(col) / (MX ? 32 : 16), stages)) = word;
+    }
+}
+
+struct DequantArgs {
+    const uint8_t *codes, *scales;
+    const float* row_scales;
+    void* out;
+    size_t ld;
+    int rows, cols, dtype, vec;
+};
+// value = code * scale (MX), code * (scale * row factor) (NV), rounded once to the output type
+template <bool MX>
+__global__ void __launch_bounds__(256) fp4_dequantize_kernel(const __grid_constant__ DequantArgs p) {
+    const size_t stages = (size_t(p.cols) + 255) / 256;
+    const int stride = (p.cols + 31) / 32 * 16, per_row = (p.cols + 15) / 16;
+    const size_t total = size_t(p.rows) * per_row;
+    grid_launch();
+    grid_wait();
+    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += size_t(gridDim.x) * 256) {
+        const size_t row = i / per_row;
+        const int col = int(i % per_row) * 16;
+        const uint2 w = *reinterpret_cast<const uint2*>(p.codes + row * size_t(stride) + col / 2);
+        const uint32_t b = p.scales[scale_offset<MX>(row, size_t(col) / (MX ? 32 : 16), stages)];
+        const float d = MX ? from_e8m0(b) : __fmul_rn(from_e4m3(b), p.row_scales[row]);
+        float v[16];
+        decode8(w.x, v);
+        decode8(w.y, v + 8);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = __fmul_rn(v[j], d);
+        if (p.vec && col + 16 <= p.cols) {
+            if (p.dtype == kFp32) {
+                float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * p.ld + col);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            } else {
+                uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + row * p.ld + col);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    q[j] = make_uint4(pack2(v[8 * j], v[8 * j + 1], p.dtype), pack2(v[8 * j + 2], v[8 * j + 3], p.dtype),
+                                      pack2(v[8 * j + 4], v[8 * j + 5], p.dtype), pack2(v[8 * j + 6], v[8 * j + 7], p.dtype));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (col + j < p.cols) store1(p.out, row * p.ld + col + j, v[j], p.dtype);
+        }
+    }
+}
+
+}  // namespace ff
+}  // namespace equarx

@@ -1,0 +1,497 @@
+"""The feed-forward operators: refusals (no GPU), and the kernels against 64-bit references."""
+import pytest
+import torch
+
+import ff_reference as ref
+import paper_2506_17615_b200 as eq
+from paper_2506_17615_b200 import binding
+from paper_2506_17615_b200 import feedforward as ff
+
+A = 0x7000_0000_0000          # a made-up, well aligned "device address"
+GB = 1 << 30
+gpu = pytest.mark.gpu
+FORMATS = [eq.FP4_MX, eq.FP4_NV]
+ACTS = [eq.ACT_SILU, eq.ACT_GELU_TANH]
+
+
+def status_of(fn, *args, **kw):
+    try:
+        fn(*args, **kw)
+    except eq.EquarxError as e:
+        return e.status
+    return 0
+
+
+# ------------------------------------------------------------------ refusals, sizes (no GPU)
+
+def quantize_args():
+    return dict(x=A, dtype=eq.BF16, rows=4, cols=64, ld=64, format=eq.FP4_NV, codes=A + GB, scales=A + 2 * GB,
+                row_scales=A + 3 * GB)
+
+
+def test_quantize_refuses_bad_arguments():
+    f, a = eq.fp4_quantize, quantize_args()
+    for key in ("x", "codes", "scales", "row_scales"):
+        assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
+        assert status_of(f, **{**a, key: a[key] + 2}) == binding.ERR_ALIGN
+    for key, bad in (("dtype", 3), ("dtype", -1), ("format", 2), ("format", -1)):
+        assert status_of(f, **{**a, key: bad}) == binding.ERR_FORMAT
+    for key, bad in (("cols", 0), ("ld", 63), ("rows", GB + 1), ("cols", GB + 1), ("ld", GB + 1)):
+        assert status_of(f, **{**a, key: bad}) == binding.ERR_COUNT
+    assert status_of(f, **{**a, "codes": A + 496}) == binding.ERR_ALIAS          # inside x's last row
+    assert status_of(f, **{**a, "scales": A + GB + 112}) == binding.ERR_ALIAS    # inside codes
+    assert status_of(f, **{**a, "rows": 0, "x": 0, "codes": 0}) == 0             # nothing to do
+
+
+def test_dequantize_refuses_bad_arguments():
+    f = eq.fp4_dequantize
+    a = dict(codes=A, scales=A + GB, row_scales=A + 2 * GB, rows=4, cols=64, format=eq.FP4_NV, out=A + 3 * GB,
+             dtype=eq.FP32, ld=64)
+    for key in ("codes", "scales", "row_scales", "out"):
+        assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
+        assert status_of(f, **{**a, key: a[key] + 4}) == binding.ERR_ALIGN
+    assert status_of(f, **{**a, "dtype": 9}) == binding.ERR_FORMAT
+    assert status_of(f, **{**a, "ld": 60}) == binding.ERR_COUNT
+    assert status_of(f, **{**a, "out": A + 112}) == binding.ERR_ALIAS
+
+
+def test_matmul_refuses_bad_arguments():
+    f = eq.fp4_matmul
+    a = dict(a_codes=A, a_scales=A + GB, a_row_scales=A + 2 * GB, b_codes=A + 3 * GB, b_scales=A + 4 * GB,
+             b_row_scales=A + 5 * GB, m=4, n=8, k=64, format=eq.FP4_NV, out=A + 6 * GB, dtype=eq.FP16, ld=8)
+    for key in ("a_codes", "a_scales", "a_row_scales", "b_codes", "b_scales", "b_row_scales", "out"):
+        assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
+        assert status_of(f, **{**a, key: a[key] + 8}) == binding.ERR_ALIGN
+    for key, bad in (("n", 0), ("k", 0), ("ld", 7), ("m", GB + 1)):
+        assert status_of(f, **{**a, key: bad}) == binding.ERR_COUNT
+    for key, bad in (("dtype", 3), ("format", 5)):
+        assert status_of(f, **{**a, key: bad}) == binding.ERR_FORMAT
+    assert status_of(f, **{**a, "out": A + 3 * GB + 16}) == binding.ERR_ALIAS
+    assert status_of(f, **{**a, "m": 0, "out": 0}) == 0
+
+
+def test_linear_and_gated_refuse_bad_arguments():
+    need = eq.fp4_linear_workspace_bytes(4, 64, eq.FP4_NV)
+    w = dict(w_codes=A + GB, w_scales=A + 2 * GB, w_row_scales=A + 3 * GB)
+    a = dict(x=A, dtype=eq.BF16, ldx=64, **w, m=4, n=8, k=64, format=eq.FP4_NV, out=A + 4 * GB, ld=8, workspace=A + 5 * GB,
+             workspace_bytes=need)
+    gu = dict(g_codes=A + GB, g_scales=A + 2 * GB, g_row_scales=A + 3 * GB, u_codes=A + 6 * GB, u_scales=A + 7 * GB,
+              u_row_scales=A + 8 * GB)
+    b = dict(x=A, dtype=eq.BF16, ldx=64, **gu, m=4, f=8, k=64, format=eq.FP4_NV, act=0, h=A + 4 * GB, ldh=8,
+             workspace=A + 5 * GB, workspace_bytes=need)
+    for f, args, out in ((eq.fp4_linear, a, "out"), (eq.fp4_gated, b, "h")):
+        pointers = [k for k in args if isinstance(args[k], int) and args[k] >= A]
+        assert len(pointers) == (6 if f is eq.fp4_linear else 9)
+        for key in pointers:
+            assert status_of(f, **{**args, key: 0}) == binding.ERR_NULL
+            assert status_of(f, **{**args, key: args[key] + 8}) == binding.ERR_ALIGN
+        assert status_of(f, **{**args, "workspace_bytes": need - 1}) == binding.ERR_WORKSPACE
+        assert status_of(f, **{**args, "dtype": eq.FP32}) == binding.ERR_FORMAT     # activations are 16-bit
+        assert status_of(f, **{**args, "ldx": 32}) == binding.ERR_COUNT
+        assert status_of(f, **{**args, out: A + 5 * GB}) == binding.ERR_ALIAS       # the workspace
+        assert status_of(f, **{**args, "m": 0}) == 0
+    assert status_of(eq.fp4_gated, **{**b, "act": 2}) == binding.ERR_FORMAT
+
+
+def test_gated_forward_and_backward_refuse_bad_arguments():
+    fwd = dict(x=A, ldx=64, wg=A + GB, ldwg=64, wu=A + 2 * GB, ldwu=64, dtype=eq.FP16, m=4, f=8, k=64, act=1, h=A + 3 * GB,
+               ldh=8, g=A + 4 * GB, u=A + 5 * GB, ldgu=8, workspace=0, workspace_bytes=0)
+    f = eq.gated_forward
+    for key in ("x", "wg", "wu", "h", "g", "u"):
+        assert status_of(f, **{**fwd, key: 0}) == binding.ERR_NULL
+        assert status_of(f, **{**fwd, key: fwd[key] + 2}) == binding.ERR_ALIGN
+    for key, bad in (("f", 0), ("k", 0), ("ldx", 63), ("ldwg", 63), ("ldwu", 63), ("ldh", 7), ("ldgu", 7)):
+        assert status_of(f, **{**fwd, key: bad}) == binding.ERR_COUNT
+    for key, bad in (("dtype", eq.FP32), ("act", 2)):
+        assert status_of(f, **{**fwd, key: bad}) == binding.ERR_FORMAT
+    assert status_of(f, **{**fwd, "h": A + GB}) == binding.ERR_ALIAS
+    assert status_of(f, **{**fwd, "ldx": 65}) == binding.ERR_NULL                 # now a workspace is needed
+    assert status_of(f, **{**fwd, "ldx": 65, "workspace": A + 9 * GB}) == binding.ERR_WORKSPACE
+
+    need = eq.gated_backward_workspace_bytes(4, 8, 64, 64, 64, 64)
+    bwd = dict(dh=A, lddh=8, x=A + GB, ldx=64, wg=A + 2 * GB, ldwg=64, wu=A + 3 * GB, ldwu=64, g=A + 4 * GB, u=A + 5 * GB,
+               ldgu=8, dtype=eq.BF16, m=4, f=8, k=64, act=0, dx=A + 6 * GB, lddx=64, dwg=A + 7 * GB, lddwg=64,
+               dwu=A + 8 * GB, lddwu=64, workspace=A + 9 * GB, workspace_bytes=need)
+    f = eq.gated_backward
+    for key in ("dh", "x", "wg", "wu", "g", "u", "dx", "dwg", "dwu", "workspace"):
+        assert status_of(f, **{**bwd, key: 0}) == binding.ERR_NULL
+        assert status_of(f, **{**bwd, key: bwd[key] + 4}) == binding.ERR_ALIGN
+    for key in ("lddh", "ldgu"):
+        assert status_of(f, **{**bwd, key: 7}) == binding.ERR_COUNT
+    for key in ("ldx", "ldwg", "ldwu", "lddx", "lddwg", "lddwu"):
+        assert status_of(f, **{**bwd, key: 63}) == binding.ERR_COUNT
+    assert status_of(f, **{**bwd, "workspace_bytes": need - 1}) == binding.ERR_WORKSPACE
+    assert status_of(f, **{**bwd, "dx": A + GB}) == binding.ERR_ALIAS             # in place is not allowed
+    assert status_of(f, **{**bwd, "dwu": A + 7 * GB}) == binding.ERR_ALIAS
+    assert eq.last_cuda_error() == 0
+
+
+def test_sizes_of_the_buffers():
+    assert eq.fp4_codes_bytes(3, 33) == 3 * 32                    # two groups of 32 codes
+    assert eq.fp4_scales_bytes(1, 1, eq.FP4_MX) == 1024           # one stage of 256 columns, 128 rows, 8 scales each
+    assert eq.fp4_scales_bytes(129, 257, eq.FP4_NV) == 2 * 2 * 2048
+    assert eq.fp4_scales_bytes(0, 64, eq.FP4_NV) == 0 and eq.fp4_codes_bytes(4, 0) == 0
+    assert eq.fp4_scales_bytes(4, 64, 7) == 0
+    assert eq.gated_forward_workspace_bytes(8, 16, 64, 64, 72, 80) == 0
+    assert eq.gated_forward_workspace_bytes(8, 16, 64, 65, 64, 64) == 8 * 64 * 2   # x is copied
+    assert eq.gated_forward_workspace_bytes(8, 16, 64, 63, 64, 64) == 0            # invalid
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    x = torch.zeros(4, 8, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        ff.fp4_quantize(x)                                        # not on a GPU
+    with pytest.raises(ValueError):
+        ff.gated_forward(x, x, x)
+
+
+# ------------------------------------------------------------------ inputs
+
+def normal(rows, cols, seed, dtype, scale=1.0, pad=0):
+    gen = torch.Generator().manual_seed(seed)
+    t = (torch.randn(rows, cols + pad, generator=gen) * scale).to(dtype).cuda()
+    return t[:, :cols]
+
+
+def hard_rows(cols, dtype):
+    """rows where a quantiser can go wrong: zeros, ties, range ends, one element alone, subnormals"""
+    gen = torch.Generator().manual_seed(5)
+    top = torch.finfo(dtype).max
+    rows = [torch.zeros(cols), torch.full((cols,), top), torch.full((cols,), torch.finfo(dtype).tiny / 4)]
+    ties = torch.tensor([0, .25, .5, .75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6, 7])
+    for scale in (1.0, 2.0 ** -9, 3.0, 2.0 ** 7):
+        t = (ties * scale).repeat(-(-cols // 16))[:cols]
+        rows += [t, -t, t.flip(0)]
+    alone = torch.zeros(cols)
+    alone[cols // 2] = -1e-3
+    rows.append(alone)
+    rows.append(torch.randn(cols, generator=gen) * torch.exp2(torch.randint(-12, 9, (cols,), generator=gen).float()))
+    wild = torch.randn(cols, generator=gen) * torch.exp2(torch.arange(cols) / cols * 20 - 10)
+    rows.append(wild)
+    if dtype != torch.float16:
+        rows += [torch.randn(cols, generator=gen) * 2.0 ** -104, torch.randn(cols, generator=gen) * 2.0 ** -99,
+                 torch.randn(cols, generator=gen) * 2.0 ** 120, torch.full((cols,), 2.0 ** -127), torch.full((cols,), 2.0 ** -100)]
+    return torch.stack(rows).clamp(-top, top).to(dtype).cuda()
+
+
+# ------------------------------------------------------------------ 4-bit quantisation
+
+def check_quantized(x, fmt):
+    q = ff.fp4_quantize(x, fmt)
+    rows, cols = x.shape
+    code, neg, byte, d, g = ref.quantize(x.double(), fmt)
+    stride = -(-cols // 32) * 16
+    assert q.codes.shape == (rows, stride)
+    nib = torch.stack([q.codes & 15, q.codes >> 4], -1).reshape(rows, -1).long()
+    flat = code.reshape(rows, -1)
+    want = torch.zeros(rows, stride * 2, dtype=torch.long, device=x.device)
+    n = min(flat.shape[1], want.shape[1])
+    want[:, :n] = flat[:, :n]
+    assert torch.equal(nib & 7, want), "magnitudes differ"
+    signs = torch.zeros_like(want, dtype=torch.bool)
+    signs[:, :n] = neg.reshape(rows, -1)[:, :n]
+    wrong = ((nib >> 3).bool() != signs) & (want > 0)            # the sign of a zero code is free
+    assert not bool(wrong.any()), "signs differ"
+    pos = ref.scale_positions(rows, byte.shape[1], cols, fmt).to(x.device)
+    assert torch.equal(q.scales[pos].long(), byte.long()), "scales differ"
+    if fmt == eq.FP4_NV:
+        assert torch.equal(q.row_scales.double(), g)
+    # scale bytes past the last column, up to the stage's end, are zero
+    per = 8 if fmt == eq.FP4_MX else 16
+    total = -(-cols // 256) * per
+    if total > byte.shape[1]:
+        tail = ref.scale_positions(rows, total, cols, fmt)[:, byte.shape[1]:].to(x.device)
+        assert not bool(q.scales[tail].any())
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        back = ff.fp4_dequantize(q, dtype)
+        assert torch.equal(back.double(), ref.f32(ref.values(x.double(), fmt)).to(dtype).double()), dtype
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 16, 0), (3, 17, 0), (5, 31, 2), (128, 256, 0), (129, 257, 7),
+                                           (33, 500, 12), (1, 5376, 0), (1300, 96, 0), (1200, 1001, 0), (300, 2050, 6)])
+def test_quantize_matches_the_definition(fmt, dtype, rows, cols, pad):
+    check_quantized(normal(rows, cols, rows + cols, dtype, 3.0, pad), fmt)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("cols", [16, 64, 333, 512])
+def test_quantize_hard_rows(fmt, dtype, cols):
+    check_quantized(hard_rows(cols, dtype), fmt)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_not_finite_elements_become_nan(fmt):
+    x = normal(6, 96, 1, torch.bfloat16)
+    x[1, 40], x[3, 0], x[4, 95] = float("inf"), float("nan"), float("-inf")
+    back = ff.fp4_dequantize(ff.fp4_quantize(x, fmt), torch.float32)
+    block = 32 if fmt == eq.FP4_MX else 96
+    nan = torch.zeros(6, 96, dtype=torch.bool, device="cuda")
+    for r, c in ((1, 40), (3, 0), (4, 95)):
+        nan[r, c // block * block:(c // block + 1) * block] = True
+    assert torch.equal(back.isnan(), nan)
+    w = ff.fp4_quantize(normal(40, 96, 2, torch.bfloat16), fmt)
+    for y in (ff.fp4_linear(x, w), ff.fp4_linear(x.repeat(40, 1), w)[:6]):
+        rows = y.isnan()
+        assert bool(rows[[1, 3, 4]].all()) and not bool(rows[[0, 2, 5]].any())
+
+
+# ------------------------------------------------------------------ products over 4-bit operands
+
+SIZES = [(1, 1, 1), (1, 16, 32), (1, 130, 300), (3, 100, 64), (16, 128, 256), (17, 129, 257), (64, 257, 1000),
+         (127, 300, 513), (128, 64, 96), (129, 128, 256), (130, 300, 500), (257, 129, 777), (300, 513, 1030),
+         (520, 1000, 2000), (1025, 260, 64)]
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_fp4_products(fmt, m, n, k):
+    for i, dtype in enumerate((torch.bfloat16, torch.float16)):
+        x = normal(m, k, m + n + i, dtype, 1.0, pad=(0, 3, 8)[(m + i) % 3])
+        w = normal(n, k, n + k + i, dtype, k ** -0.5)
+        wq = ff.fp4_quantize(w, fmt)
+        y = ff.fp4_linear(x, wq)
+        value, bound = ref.product(ref.values(x.double(), fmt), ref.values(w.double(), fmt))
+        assert y.dtype == dtype
+        ref.assert_within(y, value, ref.rounded(value, bound, dtype), "linear")
+        xq = ff.fp4_quantize(x, fmt)
+        assert torch.equal(ff.fp4_matmul(xq, wq, dtype), y)                       # the same product
+        y32 = ff.fp4_matmul(xq, wq, torch.float32)
+        ref.assert_within(y32, value, ref.rounded(value, bound, torch.float32), "matmul, fp32")
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("m,f,k", SIZES)
+def test_fp4_gated(fmt, act, m, f, k):
+    dtype = torch.bfloat16 if (m + f) % 2 else torch.float16
+    x = normal(m, k, m + f, dtype, 1.0, pad=(0, 1, 8)[m % 3])
+    wg, wu = normal(f, k, f + 1, dtype, 2 * k ** -0.5), normal(f, k, f + 2, dtype, k ** -0.5)
+    h = ff.fp4_gated(x, ff.fp4_quantize(wg, fmt), ff.fp4_quantize(wu, fmt), act)
+    value, bound, _, _ = ref.gated(*(ref.values(t.double(), fmt) for t in (x, wg, wu)), act)
+    ref.assert_within(h, value, ref.rounded(value, bound, dtype), "h")
+    ff.check()
+
+
+# ------------------------------------------------------------------ 16-bit block and its gradients
+
+def backward_reference(dh, x, wg, wu, g, u, act, unit):
+    """gradients from the saved g and u, and bounds: dG and dU carry one 16-bit rounding each"""
+    a, s = ref.act(g, act), ref.slope(g, act)
+    du, dg = dh * a, dh * u * s
+    # fp32 evaluation: the slope is a sum of terms up to 1 + |g| in size
+    edu = (unit + 2.0 ** -18) * du.abs() + ref.TINY[torch.float16]
+    edg = unit * dg.abs() + (2.0 ** -18) * (dh * u).abs() * (1 + g.abs()) + ref.TINY[torch.float16]
+    f, m = wg.shape[0], x.shape[0]
+    dx = dg @ wg + du @ wu
+    acc = 2 * f * ref.ACC
+    ex = (edg + acc * dg.abs()) @ wg.abs() + (edu + acc * du.abs()) @ wu.abs()
+    dwg, dwu = dg.T @ x, du.T @ x
+    ewg = (edg + m * ref.ACC * dg.abs()).T @ x.abs()
+    ewu = (edu + m * ref.ACC * du.abs()).T @ x.abs()
+    return (dx, ex), (dwg, ewg), (dwu, ewu)
+
+
+TRAIN = [(1, 1, 1), (1, 64, 64), (2, 130, 72), (16, 128, 256), (33, 65, 129), (128, 200, 300), (129, 256, 128),
+         (200, 77, 1001), (257, 300, 513), (512, 520, 264), (1030, 128, 200)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("m,f,k", TRAIN)
+def test_gated_forward_and_backward(dtype, act, m, f, k):
+    pad = (0, 8, 3)[(m + f) % 3]
+    x = normal(m, k, m + f, dtype, 1.0, pad)
+    wg, wu = normal(f, k, f + 1, dtype, 2 * k ** -0.5, pad), normal(f, k, f + 2, dtype, k ** -0.5, (0, 5)[k % 2])
+    dh = normal(m, f, m + 3, dtype, 1.0, pad)
+    h, g, u = ff.gated_forward(x, wg, wu, act, save=True)
+    xd, wgd, wud, dhd = (t.double() for t in (x, wg, wu, dh))
+    value, bound, (gv, eg), (uv, eu) = ref.gated(xd, wgd, wud, act)
+    ref.assert_within(h, value, ref.rounded(value, bound, dtype), "h")
+    ref.assert_within(g, gv, ref.rounded(gv, eg, dtype), "g")
+    ref.assert_within(u, uv, ref.rounded(uv, eu, dtype), "u")
+    assert torch.equal(ff.gated_forward(x, wg, wu, act), h)
+    grads = ff.gated_backward(dh, x, wg, wu, g, u, act)
+    want = backward_reference(dhd, xd, wgd, wud, g.double(), u.double(), act, ref.UNIT[dtype])
+    for name, got, (v, e) in zip(("dx", "dwg", "dwu"), grads, want):
+        assert got.dtype == dtype
+        ref.assert_within(got, v, ref.rounded(v, e, dtype), name)
+    again = ff.gated_backward(dh, x, wg, wu, g, u, act)
+    assert all(torch.equal(p, q) for p, q in zip(grads, again)), "not deterministic"
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("m,f,k", [(5, 40, 24), (150, 96, 136)])
+def test_gradients_against_differences(act, m, f, k):
+    """<gradient, v> against a central difference of the 64-bit block along v.  The difference's own error
+    is O(step^2) of the third derivative (below 1e-6 here); the gradient's is its bound summed along |v|,
+    with g and u off by their 16-bit rounding as well."""
+    dtype = torch.float16
+    x, wg, wu = normal(m, k, 1, dtype), normal(f, k, 2, dtype, k ** -0.5), normal(f, k, 3, dtype, k ** -0.5)
+    dh = normal(m, f, 4, dtype)
+    _, g, u = ff.gated_forward(x, wg, wu, act, save=True)
+    grads = ff.gated_backward(dh, x, wg, wu, g, u, act)
+    args = [t.double() for t in (x, wg, wu)]
+    unit = ref.UNIT[dtype]
+
+    def loss(x, wg, wu):
+        return (dh.double() * ref.act(x @ wg.T, act) * (x @ wu.T)).sum()
+
+    # slopes change by at most 1.2 times the change of g (the second derivatives stay below 1.2)
+    bounds = backward_reference(dh.double(), *args, g.double(), u.double(), act, unit)
+    eg, eu = unit * g.double().abs(), unit * u.double().abs()
+    s = ref.slope(g.double(), act).abs()
+    ddg = dh.double().abs() * (eu * (s + 1.2 * eg) + u.double().abs() * 1.2 * eg)
+    ddu = dh.double().abs() * 1.2 * eg
+    moved = (ddg @ args[1].abs() + ddu @ args[2].abs(), ddg.T @ args[0].abs(), ddu.T @ args[0].abs())
+    for i, (got, (v, e), extra) in enumerate(zip(grads, bounds, moved)):
+        gen = torch.Generator().manual_seed(10 + i)
+        direction = torch.randn(got.shape, generator=gen, dtype=torch.float64).cuda()
+        step = 1e-4
+        plus, minus = list(args), list(args)
+        plus[i], minus[i] = args[i] + step * direction, args[i] - step * direction
+        numeric = (loss(*plus) - loss(*minus)) / (2 * step)
+        tol = ((ref.rounded(v, e, dtype) + extra) * direction.abs()).sum() + 1e-5 * numeric.abs() + 1e-6
+        assert abs(float((got.double() * direction).sum() - numeric)) <= float(tol), i
+
+
+# ------------------------------------------------------------------ no tokens, streams, not finite, guards
+
+@gpu
+def test_no_tokens():
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    w = normal(40, 64, 1, torch.bfloat16)
+    for fmt in FORMATS:
+        wq = ff.fp4_quantize(w, fmt)
+        assert ff.fp4_linear(x, wq).shape == (0, 40) and ff.fp4_gated(x, wq, wq).shape == (0, 40)
+        assert ff.fp4_dequantize(ff.fp4_quantize(x, fmt)).shape == (0, 64)
+    h, g, u = ff.gated_forward(x, w, w, save=True)
+    assert h.shape == (0, 40)
+    dx, dwg, dwu = ff.gated_backward(h, x, w, w, g, u)
+    assert dx.shape == (0, 64) and not bool(dwg.any()) and not bool(dwu.any())    # sums over nothing
+
+
+@gpu
+def test_on_a_stream_of_its_own():
+    """inputs made on one stream, used on another that waits for it; the outputs are the same bits"""
+    x, wg, wu = normal(300, 200, 1, torch.bfloat16), normal(256, 200, 2, torch.bfloat16, 0.1), normal(256, 200, 3, torch.bfloat16, 0.1)
+    want = ff.gated_forward(x, wg, wu)
+    q = ff.fp4_quantize(wg)
+    want4 = ff.fp4_linear(x, q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y = [ff.gated_forward(x * 1, wg, wu) for _ in range(3)]
+        y4 = [ff.fp4_linear(x * 1, q) for _ in range(3)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(t, want) for t in y) and all(torch.equal(t, want4) for t in y4)
+
+
+@gpu
+@pytest.mark.parametrize("m", [7, 200])
+def test_not_finite_values_stay_in_their_rows(m):
+    x, wg, wu = normal(m, 100, 1, torch.float16), normal(70, 100, 2, torch.float16, 0.1), normal(70, 100, 3, torch.float16, 0.1)
+    clean = ff.gated_forward(x, wg, wu)
+    dirty = x.clone()
+    dirty[3, 99], dirty[5, 0] = float("nan"), float("inf")
+    h, g, u = ff.gated_forward(dirty, wg, wu, save=True)
+    keep = [r for r in range(m) if r not in (3, 5)]
+    assert torch.equal(h[keep], clean[keep])
+    assert bool(h[3].isnan().all()) and not bool(g[5].isfinite().any())
+    dx, _, _ = ff.gated_backward(normal(m, 70, 4, torch.float16), dirty, wg, wu, g, u)
+    assert bool(dx[keep].isfinite().all()) and bool(dx[3].isnan().all())
+
+
+@gpu
+@pytest.mark.parametrize("m,f,k", [(3, 130, 70), (129, 130, 260), (140, 33, 8)])
+def test_strided_outputs_and_no_writes_outside(m, f, k):
+    """through the C ABI, into rows inside wider buffers; everything else keeps its canary"""
+    dtype, stream = torch.bfloat16, torch.cuda.current_stream().cuda_stream
+    x, wg, wu, dh = normal(m, k, 1, dtype), normal(f, k, 2, dtype), normal(f, k, 3, dtype), normal(m, f, 4, dtype)
+    h0, g0, u0 = ff.gated_forward(x, wg, wu, save=True)
+    grads0 = ff.gated_backward(dh, x, wg, wu, g0, u0)
+    for extra in (8, 3):
+        def wide(rows, cols):
+            return torch.full((rows + 2, cols + extra), -77.0, dtype=dtype, device="cuda")
+
+        def inner(t):        # the row after the first, so that writes in front show too
+            return t.data_ptr() + (0 if t.stride(0) % 8 else 2 * t.stride(0))
+
+        def split(t, rows, cols):
+            first = 0 if t.stride(0) % 8 else 1
+            body = t[first:first + rows, :cols]
+            rest = t.clone()
+            rest[first:first + rows, :cols] = -77.0
+            assert bool((rest == -77.0).all()), "written outside the output"
+            return body
+
+        ph, pg, pu = wide(m, f), wide(m, f), wide(m, f)
+        nb = eq.gated_forward_workspace_bytes(m, f, k, k, k, k)
+        ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
+        eq.gated_forward(x, k, wg, k, wu, k, eq.BF16, m, f, k, eq.ACT_GELU_TANH, inner(ph), f + extra, inner(pg), inner(pu),
+                         f + extra, ws, nb, stream)
+        for t, want in ((ph, h0), (pg, g0), (pu, u0)):
+            assert torch.equal(split(t, m, f), want)
+        px, pwg, pwu = wide(m, k), wide(f, k), wide(f, k)
+        nb = eq.gated_backward_workspace_bytes(m, f, k, k, k, k)
+        ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+        eq.gated_backward(dh, f, x, k, wg, k, wu, k, inner(pg), inner(pu), f + extra, eq.BF16, m, f, k, eq.ACT_GELU_TANH,
+                          inner(px), k + extra, inner(pwg), k + extra, inner(pwu), k + extra, ws, nb, stream)
+        for t, want, rows in ((px, grads0[0], m), (pwg, grads0[1], f), (pwu, grads0[2], f)):
+            assert torch.equal(split(t, rows, k), want)
+    ff.check()
+
+
+@gpu
+def test_recorded_in_a_cuda_graph():
+    x, w = normal(4, 256, 1, torch.bfloat16), ff.fp4_quantize(normal(200, 256, 2, torch.bfloat16))
+    wg, wu = normal(64, 256, 3, torch.bfloat16), normal(64, 256, 4, torch.bfloat16)
+    want = ff.fp4_linear(x, w), ff.gated_forward(x, wg, wu)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ff.fp4_linear(x, w), ff.gated_forward(x, wg, wu)
+    for _ in range(2):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
+def test_launch_errors_come_back(monkeypatch):
+    x, w = normal(4, 64, 1, torch.bfloat16), normal(8, 64, 2, torch.bfloat16)
+    monkeypatch.setenv("EQUARX_INJECT_LAUNCH_ERROR", "719")
+    for call in (lambda: ff.fp4_quantize(x), lambda: ff.gated_forward(x, w, w)):
+        with pytest.raises(eq.EquarxError) as err:
+            call()
+        assert err.value.status == binding.ERR_CUDA and eq.last_cuda_error() == 719
+    monkeypatch.delenv("EQUARX_INJECT_LAUNCH_ERROR")
+    ff.gated_forward(x, w, w)
+    ff.check()
+
+
+@gpu
+def test_shapes_that_do_not_fit():
+    x, w = normal(4, 64, 1, torch.bfloat16), normal(8, 64, 2, torch.bfloat16)
+    for bad in ((x, w, w[:, :63]), (x, w, w[:7]), (x.T, w, w), (x, w, w.to(torch.float16)), (x[0], w, w)):
+        with pytest.raises(ValueError):
+            ff.gated_forward(*bad)
+    mx, nv = ff.fp4_quantize(w, eq.FP4_MX), ff.fp4_quantize(w, eq.FP4_NV)
+    with pytest.raises(ValueError):
+        ff.fp4_matmul(mx, nv)
+    with pytest.raises(ValueError):
+        ff.fp4_gated(x, mx, nv)
+    with pytest.raises(eq.EquarxError):
+        ff.fp4_linear(x.float(), nv)                               # activations are 16-bit
