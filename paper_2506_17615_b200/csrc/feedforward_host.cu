@@ -50,6 +50,9 @@ inline bool is_format(int f) { return f == EQUARX_FP4_MX || f == EQUARX_FP4_NV; 
 inline bool is_act(int a) { return a == EQUARX_ACT_SILU || a == EQUARX_ACT_GELU_TANH; }
 inline size_t size_of(int dtype) { return dtype == EQUARX_FP32 ? 4 : 2; }
 
+inline size_t codes_stride(size_t cols) { return ceil_div(cols, 32) * 16; }
+inline size_t fp4_stages(size_t cols) { return ceil_div(cols, 256); }
+
 // ---------------------------------------------------------------- device facts, constant for the process
 int current_device(int& sms) {
     static std::mutex mu;
@@ -136,18 +139,26 @@ Encode encoder() {
     return fn;
 }
 
-// rows x inner elements of 1 or 2 bytes, row stride in bytes; boxes of box_rows x 128 bytes, swizzled;
-// elements outside the matrix read as zero
-int make_map(CUtensorMap& map, const void* base, size_t elem, size_t inner, size_t rows, size_t stride, size_t box_rows) {
+// rows x inner elements of 1 or 2 bytes, row stride in bytes; boxes of box_rows x 128 bytes (64 with the
+// 64-byte swizzle); elements outside the matrix read as zero
+int make_map(CUtensorMap& map, const void* base, size_t elem, size_t inner, size_t rows, size_t stride, size_t box_rows,
+             CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     const cuuint64_t dims[2] = {inner, rows}, strides[1] = {stride};
-    const cuuint32_t box[2] = {cuuint32_t(kRowBytes / elem), cuuint32_t(box_rows)}, steps[2] = {1, 1};
+    const cuuint32_t box[2] = {cuuint32_t((swizzle == CU_TENSOR_MAP_SWIZZLE_64B ? 64 : kRowBytes) / elem), cuuint32_t(box_rows)},
+                     steps[2] = {1, 1};
     const Encode fn = encoder();
     if (!fn) return cuda_failure(cudaErrorNotSupported);
     const CUresult r = fn(&map, elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2,
                           const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                          swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? EQUARX_OK : cuda_failure(cudaErrorInvalidValue);
+}
+
+// scales of a 4-bit matrix as rows of 128 bytes, those of one 128-row group and one stage together
+int scale_map(CUtensorMap& map, const uint8_t* scales, size_t rows, size_t cols, int format) {
+    const size_t box_rows = (format == EQUARX_FP4_MX ? kScaleBytes<kMx> : kScaleBytes<kNv>) / 128;
+    return make_map(map, scales, 1, 128, ceil_div(rows, 128) * fp4_stages(cols) * box_rows, 128, box_rows,
+                    CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 #define TRY(call)                              \
@@ -164,8 +175,6 @@ struct Fp4 {
     const uint8_t *codes, *scales;
     const float* row_scales;
 };
-inline size_t codes_stride(size_t cols) { return ceil_div(cols, 32) * 16; }
-inline size_t fp4_stages(size_t cols) { return ceil_div(cols, 256); }
 inline size_t scales_bytes(size_t rows, size_t cols, int format) {
     return ceil_div(rows, 128) * fp4_stages(cols) * (format == EQUARX_FP4_MX ? kScaleBytes<kMx> : kScaleBytes<kNv>);
 }
@@ -209,18 +218,36 @@ int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int 
 // Tokens up to which the transposed kernel is used.
 constexpr size_t kFewTokens = 128;
 
+// Columns of a tile.  The pairs of SMs work through whole rounds of tiles, so the time goes with rounds *
+// (bn + a share for starting and ending a tile); a narrower tile may save a round, or give every pair
+// work when there is little.  4-bit operands: their scales come in groups of 128 columns.
+int tile_width(size_t rows, size_t cols, int outputs, bool gated, bool fp4, int sms) {
+    int best = 256;
+    size_t best_cost = ~size_t(0);
+    const int step = fp4 ? 128 : gated ? 64 : 32;
+    for (int bn = 256; bn >= (gated && fp4 ? 256 : step); bn -= step) {
+        const size_t tiles = ceil_div(rows, kTileM) * ceil_div(cols, gated ? bn / 2 : bn) * outputs;
+        const size_t cost = ceil_div(tiles, sms / 2) * size_t(bn + 48);
+        if (cost < best_cost) best = bn, best_cost = cost;
+    }
+    return best;
+}
+
 template <int KIND, int MODE, bool A_MN, bool B_MN>
 int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
     int sms;
     TRY(current_device(sms));
     a.m = int(m);
     a.n = int(n);
-    const int half = MODE == kGated ? a.bn / 2 : a.bn;
-    a.tiles_m = int(ceil_div(m, kRowsM));
-    a.tiles_n = int(ceil_div(n, half));
-    a.group = 16;
+    a.tiles_m = int(ceil_div(m, kTileM));
+    a.tiles_n = int(ceil_div(n, MODE == kGated ? a.bn / 2 : a.bn));
+    a.group = 8;
+    for (int i = 0; i < 3; ++i)
+        if (a.out[i].p && a.out[i].vec && a.out[i].dtype != EQUARX_FP32)
+            TRY(make_map(a.store[i], a.out[i].p, 2, n, m, a.out[i].ld * 2, 32, CU_TENSOR_MAP_SWIZZLE_64B));
     const size_t tiles = size_t(a.tiles_m) * a.tiles_n * (MODE == kOut2 ? 2 : 1);
-    return launch(tile_kernel<KIND, MODE, A_MN, B_MN>, dim3(unsigned(std::min<size_t>(tiles, sms))), kTileThreads,
+    // a pair of CTAs on the two SMs of each TPC; the kernel declares the cluster
+    return launch(tile_kernel<KIND, MODE, A_MN, B_MN>, dim3(unsigned(2 * std::min<size_t>(tiles, sms / 2))), kTileThreads,
                   kTileSmem<KIND>, 1, a, stream);
 }
 
@@ -265,14 +292,16 @@ int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int ac
         return launch_split<KIND, MODE, false>(a, n, m, stream);
     }
     TileArgs a = {};
-    a.bn = 256;
+    int sms;
+    TRY(current_device(sms));
+    a.bn = tile_width(m, n, 1, MODE == kGated, true, sms);
     TRY(make_map(a.a[0], x.codes, 1, stride, m, stride, kRowsM));
     for (int i = 0; i < NW; ++i) {
-        TRY(make_map(a.b[i], w[i].codes, 1, stride, n, stride, a.bn / NW));
-        a.scales_b[i] = w[i].scales;
+        TRY(make_map(a.b[i], w[i].codes, 1, stride, n, stride, a.bn / 2));
+        TRY(scale_map(a.scales_b[i], w[i].scales, n, k, KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV));
         a.row_b[i] = w[i].row_scales;
     }
-    a.scales_a = x.scales;
+    TRY(scale_map(a.scales_a, x.scales, m, k, KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV));
     a.row_a = x.row_scales;
     a.out[0] = out;
     a.stages = int(fp4_stages(k));
@@ -494,7 +523,9 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
         return launch_split<kHalf, kGated, false>(a, f, m, stream);
     }
     TileArgs a = {};
-    a.bn = 256;
+    int sms;
+    TRY(current_device(sms));
+    a.bn = tile_width(m, f, 1, true, false, sms);
     TRY(map16(a.a[0], ox, m, k, kRowsM));
     TRY(map16(a.b[0], og, f, k, a.bn / 2));
     TRY(map16(a.b[1], ou, f, k, a.bn / 2));
@@ -579,7 +610,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
         TRY((launch_split<kHalf, kSum2, true>(a, k, m, stream)));
     } else {
         TileArgs a = {};
-        a.bn = 256;
+        a.bn = tile_width(m, k, 1, false, false, sms);
         TRY(map16(a.a[0], dg, m, f, kRowsM));
         TRY(map16(a.a[1], du, m, f, kRowsM));
         TRY(map16(a.b[0], og, f, k, 64));
@@ -591,7 +622,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     }
     // dWg = dG^T x, dWu = dU^T x: the reduction runs over the tokens
     TileArgs a = {};
-    a.bn = 256;
+    a.bn = tile_width(f, k, 2, false, false, sms);
     TRY(map16(a.a[0], dg, m, f, 64));
     TRY(map16(a.a[1], du, m, f, 64));
     TRY(map16(a.b[0], ox, m, k, 64));

@@ -2,7 +2,7 @@
 // products and gated products of 16-bit and of microscaled 4-bit operands, their gradients, and the
 // 4-bit quantiser.
 //
-//   tile_kernel       persistent 128 x bn output tiles on the tensor cores
+//   tile_kernel       persistent 256 x bn output tiles on the tensor cores of two SMs
 //   split_kernel      few tokens: weights on the 128-row side, the reduction split over a cluster
 //   gate_grad_kernel  gradients of the two projections from dh, g and u
 //   pack_kernel       rows that TMA cannot read (a stride that is no multiple of 16 bytes) -> rows it can
@@ -107,27 +107,40 @@ __device__ __forceinline__ void transpose32(float (&v)[32]) {
     }
 }
 
-// A warp's 32 rows x 32 columns, lane t holding row t.  Aligned rows: each lane writes its own 64 (128)
-// bytes, whole sectors.  Otherwise the tile is transposed so that a row's columns are written by
-// neighbouring lanes together; writing them lane by lane would touch each sector sixteen times.
-__device__ __forceinline__ void store_tile(const Out& o, int row0, int col0, int rows, int cols, float (&v)[32]) {
+constexpr int kStageOut = 32 * 32 * 2;        // bytes of a staged 32 x 32 block of 16-bit outputs
+
+// A warp's 32 rows x 32 columns, lane t holding row t, to an output whose rows TMA can write: through one
+// of the warp's two buffers in shared memory (rows of 64 bytes, 16-byte pieces swizzled as the tensor map
+// says, so that the lanes' writes meet no bank twice).  The store itself is asynchronous; the buffer is
+// free again when at most one later store has not been read.
+__device__ __forceinline__ void store_staged(const CUtensorMap* map, uint32_t buf, int row0, int col0, int dtype,
+                                             const float (&v)[32]) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (lane == 0) tma_store_wait_read<1>();
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        st_shared_v4(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), pack2(v[8 * c], v[8 * c + 1], dtype),
+                     pack2(v[8 * c + 2], v[8 * c + 3], dtype), pack2(v[8 * c + 4], v[8 * c + 5], dtype),
+                     pack2(v[8 * c + 6], v[8 * c + 7], dtype));
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) tma_store_2d(map, buf, col0, row0);
+}
+
+// The same to any other output.  fp32 rows that are aligned: each lane writes its own 128 bytes.  Rows that
+// are not: the block is transposed so that a row's columns are written by neighbouring lanes together;
+// writing them lane by lane would touch each sector sixteen times.
+__device__ __forceinline__ void store_direct(const Out& o, int row0, int col0, int rows, int cols, float (&v)[32]) {
     const int lane = threadIdx.x & 31;
-    if (o.vec && col0 + 32 <= cols) {
-        if (row0 + lane >= rows) return;
-        if (o.dtype == kFp32) {
+    if (o.vec && o.dtype == kFp32 && col0 + 32 <= cols) {
+        if (row0 + lane < rows) {
             float4* q = reinterpret_cast<float4*>(static_cast<float*>(o.p) + size_t(row0 + lane) * o.ld + col0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        } else {
-            uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(o.p) + size_t(row0 + lane) * o.ld + col0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                q[i] = make_uint4(pack2(v[8 * i], v[8 * i + 1], o.dtype), pack2(v[8 * i + 2], v[8 * i + 3], o.dtype),
-                                  pack2(v[8 * i + 4], v[8 * i + 5], o.dtype), pack2(v[8 * i + 6], v[8 * i + 7], o.dtype));
         }
         return;
     }
-    if (col0 >= cols) return;
     transpose32(v);
     if (col0 + lane < cols) {
 #pragma unroll
@@ -136,26 +149,48 @@ __device__ __forceinline__ void store_tile(const Out& o, int row0, int col0, int
     }
 }
 
+// v *= row factor * column factors, in that order: the product of two factors alone could underflow
+__device__ __forceinline__ void scale_columns(float (&v)[32], float row, const float* cols, int col0, int n) {
+    if (col0 + 32 <= n) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float4 c = reinterpret_cast<const float4*>(cols + col0)[j];
+            v[4 * j] = v[4 * j] * row * c.x;
+            v[4 * j + 1] = v[4 * j + 1] * row * c.y;
+            v[4 * j + 2] = v[4 * j + 2] * row * c.z;
+            v[4 * j + 3] = v[4 * j + 3] * row * c.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (col0 + j < n) v[j] = v[j] * row * cols[col0 + j];
+    }
+}
+
 // ---------------------------------------------------------------- persistent tiles
 struct TileArgs {
     CUtensorMap a[2], b[2];
-    const uint8_t* scales_a;
-    const uint8_t* scales_b[2];
-    const float* row_a;               // NV: one factor for each row of a and of b
+    CUtensorMap scales_a, scales_b[2];    // 4-bit: the scales of 128 rows and one stage are rows of 128 bytes
+    CUtensorMap store[3];                 // 16-bit outputs with aligned rows: blocks of 32 x 32
+    const float* row_a;                   // NV: one factor for each row of a and of b
     const float* row_b[2];
-    Out out[3];                       // gated: h, g, u; two outputs: one each
-    int m, n;                         // rows and columns of an output
-    int stages;                       // stages of the reduction axis (of each of the two parts of kSum2)
+    Out out[3];                           // gated: h, g, u; two outputs: one each
+    int m, n;                             // rows and columns of an output
+    int stages;                           // stages of the reduction axis (of each of the two parts of kSum2)
     int tiles_m, tiles_n, bn, group;
     int act, bf16, save;
 };
 
-template <int KIND> constexpr int kPipe = 4;
-template <int KIND> constexpr int kStageBytes = kTileBytes + 2 * kTileBytes + 3 * kScaleBytes<KIND>;
+constexpr int kTileM = 256;               // rows of a tile: 128 in each CTA of a pair
+// shared memory of a stage, in each CTA: its 128 rows of a, its half of the tile's columns of b, and
+// the scales of its rows of a and of all columns of b
+template <int KIND> constexpr int kStageBytes = 2 * kTileBytes + 3 * kScaleBytes<KIND>;
+template <int KIND> constexpr int kPipe = KIND == kHalf ? 6 : 5;
 constexpr int kEpilogueWarps = 8;
 constexpr int kTileThreads = 32 * (kEpilogueWarps + 2);
-constexpr int kSmemSlack = 1024;      // 128-byte swizzle atoms start on multiples of 1024 bytes
-template <int KIND> constexpr int kTileSmem = kPipe<KIND> * kStageBytes<KIND> + kSmemSlack;
+constexpr int kSmemSlack = 1024;          // 128-byte swizzle atoms start on multiples of 1024 bytes
+constexpr int kStaging = kEpilogueWarps * 2 * kStageOut;
+template <int KIND> constexpr int kTileSmem = kPipe<KIND> * kStageBytes<KIND> + kStaging + kSmemSlack;
 
 // tile t in an order that walks `group` row tiles before the next column tile: the tiles that run at
 // one time share operands in L2
@@ -166,17 +201,21 @@ __device__ __forceinline__ void tile_at(const TileArgs& p, int t, int& mt, int& 
     nt = r / gm;
 }
 
-// Output tiles of 128 x bn.  One thread starts TMA loads through a ring of stages, one thread issues
-// the products, eight warps move finished accumulators from tensor memory to the output; two
-// accumulators let the next tile's products run meanwhile.  4-bit operands: the scales need tensor
-// memory too, so the second accumulator begins 64 columns inside the first, and each is drained from
-// that end first.
+// Output tiles of 256 x bn by pairs of CTAs: each holds half of the rows of a and half of the columns
+// of b, the tensor cores of both read both halves of b, so a pair loads (256 + bn) rows a stage where
+// two single CTAs would load 2 (128 + bn); L2 to SM traffic, not the tensor cores, bounds the single
+// form.  In each CTA one thread starts TMA loads through a ring of stages; in the first CTA one thread
+// issues the products for both; eight warps move finished accumulators from tensor memory to the
+// output.  Two accumulators let the next tile's products run meanwhile.  4-bit operands: the scales
+// need tensor memory too, so the second accumulator begins 64 columns inside the first, and each is
+// drained from that end first.
 //
-// kGated: columns [0, bn/2) of the tile are x Wg^T and [bn/2, bn) the same columns of x Wu^T, so a
-// thread finds g and u of one element in its own row and writes act(g) u.
+// kGated: columns [0, bn/2) of the tile, the first CTA's half of b, are x Wg^T and [bn/2, bn) the same
+// columns of x Wu^T, so a thread finds g and u of one element in its own row and writes act(g) u.
 // kSum2: out = a0 b0 + a1 b1.  kOut2: out0 = a0 b0, out1 = a1 b0, tiles of both in one launch.
 template <int KIND, int MODE, bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_constant__ TileArgs p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
+    tile_kernel(const __grid_constant__ TileArgs p) {
     constexpr bool FP4 = KIND != kHalf;
     constexpr int PIPE = kPipe<KIND>, STAGE = kStageBytes<KIND>, SB = kScaleBytes<KIND>;
     constexpr uint32_t kSecond = FP4 ? 192 : 256;       // first column of the second accumulator
@@ -189,7 +228,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t full = smem_addr(bars), empty = full + 8 * PIPE, ready = empty + 8 * PIPE, drained = ready + 16,
                    drain = drained + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int rank = uniform(cluster_rank()), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < PIPE; ++i) {
@@ -198,122 +238,128 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(ready + 8 * i, 1);
-            barrier_init(drained + 8 * i, kEpilogueWarps);
+            barrier_init(drained + 8 * i, 2 * kEpilogueWarps);
         }
         barrier_init(drain, 1);
         abort = 0;
         fence_barrier_init();
     }
-    if (warp == kEpilogueWarps) tmem_alloc(smem_addr(&tmem_slot), 512);
+    if (warp == kEpilogueWarps) tmem_alloc<2>(smem_addr(&tmem_slot), 512);
     fence_before();
     __syncthreads();
+    cluster_sync();                                     // the other CTA's barriers are ready too
     fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = uniform(tmem_slot);
 
     const int tiles = p.tiles_m * p.tiles_n * (MODE == kOut2 ? 2 : 1);
     const int stages = p.stages * (MODE == kSum2 ? 2 : 1);
-    const int half = MODE == kGated ? p.bn / 2 : p.bn;
+    const int half = p.bn / 2;                          // columns of b in each CTA
+    const int width = MODE == kGated ? half : p.bn;     // output columns of a tile
     grid_launch();
     grid_wait();
 
     if (warp == kEpilogueWarps + 1) {
-        if (lane == 0) {
+        {
             // ------------------------------------------------ loads
             uint32_t it = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            for (int t = pair; t < tiles && ok; t += pairs) {
                 const int which = MODE == kOut2 ? t >= p.tiles_m * p.tiles_n : 0;
                 int mt, nt;
                 tile_at(p, t - which * p.tiles_m * p.tiles_n, mt, nt);
-                const int m0 = mt * kRowsM, n0 = nt * half;
-                const int sn0 = n0 / 128, sn = FP4 ? min(half / 128, (p.n + 127) / 128 - sn0) : 0;
+                const int m0 = mt * kTileM + rank * kRowsM;
+                const int n0 = nt * width + (MODE == kGated ? 0 : rank * half);
+                // scales: 128-row groups of a (the second may not exist) and of b (each CTA takes all)
+                const int groups_a = FP4 ? (p.m + 127) / 128 : 0, ga = mt * 2 + rank;
+                const int gb = nt * width / 128, nb = FP4 ? min(width / 128, (p.n + 127) / 128 - gb) : 0;
+                uint32_t bytes = 2 * kTileBytes + 2 * (B_MN ? (half + 63) / 64 * kChunkBytes : half * kRowBytes);
+                if (FP4) bytes += SB * (min(2, groups_a - mt * 2) + 2 * nb * (MODE == kGated ? 2 : 1));
                 for (int s = 0; s < stages; ++s, ++it) {
                     const uint32_t slot = it % PIPE;
-                    if (!(ok = barrier_wait(empty + 8 * slot, (it / PIPE & 1) ^ 1, &abort))) break;
-                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, bar = full + 8 * slot;
+                    if (!(ok = barrier_wait_warp(empty + 8 * slot, (it / PIPE & 1) ^ 1, &abort))) break;
+                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes;
+                    // both CTAs' loads count on the first one's barrier
+                    if (rank == 0) barrier_expect_warp(full + 8 * slot, bytes);
+                    const uint32_t bar = peer_addr(full + 8 * slot, 0);
                     const int part = MODE == kSum2 ? s >= p.stages : 0;
                     const int ks = s - part * p.stages;
                     const CUtensorMap* ma = &p.a[MODE == kOut2 ? which : part];
-                    uint32_t bytes = kTileBytes;
-                    if (B_MN) bytes += (p.bn + 63) / 64 * kChunkBytes; else bytes += p.bn * kRowBytes;
-                    if (FP4) bytes += SB * (1 + (MODE == kGated ? 2 : 1) * sn);
-                    barrier_expect(bar, bytes);
+                    const CUtensorMap* mb = &p.b[MODE == kGated ? rank : part];
                     const int kc = FP4 ? ks * kRowBytes : ks * 64;     // 4-bit codes travel as bytes
                     if (A_MN) {
-                        tma_load_2d(sa, ma, m0, kc, bar);
-                        tma_load_2d(sa + kChunkBytes, ma, m0 + 64, kc, bar);
+                        tma_load_2d_pair(sa, ma, m0, kc, bar);
+                        tma_load_2d_pair(sa + kChunkBytes, ma, m0 + 64, kc, bar);
                     } else {
-                        tma_load_2d(sa, ma, kc, m0, bar);
+                        tma_load_2d_pair(sa, ma, kc, m0, bar);
                     }
                     if (B_MN) {
-                        for (int c = 0; c < p.bn; c += 64)
-                            tma_load_2d(sb + c / 64 * kChunkBytes, &p.b[part], n0 + c, kc, bar);
+                        for (int c = 0; c < half; c += 64)
+                            tma_load_2d_pair(sb + c / 64 * kChunkBytes, mb, n0 + c, kc, bar);
                     } else {
-                        tma_load_2d(sb, &p.b[part], kc, n0, bar);
-                        if (MODE == kGated) tma_load_2d(sb + half * kRowBytes, &p.b[1], kc, n0, bar);
+                        tma_load_2d_pair(sb, mb, kc, n0, bar);
                     }
                     if (FP4) {
-                        const uint32_t ss = sb + 2 * kTileBytes;
-                        bulk_load(ss, p.scales_a + (size_t(mt) * p.stages + ks) * SB, SB, bar);
+                        const uint32_t ss = sb + kTileBytes;
+                        if (ga < groups_a) tma_load_2d_pair(ss, &p.scales_a, 0, (ga * p.stages + ks) * (SB / 128), bar);
                         for (int q = 0; q < (MODE == kGated ? 2 : 1); ++q)
-                            for (int i = 0; i < sn; ++i)
-                                bulk_load(ss + SB * (1 + q + i), p.scales_b[q] + (size_t(sn0 + i) * p.stages + ks) * SB, SB,
-                                          bar);
+                            for (int i = 0; i < nb; ++i)
+                                tma_load_2d_pair(ss + SB * (1 + q + i), &p.scales_b[q], 0,
+                                                 ((gb + i) * p.stages + ks) * (SB / 128), bar);
                     }
                 }
             }
-            if (abort)          // what has been started lands before the shared memory goes away
+            if (abort && rank == 0)     // what has been started lands before the shared memory goes away
                 for (uint32_t i = it > PIPE ? it - PIPE : 0; i < it; ++i) barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
         }
         __syncwarp();
     } else if (warp == kEpilogueWarps) {
-        if (lane == 0) {
+        if (rank == 0) {
             // ------------------------------------------------ products
             const uint32_t ta = tmem + kScaleCol, tb = ta + 4 * kScaleTiles<KIND>;
             uint32_t it = 0, local = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++local) {
+            for (int t = pair; t < tiles && ok; t += pairs, ++local) {
                 const uint32_t buf = local & 1, d = tmem + buf * kSecond;
                 if (FP4) {
                     // the tile before has given up the columns that both accumulators use
-                    if (local && !(ok = barrier_wait(drained, (local - 1) & 1, &abort))) break;
+                    if (local && !(ok = barrier_wait_warp(drained, (local - 1) & 1, &abort))) break;
                 } else {
-                    if (local > 1 && !(ok = barrier_wait(drained + 8 * buf, (local / 2 - 1) & 1, &abort))) break;
+                    if (local > 1 && !(ok = barrier_wait_warp(drained + 8 * buf, (local / 2 - 1) & 1, &abort))) break;
                 }
                 fence_after();
                 for (int s = 0; s < stages; ++s, ++it) {
                     const uint32_t slot = it % PIPE;
-                    if (!(ok = barrier_wait(full + 8 * slot, it / PIPE & 1, &abort))) break;
+                    if (!(ok = barrier_wait_warp(full + 8 * slot, it / PIPE & 1, &abort))) break;
                     fence_after();
-                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, ss = sb + 2 * kTileBytes;
+                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, ss = sb + kTileBytes;
                     if (FP4) {
 #pragma unroll
                         for (int j = 0; j < kScaleTiles<KIND>; ++j) {
-                            copy_scales(ta + 4 * j, ss + 512 * j);
-                            copy_scales(tb + 8 * j, ss + SB + 512 * j);
-                            if (p.bn > 128) copy_scales(tb + 8 * j + 4, ss + 2 * SB + 512 * j);
+                            copy_scales<2>(ta + 4 * j, ss + 512 * j);
+                            copy_scales<2>(tb + 8 * j, ss + SB + 512 * j);
+                            if (p.bn > 128) copy_scales<2>(tb + 8 * j + 4, ss + 2 * SB + 512 * j);
                         }
                     }
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) {
-                        const uint64_t da = A_MN ? swizzled_desc(sa + 2048 * kk, kChunkBytes, 1024)
-                                                 : swizzled_desc(sa + 32 * kk, 16, 1024);
-                        const uint64_t db = B_MN ? swizzled_desc(sb + 2048 * kk, kChunkBytes, 1024)
-                                                 : swizzled_desc(sb + 32 * kk, 16, 1024);
+                        const uint32_t da = A_MN ? swizzled_desc(sa + 2048 * kk, kChunkBytes)
+                                                 : swizzled_desc(sa + 32 * kk, 16);
+                        const uint32_t db = B_MN ? swizzled_desc(sb + 2048 * kk, kChunkBytes)
+                                                 : swizzled_desc(sb + 32 * kk, 16);
                         if constexpr (FP4) {
                             const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
-                            mma_fp4<KIND == kMx>(d, da, db, desc_fp4(KIND == kMx, p.bn, which), ta + 4 * j, tb + 8 * j,
-                                                 s | kk);
+                            mma_fp4<2, KIND == kMx>(d, da, db, desc_fp4(KIND == kMx, kTileM, p.bn, which), ta + 4 * j,
+                                                    tb + 8 * j, s | kk);
                         } else {
-                            mma_16bit(d, da, db, desc_16bit(p.bf16, A_MN, B_MN, p.bn), s | kk);
+                            mma_16bit<2>(d, da, db, desc_16bit(p.bf16, A_MN, B_MN, kTileM, p.bn), s | kk);
                         }
                     }
-                    mma_commit(empty + 8 * slot);
+                    mma_commit<2>(empty + 8 * slot);
                 }
-                if (ok) mma_commit(ready + 8 * buf);
+                if (ok) mma_commit<2>(ready + 8 * buf);
             }
             if (abort) {        // products in flight read this shared memory
-                mma_commit(drain);
+                mma_commit<2>(drain);
                 barrier_drain(drain, 0);
             }
         }
@@ -321,14 +367,25 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
     } else {
         // ---------------------------------------------------- outputs
         const int quarter = warp & 3, side = warp >> 2;
-        const int units = half / 32;                       // blocks of 32 output columns
-        uint32_t local = 0;
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++local) {
+        const int units = width / 32;                      // blocks of 32 output columns
+        uint32_t local = 0, flip = 0;
+        const uint32_t staging = smem + PIPE * STAGE + warp * 2 * kStageOut;
+        auto store = [&](int i, int row0, int col0, float (&v)[32]) {
+            if (row0 >= p.m || col0 >= p.n) return;
+            if (p.out[i].vec && p.out[i].dtype != kFp32) {
+                store_staged(&p.store[i], staging + flip, row0, col0, p.out[i].dtype, v);
+                flip ^= kStageOut;
+            } else {
+                store_direct(p.out[i], row0, col0, p.m, p.n, v);
+            }
+        };
+        for (int t = pair; t < tiles; t += pairs, ++local) {
             const int which = MODE == kOut2 ? t >= p.tiles_m * p.tiles_n : 0;
             int mt, nt;
             tile_at(p, t - which * p.tiles_m * p.tiles_n, mt, nt);
-            const int row0 = mt * kRowsM + quarter * 32, n0 = nt * half;
+            const int row0 = mt * kTileM + rank * kRowsM + quarter * 32, n0 = nt * width;
             const uint32_t buf = local & 1, acc = tmem + buf * kSecond + (uint32_t(quarter * 32) << 16);
+            const uint32_t done = peer_addr(FP4 ? drained : drained + 8 * buf, 0);
             float ra = 1.0f;
             if (KIND == kNv && row0 + lane < p.m) ra = p.row_a[row0 + lane];
             if (!barrier_wait(ready + 8 * buf, local / 2 & 1, &abort)) break;
@@ -349,56 +406,41 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(const __grid_cons
                 if (i == (FP4 ? 0 : steps - 1)) {
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) barrier_arrive(FP4 ? drained : drained + 8 * buf);
+                    if (lane == 0) barrier_arrive_cluster(done);
                 }
                 if (!live) continue;
                 const int col0 = n0 + 32 * u;
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-                if (KIND == kNv) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] *= ra;
-                    if (col0 + 32 <= p.n) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float4 b = reinterpret_cast<const float4*>(p.row_b[0] + col0)[j];
-                            v[4 * j] *= b.x; v[4 * j + 1] *= b.y; v[4 * j + 2] *= b.z; v[4 * j + 3] *= b.w;
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col0 + j < p.n) v[j] *= p.row_b[0][col0 + j];
-                    }
-                }
+                if (KIND == kNv) scale_columns(v, ra, p.row_b[0], col0, p.n);
                 if constexpr (MODE == kGated) {
                     float w[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) w[j] = __uint_as_float(q[j]);
-                    if (KIND == kNv) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col0 + j < p.n) w[j] = w[j] * ra * p.row_b[1][col0 + j];
-                    }
+                    if (KIND == kNv) scale_columns(w, ra, p.row_b[1], col0, p.n);
                     float h[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) h[j] = act(v[j], p.act) * w[j];
-                    store_tile(p.out[0], row0, col0, p.m, p.n, h);
+                    store(0, row0, col0, h);
                     if (KIND == kHalf && p.save) {
-                        store_tile(p.out[1], row0, col0, p.m, p.n, v);
-                        store_tile(p.out[2], row0, col0, p.m, p.n, w);
+                        store(1, row0, col0, v);
+                        store(2, row0, col0, w);
                     }
                 } else {
-                    store_tile(p.out[which], row0, col0, p.m, p.n, v);
+                    store(which, row0, col0, v);
                 }
             }
         }
+        if (lane == 0) tma_store_wait_all();
+        __syncwarp();
     }
     fence_before();
     __syncthreads();
+    cluster_sync();             // the other CTA reads this one's shared memory and arrives on its barriers
     if (warp == kEpilogueWarps) {
         fence_after();
-        tmem_free(tmem, 512);
+        tmem_free<2>(tmem, 512);
     }
 }
 
@@ -442,7 +484,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     float* const part = reinterpret_cast<float*>(smem_raw + pad);          // [NW * nt][128], after the products
     const uint32_t full = smem_addr(bars), empty = full + 8 * kSplitMaxPipe, ready = empty + 8 * kSplitMaxPipe,
                    drain = ready + 8;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const uint32_t xb = p.nt * kRowBytes, STAGE = NW * (kTileBytes + SB) + xb + SB;
 
     if (threadIdx.x == 0) {
@@ -455,13 +497,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         abort = 0;
         fence_barrier_init();
     }
-    if (warp == 5) tmem_alloc(smem_addr(&tmem_slot), 512);
+    if (warp == 5) tmem_alloc<1>(smem_addr(&tmem_slot), 512);
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = uniform(tmem_slot);
 
-    const int ranks = gridDim.x, rank = cluster_rank();
+    const int ranks = gridDim.x, rank = uniform(cluster_rank());
     const int total = p.stages * (MODE == kSum2 ? 2 : 1);
     const int s0 = int(int64_t(total) * rank / ranks), s1 = int(int64_t(total) * (rank + 1) / ranks);
     const int f0 = blockIdx.y * kRowsM, t0 = blockIdx.z * p.nt;
@@ -469,16 +511,16 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     grid_wait();
 
     if (warp == 4) {
-        if (lane == 0) {
+        {
             bool ok = true;
             int it = 0;
             for (int s = s0; s < s1; ++s, ++it) {
                 const int slot = it % p.pipe;
-                if (!(ok = barrier_wait(empty + 8 * slot, (it / p.pipe & 1) ^ 1, &abort))) break;
+                if (!(ok = barrier_wait_warp(empty + 8 * slot, (it / p.pipe & 1) ^ 1, &abort))) break;
                 const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb, bar = full + 8 * slot;
                 const int second = MODE == kSum2 ? s >= p.stages : 0, ks = s - second * p.stages;
                 const int kc = FP4 ? ks * kRowBytes : ks * 64;
-                barrier_expect(bar, NW * kTileBytes + xb + (FP4 ? (NW + 1) * SB : 0));
+                barrier_expect_warp(bar, NW * kTileBytes + xb + (FP4 ? (NW + 1) * SB : 0));
                 for (int q = 0; q < NW; ++q) {
                     const CUtensorMap* mw = &p.w[MODE == kSum2 ? second : q];
                     if (W_MN) {
@@ -497,13 +539,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         }
         __syncwarp();
     } else if (warp == 5) {
-        if (lane == 0) {
+        {
             const uint32_t tw = tmem + kScaleCol, tx = tw + NW * 4 * kScaleTiles<KIND>;
             bool ok = true;
             int it = 0;
             for (int s = s0; s < s1; ++s, ++it) {
                 const int slot = it % p.pipe;
-                if (!(ok = barrier_wait(full + 8 * slot, it / p.pipe & 1, &abort))) break;
+                if (!(ok = barrier_wait_warp(full + 8 * slot, it / p.pipe & 1, &abort))) break;
                 fence_after();
                 const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb;
                 if (FP4) {
@@ -511,32 +553,32 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
                     for (int j = 0; j < kScaleTiles<KIND>; ++j) {
 #pragma unroll
                         for (int q = 0; q < NW; ++q)
-                            copy_scales(tw + (q * kScaleTiles<KIND> + j) * 4, ss + SB * q + 512 * j);
-                        copy_scales(tx + 4 * j, ss + SB * NW + 512 * j);
+                            copy_scales<1>(tw + (q * kScaleTiles<KIND> + j) * 4, ss + SB * q + 512 * j);
+                        copy_scales<1>(tx + 4 * j, ss + SB * NW + 512 * j);
                     }
                 }
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk) {
-                    const uint64_t dx = swizzled_desc(sx + 32 * kk, 16, 1024);
+                    const uint32_t dx = swizzled_desc(sx + 32 * kk, 16);
 #pragma unroll
                     for (int q = 0; q < NW; ++q) {
                         const uint32_t a = sw + q * kTileBytes;
-                        const uint64_t dw = W_MN ? swizzled_desc(a + 2048 * kk, kChunkBytes, 1024)
-                                                 : swizzled_desc(a + 32 * kk, 16, 1024);
+                        const uint32_t dw = W_MN ? swizzled_desc(a + 2048 * kk, kChunkBytes)
+                                                 : swizzled_desc(a + 32 * kk, 16);
                         if constexpr (FP4) {
                             const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
-                            mma_fp4<KIND == kMx>(tmem + q * p.nt, dw, dx, desc_fp4(KIND == kMx, p.nt, which),
+                            mma_fp4<1, KIND == kMx>(tmem + q * p.nt, dw, dx, desc_fp4(KIND == kMx, 128, p.nt, which),
                                                  tw + (q * kScaleTiles<KIND> + j) * 4, tx + 4 * j, it | kk);
                         } else {
-                            mma_16bit(tmem + q * p.nt, dw, dx, desc_16bit(p.bf16, W_MN, false, p.nt), it | kk);
+                            mma_16bit<1>(tmem + q * p.nt, dw, dx, desc_16bit(p.bf16, W_MN, false, 128, p.nt), it | kk);
                         }
                     }
                 }
-                mma_commit(empty + 8 * slot);
+                mma_commit<1>(empty + 8 * slot);
             }
-            if (ok) mma_commit(ready);
+            if (ok) mma_commit<1>(ready);
             if (abort) {
-                mma_commit(drain);
+                mma_commit<1>(drain);
                 barrier_drain(drain, 0);
             }
         }
@@ -559,7 +601,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     __syncthreads();
     if (warp == 5) {
         fence_after();
-        tmem_free(tmem, 512);
+        tmem_free<1>(tmem, 512);
     }
     cluster_sync();
 

@@ -59,6 +59,9 @@ __device__ __forceinline__ void barrier_drain(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void fence_barrier_init() {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ---------------------------------------------------------------- clusters, dependent launches
@@ -69,6 +72,15 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 }
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of the same shared variable in another CTA of the cluster
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void barrier_arrive_cluster(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr, uint32_t rank) {
     float v;
@@ -81,17 +93,59 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// ---------------------------------------------------------------- instructions of one thread
+// Loads and products are issued by one lane of a warp whose 32 lanes run the loop together: with uniform
+// control flow the addresses and descriptors stay in uniform registers, where these instructions want
+// them.  (A loop run by lane 0 alone took 63 cycles for each instruction it issued, more than the
+// tensor cores need for a 256 x 256 x 16 product between them.)
+#define EQUARX_ELECT "{\n .reg .pred elected;\n elect.sync _|elected, 0xFFFFFFFF;\n @elected "
+
+// a value that all lanes share, as one the compiler knows to be shared
+template <typename T>
+__device__ __forceinline__ T uniform(T v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+
+// false in every lane as soon as one lane's wait gave up
+__device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort) {
+    return __all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, abort));
+}
+__device__ __forceinline__ void barrier_expect_warp(uint32_t bar, uint32_t bytes) {
+    asm volatile(EQUARX_ELECT "mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar), "r"(bytes) : "memory");
+}
+
 // ---------------------------------------------------------------- TMA
 // 2-D tile load; x (the contiguous coordinate) always is a multiple of 16 bytes here.
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(bar)
-        : "memory");
+    asm volatile(EQUARX_ELECT
+                 "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}" ::"r"(
+                     dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
 }
+// the same for a pair of CTAs that work on one tile: into this CTA's memory, counted on a barrier of
+// either CTA (a shared::cluster address); no multicast
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t cluster_bar) {
+    asm volatile(EQUARX_ELECT
+                 "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+                 "[%0], [%1, {%2, %3}], [%4];\n}" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
+                 : "memory");
+}
+// 2-D tile store; the part outside the matrix is dropped
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];\n"
+                 "cp.async.bulk.commit_group;" ::"l"(map),
+                 "r"(src), "r"(x), "r"(y)
+                 : "memory");
+}
+// at most PENDING of this thread's stores still read shared memory
+template <int PENDING>
+__device__ __forceinline__ void tma_store_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory");
+}
+__device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-                 "r"(bytes), "r"(bar)
+    asm volatile(EQUARX_ELECT "cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n}" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
                  : "memory");
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
@@ -99,12 +153,24 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
 }
 
 // ---------------------------------------------------------------- tensor memory
+// CTAS is 1 or 2 throughout a kernel: with 2 the pair of CTAs of a cluster works on one tile, one of
+// them issues the products and copies for both.
+template <int CTAS>
 __device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t columns) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if constexpr (CTAS == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
 }
+template <int CTAS>
 __device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
+    else
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -139,59 +205,81 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
 // offset is not used.  Operands whose other axis is contiguous ("MN-major"): atoms of 64 elements (128
 // bytes) x 8 steps of the reduction axis, `stride` from one group of 8 steps to the next and `leading`
 // from one group of 64 elements to the next.
-__device__ __forceinline__ uint64_t swizzled_desc(uint32_t addr, uint32_t leading, uint32_t stride) {
-    return uint64_t((addr >> 4) & 0x3FFF) | (uint64_t((leading >> 4) & 0x3FFF) << 16) |
-           (uint64_t((stride >> 4) & 0x3FFF) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+// Only the low word (address and leading offset) changes; the high one is the stride and constants.
+__device__ __forceinline__ uint32_t swizzled_desc(uint32_t addr, uint32_t leading) {
+    return ((addr >> 4) & 0x3FFF) | (leading >> 4) << 16;
 }
+constexpr uint32_t kSwizzledHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
 // 32 rows x 16 bytes, unswizzled, 128 bytes for each 8 rows: one scale tile
-__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
-    return uint64_t((addr >> 4) & 0x3FFF) | (uint64_t(8) << 32) | (uint64_t(1) << 46);
-}
+__device__ __forceinline__ uint32_t scale_desc(uint32_t addr) { return (addr >> 4) & 0x3FFF; }
+constexpr uint32_t kScaleHigh = (128 >> 4) | 1u << 14;
 
-// Instruction descriptors.  16-bit operands, fp32 accumulation, 128 x n:
-__host__ __device__ constexpr uint32_t desc_16bit(bool bf16, bool a_mn, bool b_mn, uint32_t n) {
+// Instruction descriptors.  16-bit operands, fp32 accumulation, m x n (m = 128 for each CTA):
+__host__ __device__ constexpr uint32_t desc_16bit(bool bf16, bool a_mn, bool b_mn, uint32_t m, uint32_t n) {
     return (1u << 4) | (uint32_t(bf16) << 7) | (uint32_t(bf16) << 10) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16) |
-           ((n >> 3) << 17) | ((128u >> 4) << 24);
+           ((n >> 3) << 17) | ((m >> 4) << 24);
 }
-// block-scaled E2M1 operands, fp32 accumulation, 128 x n; `which` selects the scale bytes (0 or 2) of a
-// 32-bit cell when one step of the reduction uses only half of them
-__host__ __device__ constexpr uint32_t desc_fp4(bool e8m0, uint32_t n, uint32_t which) {
-    return (which << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (uint32_t(e8m0) << 23) | ((128u >> 7) << 27) |
-           (which << 29);
+// block-scaled E2M1 operands, fp32 accumulation; `which` selects the scale bytes (0 or 2) of a 32-bit
+// cell when one step of the reduction uses only half of them
+__host__ __device__ constexpr uint32_t desc_fp4(bool e8m0, uint32_t m, uint32_t n, uint32_t which) {
+    return (which << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (uint32_t(e8m0) << 23) | ((m >> 7) << 27) | (which << 29);
 }
 
-__device__ __forceinline__ void mma_16bit(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
-        : "memory");
+#define EQUARX_MMA_16BIT(GROUP)                                                                             \
+    asm volatile("{\n .reg .pred elected, p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n" \
+                 " setp.ne.u32 p, %4, 0;\n elect.sync _|elected, 0xFFFFFFFF;\n"                             \
+                 " @elected tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d),     \
+                 "r"(a), "r"(b), "r"(idesc), "r"(uint32_t(accumulate)), "n"(kSwizzledHigh)                  \
+                 : "memory")
+#define EQUARX_MMA_FP4(GROUP, KIND)                                                                         \
+    asm volatile("{\n .reg .pred elected, p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %7};\n mov.b64 b, {%2, %7};\n" \
+                 " setp.ne.u32 p, %6, 0;\n elect.sync _|elected, 0xFFFFFFFF;\n"                             \
+                 " @elected tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], a, b, %3, [%4], [%5], p;\n}" ::"r"(d), \
+                 "r"(a), "r"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(uint32_t(accumulate)), "n"(kSwizzledHigh) \
+                 : "memory")
+
+// 16 elements of the reduction axis
+template <int CTAS>
+__device__ __forceinline__ void mma_16bit(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
+    if constexpr (CTAS == 1) EQUARX_MMA_16BIT("1");
+    else EQUARX_MMA_16BIT("2");
 }
 // 64 elements of the reduction axis; one E4M3 scale for each 16 of them (NV) or one E8M0 for each 32 (MX)
-template <bool MX>
-__device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+template <int CTAS, bool MX>
+__device__ __forceinline__ void mma_fp4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
                                         bool accumulate) {
-    if constexpr (MX)
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-            " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(uint32_t(accumulate))
-            : "memory");
-    else
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-            " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(uint32_t(accumulate))
-            : "memory");
+    if constexpr (CTAS == 1 && MX) EQUARX_MMA_FP4("1", "mxf4.block_scale.scale_vec::2X");
+    else if constexpr (CTAS == 1) EQUARX_MMA_FP4("1", "mxf4nvf4.block_scale.scale_vec::4X");
+    else if constexpr (MX) EQUARX_MMA_FP4("2", "mxf4.block_scale.scale_vec::2X");
+    else EQUARX_MMA_FP4("2", "mxf4nvf4.block_scale.scale_vec::4X");
 }
+#undef EQUARX_MMA_16BIT
+#undef EQUARX_MMA_FP4
 // one scale tile (128 rows x 4 scales) from shared to tensor memory, where each quarter of the lanes
-// gets its own copy, as the block-scaled product wants it
+// gets its own copy, as the block-scaled product wants it; with two CTAs, in each of them
+template <int CTAS>
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(scale_desc(smem)) : "memory");
+#define EQUARX_COPY(GROUP)                                                                            \
+    asm volatile("{\n .reg .pred elected;\n .reg .b64 a;\n mov.b64 a, {%1, %2};\n"                   \
+                 " elect.sync _|elected, 0xFFFFFFFF;\n"                                               \
+                 " @elected tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [%0], a;\n}" ::"r"(tmem),   \
+                 "r"(scale_desc(smem)), "n"(kScaleHigh)                                               \
+                 : "memory")
+    if constexpr (CTAS == 1) EQUARX_COPY("1");
+    else EQUARX_COPY("2");
+#undef EQUARX_COPY
 }
-// arrives on `bar` when everything this thread has issued before is done
+// arrives on `bar` (of both CTAs, with two) when everything this warp has issued before is done
+template <int CTAS>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile(EQUARX_ELECT "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar)
+                     : "memory");
+    else
+        asm volatile(EQUARX_ELECT
+                     "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(bar),
+                     "h"(uint16_t(3))
+                     : "memory");
 }
 
 }  // namespace tc
