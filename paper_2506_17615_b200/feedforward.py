@@ -6,81 +6,125 @@
 with 16-bit weights and their gradients (gated_forward, gated_backward), or with weights and
 activations in microscaled 4-bit floating point (fp4_quantize, fp4_dequantize, fp4_matmul, fp4_linear,
 fp4_gated).  Marshalling only: outputs and workspaces are allocated with torch on the current stream,
-the kernels run on it, and every argument check but those on shapes and strides is the library's own
-(include/equarx.h has the formulas and layouts).  A failed call raises EquarxError, tensors that do not
-fit together raise ValueError; there is no CPU path.
+the kernels run on it, and every argument check but those on shapes, strides and devices is the library's
+own (include/equarx.h has the formulas and layouts).  A failed call raises EquarxError, tensors that do
+not fit together raise ValueError; there is no CPU path.
 
-Matrices are [rows, columns] with unit column stride; the row stride is free.
+Matrices are [rows, columns] with unit column stride; the row stride is free.  A call for a few tokens is
+over in a few microseconds on the GPU, so what it costs on the host counts: one output allocation, one
+workspace allocation where one is needed, plain integers into the library.
 """
-from dataclasses import dataclass
+from functools import lru_cache
 
 import torch
 
 from . import binding
-from .binding import ACT_GELU_TANH, ACT_SILU, FP4_MX, FP4_NV  # noqa: F401  (part of this module's interface)
+from .binding import ACT_GELU_TANH, ACT_SILU, FP4_MX, FP4_NV, EquarxError  # noqa: F401  (part of this module's interface)
 
 _DTYPES = {torch.bfloat16: binding.BF16, torch.float16: binding.FP16, torch.float32: binding.FP32}
+_lib = binding.lib
+
+# what a call needs beside its tensors depends on its shape alone
+_scales_bytes = lru_cache(maxsize=4096)(_lib.equarx_fp4_scales_bytes)
+_linear_workspace = lru_cache(maxsize=4096)(_lib.equarx_fp4_linear_workspace_bytes)
+_forward_workspace = lru_cache(maxsize=4096)(_lib.equarx_gated_forward_workspace_bytes)
+_backward_workspace = lru_cache(maxsize=4096)(_lib.equarx_gated_backward_workspace_bytes)
 
 
-@dataclass(frozen=True)
+def _up(n, to):
+    return -(-n // to) * to
+
+
 class Fp4Matrix:
-    """A rows x cols matrix in microscaled 4-bit floating point (FP4_MX or FP4_NV)."""
-    codes: torch.Tensor                  # uint8 [rows, ceil(cols/32)*16]
-    scales: torch.Tensor                 # uint8, in the tiled order of include/equarx.h
-    row_scales: torch.Tensor | None      # float32 [rows] (FP4_NV)
-    rows: int
-    cols: int
-    format: int
+    """A rows x cols matrix in microscaled 4-bit floating point (FP4_MX or FP4_NV): one buffer that holds
+    scales, row factors and codes, each part starting on a multiple of 256 bytes."""
+    __slots__ = ("data", "rows", "cols", "format", "_parts")
+
+    def __init__(self, data, rows, cols, format):
+        self.data, self.rows, self.cols, self.format = data, rows, cols, format
+        base = data.data_ptr()
+        row_scales = _up(_scales_bytes(rows, cols, format), 256)
+        codes = row_scales + (_up(4 * rows, 256) if format == FP4_NV else 0)
+        self._parts = (base + codes, base, base + row_scales if format == FP4_NV else 0)
+
+    @staticmethod
+    def nbytes(rows, cols, format):
+        return _up(_scales_bytes(rows, cols, format), 256) + (_up(4 * rows, 256) if format == FP4_NV else 0) + \
+            rows * (_up(cols, 32) // 2)
+
+    @property
+    def codes(self):
+        """uint8 [rows, ceil(cols/32)*16], two codes a byte, the first in the low half"""
+        return self.data[self._parts[0] - self.data.data_ptr():].view(self.rows, _up(self.cols, 32) // 2)
+
+    @property
+    def scales(self):
+        """uint8, in the tiled order of include/equarx.h"""
+        return self.data[:_scales_bytes(self.rows, self.cols, self.format)]
+
+    @property
+    def row_scales(self):
+        """float32 [rows] (FP4_NV), None (FP4_MX)"""
+        if self.format != FP4_NV:
+            return None
+        first = self._parts[2] - self.data.data_ptr()
+        return self.data[first:first + 4 * self.rows].view(torch.float32)
 
 
-def _matrix(t, what, rows=None, cols=None, dtype=None):
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what} must be a matrix whose columns are contiguous")
+def _matrix(t, what, rows=None, cols=None, dtype=None, device=None):
+    """t's shape, row stride and device, after the checks"""
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be a matrix")
+    r, c = t.shape
+    ld, unit = t.stride()
+    if unit != 1 and c > 1:
+        raise ValueError(f"{what} must have contiguous columns")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA tensor")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{what} is {tuple(t.shape)}, expected ({rows}, {cols})")
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{what} is ({r}, {c}), expected ({rows}, {cols})")
     if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{what} has type {t.dtype}")
-    return t
+    dev = t.get_device()
+    if device is not None and dev != device:
+        raise ValueError(f"{what} is on device {dev}, expected {device}")
+    # torch reports any stride for a single row
+    return r, c, ld if r > 1 else max(ld, c), dev
 
 
-def _ld(t):
-    # torch reports an arbitrary row stride for a single row
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _call(device, fn, *args):
+    """fn(*args, current stream of the device), with the device current"""
+    stream = torch._C._cuda_getCurrentRawStream(device)
+    if torch._C._cuda_getDevice() == device:
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, stream)
+    if status:
+        raise EquarxError(status, fn.__name__)
 
 
-def _stream(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
-
-
-def _workspace(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
-def _on(t):
-    """The library launches on the current device: make it the tensor's own."""
-    return torch.cuda.device(t.device)
+def _workspace(like, nbytes):
+    """(tensor to keep until the call has been enqueued, its address)"""
+    if not nbytes:
+        return None, 0
+    ws = like.new_empty(nbytes, dtype=torch.uint8)
+    return ws, ws.data_ptr()
 
 
 def fp4_quantize(x, format=FP4_NV):
     """x [rows, cols], bfloat16, float16 or float32 -> Fp4Matrix."""
-    _matrix(x, "x")
-    rows, cols = x.shape
-    codes = torch.empty((rows, -(-cols // 32) * 16), dtype=torch.uint8, device=x.device)
-    scales = torch.empty(binding.fp4_scales_bytes(rows, cols, format), dtype=torch.uint8, device=x.device)
-    row_scales = torch.empty(rows, dtype=torch.float32, device=x.device) if format == FP4_NV else None
-    with _on(x):
-        binding.fp4_quantize(x, _DTYPES[x.dtype], rows, cols, _ld(x), format, codes, scales, row_scales, _stream(x))
-    return Fp4Matrix(codes, scales, row_scales, rows, cols, format)
+    rows, cols, ld, dev = _matrix(x, "x")
+    q = Fp4Matrix(x.new_empty(Fp4Matrix.nbytes(rows, cols, format), dtype=torch.uint8), rows, cols, format)
+    _call(dev, _lib.equarx_fp4_quantize, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, format, *q._parts)
+    return q
 
 
 def fp4_dequantize(q, dtype=torch.bfloat16):
     """The values that q's codes stand for, rounded once to dtype."""
-    out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.codes.device)
-    with _on(out):
-        binding.fp4_dequantize(q.codes, q.scales, q.row_scales, q.rows, q.cols, q.format, out, _DTYPES[dtype], q.cols,
-                               _stream(out))
+    out = q.data.new_empty((q.rows, q.cols), dtype=dtype)
+    _call(out.get_device(), _lib.equarx_fp4_dequantize, *q._parts, q.rows, q.cols, q.format, out.data_ptr(), _DTYPES[dtype],
+          q.cols)
     return out
 
 
@@ -88,78 +132,79 @@ def fp4_matmul(a, b, dtype=torch.bfloat16):
     """a b^T of two Fp4Matrix of one format: [a.rows, b.rows]."""
     if a.cols != b.cols or a.format != b.format:
         raise ValueError("the operands differ in columns or format")
-    out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.codes.device)
-    with _on(out):
-        binding.fp4_matmul(a.codes, a.scales, a.row_scales, b.codes, b.scales, b.row_scales, a.rows, b.rows, a.cols, a.format,
-                           out, _DTYPES[dtype], b.rows, _stream(out))
+    out = a.data.new_empty((a.rows, b.rows), dtype=dtype)
+    dev = out.get_device()
+    if b.data.get_device() != dev:
+        raise ValueError("the operands are on different devices")
+    _call(dev, _lib.equarx_fp4_matmul, *a._parts, *b._parts, a.rows, b.rows, a.cols, a.format, out.data_ptr(), _DTYPES[dtype],
+          b.rows)
     return out
 
 
 def fp4_linear(x, w):
     """x w^T: x [tokens, k] in 16 bits is quantized in the call, w is an Fp4Matrix [n, k]."""
-    _matrix(x, "x", cols=w.cols)
-    m = x.shape[0]
-    out = torch.empty((m, w.rows), dtype=x.dtype, device=x.device)
-    nbytes = binding.fp4_linear_workspace_bytes(m, w.cols, w.format)
-    ws = _workspace(nbytes, x.device)
-    with _on(x):
-        binding.fp4_linear(x, _DTYPES[x.dtype], _ld(x), w.codes, w.scales, w.row_scales, m, w.rows, w.cols, w.format, out,
-                           w.rows, ws, nbytes, _stream(x))
+    m, k, ld, dev = _matrix(x, "x", None, w.cols, None, w.data.get_device())
+    out = x.new_empty((m, w.rows))
+    nbytes = _linear_workspace(m, k, w.format)
+    ws, ptr = _workspace(x, nbytes)
+    _call(dev, _lib.equarx_fp4_linear, x.data_ptr(), _DTYPES[x.dtype], ld, *w._parts, m, w.rows, k, w.format, out.data_ptr(),
+          w.rows, ptr, nbytes)
     return out
 
 
 def fp4_gated(x, wg, wu, act=ACT_GELU_TANH):
     """act(x wg^T) * (x wu^T): x [tokens, k] in 16 bits, wg and wu Fp4Matrix [f, k] of one format."""
-    if (wg.rows, wg.cols, wg.format) != (wu.rows, wu.cols, wu.format):
+    if wg.rows != wu.rows or wg.cols != wu.cols or wg.format != wu.format:
         raise ValueError("the two weights differ in shape or format")
-    _matrix(x, "x", cols=wg.cols)
-    m = x.shape[0]
-    h = torch.empty((m, wg.rows), dtype=x.dtype, device=x.device)
-    nbytes = binding.fp4_linear_workspace_bytes(m, wg.cols, wg.format)
-    ws = _workspace(nbytes, x.device)
-    with _on(x):
-        binding.fp4_gated(x, _DTYPES[x.dtype], _ld(x), wg.codes, wg.scales, wg.row_scales, wu.codes, wu.scales, wu.row_scales,
-                          m, wg.rows, wg.cols, wg.format, act, h, wg.rows, ws, nbytes, _stream(x))
+    m, k, ld, dev = _matrix(x, "x", None, wg.cols, None, wg.data.get_device())
+    if wu.data.get_device() != dev:
+        raise ValueError("the two weights are on different devices")
+    h = x.new_empty((m, wg.rows))
+    nbytes = _linear_workspace(m, k, wg.format)
+    ws, ptr = _workspace(x, nbytes)
+    _call(dev, _lib.equarx_fp4_gated, x.data_ptr(), _DTYPES[x.dtype], ld, *wg._parts, *wu._parts, m, wg.rows, k, wg.format,
+          act, h.data_ptr(), wg.rows, ptr, nbytes)
     return h
 
 
 def gated_forward(x, wg, wu, act=ACT_GELU_TANH, save=False):
     """h = act(x wg^T) * (x wu^T) for x [tokens, k], wg and wu [f, k], all bfloat16 or all float16.
-    With save: (h, g, u), where g and u are the two projections that gated_backward needs."""
-    _matrix(x, "x")
-    m, k = x.shape
-    f = wg.shape[0]
-    _matrix(wg, "wg", f, k, x.dtype)
-    _matrix(wu, "wu", f, k, x.dtype)
-    h = torch.empty((m, f), dtype=x.dtype, device=x.device)
-    g, u = (torch.empty_like(h), torch.empty_like(h)) if save else (None, None)
-    ldx, ldwg, ldwu = _ld(x), _ld(wg), _ld(wu)
-    nbytes = binding.gated_forward_workspace_bytes(m, f, k, ldx, ldwg, ldwu)
-    ws = _workspace(nbytes, x.device)
-    with _on(x):
-        binding.gated_forward(x, ldx, wg, ldwg, wu, ldwu, _DTYPES[x.dtype], m, f, k, act, h, f, g, u, f, ws, nbytes,
-                              _stream(x))
-    return (h, g, u) if save else h
+    With save: (h, g, u), where g and u are the two projections that gated_backward needs (the two halves
+    of one allocation)."""
+    m, k, ldx, dev = _matrix(x, "x")
+    f, _, ldg, _ = _matrix(wg, "wg", None, k, x.dtype, dev)
+    _, _, ldu, _ = _matrix(wu, "wu", f, k, x.dtype, dev)
+    h = x.new_empty((m, f))
+    gu, gp, up = None, 0, 0
+    if save:
+        half = _up(m * f, 8)                 # the second half starts on a multiple of 16 bytes
+        gu = x.new_empty(2 * half)
+        gp = gu.data_ptr()
+        up = gp + 2 * half
+    nbytes = _forward_workspace(m, f, k, ldx, ldg, ldu)
+    ws, ptr = _workspace(x, nbytes)
+    _call(dev, _lib.equarx_gated_forward, x.data_ptr(), ldx, wg.data_ptr(), ldg, wu.data_ptr(), ldu, _DTYPES[x.dtype], m, f, k,
+          act, h.data_ptr(), f, gp, up, f, ptr, nbytes)
+    if not save:
+        return h
+    return h, gu.as_strided((m, f), (f, 1), 0), gu.as_strided((m, f), (f, 1), half)
 
 
 def gated_backward(dh, x, wg, wu, g, u, act=ACT_GELU_TANH):
     """(dx, dwg, dwu) of gated_forward from dh [tokens, f] and the g and u it saved."""
-    _matrix(x, "x")
-    m, k = x.shape
-    f = wg.shape[0]
-    for t, what, rows, cols in ((wg, "wg", f, k), (wu, "wu", f, k), (dh, "dh", m, f), (g, "g", m, f), (u, "u", m, f)):
-        _matrix(t, what, rows, cols, x.dtype)
-    ldgu = _ld(g)
-    if _ld(u) != ldgu:
+    m, k, ldx, dev = _matrix(x, "x")
+    f, _, ldwg, _ = _matrix(wg, "wg", None, k, x.dtype, dev)
+    _, _, ldwu, _ = _matrix(wu, "wu", f, k, x.dtype, dev)
+    _, _, lddh, _ = _matrix(dh, "dh", m, f, x.dtype, dev)
+    _, _, ldgu, _ = _matrix(g, "g", m, f, x.dtype, dev)
+    if _matrix(u, "u", m, f, x.dtype, dev)[2] != ldgu:
         raise ValueError("g and u have different row strides")
-    dx = torch.empty((m, k), dtype=x.dtype, device=x.device)
-    dwg, dwu = torch.empty((f, k), dtype=x.dtype, device=x.device), torch.empty((f, k), dtype=x.dtype, device=x.device)
-    ldx, ldwg, ldwu = _ld(x), _ld(wg), _ld(wu)
-    nbytes = binding.gated_backward_workspace_bytes(m, f, k, ldx, ldwg, ldwu)
-    ws = _workspace(nbytes, x.device)
-    with _on(x):
-        binding.gated_backward(dh, _ld(dh), x, ldx, wg, ldwg, wu, ldwu, g, u, ldgu, _DTYPES[x.dtype], m, f, k, act, dx, k,
-                               dwg, k, dwu, k, ws, nbytes, _stream(x))
+    dx, dwg, dwu = x.new_empty((m, k)), x.new_empty((f, k)), x.new_empty((f, k))
+    nbytes = _backward_workspace(m, f, k, ldx, ldwg, ldwu)
+    ws, ptr = _workspace(x, nbytes)
+    _call(dev, _lib.equarx_gated_backward, dh.data_ptr(), lddh, x.data_ptr(), ldx, wg.data_ptr(), ldwg, wu.data_ptr(), ldwu,
+          g.data_ptr(), u.data_ptr(), ldgu, _DTYPES[x.dtype], m, f, k, act, dx.data_ptr(), k, dwg.data_ptr(), k, dwu.data_ptr(),
+          k, ptr, nbytes)
     return dx, dwg, dwu
 
 
