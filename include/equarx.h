@@ -489,6 +489,7 @@ int equarx_fp4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const flo
 /*
  * out = x w^T, x (m x k, BF16 or FP16) quantized by this call, w (n x k) before:
  * exactly equarx_fp4_quantize followed by equarx_fp4_matmul.  out has x's type.
+ * For a few tokens the product quantizes x itself and the workspace is 0 bytes.
  */
 size_t equarx_fp4_linear_workspace_bytes(size_t m, size_t k, int format);
 int equarx_fp4_linear(const void *x, int dtype, size_t ldx,

@@ -14,6 +14,7 @@ using namespace equarx::ff;
 
 constexpr size_t kMaxDim = size_t(1) << 30;
 constexpr size_t kBigSmem = 227 * 1024;
+constexpr size_t kSplitSmem = 224 * 1024;      // dynamic; the kernel's own variables need a few hundred bytes more
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
@@ -67,6 +68,44 @@ int current_device(int& sms) {
         if (e != cudaSuccess) return cuda_failure(e);
     }
     sms = counts[dev];
+    return EQUARX_OK;
+}
+
+// Clusters of 1 .. 8 CTAs that run at one time when each CTA has an SM to itself: a cluster stays inside a
+// GPC, so this is less than the number of SMs divided by the size.
+int resident_clusters(const void* kernel, int (&out)[9]) {
+    struct Entry {
+        int dev, clusters[9];
+    };
+    static std::mutex mu;
+    static std::vector<Entry> seen;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_failure(e);
+    std::lock_guard<std::mutex> lock(mu);
+    for (const Entry& en : seen)
+        if (en.dev == dev) {
+            std::copy(en.clusters, en.clusters + 9, out);
+            return EQUARX_OK;
+        }
+    Entry en = {};
+    en.dev = dev;
+    for (int size = 1; size <= 8; ++size) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(size * 148);
+        cfg.blockDim = dim3(kSplitThreads);
+        cfg.dynamicSmemBytes = kSplitSmem;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = size;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&en.clusters[size], kernel, &cfg);
+        if (e != cudaSuccess) return cuda_failure(e);
+    }
+    seen.push_back(en);
+    std::copy(en.clusters, en.clusters + 9, out);
     return EQUARX_OK;
 }
 
@@ -192,31 +231,48 @@ inline Span rows_span(const Fp4& q, size_t rows, int format) {
     return Span{format == EQUARX_FP4_NV ? q.row_scales : nullptr, rows * sizeof(float)};
 }
 
+// threads of a row's CTA: three groups of 16 elements each, a whole number of warps
+inline int row_threads(size_t cols) { return int(std::min<size_t>(512, up(ceil_div(cols, 16 * kRowChunks), 32))); }
+
 template <bool MX>
-int launch_quantize(const QuantArgs& a, int sms, cudaStream_t stream) {
-    // A warp for each row once that gives every SM eight of them; below, a CTA for each row.
-    if (a.rows >= 8 * sms) return launch(fp4_quantize_kernel<MX, 1>, dim3(ceil_div(a.rows, 8)), 256, 0, 1, a, stream);
-    return launch(fp4_quantize_kernel<MX, 8>, dim3(a.rows), 256, 0, 1, a, stream);
+int launch_quantize(const QuantArgs& a, cudaStream_t stream) {
+    const dim3 grid(a.rows);
+    const int threads = row_threads(a.cols);
+    if (a.dtype == EQUARX_BF16) return launch(fp4_quantize_kernel<MX, kBf16>, grid, threads, 0, 1, a, stream);
+    if (a.dtype == EQUARX_FP16) return launch(fp4_quantize_kernel<MX, kFp16>, grid, threads, 0, 1, a, stream);
+    return launch(fp4_quantize_kernel<MX, kFp32>, grid, threads, 0, 1, a, stream);
 }
-int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int format, const Fp4& q, cudaStream_t stream) {
-    int sms;
-    TRY(current_device(sms));
+QuantArgs rows_to_quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld) {
     QuantArgs a = {};
     a.x = x;
-    a.codes = const_cast<uint8_t*>(q.codes);
-    a.scales = const_cast<uint8_t*>(q.scales);
-    a.row_scales = const_cast<float*>(q.row_scales);
     a.ld = ld;
     a.rows = int(rows);
     a.cols = int(cols);
     a.dtype = dtype;
-    a.vec = aligned(x, 16) && ld * size_of(dtype) % 16 == 0;
-    return format == EQUARX_FP4_MX ? launch_quantize<true>(a, sms, stream) : launch_quantize<false>(a, sms, stream);
+    a.vec = ld * size_of(dtype) % 16 == 0;
+    return a;
+}
+int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int format, const Fp4& q, cudaStream_t stream) {
+    QuantArgs a = rows_to_quantize(x, dtype, rows, cols, ld);
+    a.codes = const_cast<uint8_t*>(q.codes);
+    a.scales = const_cast<uint8_t*>(q.scales);
+    a.row_scales = const_cast<float*>(q.row_scales);
+    return format == EQUARX_FP4_MX ? launch_quantize<true>(a, stream) : launch_quantize<false>(a, stream);
 }
 
 // ---------------------------------------------------------------- launches of the products
-// Tokens up to which the transposed kernel is used.
-constexpr size_t kFewTokens = 128;
+// Tokens up to which the transposed kernel is used.  Measured on both sides (us, transposed / 256-row tiles):
+// 4-bit gated, 5376 -> 2688: 32 tokens 13.2 / 18.2, 64 tokens 17.1 / 18.5, 128 tokens 25.6 / 18.6;
+// 4-bit product, 2688 -> 5376: 32 tokens 16.1 / 13.5, 64 tokens 20.9 / 13.8;
+// 16-bit gated, 5376 -> 2688: 64 tokens 20.8 / 24.9, 128 tokens 37.8 / 24.9;
+// gradients, 5376 -> 2688 (all of the call): 64 tokens 43 / 48, 128 tokens 51 / 50; 2688 -> 5376: 49 / 63.
+constexpr size_t kFewTokensFp4 = 32, kFewTokensGated = 64, kFewTokensGradient = 128;
+// Tokens up to which a product quantizes its own activations.  It saves a launch on the host (13 -> 9 us for
+// the whole call), and on the GPU, warm, 5376 -> 2688, fused / two launches (us): MX 1 token 4.8 / 5.5,
+// 8 tokens 5.7 / 5.8, 16 tokens 7.8 / 5.9; NV, whose rows' maxima go round the cluster first, 1 token
+// 6.9 / 6.8, 2 tokens 7.0 / 6.8, 4 tokens 7.8 / 6.8.
+constexpr size_t kFusedMxTokens = 8, kFusedNvTokens = 2;
+static_assert(kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, "the fused form takes one tile of tokens");
 
 // Columns of a tile.  The pairs of SMs work through whole rounds of tiles, so the time goes with rounds *
 // (bn + a share for starting and ending a tile); a narrower tile may save a round, or give every pair
@@ -251,43 +307,57 @@ int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
                   kTileSmem<KIND>, 1, a, stream);
 }
 
-template <int KIND, int MODE, bool W_MN>
+template <int KIND, int MODE, bool W_MN, bool FUSED = false>
 int launch_split(SplitArgs& a, size_t features, size_t tokens, cudaStream_t stream) {
-    int sms;
-    TRY(current_device(sms));
     a.features = int(features);
     a.tokens = int(tokens);
     const size_t tiles = ceil_div(features, kRowsM) * ceil_div(tokens, a.nt);
     const int total = a.stages * (MODE == kSum2 ? 2 : 1);
-    // as many parts of the reduction axis as fill the SMs: at most 8, the portable cluster size
-    const int ranks = int(std::max<size_t>(1, std::min<size_t>({8, size_t(total), size_t(sms) / tiles})));
-    const int stage = split_stage_bytes<KIND, MODE>(a.nt);
-    const int partial = (MODE == kGated ? 2 : 1) * a.nt * 128 * 4;
-    a.pipe = std::min({kSplitMaxPipe, int(ceil_div(total, ranks)), (200 * 1024) / stage});
-    const size_t smem = std::max(a.pipe * stage, partial) + kSmemSlack;
+    // The reduction axis is split over as many CTAs as run at one time for all tiles: at most 8, the
+    // portable cluster size.  (5376 -> 2688 gated in 16 bits, one token: 21 tiles of 7 CTAs would take two
+    // rounds, 23 us; of 6, one, 14 us.)
+    const auto kernel = split_kernel<KIND, MODE, W_MN, FUSED>;
+    if (const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel))) return cuda_failure(e);
+    int clusters[9];
+    TRY(resident_clusters(reinterpret_cast<const void*>(kernel), clusters));
+    int ranks = 1;
+    for (int size = 2; size <= std::min(8, total); ++size)
+        if (size_t(clusters[size]) >= tiles) ranks = size;
+    const int stage = split_stage_bytes<KIND, MODE>(a.nt), parts = split_part_bytes<MODE>(a.nt, ranks);
+    a.pipe = std::min({kSplitMaxPipe, int(ceil_div(total, ranks)), (int(kSplitSmem) - kSmemSlack - parts) / stage});
+    const int columns = (MODE == kGated ? 2 : 1) * (a.nt + 4 * kScaleTiles<KIND>) + 4 * kScaleTiles<KIND>;
+    for (a.columns = 32; a.columns < columns;) a.columns *= 2;
+    const size_t smem = size_t(a.pipe) * stage + parts + kSmemSlack;
     const dim3 grid(ranks, unsigned(ceil_div(features, kRowsM)), unsigned(ceil_div(tokens, a.nt)));
-    return launch(split_kernel<KIND, MODE, W_MN>, grid, kSplitThreads, smem, ranks, a, stream);
+    return launch(kernel, grid, kSplitThreads, smem, ranks, a, stream);
 }
 
 inline int token_tile(size_t tokens) { return int(std::min<size_t>(128, up(tokens, 16))); }
 
+// weights of the transposed kernel
+template <int KIND, int MODE>
+int split_weights(SplitArgs& a, const Fp4* w, size_t n, size_t k) {
+    const size_t stride = codes_stride(k);
+    for (int i = 0; i < (MODE == kGated ? 2 : 1); ++i) {
+        TRY(make_map(a.w[i], w[i].codes, 1, stride, n, stride, kRowsM));
+        a.scales_w[i] = w[i].scales;
+        a.row_w[i] = w[i].row_scales;
+    }
+    a.stages = int(fp4_stages(k));
+    return EQUARX_OK;
+}
+
 template <int KIND, int MODE>
 int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, cudaStream_t stream) {
     const size_t stride = codes_stride(k);
-    constexpr int NW = MODE == kGated ? 2 : 1;
-    if (m <= kFewTokens) {
+    if (m <= kFewTokensFp4) {
         SplitArgs a = {};
         a.nt = token_tile(m);
-        for (int i = 0; i < NW; ++i) {
-            TRY(make_map(a.w[i], w[i].codes, 1, stride, n, stride, kRowsM));
-            a.scales_w[i] = w[i].scales;
-            a.row_w[i] = w[i].row_scales;
-        }
+        TRY((split_weights<KIND, MODE>(a, w, n, k)));
         TRY(make_map(a.x[0], x.codes, 1, stride, m, stride, a.nt));
         a.scales_x = x.scales;
         a.row_x = x.row_scales;
         a.out[0] = out;
-        a.stages = int(fp4_stages(k));
         a.act = act;
         return launch_split<KIND, MODE, false>(a, n, m, stream);
     }
@@ -295,14 +365,15 @@ int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int ac
     int sms;
     TRY(current_device(sms));
     a.bn = tile_width(m, n, 1, MODE == kGated, true, sms);
+    const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
     TRY(make_map(a.a[0], x.codes, 1, stride, m, stride, kRowsM));
-    for (int i = 0; i < NW; ++i) {
+    TRY(scale_map(a.scales_a, x.scales, m, k, format));
+    a.row_a = x.row_scales;
+    for (int i = 0; i < (MODE == kGated ? 2 : 1); ++i) {
         TRY(make_map(a.b[i], w[i].codes, 1, stride, n, stride, a.bn / 2));
-        TRY(scale_map(a.scales_b[i], w[i].scales, n, k, KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV));
+        TRY(scale_map(a.scales_b[i], w[i].scales, n, k, format));
         a.row_b[i] = w[i].row_scales;
     }
-    TRY(scale_map(a.scales_a, x.scales, m, k, KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV));
-    a.row_a = x.row_scales;
     a.out[0] = out;
     a.stages = int(fp4_stages(k));
     a.act = act;
@@ -322,6 +393,31 @@ Fp4 carve(void* ws, size_t rows, size_t cols, int format) {
 }
 inline size_t carved_bytes(size_t rows, size_t cols, int format) {
     return up(scales_bytes(rows, cols, format), 256) + up(rows * sizeof(float), 256) + up(rows * codes_stride(cols), 256);
+}
+
+inline bool quantizes_itself(size_t m, int format) { return m <= (format == EQUARX_FP4_MX ? kFusedMxTokens : kFusedNvTokens); }
+
+inline size_t product_workspace(size_t m, size_t k, int format) {
+    return quantizes_itself(m, format) ? 0 : carved_bytes(m, k, format);
+}
+
+// x (16 bits) quantized and multiplied with one or two weights
+template <int KIND, int MODE>
+int quantized_product(const QuantArgs& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, void* workspace,
+                      cudaStream_t stream) {
+    const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
+    if (quantizes_itself(m, format)) {
+        SplitArgs a = {};
+        a.nt = kFusedTokens;
+        TRY((split_weights<KIND, MODE>(a, w, n, k)));
+        a.raw = x;
+        a.out[0] = out;
+        a.act = act;
+        return launch_split<KIND, MODE, false, true>(a, n, m, stream);
+    }
+    const Fp4 q = carve(workspace, m, k, format);
+    TRY(quantize(x.x, x.dtype, m, k, x.ld, format, q, stream));
+    return fp4_product<KIND, MODE>(q, w, m, n, k, act, out, stream);
 }
 
 // ---------------------------------------------------------------- 16-bit operands
@@ -392,8 +488,6 @@ int equarx_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, const flo
     if (!aligned(out, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({codes_span(q, rows, cols), scales_span(q, rows, cols, format), rows_span(q, rows, format)},
                       {matrix(out, rows, cols, ld, size_of(dtype))}));
-    int sms;
-    TRY(current_device(sms));
     DequantArgs a = {};
     a.codes = codes;
     a.scales = scales;
@@ -404,10 +498,10 @@ int equarx_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, const flo
     a.cols = int(cols);
     a.dtype = dtype;
     a.vec = ld * size_of(dtype) % 16 == 0;
-    const size_t groups = rows * ceil_div(cols, 16);
-    const dim3 grid(unsigned(std::min<size_t>(ceil_div(groups, 256), size_t(sms) * 8)));
-    return format == EQUARX_FP4_MX ? launch(fp4_dequantize_kernel<true>, grid, 256, 0, 1, a, stream)
-                                   : launch(fp4_dequantize_kernel<false>, grid, 256, 0, 1, a, stream);
+    const dim3 grid{unsigned(rows)};
+    const int threads = row_threads(cols);
+    return format == EQUARX_FP4_MX ? launch(fp4_dequantize_kernel<true>, grid, threads, 0, 1, a, stream)
+                                   : launch(fp4_dequantize_kernel<false>, grid, threads, 0, 1, a, stream);
 }
 
 int equarx_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_row_scales, const uint8_t* b_codes,
@@ -430,7 +524,7 @@ int equarx_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const flo
 }
 
 size_t equarx_fp4_linear_workspace_bytes(size_t m, size_t k, int format) {
-    return m > kMaxDim || bad_dim(k) || !is_format(format) ? 0 : carved_bytes(m, k, format);
+    return m > kMaxDim || bad_dim(k) || !is_format(format) ? 0 : product_workspace(m, k, format);
 }
 
 int equarx_fp4_linear(const void* x, int dtype, size_t ldx, const uint8_t* w_codes, const uint8_t* w_scales,
@@ -440,17 +534,17 @@ int equarx_fp4_linear(const void* x, int dtype, size_t ldx, const uint8_t* w_cod
     if (m > kMaxDim || bad_dim(n) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ld, n)) return EQUARX_ERR_COUNT;
     if (m == 0) return EQUARX_OK;
     const Fp4 w{w_codes, w_scales, w_row_scales};
-    if (!x || !out || !workspace) return EQUARX_ERR_NULL;
+    const size_t need = product_workspace(m, k, format);
+    if (!x || !out || (need && !workspace)) return EQUARX_ERR_NULL;
     TRY(check_fp4(w, format));
-    if (workspace_bytes < carved_bytes(m, k, format)) return EQUARX_ERR_WORKSPACE;
+    if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
     if (!aligned(x, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(x, m, k, ldx, 2), codes_span(w, n, k), scales_span(w, n, k, format), rows_span(w, n, format)},
-                      {matrix(out, m, n, ld, 2), Span{workspace, workspace_bytes}}));
-    const Fp4 q = carve(workspace, m, k, format);
-    TRY(quantize(x, dtype, m, k, ldx, format, q, stream));
+                      {matrix(out, m, n, ld, 2), Span{workspace, need}}));
+    const QuantArgs a = rows_to_quantize(x, dtype, m, k, ldx);
     const Out o = out_rows(out, ld, dtype);
-    return format == EQUARX_FP4_MX ? fp4_product<kMx, kPlain>(q, &w, m, n, k, 0, o, stream)
-                                   : fp4_product<kNv, kPlain>(q, &w, m, n, k, 0, o, stream);
+    return format == EQUARX_FP4_MX ? quantized_product<kMx, kPlain>(a, &w, m, n, k, 0, o, workspace, stream)
+                                   : quantized_product<kNv, kPlain>(a, &w, m, n, k, 0, o, workspace, stream);
 }
 
 int equarx_fp4_gated(const void* x, int dtype, size_t ldx, const uint8_t* g_codes, const uint8_t* g_scales,
@@ -461,20 +555,20 @@ int equarx_fp4_gated(const void* x, int dtype, size_t ldx, const uint8_t* g_code
     if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldh, f)) return EQUARX_ERR_COUNT;
     if (m == 0) return EQUARX_OK;
     const Fp4 w[2] = {{g_codes, g_scales, g_row_scales}, {u_codes, u_scales, u_row_scales}};
-    if (!x || !h || !workspace) return EQUARX_ERR_NULL;
+    const size_t need = product_workspace(m, k, format);
+    if (!x || !h || (need && !workspace)) return EQUARX_ERR_NULL;
     TRY(check_fp4(w[0], format));
     TRY(check_fp4(w[1], format));
-    if (workspace_bytes < carved_bytes(m, k, format)) return EQUARX_ERR_WORKSPACE;
+    if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
     if (!aligned(x, 16) || !aligned(h, 16) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(x, m, k, ldx, 2), codes_span(w[0], f, k), scales_span(w[0], f, k, format),
                        rows_span(w[0], f, format), codes_span(w[1], f, k), scales_span(w[1], f, k, format),
                        rows_span(w[1], f, format)},
-                      {matrix(h, m, f, ldh, 2), Span{workspace, workspace_bytes}}));
-    const Fp4 q = carve(workspace, m, k, format);
-    TRY(quantize(x, dtype, m, k, ldx, format, q, stream));
+                      {matrix(h, m, f, ldh, 2), Span{workspace, need}}));
+    const QuantArgs a = rows_to_quantize(x, dtype, m, k, ldx);
     const Out o = out_rows(h, ldh, dtype);
-    return format == EQUARX_FP4_MX ? fp4_product<kMx, kGated>(q, w, m, f, k, act, o, stream)
-                                   : fp4_product<kNv, kGated>(q, w, m, f, k, act, o, stream);
+    return format == EQUARX_FP4_MX ? quantized_product<kMx, kGated>(a, w, m, f, k, act, o, workspace, stream)
+                                   : quantized_product<kNv, kGated>(a, w, m, f, k, act, o, workspace, stream);
 }
 
 size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu) {
@@ -507,7 +601,7 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     TRY(readable(ou, f, k, ws, stream));
     const Out oh = out_rows(h, ldh, dtype), sg = out_rows(g, ldgu, dtype), su = out_rows(u, ldgu, dtype);
     const int stages = int(ceil_div(k, 64));
-    if (m <= kFewTokens) {
+    if (m <= kFewTokensGated) {
         SplitArgs a = {};
         a.nt = token_tile(m);
         TRY(map16(a.w[0], og, f, k, kRowsM));
@@ -597,7 +691,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
                stream));
 
     // dx = dG Wg + dU Wu: the reduction runs over f, twice
-    if (m <= kFewTokens) {
+    if (m <= kFewTokensGradient) {
         SplitArgs a = {};
         a.nt = token_tile(m);
         TRY(map16(a.w[0], og, f, k, 64));

@@ -444,196 +444,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
     }
 }
 
-// ---------------------------------------------------------------- few tokens
-struct SplitArgs {
-    CUtensorMap w[2], x[2];
-    const uint8_t* scales_w[2];
-    const uint8_t* scales_x;
-    const float* row_w[2];
-    const float* row_x;
-    Out out[3];
-    int features, tokens;             // rows of w, rows of x
-    int stages;                       // stages of the reduction axis (of each part of kSum2)
-    int nt;                           // tokens of a tile: a multiple of 16, at most 128
-    int pipe;                         // stages in shared memory
-    int act, bf16, save;
-};
-constexpr int kSplitThreads = 192, kSplitMaxPipe = 12;
-template <int KIND, int MODE>
-__host__ __device__ constexpr int split_stage_bytes(int nt) {
-    return (MODE == kGated ? 2 : 1) * (kTileBytes + kScaleBytes<KIND>) + nt * kRowBytes + kScaleBytes<KIND>;
-}
-
-// The output transposed: 128 features x nt tokens, so that a single token costs one narrow product over
-// each weight tile instead of a 128-row one, and the weights, which are all the bytes there are, are
-// read once.  The reduction axis is split over the CTAs of a cluster (cluster dimension x) because
-// features / 128 tiles alone would leave most SMs without work; the parts are added through distributed
-// shared memory, in rank order, so the sum does not depend on timing.
-template <int KIND, int MODE, bool W_MN>
-__global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_constant__ SplitArgs p) {
-    constexpr bool FP4 = KIND != kHalf;
-    constexpr int SB = kScaleBytes<KIND>, NW = MODE == kGated ? 2 : 1;
-    constexpr uint32_t kScaleCol = 256;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * kSplitMaxPipe + 2];
-    __shared__ uint32_t tmem_slot;
-    __shared__ volatile uint32_t abort;
-
-    const uint32_t pad = (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u;
-    const uint32_t smem = smem_addr(smem_raw) + pad;
-    float* const part = reinterpret_cast<float*>(smem_raw + pad);          // [NW * nt][128], after the products
-    const uint32_t full = smem_addr(bars), empty = full + 8 * kSplitMaxPipe, ready = empty + 8 * kSplitMaxPipe,
-                   drain = ready + 8;
-    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const uint32_t xb = p.nt * kRowBytes, STAGE = NW * (kTileBytes + SB) + xb + SB;
-
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < p.pipe; ++i) {
-            barrier_init(full + 8 * i, 1);
-            barrier_init(empty + 8 * i, 1);
-        }
-        barrier_init(ready, 1);
-        barrier_init(drain, 1);
-        abort = 0;
-        fence_barrier_init();
-    }
-    if (warp == 5) tmem_alloc<1>(smem_addr(&tmem_slot), 512);
-    fence_before();
-    __syncthreads();
-    fence_after();
-    const uint32_t tmem = uniform(tmem_slot);
-
-    const int ranks = gridDim.x, rank = uniform(cluster_rank());
-    const int total = p.stages * (MODE == kSum2 ? 2 : 1);
-    const int s0 = int(int64_t(total) * rank / ranks), s1 = int(int64_t(total) * (rank + 1) / ranks);
-    const int f0 = blockIdx.y * kRowsM, t0 = blockIdx.z * p.nt;
-    grid_launch();
-    grid_wait();
-
-    if (warp == 4) {
-        {
-            bool ok = true;
-            int it = 0;
-            for (int s = s0; s < s1; ++s, ++it) {
-                const int slot = it % p.pipe;
-                if (!(ok = barrier_wait_warp(empty + 8 * slot, (it / p.pipe & 1) ^ 1, &abort))) break;
-                const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb, bar = full + 8 * slot;
-                const int second = MODE == kSum2 ? s >= p.stages : 0, ks = s - second * p.stages;
-                const int kc = FP4 ? ks * kRowBytes : ks * 64;
-                barrier_expect_warp(bar, NW * kTileBytes + xb + (FP4 ? (NW + 1) * SB : 0));
-                for (int q = 0; q < NW; ++q) {
-                    const CUtensorMap* mw = &p.w[MODE == kSum2 ? second : q];
-                    if (W_MN) {
-                        tma_load_2d(sw, mw, f0, kc, bar);
-                        tma_load_2d(sw + kChunkBytes, mw, f0 + 64, kc, bar);
-                    } else {
-                        tma_load_2d(sw + q * kTileBytes, mw, kc, f0, bar);
-                    }
-                    if (FP4) bulk_load(ss + SB * q, p.scales_w[q] + (size_t(f0 / 128) * p.stages + ks) * SB, SB, bar);
-                }
-                tma_load_2d(sx, &p.x[second], kc, t0, bar);
-                if (FP4) bulk_load(ss + SB * NW, p.scales_x + (size_t(t0 / 128) * p.stages + ks) * SB, SB, bar);
-            }
-            if (abort)
-                for (int i = it > p.pipe ? it - p.pipe : 0; i < it; ++i) barrier_drain(full + 8 * (i % p.pipe), i / p.pipe & 1);
-        }
-        __syncwarp();
-    } else if (warp == 5) {
-        {
-            const uint32_t tw = tmem + kScaleCol, tx = tw + NW * 4 * kScaleTiles<KIND>;
-            bool ok = true;
-            int it = 0;
-            for (int s = s0; s < s1; ++s, ++it) {
-                const int slot = it % p.pipe;
-                if (!(ok = barrier_wait_warp(full + 8 * slot, it / p.pipe & 1, &abort))) break;
-                fence_after();
-                const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb;
-                if (FP4) {
-#pragma unroll
-                    for (int j = 0; j < kScaleTiles<KIND>; ++j) {
-#pragma unroll
-                        for (int q = 0; q < NW; ++q)
-                            copy_scales<1>(tw + (q * kScaleTiles<KIND> + j) * 4, ss + SB * q + 512 * j);
-                        copy_scales<1>(tx + 4 * j, ss + SB * NW + 512 * j);
-                    }
-                }
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    const uint32_t dx = swizzled_desc(sx + 32 * kk, 16);
-#pragma unroll
-                    for (int q = 0; q < NW; ++q) {
-                        const uint32_t a = sw + q * kTileBytes;
-                        const uint32_t dw = W_MN ? swizzled_desc(a + 2048 * kk, kChunkBytes)
-                                                 : swizzled_desc(a + 32 * kk, 16);
-                        if constexpr (FP4) {
-                            const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
-                            mma_fp4<1, KIND == kMx>(tmem + q * p.nt, dw, dx, desc_fp4(KIND == kMx, 128, p.nt, which),
-                                                 tw + (q * kScaleTiles<KIND> + j) * 4, tx + 4 * j, it | kk);
-                        } else {
-                            mma_16bit<1>(tmem + q * p.nt, dw, dx, desc_16bit(p.bf16, W_MN, false, 128, p.nt), it | kk);
-                        }
-                    }
-                }
-                mma_commit<1>(empty + 8 * slot);
-            }
-            if (ok) mma_commit<1>(ready);
-            if (abort) {
-                mma_commit<1>(drain);
-                barrier_drain(drain, 0);
-            }
-        }
-        __syncwarp();
-    } else {
-        if (barrier_wait(ready, 0, &abort)) {
-            __syncwarp();
-            fence_after();
-            // every load has landed and every product has read it: the stages now hold the partial sums
-            for (int c = 0; c < NW * p.nt; c += 16) {
-                uint32_t r[16];
-                tmem_load16(tmem + c + (uint32_t(warp * 32) << 16), r);
-                tmem_wait_loads();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) part[(c + j) * 128 + warp * 32 + lane] = __uint_as_float(r[j]);
-            }
-        }
-    }
-    fence_before();
-    __syncthreads();
-    if (warp == 5) {
-        fence_after();
-        tmem_free<1>(tmem, 512);
-    }
-    cluster_sync();
-
-    const int count = min(p.nt, p.tokens - t0) * 128;
-    const uint32_t base = smem_addr(part);
-    for (int e = rank * kSplitThreads + int(threadIdx.x); e < count; e += ranks * kSplitThreads) {
-        const int t = e >> 7, f = f0 + (e & 127);
-        if (f >= p.features) continue;
-        float v = 0.0f, w = 0.0f;
-        for (int r = 0; r < ranks; ++r) {
-            v += ld_cluster_f32(base + 4 * e, r);
-            if (MODE == kGated) w += ld_cluster_f32(base + 4 * (p.nt * 128 + e), r);
-        }
-        if (KIND == kNv) {
-            const float rx = p.row_x[t0 + t];
-            v = v * rx * p.row_w[0][f];
-            if (MODE == kGated) w = w * rx * p.row_w[1][f];
-        }
-        if (MODE == kGated) {
-            const size_t row = size_t(t0 + t);
-            store1(p.out[0].p, row * p.out[0].ld + f, act(v, p.act) * w, p.out[0].dtype);
-            if (KIND == kHalf && p.save) {
-                store1(p.out[1].p, row * p.out[1].ld + f, v, p.out[1].dtype);
-                store1(p.out[2].p, row * p.out[2].ld + f, w, p.out[2].dtype);
-            }
-        } else {
-            store1(p.out[0].p, size_t(t0 + t) * p.out[0].ld + f, v, p.out[0].dtype);
-        }
-    }
-    cluster_sync();       // nobody leaves while a neighbour may still read its partial sums
-}
-
 // ---------------------------------------------------------------- 16-bit rows, element by element
 // dU = dh act(g), dG = dh u act'(g) in fp32, rounded to the 16-bit type that the gradients' products
 // read (the tensor cores take 16-bit operands; the sums over them stay in fp32).
@@ -774,116 +584,188 @@ __device__ __forceinline__ float from_e8m0(uint32_t b) {
     return b ? __uint_as_float(b << 23) : __uint_as_float(0x00400000u);
 }
 
-__device__ __forceinline__ void load16(const QuantArgs& p, size_t row, int col, float (&v)[16]) {
+constexpr uint32_t kInfBits = 0x7F800000u;
+constexpr int kRowChunks = 3;                    // groups of 16 elements that a thread holds in registers
+
+// 16 neighbouring elements as they are stored: 8 registers of 16-bit pairs or 16 floats
+template <int DT> struct Group {
+    uint32_t w[DT == kFp32 ? 16 : 8];
+};
+
+template <int DT>
+__device__ __forceinline__ void load_group(const QuantArgs& p, size_t row, int col, Group<DT>& g) {
+    constexpr int W = DT == kFp32 ? 16 : 8, PER = 16 / W;
     if (p.vec && col + 16 <= p.cols) {
-        if (p.dtype == kFp32) {
-            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + row * p.ld + col);
+        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (row * p.ld + col) * (4 / PER));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 f = q[i];
-                v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
-            }
-        } else {
-            const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.x) + row * p.ld + col);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint4 w = q[i];
-                float2 f;
-                f = unpack2(w.x, p.dtype); v[8 * i] = f.x; v[8 * i + 1] = f.y;
-                f = unpack2(w.y, p.dtype); v[8 * i + 2] = f.x; v[8 * i + 3] = f.y;
-                f = unpack2(w.z, p.dtype); v[8 * i + 4] = f.x; v[8 * i + 5] = f.y;
-                f = unpack2(w.w, p.dtype); v[8 * i + 6] = f.x; v[8 * i + 7] = f.y;
-            }
+        for (int i = 0; i < W / 4; ++i) {
+            const uint4 v = q[i];
+            g.w[4 * i] = v.x; g.w[4 * i + 1] = v.y; g.w[4 * i + 2] = v.z; g.w[4 * i + 3] = v.w;
         }
-    } else {
+    } else if (DT == kFp32) {
+        const uint32_t* q = static_cast<const uint32_t*>(p.x) + row * p.ld;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = col + i < p.cols ? load1(p.x, row * p.ld + col + i, p.dtype) : 0.0f;
+        for (int i = 0; i < W; ++i) g.w[i] = col + i < p.cols ? q[col + i] : 0;
+    } else if (p.ld % 2 == 0 && col + 16 <= p.cols) {      // rows start on multiples of 4 bytes
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.x) + row * p.ld + col);
+#pragma unroll
+        for (int i = 0; i < W; ++i) g.w[i] = q[i];
+    } else {
+        const uint16_t* q = static_cast<const uint16_t*>(p.x) + row * p.ld;
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            g.w[i] = (col + 2 * i < p.cols ? q[col + 2 * i] : 0) | uint32_t(col + 2 * i + 1 < p.cols ? q[col + 2 * i + 1] : 0) << 16;
     }
 }
 
-// magnitudes compared as integers, so that NaN and infinity come out on top
-__device__ __forceinline__ uint32_t amax16(const float (&v)[16]) {
+// the largest magnitude as fp32 bits; infinity and NaN come out on top.  Magnitudes of one format order
+// like their bits: pairs are compared as 16-bit integers, and only the largest is widened.
+template <int DT>
+__device__ __forceinline__ uint32_t group_amax(const Group<DT>& g) {
     uint32_t m = 0;
+    if constexpr (DT == kFp32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return m;
+        for (int i = 0; i < 16; ++i) m = max(m, g.w[i] & 0x7FFFFFFFu);
+        return m;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(g.w[i] & 0x7FFF7FFFu));
+        m = max(m >> 16, m & 0xFFFFu);
+        return DT == kBf16 ? m << 16 : __float_as_uint(unpack2(m, kFp16).x) & 0x7FFFFFFFu;
+    }
 }
-constexpr uint32_t kInfBits = 0x7F800000u;
+template <int DT>
+__device__ __forceinline__ void group_values(const Group<DT>& g, float (&v)[16]) {
+    if constexpr (DT == kFp32) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(g.w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = unpack2(g.w[i], DT);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+}
 
-// One lane takes 16 neighbouring elements; WARPS warps share a row.
+// The scale of a block and what its elements are multiplied by, from the block's largest magnitude (as
+// fp32 bits).
 //   MX: 32 elements share e = max(floor(log2 amax) - 2, -127): the power of two that brings the largest
 //       element into [4, 8); code = rn(v / 2^e), above 6 it saturates.  Every step but the rounding is exact.
-//   NV: 16 elements share s = e4m3_rn(min(amax * (448 / A), 448)), A the row's amax; d = s * (A / 2688);
-//       code = rn(v * (1 / d)), all zero where s is.  A < 2^-100: the row is zero.
-// A value that is not finite makes its block's scale (MX) or its row's factor (NV) NaN.
-template <bool MX, int WARPS>
-__global__ void __launch_bounds__(256) fp4_quantize_kernel(const __grid_constant__ QuantArgs p) {
-    constexpr int ROWS = 8 / WARPS, LANES = 32 * WARPS;
-    const int lane = int(threadIdx.x) % LANES;
-    const size_t row = size_t(blockIdx.x) * ROWS + threadIdx.x / LANES;
+//   NV: 16 elements share s = e4m3_rn(min(amax * up, 448)), up = 448 / A, A the row's amax; d = s * g, g =
+//       A / 2688; code = rn(v * (1 / d)), all zero where s is.  A row below 2^-100 is zero (up = 0).
+// A value that is not finite makes its block's scale (MX) or its row's g (NV) NaN.
+template <bool MX>
+__device__ __forceinline__ void block_scale(uint32_t amax, float up, float g, uint32_t& byte, float& inv) {
+    if (MX) {
+        const int e = max(int(amax >> 23) - 2, 0);         // the stored byte: exponent + 127
+        byte = amax >= kInfBits ? 255u : uint32_t(e);
+        inv = amax >= kInfBits ? 0.0f : __uint_as_float(uint32_t(254 - e) << 23);
+    } else {
+        byte = up > 0.0f ? to_e4m3(fminf(__fmul_rn(__uint_as_float(amax), up), 448.0f)) : 0;
+        const float s = from_e4m3(byte);
+        inv = s > 0.0f ? __frcp_rn(__fmul_rn(s, g)) : 0.0f;
+    }
+}
+// the row's factor g and up, from the row's largest magnitude
+__device__ __forceinline__ void row_factors(uint32_t amax, float& up, float& g) {
+    const float a = __uint_as_float(amax);
+    up = 0.0f;
+    g = 0.0f;
+    if (amax >= kInfBits) {
+        g = __uint_as_float(0x7FFFFFFFu);
+    } else if (a >= 0x1p-100f) {
+        g = __fdiv_rn(a, 2688.0f);
+        up = __fdiv_rn(448.0f, a);
+    }
+}
+// two products with one instruction, each rounded as a single one is
+__device__ __forceinline__ void mul2(float& a, float& b, float c) {
+    uint64_t v, w;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(w) : "f"(c));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(w));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint2 encode_values(float (&v)[16], float inv) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) mul2(v[i], v[i + 1], inv);
+    return make_uint2(encode8(v), encode8(v + 8));
+}
+template <int DT>
+__device__ __forceinline__ uint2 encode_group(const Group<DT>& g, float inv) {
+    float v[16];
+    group_values<DT>(g, v);
+    return encode_values(v, inv);
+}
+// the four scale bytes of 4 neighbouring blocks as one word; a block is PER lanes
+template <int PER>
+__device__ __forceinline__ uint32_t gather_scales(uint32_t byte) {
+    uint32_t word = byte << (8 * (threadIdx.x / PER % 4));
+    word |= __shfl_xor_sync(0xFFFFFFFFu, word, PER);
+    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2 * PER);
+    return word;
+}
+
+// One CTA a row, one thread 16 neighbouring elements at a time.  A thread's three groups are loaded together
+// and stay in registers between the row's maximum and the rounding, so a row of up to 48 elements a thread
+// is read once; only longer rows (above 24576 elements) are read a second time for the NV form.
+template <bool MX, int DT>
+__global__ void __launch_bounds__(512) fp4_quantize_kernel(const __grid_constant__ QuantArgs p) {
+    __shared__ uint32_t top[16];
+    const int tid = threadIdx.x, threads = blockDim.x, span = threads * 16 * kRowChunks;
+    const size_t row = blockIdx.x;
     const size_t stages = (size_t(p.cols) + 255) / 256;
     const int padded = int(stages * 256);
     const int stride = (p.cols + 31) / 32 * 16;            // bytes of a row of codes
     grid_launch();
     grid_wait();
-    const bool live = row < size_t(p.rows);
 
+    Group<DT> x[kRowChunks];
+    uint32_t peak[kRowChunks];
+    auto load = [&](int first) {
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) load_group<DT>(p, row, first + (c * threads + tid) * 16, x[c]);
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) peak[c] = group_amax<DT>(x[c]);
+    };
+    const bool once = span >= padded;
     float up = 0.0f, g = 0.0f;
     if (!MX) {
         uint32_t m = 0;
-        if (live)
-            for (int col = lane * 16; col < p.cols; col += LANES * 16) {
-                float v[16];
-                load16(p, row, col, v);
-                m = max(m, amax16(v));
-            }
+        for (int first = 0; first < p.cols; first += span) {
+            load(first);
+#pragma unroll
+            for (int c = 0; c < kRowChunks; ++c) m = max(m, peak[c]);
+        }
         m = __reduce_max_sync(0xFFFFFFFFu, m);
-        if (WARPS > 1) {
-            __shared__ uint32_t top[8];
-            if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = m;
+        if (threads > 32) {
+            if ((tid & 31) == 0) top[tid >> 5] = m;
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < WARPS; ++i) m = max(m, top[threadIdx.x / LANES * WARPS + i]);
+            m = __reduce_max_sync(0xFFFFFFFFu, (tid & 31) < threads / 32 ? top[tid & 31] : 0);
         }
-        const float amax = __uint_as_float(m);
-        if (m >= kInfBits) {
-            g = __uint_as_float(0x7FFFFFFFu);
-        } else if (amax >= 0x1p-100f) {
-            g = __fdiv_rn(amax, 2688.0f);
-            up = __fdiv_rn(448.0f, amax);
-        }
-        if (live && lane == 0) p.row_scales[row] = g;
+        row_factors(m, up, g);
+        if (tid == 0) p.row_scales[row] = g;
     }
-    if (!live) return;                                     // whole warps leave
-
-    for (int col0 = 0; col0 < padded; col0 += LANES * 16) {
-        const int col = col0 + lane * 16;
-        float v[16];
-        load16(p, row, col, v);                            // zeros beyond the row
-        uint32_t m = amax16(v), byte;
-        float inv;
-        if (MX) {
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-            const int field = int(m >> 23);                // exponent + 127
-            const int e = max(field - 2, 0);               // the stored byte
-            byte = m >= kInfBits ? 255u : uint32_t(e);
-            inv = m >= kInfBits ? 0.0f : __uint_as_float(uint32_t(254 - e) << 23);
-        } else {
-            const float s = from_e4m3(byte = to_e4m3(fminf(__fmul_rn(__uint_as_float(m), up), 448.0f)));
-            inv = s > 0.0f && up > 0.0f ? __fdiv_rn(1.0f, __fmul_rn(s, g)) : 0.0f;
-            if (up == 0.0f) byte = 0;
-        }
+    uint8_t* const codes = p.codes + row * size_t(stride) + tid * 8;
+    uint8_t* const scales = p.scales + scale_offset<MX>(row, 0, stages);
+    for (int first = 0; first < padded; first += span) {
+        if (MX || !once) load(first);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = inv == 0.0f ? 0.0f : __fmul_rn(v[i], inv);
-        const uint2 code = make_uint2(encode8(v), encode8(v + 8));
-        if (col / 2 + 8 <= stride) *reinterpret_cast<uint2*>(p.codes + row * size_t(stride) + col / 2) = code;
-        // four scales of a row are one 32-bit word
-        constexpr int PER = MX ? 2 : 1;                    // lanes of a block
-        uint32_t word = byte << (8 * (lane / PER % 4));
-        word |= __shfl_xor_sync(0xFFFFFFFFu, word, PER);
-        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2 * PER);
-        if (lane % (4 * PER) == 0 && col < padded)
-            *reinterpret_cast<uint32_t*>(p.scales + scale_offset<MX>(row, size_t(col) / (MX ? 32 : 16), stages)) = word;
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + (c * threads + tid) * 16;
+            constexpr int PER = MX ? 2 : 1;                // threads of a block
+            uint32_t m = peak[c], byte;
+            if (MX) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+            float inv;
+            block_scale<MX>(m, up, g, byte, inv);
+            const uint2 code = encode_group<DT>(x[c], inv);
+            if (col / 2 + 8 <= stride) *reinterpret_cast<uint2*>(codes + (first + c * threads * 16) / 2) = code;
+            const uint32_t word = gather_scales<PER>(byte);
+            if (tid % (4 * PER) == 0 && col < padded)      // 4 scales of the row lie together, 512 bytes from the next 4
+                *reinterpret_cast<uint32_t*>(scales + size_t(col / (64 * PER)) * 512) = word;
+        }
     }
 }
 
@@ -894,41 +776,365 @@ struct DequantArgs {
     size_t ld;
     int rows, cols, dtype, vec;
 };
-// value = code * scale (MX), code * (scale * row factor) (NV), rounded once to the output type
+// value = code * scale (MX), code * (scale * row factor) (NV) in fp32, rounded once to the output type.
+// One CTA a row as above: a thread's three groups are in flight together.
 template <bool MX>
-__global__ void __launch_bounds__(256) fp4_dequantize_kernel(const __grid_constant__ DequantArgs p) {
-    const size_t stages = (size_t(p.cols) + 255) / 256;
-    const int stride = (p.cols + 31) / 32 * 16, per_row = (p.cols + 15) / 16;
-    const size_t total = size_t(p.rows) * per_row;
+__global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_constant__ DequantArgs p) {
+    const int tid = threadIdx.x, threads = blockDim.x, span = threads * 16 * kRowChunks;
+    const size_t row = blockIdx.x, stages = (size_t(p.cols) + 255) / 256;
+    const int stride = (p.cols + 31) / 32 * 16;
     grid_launch();
     grid_wait();
-    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += size_t(gridDim.x) * 256) {
-        const size_t row = i / per_row;
-        const int col = int(i % per_row) * 16;
-        const uint2 w = *reinterpret_cast<const uint2*>(p.codes + row * size_t(stride) + col / 2);
-        const uint32_t b = p.scales[scale_offset<MX>(row, size_t(col) / (MX ? 32 : 16), stages)];
-        const float d = MX ? from_e8m0(b) : __fmul_rn(from_e4m3(b), p.row_scales[row]);
-        float v[16];
-        decode8(w.x, v);
-        decode8(w.y, v + 8);
+    const float g = MX ? 1.0f : p.row_scales[row];
+    for (int first = 0; first < p.cols; first += span) {
+        uint2 w[kRowChunks];
+        uint32_t b[kRowChunks];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = __fmul_rn(v[j], d);
-        if (p.vec && col + 16 <= p.cols) {
-            if (p.dtype == kFp32) {
-                float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * p.ld + col);
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + (c * threads + tid) * 16;
+            if (col >= p.cols) continue;
+            w[c] = *reinterpret_cast<const uint2*>(p.codes + row * size_t(stride) + col / 2);
+            b[c] = p.scales[scale_offset<MX>(row, size_t(col) / (MX ? 32 : 16), stages)];
+        }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + (c * threads + tid) * 16;
+            if (col >= p.cols) continue;
+            const float d = MX ? from_e8m0(b[c]) : __fmul_rn(from_e4m3(b[c]), g);
+            float v[16];
+            decode8(w[c].x, v);
+            decode8(w[c].y, v + 8);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = __fmul_rn(v[j], d);
+            if (p.vec && col + 16 <= p.cols) {
+                if (p.dtype == kFp32) {
+                    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * p.ld + col);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                } else {
+                    uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + row * p.ld + col);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        q[j] = make_uint4(pack2(v[8 * j], v[8 * j + 1], p.dtype), pack2(v[8 * j + 2], v[8 * j + 3], p.dtype),
+                                          pack2(v[8 * j + 4], v[8 * j + 5], p.dtype), pack2(v[8 * j + 6], v[8 * j + 7], p.dtype));
+                }
+            } else if (p.dtype != kFp32 && p.ld % 2 == 0 && col + 16 <= p.cols) {
+                uint32_t* q = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + row * p.ld + col);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[j] = pack2(v[2 * j], v[2 * j + 1], p.dtype);
             } else {
-                uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + row * p.ld + col);
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    q[j] = make_uint4(pack2(v[8 * j], v[8 * j + 1], p.dtype), pack2(v[8 * j + 2], v[8 * j + 3], p.dtype),
-                                      pack2(v[8 * j + 4], v[8 * j + 5], p.dtype), pack2(v[8 * j + 6], v[8 * j + 7], p.dtype));
+                for (int j = 0; j < 16; ++j)
+                    if (col + j < p.cols) store1(p.out, row * p.ld + col + j, v[j], p.dtype);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- few tokens
+struct SplitArgs {
+    CUtensorMap w[2], x[2];
+    const uint8_t* scales_w[2];
+    const uint8_t* scales_x;
+    const float* row_w[2];
+    const float* row_x;
+    QuantArgs raw;                    // fused: x in 16 bits, quantized by the kernel itself
+    Out out[3];
+    int features, tokens;             // rows of w, rows of x
+    int stages;                       // stages of the reduction axis (of each part of kSum2)
+    int nt;                           // tokens of a tile: a multiple of 16, at most 128
+    int pipe;                         // stages in shared memory
+    int columns;                      // of tensor memory: a power of two
+    int act, bf16, save;
+};
+constexpr int kSplitThreads = 192, kSplitMaxPipe = 12;
+constexpr int kFusedTokens = 16;      // tokens of a tile of the fused form
+template <int KIND, int MODE>
+__host__ __device__ constexpr int split_stage_bytes(int nt) {
+    return (MODE == kGated ? 2 : 1) * (kTileBytes + kScaleBytes<KIND>) + nt * kRowBytes + kScaleBytes<KIND>;
+}
+// rows of the 128 that one of `ranks` CTAs adds up, and the bytes of the parts it receives for them
+__host__ __device__ constexpr int split_rows(int ranks) { return (128 + ranks - 1) / ranks; }
+template <int MODE>
+__host__ __device__ constexpr int split_part_bytes(int nt, int ranks) {
+    return ranks * (MODE == kGated ? 2 : 1) * nt * split_rows(ranks) * 4;
+}
+
+// The output transposed: 128 features x nt tokens, so that a single token costs one narrow product over
+// each weight tile instead of a 256-row one, and the weights, which are all the bytes there are, are
+// read once.  The reduction axis is split over the CTAs of a cluster (cluster dimension x) because
+// features / 128 tiles alone would leave most SMs without work.  Each CTA sends its partial sums to the
+// CTAs that own their rows, through distributed shared memory into a place of their own, and the owner
+// adds them in rank order, so the sum does not depend on timing.
+//
+// FUSED (4-bit, at most 16 tokens): x comes in 16 bits; the warps that write the output later quantize
+// the stages of x first, straight into the swizzled rows that the products read, which saves a launch
+// and a round trip of x.
+template <int KIND, int MODE, bool W_MN, bool FUSED>
+__global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_constant__ SplitArgs p) {
+    constexpr bool FP4 = KIND != kHalf, MX = KIND == kMx;
+    constexpr int SB = kScaleBytes<KIND>, NW = MODE == kGated ? 2 : 1;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * kSplitMaxPipe + 2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile uint32_t abort;
+    __shared__ uint32_t row_max[kFusedTokens];          // fused NV: largest magnitudes of the tokens
+
+    const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    uint8_t* const smem_ptr = smem_raw + (smem - smem_addr(smem_raw));
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kSplitMaxPipe, ready = empty + 8 * kSplitMaxPipe,
+                   drain = ready + 8;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const uint32_t xb = p.nt * kRowBytes, STAGE = NW * (kTileBytes + SB) + xb + SB;
+    const uint32_t parts = smem + p.pipe * STAGE;       // [ranks][NW * nt][split_rows]
+
+    const int ranks = gridDim.x, rank = uniform(cluster_rank());
+    const int total = p.stages * (MODE == kSum2 ? 2 : 1);
+    const int s0 = int(int64_t(total) * rank / ranks), s1 = int(int64_t(total) * (rank + 1) / ranks);
+    const int f0 = blockIdx.y * kRowsM, t0 = blockIdx.z * p.nt;
+
+    // Tensor memory is waited for when another kernel's CTA still has it.  So that CTAs of two clusters
+    // cannot wait for each other's in a circle, a CTA says that it has started before it asks for tensor
+    // memory, and gives it back before it waits for its cluster's sums.
+    cluster_arrive();
+
+    // the loading warp prepares the barriers and starts; everybody else meets it below
+    if (FUSED && threadIdx.x < kFusedTokens) row_max[threadIdx.x] = 0;
+    if (warp == 4) {
+        if (lane == 0) {
+            prefetch_map(&p.w[0]);
+            if (NW == 2 || MODE == kSum2) prefetch_map(&p.w[1]);
+            if (!FUSED) prefetch_map(&p.x[0]);
+            for (int i = 0; i < p.pipe; ++i) {
+                barrier_init(full + 8 * i, FUSED ? 1 + p.tokens : 1);
+                barrier_init(empty + 8 * i, 1);
+            }
+            barrier_init(ready, 1);
+            barrier_init(drain, 1);
+            abort = 0;
+            fence_barrier_init();
+        }
+        __syncwarp();
+    } else if (warp == 5) {
+        tmem_alloc<1>(smem_addr(&tmem_slot), p.columns);
+        fence_before();
+    }
+    auto load_stage = [&](int it) {
+        const int slot = it % p.pipe, s = s0 + it;
+        const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb, bar = full + 8 * slot;
+        const int second = MODE == kSum2 ? s >= p.stages : 0, ks = s - second * p.stages;
+        const int kc = FP4 ? ks * kRowBytes : ks * 64;
+        barrier_expect_warp(bar, NW * kTileBytes + (FUSED ? 0 : xb) + (FP4 ? (NW + (FUSED ? 0 : 1)) * SB : 0));
+        for (int q = 0; q < NW; ++q) {
+            const CUtensorMap* mw = &p.w[MODE == kSum2 ? second : q];
+            if (W_MN) {
+                tma_load_2d(sw, mw, f0, kc, bar);
+                tma_load_2d(sw + kChunkBytes, mw, f0 + 64, kc, bar);
+            } else {
+                tma_load_2d(sw + q * kTileBytes, mw, kc, f0, bar);
+            }
+            if (FP4) bulk_load(ss + SB * q, p.scales_w[q] + (size_t(f0 / 128) * p.stages + ks) * SB, SB, bar);
+        }
+        if (!FUSED) {
+            tma_load_2d(sx, &p.x[second], kc, t0, bar);
+            if (FP4) bulk_load(ss + SB * NW, p.scales_x + (size_t(t0 / 128) * p.stages + ks) * SB, SB, bar);
+        }
+    };
+    grid_launch();
+    grid_wait();
+    const int early = min(s1 - s0, p.pipe);
+    if (warp == 4) {
+        for (int it = 0; it < early; ++it) load_stage(it);
+    }
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = uniform(tmem_slot);
+
+    // FUSED.  A unit is one token's part of one stage: 16 groups of 16 elements, half a warp.  The first four
+    // warps take the units in the order of the stages, the next one's loads under way.  One body for both
+    // 16-bit types and no unrolling: what runs a few times costs mostly the fetching of its instructions.
+    const int j = lane & 15;
+    auto for_units = [&](auto&& body) {
+        const int n = s1 - s0;
+        int it = 0, t = warp * 2 + (lane >> 4);
+        auto settle = [&] {
+            while (t >= p.tokens && it < n) {
+                t -= p.tokens;
+                ++it;
+            }
+        };
+        settle();
+        Group<kBf16> next = {};                          // the bits of either type
+        if (it < n) load_group<kBf16>(p.raw, t, (s0 + it) * 256 + j * 16, next);
+#pragma unroll 1
+        while (__any_sync(0xFFFFFFFFu, it < n)) {
+            const Group<kBf16> g = next;
+            const int at = it, row = t;
+            t += 8;
+            settle();
+            if (it < n) load_group<kBf16>(p.raw, t, (s0 + it) * 256 + j * 16, next);
+            float v[16];
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float2 f = unpack2(g.w[i], p.raw.dtype);
+                v[2 * i] = f.x;
+                v[2 * i + 1] = f.y;
+                m = max(m, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
+            }
+            body(at, row, at < n, v, m);
+        }
+    };
+    if constexpr (FUSED && !MX) {
+        // The rows' maxima: the cluster's CTAs have the whole of each row between them, and each tells all.
+        cluster_wait();                                 // every CTA of the cluster has started
+        if (warp < 4) {
+            for_units([&](int, int row, bool in, float (&)[16], uint32_t m) {
+                // a group past the row's end holds zeros, and so does a unit that does not exist
+#pragma unroll
+                for (int d = 8; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+                if (in && j == 0)
+                    for (int r = 0; r < ranks; ++r) max_cluster_u32(peer_addr(smem_addr(&row_max[row]), r), m);
+            });
+        }
+        __syncwarp();
+        cluster_sync();
+    }
+
+    if (warp == 4) {
+        bool ok = true;
+        int it = early;
+        for (; it < s1 - s0; ++it) {
+            const int slot = it % p.pipe;
+            if (!(ok = barrier_wait_warp(empty + 8 * slot, (it / p.pipe & 1) ^ 1, &abort))) break;
+            load_stage(it);
+        }
+        if (abort)
+            for (int i = it > p.pipe ? it - p.pipe : 0; i < it; ++i) barrier_drain(full + 8 * (i % p.pipe), i / p.pipe & 1);
+        __syncwarp();
+    } else if (warp == 5) {
+        const uint32_t tw = tmem + NW * p.nt, tx = tw + NW * 4 * kScaleTiles<KIND>;
+        bool ok = true;
+        for (int it = 0; it < s1 - s0; ++it) {
+            const int slot = it % p.pipe;
+            if (!(ok = barrier_wait_warp(full + 8 * slot, it / p.pipe & 1, &abort))) break;
+            fence_after();
+            const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb;
+            if (FP4) {
+#pragma unroll
+                for (int j = 0; j < kScaleTiles<KIND>; ++j) {
+#pragma unroll
+                    for (int q = 0; q < NW; ++q)
+                        copy_scales<1>(tw + (q * kScaleTiles<KIND> + j) * 4, ss + SB * q + 512 * j);
+                    copy_scales<1>(tx + 4 * j, ss + SB * NW + 512 * j);
+                }
+            }
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                const uint32_t dx = swizzled_desc(sx + 32 * kk, 16);
+#pragma unroll
+                for (int q = 0; q < NW; ++q) {
+                    const uint32_t a = sw + q * kTileBytes;
+                    const uint32_t dw = W_MN ? swizzled_desc(a + 2048 * kk, kChunkBytes) : swizzled_desc(a + 32 * kk, 16);
+                    if constexpr (FP4) {
+                        const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
+                        mma_fp4<1, MX>(tmem + q * p.nt, dw, dx, desc_fp4(MX, 128, p.nt, which),
+                                       tw + (q * kScaleTiles<KIND> + j) * 4, tx + 4 * j, it | kk);
+                    } else {
+                        mma_16bit<1>(tmem + q * p.nt, dw, dx, desc_16bit(p.bf16, W_MN, false, 128, p.nt), it | kk);
+                    }
+                }
+            }
+            mma_commit<1>(empty + 8 * slot);
+        }
+        if (ok) mma_commit<1>(ready);
+        if (abort) {
+            mma_commit<1>(drain);
+            barrier_drain(drain, 0);
+        }
+        __syncwarp();
+    } else if constexpr (FUSED) {
+        // each unit arrives on its stage's barrier
+        bool ok = true;
+        for_units([&](int at, int row, bool in, float (&v)[16], uint32_t m) {
+            const int slot = at % p.pipe;
+            float up = 0.0f, factor = 0.0f, inv;
+            uint32_t byte;
+            if (MX) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+            if (!MX && in) row_factors(row_max[row], up, factor);
+            block_scale<MX>(m, up, factor, byte, inv);
+            const uint2 code = encode_values(v, inv);
+            if (in && at >= p.pipe) ok = ok && barrier_wait(empty + 8 * slot, (at / p.pipe & 1) ^ 1, &abort);
+            if (in && ok) {
+                uint8_t* const sx = smem_ptr + slot * STAGE + NW * kTileBytes;
+                uint8_t* const ss = sx + xb + SB * NW;
+                // byte 8 j of the row's 128: 16-byte pieces are swizzled by the row
+                *reinterpret_cast<uint2*>(sx + row * 128 + (((j >> 1) ^ (row & 7)) << 4) + (j & 1) * 8) = code;
+                const int block = MX ? j >> 1 : j;
+                if (!MX || !(j & 1)) ss[(block >> 2) * 512 + row * 16 + (block & 3)] = uint8_t(byte);
+                fence_async_shared();
+            }
+            __syncwarp();
+            if (in && ok && j == 0) barrier_arrive(full + 8 * slot);
+        });
+    }
+    // ---------------------------------------------------- partial sums to their owners
+    __syncwarp();
+    if constexpr (!FUSED || MX) cluster_wait();         // every CTA of the cluster has started
+    const int rows = split_rows(ranks), wide = NW * p.nt;
+    if (warp < 4) {
+        __syncwarp();
+        if (barrier_wait(ready, 0, &abort)) {
+            __syncwarp();
+            fence_after();
+            const int row = warp * 32 + lane, owner = row / rows;
+            const int cols = min(p.nt, p.tokens - t0);  // those that exist
+            const uint32_t to = peer_addr(parts + ((rank * wide) * rows + row - owner * rows) * 4, owner);
+            for (int c = 0; c < wide; c += 16) {
+                if (c % p.nt >= cols) continue;
+                uint32_t r[16];
+                tmem_load16(tmem + c + (uint32_t(warp * 32) << 16), r);
+                tmem_wait_loads();
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (c % p.nt + j < cols) st_cluster_f32(to + (c + j) * rows * 4, __uint_as_float(r[j]));
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 5) {
+        fence_after();
+        tmem_free<1>(tmem, p.columns);
+    }
+    __syncwarp();
+    cluster_sync();
+
+    const int first = rank * rows, mine = min(rows, 128 - first), count = min(p.nt, p.tokens - t0) * rows;
+    const float* const sums = reinterpret_cast<const float*>(smem_ptr + p.pipe * STAGE);
+    for (int e = threadIdx.x; e < count; e += kSplitThreads) {
+        const int t = e / rows, i = e - t * rows, f = f0 + first + i;
+        if (i >= mine || f >= p.features) continue;
+        float v = 0.0f, w = 0.0f;
+        for (int r = 0; r < ranks; ++r) {
+            v += sums[(r * wide + t) * rows + i];
+            if (MODE == kGated) w += sums[(r * wide + p.nt + t) * rows + i];
+        }
+        if (KIND == kNv) {
+            float up, rx;
+            if (FUSED) row_factors(row_max[t], up, rx); else rx = p.row_x[t0 + t];
+            v = v * rx * p.row_w[0][f];
+            if (MODE == kGated) w = w * rx * p.row_w[1][f];
+        }
+        const size_t row = size_t(t0 + t);
+        if (MODE == kGated) {
+            store1(p.out[0].p, row * p.out[0].ld + f, act(v, p.act) * w, p.out[0].dtype);
+            if (KIND == kHalf && p.save) {
+                store1(p.out[1].p, row * p.out[1].ld + f, v, p.out[1].dtype);
+                store1(p.out[2].p, row * p.out[2].ld + f, w, p.out[2].dtype);
             }
         } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (col + j < p.cols) store1(p.out, row * p.ld + col + j, v[j], p.dtype);
+            store1(p.out[0].p, row * p.out[0].ld + f, v, p.out[0].dtype);
         }
     }
 }

@@ -71,13 +71,13 @@ def test_matmul_refuses_bad_arguments():
 
 
 def test_linear_and_gated_refuse_bad_arguments():
-    need = eq.fp4_linear_workspace_bytes(4, 64, eq.FP4_NV)
+    need = eq.fp4_linear_workspace_bytes(40, 64, eq.FP4_NV)
     w = dict(w_codes=A + GB, w_scales=A + 2 * GB, w_row_scales=A + 3 * GB)
-    a = dict(x=A, dtype=eq.BF16, ldx=64, **w, m=4, n=8, k=64, format=eq.FP4_NV, out=A + 4 * GB, ld=8, workspace=A + 5 * GB,
+    a = dict(x=A, dtype=eq.BF16, ldx=64, **w, m=40, n=8, k=64, format=eq.FP4_NV, out=A + 4 * GB, ld=8, workspace=A + 5 * GB,
              workspace_bytes=need)
     gu = dict(g_codes=A + GB, g_scales=A + 2 * GB, g_row_scales=A + 3 * GB, u_codes=A + 6 * GB, u_scales=A + 7 * GB,
               u_row_scales=A + 8 * GB)
-    b = dict(x=A, dtype=eq.BF16, ldx=64, **gu, m=4, f=8, k=64, format=eq.FP4_NV, act=0, h=A + 4 * GB, ldh=8,
+    b = dict(x=A, dtype=eq.BF16, ldx=64, **gu, m=40, f=8, k=64, format=eq.FP4_NV, act=0, h=A + 4 * GB, ldh=8,
              workspace=A + 5 * GB, workspace_bytes=need)
     for f, args, out in ((eq.fp4_linear, a, "out"), (eq.fp4_gated, b, "h")):
         pointers = [k for k in args if isinstance(args[k], int) and args[k] >= A]
@@ -91,6 +91,7 @@ def test_linear_and_gated_refuse_bad_arguments():
         assert status_of(f, **{**args, out: A + 5 * GB}) == binding.ERR_ALIAS       # the workspace
         assert status_of(f, **{**args, "m": 0}) == 0
     assert status_of(eq.fp4_gated, **{**b, "act": 2}) == binding.ERR_FORMAT
+    assert eq.fp4_linear_workspace_bytes(1, 64, eq.FP4_NV) == 0       # a few tokens are quantized by the product
 
 
 def test_gated_forward_and_backward_refuse_bad_arguments():
