@@ -274,16 +274,18 @@ constexpr size_t kFewTokensFp4 = 32, kFewTokensGated = 64, kFewTokensGradient = 
 constexpr size_t kFusedMxTokens = 8, kFusedNvTokens = 2;
 static_assert(kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, "the fused form takes one tile of tokens");
 
-// Columns of a tile.  The pairs of SMs work through whole rounds of tiles, so the time goes with rounds *
-// (bn + a share for starting and ending a tile); a narrower tile may save a round, or give every pair
-// work when there is little.  4-bit operands: their scales come in groups of 128 columns.
-int tile_width(size_t rows, size_t cols, int outputs, bool gated, bool fp4, int sms) {
+// Columns of a tile.  The pairs of SMs work through whole rounds of tiles.  A stage takes a pair the time to
+// load (256 + bn) rows of 128 bytes, about as long as the products of the widest tile and longer than those
+// of a narrower one, and a tile costs some stages' time to begin and to drain; a narrower tile may still save
+// a round, or give every pair work when there is little.  4-bit operands: their scales come in groups of 128
+// columns.
+int tile_width(size_t rows, size_t cols, int outputs, size_t stages, bool gated, bool fp4, int sms) {
     int best = 256;
     size_t best_cost = ~size_t(0);
     const int step = fp4 ? 128 : gated ? 64 : 32;
     for (int bn = 256; bn >= (gated && fp4 ? 256 : step); bn -= step) {
         const size_t tiles = ceil_div(rows, kTileM) * ceil_div(cols, gated ? bn / 2 : bn) * outputs;
-        const size_t cost = ceil_div(tiles, sms / 2) * size_t(bn + 48);
+        const size_t cost = ceil_div(tiles, sms / 2) * (256 + bn) * (stages + 4);
         if (cost < best_cost) best = bn, best_cost = cost;
     }
     return best;
@@ -364,7 +366,7 @@ int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int ac
     TileArgs a = {};
     int sms;
     TRY(current_device(sms));
-    a.bn = tile_width(m, n, 1, MODE == kGated, true, sms);
+    a.bn = tile_width(m, n, 1, fp4_stages(k), MODE == kGated, true, sms);
     const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
     TRY(make_map(a.a[0], x.codes, 1, stride, m, stride, kRowsM));
     TRY(scale_map(a.scales_a, x.scales, m, k, format));
@@ -619,7 +621,7 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     TileArgs a = {};
     int sms;
     TRY(current_device(sms));
-    a.bn = tile_width(m, f, 1, true, false, sms);
+    a.bn = tile_width(m, f, 1, stages, true, false, sms);
     TRY(map16(a.a[0], ox, m, k, kRowsM));
     TRY(map16(a.b[0], og, f, k, a.bn / 2));
     TRY(map16(a.b[1], ou, f, k, a.bn / 2));
@@ -704,7 +706,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
         TRY((launch_split<kHalf, kSum2, true>(a, k, m, stream)));
     } else {
         TileArgs a = {};
-        a.bn = tile_width(m, k, 1, false, false, sms);
+        a.bn = tile_width(m, k, 1, 2 * ceil_div(f, 64), false, false, sms);
         TRY(map16(a.a[0], dg, m, f, kRowsM));
         TRY(map16(a.a[1], du, m, f, kRowsM));
         TRY(map16(a.b[0], og, f, k, 64));
@@ -716,7 +718,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     }
     // dWg = dG^T x, dWu = dU^T x: the reduction runs over the tokens
     TileArgs a = {};
-    a.bn = tile_width(f, k, 2, false, false, sms);
+    a.bn = tile_width(f, k, 2, ceil_div(m, 64), false, false, sms);
     TRY(map16(a.a[0], dg, m, f, 64));
     TRY(map16(a.a[1], du, m, f, 64));
     TRY(map16(a.b[0], ox, m, k, 64));

@@ -91,79 +91,102 @@ struct Out {
     int vec;      // 1: base and row stride are multiples of 16 bytes
 };
 
-// 32 x 32 transpose inside a warp: lane t holds row t before and column t after
-__device__ __forceinline__ void transpose32(float (&v)[32]) {
-    const uint32_t lane = threadIdx.x & 31;
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) {
-        const bool up = lane & s;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            if (i & s) continue;
-            const float give = up ? v[i] : v[i + s];
-            const float got = __shfl_xor_sync(0xFFFFFFFFu, give, s);
-            if (up) v[i] = got; else v[i + s] = got;
-        }
-    }
-}
-
 constexpr int kStageOut = 32 * 32 * 2;        // bytes of a staged 32 x 32 block of 16-bit outputs
 
-// A warp's 32 rows x 32 columns, lane t holding row t, to an output whose rows TMA can write: through one
-// of the warp's two buffers in shared memory (rows of 64 bytes, 16-byte pieces swizzled as the tensor map
-// says, so that the lanes' writes meet no bank twice).  The store itself is asynchronous; the buffer is
+// 32 x 32 outputs of a warp, lane t holding row t, as 16-bit rows of 64 bytes in shared memory; 16-byte
+// pieces are swizzled (as the 64-byte swizzle of a tensor map), so that the lanes meet no bank twice
+__device__ __forceinline__ uint32_t staged_at(uint32_t row, uint32_t byte) {
+    return row * 64 + ((((byte >> 4) ^ (row >> 1)) & 3) << 4) + (byte & 15);
+}
+__device__ __forceinline__ void stage_rows(uint32_t buf, int dtype, const float (&v)[32]) {
+    const uint32_t lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        st_shared_v4(buf + staged_at(lane, 16 * c), pack2(v[8 * c], v[8 * c + 1], dtype), pack2(v[8 * c + 2], v[8 * c + 3], dtype),
+                     pack2(v[8 * c + 4], v[8 * c + 5], dtype), pack2(v[8 * c + 6], v[8 * c + 7], dtype));
+}
+
+// To an output whose rows TMA can write.  The store is asynchronous; of the warp's two buffers one is
 // free again when at most one later store has not been read.
 __device__ __forceinline__ void store_staged(const CUtensorMap* map, uint32_t buf, int row0, int col0, int dtype,
                                              const float (&v)[32]) {
     const uint32_t lane = threadIdx.x & 31;
     if (lane == 0) tma_store_wait_read<1>();
     __syncwarp();
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        st_shared_v4(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), pack2(v[8 * c], v[8 * c + 1], dtype),
-                     pack2(v[8 * c + 2], v[8 * c + 3], dtype), pack2(v[8 * c + 4], v[8 * c + 5], dtype),
-                     pack2(v[8 * c + 6], v[8 * c + 7], dtype));
+    stage_rows(buf, dtype, v);
     fence_async_shared();
     __syncwarp();
     if (lane == 0) tma_store_2d(map, buf, col0, row0);
 }
 
-// The same to any other output.  fp32 rows that are aligned: each lane writes its own 128 bytes.  Rows that
-// are not: the block is transposed so that a row's columns are written by neighbouring lanes together;
-// writing them lane by lane would touch each sector sixteen times.
-__device__ __forceinline__ void store_direct(const Out& o, int row0, int col0, int rows, int cols, float (&v)[32]) {
-    const int lane = threadIdx.x & 31;
-    if (o.vec && o.dtype == kFp32 && col0 + 32 <= cols) {
-        if (row0 + lane < rows) {
-            float4* q = reinterpret_cast<float4*>(static_cast<float*>(o.p) + size_t(row0 + lane) * o.ld + col0);
+// To any other output.  16-bit: neighbouring lanes write a row's neighbouring columns, in units of 8, 4 or
+// 2 bytes as the row stride allows; each lane writing its own row would touch every sector many times.
+// fp32: each lane writes its own row.
+__device__ __forceinline__ void store_direct(const Out& o, uint32_t buf, int row0, int col0, int rows, int cols,
+                                             const float (&v)[32]) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (o.dtype == kFp32) {
+        float* q = static_cast<float*>(o.p) + size_t(row0 + lane) * o.ld + col0;
+        if (row0 + int(lane) >= rows) return;
+        if (o.vec && col0 + 32 <= cols) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < 8; ++i)
+                reinterpret_cast<float4*>(q)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (col0 + i < cols) q[i] = v[i];
         }
         return;
     }
-    transpose32(v);
-    if (col0 + lane < cols) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (row0 + i < rows) store1(o.p, size_t(row0 + i) * o.ld + col0 + lane, v[i], o.dtype);
-    }
-}
-
-// v *= row factor * column factors, in that order: the product of two factors alone could underflow
-__device__ __forceinline__ void scale_columns(float (&v)[32], float row, const float* cols, int col0, int n) {
-    if (col0 + 32 <= n) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float4 c = reinterpret_cast<const float4*>(cols + col0)[j];
-            v[4 * j] = v[4 * j] * row * c.x;
-            v[4 * j + 1] = v[4 * j + 1] * row * c.y;
-            v[4 * j + 2] = v[4 * j + 2] * row * c.z;
-            v[4 * j + 3] = v[4 * j + 3] * row * c.w;
+    if (lane == 0) tma_store_wait_read<0>();
+    __syncwarp();
+    stage_rows(buf, o.dtype, v);
+    __syncwarp();
+    uint16_t* const base = static_cast<uint16_t*>(o.p) + size_t(row0) * o.ld + col0;
+    const int height = min(32, rows - row0), width = min(32, cols - col0);
+    if (o.ld % 4 == 0) {
+        const int c = (lane & 7) * 4;
+#pragma unroll 4
+        for (int r = lane >> 3; r < height; r += 4) {
+            uint32_t a, b;
+            ld_shared_v2(buf + staged_at(r, c * 2), a, b);
+            uint16_t* q = base + size_t(r) * o.ld + c;
+            if (c + 4 <= width) {
+                *reinterpret_cast<uint2*>(q) = make_uint2(a, b);
+            } else {
+                if (c < width) q[0] = uint16_t(a);
+                if (c + 1 < width) q[1] = uint16_t(a >> 16);
+                if (c + 2 < width) q[2] = uint16_t(b);
+            }
+        }
+    } else if (o.ld % 2 == 0) {
+        const int c = (lane & 15) * 2;
+#pragma unroll 4
+        for (int r = lane >> 4; r < height; r += 2) {
+            const uint32_t a = ld_shared_u32(buf + staged_at(r, c * 2));
+            uint16_t* q = base + size_t(r) * o.ld + c;
+            if (c + 2 <= width) *reinterpret_cast<uint32_t*>(q) = a;
+            else if (c < width) q[0] = uint16_t(a);
         }
     } else {
+#pragma unroll 4
+        for (int r = 0; r < height; ++r)
+            if (int(lane) < width) base[size_t(r) * o.ld + lane] = uint16_t(ld_shared_u16(buf + staged_at(r, lane * 2)));
+    }
+    __syncwarp();
+}
+
+// v *= row factor * column factors (in shared memory), in that order: the product of two factors alone
+// could underflow
+__device__ __forceinline__ void scale_columns(float (&v)[32], float row, const float* cols) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (col0 + j < n) v[j] = v[j] * row * cols[col0 + j];
+    for (int j = 0; j < 8; ++j) {
+        const float4 c = reinterpret_cast<const float4*>(cols)[j];
+        v[4 * j] = v[4 * j] * row * c.x;
+        v[4 * j + 1] = v[4 * j + 1] * row * c.y;
+        v[4 * j + 2] = v[4 * j + 2] * row * c.z;
+        v[4 * j + 3] = v[4 * j + 3] * row * c.w;
     }
 }
 
@@ -224,6 +247,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
     __shared__ uint64_t bars[2 * PIPE + 5];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t abort;
+    __shared__ __align__(16) float factors[2][KIND == kNv ? 256 : 4];
 
     const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t full = smem_addr(bars), empty = full + 8 * PIPE, ready = empty + 8 * PIPE, drained = ready + 16,
@@ -376,7 +400,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
                 store_staged(&p.store[i], staging + flip, row0, col0, p.out[i].dtype, v);
                 flip ^= kStageOut;
             } else {
-                store_direct(p.out[i], row0, col0, p.m, p.n, v);
+                store_direct(p.out[i], staging, row0, col0, p.m, p.n, v);
             }
         };
         for (int t = pair; t < tiles; t += pairs, ++local) {
@@ -387,7 +411,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
             const uint32_t buf = local & 1, acc = tmem + buf * kSecond + (uint32_t(quarter * 32) << 16);
             const uint32_t done = peer_addr(FP4 ? drained : drained + 8 * buf, 0);
             float ra = 1.0f;
-            if (KIND == kNv && row0 + lane < p.m) ra = p.row_a[row0 + lane];
+            if (KIND == kNv) {
+                // the factors of the tile's columns, gate before up, while the products run
+                if (row0 + lane < p.m) ra = p.row_a[row0 + lane];
+                const int i = threadIdx.x, col = n0 + i % width;
+                const float f = i < p.bn && col < p.n ? p.row_b[MODE == kGated && i >= width][col] : 0.0f;
+                factors[buf][i] = f;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
             if (!barrier_wait(ready + 8 * buf, local / 2 & 1, &abort)) break;
             __syncwarp();
             fence_after();
@@ -413,12 +444,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-                if (KIND == kNv) scale_columns(v, ra, p.row_b[0], col0, p.n);
+                if (KIND == kNv) scale_columns(v, ra, factors[buf] + 32 * u);
                 if constexpr (MODE == kGated) {
                     float w[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) w[j] = __uint_as_float(q[j]);
-                    if (KIND == kNv) scale_columns(w, ra, p.row_b[1], col0, p.n);
+                    if (KIND == kNv) scale_columns(w, ra, factors[buf] + width + 32 * u);
                     float h[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) h[j] = act(v[j], p.act) * w[j];
