@@ -438,12 +438,9 @@ int readable(Operand& o, size_t rows, size_t cols, uint8_t*& ws, cudaStream_t st
     a.dst = reinterpret_cast<uint16_t*>(ws);
     a.ld_src = o.ld;
     a.ld_dst = up(cols, 8);
-    a.rows = int(rows);
     a.cols = int(cols);
-    int sms;
-    TRY(current_device(sms));
-    const size_t groups = rows * (a.ld_dst / 8);
-    TRY(launch(pack_kernel, dim3(unsigned(std::min<size_t>(ceil_div(groups, 256), size_t(sms) * 8))), 256, 0, 1, a, stream));
+    const int threads = int(std::min<size_t>(512, up(ceil_div(a.ld_dst, 4), 32)));
+    TRY(launch(pack_kernel, dim3(unsigned(rows)), threads, 0, 1, a, stream));
     ws += copy_bytes(rows, cols, o.ld);
     o.p = a.dst;
     o.ld = a.ld_dst;
@@ -684,13 +681,12 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     e.ld_dh = lddh;
     e.ld_gu = ldgu;
     e.ld_out = ldd;
-    e.rows = int(m);
     e.cols = int(f);
     e.act = act;
     e.dtype = dtype;
     e.vec = lddh % 8 == 0 && ldgu % 8 == 0;
-    TRY(launch(gate_grad_kernel, dim3(unsigned(std::min<size_t>(ceil_div(m * (ldd / 8), 256), size_t(sms) * 8))), 256, 0, 1, e,
-               stream));
+    const int threads = int(std::min<size_t>(512, up(ceil_div(f, 8 * kGradGroups), 32)));
+    TRY(launch(gate_grad_kernel, dim3(unsigned(m)), threads, 0, 1, e, stream));
 
     // dx = dG Wg + dU Wu: the reduction runs over f, twice
     if (m <= kFewTokensGradient) {

@@ -482,52 +482,55 @@ struct GradArgs {
     const void *dh, *g, *u;
     void *dg, *du;
     size_t ld_dh, ld_gu, ld_out;      // ld_out is a multiple of 8; columns [cols, ld_out) are not read
-    int rows, cols, act, dtype, vec;
+    int cols, act, dtype, vec;        // vec: rows of dh, g and u start on multiples of 16 bytes
 };
-__global__ void __launch_bounds__(256) gate_grad_kernel(const __grid_constant__ GradArgs p) {
+constexpr int kGradGroups = 2;        // groups of 8 elements of a thread, loaded together
+
+// One CTA a row.
+__global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ GradArgs p) {
+    const size_t row = blockIdx.x;
+    const int span = blockDim.x * 8;
+    const uint16_t* const dh = static_cast<const uint16_t*>(p.dh) + row * p.ld_dh;
+    const uint16_t* const g = static_cast<const uint16_t*>(p.g) + row * p.ld_gu;
+    const uint16_t* const u = static_cast<const uint16_t*>(p.u) + row * p.ld_gu;
     grid_launch();
     grid_wait();
-    const int per_row = (p.cols + 7) / 8;
-    const size_t total = size_t(p.rows) * per_row;
-    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += size_t(gridDim.x) * 256) {
-        const size_t row = i / per_row;
-        const int col = int(i % per_row) * 8, n = min(8, p.cols - col);
-        float dh[8], g[8], u[8], dg[8], du[8];
-        if (p.vec && n == 8) {
-            const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.dh) + row * p.ld_dh + col);
-            const uint4 b = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.g) + row * p.ld_gu + col);
-            const uint4 c = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.u) + row * p.ld_gu + col);
-            const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w}, wc[4] = {c.x, c.y, c.z, c.w};
+    auto load = [&](const uint16_t* src, int col) {
+        if (p.vec && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = col + j < p.cols ? src[col + j] : 0;
+        return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    };
+    for (int first = threadIdx.x * 8; first < p.cols; first += span * kGradGroups) {
+        uint4 a[kGradGroups], b[kGradGroups], c[kGradGroups];
+#pragma unroll
+        for (int i = 0; i < kGradGroups; ++i) {
+            const int col = first + i * span;
+            if (col >= p.cols) continue;
+            a[i] = load(dh, col);
+            b[i] = load(g, col);
+            c[i] = load(u, col);
+        }
+#pragma unroll
+        for (int i = 0; i < kGradGroups; ++i) {
+            const int col = first + i * span;
+            if (col >= p.cols) continue;
+            const uint32_t wa[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, wb[4] = {b[i].x, b[i].y, b[i].z, b[i].w},
+                           wc[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+            uint32_t og[4], ou[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 fa = unpack2(wa[j], p.dtype), fb = unpack2(wb[j], p.dtype), fc = unpack2(wc[j], p.dtype);
-                dh[2 * j] = fa.x; dh[2 * j + 1] = fa.y;
-                g[2 * j] = fb.x; g[2 * j + 1] = fb.y;
-                u[2 * j] = fc.x; u[2 * j + 1] = fc.y;
+                const float2 fh = unpack2(wa[j], p.dtype), fg = unpack2(wb[j], p.dtype), fu = unpack2(wc[j], p.dtype);
+                float v0, v1, s0, s1;
+                act_grad(fg.x, p.act, v0, s0);
+                act_grad(fg.y, p.act, v1, s1);
+                ou[j] = pack2(fh.x * v0, fh.y * v1, p.dtype);
+                og[j] = pack2(fh.x * fu.x * s0, fh.y * fu.y * s1, p.dtype);
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = j < n;
-                dh[j] = in ? load1(p.dh, row * p.ld_dh + col + j, p.dtype) : 0.0f;
-                g[j] = in ? load1(p.g, row * p.ld_gu + col + j, p.dtype) : 0.0f;
-                u[j] = in ? load1(p.u, row * p.ld_gu + col + j, p.dtype) : 0.0f;
-            }
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dg) + row * p.ld_out + col) = make_uint4(og[0], og[1], og[2], og[3]);
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.du) + row * p.ld_out + col) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float a, slope;
-            act_grad(g[j], p.act, a, slope);
-            du[j] = dh[j] * a;
-            dg[j] = dh[j] * u[j] * slope;
-        }
-        uint4 og, ou;
-        og = make_uint4(pack2(dg[0], dg[1], p.dtype), pack2(dg[2], dg[3], p.dtype), pack2(dg[4], dg[5], p.dtype),
-                        pack2(dg[6], dg[7], p.dtype));
-        ou = make_uint4(pack2(du[0], du[1], p.dtype), pack2(du[2], du[3], p.dtype), pack2(du[4], du[5], p.dtype),
-                        pack2(du[6], du[7], p.dtype));
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dg) + row * p.ld_out + col) = og;
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.du) + row * p.ld_out + col) = ou;
     }
 }
 
@@ -536,21 +539,21 @@ struct PackArgs {
     const uint16_t* src;
     uint16_t* dst;
     size_t ld_src, ld_dst;
-    int rows, cols;
+    int cols;
 };
-__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs p) {
+// One CTA a row.  The source is read in words of 4 bytes where its rows start on such, else of 2.
+__global__ void __launch_bounds__(512) pack_kernel(const __grid_constant__ PackArgs p) {
     grid_launch();
     grid_wait();
-    const int per_row = int(p.ld_dst) / 8;
-    const size_t total = size_t(p.rows) * per_row;
-    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += size_t(gridDim.x) * 256) {
-        const size_t row = i / per_row;
-        const int col = int(i % per_row) * 8;
-        uint32_t w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = col + j < p.cols ? p.src[row * p.ld_src + col + j] : 0;
-        *reinterpret_cast<uint4*>(p.dst + row * p.ld_dst + col) =
-            make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    const uint16_t* const src = p.src + blockIdx.x * p.ld_src;
+    uint16_t* const dst = p.dst + blockIdx.x * p.ld_dst;
+    for (int col = threadIdx.x * 2; col < int(p.ld_dst); col += blockDim.x * 2) {
+        uint32_t w;
+        if (p.ld_src % 2 == 0 && col + 2 <= p.cols)
+            w = *reinterpret_cast<const uint32_t*>(src + col);
+        else
+            w = (col < p.cols ? src[col] : 0) | uint32_t(col + 1 < p.cols ? src[col + 1] : 0) << 16;
+        *reinterpret_cast<uint32_t*>(dst + col) = w;
     }
 }
 
