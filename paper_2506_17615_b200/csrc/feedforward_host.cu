@@ -73,7 +73,8 @@ int current_device(int& sms) {
 
 // Clusters of 1 .. 8 CTAs that run at one time when each CTA has an SM to itself: a cluster stays inside a
 // GPC, so this is less than the number of SMs divided by the size.
-int resident_clusters(const void* kernel, int (&out)[9]) {
+int resident_clusters(int (&out)[9]) {
+    const void* const kernel = reinterpret_cast<const void*>(split_kernel<kHalf, kGated, false, false, false>);
     struct Entry {
         int dev, clusters[9];
     };
@@ -88,6 +89,8 @@ int resident_clusters(const void* kernel, int (&out)[9]) {
             std::copy(en.clusters, en.clusters + 9, out);
             return EQUARX_OK;
         }
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSplitSmem));
+    if (e != cudaSuccess) return cuda_failure(e);
     Entry en = {};
     en.dev = dev;
     for (int size = 1; size <= 8; ++size) {
@@ -261,12 +264,6 @@ int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int 
 }
 
 // ---------------------------------------------------------------- launches of the products
-// Tokens up to which the transposed kernel is used.  Measured on both sides (us, transposed / 256-row tiles):
-// 4-bit gated, 5376 -> 2688: 32 tokens 13.2 / 18.2, 64 tokens 17.1 / 18.5, 128 tokens 25.6 / 18.6;
-// 4-bit product, 2688 -> 5376: 32 tokens 16.1 / 13.5, 64 tokens 20.9 / 13.8;
-// 16-bit gated, 5376 -> 2688: 64 tokens 20.8 / 24.9, 128 tokens 37.8 / 24.9;
-// gradients, 5376 -> 2688 (all of the call): 64 tokens 43 / 48, 128 tokens 51 / 50; 2688 -> 5376: 49 / 63.
-constexpr size_t kFewTokensFp4 = 32, kFewTokensGated = 64, kFewTokensGradient = 128;
 // Tokens up to which a product quantizes its own activations.  It saves a launch on the host (13 -> 9 us for
 // the whole call), and on the GPU, warm, 5376 -> 2688, fused / two launches (us): MX 1 token 4.8 / 5.5,
 // 8 tokens 5.7 / 5.8, 16 tokens 7.8 / 5.9; NV, whose rows' maxima go round the cluster first, 1 token
@@ -274,19 +271,24 @@ constexpr size_t kFewTokensFp4 = 32, kFewTokensGated = 64, kFewTokensGradient = 
 constexpr size_t kFusedMxTokens = 8, kFusedNvTokens = 2;
 static_assert(kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, "the fused form takes one tile of tokens");
 
-// Columns of a tile.  The pairs of SMs work through whole rounds of tiles.  A stage takes a pair the time to
-// load (256 + bn) rows of 128 bytes, about as long as the products of the widest tile and longer than those
-// of a narrower one, and a tile costs some stages' time to begin and to drain; a narrower tile may still save
-// a round, or give every pair work when there is little.  4-bit operands: their scales come in groups of 128
+// Columns of a tile, and what the launch is expected to take in cycles of an SM.  The pairs of SMs work
+// through whole rounds of tiles.  A stage takes a pair 1.3 cycles for each of the (256 + bn) rows of 128 bytes
+// that it loads (678 cycles at bn = 256, where the products alone need 512), a tile 3500 to drain, the launch
+// 8000.  A narrower tile loads more for each product, but may save a round, or give every pair work when
+// there is little.  Measured / expected, us: 16-bit gated, 5376 -> 2688, 128 tokens 24.4 / 24.4, 8192 tokens
+// 301 / 325; NV product 5376 -> 2688, 128 tokens 12.1 / 11.6.  4-bit operands: their scales come in groups of 128
 // columns.
-int tile_width(size_t rows, size_t cols, int outputs, size_t stages, bool gated, bool fp4, int sms) {
-    int best = 256;
-    size_t best_cost = ~size_t(0);
+struct TilePlan {
+    int bn;
+    size_t cost;
+};
+TilePlan plan_tiles(size_t rows, size_t cols, int outputs, size_t stages, bool gated, bool fp4, int sms) {
+    TilePlan best = {256, ~size_t(0)};
     const int step = fp4 ? 128 : gated ? 64 : 32;
     for (int bn = 256; bn >= (gated && fp4 ? 256 : step); bn -= step) {
         const size_t tiles = ceil_div(rows, kTileM) * ceil_div(cols, gated ? bn / 2 : bn) * outputs;
-        const size_t cost = ceil_div(tiles, sms / 2) * (256 + bn) * (stages + 4);
-        if (cost < best_cost) best = bn, best_cost = cost;
+        const size_t cost = 8000 + ceil_div(tiles, sms / 2) * (stages * (256 + bn) * 13 / 10 + 3500);
+        if (cost < best.cost) best = {bn, cost};
     }
     return best;
 }
@@ -309,32 +311,57 @@ int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
                   kTileSmem<KIND>, 1, a, stream);
 }
 
-template <int KIND, int MODE, bool W_MN, bool FUSED = false>
-int launch_split(SplitArgs& a, size_t features, size_t tokens, cudaStream_t stream) {
-    a.features = int(features);
-    a.tokens = int(tokens);
-    const size_t tiles = ceil_div(features, kRowsM) * ceil_div(tokens, a.nt);
-    const int total = a.stages * (MODE == kSum2 ? 2 : 1);
+// Shape of a launch of the transposed kernel, and what it is expected to take in cycles of an SM.
+struct SplitPlan {
+    int nt, ranks, pipe, reuse;
+    size_t tiles, smem, cost;
+};
+
+template <int KIND, int MODE, bool X_MN>
+int plan_split(SplitPlan& plan, size_t features, size_t tokens, int total) {
+    // Tiles of at most 128 tokens.  4-bit operands: their scales come in groups of 128 tokens, so more than
+    // one tile means tiles of 128; MN-major operands come in pieces of 64.
+    const size_t unit = X_MN ? 64 : 16, parts_of = ceil_div(tokens, 128);
+    plan.nt = int(KIND != kHalf && tokens > 128 ? 128 : up(ceil_div(tokens, parts_of), unit));
+    plan.tiles = ceil_div(features, kRowsM) * ceil_div(tokens, plan.nt) * (MODE == kOut2 ? 2 : 1);
     // The reduction axis is split over as many CTAs as run at one time for all tiles: at most 8, the
     // portable cluster size.  (5376 -> 2688 gated in 16 bits, one token: 21 tiles of 7 CTAs would take two
     // rounds, 23 us; of 6, one, 14 us.)
-    const auto kernel = split_kernel<KIND, MODE, W_MN, FUSED>;
-    if (const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel))) return cuda_failure(e);
     int clusters[9];
-    TRY(resident_clusters(reinterpret_cast<const void*>(kernel), clusters));
-    int ranks = 1;
+    TRY(resident_clusters(clusters));
+    plan.ranks = 1;
     for (int size = 2; size <= std::min(8, total); ++size)
-        if (size_t(clusters[size]) >= tiles) ranks = size;
-    const int stage = split_stage_bytes<KIND, MODE>(a.nt), parts = split_part_bytes<MODE>(a.nt, ranks);
-    a.pipe = std::min({kSplitMaxPipe, int(ceil_div(total, ranks)), (int(kSplitSmem) - kSmemSlack - parts) / stage});
-    const int columns = (MODE == kGated ? 2 : 1) * (a.nt + 4 * kScaleTiles<KIND>) + 4 * kScaleTiles<KIND>;
-    for (a.columns = 32; a.columns < columns;) a.columns *= 2;
-    const size_t smem = size_t(a.pipe) * stage + parts + kSmemSlack;
-    const dim3 grid(ranks, unsigned(ceil_div(features, kRowsM)), unsigned(ceil_div(tokens, a.nt)));
-    return launch(kernel, grid, kSplitThreads, smem, ranks, a, stream);
+        if (size_t(clusters[size]) >= plan.tiles) plan.ranks = size;
+    const int stage = split_stage_bytes<KIND, MODE>(plan.nt), parts = split_part_bytes<MODE>(plan.nt, plan.ranks);
+    const int room = int(kSplitSmem) - kSmemSlack, wanted = std::min(kSplitMaxPipe, int(ceil_div(total, plan.ranks)));
+    // parts that would cost stages lie where the stages were
+    plan.reuse = room - parts < wanted * stage && plan.nt > kFusedTokens;
+    plan.pipe = std::min(wanted, (plan.reuse ? room : room - parts) / stage);
+    plan.smem = plan.reuse ? kSplitSmem : size_t(plan.pipe) * stage + parts + kSmemSlack;
+    // Fitted to what the kernels take (16 .. 8192 tokens, 256 .. 5376 wide): 8500 cycles to start and end, a
+    // stage's loads at 32 bytes a cycle, and for each token of a tile the exchange of its sums.  Measured /
+    // expected, us: 16-bit gated, 5376 -> 2688, 128 tokens 21.2 / 21; 1000 -> 700, 64 tokens 8.1 / 8.4; NV product
+    // 5376 -> 2688, 128 tokens 11.0 / 10.5; dx, 2688 -> 5376, 128 tokens 17.5 / 24.
+    const size_t rounds = ceil_div(plan.tiles, clusters[plan.ranks]);
+    const size_t token = MODE == kGated ? 65 + 90 / plan.ranks : 40 + 80 / plan.ranks;
+    plan.cost = 8500 + rounds * (ceil_div(total, plan.ranks) * (stage / 32) + plan.nt * token);
+    return EQUARX_OK;
 }
 
-inline int token_tile(size_t tokens) { return int(std::min<size_t>(128, up(tokens, 16))); }
+template <int KIND, int MODE, bool W_MN, bool X_MN, bool FUSED>
+int launch_split(SplitArgs& a, const SplitPlan& plan, size_t features, size_t tokens, cudaStream_t stream) {
+    a.features = int(features);
+    a.tokens = int(tokens);
+    a.nt = plan.nt;
+    a.pipe = plan.pipe;
+    a.reuse = plan.reuse;
+    a.own = int(ceil_div(plan.nt, plan.ranks));
+    const int columns = (MODE == kGated ? 2 : 1) * (a.nt + 4 * kScaleTiles<KIND>) + 4 * kScaleTiles<KIND>;
+    for (a.columns = 32; a.columns < columns;) a.columns *= 2;
+    const dim3 grid(plan.ranks, unsigned(ceil_div(features, kRowsM)),
+                    unsigned(ceil_div(tokens, a.nt) * (MODE == kOut2 ? 2 : 1)));
+    return launch(split_kernel<KIND, MODE, W_MN, X_MN, FUSED>, grid, kSplitThreads, plan.smem, plan.ranks, a, stream);
+}
 
 // weights of the transposed kernel
 template <int KIND, int MODE>
@@ -352,21 +379,23 @@ int split_weights(SplitArgs& a, const Fp4* w, size_t n, size_t k) {
 template <int KIND, int MODE>
 int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, cudaStream_t stream) {
     const size_t stride = codes_stride(k);
-    if (m <= kFewTokensFp4) {
+    int sms;
+    TRY(current_device(sms));
+    const TilePlan tiles = plan_tiles(m, n, 1, fp4_stages(k), MODE == kGated, true, sms);
+    SplitPlan split;
+    TRY((plan_split<KIND, MODE, false>(split, n, m, int(fp4_stages(k)))));
+    if (split.cost < tiles.cost) {
         SplitArgs a = {};
-        a.nt = token_tile(m);
         TRY((split_weights<KIND, MODE>(a, w, n, k)));
-        TRY(make_map(a.x[0], x.codes, 1, stride, m, stride, a.nt));
+        TRY(make_map(a.x[0], x.codes, 1, stride, m, stride, split.nt));
         a.scales_x = x.scales;
         a.row_x = x.row_scales;
         a.out[0] = out;
         a.act = act;
-        return launch_split<KIND, MODE, false>(a, n, m, stream);
+        return launch_split<KIND, MODE, false, false, false>(a, split, n, m, stream);
     }
     TileArgs a = {};
-    int sms;
-    TRY(current_device(sms));
-    a.bn = tile_width(m, n, 1, fp4_stages(k), MODE == kGated, true, sms);
+    a.bn = tiles.bn;
     const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
     TRY(make_map(a.a[0], x.codes, 1, stride, m, stride, kRowsM));
     TRY(scale_map(a.scales_a, x.scales, m, k, format));
@@ -410,12 +439,13 @@ int quantized_product(const QuantArgs& x, const Fp4* w, size_t m, size_t n, size
     const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
     if (quantizes_itself(m, format)) {
         SplitArgs a = {};
-        a.nt = kFusedTokens;
+        SplitPlan split;
+        TRY((plan_split<KIND, MODE, false>(split, n, m, int(fp4_stages(k)))));
         TRY((split_weights<KIND, MODE>(a, w, n, k)));
         a.raw = x;
         a.out[0] = out;
         a.act = act;
-        return launch_split<KIND, MODE, false, true>(a, n, m, stream);
+        return launch_split<KIND, MODE, false, false, true>(a, split, n, m, stream);
     }
     const Fp4 q = carve(workspace, m, k, format);
     TRY(quantize(x.x, x.dtype, m, k, x.ld, format, q, stream));
@@ -600,12 +630,16 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     TRY(readable(ou, f, k, ws, stream));
     const Out oh = out_rows(h, ldh, dtype), sg = out_rows(g, ldgu, dtype), su = out_rows(u, ldgu, dtype);
     const int stages = int(ceil_div(k, 64));
-    if (m <= kFewTokensGated) {
+    int sms;
+    TRY(current_device(sms));
+    const TilePlan tiles = plan_tiles(m, f, 1, stages, true, false, sms);
+    SplitPlan split;
+    TRY((plan_split<kHalf, kGated, false>(split, f, m, stages)));
+    if (split.cost < tiles.cost) {
         SplitArgs a = {};
-        a.nt = token_tile(m);
         TRY(map16(a.w[0], og, f, k, kRowsM));
         TRY(map16(a.w[1], ou, f, k, kRowsM));
-        TRY(map16(a.x[0], ox, m, k, a.nt));
+        TRY(map16(a.x[0], ox, m, k, split.nt));
         a.out[0] = oh;
         a.out[1] = sg;
         a.out[2] = su;
@@ -613,12 +647,10 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
         a.act = act;
         a.bf16 = dtype == EQUARX_BF16;
         a.save = g != nullptr;
-        return launch_split<kHalf, kGated, false>(a, f, m, stream);
+        return launch_split<kHalf, kGated, false, false, false>(a, split, f, m, stream);
     }
     TileArgs a = {};
-    int sms;
-    TRY(current_device(sms));
-    a.bn = tile_width(m, f, 1, stages, true, false, sms);
+    a.bn = tiles.bn;
     TRY(map16(a.a[0], ox, m, k, kRowsM));
     TRY(map16(a.b[0], og, f, k, a.bn / 2));
     TRY(map16(a.b[1], ou, f, k, a.bn / 2));
@@ -689,39 +721,55 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     TRY(launch(gate_grad_kernel, dim3(unsigned(m)), threads, 0, 1, e, stream));
 
     // dx = dG Wg + dU Wu: the reduction runs over f, twice
-    if (m <= kFewTokensGradient) {
+    const int fs = int(ceil_div(f, 64)), ms = int(ceil_div(m, 64)), bf16 = dtype == EQUARX_BF16;
+    TilePlan tiles = plan_tiles(m, k, 1, 2 * fs, false, false, sms);
+    SplitPlan split;
+    TRY((plan_split<kHalf, kSum2, false>(split, k, m, 2 * fs)));
+    if (split.cost < tiles.cost) {
         SplitArgs a = {};
-        a.nt = token_tile(m);
         TRY(map16(a.w[0], og, f, k, 64));
         TRY(map16(a.w[1], ou, f, k, 64));
-        TRY(map16(a.x[0], dg, m, f, a.nt));
-        TRY(map16(a.x[1], du, m, f, a.nt));
+        TRY(map16(a.x[0], dg, m, f, split.nt));
+        TRY(map16(a.x[1], du, m, f, split.nt));
         a.out[0] = out_rows(dx, lddx, dtype);
-        a.stages = int(ceil_div(f, 64));
-        a.bf16 = dtype == EQUARX_BF16;
-        TRY((launch_split<kHalf, kSum2, true>(a, k, m, stream)));
+        a.stages = fs;
+        a.bf16 = bf16;
+        TRY((launch_split<kHalf, kSum2, true, false, false>(a, split, k, m, stream)));
     } else {
         TileArgs a = {};
-        a.bn = tile_width(m, k, 1, 2 * ceil_div(f, 64), false, false, sms);
+        a.bn = tiles.bn;
         TRY(map16(a.a[0], dg, m, f, kRowsM));
         TRY(map16(a.a[1], du, m, f, kRowsM));
         TRY(map16(a.b[0], og, f, k, 64));
         TRY(map16(a.b[1], ou, f, k, 64));
         a.out[0] = out_rows(dx, lddx, dtype);
-        a.stages = int(ceil_div(f, 64));
-        a.bf16 = dtype == EQUARX_BF16;
+        a.stages = fs;
+        a.bf16 = bf16;
         TRY((launch_tiles<kHalf, kSum2, false, true>(a, m, k, stream)));
     }
     // dWg = dG^T x, dWu = dU^T x: the reduction runs over the tokens
+    tiles = plan_tiles(f, k, 2, ms, false, false, sms);
+    TRY((plan_split<kHalf, kOut2, true>(split, k, f, ms)));
+    if (split.cost < tiles.cost) {
+        SplitArgs a = {};
+        TRY(map16(a.w[0], ox, m, k, 64));
+        TRY(map16(a.x[0], dg, m, f, 64));
+        TRY(map16(a.x[1], du, m, f, 64));
+        a.out[0] = out_rows(dwg, lddwg, dtype);
+        a.out[1] = out_rows(dwu, lddwu, dtype);
+        a.stages = ms;
+        a.bf16 = bf16;
+        return launch_split<kHalf, kOut2, true, true, false>(a, split, k, f, stream);
+    }
     TileArgs a = {};
-    a.bn = tile_width(f, k, 2, ceil_div(m, 64), false, false, sms);
+    a.bn = tiles.bn;
     TRY(map16(a.a[0], dg, m, f, 64));
     TRY(map16(a.a[1], du, m, f, 64));
     TRY(map16(a.b[0], ox, m, k, 64));
     a.out[0] = out_rows(dwg, lddwg, dtype);
     a.out[1] = out_rows(dwu, lddwu, dtype);
-    a.stages = int(ceil_div(m, 64));
-    a.bf16 = dtype == EQUARX_BF16;
+    a.stages = ms;
+    a.bf16 = bf16;
     return launch_tiles<kHalf, kOut2, true, true>(a, f, k, stream);
 }
 

@@ -91,6 +91,22 @@ struct Out {
     int vec;      // 1: base and row stride are multiples of 16 bytes
 };
 
+// n <= 4 neighbouring columns of one row, the first a multiple of 4
+__device__ __forceinline__ void store4(const Out& o, size_t row, int col, int n, const float (&v)[4]) {
+    const size_t at = row * o.ld + col;
+    if (n == 4 && o.ld % 4 == 0) {
+        if (o.dtype == kFp32)
+            *reinterpret_cast<float4*>(static_cast<float*>(o.p) + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(o.p) + at) =
+                make_uint2(pack2(v[0], v[1], o.dtype), pack2(v[2], v[3], o.dtype));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) store1(o.p, at + i, v[i], o.dtype);
+    }
+}
+
 constexpr int kStageOut = 32 * 32 * 2;        // bytes of a staged 32 x 32 block of 16-bit outputs
 
 // 32 x 32 outputs of a warp, lane t holding row t, as 16-bit rows of 64 bytes in shared memory; 16-byte
@@ -879,6 +895,8 @@ struct SplitArgs {
     int nt;                           // tokens of a tile: a multiple of 16, at most 128
     int pipe;                         // stages in shared memory
     int columns;                      // of tensor memory: a power of two
+    int own;                          // tokens of a tile that one CTA of the cluster adds up
+    int reuse;                        // the parts lie where the stages were
     int act, bf16, save;
 };
 constexpr int kSplitThreads = 192, kSplitMaxPipe = 12;
@@ -887,24 +905,28 @@ template <int KIND, int MODE>
 __host__ __device__ constexpr int split_stage_bytes(int nt) {
     return (MODE == kGated ? 2 : 1) * (kTileBytes + kScaleBytes<KIND>) + nt * kRowBytes + kScaleBytes<KIND>;
 }
-// rows of the 128 that one of `ranks` CTAs adds up, and the bytes of the parts it receives for them
-__host__ __device__ constexpr int split_rows(int ranks) { return (128 + ranks - 1) / ranks; }
+// bytes of the parts that a CTA receives for the tokens it adds up
 template <int MODE>
 __host__ __device__ constexpr int split_part_bytes(int nt, int ranks) {
-    return ranks * (MODE == kGated ? 2 : 1) * nt * split_rows(ranks) * 4;
+    return ranks * (MODE == kGated ? 2 : 1) * ((nt + ranks - 1) / ranks) * 128 * 4;
 }
 
 // The output transposed: 128 features x nt tokens, so that a single token costs one narrow product over
 // each weight tile instead of a 256-row one, and the weights, which are all the bytes there are, are
 // read once.  The reduction axis is split over the CTAs of a cluster (cluster dimension x) because
 // features / 128 tiles alone would leave most SMs without work.  Each CTA sends its partial sums to the
-// CTAs that own their rows, through distributed shared memory into a place of their own, and the owner
-// adds them in rank order, so the sum does not depend on timing.
+// CTAs that own their tokens, through distributed shared memory, and the owner adds them in rank order, so
+// the sum does not depend on timing.  Few tokens: the parts have a place of their own, and a CTA may send
+// as soon as the others have started; many: they lie where the stages were (`reuse`), once all are done.
+//
+// Gradients: kSum2 with weights whose other axis is contiguous (W_MN); kOut2 with the tokens as the
+// reduction axis (W_MN and X_MN), features = columns of x and "tokens" = rows of a weight, the second half
+// of grid.z being the second output.
 //
 // FUSED (4-bit, at most 16 tokens): x comes in 16 bits; the warps that write the output later quantize
 // the stages of x first, straight into the swizzled rows that the products read, which saves a launch
 // and a round trip of x.
-template <int KIND, int MODE, bool W_MN, bool FUSED>
+template <int KIND, int MODE, bool W_MN, bool X_MN, bool FUSED>
 __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_constant__ SplitArgs p) {
     constexpr bool FP4 = KIND != kHalf, MX = KIND == kMx;
     constexpr int SB = kScaleBytes<KIND>, NW = MODE == kGated ? 2 : 1;
@@ -920,17 +942,20 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
                    drain = ready + 8;
     const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const uint32_t xb = p.nt * kRowBytes, STAGE = NW * (kTileBytes + SB) + xb + SB;
-    const uint32_t parts = smem + p.pipe * STAGE;       // [ranks][NW * nt][split_rows]
+    const uint32_t parts = p.reuse ? 0 : p.pipe * STAGE;      // offset of [ranks][NW][own][128] sums
 
     const int ranks = gridDim.x, rank = uniform(cluster_rank());
     const int total = p.stages * (MODE == kSum2 ? 2 : 1);
     const int s0 = int(int64_t(total) * rank / ranks), s1 = int(int64_t(total) * (rank + 1) / ranks);
-    const int f0 = blockIdx.y * kRowsM, t0 = blockIdx.z * p.nt;
+    const int ztiles = MODE == kOut2 ? gridDim.z / 2 : gridDim.z, which = MODE == kOut2 ? blockIdx.z / ztiles : 0;
+    const int f0 = blockIdx.y * kRowsM, t0 = (blockIdx.z - which * ztiles) * p.nt;
 
     // Tensor memory is waited for when another kernel's CTA still has it.  So that CTAs of two clusters
-    // cannot wait for each other's in a circle, a CTA says that it has started before it asks for tensor
-    // memory, and gives it back before it waits for its cluster's sums.
-    cluster_arrive();
+    // cannot wait for each other's in a circle, no CTA waits for its cluster while it has tensor memory: it
+    // says that it has started before it asks, and gives the memory back before it waits for the sums.  (With `reuse` it says so only when
+    // its products are done; the launch then takes all of an SM's shared memory, and no other CTA with
+    // tensor memory shares the SM.)
+    if (!p.reuse) cluster_arrive();
 
     // the loading warp prepares the barriers and starts; everybody else meets it below
     if (FUSED && threadIdx.x < kFusedTokens) row_max[threadIdx.x] = 0;
@@ -949,9 +974,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             fence_barrier_init();
         }
         __syncwarp();
-    } else if (warp == 5) {
-        tmem_alloc<1>(smem_addr(&tmem_slot), p.columns);
-        fence_before();
     }
     auto load_stage = [&](int it) {
         const int slot = it % p.pipe, s = s0 + it;
@@ -970,7 +992,11 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             if (FP4) bulk_load(ss + SB * q, p.scales_w[q] + (size_t(f0 / 128) * p.stages + ks) * SB, SB, bar);
         }
         if (!FUSED) {
-            tma_load_2d(sx, &p.x[second], kc, t0, bar);
+            if (X_MN) {
+                for (int c = 0; c < p.nt; c += 64) tma_load_2d(sx + c / 64 * kChunkBytes, &p.x[which], t0 + c, kc, bar);
+            } else {
+                tma_load_2d(sx, &p.x[second], kc, t0, bar);
+            }
             if (FP4) bulk_load(ss + SB * NW, p.scales_x + (size_t(t0 / 128) * p.stages + ks) * SB, SB, bar);
         }
     };
@@ -980,10 +1006,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     if (warp == 4) {
         for (int it = 0; it < early; ++it) load_stage(it);
     }
-    __syncthreads();
-    fence_after();
-    const uint32_t tmem = uniform(tmem_slot);
-
     // FUSED.  A unit is one token's part of one stage: 16 groups of 16 elements, half a warp.  The first four
     // warps take the units in the order of the stages, the next one's loads under way.  One body for both
     // 16-bit types and no unrolling: what runs a few times costs mostly the fetching of its instructions.
@@ -1021,6 +1043,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     };
     if constexpr (FUSED && !MX) {
         // The rows' maxima: the cluster's CTAs have the whole of each row between them, and each tells all.
+        __syncthreads();
         cluster_wait();                                 // every CTA of the cluster has started
         if (warp < 4) {
             for_units([&](int, int row, bool in, float (&)[16], uint32_t m) {
@@ -1034,6 +1057,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         __syncwarp();
         cluster_sync();
     }
+    if (warp == 5) {
+        tmem_alloc<1>(smem_addr(&tmem_slot), p.columns);
+        fence_before();
+    }
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = uniform(tmem_slot);
 
     if (warp == 4) {
         bool ok = true;
@@ -1065,7 +1095,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             }
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-                const uint32_t dx = swizzled_desc(sx + 32 * kk, 16);
+                const uint32_t dx = X_MN ? swizzled_desc(sx + 2048 * kk, kChunkBytes) : swizzled_desc(sx + 32 * kk, 16);
 #pragma unroll
                 for (int q = 0; q < NW; ++q) {
                     const uint32_t a = sw + q * kTileBytes;
@@ -1075,7 +1105,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
                         mma_fp4<1, MX>(tmem + q * p.nt, dw, dx, desc_fp4(MX, 128, p.nt, which),
                                        tw + (q * kScaleTiles<KIND> + j) * 4, tx + 4 * j, it | kk);
                     } else {
-                        mma_16bit<1>(tmem + q * p.nt, dw, dx, desc_16bit(p.bf16, W_MN, false, 128, p.nt), it | kk);
+                        mma_16bit<1>(tmem + q * p.nt, dw, dx, desc_16bit(p.bf16, W_MN, X_MN, 128, p.nt), it | kk);
                     }
                 }
             }
@@ -1114,24 +1144,34 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     }
     // ---------------------------------------------------- partial sums to their owners
     __syncwarp();
-    if constexpr (!FUSED || MX) cluster_wait();         // every CTA of the cluster has started
-    const int rows = split_rows(ranks), wide = NW * p.nt;
+    const int cols = min(p.nt, p.tokens - t0);          // tokens that exist
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    bool good = true;
     if (warp < 4) {
+        good = barrier_wait(ready, 0, &abort);
         __syncwarp();
-        if (barrier_wait(ready, 0, &abort)) {
-            __syncwarp();
-            fence_after();
-            const int row = warp * 32 + lane, owner = row / rows;
-            const int cols = min(p.nt, p.tokens - t0);  // those that exist
-            const uint32_t to = peer_addr(parts + ((rank * wide) * rows + row - owner * rows) * 4, owner);
-            for (int c = 0; c < wide; c += 16) {
-                if (c % p.nt >= cols) continue;
+        fence_after();
+    }
+    if (p.reuse) cluster_arrive();                      // this CTA's loads and products are done
+    if constexpr (!FUSED || MX) cluster_wait();         // the others' memory may be written
+    if (warp < 4 && good) {
+        const uint32_t row = warp * 32 + lane;
+        for (int q = 0; q < NW; ++q) {
+            int owner = 0, local = 0;
+            for (int c = 0; c < cols; c += 16) {
                 uint32_t r[16];
-                tmem_load16(tmem + c + (uint32_t(warp * 32) << 16), r);
+                tmem_load16(tmem + q * p.nt + c + lanes, r);
                 tmem_wait_loads();
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (c % p.nt + j < cols) st_cluster_f32(to + (c + j) * rows * 4, __uint_as_float(r[j]));
+                for (int j = 0; j < 16; ++j) {
+                    if (c + j < cols)
+                        st_cluster_f32(peer_addr(smem + parts + (((rank * NW + q) * p.own + local) * 128 + row) * 4, owner),
+                                       __uint_as_float(r[j]));
+                    if (++local == p.own) {
+                        local = 0;
+                        ++owner;
+                    }
+                }
             }
         }
     }
@@ -1144,31 +1184,41 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     __syncwarp();
     cluster_sync();
 
-    const int first = rank * rows, mine = min(rows, 128 - first), count = min(p.nt, p.tokens - t0) * rows;
-    const float* const sums = reinterpret_cast<const float*>(smem_ptr + p.pipe * STAGE);
+    // A thread adds four neighbouring features of a token.  (One at a time, 128 tokens of 2 parts took 9 us.)
+    const int first = rank * p.own, count = min(p.own, cols - first) * 32;
+    const float4* const sums = reinterpret_cast<const float4*>(smem_ptr + parts);
     for (int e = threadIdx.x; e < count; e += kSplitThreads) {
-        const int t = e / rows, i = e - t * rows, f = f0 + first + i;
-        if (i >= mine || f >= p.features) continue;
-        float v = 0.0f, w = 0.0f;
+        const int t = first + (e >> 5), f = f0 + (e & 31) * 4, n = min(4, p.features - f);
+        if (n <= 0) continue;
+        float v[4] = {}, w[4] = {};
         for (int r = 0; r < ranks; ++r) {
-            v += sums[(r * wide + t) * rows + i];
-            if (MODE == kGated) w += sums[(r * wide + p.nt + t) * rows + i];
+            const float4 a = sums[r * NW * p.own * 32 + e];
+            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+            if (MODE == kGated) {
+                const float4 b = sums[(r * NW + 1) * p.own * 32 + e];
+                w[0] += b.x; w[1] += b.y; w[2] += b.z; w[3] += b.w;
+            }
         }
         if (KIND == kNv) {
             float up, rx;
             if (FUSED) row_factors(row_max[t], up, rx); else rx = p.row_x[t0 + t];
-            v = v * rx * p.row_w[0][f];
-            if (MODE == kGated) w = w * rx * p.row_w[1][f];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i < n) v[i] = v[i] * rx * p.row_w[0][f + i];
+                if (MODE == kGated && i < n) w[i] = w[i] * rx * p.row_w[1][f + i];
+            }
         }
         const size_t row = size_t(t0 + t);
         if (MODE == kGated) {
-            store1(p.out[0].p, row * p.out[0].ld + f, act(v, p.act) * w, p.out[0].dtype);
             if (KIND == kHalf && p.save) {
-                store1(p.out[1].p, row * p.out[1].ld + f, v, p.out[1].dtype);
-                store1(p.out[2].p, row * p.out[2].ld + f, w, p.out[2].dtype);
+                store4(p.out[1], row, f, n, v);
+                store4(p.out[2], row, f, n, w);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = act(v[i], p.act) * w[i];
+            store4(p.out[0], row, f, n, v);
         } else {
-            store1(p.out[0].p, row * p.out[0].ld + f, v, p.out[0].dtype);
+            store4(p.out[which], row, f, n, v);
         }
     }
 }
