@@ -273,8 +273,8 @@ static_assert(kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, 
 
 // Columns of a tile, and what the launch is expected to take in cycles of an SM.  The pairs of SMs work
 // through whole rounds of tiles.  A stage takes a pair 1.3 cycles for each of the (256 + bn) rows of 128 bytes
-// that it loads (678 cycles at bn = 256, where the products alone need 512), a tile 3500 to drain, the launch
-// 8000.  A narrower tile loads more for each product, but may save a round, or give every pair work when
+// that it loads (678 cycles at bn = 256, where the products alone need 512), a tile 3500 to drain (6000 where
+// 256 columns go through the activation), the launch 8000.  A narrower tile loads more for each product, but may save a round, or give every pair work when
 // there is little.  Measured / expected, us: 16-bit gated, 5376 -> 2688, 128 tokens 24.4 / 24.4, 8192 tokens
 // 301 / 325; NV product 5376 -> 2688, 128 tokens 12.1 / 11.6.  4-bit operands: their scales come in groups of 128
 // columns.
@@ -282,12 +282,12 @@ struct TilePlan {
     int bn;
     size_t cost;
 };
-TilePlan plan_tiles(size_t rows, size_t cols, int outputs, size_t stages, bool gated, bool fp4, int sms) {
+TilePlan plan_tiles(size_t tiles_m, size_t cols, size_t stages, bool gated, bool fp4, int sms) {
     TilePlan best = {256, ~size_t(0)};
     const int step = fp4 ? 128 : gated ? 64 : 32;
     for (int bn = 256; bn >= (gated && fp4 ? 256 : step); bn -= step) {
-        const size_t tiles = ceil_div(rows, kTileM) * ceil_div(cols, gated ? bn / 2 : bn) * outputs;
-        const size_t cost = 8000 + ceil_div(tiles, sms / 2) * (stages * (256 + bn) * 13 / 10 + 3500);
+        const size_t tiles = tiles_m * ceil_div(cols, gated ? bn / 2 : bn);
+        const size_t cost = 8000 + ceil_div(tiles, sms / 2) * (stages * (256 + bn) * 13 / 10 + (gated && fp4 ? 6000 : 3500));
         if (cost < best.cost) best = {bn, cost};
     }
     return best;
@@ -299,13 +299,13 @@ int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
     TRY(current_device(sms));
     a.m = int(m);
     a.n = int(n);
-    a.tiles_m = int(ceil_div(m, kTileM));
+    a.tiles_m = int(MODE == kOut2 ? ceil_div(m, kRowsM) : ceil_div(m, kTileM));
     a.tiles_n = int(ceil_div(n, MODE == kGated ? a.bn / 2 : a.bn));
     a.group = 8;
     for (int i = 0; i < 3; ++i)
         if (a.out[i].p && a.out[i].vec && a.out[i].dtype != EQUARX_FP32)
             TRY(make_map(a.store[i], a.out[i].p, 2, n, m, a.out[i].ld * 2, 32, CU_TENSOR_MAP_SWIZZLE_64B));
-    const size_t tiles = size_t(a.tiles_m) * a.tiles_n * (MODE == kOut2 ? 2 : 1);
+    const size_t tiles = size_t(a.tiles_m) * a.tiles_n;
     // a pair of CTAs on the two SMs of each TPC; the kernel declares the cluster
     return launch(tile_kernel<KIND, MODE, A_MN, B_MN>, dim3(unsigned(2 * std::min<size_t>(tiles, sms / 2))), kTileThreads,
                   kTileSmem<KIND>, 1, a, stream);
@@ -381,7 +381,7 @@ int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int ac
     const size_t stride = codes_stride(k);
     int sms;
     TRY(current_device(sms));
-    const TilePlan tiles = plan_tiles(m, n, 1, fp4_stages(k), MODE == kGated, true, sms);
+    const TilePlan tiles = plan_tiles(ceil_div(m, kTileM), n, fp4_stages(k), MODE == kGated, true, sms);
     SplitPlan split;
     TRY((plan_split<KIND, MODE, false>(split, n, m, int(fp4_stages(k)))));
     if (split.cost < tiles.cost) {
@@ -632,7 +632,7 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     const int stages = int(ceil_div(k, 64));
     int sms;
     TRY(current_device(sms));
-    const TilePlan tiles = plan_tiles(m, f, 1, stages, true, false, sms);
+    const TilePlan tiles = plan_tiles(ceil_div(m, kTileM), f, stages, true, false, sms);
     SplitPlan split;
     TRY((plan_split<kHalf, kGated, false>(split, f, m, stages)));
     if (split.cost < tiles.cost) {
@@ -716,13 +716,13 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     e.cols = int(f);
     e.act = act;
     e.dtype = dtype;
-    e.vec = lddh % 8 == 0 && ldgu % 8 == 0;
+    e.vec = lddh % 8 == 0 && ldgu % 8 == 0 ? 16 : lddh % 2 == 0 && ldgu % 2 == 0 ? 4 : 2;
     const int threads = int(std::min<size_t>(512, up(ceil_div(f, 8 * kGradGroups), 32)));
     TRY(launch(gate_grad_kernel, dim3(unsigned(m)), threads, 0, 1, e, stream));
 
     // dx = dG Wg + dU Wu: the reduction runs over f, twice
     const int fs = int(ceil_div(f, 64)), ms = int(ceil_div(m, 64)), bf16 = dtype == EQUARX_BF16;
-    TilePlan tiles = plan_tiles(m, k, 1, 2 * fs, false, false, sms);
+    TilePlan tiles = plan_tiles(ceil_div(m, kTileM), k, 2 * fs, false, false, sms);
     SplitPlan split;
     TRY((plan_split<kHalf, kSum2, false>(split, k, m, 2 * fs)));
     if (split.cost < tiles.cost) {
@@ -734,6 +734,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
         a.out[0] = out_rows(dx, lddx, dtype);
         a.stages = fs;
         a.bf16 = bf16;
+        a.order = kForwarding;
         TRY((launch_split<kHalf, kSum2, true, false, false>(a, split, k, m, stream)));
     } else {
         TileArgs a = {};
@@ -745,10 +746,12 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
         a.out[0] = out_rows(dx, lddx, dtype);
         a.stages = fs;
         a.bf16 = bf16;
+        a.order = kForwarding;
         TRY((launch_tiles<kHalf, kSum2, false, true>(a, m, k, stream)));
     }
-    // dWg = dG^T x, dWu = dU^T x: the reduction runs over the tokens
-    tiles = plan_tiles(f, k, 2, ms, false, false, sms);
+    // dWg = dG^T x, dWu = dU^T x: the reduction runs over the tokens.  Needs nothing of dx's launch, so it begins on
+    // the SMs that dx leaves idle.
+    tiles = plan_tiles(ceil_div(f, kRowsM), k, ms, false, false, sms);
     TRY((plan_split<kHalf, kOut2, true>(split, k, f, ms)));
     if (split.cost < tiles.cost) {
         SplitArgs a = {};
@@ -759,6 +762,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
         a.out[1] = out_rows(dwu, lddwu, dtype);
         a.stages = ms;
         a.bf16 = bf16;
+        a.order = kBeside;
         return launch_split<kHalf, kOut2, true, true, false>(a, split, k, f, stream);
     }
     TileArgs a = {};
@@ -770,6 +774,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     a.out[1] = out_rows(dwu, lddwu, dtype);
     a.stages = ms;
     a.bf16 = bf16;
+    a.order = kBeside;
     return launch_tiles<kHalf, kOut2, true, true>(a, f, k, stream);
 }
 

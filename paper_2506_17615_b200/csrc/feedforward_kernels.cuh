@@ -217,7 +217,7 @@ struct TileArgs {
     int m, n;                             // rows and columns of an output
     int stages;                           // stages of the reduction axis (of each of the two parts of kSum2)
     int tiles_m, tiles_n, bn, group;
-    int act, bf16, save;
+    int act, bf16, save, order;
 };
 
 constexpr int kTileM = 256;               // rows of a tile: 128 in each CTA of a pair
@@ -251,7 +251,8 @@ __device__ __forceinline__ void tile_at(const TileArgs& p, int t, int& mt, int& 
 //
 // kGated: columns [0, bn/2) of the tile, the first CTA's half of b, are x Wg^T and [bn/2, bn) the same
 // columns of x Wu^T, so a thread finds g and u of one element in its own row and writes act(g) u.
-// kSum2: out = a0 b0 + a1 b1.  kOut2: out0 = a0 b0, out1 = a1 b0, tiles of both in one launch.
+// kSum2: out = a0 b0 + a1 b1.  kOut2: out0 = a0 b0, out1 = a1 b0, the rows of both one below the other in
+// blocks of 128: a CTA's block belongs to one of them (21 blocks each of 2688 rows make 21 tiles, not 2 x 11).
 template <int KIND, int MODE, bool A_MN, bool B_MN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
     tile_kernel(const __grid_constant__ TileArgs p) {
@@ -291,12 +292,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
     fence_after();
     const uint32_t tmem = uniform(tmem_slot);
 
-    const int tiles = p.tiles_m * p.tiles_n * (MODE == kOut2 ? 2 : 1);
+    const int tiles = p.tiles_m * p.tiles_n;
     const int stages = p.stages * (MODE == kSum2 ? 2 : 1);
     const int half = p.bn / 2;                          // columns of b in each CTA
     const int width = MODE == kGated ? half : p.bn;     // output columns of a tile
-    grid_launch();
-    grid_wait();
+    // this CTA's rows of row tile mt, and the output they belong to
+    auto rows_of = [&](int mt, int& which) {
+        const int block = mt * 2 + rank, blocks = (p.m + kRowsM - 1) / kRowsM;
+        which = MODE == kOut2 && block >= blocks;
+        return (block - which * blocks) * kRowsM;
+    };
+    grid_begin(p.order);
 
     if (warp == kEpilogueWarps + 1) {
         {
@@ -304,10 +310,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
             uint32_t it = 0;
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs) {
-                const int which = MODE == kOut2 ? t >= p.tiles_m * p.tiles_n : 0;
-                int mt, nt;
-                tile_at(p, t - which * p.tiles_m * p.tiles_n, mt, nt);
-                const int m0 = mt * kTileM + rank * kRowsM;
+                int mt, nt, which;
+                tile_at(p, t, mt, nt);
+                const int m0 = rows_of(mt, which);
                 const int n0 = nt * width + (MODE == kGated ? 0 : rank * half);
                 // scales: 128-row groups of a (the second may not exist) and of b (each CTA takes all)
                 const int groups_a = FP4 ? (p.m + 127) / 128 : 0, ga = mt * 2 + rank;
@@ -420,10 +425,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
             }
         };
         for (int t = pair; t < tiles; t += pairs, ++local) {
-            const int which = MODE == kOut2 ? t >= p.tiles_m * p.tiles_n : 0;
-            int mt, nt;
-            tile_at(p, t - which * p.tiles_m * p.tiles_n, mt, nt);
-            const int row0 = mt * kTileM + rank * kRowsM + quarter * 32, n0 = nt * width;
+            int mt, nt, which;
+            tile_at(p, t, mt, nt);
+            const int row0 = rows_of(mt, which) + quarter * 32, n0 = nt * width;
             const uint32_t buf = local & 1, acc = tmem + buf * kSecond + (uint32_t(quarter * 32) << 16);
             const uint32_t done = peer_addr(FP4 ? drained : drained + 8 * buf, 0);
             float ra = 1.0f;
@@ -489,6 +493,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
         fence_after();
         tmem_free<2>(tmem, 512);
     }
+    grid_end(p.order);
 }
 
 // ---------------------------------------------------------------- 16-bit rows, element by element
@@ -498,7 +503,7 @@ struct GradArgs {
     const void *dh, *g, *u;
     void *dg, *du;
     size_t ld_dh, ld_gu, ld_out;      // ld_out is a multiple of 8; columns [cols, ld_out) are not read
-    int cols, act, dtype, vec;        // vec: rows of dh, g and u start on multiples of 16 bytes
+    int cols, act, dtype, vec;        // vec: rows of dh, g and u start on multiples of so many bytes (16, 4 or 2)
 };
 constexpr int kGradGroups = 2;        // groups of 8 elements of a thread, loaded together
 
@@ -512,7 +517,11 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
     grid_launch();
     grid_wait();
     auto load = [&](const uint16_t* src, int col) {
-        if (p.vec && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
+        if (p.vec == 16 && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
+        if (p.vec == 4 && col + 8 <= p.cols) {
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(src + col);
+            return make_uint4(q[0], q[1], q[2], q[3]);
+        }
         uint32_t w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = col + j < p.cols ? src[col + j] : 0;
@@ -897,7 +906,7 @@ struct SplitArgs {
     int columns;                      // of tensor memory: a power of two
     int own;                          // tokens of a tile that one CTA of the cluster adds up
     int reuse;                        // the parts lie where the stages were
-    int act, bf16, save;
+    int act, bf16, save, order;
 };
 constexpr int kSplitThreads = 192, kSplitMaxPipe = 12;
 constexpr int kFusedTokens = 16;      // tokens of a tile of the fused form
@@ -1000,8 +1009,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             if (FP4) bulk_load(ss + SB * NW, p.scales_x + (size_t(t0 / 128) * p.stages + ks) * SB, SB, bar);
         }
     };
-    grid_launch();
-    grid_wait();
+    grid_begin(p.order);
     const int early = min(s1 - s0, p.pipe);
     if (warp == 4) {
         for (int it = 0; it < early; ++it) load_stage(it);
@@ -1221,6 +1229,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             store4(p.out[which], row, f, n, v);
         }
     }
+    grid_end(p.order);
 }
 
 }  // namespace ff

@@ -104,7 +104,23 @@ __device__ __forceinline__ void max_cluster_u32(uint32_t cluster_addr, uint32_t 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// A kernel's place in a sequence of dependent launches.
+//   kOrdered    reads what the launch before wrote: waits for it before anything else
+//   kForwarding the same, and lets the next launch begin only then, so that the next one may count on
+//               everything up to the launch before this one
+//   kBeside     behind a kForwarding launch whose outputs it does not touch: runs beside it and waits for it
+//               only at its end, so that what follows still finds both complete
+enum Order { kOrdered = 0, kForwarding = 1, kBeside = 2 };
 __device__ __forceinline__ void grid_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+__device__ __forceinline__ void grid_begin(int order) {
+    if (order != kForwarding) grid_launch();
+    if (order != kBeside) grid_wait();
+    if (order == kForwarding) grid_launch();
+}
+__device__ __forceinline__ void grid_end(int order) {
+    if (order == kBeside) grid_wait();
+}
 
 // ---------------------------------------------------------------- instructions of one thread
 // Loads and products are issued by one lane of a warp whose 32 lanes run the loop together: with uniform
