@@ -71,6 +71,6 @@ __all__ = list(_BINDING_NAMES) + ["binding", "workloads"]
 def __getattr__(name):
     if name in _BINDING_NAMES:
         return getattr(importlib.import_module(".binding", __name__), name)
-    if name in ("binding", "workloads", "ring", "feedforward"):
+    if name in ("binding", "workloads", "ring", "feedforward", "block"):
         return importlib.import_module("." + name, __name__)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -71,25 +71,33 @@ class Fp4Matrix:
         return self.data[first:first + 4 * self.rows].view(torch.float32)
 
 
-def _matrix(t, what, rows=None, cols=None, dtype=None, device=None):
-    """t's shape, row stride and device, after the checks"""
+def _matrix(t, what):
+    """t's shape, row stride, type and device, after the checks"""
     if t.dim() != 2:
         raise ValueError(f"{what} must be a matrix")
     r, c = t.shape
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    dtype = t.dtype
+    if dtype not in _DTYPES:
+        raise ValueError(f"{what} has type {dtype}")
+    return r, c, _row_stride(t, what, r, c), dtype, dev
+
+
+def _row_stride(t, what, r, c):
     ld, unit = t.stride()
     if unit != 1 and c > 1:
         raise ValueError(f"{what} must have contiguous columns")
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
-    if (rows is not None and r != rows) or (cols is not None and c != cols):
-        raise ValueError(f"{what} is ({r}, {c}), expected ({rows}, {cols})")
-    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{what} has type {t.dtype}")
-    dev = t.get_device()
-    if device is not None and dev != device:
-        raise ValueError(f"{what} is on device {dev}, expected {device}")
     # torch reports any stride for a single row
-    return r, c, ld if r > 1 else max(ld, c), dev
+    return ld if r > 1 else max(ld, c)
+
+
+def _fits(t, what, r, c, dtype, dev):
+    """t's row stride, where t has to be r x c, of this type and on this device"""
+    if t.shape != (r, c) or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what} is {tuple(t.shape)} {t.dtype} on device {t.get_device()}, expected ({r}, {c}) {dtype} on {dev}")
+    return _row_stride(t, what, r, c)
 
 
 def _call(device, fn, *args):
@@ -114,9 +122,9 @@ def _workspace(like, nbytes):
 
 def fp4_quantize(x, format=FP4_NV):
     """x [rows, cols], bfloat16, float16 or float32 -> Fp4Matrix."""
-    rows, cols, ld, dev = _matrix(x, "x")
+    rows, cols, ld, dtype, dev = _matrix(x, "x")
     q = Fp4Matrix(x.new_empty(Fp4Matrix.nbytes(rows, cols, format), dtype=torch.uint8), rows, cols, format)
-    _call(dev, _lib.equarx_fp4_quantize, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, format, *q._parts)
+    _call(dev, _lib.equarx_fp4_quantize, x.data_ptr(), _DTYPES[dtype], rows, cols, ld, format, *q._parts)
     return q
 
 
@@ -143,11 +151,13 @@ def fp4_matmul(a, b, dtype=torch.bfloat16):
 
 def fp4_linear(x, w):
     """x w^T: x [tokens, k] in 16 bits is quantized in the call, w is an Fp4Matrix [n, k]."""
-    m, k, ld, dev = _matrix(x, "x", None, w.cols, None, w.data.get_device())
+    m, k, ld, dtype, dev = _matrix(x, "x")
+    if k != w.cols or dev != w.data.get_device():
+        raise ValueError(f"x has {k} columns on device {dev}, the weight {w.cols} on {w.data.get_device()}")
     out = x.new_empty((m, w.rows))
     nbytes = _linear_workspace(m, k, w.format)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_fp4_linear, x.data_ptr(), _DTYPES[x.dtype], ld, *w._parts, m, w.rows, k, w.format, out.data_ptr(),
+    _call(dev, _lib.equarx_fp4_linear, x.data_ptr(), _DTYPES[dtype], ld, *w._parts, m, w.rows, k, w.format, out.data_ptr(),
           w.rows, ptr, nbytes)
     return out
 
@@ -156,54 +166,48 @@ def fp4_gated(x, wg, wu, act=ACT_GELU_TANH):
     """act(x wg^T) * (x wu^T): x [tokens, k] in 16 bits, wg and wu Fp4Matrix [f, k] of one format."""
     if wg.rows != wu.rows or wg.cols != wu.cols or wg.format != wu.format:
         raise ValueError("the two weights differ in shape or format")
-    m, k, ld, dev = _matrix(x, "x", None, wg.cols, None, wg.data.get_device())
-    if wu.data.get_device() != dev:
-        raise ValueError("the two weights are on different devices")
+    m, k, ld, dtype, dev = _matrix(x, "x")
+    if k != wg.cols or dev != wg.data.get_device() or dev != wu.data.get_device():
+        raise ValueError(f"x has {k} columns on device {dev}, the weights {wg.cols} on {wg.data.get_device()}, {wu.data.get_device()}")
     h = x.new_empty((m, wg.rows))
     nbytes = _linear_workspace(m, k, wg.format)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_fp4_gated, x.data_ptr(), _DTYPES[x.dtype], ld, *wg._parts, *wu._parts, m, wg.rows, k, wg.format,
+    _call(dev, _lib.equarx_fp4_gated, x.data_ptr(), _DTYPES[dtype], ld, *wg._parts, *wu._parts, m, wg.rows, k, wg.format,
           act, h.data_ptr(), wg.rows, ptr, nbytes)
     return h
 
 
 def gated_forward(x, wg, wu, act=ACT_GELU_TANH, save=False):
     """h = act(x wg^T) * (x wu^T) for x [tokens, k], wg and wu [f, k], all bfloat16 or all float16.
-    With save: (h, g, u), where g and u are the two projections that gated_backward needs (the two halves
-    of one allocation)."""
-    m, k, ldx, dev = _matrix(x, "x")
-    f, _, ldg, _ = _matrix(wg, "wg", None, k, x.dtype, dev)
-    _, _, ldu, _ = _matrix(wu, "wu", f, k, x.dtype, dev)
+    With save: (h, g, u), where g and u are the two projections that gated_backward needs."""
+    m, k, ldx, dtype, dev = _matrix(x, "x")
+    f = wg.shape[0]
+    ldg, ldu = _fits(wg, "wg", f, k, dtype, dev), _fits(wu, "wu", f, k, dtype, dev)
     h = x.new_empty((m, f))
-    gu, gp, up = None, 0, 0
+    g = u = None
     if save:
-        half = _up(m * f, 8)                 # the second half starts on a multiple of 16 bytes
-        gu = x.new_empty(2 * half)
-        gp = gu.data_ptr()
-        up = gp + 2 * half
+        g, u = torch.empty_like(h), torch.empty_like(h)
     nbytes = _forward_workspace(m, f, k, ldx, ldg, ldu)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_gated_forward, x.data_ptr(), ldx, wg.data_ptr(), ldg, wu.data_ptr(), ldu, _DTYPES[x.dtype], m, f, k,
-          act, h.data_ptr(), f, gp, up, f, ptr, nbytes)
-    if not save:
-        return h
-    return h, gu.as_strided((m, f), (f, 1), 0), gu.as_strided((m, f), (f, 1), half)
+    _call(dev, _lib.equarx_gated_forward, x.data_ptr(), ldx, wg.data_ptr(), ldg, wu.data_ptr(), ldu, _DTYPES[dtype], m, f, k,
+          act, h.data_ptr(), f, g.data_ptr() if save else 0, u.data_ptr() if save else 0, f, ptr, nbytes)
+    return (h, g, u) if save else h
 
 
 def gated_backward(dh, x, wg, wu, g, u, act=ACT_GELU_TANH):
     """(dx, dwg, dwu) of gated_forward from dh [tokens, f] and the g and u it saved."""
-    m, k, ldx, dev = _matrix(x, "x")
-    f, _, ldwg, _ = _matrix(wg, "wg", None, k, x.dtype, dev)
-    _, _, ldwu, _ = _matrix(wu, "wu", f, k, x.dtype, dev)
-    _, _, lddh, _ = _matrix(dh, "dh", m, f, x.dtype, dev)
-    _, _, ldgu, _ = _matrix(g, "g", m, f, x.dtype, dev)
-    if _matrix(u, "u", m, f, x.dtype, dev)[2] != ldgu:
+    m, k, ldx, dtype, dev = _matrix(x, "x")
+    f = wg.shape[0]
+    ldwg, ldwu = _fits(wg, "wg", f, k, dtype, dev), _fits(wu, "wu", f, k, dtype, dev)
+    lddh, ldgu = _fits(dh, "dh", m, f, dtype, dev), _fits(g, "g", m, f, dtype, dev)
+    if _fits(u, "u", m, f, dtype, dev) != ldgu:
         raise ValueError("g and u have different row strides")
-    dx, dwg, dwu = x.new_empty((m, k)), x.new_empty((f, k)), x.new_empty((f, k))
+    dx, dwg = x.new_empty((m, k)), x.new_empty((f, k))
+    dwu = torch.empty_like(dwg)
     nbytes = _backward_workspace(m, f, k, ldx, ldwg, ldwu)
     ws, ptr = _workspace(x, nbytes)
     _call(dev, _lib.equarx_gated_backward, dh.data_ptr(), lddh, x.data_ptr(), ldx, wg.data_ptr(), ldwg, wu.data_ptr(), ldwu,
-          g.data_ptr(), u.data_ptr(), ldgu, _DTYPES[x.dtype], m, f, k, act, dx.data_ptr(), k, dwg.data_ptr(), k, dwu.data_ptr(),
+          g.data_ptr(), u.data_ptr(), ldgu, _DTYPES[dtype], m, f, k, act, dx.data_ptr(), k, dwg.data_ptr(), k, dwu.data_ptr(),
           k, ptr, nbytes)
     return dx, dwg, dwu
 

@@ -213,7 +213,8 @@ def check_quantized(x, fmt):
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 @pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 16, 0), (3, 17, 0), (5, 31, 2), (128, 256, 0), (129, 257, 7),
-                                           (33, 500, 12), (1, 5376, 0), (1300, 96, 0), (1200, 1001, 0), (300, 2050, 6)])
+                                           (33, 500, 12), (1, 5376, 0), (1300, 96, 0), (1200, 1001, 0), (300, 2050, 6),
+                                           (2, 24576, 0), (3, 30001, 0)])
 def test_quantize_matches_the_definition(fmt, dtype, rows, cols, pad):
     check_quantized(normal(rows, cols, rows + cols, dtype, 3.0, pad), fmt)
 
@@ -247,7 +248,8 @@ def test_not_finite_elements_become_nan(fmt):
 
 SIZES = [(1, 1, 1), (1, 16, 32), (1, 130, 300), (3, 100, 64), (16, 128, 256), (17, 129, 257), (64, 257, 1000),
          (127, 300, 513), (128, 64, 96), (129, 128, 256), (130, 300, 500), (257, 129, 777), (300, 513, 1030),
-         (520, 1000, 2000), (1025, 260, 64)]
+         (520, 1000, 2000), (1025, 260, 64), (2, 140, 2049), (8, 700, 1500), (9, 129, 1025), (16, 260, 4100), (128, 300, 5000),
+         (64, 520, 3000)]
 
 
 @gpu
@@ -303,7 +305,8 @@ def backward_reference(dh, x, wg, wu, g, u, act, unit):
 
 
 TRAIN = [(1, 1, 1), (1, 64, 64), (2, 130, 72), (16, 128, 256), (33, 65, 129), (128, 200, 300), (129, 256, 128),
-         (200, 77, 1001), (257, 300, 513), (512, 520, 264), (1030, 128, 200)]
+         (200, 77, 1001), (257, 300, 513), (512, 520, 264), (1030, 128, 200), (128, 256, 3000), (4100, 100, 136), (2100, 130, 65),
+         (100, 1500, 96)]
 
 
 @gpu
@@ -452,6 +455,99 @@ def test_strided_outputs_and_no_writes_outside(m, f, k):
                           inner(px), k + extra, inner(pwg), k + extra, inner(pwu), k + extra, ws, nb, stream)
         for t, want, rows in ((px, grads0[0], m), (pwg, grads0[1], f), (pwu, grads0[2], f)):
             assert torch.equal(split(t, rows, k), want)
+    ff.check()
+
+
+@gpu
+def test_offsets_beyond_32_bits():
+    """rows 2^26 elements apart: the last ones lie more than 4 GB (and 2^32 elements) after the first"""
+    rows, ld = 70, 1 << 26
+    store = torch.empty((rows - 1) * ld + 4096, dtype=torch.bfloat16, device="cuda")
+    x = store.as_strided((rows, 96), (ld, 1))
+    x.copy_(normal(rows, 96, 1, torch.bfloat16))
+    w, wu = normal(40, 96, 2, torch.bfloat16), normal(40, 96, 3, torch.bfloat16)
+    dense = x.contiguous()
+    for fmt in FORMATS:
+        q = ff.fp4_quantize(w, fmt)
+        assert torch.equal(ff.fp4_linear(x, q), ff.fp4_linear(dense, q))
+    h, g, u = ff.gated_forward(dense, w, wu, save=True)
+    assert torch.equal(ff.gated_forward(x, w, wu), h)
+    for a, b in zip(ff.gated_backward(h, x, w, wu, g, u), ff.gated_backward(h, dense, w, wu, g, u)):
+        assert torch.equal(a, b)
+    # and outputs that far apart: h beside x, in the same rows
+    out = store.as_strided((rows, 40), (ld, 1), 1024)
+    stream = torch.cuda.current_stream().cuda_stream
+    eq.gated_forward(dense, 96, w, 96, wu, 96, eq.BF16, rows, 40, 96, eq.ACT_GELU_TANH, out.data_ptr(), ld, 0, 0, 0, 0, 0, stream)
+    assert torch.equal(out, h)
+    q = ff.fp4_quantize(dense)
+    eq.fp4_dequantize(*q._parts, rows, 96, eq.FP4_NV, store.as_strided((rows, 96), (ld, 1), 2048).data_ptr(), eq.BF16, ld, stream)
+    assert torch.equal(store.as_strided((rows, 96), (ld, 1), 2048), ff.fp4_dequantize(q))
+    ff.check()
+
+
+@gpu
+def test_results_do_not_depend_on_the_other_tokens():
+    """NV and MX: a token's result is the same alone and among others of the same form of the product"""
+    w, wu = normal(300, 500, 2, torch.bfloat16), normal(300, 500, 3, torch.bfloat16)
+    x = normal(2000, 500, 1, torch.bfloat16)
+    for fmt in FORMATS:
+        q, qu = ff.fp4_quantize(w, fmt), ff.fp4_quantize(wu, fmt)
+        whole = ff.fp4_matmul(ff.fp4_quantize(x, fmt), q, torch.float32)
+        some = ff.fp4_matmul(ff.fp4_quantize(x[700:1700], fmt), q, torch.float32)
+        assert torch.equal(whole[700:1700], some)
+        assert torch.equal(ff.fp4_gated(x, q, qu)[700:1700], ff.fp4_gated(x[700:1700], q, qu))
+
+
+@gpu
+def test_backward_overlaps_nothing_it_must_not():
+    """The launches of a backward pass overlap; called back to back on the same buffers, with their outputs
+    feeding the next call, they give what separate calls give."""
+    x, wg, wu = normal(400, 256, 1, torch.bfloat16), normal(200, 256, 2, torch.bfloat16, 0.1), normal(200, 256, 3, torch.bfloat16, 0.1)
+
+    def steps(sync):
+        a, w0, w1, out = x.clone(), wg.clone(), wu.clone(), []
+        for _ in range(6):
+            h, g, u = ff.gated_forward(a, w0, w1, save=True)
+            dx, d0, d1 = ff.gated_backward(h, a, w0, w1, g, u)
+            if sync:
+                torch.cuda.synchronize()
+            out.append((h, dx, d0, d1))
+            a, w0, w1 = dx, d0, d1                         # every output is the next call's input
+            if sync:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return out
+
+    for p, q in zip(steps(False), steps(True)):
+        for s, t in zip(p, q):
+            assert torch.equal(s.view(torch.int16), t.view(torch.int16))
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_block_with_the_allreduce(fmt):
+    """Four ranks' slices of a block, their partial sums added by the quantized AllReduce: the same bits as
+    the CPU oracle gives for these partial sums; close to the unsharded block in 16 bits."""
+    import oracle
+    from paper_2506_17615_b200 import block as blk, workloads as wl
+    ranks, tokens, hidden, width = 4, 96, 256, 1024
+    b = blk.Block(ranks, hidden, width, ff.ACT_SILU, fmt, seed=3)
+    x, dy = normal(tokens, hidden, 1, torch.bfloat16), normal(tokens, hidden, 2, torch.bfloat16)
+    for parts in (b.partials(x), [dx for dx, _, _ in b.train_partials(x, dy)]):
+        want = oracle.allreduce(wl.as_u16(torch.stack([p.reshape(-1) for p in parts])), 256)["out"]
+        got = b.allreduce([p.clone() for p in parts])
+        for r in range(ranks):
+            assert (wl.as_u16(got[r].reshape(-1)) == want[r]).all()
+    y_ref, dx_ref = blk.reference(b, x, dy)
+    dx, dwg, dwu = b.train(x, dy)
+    # 4 ranks' bf16 roundings and the AllReduce's int8 steps: each int8 step is at most 1/254 of its block's
+    # largest element, about 3 times the block's rms, so 4 steps stay below 4 * 3 / 254 = 0.05 of the norm
+    assert float((dx.float() - dx_ref).norm() / dx_ref.norm()) < 0.06
+    assert len(dwg) == ranks and all(t.shape == (width // ranks, hidden) for t in dwg + dwu)
+    # 4 bits: an element is off by at most a quarter of itself (2^-2, halfway between 1 and 1.5), which
+    # bounds each of the three quantised products' relative error by 2 * 0.25
+    y = b.serve(x)
+    assert float((y.float() - y_ref).norm() / y_ref.norm()) < 0.5
     ff.check()
 
 
