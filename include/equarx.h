@@ -421,8 +421,10 @@ int equarx_ring_allreduce(const void *const *in_bf16, void *const *out_bf16,
  * Conventions, in addition to those at the top of this file
  *   - Matrices are row-major: element (r, c) of a matrix with row stride ld is at
  *     index r * ld + c; ld counts elements and is at least the number of columns.
- *     Bases are 16-byte aligned; row strides are free (a 16-bit operand whose row
- *     stride is no multiple of 8 elements is first copied into the workspace).
+ *     Bases are aligned to their elements and row strides are free; rows that start
+ *     on multiples of 16 bytes are read and written fastest (a 16-bit operand of
+ *     gated_forward or gated_backward whose rows do not is first copied into the
+ *     workspace).
  *   - A dimension is at most 2^30.  Zero tokens are allowed (nothing is launched,
  *     gradients of weights become zero); the other dimensions are at least 1.
  *   - Element types: EQUARX_BF16, EQUARX_FP16 and, where a call says so,
@@ -513,10 +515,12 @@ int equarx_fp4_gated(const void *x, int dtype, size_t ldx,
  * h = act(x Wg^T) * (x Wu^T) over 16-bit weights, in one kernel: x is m x k, wg and wu
  * are f x k, h is m x f, all of one type (BF16 or FP16).  g and u, both m x f with row
  * stride ldgu, receive the projections x Wg^T and x Wu^T for the backward call; both
- * are NULL when no gradient is wanted.  Workspace (the copies that row strides make
- * necessary, often 0 bytes): equarx_gated_forward_workspace_bytes.
+ * are NULL when no gradient is wanted.  Workspace (the copies that alignment makes
+ * necessary, often 0 bytes): equarx_gated_forward_workspace_bytes, which looks at the
+ * alignment of the pointers and strides and reads nothing.
  */
-size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu);
+size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, const void *x, size_t ldx,
+                                             const void *wg, size_t ldwg, const void *wu, size_t ldwu);
 int equarx_gated_forward(const void *x, size_t ldx, const void *wg, size_t ldwg, const void *wu, size_t ldwu,
                          int dtype, size_t m, size_t f, size_t k, int act,
                          void *h, size_t ldh, void *g, void *u, size_t ldgu,
@@ -528,7 +532,8 @@ int equarx_gated_forward(const void *x, size_t ldx, const void *wg, size_t ldwg,
  * dU and dG are computed in fp32 and rounded to the 16-bit type that the products read.
  * dx is m x k, dwg and dwu are f x k, of the inputs' type.
  */
-size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu);
+size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, const void *x, size_t ldx,
+                                             const void *wg, size_t ldwg, const void *wu, size_t ldwu);
 int equarx_gated_backward(const void *dh, size_t lddh, const void *x, size_t ldx,
                           const void *wg, size_t ldwg, const void *wu, size_t ldwu,
                           const void *g, const void *u, size_t ldgu,

@@ -98,9 +98,9 @@ def _load():
     lib.equarx_fp4_linear_workspace_bytes.argtypes = [sz, sz, ci]
     lib.equarx_fp4_linear.argtypes = [vp, ci, sz, vp, vp, vp, sz, sz, sz, ci, vp, sz, vp, sz, vp]
     lib.equarx_fp4_gated.argtypes = [vp, ci, sz] + [vp] * 6 + [sz, sz, sz, ci, ci, vp, sz, vp, sz, vp]
-    lib.equarx_gated_forward_workspace_bytes.argtypes = [sz] * 6
+    lib.equarx_gated_forward_workspace_bytes.argtypes = [sz, sz, sz, vp, sz, vp, sz, vp, sz]
     lib.equarx_gated_forward.argtypes = [vp, sz, vp, sz, vp, sz, ci, sz, sz, sz, ci, vp, sz, vp, vp, sz, vp, sz, vp]
-    lib.equarx_gated_backward_workspace_bytes.argtypes = [sz] * 6
+    lib.equarx_gated_backward_workspace_bytes.argtypes = [sz, sz, sz, vp, sz, vp, sz, vp, sz]
     lib.equarx_gated_backward.argtypes = [vp, sz, vp, sz, vp, sz, vp, sz, vp, vp, sz, ci, sz, sz, sz, ci, vp, sz, vp, sz,
                                           vp, sz, vp, sz, vp]
     for name in ("fp4_codes_bytes", "fp4_scales_bytes", "fp4_linear_workspace_bytes", "gated_forward_workspace_bytes",
@@ -302,8 +302,8 @@ def fp4_gated(x, dtype, ldx, g_codes, g_scales, g_row_scales, u_codes, u_scales,
            "equarx_fp4_gated")
 
 
-def gated_forward_workspace_bytes(m, f, k, ldx, ldwg, ldwu):
-    return lib.equarx_gated_forward_workspace_bytes(m, f, k, ldx, ldwg, ldwu)
+def gated_forward_workspace_bytes(m, f, k, x, ldx, wg, ldwg, wu, ldwu):
+    return lib.equarx_gated_forward_workspace_bytes(m, f, k, _ptr(x), ldx, _ptr(wg), ldwg, _ptr(wu), ldwu)
 
 
 def gated_forward(x, ldx, wg, ldwg, wu, ldwu, dtype, m, f, k, act, h, ldh, g, u, ldgu, workspace, workspace_bytes, stream=0):
@@ -312,8 +312,8 @@ def gated_forward(x, ldx, wg, ldwg, wu, ldwu, dtype, m, f, k, act, h, ldh, g, u,
            "equarx_gated_forward")
 
 
-def gated_backward_workspace_bytes(m, f, k, ldx, ldwg, ldwu):
-    return lib.equarx_gated_backward_workspace_bytes(m, f, k, ldx, ldwg, ldwu)
+def gated_backward_workspace_bytes(m, f, k, x, ldx, wg, ldwg, wu, ldwu):
+    return lib.equarx_gated_backward_workspace_bytes(m, f, k, _ptr(x), ldx, _ptr(wg), ldwg, _ptr(wu), ldwu)
 
 
 def gated_backward(dh, lddh, x, ldx, wg, ldwg, wu, ldwu, g, u, ldgu, dtype, m, f, k, act, dx, lddx, dwg, lddwg, dwu, lddwu,

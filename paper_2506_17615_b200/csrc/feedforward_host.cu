@@ -49,6 +49,11 @@ inline bool is_16bit(int dtype) { return dtype == EQUARX_BF16 || dtype == EQUARX
 inline bool is_float(int dtype) { return is_16bit(dtype) || dtype == EQUARX_FP32; }
 inline bool is_format(int f) { return f == EQUARX_FP4_MX || f == EQUARX_FP4_NV; }
 inline bool is_act(int a) { return a == EQUARX_ACT_SILU || a == EQUARX_ACT_GELU_TANH; }
+// bytes, at most 16, that a base and a row stride are multiples of
+inline int unit_of(const void* p, size_t ld, size_t size) {
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (ld * size) | 16;
+    return int(bits & (~bits + 1));
+}
 inline size_t size_of(int dtype) { return dtype == EQUARX_FP32 ? 4 : 2; }
 
 inline size_t codes_stride(size_t cols) { return ceil_div(cols, 32) * 16; }
@@ -209,7 +214,7 @@ int scale_map(CUtensorMap& map, const uint8_t* scales, size_t rows, size_t cols,
     } while (0)
 
 inline Out out_rows(void* p, size_t ld, int dtype) {
-    return Out{p, ld, dtype, int(aligned(p, 16) && ld * size_of(dtype) % 16 == 0)};
+    return Out{p, ld, dtype, unit_of(p, ld, size_of(dtype))};
 }
 
 // ---------------------------------------------------------------- 4-bit matrices
@@ -252,7 +257,7 @@ QuantArgs rows_to_quantize(const void* x, int dtype, size_t rows, size_t cols, s
     a.rows = int(rows);
     a.cols = int(cols);
     a.dtype = dtype;
-    a.vec = ld * size_of(dtype) % 16 == 0;
+    a.unit = unit_of(x, ld, size_of(dtype));
     return a;
 }
 int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int format, const Fp4& q, cudaStream_t stream) {
@@ -303,7 +308,7 @@ int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
     a.tiles_n = int(ceil_div(n, MODE == kGated ? a.bn / 2 : a.bn));
     a.group = 8;
     for (int i = 0; i < 3; ++i)
-        if (a.out[i].p && a.out[i].vec && a.out[i].dtype != EQUARX_FP32)
+        if (a.out[i].p && a.out[i].unit == 16 && a.out[i].dtype != EQUARX_FP32)
             TRY(make_map(a.store[i], a.out[i].p, 2, n, m, a.out[i].ld * 2, 32, CU_TENSOR_MAP_SWIZZLE_64B));
     const size_t tiles = size_t(a.tiles_m) * a.tiles_n;
     // a pair of CTAs on the two SMs of each TPC; the kernel declares the cluster
@@ -453,25 +458,28 @@ int quantized_product(const QuantArgs& x, const Fp4* w, size_t m, size_t n, size
 }
 
 // ---------------------------------------------------------------- 16-bit operands
-// TMA reads rows whose stride is a multiple of 16 bytes; others are copied
-inline bool needs_copy(size_t ld) { return ld % 8 != 0; }
-inline size_t copy_bytes(size_t rows, size_t cols, size_t ld) { return needs_copy(ld) ? up(rows * up(cols, 8) * 2, 256) : 0; }
+// TMA reads rows that start on multiples of 16 bytes; others are copied
+inline bool needs_copy(const void* p, size_t ld) { return unit_of(p, ld, 2) < 16; }
+inline size_t copy_bytes(size_t rows, size_t cols, const void* p, size_t ld) {
+    return needs_copy(p, ld) ? up(rows * up(cols, 8) * 2, 256) : 0;
+}
 
 struct Operand {
     const void* p;
     size_t ld;
 };
 int readable(Operand& o, size_t rows, size_t cols, uint8_t*& ws, cudaStream_t stream) {
-    if (!needs_copy(o.ld)) return EQUARX_OK;
+    if (!needs_copy(o.p, o.ld)) return EQUARX_OK;
     PackArgs a = {};
     a.src = static_cast<const uint16_t*>(o.p);
     a.dst = reinterpret_cast<uint16_t*>(ws);
     a.ld_src = o.ld;
     a.ld_dst = up(cols, 8);
     a.cols = int(cols);
+    a.unit = unit_of(o.p, o.ld, 2);
     const int threads = int(std::min<size_t>(512, up(ceil_div(a.ld_dst, 4), 32)));
     TRY(launch(pack_kernel, dim3(unsigned(rows)), threads, 0, 1, a, stream));
-    ws += copy_bytes(rows, cols, o.ld);
+    ws += copy_bytes(rows, cols, o.p, o.ld);
     o.p = a.dst;
     o.ld = a.ld_dst;
     return EQUARX_OK;
@@ -500,7 +508,7 @@ int equarx_fp4_quantize(const void* x, int dtype, size_t rows, size_t cols, size
     const Fp4 q{codes, scales, row_scales};
     if (!x) return EQUARX_ERR_NULL;
     TRY(check_fp4(q, format));
-    if (!aligned(x, 16)) return EQUARX_ERR_ALIGN;
+    if (!aligned(x, size_of(dtype))) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(x, rows, cols, ld, size_of(dtype))},
                       {codes_span(q, rows, cols), scales_span(q, rows, cols, format), rows_span(q, rows, format)}));
     return quantize(x, dtype, rows, cols, ld, format, q, stream);
@@ -514,7 +522,7 @@ int equarx_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, const flo
     const Fp4 q{codes, scales, row_scales};
     if (!out) return EQUARX_ERR_NULL;
     TRY(check_fp4(q, format));
-    if (!aligned(out, 16)) return EQUARX_ERR_ALIGN;
+    if (!aligned(out, size_of(dtype))) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({codes_span(q, rows, cols), scales_span(q, rows, cols, format), rows_span(q, rows, format)},
                       {matrix(out, rows, cols, ld, size_of(dtype))}));
     DequantArgs a = {};
@@ -526,7 +534,7 @@ int equarx_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, const flo
     a.rows = int(rows);
     a.cols = int(cols);
     a.dtype = dtype;
-    a.vec = ld * size_of(dtype) % 16 == 0;
+    a.unit = unit_of(out, ld, size_of(dtype));
     const dim3 grid{unsigned(rows)};
     const int threads = row_threads(cols);
     return format == EQUARX_FP4_MX ? launch(fp4_dequantize_kernel<true>, grid, threads, 0, 1, a, stream)
@@ -543,7 +551,7 @@ int equarx_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const flo
     if (!out) return EQUARX_ERR_NULL;
     TRY(check_fp4(a, format));
     TRY(check_fp4(b, format));
-    if (!aligned(out, 16)) return EQUARX_ERR_ALIGN;
+    if (!aligned(out, size_of(dtype))) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({codes_span(a, m, k), scales_span(a, m, k, format), rows_span(a, m, format), codes_span(b, n, k),
                        scales_span(b, n, k, format), rows_span(b, n, format)},
                       {matrix(out, m, n, ld, size_of(dtype))}));
@@ -567,7 +575,7 @@ int equarx_fp4_linear(const void* x, int dtype, size_t ldx, const uint8_t* w_cod
     if (!x || !out || (need && !workspace)) return EQUARX_ERR_NULL;
     TRY(check_fp4(w, format));
     if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
-    if (!aligned(x, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    if (!aligned(x, 2) || !aligned(out, 2) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(x, m, k, ldx, 2), codes_span(w, n, k), scales_span(w, n, k, format), rows_span(w, n, format)},
                       {matrix(out, m, n, ld, 2), Span{workspace, need}}));
     const QuantArgs a = rows_to_quantize(x, dtype, m, k, ldx);
@@ -589,7 +597,7 @@ int equarx_fp4_gated(const void* x, int dtype, size_t ldx, const uint8_t* g_code
     TRY(check_fp4(w[0], format));
     TRY(check_fp4(w[1], format));
     if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
-    if (!aligned(x, 16) || !aligned(h, 16) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    if (!aligned(x, 2) || !aligned(h, 2) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(x, m, k, ldx, 2), codes_span(w[0], f, k), scales_span(w[0], f, k, format),
                        rows_span(w[0], f, format), codes_span(w[1], f, k), scales_span(w[1], f, k, format),
                        rows_span(w[1], f, format)},
@@ -600,9 +608,10 @@ int equarx_fp4_gated(const void* x, int dtype, size_t ldx, const uint8_t* g_code
                                    : quantized_product<kNv, kGated>(a, w, m, f, k, act, o, workspace, stream);
 }
 
-size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu) {
+size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, const void* x, size_t ldx, const void* wg, size_t ldwg,
+                                             const void* wu, size_t ldwu) {
     if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k)) return 0;
-    return copy_bytes(m, k, ldx) + copy_bytes(f, k, ldwg) + copy_bytes(f, k, ldwu);
+    return copy_bytes(m, k, x, ldx) + copy_bytes(f, k, wg, ldwg) + copy_bytes(f, k, wu, ldwu);
 }
 
 int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg, const void* wu, size_t ldwu, int dtype,
@@ -614,12 +623,12 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     if (m == 0) return EQUARX_OK;
     if (!x || !wg || !wu || !h || (!g) != (!u)) return EQUARX_ERR_NULL;
     if (g && bad_ld(ldgu, f)) return EQUARX_ERR_COUNT;
-    const size_t need = equarx_gated_forward_workspace_bytes(m, f, k, ldx, ldwg, ldwu);
+    const size_t need = equarx_gated_forward_workspace_bytes(m, f, k, x, ldx, wg, ldwg, wu, ldwu);
     if (need && !workspace) return EQUARX_ERR_NULL;
     if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
-    for (const void* p : {x, wg, wu, static_cast<const void*>(h), static_cast<const void*>(g), static_cast<const void*>(u),
-                          static_cast<const void*>(workspace)})
-        if (!aligned(p, 16)) return EQUARX_ERR_ALIGN;
+    for (const void* p : {x, wg, wu, static_cast<const void*>(h), static_cast<const void*>(g), static_cast<const void*>(u)})
+        if (!aligned(p, 2)) return EQUARX_ERR_ALIGN;
+    if (!aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(x, m, k, ldx, 2), matrix(wg, f, k, ldwg, 2), matrix(wu, f, k, ldwu, 2)},
                       {matrix(h, m, f, ldh, 2), matrix(g, m, f, ldgu, 2), matrix(u, m, f, ldgu, 2), Span{workspace, need}}));
 
@@ -664,9 +673,10 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     return launch_tiles<kHalf, kGated, false, false>(a, m, f, stream);
 }
 
-size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, size_t ldx, size_t ldwg, size_t ldwu) {
+size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, const void* x, size_t ldx, const void* wg, size_t ldwg,
+                                             const void* wu, size_t ldwu) {
     if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k)) return 0;
-    return copy_bytes(m, k, ldx) + copy_bytes(f, k, ldwg) + copy_bytes(f, k, ldwu) + 2 * up(m * up(f, 8) * 2, 256);
+    return copy_bytes(m, k, x, ldx) + copy_bytes(f, k, wg, ldwg) + copy_bytes(f, k, wu, ldwu) + 2 * up(m * up(f, 8) * 2, 256);
 }
 
 int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx, const void* wg, size_t ldwg, const void* wu,
@@ -678,11 +688,12 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
         bad_ld(ldgu, f) || bad_ld(lddx, k) || bad_ld(lddwg, k) || bad_ld(lddwu, k))
         return EQUARX_ERR_COUNT;
     if (!dwg || !dwu || (m && (!dh || !x || !wg || !wu || !g || !u || !dx || !workspace))) return EQUARX_ERR_NULL;
-    const size_t need = equarx_gated_backward_workspace_bytes(m, f, k, ldx, ldwg, ldwu);
+    const size_t need = equarx_gated_backward_workspace_bytes(m, f, k, x, ldx, wg, ldwg, wu, ldwu);
     if (m && workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
     for (const void* p : {dh, x, wg, wu, g, u, static_cast<const void*>(dx), static_cast<const void*>(dwg),
-                          static_cast<const void*>(dwu), static_cast<const void*>(workspace)})
-        if (!aligned(p, 16)) return EQUARX_ERR_ALIGN;
+                          static_cast<const void*>(dwu)})
+        if (!aligned(p, 2)) return EQUARX_ERR_ALIGN;
+    if (!aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(dh, m, f, lddh, 2), matrix(x, m, k, ldx, 2), matrix(wg, f, k, ldwg, 2),
                        matrix(wu, f, k, ldwu, 2), matrix(g, m, f, ldgu, 2), matrix(u, m, f, ldgu, 2)},
                       {matrix(dx, m, k, lddx, 2), matrix(dwg, f, k, lddwg, 2), matrix(dwu, f, k, lddwu, 2),
@@ -716,7 +727,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     e.cols = int(f);
     e.act = act;
     e.dtype = dtype;
-    e.vec = lddh % 8 == 0 && ldgu % 8 == 0 ? 16 : lddh % 2 == 0 && ldgu % 2 == 0 ? 4 : 2;
+    e.unit = std::min({unit_of(dh, lddh, 2), unit_of(g, ldgu, 2), unit_of(u, ldgu, 2)});
     const int threads = int(std::min<size_t>(512, up(ceil_div(f, 8 * kGradGroups), 32)));
     TRY(launch(gate_grad_kernel, dim3(unsigned(m)), threads, 0, 1, e, stream));
 

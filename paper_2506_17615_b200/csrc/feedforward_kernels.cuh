@@ -88,13 +88,13 @@ struct Out {
     void* p;
     size_t ld;
     int dtype;
-    int vec;      // 1: base and row stride are multiples of 16 bytes
+    int unit;     // bytes that base and row stride are multiples of: 16, 8, 4 or 2
 };
 
 // n <= 4 neighbouring columns of one row, the first a multiple of 4
 __device__ __forceinline__ void store4(const Out& o, size_t row, int col, int n, const float (&v)[4]) {
     const size_t at = row * o.ld + col;
-    if (n == 4 && o.ld % 4 == 0) {
+    if (n == 4 && o.unit >= (o.dtype == kFp32 ? 16 : 8)) {
         if (o.dtype == kFp32)
             *reinterpret_cast<float4*>(static_cast<float*>(o.p) + at) = make_float4(v[0], v[1], v[2], v[3]);
         else
@@ -136,7 +136,7 @@ __device__ __forceinline__ void store_staged(const CUtensorMap* map, uint32_t bu
 }
 
 // To any other output.  16-bit: neighbouring lanes write a row's neighbouring columns, in units of 8, 4 or
-// 2 bytes as the row stride allows; each lane writing its own row would touch every sector many times.
+// 2 bytes as base and row stride allow; each lane writing its own row would touch every sector many times.
 // fp32: each lane writes its own row.
 __device__ __forceinline__ void store_direct(const Out& o, uint32_t buf, int row0, int col0, int rows, int cols,
                                              const float (&v)[32]) {
@@ -144,7 +144,7 @@ __device__ __forceinline__ void store_direct(const Out& o, uint32_t buf, int row
     if (o.dtype == kFp32) {
         float* q = static_cast<float*>(o.p) + size_t(row0 + lane) * o.ld + col0;
         if (row0 + int(lane) >= rows) return;
-        if (o.vec && col0 + 32 <= cols) {
+        if (o.unit == 16 && col0 + 32 <= cols) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 reinterpret_cast<float4*>(q)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
@@ -161,7 +161,7 @@ __device__ __forceinline__ void store_direct(const Out& o, uint32_t buf, int row
     __syncwarp();
     uint16_t* const base = static_cast<uint16_t*>(o.p) + size_t(row0) * o.ld + col0;
     const int height = min(32, rows - row0), width = min(32, cols - col0);
-    if (o.ld % 4 == 0) {
+    if (o.unit >= 8) {
         const int c = (lane & 7) * 4;
 #pragma unroll 4
         for (int r = lane >> 3; r < height; r += 4) {
@@ -176,7 +176,7 @@ __device__ __forceinline__ void store_direct(const Out& o, uint32_t buf, int row
                 if (c + 2 < width) q[2] = uint16_t(b);
             }
         }
-    } else if (o.ld % 2 == 0) {
+    } else if (o.unit == 4) {
         const int c = (lane & 15) * 2;
 #pragma unroll 4
         for (int r = lane >> 4; r < height; r += 2) {
@@ -417,7 +417,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
         const uint32_t staging = smem + PIPE * STAGE + warp * 2 * kStageOut;
         auto store = [&](int i, int row0, int col0, float (&v)[32]) {
             if (row0 >= p.m || col0 >= p.n) return;
-            if (p.out[i].vec && p.out[i].dtype != kFp32) {
+            if (p.out[i].unit == 16 && p.out[i].dtype != kFp32) {
                 store_staged(&p.store[i], staging + flip, row0, col0, p.out[i].dtype, v);
                 flip ^= kStageOut;
             } else {
@@ -503,7 +503,7 @@ struct GradArgs {
     const void *dh, *g, *u;
     void *dg, *du;
     size_t ld_dh, ld_gu, ld_out;      // ld_out is a multiple of 8; columns [cols, ld_out) are not read
-    int cols, act, dtype, vec;        // vec: rows of dh, g and u start on multiples of so many bytes (16, 4 or 2)
+    int cols, act, dtype, unit;       // unit: bytes that the rows of dh, g and u start on multiples of
 };
 constexpr int kGradGroups = 2;        // groups of 8 elements of a thread, loaded together
 
@@ -517,8 +517,8 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
     grid_launch();
     grid_wait();
     auto load = [&](const uint16_t* src, int col) {
-        if (p.vec == 16 && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
-        if (p.vec == 4 && col + 8 <= p.cols) {
+        if (p.unit == 16 && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
+        if (p.unit >= 4 && col + 8 <= p.cols) {
             const uint32_t* q = reinterpret_cast<const uint32_t*>(src + col);
             return make_uint4(q[0], q[1], q[2], q[3]);
         }
@@ -564,7 +564,7 @@ struct PackArgs {
     const uint16_t* src;
     uint16_t* dst;
     size_t ld_src, ld_dst;
-    int cols;
+    int cols, unit;
 };
 // One CTA a row.  The source is read in words of 4 bytes where its rows start on such, else of 2.
 __global__ void __launch_bounds__(512) pack_kernel(const __grid_constant__ PackArgs p) {
@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(512) pack_kernel(const __grid_constant__ PackA
     uint16_t* const dst = p.dst + blockIdx.x * p.ld_dst;
     for (int col = threadIdx.x * 2; col < int(p.ld_dst); col += blockDim.x * 2) {
         uint32_t w;
-        if (p.ld_src % 2 == 0 && col + 2 <= p.cols)
+        if (p.unit >= 4 && col + 2 <= p.cols)
             w = *reinterpret_cast<const uint32_t*>(src + col);
         else
             w = (col < p.cols ? src[col] : 0) | uint32_t(col + 1 < p.cols ? src[col + 1] : 0) << 16;
@@ -599,7 +599,7 @@ struct QuantArgs {
     uint8_t *codes, *scales;
     float* row_scales;
     size_t ld;
-    int rows, cols, dtype, vec;       // vec: base and row stride are multiples of 16 bytes
+    int rows, cols, dtype, unit;      // unit: bytes that base and row stride are multiples of: 16, 8, 4 or 2
 };
 
 // eight codes, the first in the lowest nibble
@@ -654,7 +654,7 @@ template <int DT> struct Group {
 template <int DT>
 __device__ __forceinline__ void load_group(const QuantArgs& p, size_t row, int col, Group<DT>& g) {
     constexpr int W = DT == kFp32 ? 16 : 8, PER = 16 / W;
-    if (p.vec && col + 16 <= p.cols) {
+    if (p.unit == 16 && col + 16 <= p.cols) {
         const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (row * p.ld + col) * (4 / PER));
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
@@ -665,7 +665,7 @@ __device__ __forceinline__ void load_group(const QuantArgs& p, size_t row, int c
         const uint32_t* q = static_cast<const uint32_t*>(p.x) + row * p.ld;
 #pragma unroll
         for (int i = 0; i < W; ++i) g.w[i] = col + i < p.cols ? q[col + i] : 0;
-    } else if (p.ld % 2 == 0 && col + 16 <= p.cols) {      // rows start on multiples of 4 bytes
+    } else if (p.unit >= 4 && col + 16 <= p.cols) {
         const uint32_t* q = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.x) + row * p.ld + col);
 #pragma unroll
         for (int i = 0; i < W; ++i) g.w[i] = q[i];
@@ -833,7 +833,7 @@ struct DequantArgs {
     const float* row_scales;
     void* out;
     size_t ld;
-    int rows, cols, dtype, vec;
+    int rows, cols, dtype, unit;
 };
 // value = code * scale (MX), code * (scale * row factor) (NV) in fp32, rounded once to the output type.
 // One CTA a row as above: a thread's three groups are in flight together.
@@ -865,7 +865,7 @@ __global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_consta
             decode8(w[c].y, v + 8);
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = __fmul_rn(v[j], d);
-            if (p.vec && col + 16 <= p.cols) {
+            if (p.unit == 16 && col + 16 <= p.cols) {
                 if (p.dtype == kFp32) {
                     float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * p.ld + col);
 #pragma unroll
@@ -877,7 +877,7 @@ __global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_consta
                         q[j] = make_uint4(pack2(v[8 * j], v[8 * j + 1], p.dtype), pack2(v[8 * j + 2], v[8 * j + 3], p.dtype),
                                           pack2(v[8 * j + 4], v[8 * j + 5], p.dtype), pack2(v[8 * j + 6], v[8 * j + 7], p.dtype));
                 }
-            } else if (p.dtype != kFp32 && p.ld % 2 == 0 && col + 16 <= p.cols) {
+            } else if (p.dtype != kFp32 && p.unit >= 4 && col + 16 <= p.cols) {
                 uint32_t* q = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + row * p.ld + col);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) q[j] = pack2(v[2 * j], v[2 * j + 1], p.dtype);

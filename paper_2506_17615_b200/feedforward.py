@@ -24,7 +24,7 @@ from .binding import ACT_GELU_TANH, ACT_SILU, FP4_MX, FP4_NV, EquarxError  # noq
 _DTYPES = {torch.bfloat16: binding.BF16, torch.float16: binding.FP16, torch.float32: binding.FP32}
 _lib = binding.lib
 
-# what a call needs beside its tensors depends on its shape alone
+# what a call needs beside its tensors depends on its shape, and on how its rows are aligned
 _scales_bytes = lru_cache(maxsize=4096)(_lib.equarx_fp4_scales_bytes)
 _linear_workspace = lru_cache(maxsize=4096)(_lib.equarx_fp4_linear_workspace_bytes)
 _forward_workspace = lru_cache(maxsize=4096)(_lib.equarx_gated_forward_workspace_bytes)
@@ -187,10 +187,10 @@ def gated_forward(x, wg, wu, act=ACT_GELU_TANH, save=False):
     g = u = None
     if save:
         g, u = torch.empty_like(h), torch.empty_like(h)
-    nbytes = _forward_workspace(m, f, k, ldx, ldg, ldu)
+    xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    nbytes = _forward_workspace(m, f, k, xp & 15, ldx, gp & 15, ldg, up & 15, ldu)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_gated_forward, x.data_ptr(), ldx, wg.data_ptr(), ldg, wu.data_ptr(), ldu, _DTYPES[dtype], m, f, k,
-          act, h.data_ptr(), f, g.data_ptr() if save else 0, u.data_ptr() if save else 0, f, ptr, nbytes)
+    _call(dev, _lib.equarx_gated_forward, xp, ldx, gp, ldg, up, ldu, _DTYPES[dtype], m, f, k, act, h.data_ptr(), f, g.data_ptr() if save else 0, u.data_ptr() if save else 0, f, ptr, nbytes)
     return (h, g, u) if save else h
 
 
@@ -204,10 +204,10 @@ def gated_backward(dh, x, wg, wu, g, u, act=ACT_GELU_TANH):
         raise ValueError("g and u have different row strides")
     dx, dwg = x.new_empty((m, k)), x.new_empty((f, k))
     dwu = torch.empty_like(dwg)
-    nbytes = _backward_workspace(m, f, k, ldx, ldwg, ldwu)
+    xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    nbytes = _backward_workspace(m, f, k, xp & 15, ldx, gp & 15, ldwg, up & 15, ldwu)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_gated_backward, dh.data_ptr(), lddh, x.data_ptr(), ldx, wg.data_ptr(), ldwg, wu.data_ptr(), ldwu,
-          g.data_ptr(), u.data_ptr(), ldgu, _DTYPES[dtype], m, f, k, act, dx.data_ptr(), k, dwg.data_ptr(), k, dwu.data_ptr(),
+    _call(dev, _lib.equarx_gated_backward, dh.data_ptr(), lddh, xp, ldx, gp, ldwg, up, ldwu, g.data_ptr(), u.data_ptr(), ldgu, _DTYPES[dtype], m, f, k, act, dx.data_ptr(), k, dwg.data_ptr(), k, dwu.data_ptr(),
           k, ptr, nbytes)
     return dx, dwg, dwu
 

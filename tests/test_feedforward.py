@@ -33,7 +33,9 @@ def test_quantize_refuses_bad_arguments():
     f, a = eq.fp4_quantize, quantize_args()
     for key in ("x", "codes", "scales", "row_scales"):
         assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
-        assert status_of(f, **{**a, key: a[key] + 2}) == binding.ERR_ALIGN
+        assert status_of(f, **{**a, key: a[key] + 1}) == binding.ERR_ALIGN
+    for key in ("codes", "scales", "row_scales"):
+        assert status_of(f, **{**a, key: a[key] + 8}) == binding.ERR_ALIGN
     for key, bad in (("dtype", 3), ("dtype", -1), ("format", 2), ("format", -1)):
         assert status_of(f, **{**a, key: bad}) == binding.ERR_FORMAT
     for key, bad in (("cols", 0), ("ld", 63), ("rows", GB + 1), ("cols", GB + 1), ("ld", GB + 1)):
@@ -49,7 +51,7 @@ def test_dequantize_refuses_bad_arguments():
              dtype=eq.FP32, ld=64)
     for key in ("codes", "scales", "row_scales", "out"):
         assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
-        assert status_of(f, **{**a, key: a[key] + 4}) == binding.ERR_ALIGN
+        assert status_of(f, **{**a, key: a[key] + 2}) == binding.ERR_ALIGN
     assert status_of(f, **{**a, "dtype": 9}) == binding.ERR_FORMAT
     assert status_of(f, **{**a, "ld": 60}) == binding.ERR_COUNT
     assert status_of(f, **{**a, "out": A + 112}) == binding.ERR_ALIAS
@@ -61,7 +63,7 @@ def test_matmul_refuses_bad_arguments():
              b_row_scales=A + 5 * GB, m=4, n=8, k=64, format=eq.FP4_NV, out=A + 6 * GB, dtype=eq.FP16, ld=8)
     for key in ("a_codes", "a_scales", "a_row_scales", "b_codes", "b_scales", "b_row_scales", "out"):
         assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
-        assert status_of(f, **{**a, key: a[key] + 8}) == binding.ERR_ALIGN
+        assert status_of(f, **{**a, key: a[key] + (1 if key == "out" else 8)}) == binding.ERR_ALIGN
     for key, bad in (("n", 0), ("k", 0), ("ld", 7), ("m", GB + 1)):
         assert status_of(f, **{**a, key: bad}) == binding.ERR_COUNT
     for key, bad in (("dtype", 3), ("format", 5)):
@@ -84,7 +86,7 @@ def test_linear_and_gated_refuse_bad_arguments():
         assert len(pointers) == (6 if f is eq.fp4_linear else 9)
         for key in pointers:
             assert status_of(f, **{**args, key: 0}) == binding.ERR_NULL
-            assert status_of(f, **{**args, key: args[key] + 8}) == binding.ERR_ALIGN
+            assert status_of(f, **{**args, key: args[key] + (1 if key in ("x", out) else 8)}) == binding.ERR_ALIGN
         assert status_of(f, **{**args, "workspace_bytes": need - 1}) == binding.ERR_WORKSPACE
         assert status_of(f, **{**args, "dtype": eq.FP32}) == binding.ERR_FORMAT     # activations are 16-bit
         assert status_of(f, **{**args, "ldx": 32}) == binding.ERR_COUNT
@@ -100,7 +102,7 @@ def test_gated_forward_and_backward_refuse_bad_arguments():
     f = eq.gated_forward
     for key in ("x", "wg", "wu", "h", "g", "u"):
         assert status_of(f, **{**fwd, key: 0}) == binding.ERR_NULL
-        assert status_of(f, **{**fwd, key: fwd[key] + 2}) == binding.ERR_ALIGN
+        assert status_of(f, **{**fwd, "workspace": A + 9 * GB, "workspace_bytes": GB, key: fwd[key] + 1}) == binding.ERR_ALIGN
     for key, bad in (("f", 0), ("k", 0), ("ldx", 63), ("ldwg", 63), ("ldwu", 63), ("ldh", 7), ("ldgu", 7)):
         assert status_of(f, **{**fwd, key: bad}) == binding.ERR_COUNT
     for key, bad in (("dtype", eq.FP32), ("act", 2)):
@@ -109,14 +111,14 @@ def test_gated_forward_and_backward_refuse_bad_arguments():
     assert status_of(f, **{**fwd, "ldx": 65}) == binding.ERR_NULL                 # now a workspace is needed
     assert status_of(f, **{**fwd, "ldx": 65, "workspace": A + 9 * GB}) == binding.ERR_WORKSPACE
 
-    need = eq.gated_backward_workspace_bytes(4, 8, 64, 64, 64, 64)
+    need = eq.gated_backward_workspace_bytes(4, 8, 64, A, 64, A, 64, A, 64)
     bwd = dict(dh=A, lddh=8, x=A + GB, ldx=64, wg=A + 2 * GB, ldwg=64, wu=A + 3 * GB, ldwu=64, g=A + 4 * GB, u=A + 5 * GB,
                ldgu=8, dtype=eq.BF16, m=4, f=8, k=64, act=0, dx=A + 6 * GB, lddx=64, dwg=A + 7 * GB, lddwg=64,
                dwu=A + 8 * GB, lddwu=64, workspace=A + 9 * GB, workspace_bytes=need)
     f = eq.gated_backward
     for key in ("dh", "x", "wg", "wu", "g", "u", "dx", "dwg", "dwu", "workspace"):
         assert status_of(f, **{**bwd, key: 0}) == binding.ERR_NULL
-        assert status_of(f, **{**bwd, key: bwd[key] + 4}) == binding.ERR_ALIGN
+        assert status_of(f, **{**bwd, "workspace_bytes": GB, key: bwd[key] + (8 if key == "workspace" else 1)}) == binding.ERR_ALIGN
     for key in ("lddh", "ldgu"):
         assert status_of(f, **{**bwd, key: 7}) == binding.ERR_COUNT
     for key in ("ldx", "ldwg", "ldwu", "lddx", "lddwg", "lddwu"):
@@ -133,9 +135,10 @@ def test_sizes_of_the_buffers():
     assert eq.fp4_scales_bytes(129, 257, eq.FP4_NV) == 2 * 2 * 2048
     assert eq.fp4_scales_bytes(0, 64, eq.FP4_NV) == 0 and eq.fp4_codes_bytes(4, 0) == 0
     assert eq.fp4_scales_bytes(4, 64, 7) == 0
-    assert eq.gated_forward_workspace_bytes(8, 16, 64, 64, 72, 80) == 0
-    assert eq.gated_forward_workspace_bytes(8, 16, 64, 65, 64, 64) == 8 * 64 * 2   # x is copied
-    assert eq.gated_forward_workspace_bytes(8, 16, 64, 63, 64, 64) == 0            # invalid
+    assert eq.gated_forward_workspace_bytes(8, 16, 64, A, 64, A, 72, A, 80) == 0
+    assert eq.gated_forward_workspace_bytes(8, 16, 64, A, 65, A, 64, A, 64) == 8 * 64 * 2        # x is copied
+    assert eq.gated_forward_workspace_bytes(8, 16, 64, A, 64, A, 64, A + 2, 64) == 16 * 64 * 2   # wu is
+    assert eq.gated_forward_workspace_bytes(8, 16, 64, A, 63, A, 64, A, 64) == 0                 # invalid
 
 
 def test_tensors_that_do_not_fit_are_refused():
@@ -442,19 +445,67 @@ def test_strided_outputs_and_no_writes_outside(m, f, k):
             return body
 
         ph, pg, pu = wide(m, f), wide(m, f), wide(m, f)
-        nb = eq.gated_forward_workspace_bytes(m, f, k, k, k, k)
+        nb = eq.gated_forward_workspace_bytes(m, f, k, x, k, wg, k, wu, k)
         ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
         eq.gated_forward(x, k, wg, k, wu, k, eq.BF16, m, f, k, eq.ACT_GELU_TANH, inner(ph), f + extra, inner(pg), inner(pu),
                          f + extra, ws, nb, stream)
         for t, want in ((ph, h0), (pg, g0), (pu, u0)):
             assert torch.equal(split(t, m, f), want)
         px, pwg, pwu = wide(m, k), wide(f, k), wide(f, k)
-        nb = eq.gated_backward_workspace_bytes(m, f, k, k, k, k)
+        nb = eq.gated_backward_workspace_bytes(m, f, k, x, k, wg, k, wu, k)
         ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
         eq.gated_backward(dh, f, x, k, wg, k, wu, k, inner(pg), inner(pu), f + extra, eq.BF16, m, f, k, eq.ACT_GELU_TANH,
                           inner(px), k + extra, inner(pwg), k + extra, inner(pwu), k + extra, ws, nb, stream)
         for t, want, rows in ((px, grads0[0], m), (pwg, grads0[1], f), (pwu, grads0[2], f)):
             assert torch.equal(split(t, rows, k), want)
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("offset", [1, 2, 4, 7])
+@pytest.mark.parametrize("m,f,k", [(5, 40, 72), (200, 136, 264)])
+def test_views_that_start_anywhere(m, f, k, offset):
+    """operands and outputs whose first element lies `offset` elements into a buffer: the bits of aligned ones"""
+    dtype = torch.bfloat16
+
+    def shifted(t):
+        store = torch.empty(t.numel() + offset, dtype=t.dtype, device="cuda")
+        view = store[offset:].view(t.shape)
+        return view.copy_(t)
+
+    x, wg, wu, dh = normal(m, k, 1, dtype), normal(f, k, 2, dtype, 0.1), normal(f, k, 3, dtype, 0.1), normal(m, f, 4, dtype)
+    h, g, u = ff.gated_forward(x, wg, wu, save=True)
+    grads = ff.gated_backward(dh, x, wg, wu, g, u)
+    sx, sg, su = shifted(x), shifted(wg), shifted(wu)
+    for a, b in zip(ff.gated_forward(sx, sg, su, save=True), (h, g, u)):
+        assert torch.equal(a, b)
+    for a, b in zip(ff.gated_backward(shifted(dh), sx, sg, su, shifted(g), shifted(u)), grads):
+        assert torch.equal(a, b)
+    stream = torch.cuda.current_stream().cuda_stream
+    ph, px, pg, pu = shifted(torch.zeros_like(h)), shifted(torch.zeros_like(x)), shifted(torch.zeros_like(wg)), shifted(torch.zeros_like(wu))
+    eq.gated_forward(x, k, wg, k, wu, k, eq.BF16, m, f, k, eq.ACT_GELU_TANH, ph, f, 0, 0, 0, 0, 0, stream)
+    assert torch.equal(ph, h)
+    nb = eq.gated_backward_workspace_bytes(m, f, k, x, k, wg, k, wu, k)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    eq.gated_backward(dh, f, x, k, wg, k, wu, k, g, u, f, eq.BF16, m, f, k, eq.ACT_GELU_TANH, px, k, pg, k, pu, k, ws, nb, stream)
+    for a, b in zip((px, pg, pu), grads):
+        assert torch.equal(a, b)
+    for fmt in FORMATS:
+        q, sq = ff.fp4_quantize(x, fmt), ff.fp4_quantize(sx, fmt)
+        for out in (torch.bfloat16, torch.float32):
+            back = ff.fp4_dequantize(q, out)
+            assert torch.equal(back, ff.fp4_dequantize(sq, out))
+            pb = shifted(torch.zeros_like(back))
+            eq.fp4_dequantize(*q._parts, m, k, fmt, pb, {torch.bfloat16: eq.BF16, torch.float32: eq.FP32}[out], k, stream)
+            assert torch.equal(pb, back)
+            w = ff.fp4_quantize(wg, fmt)
+            y = ff.fp4_matmul(q, w, out)
+            py = shifted(torch.zeros_like(y))
+            eq.fp4_matmul(*q._parts, *w._parts, m, f, k, fmt, py, {torch.bfloat16: eq.BF16, torch.float32: eq.FP32}[out], f, stream)
+            assert torch.equal(py, y)
+        w = ff.fp4_quantize(wg, fmt)
+        for rows in (1, m):
+            assert torch.equal(ff.fp4_linear(sx[:rows], w), ff.fp4_linear(x[:rows], w))
     ff.check()
 
 
