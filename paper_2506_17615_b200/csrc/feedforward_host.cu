@@ -278,8 +278,8 @@ static_assert(kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, 
 
 // Columns of a tile, and what the launch is expected to take in cycles of an SM.  The pairs of SMs work
 // through whole rounds of tiles.  A stage takes a pair 1.3 cycles for each of the (256 + bn) rows of 128 bytes
-// that it loads (678 cycles at bn = 256, where the products alone need 512), a tile 3500 to drain (6000 where
-// 256 columns go through the activation), the launch 8000.  A narrower tile loads more for each product, but may save a round, or give every pair work when
+// that it loads (the products alone need 2 bn), a tile 3500 to drain (6000 where 256 columns of 4-bit operands go
+// through the activation), the launch 8000.  A narrower tile loads more for each product, but may save a round, or give every pair work when
 // there is little.  Measured / expected, us: 16-bit gated, 5376 -> 2688, 128 tokens 24.4 / 24.4, 8192 tokens
 // 301 / 325; NV product 5376 -> 2688, 128 tokens 12.1 / 11.6.  4-bit operands: their scales come in groups of 128
 // columns.
