@@ -312,7 +312,7 @@ int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
             TRY(make_map(a.store[i], a.out[i].p, 2, n, m, a.out[i].ld * 2, 32, CU_TENSOR_MAP_SWIZZLE_64B));
     const size_t tiles = size_t(a.tiles_m) * a.tiles_n;
     // a pair of CTAs on the two SMs of each TPC; the kernel declares the cluster
-    return launch(tile_kernel<KIND, MODE, A_MN, B_MN>, dim3(unsigned(2 * std::min<size_t>(tiles, sms / 2))), kTileThreads,
+    return launch(tile_kernel<KIND, MODE, A_MN, B_MN>, dim3(unsigned(2 * std::min<size_t>(tiles, sms / 2))), kTileThreads<KIND>,
                   kTileSmem<KIND>, 1, a, stream);
 }
 

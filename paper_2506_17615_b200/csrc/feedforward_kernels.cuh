@@ -226,7 +226,7 @@ constexpr int kTileM = 256;               // rows of a tile: 128 in each CTA of 
 template <int KIND> constexpr int kStageBytes = 2 * kTileBytes + 3 * kScaleBytes<KIND>;
 template <int KIND> constexpr int kPipe = KIND == kHalf ? 6 : 5;
 constexpr int kEpilogueWarps = 8;
-constexpr int kTileThreads = 32 * (kEpilogueWarps + 2);
+template <int KIND> constexpr int kTileThreads = 32 * (kEpilogueWarps + (KIND == kHalf ? 2 : 3));
 constexpr int kSmemSlack = 1024;          // 128-byte swizzle atoms start on multiples of 1024 bytes
 constexpr int kStaging = kEpilogueWarps * 2 * kStageOut;
 template <int KIND> constexpr int kTileSmem = kPipe<KIND> * kStageBytes<KIND> + kStaging + kSmemSlack;
@@ -245,8 +245,8 @@ __device__ __forceinline__ void tile_at(const TileArgs& p, int t, int& mt, int& 
 // Output tiles of 256 x bn by pairs of CTAs: each holds half of the rows of a and half of the columns
 // of b, the tensor cores of both read both halves of b, so a pair loads (256 + bn) rows a stage where
 // two single CTAs would load 2 (128 + bn); L2 to SM traffic, not the tensor cores, bounds the single
-// form.  In each CTA one thread starts TMA loads through a ring of stages; in the first CTA one thread
-// issues the products for both; eight warps move finished accumulators from tensor memory to the
+// form.  In each CTA one warp starts TMA loads through a ring of stages (a second one those of the scales);
+// in the first CTA one warp issues the products for both; eight warps move finished accumulators from tensor memory to the
 // output.  Two accumulators let the next tile's products run meanwhile.  4-bit operands: the scales
 // need tensor memory too, so of 256 columns the second accumulator begins 64 inside the first, and each is
 // drained from that end first.  (Tiles of 192 columns, whose accumulators share none, load more for each
@@ -257,7 +257,7 @@ __device__ __forceinline__ void tile_at(const TileArgs& p, int t, int& mt, int& 
 // kSum2: out = a0 b0 + a1 b1.  kOut2: out0 = a0 b0, out1 = a1 b0, the rows of both one below the other in
 // blocks of 128: a CTA's block belongs to one of them (21 blocks each of 2688 rows make 21 tiles, not 2 x 11).
 template <int KIND, int MODE, bool A_MN, bool B_MN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 1)
     tile_kernel(const __grid_constant__ TileArgs p) {
     constexpr bool FP4 = KIND != kHalf;
     constexpr int PIPE = kPipe<KIND>, STAGE = kStageBytes<KIND>, SB = kScaleBytes<KIND>;
@@ -308,32 +308,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
     grid_begin(p.order);
 
     if (warp == kEpilogueWarps + 1) {
-        {
-            // ------------------------------------------------ loads
-            uint32_t it = 0;
-            bool ok = true;
-            for (int t = pair; t < tiles && ok; t += pairs) {
-                int mt, nt, which;
-                tile_at(p, t, mt, nt);
-                const int m0 = rows_of(mt, which);
-                const int n0 = nt * width + (MODE == kGated ? 0 : rank * half);
-                // scales: 128-row groups of a (the second may not exist) and of b (each CTA takes all)
-                const int groups_a = FP4 ? (p.m + 127) / 128 : 0, ga = mt * 2 + rank;
-                const int gb = nt * width / 128, nb = FP4 ? min(width / 128, (p.n + 127) / 128 - gb) : 0;
-                uint32_t bytes = 2 * kTileBytes + 2 * (B_MN ? (half + 63) / 64 * kChunkBytes : half * kRowBytes);
-                if (FP4) bytes += SB * (min(2, groups_a - mt * 2) + 2 * nb * (MODE == kGated ? 2 : 1));
-                for (int s = 0; s < stages; ++s, ++it) {
-                    const uint32_t slot = it % PIPE;
-                    if (!(ok = barrier_wait_warp(empty + 8 * slot, (it / PIPE & 1) ^ 1, &abort))) break;
-                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes;
-                    // both CTAs' loads count on the first one's barrier
+        // ---------------------------------------------------- loads of a and b
+        // (addresses that do not change are kept out of the loops: with five loads a stage this warp
+        // needed 690 cycles for each where the products need 512)
+        const uint32_t counted = peer_addr(full, 0);       // both CTAs' loads count on the first one's barriers
+        uint32_t slot = 0, phase = 1, issued = 0;
+        bool ok = true;
+        for (int t = pair; t < tiles && ok; t += pairs) {
+            int mt, nt, which;
+            tile_at(p, t, mt, nt);
+            const int m0 = rows_of(mt, which);
+            const int n0 = nt * width + (MODE == kGated ? 0 : rank * half);
+            uint32_t bytes = 2 * kTileBytes + 2 * (B_MN ? (half + 63) / 64 * kChunkBytes : half * kRowBytes);
+            if (FP4) {
+                const int groups_a = (p.m + 127) / 128, nb = min(width / 128, (p.n + 127) / 128 - nt * width / 128);
+                bytes += SB * (min(2, groups_a - mt * 2) + 2 * nb * (MODE == kGated ? 2 : 1));
+            }
+#pragma unroll
+            for (int part = 0; part < (MODE == kSum2 ? 2 : 1); ++part) {
+                const CUtensorMap* const ma = &p.a[MODE == kOut2 ? which : part];
+                const CUtensorMap* const mb = &p.b[MODE == kGated ? rank : part];
+                int kc = 0;
+                for (int s = 0; s < p.stages; ++s, kc += FP4 ? kRowBytes : 64) {      // 4-bit codes travel as bytes
+                    if (!(ok = barrier_wait_warp(empty + 8 * slot, phase, &abort))) break;
+                    const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, bar = counted + 8 * slot;
                     if (rank == 0) barrier_expect_warp(full + 8 * slot, bytes);
-                    const uint32_t bar = peer_addr(full + 8 * slot, 0);
-                    const int part = MODE == kSum2 ? s >= p.stages : 0;
-                    const int ks = s - part * p.stages;
-                    const CUtensorMap* ma = &p.a[MODE == kOut2 ? which : part];
-                    const CUtensorMap* mb = &p.b[MODE == kGated ? rank : part];
-                    const int kc = FP4 ? ks * kRowBytes : ks * 64;     // 4-bit codes travel as bytes
                     if (A_MN) {
                         tma_load_2d_pair(sa, ma, m0, kc, bar);
                         tma_load_2d_pair(sa + kChunkBytes, ma, m0 + 64, kc, bar);
@@ -346,31 +345,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
                     } else {
                         tma_load_2d_pair(sb, mb, kc, n0, bar);
                     }
-                    if (FP4) {
-                        const uint32_t ss = sb + kTileBytes;
-                        if (ga < groups_a) tma_load_2d_pair(ss, &p.scales_a, 0, (ga * p.stages + ks) * (SB / 128), bar);
-                        for (int q = 0; q < (MODE == kGated ? 2 : 1); ++q)
-                            for (int i = 0; i < nb; ++i)
-                                tma_load_2d_pair(ss + SB * (1 + q + i), &p.scales_b[q], 0,
-                                                 ((gb + i) * p.stages + ks) * (SB / 128), bar);
+                    ++issued;
+                    if (++slot == PIPE) {
+                        slot = 0;
+                        phase ^= 1;
                     }
                 }
+                if (!ok) break;
             }
-            if (abort && rank == 0)     // what has been started lands before the shared memory goes away
-                for (uint32_t i = it > PIPE ? it - PIPE : 0; i < it; ++i) barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
+        }
+        if (abort && rank == 0)         // what has been started lands before the shared memory goes away
+            for (uint32_t i = issued > PIPE ? issued - PIPE : 0; i < issued; ++i)
+                barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
+        __syncwarp();
+    } else if (FP4 && warp == kEpilogueWarps + 2) {
+        // ---------------------------------------------------- loads of the scales, counted with those
+        const uint32_t counted = peer_addr(full, 0);
+        uint32_t slot = 0, phase = 1;
+        bool ok = true;
+        for (int t = pair; t < tiles && ok; t += pairs) {
+            int mt, nt;
+            tile_at(p, t, mt, nt);
+            // groups of 128 rows: of a this CTA's own (which may not exist), of b all of the tile's
+            const int ga = mt * 2 + rank, gb = nt * width / 128, nb = min(width / 128, (p.n + 127) / 128 - gb);
+            const bool has_a = ga < (p.m + 127) / 128;
+            int ya = ga * p.stages * (SB / 128), yb = gb * p.stages * (SB / 128);
+            const int next = p.stages * (SB / 128);
+            for (int s = 0; s < p.stages; ++s, ya += SB / 128, yb += SB / 128) {
+                if (!(ok = barrier_wait_warp(empty + 8 * slot, phase, &abort))) break;
+                const uint32_t ss = smem + slot * STAGE + 2 * kTileBytes, bar = counted + 8 * slot;
+                if (has_a) tma_load_2d_pair(ss, &p.scales_a, 0, ya, bar);
+                tma_load_2d_pair(ss + SB, &p.scales_b[0], 0, yb, bar);
+                if (MODE == kGated) tma_load_2d_pair(ss + 2 * SB, &p.scales_b[1], 0, yb, bar);
+                else if (nb > 1) tma_load_2d_pair(ss + 2 * SB, &p.scales_b[0], 0, yb + next, bar);
+                if (++slot == PIPE) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+            }
         }
         __syncwarp();
     } else if (warp == kEpilogueWarps) {
         if (rank == 0) {
             // ------------------------------------------------ products
             const uint32_t ta = tmem + kScaleCol, tb = ta + 4 * kScaleTiles<KIND>;
-            uint32_t it = 0, local = 0;
+            uint32_t slot = 0, phase = 0, local = 0;
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs, ++local) {
                 const uint32_t buf = local & 1, d = tmem + buf * kSecond;
-                for (int s = 0; s < stages; ++s, ++it) {
-                    const uint32_t slot = it % PIPE;
-                    if (!(ok = barrier_wait_warp(full + 8 * slot, it / PIPE & 1, &abort))) break;
+                for (int s = 0; s < stages; ++s) {
+                    if (!(ok = barrier_wait_warp(full + 8 * slot, phase, &abort))) break;
                     fence_after();
                     const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, ss = sb + kTileBytes;
                     if (FP4) {
@@ -406,6 +430,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
                         }
                     }
                     mma_commit<2>(empty + 8 * slot);
+                    if (++slot == PIPE) {
+                        slot = 0;
+                        phase ^= 1;
+                    }
                 }
                 if (ok) mma_commit<2>(ready + 8 * buf);
             }
