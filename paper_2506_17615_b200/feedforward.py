@@ -25,7 +25,6 @@ _DTYPES = {torch.bfloat16: binding.BF16, torch.float16: binding.FP16, torch.floa
 _lib = binding.lib
 
 # what a call needs beside its tensors depends on its shape, and on how its rows are aligned
-_scales_bytes = lru_cache(maxsize=4096)(_lib.equarx_fp4_scales_bytes)
 _linear_workspace = lru_cache(maxsize=4096)(_lib.equarx_fp4_linear_workspace_bytes)
 _forward_workspace = lru_cache(maxsize=4096)(_lib.equarx_gated_forward_workspace_bytes)
 _backward_workspace = lru_cache(maxsize=4096)(_lib.equarx_gated_backward_workspace_bytes)
@@ -33,6 +32,14 @@ _backward_workspace = lru_cache(maxsize=4096)(_lib.equarx_gated_backward_workspa
 
 def _up(n, to):
     return -(-n // to) * to
+
+
+@lru_cache(maxsize=4096)
+def _layout(rows, cols, format):
+    """offsets of codes and row factors in the buffer of an Fp4Matrix, and its size; scales come first"""
+    row_scales = _up(_lib.equarx_fp4_scales_bytes(rows, cols, format), 256)
+    codes = row_scales + (_up(4 * rows, 256) if format == FP4_NV else 0)
+    return codes, row_scales, codes + _lib.equarx_fp4_codes_bytes(rows, cols)
 
 
 class Fp4Matrix:
@@ -43,31 +50,30 @@ class Fp4Matrix:
     def __init__(self, data, rows, cols, format):
         self.data, self.rows, self.cols, self.format = data, rows, cols, format
         base = data.data_ptr()
-        row_scales = _up(_scales_bytes(rows, cols, format), 256)
-        codes = row_scales + (_up(4 * rows, 256) if format == FP4_NV else 0)
+        codes, row_scales, _ = _layout(rows, cols, format)
         self._parts = (base + codes, base, base + row_scales if format == FP4_NV else 0)
 
     @staticmethod
     def nbytes(rows, cols, format):
-        return _up(_scales_bytes(rows, cols, format), 256) + (_up(4 * rows, 256) if format == FP4_NV else 0) + \
-            rows * (_up(cols, 32) // 2)
+        return _layout(rows, cols, format)[2]
 
     @property
     def codes(self):
         """uint8 [rows, ceil(cols/32)*16], two codes a byte, the first in the low half"""
-        return self.data[self._parts[0] - self.data.data_ptr():].view(self.rows, _up(self.cols, 32) // 2)
+        first, _, end = _layout(self.rows, self.cols, self.format)
+        return self.data[first:end].view(self.rows, _up(self.cols, 32) // 2)
 
     @property
     def scales(self):
         """uint8, in the tiled order of include/equarx.h"""
-        return self.data[:_scales_bytes(self.rows, self.cols, self.format)]
+        return self.data[:_lib.equarx_fp4_scales_bytes(self.rows, self.cols, self.format)]
 
     @property
     def row_scales(self):
         """float32 [rows] (FP4_NV), None (FP4_MX)"""
         if self.format != FP4_NV:
             return None
-        first = self._parts[2] - self.data.data_ptr()
+        first = _layout(self.rows, self.cols, self.format)[1]
         return self.data[first:first + 4 * self.rows].view(torch.float32)
 
 
@@ -123,7 +129,7 @@ def _workspace(like, nbytes):
 def fp4_quantize(x, format=FP4_NV):
     """x [rows, cols], bfloat16, float16 or float32 -> Fp4Matrix."""
     rows, cols, ld, dtype, dev = _matrix(x, "x")
-    q = Fp4Matrix(x.new_empty(Fp4Matrix.nbytes(rows, cols, format), dtype=torch.uint8), rows, cols, format)
+    q = Fp4Matrix(x.new_empty(_layout(rows, cols, format)[2], dtype=torch.uint8), rows, cols, format)
     _call(dev, _lib.equarx_fp4_quantize, x.data_ptr(), _DTYPES[dtype], rows, cols, ld, format, *q._parts)
     return q
 
