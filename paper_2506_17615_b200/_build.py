@@ -3,6 +3,7 @@ import fcntl
 import os
 import shutil
 import subprocess
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
@@ -11,6 +12,8 @@ DEPENDS = SOURCES + [os.path.join(_CSRC, name) for name in ("equarx_kernels.cuh"
                                                             "feedforward_kernels.cuh")] + \
     [os.path.join(os.path.dirname(_HERE), "include", "equarx.h")]
 LIB = os.path.join(_HERE, "libequarx.so")
+FASTCALL_SOURCE = os.path.join(_CSRC, "fastcall.c")
+FASTCALL = os.path.join(_HERE, "_fastcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
@@ -56,3 +59,25 @@ def build(force=False, verbose=False):
         finally:
             fcntl.flock(lock, fcntl.LOCK_UN)
     return LIB
+
+
+def build_fastcall(force=False):
+    """Compile the extension module that calls the feed-forward entry points without ctypes; returns its path.
+    It depends on the header alone, not on the library, and needs a C compiler and Python's headers."""
+    sources = (FASTCALL_SOURCE, os.path.join(os.path.dirname(_HERE), "include", "equarx.h"))
+
+    def stale():
+        return not os.path.exists(FASTCALL) or any(os.path.getmtime(p) > os.path.getmtime(FASTCALL) for p in sources)
+
+    if force or stale():
+        with open(FASTCALL + ".lock", "w") as lock:
+            fcntl.flock(lock, fcntl.LOCK_EX)
+            try:
+                if force or stale():
+                    tmp = f"{FASTCALL}.{os.getpid()}.tmp"
+                    subprocess.run([os.environ.get("CC") or "gcc", "-O2", "-std=c11", "-Wall", "-shared", "-fPIC",
+                                    "-I", sysconfig.get_paths()["include"], "-o", tmp, FASTCALL_SOURCE], check=True)
+                    os.replace(tmp, FASTCALL)
+            finally:
+                fcntl.flock(lock, fcntl.LOCK_UN)
+    return FASTCALL

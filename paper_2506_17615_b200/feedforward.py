@@ -14,15 +14,23 @@ Matrices are [rows, columns] with unit column stride; the row stride is free.  A
 over in a few microseconds on the GPU, so what it costs on the host counts: one output allocation, one
 workspace allocation where one is needed, plain integers into the library.
 """
+import ctypes
+import importlib
 from functools import lru_cache
 
 import torch
 
-from . import binding
+from . import _build, binding
 from .binding import ACT_GELU_TANH, ACT_SILU, FP4_MX, FP4_NV, EquarxError  # noqa: F401  (part of this module's interface)
 
 _DTYPES = {torch.bfloat16: binding.BF16, torch.float16: binding.FP16, torch.float32: binding.FP32}
 _lib = binding.lib
+
+# the entry points, by way of the extension module (csrc/fastcall.c) rather than ctypes
+_build.build_fastcall()
+_fast = importlib.import_module("._fastcall", __package__)
+for _name in ("fp4_quantize", "fp4_dequantize", "fp4_matmul", "fp4_linear", "fp4_gated", "gated_forward", "gated_backward"):
+    _fast.bind(_name, ctypes.cast(getattr(_lib, "equarx_" + _name), ctypes.c_void_p).value)
 
 # what a call needs beside its tensors depends on its shape, and on how its rows are aligned
 _linear_workspace = lru_cache(maxsize=4096)(_lib.equarx_fp4_linear_workspace_bytes)
@@ -115,7 +123,7 @@ def _call(device, fn, *args):
         with torch.cuda.device(device):
             status = fn(*args, stream)
     if status:
-        raise EquarxError(status, fn.__name__)
+        raise EquarxError(status, "equarx_" + fn.__name__)
 
 
 def _workspace(like, nbytes):
@@ -130,14 +138,14 @@ def fp4_quantize(x, format=FP4_NV):
     """x [rows, cols], bfloat16, float16 or float32 -> Fp4Matrix."""
     rows, cols, ld, dtype, dev = _matrix(x, "x")
     q = Fp4Matrix(x.new_empty(_layout(rows, cols, format)[2], dtype=torch.uint8), rows, cols, format)
-    _call(dev, _lib.equarx_fp4_quantize, x.data_ptr(), _DTYPES[dtype], rows, cols, ld, format, *q._parts)
+    _call(dev, _fast.fp4_quantize, x.data_ptr(), _DTYPES[dtype], rows, cols, ld, format, *q._parts)
     return q
 
 
 def fp4_dequantize(q, dtype=torch.bfloat16):
     """The values that q's codes stand for, rounded once to dtype."""
     out = q.data.new_empty((q.rows, q.cols), dtype=dtype)
-    _call(out.get_device(), _lib.equarx_fp4_dequantize, *q._parts, q.rows, q.cols, q.format, out.data_ptr(), _DTYPES[dtype],
+    _call(out.get_device(), _fast.fp4_dequantize, *q._parts, q.rows, q.cols, q.format, out.data_ptr(), _DTYPES[dtype],
           q.cols)
     return out
 
@@ -150,7 +158,7 @@ def fp4_matmul(a, b, dtype=torch.bfloat16):
     dev = out.get_device()
     if b.data.get_device() != dev:
         raise ValueError("the operands are on different devices")
-    _call(dev, _lib.equarx_fp4_matmul, *a._parts, *b._parts, a.rows, b.rows, a.cols, a.format, out.data_ptr(), _DTYPES[dtype],
+    _call(dev, _fast.fp4_matmul, *a._parts, *b._parts, a.rows, b.rows, a.cols, a.format, out.data_ptr(), _DTYPES[dtype],
           b.rows)
     return out
 
@@ -163,7 +171,7 @@ def fp4_linear(x, w):
     out = x.new_empty((m, w.rows))
     nbytes = _linear_workspace(m, k, w.format)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_fp4_linear, x.data_ptr(), _DTYPES[dtype], ld, *w._parts, m, w.rows, k, w.format, out.data_ptr(),
+    _call(dev, _fast.fp4_linear, x.data_ptr(), _DTYPES[dtype], ld, *w._parts, m, w.rows, k, w.format, out.data_ptr(),
           w.rows, ptr, nbytes)
     return out
 
@@ -178,7 +186,7 @@ def fp4_gated(x, wg, wu, act=ACT_GELU_TANH):
     h = x.new_empty((m, wg.rows))
     nbytes = _linear_workspace(m, k, wg.format)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_fp4_gated, x.data_ptr(), _DTYPES[dtype], ld, *wg._parts, *wu._parts, m, wg.rows, k, wg.format,
+    _call(dev, _fast.fp4_gated, x.data_ptr(), _DTYPES[dtype], ld, *wg._parts, *wu._parts, m, wg.rows, k, wg.format,
           act, h.data_ptr(), wg.rows, ptr, nbytes)
     return h
 
@@ -196,7 +204,7 @@ def gated_forward(x, wg, wu, act=ACT_GELU_TANH, save=False):
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
     nbytes = _forward_workspace(m, f, k, xp & 15, ldx, gp & 15, ldg, up & 15, ldu)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_gated_forward, xp, ldx, gp, ldg, up, ldu, _DTYPES[dtype], m, f, k, act, h.data_ptr(), f, g.data_ptr() if save else 0, u.data_ptr() if save else 0, f, ptr, nbytes)
+    _call(dev, _fast.gated_forward, xp, ldx, gp, ldg, up, ldu, _DTYPES[dtype], m, f, k, act, h.data_ptr(), f, g.data_ptr() if save else 0, u.data_ptr() if save else 0, f, ptr, nbytes)
     return (h, g, u) if save else h
 
 
@@ -213,7 +221,7 @@ def gated_backward(dh, x, wg, wu, g, u, act=ACT_GELU_TANH):
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
     nbytes = _backward_workspace(m, f, k, xp & 15, ldx, gp & 15, ldwg, up & 15, ldwu)
     ws, ptr = _workspace(x, nbytes)
-    _call(dev, _lib.equarx_gated_backward, dh.data_ptr(), lddh, xp, ldx, gp, ldwg, up, ldwu, g.data_ptr(), u.data_ptr(), ldgu, _DTYPES[dtype], m, f, k, act, dx.data_ptr(), k, dwg.data_ptr(), k, dwu.data_ptr(),
+    _call(dev, _fast.gated_backward, dh.data_ptr(), lddh, xp, ldx, gp, ldwg, up, ldwu, g.data_ptr(), u.data_ptr(), ldgu, _DTYPES[dtype], m, f, k, act, dx.data_ptr(), k, dwg.data_ptr(), k, dwu.data_ptr(),
           k, ptr, nbytes)
     return dx, dwg, dwu
 

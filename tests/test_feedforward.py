@@ -149,6 +149,26 @@ def test_tensors_that_do_not_fit_are_refused():
         ff.gated_forward(x, x, x)
 
 
+def test_the_extension_module_calls_the_library():
+    """the functions that feedforward calls: the library's own status for bad arguments, an exception for
+    arguments that are no integers or too few"""
+    fast = ff._fast
+    assert fast.fp4_quantize(A, 9, 4, 64, 64, 1, A, A, A, 0) == binding.ERR_FORMAT
+    assert fast.fp4_quantize(A, 1 << 32, 4, 64, 64, 1, A, A, A, 0) == binding.ERR_FORMAT
+    assert fast.fp4_quantize(0, 0, 4, 64, 64, 1, A, A, A, 0) == binding.ERR_NULL
+    assert fast.fp4_dequantize(A, A, A, 4, 64, 1, A, 0, 60, 0) == binding.ERR_COUNT
+    assert fast.fp4_matmul(A, A, A, A, A, A, 4, 8, 64, 7, A, 0, 8, 0) == binding.ERR_FORMAT
+    assert fast.fp4_linear(A, 0, 64, A, A, A, 40, 8, 64, 1, A + GB, 8, A + 2 * GB, 0, 0) == binding.ERR_WORKSPACE
+    assert fast.fp4_gated(A, 0, 64, A, A, A, A, A, A, 4, 8, 64, 1, 5, A, 8, 0, 0, 0) == binding.ERR_FORMAT
+    assert fast.gated_forward(A, 64, A, 64, A, 64, 0, 4, 8, 64, 0, A, 7, 0, 0, 0, 0, 0, 0) == binding.ERR_COUNT
+    assert fast.gated_backward(*[A, 64] * 4, A, A, 64, 0, 4, 8, 64, 0, *[A, 64] * 3, 0, 0, 0) == binding.ERR_NULL
+    for bad in ((), (1,) * 9, (1,) * 11, (1.0,) + (1,) * 9, (-1,) + (1,) * 9, (None,) * 10):
+        with pytest.raises((TypeError, OverflowError, ValueError)):
+            fast.fp4_quantize(*bad)
+    with pytest.raises(ValueError):
+        fast.bind("nothing", A)
+
+
 # ------------------------------------------------------------------ inputs
 
 def normal(rows, cols, seed, dtype, scale=1.0, pad=0):
