@@ -49,9 +49,9 @@ inline bool is_16bit(int dtype) { return dtype == EQUARX_BF16 || dtype == EQUARX
 inline bool is_float(int dtype) { return is_16bit(dtype) || dtype == EQUARX_FP32; }
 inline bool is_format(int f) { return f == EQUARX_FP4_MX || f == EQUARX_FP4_NV; }
 inline bool is_act(int a) { return a == EQUARX_ACT_SILU || a == EQUARX_ACT_GELU_TANH; }
-// bytes, at most 16, that a base and a row stride are multiples of
+// bytes, at most 32, that a base and a row stride are multiples of
 inline int unit_of(const void* p, size_t ld, size_t size) {
-    const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (ld * size) | 16;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (ld * size) | 32;
     return int(bits & (~bits + 1));
 }
 inline size_t size_of(int dtype) { return dtype == EQUARX_FP32 ? 4 : 2; }
@@ -308,7 +308,7 @@ int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
     a.tiles_n = int(ceil_div(n, MODE == kGated ? a.bn / 2 : a.bn));
     a.group = 8;
     for (int i = 0; i < 3; ++i)
-        if (a.out[i].p && a.out[i].unit == 16 && a.out[i].dtype != EQUARX_FP32)
+        if (a.out[i].p && a.out[i].unit >= 16 && a.out[i].dtype != EQUARX_FP32)
             TRY(make_map(a.store[i], a.out[i].p, 2, n, m, a.out[i].ld * 2, 32, CU_TENSOR_MAP_SWIZZLE_64B));
     const size_t tiles = size_t(a.tiles_m) * a.tiles_n;
     // a pair of CTAs on the two SMs of each TPC; the kernel declares the cluster

@@ -28,7 +28,6 @@ constexpr int kRowBytes = 128;            // one stage of the reduction axis: 64
 constexpr int kTileBytes = kRowsM * kRowBytes;
 constexpr int kChunkBytes = 64 * kRowBytes;   // MN-major operands: 64 elements x 64 steps of the reduction
 
-template <int KIND> constexpr int kStageElems = KIND == kHalf ? 64 : 256;
 // scales of 128 rows for one stage: 512-byte tiles of 128 rows x 4 scales
 template <int KIND> constexpr int kScaleTiles = KIND == kNv ? 4 : KIND == kMx ? 2 : 0;
 template <int KIND> constexpr int kScaleBytes = 512 * kScaleTiles<KIND>;
@@ -88,7 +87,7 @@ struct Out {
     void* p;
     size_t ld;
     int dtype;
-    int unit;     // bytes that base and row stride are multiples of: 16, 8, 4 or 2
+    int unit;     // bytes that base and row stride are multiples of: 32, 16, 8, 4 or 2
 };
 
 // n <= 4 neighbouring columns of one row, the first a multiple of 4
@@ -144,7 +143,7 @@ __device__ __forceinline__ void store_direct(const Out& o, uint32_t buf, int row
     if (o.dtype == kFp32) {
         float* q = static_cast<float*>(o.p) + size_t(row0 + lane) * o.ld + col0;
         if (row0 + int(lane) >= rows) return;
-        if (o.unit == 16 && col0 + 32 <= cols) {
+        if (o.unit >= 16 && col0 + 32 <= cols) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 reinterpret_cast<float4*>(q)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
@@ -451,7 +450,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
         const uint32_t staging = smem + PIPE * STAGE + warp * 2 * kStageOut;
         auto store = [&](int i, int row0, int col0, float (&v)[32]) {
             if (row0 >= p.m || col0 >= p.n) return;
-            if (p.out[i].unit == 16 && p.out[i].dtype != kFp32) {
+            if (p.out[i].unit >= 16 && p.out[i].dtype != kFp32) {
                 store_staged(&p.store[i], staging + flip, row0, col0, p.out[i].dtype, v);
                 flip ^= kStageOut;
             } else {
@@ -563,7 +562,7 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
     grid_launch();
     grid_wait();
     auto load = [&](const uint16_t* src, int col) {
-        if (p.unit == 16 && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
+        if (p.unit >= 16 && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
         if (p.unit >= 4 && col + 8 <= p.cols) {
             const uint32_t* q = reinterpret_cast<const uint32_t*>(src + col);
             return make_uint4(q[0], q[1], q[2], q[3]);
@@ -645,7 +644,7 @@ struct QuantArgs {
     uint8_t *codes, *scales;
     float* row_scales;
     size_t ld;
-    int rows, cols, dtype, unit;      // unit: bytes that base and row stride are multiples of: 16, 8, 4 or 2
+    int rows, cols, dtype, unit;      // unit: bytes that base and row stride are multiples of: 32, 16, 8, 4 or 2
 };
 
 // eight codes, the first in the lowest nibble
@@ -673,6 +672,12 @@ __device__ __forceinline__ void decode8(uint32_t w, float* v) {
         v[2 * i + 1] = f.y;
     }
 }
+// one code: from 2 on, exponent and mantissa bits are those of the number, with another bias; 0 and 1 are 0 and .5
+__device__ __forceinline__ float decode1(uint32_t code) {
+    const uint32_t m = code & 7;
+    const uint32_t bits = m >= 2 ? (m << 22) + (126u << 23) : m * (126u << 23);
+    return __uint_as_float(bits | (code & 8) << 28);
+}
 __device__ __forceinline__ uint32_t to_e4m3(float v) {
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
@@ -697,10 +702,27 @@ template <int DT> struct Group {
     uint32_t w[DT == kFp32 ? 16 : 8];
 };
 
+// 256-bit accesses (sm_100): what is read once, or written and not read again here
+__device__ __forceinline__ void load_256(const void* p, uint32_t* w) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void store_256(void* p, const uint32_t* w) {
+    asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+
 template <int DT>
 __device__ __forceinline__ void load_group(const QuantArgs& p, size_t row, int col, Group<DT>& g) {
     constexpr int W = DT == kFp32 ? 16 : 8, PER = 16 / W;
-    if (p.unit == 16 && col + 16 <= p.cols) {
+    if (p.unit == 32 && col + 16 <= p.cols) {
+        const uint8_t* q = static_cast<const uint8_t*>(p.x) + (row * p.ld + col) * (4 / PER);
+#pragma unroll
+        for (int i = 0; i < W / 8; ++i) load_256(q + 32 * i, g.w + 8 * i);
+    } else if (p.unit == 16 && col + 16 <= p.cols) {
         const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (row * p.ld + col) * (4 / PER));
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
@@ -891,6 +913,26 @@ __global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_consta
     grid_launch();
     grid_wait();
     const float g = MX ? 1.0f : p.row_scales[row];
+    if (p.unit < 16) {
+        // output rows that do not start on multiples of 16 bytes: two elements a thread, so that a warp
+        // still writes neighbouring bytes
+        const uint8_t* const scales = p.scales + scale_offset<MX>(row, 0, stages);
+        for (int col = tid * 2; col < p.cols; col += threads * 2) {
+            const int block = col / (MX ? 32 : 16);
+            const uint32_t b = scales[size_t(block / 4) * 512 + block % 4];
+            const float d = MX ? from_e8m0(b) : __fmul_rn(from_e4m3(b), g);
+            const uint32_t pair = p.codes[row * size_t(stride) + col / 2];
+            const float v0 = __fmul_rn(decode1(pair & 15), d), v1 = __fmul_rn(decode1(pair >> 4), d);
+            const size_t at = row * p.ld + col;
+            if (p.unit >= 4 && p.dtype != kFp32 && col + 2 <= p.cols) {
+                *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at) = pack2(v0, v1, p.dtype);
+            } else {
+                store1(p.out, at, v0, p.dtype);
+                if (col + 1 < p.cols) store1(p.out, at + 1, v1, p.dtype);
+            }
+        }
+        return;
+    }
     for (int first = 0; first < p.cols; first += span) {
         uint2 w[kRowChunks];
         uint32_t b[kRowChunks];
@@ -911,26 +953,26 @@ __global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_consta
             decode8(w[c].y, v + 8);
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = __fmul_rn(v[j], d);
-            if (p.unit == 16 && col + 16 <= p.cols) {
-                if (p.dtype == kFp32) {
-                    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * p.ld + col);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                } else {
-                    uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + row * p.ld + col);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        q[j] = make_uint4(pack2(v[8 * j], v[8 * j + 1], p.dtype), pack2(v[8 * j + 2], v[8 * j + 3], p.dtype),
-                                          pack2(v[8 * j + 4], v[8 * j + 5], p.dtype), pack2(v[8 * j + 6], v[8 * j + 7], p.dtype));
-                }
-            } else if (p.dtype != kFp32 && p.unit >= 4 && col + 16 <= p.cols) {
-                uint32_t* q = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + row * p.ld + col);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = pack2(v[2 * j], v[2 * j + 1], p.dtype);
-            } else {
+            const size_t at = row * p.ld + col;
+            if (col + 16 > p.cols) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (col + j < p.cols) store1(p.out, row * p.ld + col + j, v[j], p.dtype);
+                    if (col + j < p.cols) store1(p.out, at + j, v[j], p.dtype);
+            } else if (p.dtype == kFp32) {
+                float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.out) + at);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            } else {
+                uint32_t o[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = pack2(v[2 * j], v[2 * j + 1], p.dtype);
+                if (p.unit == 32) {
+                    store_256(static_cast<uint16_t*>(p.out) + at, o);
+                } else {
+                    uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at);
+                    q[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                    q[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                }
             }
         }
     }

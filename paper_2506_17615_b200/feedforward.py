@@ -126,6 +126,11 @@ def _call(device, fn, *args):
         raise EquarxError(status, "equarx_" + fn.__name__)
 
 
+def _like(t):
+    """a contiguous matrix of t's shape and type"""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _workspace(like, nbytes):
     """(tensor to keep until the call has been enqueued, its address)"""
     if not nbytes:
@@ -216,8 +221,7 @@ def gated_backward(dh, x, wg, wu, g, u, act=ACT_GELU_TANH):
     lddh, ldgu = _fits(dh, "dh", m, f, dtype, dev), _fits(g, "g", m, f, dtype, dev)
     if _fits(u, "u", m, f, dtype, dev) != ldgu:
         raise ValueError("g and u have different row strides")
-    dx, dwg = x.new_empty((m, k)), x.new_empty((f, k))
-    dwu = torch.empty_like(dwg)
+    dx, dwg, dwu = _like(x), _like(wg), _like(wu)
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
     nbytes = _backward_workspace(m, f, k, xp & 15, ldx, gp & 15, ldwg, up & 15, ldwu)
     ws, ptr = _workspace(x, nbytes)
