@@ -1,7 +1,6 @@
 // C ABI of the feed-forward block (include/equarx.h): argument checks, tensor maps, launches.
 #include <algorithm>
 #include <mutex>
-#include <vector>
 
 #include "../../include/equarx.h"
 #include "equarx_internal.h"
@@ -60,82 +59,92 @@ inline size_t codes_stride(size_t cols) { return ceil_div(cols, 32) * 16; }
 inline size_t fp4_stages(size_t cols) { return ceil_div(cols, 256); }
 
 // ---------------------------------------------------------------- device facts, constant for the process
-int current_device(int& sms) {
-    static std::mutex mu;
-    static std::vector<int> counts;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+// (kept in arrays of a fixed size: nothing here may throw into a C caller)
+constexpr int kMaxDevices = 64, kMaxKernels = 64;
+
+struct DeviceFacts {
+    int sms = 0;                 // 0: not looked up yet
+    int clusters[9] = {};        // clusters of so many CTAs that run at one time
+    bool has_clusters = false;
+};
+std::mutex g_facts_mutex;
+DeviceFacts g_facts[kMaxDevices];
+
+int device_index(int& dev) {
+    const cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_failure(e);
-    std::lock_guard<std::mutex> lock(mu);
-    if (int(counts.size()) <= dev) counts.resize(dev + 1, 0);
-    if (!counts[dev]) {
-        e = cudaDeviceGetAttribute(&counts[dev], cudaDevAttrMultiProcessorCount, dev);
+    return dev < kMaxDevices ? EQUARX_OK : cuda_failure(cudaErrorInvalidDevice);
+}
+
+int current_device(int& sms) {
+    int dev;
+    if (const int st = device_index(dev)) return st;
+    std::lock_guard<std::mutex> lock(g_facts_mutex);
+    if (!g_facts[dev].sms) {
+        const cudaError_t e = cudaDeviceGetAttribute(&g_facts[dev].sms, cudaDevAttrMultiProcessorCount, dev);
         if (e != cudaSuccess) return cuda_failure(e);
     }
-    sms = counts[dev];
+    sms = g_facts[dev].sms;
     return EQUARX_OK;
 }
 
 // Clusters of 1 .. 8 CTAs that run at one time when each CTA has an SM to itself: a cluster stays inside a
 // GPC, so this is less than the number of SMs divided by the size.
 int resident_clusters(int (&out)[9]) {
-    const void* const kernel = reinterpret_cast<const void*>(split_kernel<kHalf, kGated, false, false, false>);
-    struct Entry {
-        int dev, clusters[9];
-    };
-    static std::mutex mu;
-    static std::vector<Entry> seen;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return cuda_failure(e);
-    std::lock_guard<std::mutex> lock(mu);
-    for (const Entry& en : seen)
-        if (en.dev == dev) {
-            std::copy(en.clusters, en.clusters + 9, out);
-            return EQUARX_OK;
+    int dev;
+    if (const int st = device_index(dev)) return st;
+    std::lock_guard<std::mutex> lock(g_facts_mutex);
+    DeviceFacts& facts = g_facts[dev];
+    if (!facts.has_clusters) {
+        const void* const kernel = reinterpret_cast<const void*>(split_kernel<kHalf, kGated, false, false, false>);
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSplitSmem));
+        for (int size = 1; size <= 8 && e == cudaSuccess; ++size) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(size * 256);
+            cfg.blockDim = dim3(kSplitThreads);
+            cfg.dynamicSmemBytes = kSplitSmem;
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = size;
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&facts.clusters[size], kernel, &cfg);
         }
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSplitSmem));
-    if (e != cudaSuccess) return cuda_failure(e);
-    Entry en = {};
-    en.dev = dev;
-    for (int size = 1; size <= 8; ++size) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(size * 148);
-        cfg.blockDim = dim3(kSplitThreads);
-        cfg.dynamicSmemBytes = kSplitSmem;
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = size;
-        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&en.clusters[size], kernel, &cfg);
         if (e != cudaSuccess) return cuda_failure(e);
+        facts.clusters[1] = std::max(1, facts.clusters[1]);
+        facts.has_clusters = true;
     }
-    seen.push_back(en);
-    std::copy(en.clusters, en.clusters + 9, out);
+    std::copy(facts.clusters, facts.clusters + 9, out);
     return EQUARX_OK;
 }
 
 // kernels that need more than 48 KB of shared memory ask for it once per device
 cudaError_t allow_smem(const void* kernel) {
     struct Entry {
-        int dev;
         const void* kernel;
+        uint64_t devices;
     };
     static std::mutex mu;
-    static std::vector<Entry> seen;
+    static Entry seen[kMaxKernels];
+    static int count = 0;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     std::lock_guard<std::mutex> lock(mu);
-    for (const Entry& en : seen)
-        if (en.dev == dev && en.kernel == kernel) return cudaSuccess;
+    int i = 0;
+    while (i < count && seen[i].kernel != kernel) ++i;
+    const uint64_t bit = dev < kMaxDevices ? uint64_t(1) << dev : 0;
+    if (i < count && (seen[i].devices & bit)) return cudaSuccess;
     cudaFuncAttributes fa;
     e = cudaFuncGetAttributes(&fa, kernel);
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kBigSmem - fa.sharedSizeBytes));
-    if (e == cudaSuccess) seen.push_back(Entry{dev, kernel});
+    if (e == cudaSuccess && i < kMaxKernels) {
+        seen[i].kernel = kernel;
+        seen[i].devices |= bit;
+        count = std::max(count, i + 1);
+    }
     return e;
 }
 
@@ -350,6 +359,7 @@ int plan_split(SplitPlan& plan, size_t features, size_t tokens, int total) {
     const size_t rounds = ceil_div(plan.tiles, clusters[plan.ranks]);
     const size_t token = MODE == kGated ? 65 + 90 / plan.ranks : 40 + 80 / plan.ranks;
     plan.cost = 8500 + rounds * (ceil_div(total, plan.ranks) * (stage / 32) + plan.nt * token);
+    if (ceil_div(tokens, plan.nt) * 2 > 65535) plan.cost = ~size_t(0);      // more than a grid's second dimension
     return EQUARX_OK;
 }
 
@@ -360,10 +370,11 @@ int launch_split(SplitArgs& a, const SplitPlan& plan, size_t features, size_t to
     a.nt = plan.nt;
     a.pipe = plan.pipe;
     a.reuse = plan.reuse;
+    a.ranks = plan.ranks;
     a.own = int(ceil_div(plan.nt, plan.ranks));
     const int columns = (MODE == kGated ? 2 : 1) * (a.nt + 4 * kScaleTiles<KIND>) + 4 * kScaleTiles<KIND>;
     for (a.columns = 32; a.columns < columns;) a.columns *= 2;
-    const dim3 grid(plan.ranks, unsigned(ceil_div(features, kRowsM)),
+    const dim3 grid(unsigned(plan.ranks * ceil_div(features, kRowsM)),
                     unsigned(ceil_div(tokens, a.nt) * (MODE == kOut2 ? 2 : 1)));
     return launch(split_kernel<KIND, MODE, W_MN, X_MN, FUSED>, grid, kSplitThreads, plan.smem, plan.ranks, a, stream);
 }

@@ -1002,6 +1002,7 @@ struct SplitArgs {
     int nt;                           // tokens of a tile: a multiple of 16, at most 128
     int pipe;                         // stages in shared memory
     int columns;                      // of tensor memory: a power of two
+    int ranks;                        // CTAs of a cluster: parts of the reduction axis
     int own;                          // tokens of a tile that one CTA of the cluster adds up
     int reuse;                        // the parts lie where the stages were
     int act, bf16, save, order;
@@ -1032,7 +1033,7 @@ __host__ __device__ constexpr int split_part_bytes(int nt, int ranks) {
 //
 // Gradients: kSum2 with weights whose other axis is contiguous (W_MN); kOut2 with the tokens as the
 // reduction axis (W_MN and X_MN), features = columns of x and "tokens" = rows of a weight, the second half
-// of grid.z being the second output.
+// of grid.y being the second output.
 //
 // FUSED (4-bit, at most 16 tokens): x comes in 16 bits; the warps that write the output later quantize
 // the stages of x first, straight into the swizzled rows that the products read, which saves a launch
@@ -1055,11 +1056,11 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     const uint32_t xb = p.nt * kRowBytes, STAGE = NW * (kTileBytes + SB) + xb + SB;
     const uint32_t parts = p.reuse ? 0 : p.pipe * STAGE;      // offset of [ranks][NW][own][128] sums
 
-    const int ranks = gridDim.x, rank = uniform(cluster_rank());
+    const int ranks = p.ranks, rank = uniform(cluster_rank());
     const int total = p.stages * (MODE == kSum2 ? 2 : 1);
     const int s0 = int(int64_t(total) * rank / ranks), s1 = int(int64_t(total) * (rank + 1) / ranks);
-    const int ztiles = MODE == kOut2 ? gridDim.z / 2 : gridDim.z, which = MODE == kOut2 ? blockIdx.z / ztiles : 0;
-    const int f0 = blockIdx.y * kRowsM, t0 = (blockIdx.z - which * ztiles) * p.nt;
+    const int ttiles = MODE == kOut2 ? gridDim.y / 2 : gridDim.y, which = MODE == kOut2 ? blockIdx.y / ttiles : 0;
+    const int f0 = int(blockIdx.x / ranks) * kRowsM, t0 = (blockIdx.y - which * ttiles) * p.nt;
 
     // Tensor memory is waited for when another kernel's CTA still has it.  So that CTAs of two clusters
     // cannot wait for each other's in a circle, no CTA waits for its cluster while it has tensor memory: it

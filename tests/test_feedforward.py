@@ -262,7 +262,7 @@ def test_not_finite_elements_become_nan(fmt):
         nan[r, c // block * block:(c // block + 1) * block] = True
     assert torch.equal(back.isnan(), nan)
     w = ff.fp4_quantize(normal(40, 96, 2, torch.bfloat16), fmt)
-    for y in (ff.fp4_linear(x, w), ff.fp4_linear(x.repeat(40, 1), w)[:6]):
+    for y in (ff.fp4_linear(x, w), ff.fp4_linear(x.repeat(40, 1), w)[:6], torch.cat([ff.fp4_linear(t, w) for t in x.split(2)])):
         rows = y.isnan()
         assert bool(rows[[1, 3, 4]].all()) and not bool(rows[[0, 2, 5]].any())
 
@@ -626,11 +626,18 @@ def test_block_with_the_allreduce(fmt):
 def test_recorded_in_a_cuda_graph():
     x, w = normal(4, 256, 1, torch.bfloat16), ff.fp4_quantize(normal(200, 256, 2, torch.bfloat16))
     wg, wu = normal(64, 256, 3, torch.bfloat16), normal(64, 256, 4, torch.bfloat16)
-    want = ff.fp4_linear(x, w), ff.gated_forward(x, wg, wu)
+    big = normal(500, 256, 5, torch.bfloat16)
+
+    def everything():
+        h, g, u = ff.gated_forward(big, wg, wu, save=True)
+        return (ff.fp4_linear(x, w), ff.fp4_linear(x[:1], w), ff.gated_forward(x, wg, wu), h,
+                *ff.gated_backward(h, big, wg, wu, g, u), ff.fp4_dequantize(ff.fp4_quantize(big, eq.FP4_MX)))
+
+    want = everything()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        got = ff.fp4_linear(x, w), ff.gated_forward(x, wg, wu)
-    for _ in range(2):
+        got = everything()
+    for _ in range(3):
         for t in got:
             t.zero_()
         graph.replay()
