@@ -490,11 +490,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
 #pragma unroll
             for (int i = 0; i < 4 / (FP4 ? SETS : 1); ++i) {
                 if (i >= steps) break;
-                if (KIND == kNv) {
-                    __syncwarp();
-#pragma unroll
-                    for (int q = 0; q < SETS; ++q) factors[warp][32 * q + lane] = factor[SETS * i + q];
-                }
                 __syncwarp();
                 const int u = unit_of_step(i);
                 const bool live = u >= 0 && u < units;
@@ -510,6 +505,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                     if (lane == 0) barrier_arrive_cluster(done);
                 }
                 if (!live) continue;
+                if constexpr (KIND == kNv) {
+                    __syncwarp();                          // the step before has been scaled
+#pragma unroll
+                    for (int q = 0; q < SETS; ++q) factors[warp][32 * q + lane] = factor[SETS * i + q];
+                    __syncwarp();
+                }
                 const int col0 = n0 + 32 * u;
                 float v[32];
 #pragma unroll
