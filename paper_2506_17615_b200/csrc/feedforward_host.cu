@@ -307,21 +307,28 @@ TilePlan plan_tiles(size_t tiles_m, size_t cols, size_t stages, bool gated, bool
     return best;
 }
 
-template <int KIND, int MODE, bool A_MN, bool B_MN>
-int launch_tiles(TileArgs& a, size_t m, size_t n, cudaStream_t stream) {
+// sizes, stores and tiles of a product whose operands and outputs are set
+int finish_product(Product& g, const TilePlan& plan, size_t m, size_t n, bool gated) {
+    g.m = int(m);
+    g.n = int(n);
+    g.bn = plan.bn;
+    g.tiles_m = int(g.two ? ceil_div(m, kRowsM) : ceil_div(m, kTileM));
+    g.tiles_n = int(ceil_div(n, gated ? g.bn / 2 : g.bn));
+    g.group = 8;
+    for (int i = 0; i < 3; ++i)
+        if (g.out[i].p && g.out[i].unit >= 16 && g.out[i].dtype != EQUARX_FP32)
+            TRY(make_map(g.store[i], g.out[i].p, 2, n, m, g.out[i].ld * 2, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+    return EQUARX_OK;
+}
+
+template <int KIND, int MODE>
+int launch_tiles(const TileArgs<MODE>& a, cudaStream_t stream) {
     int sms;
     TRY(current_device(sms));
-    a.m = int(m);
-    a.n = int(n);
-    a.tiles_m = int(MODE == kOut2 ? ceil_div(m, kRowsM) : ceil_div(m, kTileM));
-    a.tiles_n = int(ceil_div(n, MODE == kGated ? a.bn / 2 : a.bn));
-    a.group = 8;
-    for (int i = 0; i < 3; ++i)
-        if (a.out[i].p && a.out[i].unit >= 16 && a.out[i].dtype != EQUARX_FP32)
-            TRY(make_map(a.store[i], a.out[i].p, 2, n, m, a.out[i].ld * 2, 32, CU_TENSOR_MAP_SWIZZLE_64B));
-    const size_t tiles = size_t(a.tiles_m) * a.tiles_n;
+    size_t tiles = 0;
+    for (const Product& g : a.product) tiles += size_t(g.tiles_m) * g.tiles_n;
     // a pair of CTAs on the two SMs of each TPC; the kernel declares the cluster
-    return launch(tile_kernel<KIND, MODE, A_MN, B_MN>, dim3(unsigned(2 * std::min<size_t>(tiles, sms / 2))), kTileThreads<KIND>,
+    return launch(tile_kernel<KIND, MODE>, dim3(unsigned(2 * std::min<size_t>(tiles, sms / 2))), kTileThreads<KIND>,
                   kTileSmem<KIND>, 1, a, stream);
 }
 
@@ -410,21 +417,23 @@ int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int ac
         a.act = act;
         return launch_split<KIND, MODE, false, false, false>(a, split, n, m, stream);
     }
-    TileArgs a = {};
-    a.bn = tiles.bn;
+    TileArgs<MODE> a = {};
+    Product& g = a.product[0];
     const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
-    TRY(make_map(a.a[0], x.codes, 1, stride, m, stride, kRowsM));
+    TRY(make_map(g.a[0], x.codes, 1, stride, m, stride, kRowsM));
     TRY(scale_map(a.scales_a, x.scales, m, k, format));
     a.row_a = x.row_scales;
     for (int i = 0; i < (MODE == kGated ? 2 : 1); ++i) {
-        TRY(make_map(a.b[i], w[i].codes, 1, stride, n, stride, a.bn / 2));
+        TRY(make_map(g.b[i], w[i].codes, 1, stride, n, stride, tiles.bn / 2));
         TRY(scale_map(a.scales_b[i], w[i].scales, n, k, format));
         a.row_b[i] = w[i].row_scales;
     }
-    a.out[0] = out;
-    a.stages = int(fp4_stages(k));
+    g.out[0] = out;
+    g.stages = int(fp4_stages(k));
+    g.parts = 1;
     a.act = act;
-    return launch_tiles<KIND, MODE, false, false>(a, m, n, stream);
+    TRY(finish_product(g, tiles, m, n, MODE == kGated));
+    return launch_tiles<KIND, MODE>(a, stream);
 }
 
 // the workspace of a quantized activation: scales, row factors, codes
@@ -478,25 +487,33 @@ inline size_t copy_bytes(size_t rows, size_t cols, const void* p, size_t ld) {
 struct Operand {
     const void* p;
     size_t ld;
+    size_t rows, cols;
 };
-int readable(Operand& o, size_t rows, size_t cols, uint8_t*& ws, cudaStream_t stream) {
-    if (!needs_copy(o.p, o.ld)) return EQUARX_OK;
+// copies those that TMA cannot read to the workspace, with one launch
+int make_readable(std::initializer_list<Operand*> operands, uint8_t*& ws, cudaStream_t stream) {
     PackArgs a = {};
-    a.src = static_cast<const uint16_t*>(o.p);
-    a.dst = reinterpret_cast<uint16_t*>(ws);
-    a.ld_src = o.ld;
-    a.ld_dst = up(cols, 8);
-    a.cols = int(cols);
-    a.unit = unit_of(o.p, o.ld, 2);
-    const int threads = int(std::min<size_t>(512, up(ceil_div(a.ld_dst, 4), 32)));
-    TRY(launch(pack_kernel, dim3(unsigned(rows)), threads, 0, 1, a, stream));
-    ws += copy_bytes(rows, cols, o.p, o.ld);
-    o.p = a.dst;
-    o.ld = a.ld_dst;
-    return EQUARX_OK;
+    size_t rows = 0;
+    int jobs = 0, threads = 32;
+    for (Operand* o : operands) {
+        if (!needs_copy(o->p, o->ld)) continue;
+        PackJob& g = a.job[jobs++];
+        g.src = static_cast<const uint16_t*>(o->p);
+        g.dst = reinterpret_cast<uint16_t*>(ws);
+        g.ld_src = o->ld;
+        g.ld_dst = up(o->cols, 8);
+        g.rows = int(o->rows);
+        g.cols = int(o->cols);
+        g.unit = unit_of(o->p, o->ld, 2);
+        rows += o->rows;
+        threads = std::max(threads, int(std::min<size_t>(512, up(ceil_div(g.ld_dst, 4), 32))));
+        ws += copy_bytes(o->rows, o->cols, o->p, o->ld);
+        o->p = g.dst;
+        o->ld = g.ld_dst;
+    }
+    return jobs ? launch(pack_kernel, dim3(unsigned(rows)), threads, 0, 1, a, stream) : EQUARX_OK;
 }
-inline int map16(CUtensorMap& map, const Operand& o, size_t rows, size_t cols, size_t box_rows) {
-    return make_map(map, o.p, 2, cols, rows, o.ld * 2, box_rows);
+inline int map16(CUtensorMap& map, const Operand& o, size_t box_rows) {
+    return make_map(map, o.p, 2, o.cols, o.rows, o.ld * 2, box_rows);
 }
 
 }  // namespace
@@ -644,10 +661,8 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
                       {matrix(h, m, f, ldh, 2), matrix(g, m, f, ldgu, 2), matrix(u, m, f, ldgu, 2), Span{workspace, need}}));
 
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    Operand ox{x, ldx}, og{wg, ldwg}, ou{wu, ldwu};
-    TRY(readable(ox, m, k, ws, stream));
-    TRY(readable(og, f, k, ws, stream));
-    TRY(readable(ou, f, k, ws, stream));
+    Operand ox{x, ldx, m, k}, og{wg, ldwg, f, k}, ou{wu, ldwu, f, k};
+    TRY(make_readable({&ox, &og, &ou}, ws, stream));
     const Out oh = out_rows(h, ldh, dtype), sg = out_rows(g, ldgu, dtype), su = out_rows(u, ldgu, dtype);
     const int stages = int(ceil_div(k, 64));
     int sms;
@@ -657,9 +672,9 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     TRY((plan_split<kHalf, kGated, false>(split, f, m, stages)));
     if (split.cost < tiles.cost) {
         SplitArgs a = {};
-        TRY(map16(a.w[0], og, f, k, kRowsM));
-        TRY(map16(a.w[1], ou, f, k, kRowsM));
-        TRY(map16(a.x[0], ox, m, k, split.nt));
+        TRY(map16(a.w[0], og, kRowsM));
+        TRY(map16(a.w[1], ou, kRowsM));
+        TRY(map16(a.x[0], ox, split.nt));
         a.out[0] = oh;
         a.out[1] = sg;
         a.out[2] = su;
@@ -669,19 +684,21 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
         a.save = g != nullptr;
         return launch_split<kHalf, kGated, false, false, false>(a, split, f, m, stream);
     }
-    TileArgs a = {};
-    a.bn = tiles.bn;
-    TRY(map16(a.a[0], ox, m, k, kRowsM));
-    TRY(map16(a.b[0], og, f, k, a.bn / 2));
-    TRY(map16(a.b[1], ou, f, k, a.bn / 2));
-    a.out[0] = oh;
-    a.out[1] = sg;
-    a.out[2] = su;
-    a.stages = stages;
+    TileArgs<kGated> a = {};
+    Product& p = a.product[0];
+    TRY(map16(p.a[0], ox, kRowsM));
+    TRY(map16(p.b[0], og, tiles.bn / 2));
+    TRY(map16(p.b[1], ou, tiles.bn / 2));
+    p.out[0] = oh;
+    p.out[1] = sg;
+    p.out[2] = su;
+    p.stages = stages;
+    p.parts = 1;
     a.act = act;
     a.bf16 = dtype == EQUARX_BF16;
     a.save = g != nullptr;
-    return launch_tiles<kHalf, kGated, false, false>(a, m, f, stream);
+    TRY(finish_product(p, tiles, m, f, true));
+    return launch_tiles<kHalf>(a, stream);
 }
 
 size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, const void* x, size_t ldx, const void* wg, size_t ldwg,
@@ -719,12 +736,10 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     int sms;
     TRY(current_device(sms));
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    Operand ox{x, ldx}, og{wg, ldwg}, ou{wu, ldwu};
-    TRY(readable(ox, m, k, ws, stream));
-    TRY(readable(og, f, k, ws, stream));
-    TRY(readable(ou, f, k, ws, stream));
+    Operand ox{x, ldx, m, k}, og{wg, ldwg, f, k}, ou{wu, ldwu, f, k};
+    TRY(make_readable({&ox, &og, &ou}, ws, stream));
     const size_t ldd = up(f, 8);
-    Operand dg{ws, ldd}, du{ws + up(m * ldd * 2, 256), ldd};
+    const Operand dg{ws, ldd, m, f}, du{ws + up(m * ldd * 2, 256), ldd, m, f};
 
     GradArgs e = {};
     e.dh = dh;
@@ -742,62 +757,69 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     const int threads = int(std::min<size_t>(512, up(ceil_div(f, 8 * kGradGroups), 32)));
     TRY(launch(gate_grad_kernel, dim3(unsigned(m)), threads, 0, 1, e, stream));
 
-    // dx = dG Wg + dU Wu: the reduction runs over f, twice
+    // dx = dG Wg + dU Wu, whose reduction runs over f, twice, and dWg = dG^T x, dWu = dU^T x, whose runs over the
+    // tokens.  Neither needs the other's result: where both take tiles they are one launch; else dx goes first and the
+    // second begins on the SMs that it leaves idle.
     const int fs = int(ceil_div(f, 64)), ms = int(ceil_div(m, 64)), bf16 = dtype == EQUARX_BF16;
-    TilePlan tiles = plan_tiles(ceil_div(m, kTileM), k, 2 * fs, false, false, sms);
-    SplitPlan split;
-    TRY((plan_split<kHalf, kSum2, false>(split, k, m, 2 * fs)));
-    if (split.cost < tiles.cost) {
+    const Out ox_out = out_rows(dx, lddx, dtype), og_out = out_rows(dwg, lddwg, dtype), ou_out = out_rows(dwu, lddwu, dtype);
+    const TilePlan tiles_x = plan_tiles(ceil_div(m, kTileM), k, 2 * fs, false, false, sms);
+    const TilePlan tiles_w = plan_tiles(ceil_div(f, kRowsM), k, ms, false, false, sms);
+    SplitPlan split_x, split_w;
+    TRY((plan_split<kHalf, kSum2, false>(split_x, k, m, 2 * fs)));
+    TRY((plan_split<kHalf, kOut2, true>(split_w, k, f, ms)));
+    const bool x_splits = split_x.cost < tiles_x.cost, w_splits = split_w.cost < tiles_w.cost;
+
+    TileArgs<kGrads> t = {};
+    t.bf16 = bf16;
+    if (!x_splits) {
+        Product& p = t.product[0];
+        TRY(map16(p.a[0], dg, kRowsM));
+        TRY(map16(p.a[1], du, kRowsM));
+        TRY(map16(p.b[0], og, 64));
+        TRY(map16(p.b[1], ou, 64));
+        p.out[0] = ox_out;
+        p.stages = fs;
+        p.parts = 2;
+        TRY(finish_product(p, tiles_x, m, k, false));
+    }
+    if (!w_splits) {
+        Product& p = t.product[1];
+        TRY(map16(p.a[0], dg, 64));
+        TRY(map16(p.a[1], du, 64));
+        TRY(map16(p.b[0], ox, 64));
+        p.out[0] = og_out;
+        p.out[1] = ou_out;
+        p.stages = ms;
+        p.parts = p.a_mn = p.two = 1;
+        TRY(finish_product(p, tiles_w, f, k, false));
+    }
+    if (x_splits) {
         SplitArgs a = {};
-        TRY(map16(a.w[0], og, f, k, 64));
-        TRY(map16(a.w[1], ou, f, k, 64));
-        TRY(map16(a.x[0], dg, m, f, split.nt));
-        TRY(map16(a.x[1], du, m, f, split.nt));
-        a.out[0] = out_rows(dx, lddx, dtype);
+        TRY(map16(a.w[0], og, 64));
+        TRY(map16(a.w[1], ou, 64));
+        TRY(map16(a.x[0], dg, split_x.nt));
+        TRY(map16(a.x[1], du, split_x.nt));
+        a.out[0] = ox_out;
         a.stages = fs;
         a.bf16 = bf16;
         a.order = kForwarding;
-        TRY((launch_split<kHalf, kSum2, true, false, false>(a, split, k, m, stream)));
-    } else {
-        TileArgs a = {};
-        a.bn = tiles.bn;
-        TRY(map16(a.a[0], dg, m, f, kRowsM));
-        TRY(map16(a.a[1], du, m, f, kRowsM));
-        TRY(map16(a.b[0], og, f, k, 64));
-        TRY(map16(a.b[1], ou, f, k, 64));
-        a.out[0] = out_rows(dx, lddx, dtype);
-        a.stages = fs;
-        a.bf16 = bf16;
-        a.order = kForwarding;
-        TRY((launch_tiles<kHalf, kSum2, false, true>(a, m, k, stream)));
+        TRY((launch_split<kHalf, kSum2, true, false, false>(a, split_x, k, m, stream)));
     }
-    // dWg = dG^T x, dWu = dU^T x: the reduction runs over the tokens.  Needs nothing of dx's launch, so it begins on
-    // the SMs that dx leaves idle.
-    tiles = plan_tiles(ceil_div(f, kRowsM), k, ms, false, false, sms);
-    TRY((plan_split<kHalf, kOut2, true>(split, k, f, ms)));
-    if (split.cost < tiles.cost) {
-        SplitArgs a = {};
-        TRY(map16(a.w[0], ox, m, k, 64));
-        TRY(map16(a.x[0], dg, m, f, 64));
-        TRY(map16(a.x[1], du, m, f, 64));
-        a.out[0] = out_rows(dwg, lddwg, dtype);
-        a.out[1] = out_rows(dwu, lddwu, dtype);
-        a.stages = ms;
-        a.bf16 = bf16;
-        a.order = kBeside;
-        return launch_split<kHalf, kOut2, true, true, false>(a, split, k, f, stream);
+    if (!x_splits || !w_splits) {
+        t.order = x_splits ? kBeside : w_splits ? kForwarding : kOrdered;
+        TRY(launch_tiles<kHalf>(t, stream));
     }
-    TileArgs a = {};
-    a.bn = tiles.bn;
-    TRY(map16(a.a[0], dg, m, f, 64));
-    TRY(map16(a.a[1], du, m, f, 64));
-    TRY(map16(a.b[0], ox, m, k, 64));
-    a.out[0] = out_rows(dwg, lddwg, dtype);
-    a.out[1] = out_rows(dwu, lddwu, dtype);
+    if (!w_splits) return EQUARX_OK;
+    SplitArgs a = {};
+    TRY(map16(a.w[0], ox, 64));
+    TRY(map16(a.x[0], dg, 64));
+    TRY(map16(a.x[1], du, 64));
+    a.out[0] = og_out;
+    a.out[1] = ou_out;
     a.stages = ms;
     a.bf16 = bf16;
     a.order = kBeside;
-    return launch_tiles<kHalf, kOut2, true, true>(a, f, k, stream);
+    return launch_split<kHalf, kOut2, true, true, false>(a, split_w, k, f, stream);
 }
 
 int equarx_feedforward_check(void) {

@@ -19,7 +19,7 @@ namespace ff {
 using namespace tc;
 
 enum Kind { kHalf = 0, kMx = 1, kNv = 2 };                 // 16-bit operands, 4-bit with either scale format
-enum Mode { kPlain = 0, kGated = 1, kSum2 = 2, kOut2 = 3 };
+enum Mode { kPlain = 0, kGated = 1, kSum2 = 2, kOut2 = 3, kGrads = 4 };
 enum DType { kBf16 = 0, kFp16 = 1, kFp32 = 2 };
 enum Act { kSilu = 0, kGeluTanh = 1 };
 
@@ -206,16 +206,24 @@ __device__ __forceinline__ void scale_columns(float (&v)[32], float row, const f
 }
 
 // ---------------------------------------------------------------- persistent tiles
-struct TileArgs {
+// One product: out = a b^T, by tiles of 256 x bn.
+struct Product {
     CUtensorMap a[2], b[2];
-    CUtensorMap scales_a, scales_b[2];    // 4-bit: the scales of 128 rows and one stage are rows of 128 bytes
     CUtensorMap store[3];                 // 16-bit outputs with aligned rows: blocks of 32 x 32
-    const float* row_a;                   // NV: one factor for each row of a and of b
-    const float* row_b[2];
     Out out[3];                           // gated: h, g, u; two outputs: one each
     int m, n;                             // rows and columns of an output
-    int stages;                           // stages of the reduction axis (of each of the two parts of kSum2)
+    int stages;                           // of the reduction axis, in each part
+    int parts;                            // 2: out = a0 b0 + a1 b1
+    int a_mn;                             // gradients: the other axis of a is the contiguous one
+    int two;                              // two outputs, out0 = a0 b0 and out1 = a1 b0
     int tiles_m, tiles_n, bn, group;
+};
+// Gradients come two products to a launch, all others one.
+template <int MODE> struct TileArgs {
+    Product product[MODE == kGrads ? 2 : 1];
+    CUtensorMap scales_a, scales_b[2];    // 4-bit: the scales of 128 rows and one stage are rows of 128 bytes
+    const float* row_a;                   // NV: one factor for each row of a and of b
+    const float* row_b[2];
     int act, bf16, save, order;
 };
 
@@ -234,7 +242,7 @@ static_assert(kTileSmem<kHalf> + 512 <= 227 * 1024 && kTileSmem<kMx> + 512 <= 22
 
 // tile t in an order that walks `group` row tiles before the next column tile: the tiles that run at
 // one time share operands in L2
-__device__ __forceinline__ void tile_at(const TileArgs& p, int t, int& mt, int& nt) {
+__device__ __forceinline__ void tile_at(const Product& p, int t, int& mt, int& nt) {
     const int per = p.group * p.tiles_n, g = t / per, first = g * p.group;
     const int gm = min(p.group, p.tiles_m - first), r = t - g * per;
     mt = first + r % gm;
@@ -253,16 +261,19 @@ __device__ __forceinline__ void tile_at(const TileArgs& p, int t, int& mt, int& 
 //
 // kGated: columns [0, bn/2) of the tile, the first CTA's half of b, are x Wg^T and [bn/2, bn) the same
 // columns of x Wu^T, so a thread finds g and u of one element in its own row and writes act(g) u.
-// Measured: 16 bits, 8192 x 5376 by 2 x (2688 x 5376): 300 us, 1.57 PFLOP/s, tensor cores active 91 % of a CTA's
-// cycles, bound by the power cap (1.3 - 1.6 GHz); single CTAs of 128 x 256 took 442.  4 bits, 8192 x 5376 x 5376: MX 88 us,
-// 5.4 PFLOP/s, NV 94 us, bound by the loads of a stage (36 and 38 KB a CTA in 500 cycles); with 2688 for the
-// reduction 57 and 60 us, where a tile's 11 stages no longer hide the 1700 cycles between accumulators.
+// kGrads: two products one after the other, dx = dG Wg + dU Wu and the weights' gradients dG^T x, dU^T x.  The
+// latter's rows lie one below the other in blocks of 128, and a CTA's block belongs to one of them (21 blocks each
+// of 2688 rows make 21 tiles, not 2 x 11).
 //
-// kSum2: out = a0 b0 + a1 b1.  kOut2: out0 = a0 b0, out1 = a1 b0, the rows of both one below the other in
-// blocks of 128: a CTA's block belongs to one of them (21 blocks each of 2688 rows make 21 tiles, not 2 x 11).
-template <int KIND, int MODE, bool A_MN, bool B_MN>
+// Measured: 16 bits, 8192 x 5376 by 2 x (2688 x 5376): 300 us, 1.57 PFLOP/s, tensor cores active 91 % of a CTA's
+// cycles, bound by the power cap (1.3 - 1.6 GHz); single CTAs of 128 x 256 took 442.  4 bits, 8192 x 2688 x 5376, MX 50 us,
+// 4.7 PFLOP/s, NV 60: a tile's 11 stages do not hide the 900 cycles between its last product and the next
+// tile's first, nor NV's scale copies; longer reductions reach 5.4 and 5.1 PFLOP/s (5376), bound by the loads of a
+// stage (36 and 38 KB a CTA in 500 cycles).
+template <int KIND, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 1)
-    tile_kernel(const __grid_constant__ TileArgs p) {
+    tile_kernel(const __grid_constant__ TileArgs<MODE> p) {
+    constexpr bool B_MN = MODE == kGrads;
     constexpr bool FP4 = KIND != kHalf;
     constexpr int PIPE = kPipe<KIND>, STAGE = kStageBytes<KIND>, SB = kScaleBytes<KIND>;
     constexpr uint32_t kSecond = FP4 ? 192 : 256;       // first column of the second accumulator
@@ -299,15 +310,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
     fence_after();
     const uint32_t tmem = uniform(tmem_slot);
 
-    const int tiles = p.tiles_m * p.tiles_n;
-    const int stages = p.stages * (MODE == kSum2 ? 2 : 1);
-    const int half = p.bn / 2;                          // columns of b in each CTA
-    const int width = MODE == kGated ? half : p.bn;     // output columns of a tile
-    // this CTA's rows of row tile mt, and the output they belong to
-    auto rows_of = [&](int mt, int& which) {
-        const int block = mt * 2 + rank, blocks = (p.m + kRowsM - 1) / kRowsM;
-        which = MODE == kOut2 && block >= blocks;
-        return (block - which * blocks) * kRowsM;
+    const int first = p.product[0].tiles_m * p.product[0].tiles_n;
+    int tiles = first;
+    if constexpr (MODE == kGrads) tiles += p.product[1].tiles_m * p.product[1].tiles_n;
+    // tile t: its product, its place there, and this CTA's rows with the output they belong to
+    auto tile_of = [&](int t, int& mt, int& nt, int& m0, int& which) -> const Product& {
+        const bool second = MODE == kGrads && t >= first;
+        const Product& g = p.product[second];
+        tile_at(g, second ? t - first : t, mt, nt);
+        const int block = mt * 2 + rank, blocks = (g.m + kRowsM - 1) / kRowsM;
+        which = MODE == kGrads && g.two && block >= blocks;
+        m0 = (block - which * blocks) * kRowsM;
+        return g;
     };
     grid_begin(p.order);
 
@@ -319,25 +333,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
         uint32_t slot = 0, phase = 1, issued = 0;
         bool ok = true;
         for (int t = pair; t < tiles && ok; t += pairs) {
-            int mt, nt, which;
-            tile_at(p, t, mt, nt);
-            const int m0 = rows_of(mt, which);
-            const int n0 = nt * width + (MODE == kGated ? 0 : rank * half);
+            int mt, nt, m0, which;
+            const Product& g = tile_of(t, mt, nt, m0, which);
+            const int half = g.bn / 2;                     // columns of b in each CTA
+            const int n0 = MODE == kGated ? nt * half : nt * g.bn + rank * half;
             uint32_t bytes = 2 * kTileBytes + 2 * (B_MN ? (half + 63) / 64 * kChunkBytes : half * kRowBytes);
             if (FP4) {
-                const int groups_a = (p.m + 127) / 128, nb = min(width / 128, (p.n + 127) / 128 - nt * width / 128);
+                const int width = MODE == kGated ? half : g.bn;
+                const int groups_a = (g.m + 127) / 128, nb = min(width / 128, (g.n + 127) / 128 - nt * width / 128);
                 bytes += SB * (min(2, groups_a - mt * 2) + 2 * nb * (MODE == kGated ? 2 : 1));
             }
-#pragma unroll
-            for (int part = 0; part < (MODE == kSum2 ? 2 : 1); ++part) {
-                const CUtensorMap* const ma = &p.a[MODE == kOut2 ? which : part];
-                const CUtensorMap* const mb = &p.b[MODE == kGated ? rank : part];
+            const int parts = MODE == kGrads ? g.parts : 1;
+            for (int part = 0; part < parts; ++part) {
+                const CUtensorMap* const ma = &g.a[which | part];      // one of them is 0
+                const CUtensorMap* const mb = &g.b[MODE == kGated ? rank : part];
+                const bool a_mn = MODE == kGrads && g.a_mn;
                 int kc = 0;
-                for (int s = 0; s < p.stages; ++s, kc += FP4 ? kRowBytes : 64) {      // 4-bit codes travel as bytes
+                for (int s = 0; s < g.stages; ++s, kc += FP4 ? kRowBytes : 64) {      // 4-bit codes travel as bytes
                     if (!(ok = barrier_wait_warp(empty + 8 * slot, phase, &abort))) break;
                     const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, bar = counted + 8 * slot;
                     if (rank == 0) barrier_expect_warp(full + 8 * slot, bytes);
-                    if (A_MN) {
+                    if (a_mn) {
                         tma_load_2d_pair(sa, ma, m0, kc, bar);
                         tma_load_2d_pair(sa + kChunkBytes, ma, m0 + 64, kc, bar);
                     } else {
@@ -368,14 +384,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
         uint32_t slot = 0, phase = 1;
         bool ok = true;
         for (int t = pair; t < tiles && ok; t += pairs) {
-            int mt, nt;
-            tile_at(p, t, mt, nt);
+            int mt, nt, m0, which;
+            const Product& g = tile_of(t, mt, nt, m0, which);
+            const int width = MODE == kGated ? g.bn / 2 : g.bn;
             // groups of 128 rows: of a this CTA's own (which may not exist), of b all of the tile's
-            const int ga = mt * 2 + rank, gb = nt * width / 128, nb = min(width / 128, (p.n + 127) / 128 - gb);
-            const bool has_a = ga < (p.m + 127) / 128;
-            int ya = ga * p.stages * (SB / 128), yb = gb * p.stages * (SB / 128);
-            const int next = p.stages * (SB / 128);
-            for (int s = 0; s < p.stages; ++s, ya += SB / 128, yb += SB / 128) {
+            const int ga = mt * 2 + rank, gb = nt * width / 128, nb = min(width / 128, (g.n + 127) / 128 - gb);
+            const bool has_a = ga < (g.m + 127) / 128;
+            const int next = g.stages * (SB / 128);
+            int ya = ga * next, yb = gb * next;
+            for (int s = 0; s < g.stages; ++s, ya += SB / 128, yb += SB / 128) {
                 if (!(ok = barrier_wait_warp(empty + 8 * slot, phase, &abort))) break;
                 const uint32_t ss = smem + slot * STAGE + 2 * kTileBytes, bar = counted + 8 * slot;
                 if (has_a) tma_load_2d_pair(ss, &p.scales_a, 0, ya, bar);
@@ -397,6 +414,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs, ++local) {
                 const uint32_t buf = local & 1, d = tmem + buf * kSecond;
+                const Product& g = p.product[MODE == kGrads && t >= first];
+                const int stages = g.stages * (MODE == kGrads ? g.parts : 1);
+                const bool a_mn = MODE == kGrads && g.a_mn;
+                const uint32_t idesc = FP4 ? 0 : desc_16bit(p.bf16, a_mn, B_MN, kTileM, g.bn);
                 for (int s = 0; s < stages; ++s) {
                     if (!(ok = barrier_wait_warp(full + 8 * slot, phase, &abort))) break;
                     fence_after();
@@ -406,7 +427,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                         for (int j = 0; j < kScaleTiles<KIND>; ++j) {
                             copy_scales<2>(ta + 4 * j, ss + 512 * j);
                             copy_scales<2>(tb + 8 * j, ss + SB + 512 * j);
-                            if (p.bn > 128) copy_scales<2>(tb + 8 * j + 4, ss + 2 * SB + 512 * j);
+                            if (g.bn > 128) copy_scales<2>(tb + 8 * j + 4, ss + 2 * SB + 512 * j);
                         }
                     }
                     if (s == 0) {
@@ -421,16 +442,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                     }
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) {
-                        const uint32_t da = A_MN ? swizzled_desc(sa + 2048 * kk, kChunkBytes)
+                        const uint32_t da = a_mn ? swizzled_desc(sa + 2048 * kk, kChunkBytes)
                                                  : swizzled_desc(sa + 32 * kk, 16);
                         const uint32_t db = B_MN ? swizzled_desc(sb + 2048 * kk, kChunkBytes)
                                                  : swizzled_desc(sb + 32 * kk, 16);
                         if constexpr (FP4) {
                             const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
-                            mma_fp4<2, KIND == kMx>(d, da, db, desc_fp4(KIND == kMx, kTileM, p.bn, which), ta + 4 * j,
+                            mma_fp4<2, KIND == kMx>(d, da, db, desc_fp4(KIND == kMx, kTileM, g.bn, which), ta + 4 * j,
                                                     tb + 8 * j, s | kk);
                         } else {
-                            mma_16bit<2>(d, da, db, desc_16bit(p.bf16, A_MN, B_MN, kTileM, p.bn), s | kk);
+                            mma_16bit<2>(d, da, db, idesc, s | kk);
                         }
                     }
                     mma_commit<2>(empty + 8 * slot);
@@ -450,22 +471,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
     } else {
         // ---------------------------------------------------- outputs
         const int quarter = warp & 3, side = warp >> 2;
-        const int units = width / 32;                      // blocks of 32 output columns
         uint32_t local = 0, flip = 0;
         const uint32_t staging = smem + PIPE * STAGE + warp * 2 * kStageOut;
-        auto store = [&](int i, int row0, int col0, float (&v)[32]) {
-            if (row0 >= p.m || col0 >= p.n) return;
-            if (p.out[i].unit >= 16 && p.out[i].dtype != kFp32) {
-                store_staged(&p.store[i], staging + flip, row0, col0, p.out[i].dtype, v);
+        auto store = [&](const Product& g, int i, int row0, int col0, float (&v)[32]) {
+            if (row0 >= g.m || col0 >= g.n) return;
+            if (g.out[i].unit >= 16 && g.out[i].dtype != kFp32) {
+                store_staged(&g.store[i], staging + flip, row0, col0, g.out[i].dtype, v);
                 flip ^= kStageOut;
             } else {
-                store_direct(p.out[i], staging, row0, col0, p.m, p.n, v);
+                store_direct(g.out[i], staging, row0, col0, g.m, g.n, v);
             }
         };
         for (int t = pair; t < tiles; t += pairs, ++local) {
-            int mt, nt, which;
-            tile_at(p, t, mt, nt);
-            const int row0 = rows_of(mt, which) + quarter * 32, n0 = nt * width;
+            int mt, nt, m0, which;
+            const Product& g = tile_of(t, mt, nt, m0, which);
+            const int half = g.bn / 2, width = MODE == kGated ? half : g.bn;
+            const int units = width / 32;                  // blocks of 32 output columns
+            const int row0 = m0 + quarter * 32, n0 = nt * width;
             const uint32_t buf = local & 1, acc = tmem + buf * kSecond + (uint32_t(quarter * 32) << 16);
             const uint32_t done = peer_addr(FP4 ? drained : drained + 8 * buf, 0);
             float ra = 1.0f;
@@ -477,11 +499,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
             constexpr int SETS = MODE == kGated ? 2 : 1;
             float factor[4];                               // of each step, gate before up: at most 4 in all
             if (KIND == kNv) {
-                if (row0 + lane < p.m) ra = p.row_a[row0 + lane];
+                if (row0 + lane < g.m) ra = p.row_a[row0 + lane];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int col = n0 + 32 * unit_of_step(i / SETS) + lane;
-                    factor[i] = col >= n0 && col < p.n ? p.row_b[i % SETS][col] : 0.0f;
+                    factor[i] = col >= n0 && col < g.n ? p.row_b[i % SETS][col] : 0.0f;
                 }
             }
             if (!barrier_wait(ready + 8 * buf, local / 2 & 1, &abort)) break;
@@ -524,13 +546,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                     float h[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) h[j] = act(v[j], p.act) * w[j];
-                    store(0, row0, col0, h);
+                    store(g, 0, row0, col0, h);
                     if (KIND == kHalf && p.save) {
-                        store(1, row0, col0, v);
-                        store(2, row0, col0, w);
+                        store(g, 1, row0, col0, v);
+                        store(g, 2, row0, col0, w);
                     }
                 } else {
-                    store(which, row0, col0, v);
+                    store(g, which, row0, col0, v);
                 }
             }
         }
@@ -611,25 +633,32 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
     }
 }
 
-// rows x cols 16-bit words to rows whose stride is a multiple of 16 bytes
-struct PackArgs {
+// 16-bit words to rows whose stride is a multiple of 16 bytes, up to three matrices in a launch
+struct PackJob {
     const uint16_t* src;
     uint16_t* dst;
     size_t ld_src, ld_dst;
-    int cols, unit;
+    int rows, cols, unit;
+};
+struct PackArgs {
+    PackJob job[3];
 };
 // One CTA a row.  The source is read in words of 4 bytes where its rows start on such, else of 2.
 __global__ void __launch_bounds__(512) pack_kernel(const __grid_constant__ PackArgs p) {
     grid_launch();
     grid_wait();
-    const uint16_t* const src = p.src + blockIdx.x * p.ld_src;
-    uint16_t* const dst = p.dst + blockIdx.x * p.ld_dst;
-    for (int col = threadIdx.x * 2; col < int(p.ld_dst); col += blockDim.x * 2) {
+    size_t row = blockIdx.x;
+    int i = 0;
+    while (i < 2 && row >= size_t(p.job[i].rows)) row -= p.job[i++].rows;
+    const PackJob& g = p.job[i];
+    const uint16_t* const src = g.src + row * g.ld_src;
+    uint16_t* const dst = g.dst + row * g.ld_dst;
+    for (int col = threadIdx.x * 2; col < int(g.ld_dst); col += blockDim.x * 2) {
         uint32_t w;
-        if (p.unit >= 4 && col + 2 <= p.cols)
+        if (g.unit >= 4 && col + 2 <= g.cols)
             w = *reinterpret_cast<const uint32_t*>(src + col);
         else
-            w = (col < p.cols ? src[col] : 0) | uint32_t(col + 1 < p.cols ? src[col + 1] : 0) << 16;
+            w = (col < g.cols ? src[col] : 0) | uint32_t(col + 1 < g.cols ? src[col + 1] : 0) << 16;
         *reinterpret_cast<uint32_t*>(dst + col) = w;
     }
 }
