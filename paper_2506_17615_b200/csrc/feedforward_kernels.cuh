@@ -8,7 +8,6 @@
 //   pack_kernel       rows that TMA cannot read (a stride that is no multiple of 16 bytes) -> rows it can
 //   fp4_quantize_kernel, fp4_dequantize_kernel
 #pragma once
-#include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "tensor_ops.cuh"
@@ -19,6 +18,7 @@ namespace ff {
 using namespace tc;
 
 enum Kind { kHalf = 0, kMx = 1, kNv = 2 };                 // 16-bit operands, 4-bit with either scale format
+// what a product kernel computes; the gradients are kGrads in tiles, kSum2 (dx) and kOut2 (dWg, dWu) transposed
 enum Mode { kPlain = 0, kGated = 1, kSum2 = 2, kOut2 = 3, kGrads = 4 };
 enum DType { kBf16 = 0, kFp16 = 1, kFp32 = 2 };
 enum Act { kSilu = 0, kGeluTanh = 1 };
@@ -46,11 +46,6 @@ __device__ __forceinline__ float2 unpack2(uint32_t w, int dtype) {
     __half2 h;
     memcpy(&h, &w, 4);
     return __half22float2(h);
-}
-__device__ __forceinline__ float load1(const void* p, size_t i, int dtype) {
-    if (dtype == kBf16) return __uint_as_float(uint32_t(static_cast<const uint16_t*>(p)[i]) << 16);
-    if (dtype == kFp16) return __half2float(static_cast<const __half*>(p)[i]);
-    return static_cast<const float*>(p)[i];
 }
 __device__ __forceinline__ void store1(void* p, size_t i, float v, int dtype) {
     if (dtype == kFp32)
@@ -249,15 +244,14 @@ __device__ __forceinline__ void tile_at(const Product& p, int t, int& mt, int& n
     nt = r / gm;
 }
 
-// Output tiles of 256 x bn by pairs of CTAs: each holds half of the rows of a and half of the columns
-// of b, the tensor cores of both read both halves of b, so a pair loads (256 + bn) rows a stage where
-// two single CTAs would load 2 (128 + bn); L2 to SM traffic, not the tensor cores, bounds the single
-// form.  In each CTA one warp starts TMA loads through a ring of stages (a second one those of the scales);
-// in the first CTA one warp issues the products for both; eight warps move finished accumulators from tensor memory to the
-// output.  Two accumulators let the next tile's products run meanwhile.  4-bit operands: the scales
-// need tensor memory too, so of 256 columns the second accumulator begins 64 inside the first, and each is
-// drained from that end first.  (Tiles of 192 columns, whose accumulators share none, load more for each
-// product: 8192 x 2688 x 5376 in MX 62.0 us, with 256 columns 57.4.)
+// Output tiles of 256 x bn by pairs of CTAs: each holds half of the rows of a and half of the columns of b, the
+// tensor cores of both read both halves of b, so a pair loads (256 + bn) rows a stage where two single CTAs would
+// load 2 (128 + bn); L2 to SM traffic, not the tensor cores, bounds the single form.  In each CTA one warp starts
+// TMA loads through a ring of stages (a second one those of the scales); in the first CTA one warp issues the
+// products for both; eight warps move finished accumulators from tensor memory to the output.  Two accumulators let
+// the next tile's products run meanwhile.  4-bit operands: the scales need tensor memory too, so of 256 columns the
+// second accumulator begins 64 inside the first, and each is drained from that end first.  (Tiles of 192 columns,
+// whose accumulators share none, load more for each product: 8192 x 2688 x 5376 in MX 62.0 us, with 256 columns 57.4.)
 //
 // kGated: columns [0, bn/2) of the tile, the first CTA's half of b, are x Wg^T and [bn/2, bn) the same
 // columns of x Wu^T, so a thread finds g and u of one element in its own row and writes act(g) u.
@@ -1094,9 +1088,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
 
     // Tensor memory is waited for when another kernel's CTA still has it.  So that CTAs of two clusters
     // cannot wait for each other's in a circle, no CTA waits for its cluster while it has tensor memory: it
-    // says that it has started before it asks, and gives the memory back before it waits for the sums.  (With `reuse` it says so only when
-    // its products are done; the launch then takes all of an SM's shared memory, and no other CTA with
-    // tensor memory shares the SM.)
+    // says that it has started before it asks, and gives the memory back before it waits for the sums.  (With
+    // `reuse` it says so only when its products are done; the launch then takes all of an SM's shared memory,
+    // and no other CTA with tensor memory shares the SM.)
     if (!p.reuse) cluster_arrive();
 
     // the loading warp prepares the barriers and starts; everybody else meets it below

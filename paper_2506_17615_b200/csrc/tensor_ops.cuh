@@ -18,9 +18,6 @@ __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t arrivals) {
 __device__ __forceinline__ void barrier_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
