@@ -12,8 +12,8 @@ DEPENDS = SOURCES + [os.path.join(_CSRC, name) for name in ("equarx_kernels.cuh"
                                                             "feedforward_kernels.cuh")] + \
     [os.path.join(os.path.dirname(_HERE), "include", "equarx.h")]
 LIB = os.path.join(_HERE, "libequarx.so")
-FASTCALL_SOURCE = os.path.join(_CSRC, "fastcall.c")
-FASTCALL = os.path.join(_HERE, "_fastcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+TORCH_SOURCE = os.path.join(_CSRC, "feedforward_torch.cpp")
+TORCH_MODULE = os.path.join(_HERE, "_feedforward" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
@@ -61,23 +61,41 @@ def build(force=False, verbose=False):
     return LIB
 
 
-def build_fastcall(force=False):
-    """Compile the extension module that calls the feed-forward entry points without ctypes; returns its path.
-    It depends on the header alone, not on the library, and needs a C compiler and Python's headers."""
-    sources = (FASTCALL_SOURCE, os.path.join(os.path.dirname(_HERE), "include", "equarx.h"))
+def find_cuda_home():
+    for cand in (os.environ.get("CUDA_HOME"), os.path.dirname(os.path.dirname(find_nvcc() or "")), "/usr/local/cuda"):
+        if cand and os.path.exists(os.path.join(cand, "include", "cuda_runtime_api.h")):
+            return cand
+    raise RuntimeError("the CUDA headers were not found; set CUDA_HOME")
+
+
+def build_torch_module(force=False):
+    """Compile the extension module behind feedforward.py (torch tensors in and out); returns its path.  It
+    depends on the library's header, not on the library, and on the installed torch: a newer torch than the
+    module rebuilds it."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    sources = (TORCH_SOURCE, os.path.join(os.path.dirname(_HERE), "include", "equarx.h"), os.path.join(root, "version.py"))
 
     def stale():
-        return not os.path.exists(FASTCALL) or any(os.path.getmtime(p) > os.path.getmtime(FASTCALL) for p in sources)
+        return not os.path.exists(TORCH_MODULE) or any(os.path.getmtime(p) > os.path.getmtime(TORCH_MODULE) for p in sources)
 
     if force or stale():
-        with open(FASTCALL + ".lock", "w") as lock:
+        with open(TORCH_MODULE + ".lock", "w") as lock:
             fcntl.flock(lock, fcntl.LOCK_EX)
             try:
                 if force or stale():
-                    tmp = f"{FASTCALL}.{os.getpid()}.tmp"
-                    subprocess.run([os.environ.get("CC") or "gcc", "-O2", "-std=c11", "-Wall", "-shared", "-fPIC",
-                                    "-I", sysconfig.get_paths()["include"], "-o", tmp, FASTCALL_SOURCE], check=True)
-                    os.replace(tmp, FASTCALL)
+                    tmp = f"{TORCH_MODULE}.{os.getpid()}.tmp"
+                    include, lib = os.path.join(root, "include"), os.path.join(root, "lib")
+                    subprocess.run([os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC",
+                                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                                    "-I", sysconfig.get_paths()["include"], "-I", include,
+                                    "-I", os.path.join(include, "torch", "csrc", "api", "include"),
+                                    "-I", os.path.join(find_cuda_home(), "include"), "-o", tmp, TORCH_SOURCE,
+                                    "-L", lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
+                                    # torch's own C++ runtime, by name: where only the static one can be
+                                    # linked, a second copy in the process breaks its streams
+                                    "-l:libstdc++.so.6", f"-Wl,-rpath,{lib}"], check=True)
+                    os.replace(tmp, TORCH_MODULE)
             finally:
                 fcntl.flock(lock, fcntl.LOCK_UN)
-    return FASTCALL
+    return TORCH_MODULE

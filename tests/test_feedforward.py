@@ -149,24 +149,19 @@ def test_tensors_that_do_not_fit_are_refused():
         ff.gated_forward(x, x, x)
 
 
-def test_the_extension_module_calls_the_library():
-    """the functions that feedforward calls: the library's own status for bad arguments, an exception for
-    arguments that are no integers or too few"""
-    fast = ff._fast
-    assert fast.fp4_quantize(A, 9, 4, 64, 64, 1, A, A, A, 0) == binding.ERR_FORMAT
-    assert fast.fp4_quantize(A, 1 << 32, 4, 64, 64, 1, A, A, A, 0) == binding.ERR_FORMAT
-    assert fast.fp4_quantize(0, 0, 4, 64, 64, 1, A, A, A, 0) == binding.ERR_NULL
-    assert fast.fp4_dequantize(A, A, A, 4, 64, 1, A, 0, 60, 0) == binding.ERR_COUNT
-    assert fast.fp4_matmul(A, A, A, A, A, A, 4, 8, 64, 7, A, 0, 8, 0) == binding.ERR_FORMAT
-    assert fast.fp4_linear(A, 0, 64, A, A, A, 40, 8, 64, 1, A + GB, 8, A + 2 * GB, 0, 0) == binding.ERR_WORKSPACE
-    assert fast.fp4_gated(A, 0, 64, A, A, A, A, A, A, 4, 8, 64, 1, 5, A, 8, 0, 0, 0) == binding.ERR_FORMAT
-    assert fast.gated_forward(A, 64, A, 64, A, 64, 0, 4, 8, 64, 0, A, 7, 0, 0, 0, 0, 0, 0) == binding.ERR_COUNT
-    assert fast.gated_backward(*[A, 64] * 4, A, A, 64, 0, 4, 8, 64, 0, *[A, 64] * 3, 0, 0, 0) == binding.ERR_NULL
-    for bad in ((), (1,) * 9, (1,) * 11, (1.0,) + (1,) * 9, (-1,) + (1,) * 9, (None,) * 10):
-        with pytest.raises((TypeError, OverflowError, ValueError)):
-            fast.fp4_quantize(*bad)
-    with pytest.raises(ValueError):
-        fast.bind("nothing", A)
+def test_what_the_extension_module_refuses():
+    """before any CUDA call: what is no tensor, no matrix, not on a GPU, or the wrong number of arguments"""
+    cpu = torch.zeros(4, 8, dtype=torch.bfloat16)
+    q = ff.Fp4Matrix(torch.zeros(16, dtype=torch.uint8), 4, 8, eq.FP4_NV)
+    for call in (lambda: ff.fp4_quantize(None), lambda: ff.fp4_linear([1], q), lambda: ff.gated_forward(cpu, cpu, 3),
+                 lambda: ff._native.quantize(cpu), lambda: ff._native.linear(), lambda: ff.fp4_quantize(cpu, "nv")):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+    for call in (lambda: ff.fp4_quantize(cpu[0]), lambda: ff.fp4_dequantize(q), lambda: ff.fp4_dequantize(q, torch.float64),
+                 lambda: ff.fp4_matmul(q, q), lambda: ff.gated_backward(cpu, cpu, cpu, cpu, cpu, cpu),
+                 lambda: ff._native.bind("nothing", A)):
+        with pytest.raises(ValueError):
+            call()
 
 
 # ------------------------------------------------------------------ inputs
@@ -516,12 +511,12 @@ def test_views_that_start_anywhere(m, f, k, offset):
             back = ff.fp4_dequantize(q, out)
             assert torch.equal(back, ff.fp4_dequantize(sq, out))
             pb = shifted(torch.zeros_like(back))
-            eq.fp4_dequantize(*q._parts, m, k, fmt, pb, {torch.bfloat16: eq.BF16, torch.float32: eq.FP32}[out], k, stream)
+            eq.fp4_dequantize(q.codes, q.scales, q.row_scales, m, k, fmt, pb, {torch.bfloat16: eq.BF16, torch.float32: eq.FP32}[out], k, stream)
             assert torch.equal(pb, back)
             w = ff.fp4_quantize(wg, fmt)
             y = ff.fp4_matmul(q, w, out)
             py = shifted(torch.zeros_like(y))
-            eq.fp4_matmul(*q._parts, *w._parts, m, f, k, fmt, py, {torch.bfloat16: eq.BF16, torch.float32: eq.FP32}[out], f, stream)
+            eq.fp4_matmul(q.codes, q.scales, q.row_scales, w.codes, w.scales, w.row_scales, m, f, k, fmt, py, {torch.bfloat16: eq.BF16, torch.float32: eq.FP32}[out], f, stream)
             assert torch.equal(py, y)
         w = ff.fp4_quantize(wg, fmt)
         for rows in (1, m):
@@ -551,7 +546,7 @@ def test_offsets_beyond_32_bits():
     eq.gated_forward(dense, 96, w, 96, wu, 96, eq.BF16, rows, 40, 96, eq.ACT_GELU_TANH, out.data_ptr(), ld, 0, 0, 0, 0, 0, stream)
     assert torch.equal(out, h)
     q = ff.fp4_quantize(dense)
-    eq.fp4_dequantize(*q._parts, rows, 96, eq.FP4_NV, store.as_strided((rows, 96), (ld, 1), 2048).data_ptr(), eq.BF16, ld, stream)
+    eq.fp4_dequantize(q.codes, q.scales, q.row_scales, rows, 96, eq.FP4_NV, store.as_strided((rows, 96), (ld, 1), 2048).data_ptr(), eq.BF16, ld, stream)
     assert torch.equal(store.as_strided((rows, 96), (ld, 1), 2048), ff.fp4_dequantize(q))
     ff.check()
 
