@@ -251,13 +251,17 @@ inline Span rows_span(const Fp4& q, size_t rows, int format) {
 // threads of a row's CTA: three groups of 16 elements each, a whole number of warps
 inline int row_threads(size_t cols) { return int(std::min<size_t>(512, up(ceil_div(cols, 16 * kRowChunks), 32))); }
 
-template <bool MX>
+template <bool MX, bool ANYWHERE>
 int launch_quantize(const QuantArgs& a, cudaStream_t stream) {
     const dim3 grid(a.rows);
     const int threads = row_threads(a.cols);
-    if (a.dtype == EQUARX_BF16) return launch(fp4_quantize_kernel<MX, kBf16>, grid, threads, 0, 1, a, stream);
-    if (a.dtype == EQUARX_FP16) return launch(fp4_quantize_kernel<MX, kFp16>, grid, threads, 0, 1, a, stream);
-    return launch(fp4_quantize_kernel<MX, kFp32>, grid, threads, 0, 1, a, stream);
+    if (a.dtype == EQUARX_BF16) return launch(fp4_quantize_kernel<MX, kBf16, ANYWHERE>, grid, threads, 0, 1, a, stream);
+    if (a.dtype == EQUARX_FP16) return launch(fp4_quantize_kernel<MX, kFp16, ANYWHERE>, grid, threads, 0, 1, a, stream);
+    return launch(fp4_quantize_kernel<MX, kFp32, ANYWHERE>, grid, threads, 0, 1, a, stream);
+}
+template <bool MX>
+int launch_quantize(const QuantArgs& a, cudaStream_t stream) {
+    return a.unit < 16 ? launch_quantize<MX, true>(a, stream) : launch_quantize<MX, false>(a, stream);
 }
 QuantArgs rows_to_quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld) {
     QuantArgs a = {};
@@ -564,7 +568,8 @@ int equarx_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, const flo
     a.dtype = dtype;
     a.unit = unit_of(out, ld, size_of(dtype));
     const dim3 grid{unsigned(rows)};
-    const int threads = row_threads(cols);
+    // groups of 16 elements, or of 8 from the first aligned one
+    const int threads = a.unit < 16 ? row_threads(2 * cols + 16) : row_threads(cols);
     return format == EQUARX_FP4_MX ? launch(fp4_dequantize_kernel<true>, grid, threads, 0, 1, a, stream)
                                    : launch(fp4_dequantize_kernel<false>, grid, threads, 0, 1, a, stream);
 }

@@ -702,12 +702,6 @@ __device__ __forceinline__ void decode8(uint32_t w, float* v) {
         v[2 * i + 1] = f.y;
     }
 }
-// one code: from 2 on, exponent and mantissa bits are those of the number, with another bias; 0 and 1 are 0 and .5
-__device__ __forceinline__ float decode1(uint32_t code) {
-    const uint32_t m = code & 7;
-    const uint32_t bits = m >= 2 ? (m << 22) + (126u << 23) : m * (126u << 23);
-    return __uint_as_float(bits | (code & 8) << 28);
-}
 __device__ __forceinline__ uint32_t to_e4m3(float v) {
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
@@ -746,6 +740,43 @@ __device__ __forceinline__ void store_256(void* p, const uint32_t* w) {
 }
 
 template <int DT>
+__device__ __forceinline__ void load_elements(const QuantArgs& p, size_t row, int col, Group<DT>& g) {
+    if constexpr (DT == kFp32) {
+        const uint32_t* q = static_cast<const uint32_t*>(p.x) + row * p.ld;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) g.w[i] = col + i < p.cols ? q[col + i] : 0;
+    } else {
+        const uint16_t* q = static_cast<const uint16_t*>(p.x) + row * p.ld;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            g.w[i] = (col + 2 * i < p.cols ? q[col + 2 * i] : 0) | uint32_t(col + 2 * i + 1 < p.cols ? q[col + 2 * i + 1] : 0) << 16;
+    }
+}
+// A group that starts anywhere, from the aligned 16-byte words around it; element by element where a word
+// would reach outside the matrix or the group outside its row.  One 2- or 4-byte load for each element or
+// pair left most of a sector unused: 8192 x 5001 bf16 NV 50.3 us, now 28.6; 8192 x 5002 fp32 84.2, now 49.2; a
+// single row of 1250, which has nothing to save, 2.3 and 2.5.
+template <int DT>
+__device__ __forceinline__ void load_shifted(const QuantArgs& p, size_t row, int col, Group<DT>& g) {
+    constexpr int W = DT == kFp32 ? 16 : 8, SIZE = DT == kFp32 ? 4 : 2;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(p.x), end = first + ((p.rows - 1) * p.ld + p.cols) * SIZE;
+    const uintptr_t at = first + (row * p.ld + col) * SIZE, from = at & ~uintptr_t(15);
+    if (col + 16 > p.cols || from < first || from + 4 * W + 16 > end) return load_elements<DT>(p, row, col, g);
+    uint32_t w[W + 4];
+#pragma unroll
+    for (int i = 0; i < W + 4; i += 4) {
+        const uint4 v = reinterpret_cast<const uint4*>(from)[i / 4];
+        w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+    }
+#pragma unroll
+    for (int i = 0; i < W + 2; ++i) w[i] = at & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < W + 1; ++i) w[i] = at & 4 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < W; ++i) g.w[i] = DT == kFp32 ? w[i] : __funnelshift_r(w[i], w[i + 1], at & 2 ? 16 : 0);
+}
+// rows on multiples of 16 bytes; WORDS (16-bit types): on any multiples, best on those of 4
+template <int DT, bool WORDS>
 __device__ __forceinline__ void load_group(const QuantArgs& p, size_t row, int col, Group<DT>& g) {
     constexpr int W = DT == kFp32 ? 16 : 8, PER = 16 / W;
     if (p.unit == 32 && col + 16 <= p.cols) {
@@ -759,19 +790,12 @@ __device__ __forceinline__ void load_group(const QuantArgs& p, size_t row, int c
             const uint4 v = q[i];
             g.w[4 * i] = v.x; g.w[4 * i + 1] = v.y; g.w[4 * i + 2] = v.z; g.w[4 * i + 3] = v.w;
         }
-    } else if (DT == kFp32) {
-        const uint32_t* q = static_cast<const uint32_t*>(p.x) + row * p.ld;
-#pragma unroll
-        for (int i = 0; i < W; ++i) g.w[i] = col + i < p.cols ? q[col + i] : 0;
-    } else if (p.unit >= 4 && col + 16 <= p.cols) {
+    } else if (WORDS && p.unit >= 4 && col + 16 <= p.cols) {
         const uint32_t* q = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.x) + row * p.ld + col);
 #pragma unroll
         for (int i = 0; i < W; ++i) g.w[i] = q[i];
     } else {
-        const uint16_t* q = static_cast<const uint16_t*>(p.x) + row * p.ld;
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            g.w[i] = (col + 2 * i < p.cols ? q[col + 2 * i] : 0) | uint32_t(col + 2 * i + 1 < p.cols ? q[col + 2 * i + 1] : 0) << 16;
+        load_elements<DT>(p, row, col, g);
     }
 }
 
@@ -871,7 +895,9 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t byte) {
 // groups were no faster (8192 x 5376 NV: 25.1, 24.2 against 24.4 us; 8192 x 2688: 13.3, 16.3 against 14.0).  8192 x
 // 5376: MX 19.6 us, 5.8 TB/s of what has to move; NV 24.4 us, 4.6 TB/s, bound by instruction issue (66 %): the
 // row's maximum, a division and two conversions for every 16 elements.
-template <bool MX, int DT>
+//
+// ANYWHERE: rows that do not start on multiples of 16 bytes.
+template <bool MX, int DT, bool ANYWHERE>
 __global__ void __launch_bounds__(512) fp4_quantize_kernel(const __grid_constant__ QuantArgs p) {
     __shared__ uint32_t top[16];
     const int tid = threadIdx.x, threads = blockDim.x, span = threads * 16 * kRowChunks;
@@ -886,7 +912,11 @@ __global__ void __launch_bounds__(512) fp4_quantize_kernel(const __grid_constant
     uint32_t peak[kRowChunks];
     auto load = [&](int first) {
 #pragma unroll
-        for (int c = 0; c < kRowChunks; ++c) load_group<DT>(p, row, first + (c * threads + tid) * 16, x[c]);
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + (c * threads + tid) * 16;
+            if constexpr (ANYWHERE) load_shifted<DT>(p, row, col, x[c]);
+            else load_group<DT, false>(p, row, col, x[c]);
+        }
 #pragma unroll
         for (int c = 0; c < kRowChunks; ++c) peak[c] = group_amax<DT>(x[c]);
     };
@@ -936,6 +966,60 @@ struct DequantArgs {
     size_t ld;
     int rows, cols, dtype, unit;
 };
+// An output row that starts anywhere: groups of 8 elements begin where the output is aligned to 16 bytes, and
+// a group's codes are cut out of two neighbouring words.  It touches at most two blocks.  Two elements a
+// thread with narrow stores took 55 us for 8192 x 5001 bf16 MX; this takes 32.4.
+template <bool MX>
+__device__ __forceinline__ void dequantize_shifted(const DequantArgs& p, size_t row, float g) {
+    constexpr int B = MX ? 32 : 16;
+    const int threads = blockDim.x, stride = (p.cols + 31) / 32 * 16;
+    const size_t stages = (size_t(p.cols) + 255) / 256;
+    const int size = p.dtype == kFp32 ? 4 : 2;
+    uint8_t* const out = static_cast<uint8_t*>(p.out) + row * p.ld * size;
+    const int head = int((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / size;
+    const uint8_t* const scales = p.scales + scale_offset<MX>(row, 0, stages);
+    const uint32_t* const codes = reinterpret_cast<const uint32_t*>(p.codes + row * size_t(stride));
+    for (int first = (head ? head - 8 : 0) + int(threadIdx.x) * 8; first < p.cols; first += threads * 8 * kRowChunks) {
+        uint32_t w[kRowChunks], b0[kRowChunks], b1[kRowChunks];
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + c * threads * 8;
+            if (col >= p.cols) continue;
+            const int word = col >> 3;                     // -1 for the group before the first boundary
+            const uint32_t lo = word >= 0 ? codes[word] : 0, hi = (word + 1) * 4 < stride ? codes[word + 1] : 0;
+            w[c] = __funnelshift_r(lo, hi, (col & 7) * 4);
+            const int i0 = max(col, 0) / B, i1 = min(col + 7, p.cols - 1) / B;
+            b0[c] = scales[size_t(i0 / 4) * 512 + i0 % 4];
+            b1[c] = scales[size_t(i1 / 4) * 512 + i1 % 4];
+        }
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + c * threads * 8;
+            if (col >= p.cols) continue;
+            const float d0 = MX ? from_e8m0(b0[c]) : __fmul_rn(from_e4m3(b0[c]), g);
+            const float d1 = MX ? from_e8m0(b1[c]) : __fmul_rn(from_e4m3(b1[c]), g);
+            const int n = (max(col, 0) / B + 1) * B - col; // elements of the first block
+            float v[8];
+            decode8(w[c], v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], j < n ? d0 : d1);
+            if (col < 0 || col + 8 > p.cols) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (col + j >= 0 && col + j < p.cols) store1(out, size_t(col + j), v[j], p.dtype);
+            } else if (p.dtype == kFp32) {
+                float4* const q = reinterpret_cast<float4*>(out + size_t(col) * 4);
+                q[0] = make_float4(v[0], v[1], v[2], v[3]);
+                q[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+                *reinterpret_cast<uint4*>(out + size_t(col) * 2) =
+                    make_uint4(pack2(v[0], v[1], p.dtype), pack2(v[2], v[3], p.dtype), pack2(v[4], v[5], p.dtype),
+                               pack2(v[6], v[7], p.dtype));
+            }
+        }
+    }
+}
+
 // value = code * scale (MX), code * (scale * row factor) (NV) in fp32, rounded once to the output type.
 // One CTA a row as above: a thread's three groups are in flight together.  8192 x 5376: MX 18.9 us, 5.9 TB/s, NV
 // 22.8 us; bound by DRAM writes.
@@ -948,23 +1032,7 @@ __global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_consta
     grid_wait();
     const float g = MX ? 1.0f : p.row_scales[row];
     if (p.unit < 16) {
-        // output rows that do not start on multiples of 16 bytes: two elements a thread, so that a warp
-        // still writes neighbouring bytes
-        const uint8_t* const scales = p.scales + scale_offset<MX>(row, 0, stages);
-        for (int col = tid * 2; col < p.cols; col += threads * 2) {
-            const int block = col / (MX ? 32 : 16);
-            const uint32_t b = scales[size_t(block / 4) * 512 + block % 4];
-            const float d = MX ? from_e8m0(b) : __fmul_rn(from_e4m3(b), g);
-            const uint32_t pair = p.codes[row * size_t(stride) + col / 2];
-            const float v0 = __fmul_rn(decode1(pair & 15), d), v1 = __fmul_rn(decode1(pair >> 4), d);
-            const size_t at = row * p.ld + col;
-            if (p.unit >= 4 && p.dtype != kFp32 && col + 2 <= p.cols) {
-                *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at) = pack2(v0, v1, p.dtype);
-            } else {
-                store1(p.out, at, v0, p.dtype);
-                if (col + 1 < p.cols) store1(p.out, at + 1, v1, p.dtype);
-            }
-        }
+        dequantize_shifted<MX>(p, row, g);
         return;
     }
     for (int first = 0; first < p.cols; first += span) {
@@ -1156,14 +1224,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         };
         settle();
         Group<kBf16> next = {};                          // the bits of either type
-        if (it < n) load_group<kBf16>(p.raw, t, (s0 + it) * 256 + j * 16, next);
+        if (it < n) load_group<kBf16, true>(p.raw, t, (s0 + it) * 256 + j * 16, next);
 #pragma unroll 1
         while (__any_sync(0xFFFFFFFFu, it < n)) {
             const Group<kBf16> g = next;
             const int at = it, row = t;
             t += 8;
             settle();
-            if (it < n) load_group<kBf16>(p.raw, t, (s0 + it) * 256 + j * 16, next);
+            if (it < n) load_group<kBf16, true>(p.raw, t, (s0 + it) * 256 + j * 16, next);
             float v[16];
             uint32_t m = 0;
 #pragma unroll

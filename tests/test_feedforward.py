@@ -525,6 +525,38 @@ def test_views_that_start_anywhere(m, f, k, offset):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("cols", [1, 7, 8, 15, 16, 17, 31, 40, 250, 1001, 5002])
+def test_quantized_rows_that_start_anywhere(cols, dtype):
+    """codes, scales and values of rows at every offset are those of aligned rows; nothing is written beside them"""
+    rows, wide = 5, (cols + 31) // 32 * 32 + 32
+    code = {torch.bfloat16: eq.BF16, torch.float16: eq.FP16, torch.float32: eq.FP32}[dtype]
+    stream = torch.cuda.current_stream().cuda_stream
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    aligned = torch.randn(rows, wide, device="cuda", generator=gen).to(dtype)[:, :cols]
+    for fmt in FORMATS:
+        want = ff.fp4_quantize(aligned, fmt)
+        out = torch.empty(rows, wide, device="cuda", dtype=dtype)
+        eq.fp4_dequantize(want.codes, want.scales, want.row_scales, rows, cols, fmt, out, code, wide, stream)
+        pos = ref.scale_positions(rows, -(-cols // (32 if fmt == eq.FP4_MX else 16)), cols, fmt).cuda()
+        for offset in range(16):
+            for ld in (cols, cols + 1, cols + 6, wide):
+                store = torch.full((offset + rows * ld + 16,), -77.0, device="cuda", dtype=dtype)
+                view = store[offset:].as_strided((rows, cols), (ld, 1))
+                view.copy_(aligned)
+                got = ff.fp4_quantize(view, fmt)
+                assert torch.equal(got.codes, want.codes) and torch.equal(got.scales[pos], want.scales[pos])
+                if fmt == eq.FP4_NV:
+                    assert torch.equal(got.row_scales, want.row_scales)
+                store.fill_(-77.0)
+                eq.fp4_dequantize(got.codes, got.scales, got.row_scales, rows, cols, fmt, view, code, ld, stream)
+                assert torch.equal(view, out[:, :cols])
+                view.fill_(-77.0)
+                assert bool((store == -77.0).all())
+    ff.check()
+
+
+@gpu
 def test_offsets_beyond_32_bits():
     """rows 2^26 elements apart: the last ones lie more than 4 GB (and 2^32 elements) after the first"""
     rows, ld = 70, 1 << 26
