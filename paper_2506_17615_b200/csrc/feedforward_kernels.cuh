@@ -1159,10 +1159,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     // says that it has started before it asks, and gives the memory back before it waits for the sums.  (With
     // `reuse` it says so only when its products are done; the launch then takes all of an SM's shared memory,
     // and no other CTA with tensor memory shares the SM.)
+    // What the others may write once they have seen this arrival is ready before it: row_max is zero (its
+    // threads' own arrivals release the zeros).
+    if (FUSED && threadIdx.x < kFusedTokens) row_max[threadIdx.x] = 0;
+    __syncwarp();
     if (!p.reuse) cluster_arrive();
 
     // the loading warp prepares the barriers and starts; everybody else meets it below
-    if (FUSED && threadIdx.x < kFusedTokens) row_max[threadIdx.x] = 0;
     if (warp == 4) {
         if (lane == 0) {
             prefetch_map(&p.w[0]);

@@ -303,6 +303,34 @@ def test_fp4_gated(fmt, act, m, f, k):
     ff.check()
 
 
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("parts", range(1, 9))
+def test_few_tokens_on_every_cluster_size(fmt, parts):
+    """A product of one tile of features over `parts` stages of 256 columns runs on a cluster of `parts` CTAs, each
+    with one stage of x.  The row's largest element lies in each CTA's part in turn: every CTA has to know it."""
+    dtype, f = torch.bfloat16, 100
+    for k in (256 * parts, 256 * parts - 77):
+        wg, wu = normal(f, k, k + 1, dtype, 2 * k ** -0.5), normal(f, k, k + 2, dtype, k ** -0.5)
+        qg, qu = ff.fp4_quantize(wg, fmt), ff.fp4_quantize(wu, fmt)
+        vg, vu = ref.values(wg.double(), fmt), ref.values(wu.double(), fmt)
+        for m in (1, 2):
+            for part in range(parts):
+                x = normal(m, k, part, dtype)
+                # the tokens' peaks in this part and, for the second token, in the one before
+                for row in range(m):
+                    x[row, (part - row) % parts * 256 + 3 + 170 * (part & 1)] = 60.0 + row
+                vx = ref.values(x.double(), fmt)
+                value, bound = ref.product(vx, vg)
+                want, limit, _, _ = ref.gated(vx, vg, vu, eq.ACT_SILU)
+                first, gated = ff.fp4_linear(x, qg), ff.fp4_gated(x, qg, qu, eq.ACT_SILU)
+                ref.assert_within(first, value, ref.rounded(value, bound, dtype), "linear")
+                ref.assert_within(gated, want, ref.rounded(want, limit, dtype), "gated")
+                for _ in range(5):
+                    assert torch.equal(ff.fp4_linear(x, qg), first) and torch.equal(ff.fp4_gated(x, qg, qu, eq.ACT_SILU), gated)
+    ff.check()
+
+
 # ------------------------------------------------------------------ 16-bit block and its gradients
 
 def backward_reference(dh, x, wg, wu, g, u, act, unit):
