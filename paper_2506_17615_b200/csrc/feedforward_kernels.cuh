@@ -428,9 +428,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                         // 4 bits: the tile before has given up the columns that both accumulators use; 16 bits: the
                         // tile before that has given up this accumulator
                         if (FP4) {
-                            if (local && !(ok = barrier_wait_warp(drained, (local - 1) & 1, &abort))) break;
+                            if (local && !(ok = barrier_wait_warp<true>(drained, (local - 1) & 1, &abort))) break;
                         } else {
-                            if (local > 1 && !(ok = barrier_wait_warp(drained + 8 * buf, (local / 2 - 1) & 1, &abort))) break;
+                            if (local > 1 && !(ok = barrier_wait_warp<true>(drained + 8 * buf, (local / 2 - 1) & 1, &abort))) break;
                         }
                         fence_after();
                     }
@@ -518,7 +518,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                 if (i == (FP4 ? 0 : steps - 1)) {
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) barrier_arrive_cluster(done);
+                    if (lane == 0) barrier_arrive_pair(done);
                 }
                 if (!live) continue;
                 if constexpr (KIND == kNv) {

@@ -27,6 +27,16 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
         : "memory");
     return done != 0;
 }
+// the same for arrivals of barrier_arrive_pair; fence_after orders what follows
+__device__ __forceinline__ bool barrier_try_pair(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
 
 // Every wait of these kernels is on this CTA's own copies and products, so it ends by itself; the
 // limit is there so that a mistake becomes a status instead of a kernel that never returns.  2^24
@@ -37,10 +47,12 @@ constexpr uint32_t kWaitLimit = 1u << 24;
 __device__ uint32_t g_gave_up = 0;
 
 // false: this wait, or another one of this CTA, gave up (then `abort` is set and every role leaves)
+template <bool PAIR = false>
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort) {
-    if (barrier_try(bar, parity)) return true;
+    auto done = [&] { return PAIR ? barrier_try_pair(bar, parity) : barrier_try(bar, parity); };
+    if (done()) return true;
     for (uint32_t i = 0; i < kWaitLimit; ++i) {
-        if (barrier_try(bar, parity)) return true;
+        if (done()) return true;
         if (*abort) return false;
     }
     *abort = 1;
@@ -89,10 +101,11 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
     return a;
 }
-// Says that this thread's tensor-memory loads are done (ordered by fence_before); no other memory is passed on,
-// so nothing is released at cluster scope, which would hold the arrival back by about 1000 cycles.
-__device__ __forceinline__ void barrier_arrive_cluster(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+// Says, to a barrier of either CTA of a pair, that this thread's tensor-memory loads are done (fence_before orders
+// them before it).  At cluster scope, since the waiter may be in the other CTA, and relaxed: no other memory is passed
+// on, and a release at this scope would hold the arrival back by about 1000 cycles.
+__device__ __forceinline__ void barrier_arrive_pair(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void st_cluster_f32(uint32_t cluster_addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
@@ -133,8 +146,9 @@ template <typename T>
 __device__ __forceinline__ T uniform(T v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
 
 // false in every lane as soon as one lane's wait gave up
+template <bool PAIR = false>
 __device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort) {
-    return __all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, abort));
+    return __all_sync(0xFFFFFFFFu, barrier_wait<PAIR>(bar, parity, abort));
 }
 __device__ __forceinline__ void barrier_expect_warp(uint32_t bar, uint32_t bytes) {
     asm volatile(EQUARX_ELECT "mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar), "r"(bytes) : "memory");

@@ -303,6 +303,44 @@ def test_fp4_gated(fmt, act, m, f, k):
     ff.check()
 
 
+# (tokens, outputs, columns) of products with more tiles than the 74 pairs of SMs, so that a pair hands accumulators over from
+# one tile to the next.  In order: 187 tiles of 256 outputs, the last ones of 40 outputs (one group of 128 scales) and
+# of 4 tokens (the pair's second CTA has none); 264 tiles, outputs that TMA cannot write; 79 tiles of 128 outputs.
+MANY = [(4100, 2600, 700), (6000, 2587, 300), (20000, 100, 500)]
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m,n,k", MANY)
+def test_fp4_products_of_many_tiles(fmt, m, n, k):
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        source = torch.bfloat16 if dtype == torch.float32 else dtype
+        x, w = normal(m, k, 1, source), normal(n, k, 2, source, k ** -0.5)
+        xq, wq = ff.fp4_quantize(x, fmt), ff.fp4_quantize(w, fmt)
+        y = ff.fp4_matmul(xq, wq, dtype)
+        value, bound = ref.product(ref.values(x.double(), fmt), ref.values(w.double(), fmt))
+        ref.assert_within(y, value, ref.rounded(value, bound, dtype), "matmul")
+        # the same bits as products of few tokens, in which no pair has a second tile
+        for first in range(0, m, 1000):
+            assert torch.equal(ff.fp4_matmul(ff.fp4_quantize(x[first:first + 1000], fmt), wq, dtype), y[first:first + 1000])
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m,f,k", [(4100, 1300, 700), (6000, 1293, 300), (20000, 70, 500)])
+def test_fp4_gated_of_many_tiles(fmt, m, f, k):
+    dtype = torch.bfloat16
+    x, wg, wu = normal(m, k, 1, dtype), normal(f, k, 2, dtype, 2 * k ** -0.5), normal(f, k, 3, dtype, k ** -0.5)
+    qg, qu = ff.fp4_quantize(wg, fmt), ff.fp4_quantize(wu, fmt)
+    h = ff.fp4_gated(x, qg, qu)
+    value, bound, _, _ = ref.gated(*(ref.values(t.double(), fmt) for t in (x, wg, wu)), eq.ACT_GELU_TANH)
+    ref.assert_within(h, value, ref.rounded(value, bound, dtype), "h")
+    for first in range(0, m, 1000):
+        assert torch.equal(ff.fp4_gated(x[first:first + 1000], qg, qu), h[first:first + 1000])
+    ff.check()
+
+
 @gpu
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("parts", range(1, 9))
@@ -378,6 +416,31 @@ def test_gated_forward_and_backward(dtype, act, m, f, k):
         ref.assert_within(got, v, ref.rounded(v, e, dtype), name)
     again = ff.gated_backward(dh, x, wg, wu, g, u, act)
     assert all(torch.equal(p, q) for p, q in zip(grads, again)), "not deterministic"
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m,f,k", [(4100, 1300, 1400), (2500, 1501, 1300), (20000, 30, 200)])
+def test_gated_forward_and_backward_of_many_tiles(dtype, m, f, k):
+    """More tiles than the 74 pairs of SMs: forward 187, 120 and 79; backward 202 and 142 of dx and the weights'
+    gradients in one launch, and 79 of dx beside weights' gradients that are split over the tokens."""
+    act = eq.ACT_GELU_TANH
+    x, wg, wu = normal(m, k, 1, dtype), normal(f, k, 2, dtype, 2 * k ** -0.5), normal(f, k, 3, dtype, k ** -0.5)
+    dh = normal(m, f, 4, dtype)
+    h, g, u = ff.gated_forward(x, wg, wu, act, save=True)
+    xd, wgd, wud, dhd = (t.double() for t in (x, wg, wu, dh))
+    value, bound, (gv, eg), (uv, eu) = ref.gated(xd, wgd, wud, act)
+    ref.assert_within(h, value, ref.rounded(value, bound, dtype), "h")
+    ref.assert_within(g, gv, ref.rounded(gv, eg, dtype), "g")
+    ref.assert_within(u, uv, ref.rounded(uv, eu, dtype), "u")
+    for first in range(0, m, 1000):
+        assert torch.equal(ff.gated_forward(x[first:first + 1000], wg, wu, act), h[first:first + 1000])
+    grads = ff.gated_backward(dh, x, wg, wu, g, u, act)
+    for name, got, (v, e) in zip(("dx", "dwg", "dwu"), grads,
+                                 backward_reference(dhd, xd, wgd, wud, g.double(), u.double(), act, ref.UNIT[dtype])):
+        ref.assert_within(got, v, ref.rounded(v, e, dtype), name)
+    assert all(torch.equal(p, q) for p, q in zip(grads, ff.gated_backward(dh, x, wg, wu, g, u, act)))
     ff.check()
 
 
