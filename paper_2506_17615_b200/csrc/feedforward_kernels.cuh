@@ -368,7 +368,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                 if (!ok) break;
             }
         }
-        if (abort && rank == 0)         // what has been started lands before the shared memory goes away
+        if (gave_up_warp(&abort) && rank == 0)         // what has been started lands before the shared memory goes away
             for (uint32_t i = issued > PIPE ? issued - PIPE : 0; i < issued; ++i)
                 barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
         __syncwarp();
@@ -456,7 +456,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                 }
                 if (ok) mma_commit<2>(ready + 8 * buf);
             }
-            if (abort) {        // products in flight read this shared memory
+            if (gave_up_warp(&abort)) {        // products in flight read this shared memory
                 mma_commit<2>(drain);
                 barrier_drain(drain, 0);
             }
@@ -500,8 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                     factor[i] = col >= n0 && col < g.n ? p.row_b[i % SETS][col] : 0.0f;
                 }
             }
-            if (!barrier_wait(ready + 8 * buf, local / 2 & 1, &abort)) break;
-            __syncwarp();
+            if (!barrier_wait_warp(ready + 8 * buf, local / 2 & 1, &abort)) break;
             fence_after();
 #pragma unroll
             for (int i = 0; i < 4 / (FP4 ? SETS : 1); ++i) {
@@ -1279,7 +1278,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             if (!(ok = barrier_wait_warp(empty + 8 * slot, (it / p.pipe & 1) ^ 1, &abort))) break;
             load_stage(it);
         }
-        if (abort)
+        if (gave_up_warp(&abort))
             for (int i = it > p.pipe ? it - p.pipe : 0; i < it; ++i) barrier_drain(full + 8 * (i % p.pipe), i / p.pipe & 1);
         __syncwarp();
     } else if (warp == 5) {
@@ -1318,7 +1317,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             mma_commit<1>(empty + 8 * slot);
         }
         if (ok) mma_commit<1>(ready);
-        if (abort) {
+        if (gave_up_warp(&abort)) {
             mma_commit<1>(drain);
             barrier_drain(drain, 0);
         }
@@ -1334,7 +1333,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             if (!MX && in) row_factors(row_max[row], up, factor);
             block_scale<MX>(m, up, factor, byte, inv);
             const uint2 code = encode_values(v, inv);
-            if (in && at >= p.pipe) ok = ok && barrier_wait(empty + 8 * slot, (at / p.pipe & 1) ^ 1, &abort);
+            // the halves of the warp may wait for different stages, and go on together
+            bool vacant = ok;
+            if (ok && in && at >= p.pipe) vacant = barrier_wait(empty + 8 * slot, (at / p.pipe & 1) ^ 1, &abort);
+            ok = __all_sync(0xFFFFFFFFu, vacant);
             if (in && ok) {
                 uint8_t* const sx = smem_ptr + slot * STAGE + NW * kTileBytes;
                 uint8_t* const ss = sx + xb + SB * NW;
@@ -1354,8 +1356,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     bool good = true;
     if (warp < 4) {
-        good = barrier_wait(ready, 0, &abort);
-        __syncwarp();
+        good = barrier_wait_warp(ready, 0, &abort);
         fence_after();
     }
     if (p.reuse) cluster_arrive();                      // this CTA's loads and products are done

@@ -145,11 +145,14 @@ __device__ __forceinline__ void grid_end(int order) {
 template <typename T>
 __device__ __forceinline__ T uniform(T v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
 
-// false in every lane as soon as one lane's wait gave up
+// Every wait of a kernel is a whole warp's, which goes on or leaves together: false in every lane as soon as one
+// lane's wait gave up
 template <bool PAIR = false>
 __device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort) {
     return __all_sync(0xFFFFFFFFu, barrier_wait<PAIR>(bar, parity, abort));
 }
+// whether a wait of this CTA has given up; one answer for the warp, which may have to issue instructions together
+__device__ __forceinline__ bool gave_up_warp(volatile uint32_t* abort) { return __any_sync(0xFFFFFFFFu, *abort != 0); }
 __device__ __forceinline__ void barrier_expect_warp(uint32_t bar, uint32_t bytes) {
     asm volatile(EQUARX_ELECT "mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar), "r"(bytes) : "memory");
 }
