@@ -542,10 +542,13 @@ int equarx_gated_backward(const void *dh, size_t lddh, const void *x, size_t ldx
                           void *workspace, size_t workspace_bytes, equarx_stream_t stream);
 
 /*
- * The kernels of the feed-forward calls wait only for their own copies and products,
- * and each wait has a limit: a kernel whose wait ran out leaves and its output is
+ * The kernels of the feed-forward calls wait only for copies and products of their own
+ * blocks, and each wait has a limit of about a second (more for a reduction of very
+ * many columns or tokens): a kernel whose wait ran out leaves and its output is
  * incomplete.  This call synchronises the current device and returns
  * EQUARX_ERR_TIMEOUT if that has happened on it since the last check, else EQUARX_OK.
+ * For tests, EQUARX_INJECT_TIMEOUT=<polls> in the environment makes it run a kernel
+ * first whose wait runs out after so many polls.
  */
 int equarx_feedforward_check(void);
 

@@ -500,7 +500,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                     factor[i] = col >= n0 && col < g.n ? p.row_b[i % SETS][col] : 0.0f;
                 }
             }
-            if (!barrier_wait_warp(ready + 8 * buf, local / 2 & 1, &abort)) break;
+            const uint32_t limit = wait_limit(g.stages * (MODE == kGrads ? g.parts : 1));
+            if (!barrier_wait_warp(ready + 8 * buf, local / 2 & 1, &abort, limit)) break;
             fence_after();
 #pragma unroll
             for (int i = 0; i < 4 / (FP4 ? SETS : 1); ++i) {
@@ -1335,7 +1336,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             const uint2 code = encode_values(v, inv);
             // the halves of the warp may wait for different stages, and go on together
             bool vacant = ok;
-            if (ok && in && at >= p.pipe) vacant = barrier_wait(empty + 8 * slot, (at / p.pipe & 1) ^ 1, &abort);
+            if (ok && in && at >= p.pipe) vacant = barrier_wait(empty + 8 * slot, (at / p.pipe & 1) ^ 1, &abort, kWaitLimit);
             ok = __all_sync(0xFFFFFFFFu, vacant);
             if (in && ok) {
                 uint8_t* const sx = smem_ptr + slot * STAGE + NW * kTileBytes;
@@ -1356,7 +1357,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     bool good = true;
     if (warp < 4) {
-        good = barrier_wait_warp(ready, 0, &abort);
+        good = barrier_wait_warp(ready, 0, &abort, wait_limit(s1 - s0));
         fence_after();
     }
     if (p.reuse) cluster_arrive();                      // this CTA's loads and products are done
@@ -1429,6 +1430,21 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         }
     }
     grid_end(p.order);
+}
+
+// ---------------------------------------------------------------- a wait that runs out
+// For tests of what the host is told: one warp waits `polls` times on a barrier on which nobody arrives, and a second
+// one, with the full limit, leaves because the first has given up.
+__global__ void __launch_bounds__(64) give_up_kernel(uint32_t polls) {
+    __shared__ uint64_t bar;
+    __shared__ volatile uint32_t abort;
+    const uint32_t never = smem_addr(&bar);
+    if (threadIdx.x == 0) {
+        barrier_init(never, 1);
+        abort = 0;
+    }
+    __syncthreads();
+    barrier_wait_warp(never, 0, &abort, threadIdx.x < 32 ? polls : kWaitLimit);
 }
 
 }  // namespace ff

@@ -38,20 +38,24 @@ __device__ __forceinline__ bool barrier_try_pair(uint32_t bar, uint32_t parity) 
     return done != 0;
 }
 
-// Every wait of these kernels is on this CTA's own copies and products, so it ends by itself; the
-// limit is there so that a mistake becomes a status instead of a kernel that never returns.  2^24
-// polls are a fifth of a second at the very least, far above the longest kernel here.
-constexpr uint32_t kWaitLimit = 1u << 24;
+// The waits are on copies and products of this CTA and, in the tile kernel, of the other CTA of the pair, so they end by
+// themselves; the limit is there so that a mistake becomes a status instead of a kernel that never returns.  A poll of
+// a barrier on which nothing happens lasts 4.0 us (measured), 2^18 of them 1.05 s, where a stage of the
+// reduction takes about 1 us.  A wait that spans many stages asks for more.  A CTA that gives up takes all its warps
+// out; the other one of its pair, which waits in vain then, comes to its own limit.
+constexpr uint32_t kWaitLimit = 1u << 18;
+// for a wait on all products of a tile: 16 us more for each stage
+__device__ __forceinline__ uint32_t wait_limit(int stages) { return kWaitLimit + 4 * uint32_t(stages); }
 
 // counts the waits that gave up on this device since the library was loaded
 __device__ uint32_t g_gave_up = 0;
 
 // false: this wait, or another one of this CTA, gave up (then `abort` is set and every role leaves)
 template <bool PAIR = false>
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort) {
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort, uint32_t limit) {
     auto done = [&] { return PAIR ? barrier_try_pair(bar, parity) : barrier_try(bar, parity); };
     if (done()) return true;
-    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+    for (uint32_t i = 0; i < limit; ++i) {
         if (done()) return true;
         if (*abort) return false;
     }
@@ -148,8 +152,9 @@ __device__ __forceinline__ T uniform(T v) { return __shfl_sync(0xFFFFFFFFu, v, 0
 // Every wait of a kernel is a whole warp's, which goes on or leaves together: false in every lane as soon as one
 // lane's wait gave up
 template <bool PAIR = false>
-__device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort) {
-    return __all_sync(0xFFFFFFFFu, barrier_wait<PAIR>(bar, parity, abort));
+__device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort,
+                                                  uint32_t limit = kWaitLimit) {
+    return __all_sync(0xFFFFFFFFu, barrier_wait<PAIR>(bar, parity, abort, limit));
 }
 // whether a wait of this CTA has given up; one answer for the warp, which may have to issue instructions together
 __device__ __forceinline__ bool gave_up_warp(volatile uint32_t* abort) { return __any_sync(0xFFFFFFFFu, *abort != 0); }

@@ -776,6 +776,21 @@ def test_launch_errors_come_back(monkeypatch):
 
 
 @gpu
+def test_a_wait_that_runs_out_is_reported_once(monkeypatch):
+    """a warp whose wait runs out and one that leaves with it; the context stays usable"""
+    x, w = normal(4, 64, 1, torch.bfloat16), normal(8, 64, 2, torch.bfloat16)
+    want = ff.gated_forward(x, w, w)
+    ff.check()
+    monkeypatch.setenv("EQUARX_INJECT_TIMEOUT", "50")             # 0.2 ms
+    with pytest.raises(eq.EquarxError) as err:
+        ff.check()
+    assert err.value.status == binding.ERR_TIMEOUT
+    monkeypatch.delenv("EQUARX_INJECT_TIMEOUT")
+    ff.check()
+    assert torch.equal(ff.gated_forward(x, w, w), want)
+
+
+@gpu
 def test_shapes_that_do_not_fit():
     x, w = normal(4, 64, 1, torch.bfloat16), normal(8, 64, 2, torch.bfloat16)
     for bad in ((x, w, w[:, :63]), (x, w, w[:7]), (x.T, w, w), (x, w, w.to(torch.float16)), (x[0], w, w)):
