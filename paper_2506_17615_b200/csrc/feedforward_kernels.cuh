@@ -1111,6 +1111,17 @@ __host__ __device__ constexpr int split_part_bytes(int nt, int ranks) {
     return ranks * (MODE == kGated ? 2 : 1) * ((nt + ranks - 1) / ranks) * 128 * 4;
 }
 
+// A tile kernel's CTA takes all tensor memory before it waits for the launch before.  If that launch had a CTA on the same SM
+// that still had to ask for its own, neither would end: the two must never share an SM.  Shared memory sees to it, also
+// for the smallest CTA of the split kernel (one stage, 16 tokens).
+constexpr int kSmemOfSm = 228 * 1024, kSmemOfCta = 1024;      // of an SM; what every CTA costs beside its own
+constexpr int kLeastSplitSmem = split_stage_bytes<kHalf, kPlain>(16) + split_part_bytes<kPlain>(16, 1) + kSmemSlack;
+static_assert(split_stage_bytes<kMx, kPlain>(16) >= split_stage_bytes<kHalf, kPlain>(16) &&
+              split_part_bytes<kPlain>(16, 8) >= split_part_bytes<kPlain>(16, 1));
+static_assert(kTileSmem<kHalf> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
+              kTileSmem<kMx> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
+              kTileSmem<kNv> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm);
+
 // The output transposed: 128 features x nt tokens, so that a single token costs one narrow product over
 // each weight tile instead of a 256-row one, and the weights, which are all the bytes there are, are
 // read once.  The reduction axis is split over the CTAs of a cluster (cluster dimension x) because
