@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -91,6 +92,18 @@ Matrix matrix(const at::Tensor& t, const char* what, size_t rows, size_t cols, c
                       what, " is ", t.sizes(), " ", t.scalar_type(), " on ", t.device(), ", expected [", rows, ", ", cols, "] ",
                       like.scalar_type(), " on ", like.device());
     return m;
+}
+
+// The library knows nothing of autograd, so an output would come back cut off from what made it.
+bool wants_gradient(const at::Tensor& t, const char* what) {
+    const auto& state = c10::AutogradState::get_tls_state();
+    TORCH_CHECK_VALUE(!state.get_fw_grad_mode() || !t._fw_grad(0).defined(), what, " has a forward-mode tangent, which the ",
+                      "feed-forward calls do not carry on");
+    return state.get_grad_mode() && t.requires_grad();
+}
+void no_gradient(const at::Tensor& t, const char* what) {
+    TORCH_CHECK_VALUE(!wants_gradient(t, what), what, " requires a gradient, which 4-bit products do not have: call under ",
+                      "torch.no_grad(), or with ", what, ".detach()");
 }
 
 at::Tensor empty(int64_t rows, int64_t cols, at::ScalarType type, const at::Device& device) {
@@ -209,6 +222,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const size_t rows = integer(a[2]), k = integer(a[3]);
     const int format = enumeration(a[4]), dtype = dtype_code(x.t.scalar_type(), "x");
     TORCH_CHECK_VALUE(x.cols == k, "x has ", x.cols, " columns, the weight ", k);
+    no_gradient(x.t, "x");
     const at::Device device = x.t.device();
     const Fp4 w = parts(dw, rows, k, format, device);
     const at::Tensor out = empty(x.rows, rows, x.t.scalar_type(), device);
@@ -230,6 +244,7 @@ PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const size_t rows = integer(a[3]), k = integer(a[4]);
     const int format = enumeration(a[5]), act = enumeration(a[6]), dtype = dtype_code(x.t.scalar_type(), "x");
     TORCH_CHECK_VALUE(x.cols == k, "x has ", x.cols, " columns, the weights ", k);
+    no_gradient(x.t, "x");
     const at::Device device = x.t.device();
     const Fp4 g = parts(dg, rows, k, format, device), u = parts(du, rows, k, format, device);
     const at::Tensor h = empty(x.rows, rows, x.t.scalar_type(), device);
@@ -242,7 +257,7 @@ PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// gated_forward(x, wg, wu, act, save)
+// gated_forward(x, wg, wu, act, save); None, and nothing is done, where autograd wants gradients
 PyObject* gated_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     arguments(n, 5);
@@ -252,6 +267,8 @@ PyObject* gated_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Matrix wg = matrix(tg, "wg", f, x.cols, x.t), wu = matrix(tensor(a[2], "wu"), "wu", f, x.cols, x.t);
     const int act = enumeration(a[3]), save = PyObject_IsTrue(a[4]), dtype = dtype_code(x.t.scalar_type(), "x");
     if (save < 0) throw python_error();
+    const bool grad[] = {wants_gradient(x.t, "x"), wants_gradient(wg.t, "wg"), wants_gradient(wu.t, "wu")};
+    if (grad[0] || grad[1] || grad[2]) Py_RETURN_NONE;
     const at::Device device = x.t.device();
     const at::Tensor h = empty(x.rows, f, x.t.scalar_type(), device);
     at::Tensor g, u;

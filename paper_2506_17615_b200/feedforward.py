@@ -12,6 +12,10 @@ layouts).  A failed call raises EquarxError, tensors that do not fit together ra
 CPU path.
 
 Matrices are [rows, columns] with unit column stride; the row stride is free.
+
+gated_forward takes part in autograd: called with tensors that require gradients, its h is connected to them by
+gated_backward.  The 4-bit products have no gradients and refuse such an x (outside torch.no_grad()); a
+quantized matrix is bytes, through which no gradient passes.  gated_backward's results have no gradients themselves.
 """
 import ctypes
 import importlib
@@ -107,12 +111,36 @@ def fp4_gated(x, wg, wu, act=ACT_GELU_TANH):
 def gated_forward(x, wg, wu, act=ACT_GELU_TANH, save=False):
     """h = act(x wg^T) * (x wu^T) for x [tokens, k], wg and wu [f, k], all bfloat16 or all float16.
     With save: (h, g, u), where g and u are the two projections that gated_backward needs."""
-    return _or_raise(_native.gated_forward(x, wg, wu, act, save), "equarx_gated_forward")
+    result = _native.gated_forward(x, wg, wu, act, save)
+    if result is None:                                  # gradients are wanted
+        return _Gated.apply(x, wg, wu, act, save)
+    return _or_raise(result, "equarx_gated_forward")
 
 
 def gated_backward(dh, x, wg, wu, g, u, act=ACT_GELU_TANH):
     """(dx, dwg, dwu) of gated_forward from dh [tokens, f] and the g and u it saved."""
     return _or_raise(_native.gated_backward(dh, x, wg, wu, g, u, act), "equarx_gated_backward")
+
+
+class _Gated(torch.autograd.Function):
+    """gated_forward and gated_backward as a pair of autograd's"""
+
+    @staticmethod
+    def forward(ctx, x, wg, wu, act, save):
+        h, g, u = gated_forward(x, wg, wu, act, save=True)
+        ctx.save_for_backward(x, wg, wu, g, u)
+        ctx.act = act
+        if not save:
+            return h
+        ctx.mark_non_differentiable(g, u)
+        return h, g, u
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh, *_):
+        if dh.stride(1) != 1 or dh.stride(0) < dh.shape[1]:     # a sum's gradient is one element, expanded
+            dh = dh.contiguous()
+        return *gated_backward(dh, *ctx.saved_tensors, ctx.act), None, None
 
 
 def check():

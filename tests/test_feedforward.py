@@ -480,6 +480,73 @@ def test_gradients_against_differences(act, m, f, k):
         assert abs(float((got.double() * direction).sum() - numeric)) <= float(tol), i
 
 
+def leaves(*tensors):
+    return [t.detach().clone().requires_grad_() for t in tensors]
+
+
+@gpu
+@pytest.mark.parametrize("save", [False, True])
+@pytest.mark.parametrize("m", [5, 300])
+def test_autograd_connects_forward_and_backward(m, save):
+    dtype = torch.bfloat16
+    x, wg, wu, dh = normal(m, 72, 1, dtype), normal(40, 72, 2, dtype, 0.1), normal(40, 72, 3, dtype, 0.1), normal(m, 40, 4, dtype)
+    h, g, u = ff.gated_forward(x, wg, wu, eq.ACT_SILU, save=True)
+
+    def run(args):
+        out = ff.gated_forward(*args, eq.ACT_SILU, save)
+        if save:
+            assert torch.equal(out[1], g) and torch.equal(out[2], u) and not out[1].requires_grad and not out[2].requires_grad
+            out = out[0]
+        assert torch.equal(out, h) and out.requires_grad
+        return out
+
+    args = leaves(x, wg, wu)
+    run(args).backward(dh)
+    for t, want in zip(args, ff.gated_backward(dh, x, wg, wu, g, u, eq.ACT_SILU)):
+        assert torch.equal(t.grad, want)
+    # a gradient that is one element expanded, and one whose columns are not neighbours
+    for grad in (torch.ones(1, 1, dtype=dtype, device="cuda").expand(m, 40), dh.T.contiguous().T):
+        args = leaves(x, wg, wu)
+        run(args).backward(grad)
+        for t, want in zip(args, ff.gated_backward(grad.contiguous(), x, wg, wu, g, u, eq.ACT_SILU)):
+            assert torch.equal(t.grad, want)
+    # only one of the three asks, in the middle of a graph
+    for i in range(3):
+        args = [x, wg, wu]
+        args[i] = leaf = args[i].clone().requires_grad_()
+        inner = list(args)
+        inner[i] = leaf * 1
+        (run(inner) * 2).backward(dh)
+        assert torch.equal(leaf.grad, ff.gated_backward(dh * 2, x, wg, wu, g, u, eq.ACT_SILU)[i])
+    with torch.no_grad():
+        out = ff.gated_forward(*args, eq.ACT_SILU)
+        assert torch.equal(out, h) and not out.requires_grad
+
+
+@gpu
+def test_gradients_that_do_not_exist_are_refused():
+    dtype = torch.bfloat16
+    x, w = normal(4, 64, 1, dtype), normal(8, 64, 2, dtype)
+    q = ff.fp4_quantize(w.clone().requires_grad_())                # bytes: nothing to connect
+    asking = x.clone().requires_grad_()
+    for call in (lambda: ff.fp4_linear(asking, q), lambda: ff.fp4_gated(asking, q, q)):
+        with pytest.raises(ValueError, match="no_grad"):
+            call()
+        with torch.no_grad():
+            call()
+    assert torch.equal(ff.fp4_linear(asking.detach(), q), ff.fp4_linear(x, q))
+    leaf = x.clone().requires_grad_()
+    grad, = torch.autograd.grad(ff.gated_forward(leaf, w, w).float().square().sum(), leaf, create_graph=True)
+    with pytest.raises(RuntimeError):                              # no second derivatives
+        grad.float().sum().backward()
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(x, x)
+        for call in (lambda: ff.gated_forward(dual, w, w), lambda: ff.gated_forward(x, w, torch.autograd.forward_ad.make_dual(w, w)),
+                     lambda: ff.fp4_linear(dual, q)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+
+
 # ------------------------------------------------------------------ no tokens, streams, not finite, guards
 
 @gpu
