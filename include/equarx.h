@@ -431,7 +431,9 @@ int equarx_ring_allreduce(const void *const *in_bf16, void *const *out_bf16,
  *     EQUARX_FP32.  Products are summed in fp32 and rounded once to the output type.
  *   - Infinities and NaN follow the arithmetic; nothing traps.  An element that is
  *     not finite quantizes to a NaN scale of its block (MX) or row (NV).
- *   - Outputs must not overlap inputs, the workspace or one another.
+ *   - Outputs must not overlap inputs, the workspace or one another.  Matrices with the
+ *     same row stride may lie side by side in the rows of one buffer (g and u, or h beside
+ *     x); with different strides they must be apart from first to last element.
  *   - Workspaces and 4-bit buffers are 16-byte aligned.
  *   - The result does not depend on timing: sums are taken in a fixed order.
  */

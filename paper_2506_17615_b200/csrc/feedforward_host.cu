@@ -23,15 +23,24 @@ inline size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
 // ---------------------------------------------------------------- checks
 struct Span {
     const void* p;
-    size_t bytes;
+    size_t bytes;           // from the first to the last
+    size_t width, stride;   // of a row, in bytes; a buffer is one row
+    Span(const void* p, size_t bytes) : Span(p, bytes, bytes, 0) {}
+    Span(const void* p, size_t bytes, size_t width, size_t stride) : p(p), bytes(bytes), width(width), stride(stride) {}
 };
-// bytes of a rows x cols matrix from its first to its last element
 inline Span matrix(const void* p, size_t rows, size_t cols, size_t ld, size_t size) {
-    return Span{p, rows ? ((rows - 1) * ld + cols) * size : 0};
+    return rows > 1 ? Span(p, ((rows - 1) * ld + cols) * size, cols * size, ld * size) : Span(p, rows * cols * size);
 }
+// Matrices of one row stride may share its rows, each with columns of its own (the two halves of a wider buffer):
+// one's rows then begin after the other's, counted from there, and end before the other's next ones.  Matrices of
+// different strides are kept apart as a whole.
 inline bool overlap(const Span& a, const Span& b) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-    return a.bytes && b.bytes && a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+    if (!(a.bytes && b.bytes && a.p && b.p && x < y + b.bytes && y < x + a.bytes)) return false;
+    const size_t stride = std::max(a.stride, b.stride);
+    if (!stride || (a.stride && b.stride && a.stride != b.stride)) return true;
+    const size_t after = y >= x ? (y - x) % stride : (stride - (x - y) % stride) % stride;
+    return after < a.width || after + b.width > stride;
 }
 // no output may meet an input or another output
 int check_overlap(std::initializer_list<Span> in, std::initializer_list<Span> out) {

@@ -129,6 +129,30 @@ def test_gated_forward_and_backward_refuse_bad_arguments():
     assert eq.last_cuda_error() == 0
 
 
+def test_matrices_side_by_side_are_no_overlap(monkeypatch):
+    """columns of one buffer are accepted, shared elements are not; no launch reaches a GPU"""
+    monkeypatch.setenv("EQUARX_INJECT_LAUNCH_ERROR", "719")
+
+    def forward(g, u, ldgu, h=A + 3 * GB, ldh=8, m=4):
+        return status_of(eq.gated_forward, x=A, ldx=64, wg=A + GB, ldwg=64, wu=A + 2 * GB, ldwu=64, dtype=eq.FP16, m=m, f=8, k=64,
+                         act=1, h=h, ldh=ldh, g=g, u=u, ldgu=ldgu, workspace=0, workspace_bytes=0)
+
+    far = A + 5 * GB
+    for g, u in ((far, far + 16), (far + 16, far), (far, far + 48), (far + 64, far + 16), (far, far + 64 * 5 + 16)):
+        assert forward(g, u, 32) == binding.ERR_CUDA, (g - far, u - far)        # rows of 64 bytes, 16 of them used
+    for g, u in ((far, far + 14), (far + 14, far), (far, far + 50), (far + 64, far + 14), (far, far), (far, far + 128)):
+        assert forward(g, u, 32) == binding.ERR_ALIAS, (g - far, u - far)
+    assert forward(far, far + 16, 16) == binding.ERR_CUDA                       # the halves fill the buffer
+    assert forward(far, far + 16, 8) == binding.ERR_ALIAS
+    # h in the rows of g and u, with their stride or another; a single row lies between rows or not
+    assert forward(far, far + 16, 32, far + 32, 32) == binding.ERR_CUDA
+    assert forward(far, far + 16, 32, far + 40, 24) == binding.ERR_ALIAS
+    assert forward(far, far + 16, 32, far + 16, 32) == binding.ERR_ALIAS
+    one = dict(dtype=eq.BF16, rows=1, cols=8, ld=8, format=eq.FP4_MX, codes=far + 2 * GB, scales=A + GB, row_scales=0)
+    assert status_of(eq.fp4_quantize, x=far + 2 * GB + 16, **one) == binding.ERR_CUDA
+    assert status_of(eq.fp4_quantize, x=far + 2 * GB + 14, **one) == binding.ERR_ALIAS
+
+
 def test_sizes_of_the_buffers():
     assert eq.fp4_codes_bytes(3, 33) == 3 * 32                    # two groups of 32 codes
     assert eq.fp4_scales_bytes(1, 1, eq.FP4_MX) == 1024           # one stage of 256 columns, 128 rows, 8 scales each
@@ -631,6 +655,31 @@ def test_strided_outputs_and_no_writes_outside(m, f, k):
                           inner(px), k + extra, inner(pwg), k + extra, inner(pwu), k + extra, ws, nb, stream)
         for t, want, rows in ((px, grads0[0], m), (pwg, grads0[1], f), (pwu, grads0[2], f)):
             assert torch.equal(split(t, rows, k), want)
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("m,f,k", [(3, 40, 72), (200, 130, 64), (300, 264, 136)])
+def test_outputs_side_by_side_in_one_buffer(m, f, k):
+    """through the C ABI: h beside x, g and u, dwg and dwu as the halves of wider rows: the bits of separate buffers"""
+    dtype, stream = torch.bfloat16, torch.cuda.current_stream().cuda_stream
+    x, wg, wu, dh = normal(m, k, 1, dtype), normal(f, k, 2, dtype), normal(f, k, 3, dtype), normal(m, f, 4, dtype)
+    h, g, u = ff.gated_forward(x, wg, wu, save=True)
+    grads = ff.gated_backward(dh, x, wg, wu, g, u)
+    row, gu, dw = torch.zeros(m, k + f, dtype=dtype, device="cuda"), torch.zeros(m, 2 * f, dtype=dtype, device="cuda"), \
+        torch.zeros(f, 2 * k, dtype=dtype, device="cuda")
+    row[:, :k] = x
+    at = lambda t, col: t.data_ptr() + 2 * col
+    nb = max(eq.gated_forward_workspace_bytes(m, f, k, row, k + f, wg, k, wu, k), 16)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    eq.gated_forward(row, k + f, wg, k, wu, k, eq.BF16, m, f, k, eq.ACT_GELU_TANH, at(row, k), k + f, gu, at(gu, f), 2 * f, ws, nb, stream)
+    assert torch.equal(row, torch.cat([x, h], 1)) and torch.equal(gu, torch.cat([g, u], 1))
+    dx = torch.zeros_like(x)
+    nb = eq.gated_backward_workspace_bytes(m, f, k, row, k + f, wg, k, wu, k)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    eq.gated_backward(dh, f, row, k + f, wg, k, wu, k, gu, at(gu, f), 2 * f, eq.BF16, m, f, k, eq.ACT_GELU_TANH, dx, k, dw, 2 * k,
+                      at(dw, k), 2 * k, ws, nb, stream)
+    assert torch.equal(dx, grads[0]) and torch.equal(dw, torch.cat(grads[1:], 1))
     ff.check()
 
 
