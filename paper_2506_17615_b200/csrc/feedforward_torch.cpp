@@ -82,8 +82,8 @@ Matrix matrix(const at::Tensor& t, const char* what) {
     TORCH_CHECK_VALUE(t.is_cuda(), what, " must be a CUDA tensor");
     const int64_t r = t.size(0), c = t.size(1), ld = t.stride(0);
     TORCH_CHECK_VALUE(t.stride(1) == 1 || c <= 1, what, " must have contiguous columns");
-    // any stride is reported for a single row
-    return {t, t.data_ptr(), size_t(r), size_t(c), size_t(r > 1 ? ld : std::max(ld, c))};
+    // any stride, in or out of the library's range, is reported for a single row, which has no next one
+    return {t, t.data_ptr(), size_t(r), size_t(c), size_t(r > 1 ? ld : (c + 15) / 16 * 16)};
 }
 // a matrix that has to be rows x cols, of the type and on the device of `like`
 Matrix matrix(const at::Tensor& t, const char* what, size_t rows, size_t cols, const at::Tensor& like) {

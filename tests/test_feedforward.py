@@ -791,6 +791,25 @@ def test_offsets_beyond_32_bits():
 
 
 @gpu
+def test_the_stride_of_a_single_row_does_not_count():
+    """a token cut out of a row of more than 2^30 elements, of an odd length"""
+    dtype = torch.bfloat16
+    store = torch.empty(1, (1 << 30) + 65, dtype=dtype, device="cuda")
+    x = store[:, :72]
+    assert x.stride(0) > 1 << 30
+    x.copy_(normal(1, 72, 1, dtype))
+    dense, wg, wu = x.contiguous(), normal(40, 72, 2, dtype), normal(40, 72, 3, dtype)
+    h, g, u = ff.gated_forward(dense, wg, wu, save=True)
+    assert torch.equal(ff.gated_forward(x, wg, wu), h)
+    for a, b in zip(ff.gated_backward(h, x, wg, wu, g, u), ff.gated_backward(h, dense, wg, wu, g, u)):
+        assert torch.equal(a, b)
+    for fmt in FORMATS:
+        q = ff.fp4_quantize(wg, fmt)
+        assert torch.equal(ff.fp4_linear(x, q), ff.fp4_linear(dense, q))
+        assert torch.equal(ff.fp4_quantize(x, fmt).codes, ff.fp4_quantize(dense, fmt).codes)
+
+
+@gpu
 def test_results_do_not_depend_on_the_other_tokens():
     """NV and MX: a token's result is the same alone and among others of the same form of the product"""
     w, wu = normal(300, 500, 2, torch.bfloat16), normal(300, 500, 3, torch.bfloat16)
