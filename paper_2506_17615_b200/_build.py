@@ -3,6 +3,7 @@ import fcntl
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -68,24 +69,37 @@ def find_cuda_home():
     raise RuntimeError("the CUDA headers were not found; set CUDA_HOME")
 
 
+def torch_stamp():
+    """what a module compiled against torch's headers depends on, beside its sources"""
+    import torch
+    return f"{torch.__version__} {torch.version.git_version} cxx11={int(torch.compiled_with_cxx11_abi())} {sys.version}"
+
+
+def torch_module_stale():
+    """Missing, older than its sources, or compiled against another torch or Python than this one: by their
+    versions, since an older torch installed over a newer one has older files."""
+    sources = (TORCH_SOURCE, os.path.join(os.path.dirname(_HERE), "include", "equarx.h"))
+    if not os.path.exists(TORCH_MODULE) or any(os.path.getmtime(p) > os.path.getmtime(TORCH_MODULE) for p in sources):
+        return True
+    try:
+        with open(TORCH_MODULE + ".stamp") as f:
+            return f.read() != torch_stamp()
+    except OSError:
+        return True
+
+
 def build_torch_module(force=False):
     """Compile the extension module behind feedforward.py (torch tensors in and out); returns its path.  It
-    depends on the library's header, not on the library, and on the installed torch: a newer torch than the
-    module rebuilds it."""
+    depends on the library's header, not on the library, and on the installed torch."""
     import torch
-    root = os.path.dirname(torch.__file__)
-    sources = (TORCH_SOURCE, os.path.join(os.path.dirname(_HERE), "include", "equarx.h"), os.path.join(root, "version.py"))
-
-    def stale():
-        return not os.path.exists(TORCH_MODULE) or any(os.path.getmtime(p) > os.path.getmtime(TORCH_MODULE) for p in sources)
-
-    if force or stale():
+    if force or torch_module_stale():
         with open(TORCH_MODULE + ".lock", "w") as lock:
             fcntl.flock(lock, fcntl.LOCK_EX)
             try:
-                if force or stale():
-                    tmp = f"{TORCH_MODULE}.{os.getpid()}.tmp"
+                if force or torch_module_stale():
+                    root = os.path.dirname(torch.__file__)
                     include, lib = os.path.join(root, "include"), os.path.join(root, "lib")
+                    tmp, stamp = f"{TORCH_MODULE}.{os.getpid()}.tmp", f"{TORCH_MODULE}.stamp.{os.getpid()}.tmp"
                     subprocess.run([os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC",
                                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
                                     "-I", sysconfig.get_paths()["include"], "-I", include,
@@ -95,7 +109,10 @@ def build_torch_module(force=False):
                                     # torch's own C++ runtime, by name: where only the static one can be
                                     # linked, a second copy in the process breaks its streams
                                     "-l:libstdc++.so.6", f"-Wl,-rpath,{lib}"], check=True)
+                    with open(stamp, "w") as f:
+                        f.write(torch_stamp())
                     os.replace(tmp, TORCH_MODULE)
+                    os.replace(stamp, TORCH_MODULE + ".stamp")
             finally:
                 fcntl.flock(lock, fcntl.LOCK_UN)
     return TORCH_MODULE

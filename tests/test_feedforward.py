@@ -188,6 +188,19 @@ def test_what_the_extension_module_refuses():
             call()
 
 
+def test_the_module_belongs_to_the_installed_torch(monkeypatch):
+    """another torch, however old its files, makes the extension module stale"""
+    from paper_2506_17615_b200 import _build
+    assert not _build.torch_module_stale()
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "1.0")
+        assert _build.torch_module_stale()
+    with monkeypatch.context() as m:
+        m.setattr(_build, "torch_stamp", lambda: "")
+        assert _build.torch_module_stale()
+    assert not _build.torch_module_stale()
+
+
 # ------------------------------------------------------------------ inputs
 
 def normal(rows, cols, seed, dtype, scale=1.0, pad=0):
