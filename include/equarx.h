@@ -531,7 +531,10 @@ int equarx_gated_forward(const void *x, size_t ldx, const void *wg, size_t ldwg,
 /*
  * Gradients of equarx_gated_forward.  From dh (m x f) and the g and u it kept:
  *     dU = dh act(g), dG = dh u act'(g), dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.
- * dU and dG are computed in fp32 and rounded to the 16-bit type that the products read.
+ * dU and dG are computed in fp32 and rounded to the 16-bit type that the products read;
+ * in FP16 they are scaled by a common power of two where its range would not hold them, so
+ * a gradient overflows or vanishes only where its own value does.  (g and u are what the
+ * forward call kept: projections above FP16's range are infinite there.)
  * dx is m x k, dwg and dwu are f x k, of the inputs' type.
  */
 size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, const void *x, size_t ldx,

@@ -719,7 +719,8 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
 size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, const void* x, size_t ldx, const void* wg, size_t ldwg,
                                              const void* wu, size_t ldwu) {
     if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k)) return 0;
-    return copy_bytes(m, k, x, ldx) + copy_bytes(f, k, wg, ldwg) + copy_bytes(f, k, wu, ldwu) + 2 * up(m * up(f, 8) * 2, 256);
+    return copy_bytes(m, k, x, ldx) + copy_bytes(f, k, wg, ldwg) + copy_bytes(f, k, wu, ldwu) + 2 * up(m * up(f, 8) * 2, 256) +
+           (m ? up((m + 1) * sizeof(float), 256) : 0);
 }
 
 int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx, const void* wg, size_t ldwg, const void* wu,
@@ -765,12 +766,16 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     e.ld_dh = lddh;
     e.ld_gu = ldgu;
     e.ld_out = ldd;
+    e.row_top = reinterpret_cast<float*>(ws + 2 * up(m * ldd * 2, 256));
+    e.factor = e.row_top + m;
+    e.rows = int(m);
     e.cols = int(f);
     e.act = act;
-    e.dtype = dtype;
     e.unit = std::min({unit_of(dh, lddh, 2), unit_of(g, ldgu, 2), unit_of(u, ldgu, 2)});
     const int threads = int(std::min<size_t>(512, up(ceil_div(f, 8 * kGradGroups), 32)));
-    TRY(launch(gate_grad_kernel, dim3(unsigned(m)), threads, 0, 1, e, stream));
+    TRY(launch(dtype == EQUARX_BF16 ? gate_grad_kernel<kBf16> : gate_grad_kernel<kFp16>, dim3(unsigned(m)), threads, 0, 1, e, stream));
+    const float* const factor = dtype == EQUARX_FP16 ? e.factor : nullptr;
+    if (factor) TRY(launch(grad_range_kernel, dim3(unsigned(std::min<size_t>(m, sms))), 512, 0, 1, e, stream));
 
     // dx = dG Wg + dU Wu, whose reduction runs over f, twice, and dWg = dG^T x, dWu = dU^T x, whose runs over the
     // tokens.  Neither needs the other's result: where both take tiles they are one launch; else dx goes first and the
@@ -786,6 +791,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
 
     TileArgs<kGrads> t = {};
     t.bf16 = bf16;
+    t.factor = factor;
     if (!x_splits) {
         Product& p = t.product[0];
         TRY(map16(p.a[0], dg, kRowsM));
@@ -817,6 +823,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
         a.out[0] = ox_out;
         a.stages = fs;
         a.bf16 = bf16;
+        a.factor = factor;
         a.order = kForwarding;
         TRY((launch_split<kHalf, kSum2, true, false, false>(a, split_x, k, m, stream)));
     }
@@ -833,6 +840,7 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     a.out[1] = ou_out;
     a.stages = ms;
     a.bf16 = bf16;
+    a.factor = factor;
     a.order = kBeside;
     return launch_split<kHalf, kOut2, true, true, false>(a, split_w, k, f, stream);
 }

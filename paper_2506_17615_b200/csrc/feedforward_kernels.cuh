@@ -5,6 +5,7 @@
 //   tile_kernel       persistent 256 x bn output tiles on the tensor cores of two SMs
 //   split_kernel      few tokens: weights on the 128-row side, the reduction split over a cluster
 //   gate_grad_kernel  gradients of the two projections from dh, g and u
+//   grad_range_kernel the same scaled, where fp16 cannot hold them
 //   pack_kernel       rows that TMA cannot read (a stride that is no multiple of 16 bytes) -> rows it can
 //   fp4_quantize_kernel, fp4_dequantize_kernel
 #pragma once
@@ -219,6 +220,7 @@ template <int MODE> struct TileArgs {
     CUtensorMap scales_a, scales_b[2];    // 4-bit: the scales of 128 rows and one stage are rows of 128 bytes
     const float* row_a;                   // NV: one factor for each row of a and of b
     const float* row_b[2];
+    const float* factor;                  // gradients in fp16: what outputs are multiplied by; else null
     int act, bf16, save, order;
 };
 
@@ -466,6 +468,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
         // ---------------------------------------------------- outputs
         const int quarter = warp & 3, side = warp >> 2;
         uint32_t local = 0, flip = 0;
+        const float scale = MODE == kGrads && p.factor ? __ldcg(p.factor) : 1.0f;
         const uint32_t staging = smem + PIPE * STAGE + warp * 2 * kStageOut;
         auto store = [&](const Product& g, int i, int row0, int col0, float (&v)[32]) {
             if (row0 >= g.m || col0 >= g.n) return;
@@ -546,6 +549,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                         store(g, 2, row0, col0, w);
                     }
                 } else {
+                    if (MODE == kGrads && scale != 1.0f) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= scale;
+                    }
                     store(g, which, row0, col0, v);
                 }
             }
@@ -571,19 +578,19 @@ struct GradArgs {
     const void *dh, *g, *u;
     void *dg, *du;
     size_t ld_dh, ld_gu, ld_out;      // ld_out is a multiple of 8; columns [cols, ld_out) are not read
-    int cols, act, dtype, unit;       // unit: bytes that the rows of dh, g and u start on multiples of
+    float *row_top, *factor;          // fp16: see below
+    int rows, cols, act, unit;        // unit: bytes that the rows of dh, g and u start on multiples of
 };
 constexpr int kGradGroups = 2;        // groups of 8 elements of a thread, loaded together
 
-// One CTA a row.
-__global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ GradArgs p) {
-    const size_t row = blockIdx.x;
+// One row by one CTA, divided by a power of two (`times`: its inverse); the largest finite magnitude that this
+// thread met, before that.
+template <int DT>
+__device__ __forceinline__ float gate_grad_row(const GradArgs& p, size_t row, float times) {
     const int span = blockDim.x * 8;
     const uint16_t* const dh = static_cast<const uint16_t*>(p.dh) + row * p.ld_dh;
     const uint16_t* const g = static_cast<const uint16_t*>(p.g) + row * p.ld_gu;
     const uint16_t* const u = static_cast<const uint16_t*>(p.u) + row * p.ld_gu;
-    grid_launch();
-    grid_wait();
     auto load = [&](const uint16_t* src, int col) {
         if (p.unit >= 16 && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
         if (p.unit >= 4 && col + 8 <= p.cols) {
@@ -594,6 +601,16 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = col + j < p.cols ? src[col + j] : 0;
         return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    };
+    float top = 0.0f;
+    auto rounded = [&](float a, float b) {
+        if constexpr (DT == kFp16) {
+            if (fabsf(a) < __uint_as_float(0x7F800000u)) top = fmaxf(top, fabsf(a));
+            if (fabsf(b) < __uint_as_float(0x7F800000u)) top = fmaxf(top, fabsf(b));
+            return pack2(a * times, b * times, DT);
+        } else {
+            return pack2(a, b, DT);
+        }
     };
     for (int first = threadIdx.x * 8; first < p.cols; first += span * kGradGroups) {
         uint4 a[kGradGroups], b[kGradGroups], c[kGradGroups];
@@ -614,17 +631,60 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
             uint32_t og[4], ou[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 fh = unpack2(wa[j], p.dtype), fg = unpack2(wb[j], p.dtype), fu = unpack2(wc[j], p.dtype);
+                const float2 fh = unpack2(wa[j], DT), fg = unpack2(wb[j], DT), fu = unpack2(wc[j], DT);
                 float v0, v1, s0, s1;
                 act_grad(fg.x, p.act, v0, s0);
                 act_grad(fg.y, p.act, v1, s1);
-                ou[j] = pack2(fh.x * v0, fh.y * v1, p.dtype);
-                og[j] = pack2(fh.x * fu.x * s0, fh.y * fu.y * s1, p.dtype);
+                ou[j] = rounded(fh.x * v0, fh.y * v1);
+                og[j] = rounded(fh.x * fu.x * s0, fh.y * fu.y * s1);
             }
             *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dg) + row * p.ld_out + col) = make_uint4(og[0], og[1], og[2], og[3]);
             *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.du) + row * p.ld_out + col) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
         }
     }
+    return top;
+}
+// the largest of all threads' values, none of them negative; every thread gets it
+__device__ __forceinline__ float block_max(float v, uint32_t (&shared)[16]) {
+    const int lane = threadIdx.x & 31, warps = blockDim.x / 32;
+    uint32_t m = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v));
+    if (lane == 0) shared[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = __reduce_max_sync(0xFFFFFFFFu, lane < warps ? shared[lane] : 0);
+    return __uint_as_float(m);
+}
+
+// One CTA a row.
+template <int DT>
+__global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ GradArgs p) {
+    __shared__ uint32_t shared[16];
+    grid_launch();
+    grid_wait();
+    float top = gate_grad_row<DT>(p, blockIdx.x, 1.0f);
+    if constexpr (DT == kFp16) {
+        top = block_max(top, shared);
+        if (threadIdx.x == 0) p.row_top[blockIdx.x] = top;
+    }
+}
+
+// fp16 alone: dU and dG are products of up to three fp16 numbers and may lie outside its range while the gradients,
+// sums over them, lie inside.  Where the largest finite one would round to infinity, or is below 2^-4 (above, no
+// rounding error exceeds 2^-21 of it, subnormal numbers included), all are computed again, divided by the power of two
+// that brings it into [2^14, 2^15); the products' outputs are multiplied by it (*factor, else 1).  One for both,
+// because dx adds products with both.  A few CTAs that each find the largest of all rows.
+__global__ void __launch_bounds__(512) grad_range_kernel(const __grid_constant__ GradArgs p) {
+    __shared__ uint32_t shared[16];
+    grid_launch();
+    grid_wait();
+    float top = 0.0f;
+    for (int row = threadIdx.x; row < p.rows; row += blockDim.x) top = fmaxf(top, p.row_top[row]);
+    top = block_max(top, shared);
+    const bool fits = top == 0.0f || (top >= 0x1p-4f && top < 65520.0f);
+    const int e = fits ? 0 : max(int(__float_as_uint(top) >> 23), 1) - 127 - 14;      // top = 1.f * 2^(e + 14)
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.factor = __uint_as_float(uint32_t(127 + max(e, -100)) << 23);
+    if (fits) return;
+    const float times = __uint_as_float(uint32_t(127 - max(e, -100)) << 23);
+    for (int row = blockIdx.x; row < p.rows; row += gridDim.x) gate_grad_row<kFp16>(p, row, times);
 }
 
 // 16-bit words to rows whose stride is a multiple of 16 bytes, up to three matrices in a launch
@@ -1087,6 +1147,7 @@ struct SplitArgs {
     const uint8_t* scales_x;
     const float* row_w[2];
     const float* row_x;
+    const float* factor;              // as in TileArgs
     QuantArgs raw;                    // fused: x in 16 bits, quantized by the kernel itself
     Out out[3];
     int features, tokens;             // rows of w, rows of x
@@ -1426,6 +1487,11 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
                 if (i < n) v[i] = v[i] * rx * p.row_w[0][f + i];
                 if (MODE == kGated && i < n) w[i] = w[i] * rx * p.row_w[1][f + i];
             }
+        }
+        if ((MODE == kSum2 || MODE == kOut2) && p.factor) {
+            const float scale = __ldcg(p.factor);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= scale;
         }
         const size_t row = size_t(t0 + t);
         if (MODE == kGated) {

@@ -1,4 +1,6 @@
 """The feed-forward operators: refusals (no GPU), and the kernels against 64-bit references."""
+import math
+
 import pytest
 import torch
 
@@ -515,6 +517,59 @@ def test_gradients_against_differences(act, m, f, k):
         numeric = (loss(*plus) - loss(*minus)) / (2 * step)
         tol = ((ref.rounded(v, e, dtype) + extra) * direction.abs()).sum() + 1e-5 * numeric.abs() + 1e-6
         assert abs(float((got.double() * direction).sum() - numeric)) <= float(tol), i
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("large", [True, False])
+@pytest.mark.parametrize("m,f,k", [(1, 64, 64), (2, 130, 72), (128, 200, 300), (200, 77, 1001), (512, 520, 264), (4100, 100, 136),
+                                   (700, 5000, 96)])
+def test_gradients_of_projections_beyond_the_range(dtype, large, m, f, k):
+    """dU and dG above 65504 or deep among fp16's subnormal numbers, while dx, dWg and dWu are within its range.  As
+    operands they carry one rounding of their type, after a power of two has brought the largest into [2^14, 2^15)."""
+    act = eq.ACT_SILU
+    if large:                                                     # u about 20, g near 0, dG about 40000 times normal squared
+        x, wg, wu = normal(m, k, 1, dtype, 2.0 ** -9), normal(f, k, 2, dtype, 2.0 ** -9), normal(f, k, 3, dtype, 10240 * k ** -0.5)
+        dh = normal(m, f, 4, torch.float32, 4000.0).clamp(-60000, 60000).to(dtype)
+    else:                                                         # u about 2^-3, dG about 2^-22
+        x, wg, wu = normal(m, k, 1, dtype, 2.0 ** 5), normal(f, k, 2, dtype, 2.0 ** -5 * k ** -0.5), \
+            normal(f, k, 3, dtype, 2.0 ** -8 * k ** -0.5)
+        dh = normal(m, f, 4, dtype, 2.0 ** -18)
+    _, g, u = ff.gated_forward(x, wg, wu, act, save=True)
+    assert bool(g.isfinite().all()) and bool(u.isfinite().all())
+    grads = ff.gated_backward(dh, x, wg, wu, g, u, act)
+    x, wg, wu, dh, g, u = (t.double() for t in (x, wg, wu, dh, g, u))
+    du, dg = dh * ref.act(g, act), dh * u * ref.slope(g, act)
+    if large and m * f > 100:
+        assert float(dg.abs().max()) > 65520
+    floor, top = 0.0, max(float(du.abs().max()), float(dg.abs().max()))
+    if dtype == torch.float16:                                     # half a step of its subnormal numbers, scaled with the rest
+        floor = 2.0 ** -25 * (1.0 if 2.0 ** -4 <= top < 65520 else 2.0 ** (math.floor(math.log2(top)) - 14))
+    # fp32 evaluation as in backward_reference
+    edu = (ref.UNIT[dtype] + 2.0 ** -18) * du.abs() + floor
+    edg = ref.UNIT[dtype] * dg.abs() + 2.0 ** -18 * (dh * u).abs() * (1 + g.abs()) + floor
+    want = ((dg @ wg + du @ wu, (edg + 2 * f * ref.ACC * dg.abs()) @ wg.abs() + (edu + 2 * f * ref.ACC * du.abs()) @ wu.abs()),
+            (dg.T @ x, (edg + m * ref.ACC * dg.abs()).T @ x.abs()), (du.T @ x, (edu + m * ref.ACC * du.abs()).T @ x.abs()))
+    for name, got, (v, e) in zip(("dx", "dwg", "dwu"), grads, want):
+        ref.assert_within(got, v, ref.rounded(v, e, dtype), name)
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("m", [9, 300])
+def test_not_finite_gradients_do_not_set_the_range(m):
+    """fp16: one token's dh is infinite, another's is NaN; the others' dG above 65504 still give a finite dx"""
+    dtype, f, k = torch.float16, 64, 72
+    x, wg, wu = normal(m, k, 1, dtype, 2.0 ** -9), normal(f, k, 2, dtype, 2.0 ** -9), normal(f, k, 3, dtype, 10240 * k ** -0.5)
+    dh = normal(m, f, 4, torch.float32, 4000.0).clamp(-60000, 60000).to(dtype)
+    dh[[2, 4]] = 0.0
+    dh[2, 5], dh[4, 0] = float("inf"), float("nan")
+    _, g, u = ff.gated_forward(x, wg, wu, save=True)
+    dx, dwg, _ = ff.gated_backward(dh, x, wg, wu, g, u)
+    rows = [r for r in range(m) if r not in (2, 4)]
+    clean, _, _ = ff.gated_backward(dh[rows], x[rows], wg, wu, g[rows], u[rows])
+    assert bool(clean.isfinite().all()) and torch.equal(dx[rows], clean)
+    assert not bool(dx[[2, 4]].isfinite().any()) and not bool(dwg[[0, 5]].isfinite().any()) and bool(dwg[1].isfinite().all())
 
 
 def leaves(*tensors):
