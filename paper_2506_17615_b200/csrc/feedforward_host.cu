@@ -292,10 +292,21 @@ int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int 
 }
 
 // ---------------------------------------------------------------- launches of the products
-// Tokens up to which a product quantizes its own activations.  It saves a launch on the host (13 -> 9 us for
-// the whole call), and on the GPU, warm, 5376 -> 2688, fused / two launches (us): MX 1 token 4.8 / 5.5,
-// 8 tokens 5.7 / 5.8, 16 tokens 7.8 / 5.9; NV, whose rows' maxima go round the cluster first, 1 token
-// 6.9 / 6.8, 2 tokens 7.0 / 6.8, 4 tokens 7.8 / 6.8.
+// Tokens up to which a product quantizes its own activations, which saves a launch.  Fused / two launches in us, weights
+// that change from call to call, as calls from Python and in a CUDA graph (the kernels alone):
+//                          2688 -> 5376           gated 5376 -> 2688      1000 -> 1250
+//   MX  1 token   calls    6.0 / 8.0              7.4 / 9.0               4.4 / 7.7
+//                 graph    5.2 / 6.2              7.0 / 8.1               3.5 / 4.4
+//       8 tokens  graph    5.9 / 6.3              7.3 / 8.3               3.6 / 4.7
+//       16        graph    7.5 / 6.4              8.8 / 8.5               4.3 / 4.9
+//   NV  1 token   calls    8.6 / 9.1              9.9 / 10.7              6.4 / 7.8
+//                 graph    7.9 / 7.7              9.4 / 9.7               5.7 / 5.0
+//       2 tokens  calls    8.6 / 9.1              9.9 / 10.7              6.3 / 7.8
+//                 graph    7.9 / 7.7              9.5 / 9.7               5.5 / 5.1
+//       4         calls    9.3 / 9.2              10.7 / 10.7             6.3 / 7.8
+//                 graph    8.6 / 7.8              10.3 / 9.7              5.7 / 5.3
+// MX wins up to 8 tokens everywhere.  NV's row maxima go round the cluster first: up to 2 tokens it wins as calls, and in
+// a graph for the gated block, where a single product loses 0.2 to 0.7 us.
 constexpr size_t kFusedMxTokens = 8, kFusedNvTokens = 2;
 static_assert(kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, "the fused form takes one tile of tokens");
 
