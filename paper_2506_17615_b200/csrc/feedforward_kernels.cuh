@@ -370,6 +370,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                 if (!ok) break;
             }
         }
+        // Arrivals on this CTA's barriers that the first CTA's products still owe come before its shared memory goes away:
+        // one more turn round the ring, whose slots that were never filled are free.  (The output warps' waits
+        // for the last product say nothing of them.)
+        for (int i = 0; i < PIPE && ok; ++i) {
+            ok = barrier_wait_warp(empty + 8 * slot, phase, &abort);
+            if (++slot == PIPE) {
+                slot = 0;
+                phase ^= 1;
+            }
+        }
         if (gave_up_warp(&abort) && rank == 0)         // what has been started lands before the shared memory goes away
             for (uint32_t i = issued > PIPE ? issued - PIPE : 0; i < issued; ++i)
                 barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
@@ -1351,6 +1361,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             if (!(ok = barrier_wait_warp(empty + 8 * slot, (it / p.pipe & 1) ^ 1, &abort))) break;
             load_stage(it);
         }
+        // arrivals that are still owed come before the shared memory goes away
+        for (int i = max(it - p.pipe, 0); i < it && ok; ++i) ok = barrier_wait_warp(empty + 8 * (i % p.pipe), i / p.pipe & 1, &abort);
         if (gave_up_warp(&abort))
             for (int i = it > p.pipe ? it - p.pipe : 0; i < it; ++i) barrier_drain(full + 8 * (i % p.pipe), i / p.pipe & 1);
         __syncwarp();
