@@ -2,7 +2,8 @@
 
 Each rank holds its slices of the weights.  Serving: the block over 4-bit weights (fp4_gated, then
 fp4_linear for the down projection) gives a bf16 partial sum for each rank, and the quantized AllReduce
-adds them.  Training: the block over 16-bit weights with its gradients; the AllReduce adds the ranks' dx.
+adds them.  Training: the block over 16-bit weights with its gradients, from dh, which a library product with the down
+projection gives, to dx and the gradients of gate and up; the AllReduce adds the ranks' dx.
 
     python -m paper_2506_17615_b200.block --ranks 8 --tokens 512 --hidden 3840 --width 15360 [--format mx]
 

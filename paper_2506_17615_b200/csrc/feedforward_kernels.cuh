@@ -681,7 +681,8 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
 // sums over them, lie inside.  Where the largest finite one would round to infinity, or is below 2^-4 (above, no
 // rounding error exceeds 2^-21 of it, subnormal numbers included), all are computed again, divided by the power of two
 // that brings it into [2^14, 2^15); the products' outputs are multiplied by it (*factor, else 1).  One for both,
-// because dx adds products with both.  A few CTAs that each find the largest of all rows.
+// because dx adds products with both.  A few CTAs that each find the largest of all rows.  Where all fit it costs 1 us
+// (backward pass of 2048 x 3840, 1920: 98.4 -> 99.5 us).
 __global__ void __launch_bounds__(512) grad_range_kernel(const __grid_constant__ GradArgs p) {
     __shared__ uint32_t shared[16];
     grid_launch();
