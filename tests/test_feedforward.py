@@ -1,5 +1,8 @@
 """The feed-forward operators: refusals (no GPU), and the kernels against 64-bit references."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -131,10 +134,7 @@ def test_gated_forward_and_backward_refuse_bad_arguments():
     assert eq.last_cuda_error() == 0
 
 
-def test_matrices_side_by_side_are_no_overlap(monkeypatch):
-    """columns of one buffer are accepted, shared elements are not; no launch reaches a GPU"""
-    monkeypatch.setenv("EQUARX_INJECT_LAUNCH_ERROR", "719")
-
+def side_by_side():
     def forward(g, u, ldgu, h=A + 3 * GB, ldh=8, m=4):
         return status_of(eq.gated_forward, x=A, ldx=64, wg=A + GB, ldwg=64, wu=A + 2 * GB, ldwu=64, dtype=eq.FP16, m=m, f=8, k=64,
                          act=1, h=h, ldh=ldh, g=g, u=u, ldgu=ldgu, workspace=0, workspace_bytes=0)
@@ -153,6 +153,16 @@ def test_matrices_side_by_side_are_no_overlap(monkeypatch):
     one = dict(dtype=eq.BF16, rows=1, cols=8, ld=8, format=eq.FP4_MX, codes=far + 2 * GB, scales=A + GB, row_scales=0)
     assert status_of(eq.fp4_quantize, x=far + 2 * GB + 16, **one) == binding.ERR_CUDA
     assert status_of(eq.fp4_quantize, x=far + 2 * GB + 14, **one) == binding.ERR_ALIAS
+
+
+def test_matrices_side_by_side_are_no_overlap():
+    """Columns of one buffer are accepted, shared elements are not.  What is accepted stops at an injected launch error,
+    which the library remembers, so this runs in a process of its own; no launch reaches a GPU."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    paths = os.pathsep.join([here, os.path.dirname(here)])
+    child = subprocess.run([sys.executable, "-c", "import test_feedforward as t; t.side_by_side()"], capture_output=True, text=True,
+                           env={**os.environ, "PYTHONPATH": paths, "EQUARX_INJECT_LAUNCH_ERROR": "719"}, timeout=300)
+    assert child.returncode == 0, child.stderr
 
 
 def test_sizes_of_the_buffers():
