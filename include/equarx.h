@@ -517,10 +517,12 @@ int equarx_fp4_gated(const void *x, int dtype, size_t ldx,
  * h = act(x Wg^T) * (x Wu^T) over 16-bit weights, in one kernel: x is m x k, wg and wu
  * are f x k, h is m x f, all of one type (BF16 or FP16).  g and u, both m x f with row
  * stride ldgu, receive the projections x Wg^T and x Wu^T for the backward call; both
- * are NULL when no gradient is wanted.  Workspace (the copies that alignment makes
+ * are NULL when no gradient is wanted.  They are of that type too, or, with
+ * EQUARX_KEPT_FP32 or-ed into dtype (here and in the backward call), fp32.  Workspace (the copies that alignment makes
  * necessary, often 0 bytes): equarx_gated_forward_workspace_bytes, which looks at the
  * alignment of the pointers and strides and reads nothing.
  */
+#define EQUARX_KEPT_FP32 0x100
 size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, const void *x, size_t ldx,
                                              const void *wg, size_t ldwg, const void *wu, size_t ldwu);
 int equarx_gated_forward(const void *x, size_t ldx, const void *wg, size_t ldwg, const void *wu, size_t ldwu,
@@ -533,8 +535,10 @@ int equarx_gated_forward(const void *x, size_t ldx, const void *wg, size_t ldwg,
  *     dU = dh act(g), dG = dh u act'(g), dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.
  * dU and dG are computed in fp32 and rounded to the 16-bit type that the products read;
  * in FP16 they are scaled by a common power of two where its range would not hold them, so
- * a gradient overflows or vanishes only where its own value does.  (g and u are what the
- * forward call kept: projections above FP16's range are infinite there.)
+ * a gradient overflows or vanishes only where its own value does.  Of the gradients' relative
+ * error, 0.0030 in BF16 and 0.00038 in FP16, the outputs' own rounding is 0.0017 and
+ * 0.00021; g and u kept in fp32 leave 0.0024 and 0.00030.  (Kept in FP16, projections above
+ * its range are infinite.)
  * dx is m x k, dwg and dwu are f x k, of the inputs' type.
  */
 size_t equarx_gated_backward_workspace_bytes(size_t m, size_t f, size_t k, const void *x, size_t ldx,

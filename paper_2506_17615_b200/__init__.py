@@ -20,6 +20,7 @@ _BINDING_NAMES = (
     "FP32",
     "FP4_MX",
     "FP4_NV",
+    "KEPT_FP32",
     "FLAVOUR_E4M3",
     "FLAVOUR_E5M2",
     "FLAVOUR_QUANT_AG",

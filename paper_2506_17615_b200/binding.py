@@ -16,6 +16,7 @@ FLAVOUR_SEMI_LOOP, FLAVOUR_QUANT_RS, FLAVOUR_QUANT_AG, FLAVOUR_E4M3, FLAVOUR_E5M
 BF16, FP16, FP32 = range(3)
 FP4_MX, FP4_NV = range(2)
 ACT_SILU, ACT_GELU_TANH = range(2)
+KEPT_FP32 = 0x100        # or-ed into the type of a gated call: g and u in fp32
 FLAVOUR_FIFO_BYTES = 16 * 1024 * 1024
 STATIC_WORKSPACE_BYTES = 16 * 1024 * 1024
 

@@ -671,6 +671,8 @@ size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, const 
 int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg, const void* wu, size_t ldwu, int dtype,
                          size_t m, size_t f, size_t k, int act, void* h, size_t ldh, void* g, void* u, size_t ldgu,
                          void* workspace, size_t workspace_bytes, equarx_stream_t stream) {
+    const int kept = dtype & EQUARX_KEPT_FP32 ? EQUARX_FP32 : dtype;            // type of g and u
+    dtype &= ~EQUARX_KEPT_FP32;
     if (!is_16bit(dtype) || !is_act(act)) return EQUARX_ERR_FORMAT;
     if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k) || bad_ld(ldh, f))
         return EQUARX_ERR_COUNT;
@@ -680,16 +682,17 @@ int equarx_gated_forward(const void* x, size_t ldx, const void* wg, size_t ldwg,
     const size_t need = equarx_gated_forward_workspace_bytes(m, f, k, x, ldx, wg, ldwg, wu, ldwu);
     if (need && !workspace) return EQUARX_ERR_NULL;
     if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
-    for (const void* p : {x, wg, wu, static_cast<const void*>(h), static_cast<const void*>(g), static_cast<const void*>(u)})
+    for (const void* p : {x, wg, wu, static_cast<const void*>(h)})
         if (!aligned(p, 2)) return EQUARX_ERR_ALIGN;
-    if (!aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    if (!aligned(g, size_of(kept)) || !aligned(u, size_of(kept)) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(x, m, k, ldx, 2), matrix(wg, f, k, ldwg, 2), matrix(wu, f, k, ldwu, 2)},
-                      {matrix(h, m, f, ldh, 2), matrix(g, m, f, ldgu, 2), matrix(u, m, f, ldgu, 2), Span{workspace, need}}));
+                      {matrix(h, m, f, ldh, 2), matrix(g, m, f, ldgu, size_of(kept)), matrix(u, m, f, ldgu, size_of(kept)),
+                       Span{workspace, need}}));
 
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     Operand ox{x, ldx, m, k}, og{wg, ldwg, f, k}, ou{wu, ldwu, f, k};
     TRY(make_readable({&ox, &og, &ou}, ws, stream));
-    const Out oh = out_rows(h, ldh, dtype), sg = out_rows(g, ldgu, dtype), su = out_rows(u, ldgu, dtype);
+    const Out oh = out_rows(h, ldh, dtype), sg = out_rows(g, ldgu, kept), su = out_rows(u, ldgu, kept);
     const int stages = int(ceil_div(k, 64));
     int sms;
     TRY(current_device(sms));
@@ -738,6 +741,9 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
                           size_t ldwu, const void* g, const void* u, size_t ldgu, int dtype, size_t m, size_t f, size_t k,
                           int act, void* dx, size_t lddx, void* dwg, size_t lddwg, void* dwu, size_t lddwu, void* workspace,
                           size_t workspace_bytes, equarx_stream_t stream) {
+    const bool wide = dtype & EQUARX_KEPT_FP32;
+    const size_t kept = wide ? 4 : 2;                                           // bytes of an element of g and u
+    dtype &= ~EQUARX_KEPT_FP32;
     if (!is_16bit(dtype) || !is_act(act)) return EQUARX_ERR_FORMAT;
     if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(lddh, f) || bad_ld(ldx, k) || bad_ld(ldwg, k) || bad_ld(ldwu, k) ||
         bad_ld(ldgu, f) || bad_ld(lddx, k) || bad_ld(lddwg, k) || bad_ld(lddwu, k))
@@ -745,12 +751,11 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     if (!dwg || !dwu || (m && (!dh || !x || !wg || !wu || !g || !u || !dx || !workspace))) return EQUARX_ERR_NULL;
     const size_t need = equarx_gated_backward_workspace_bytes(m, f, k, x, ldx, wg, ldwg, wu, ldwu);
     if (m && workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
-    for (const void* p : {dh, x, wg, wu, g, u, static_cast<const void*>(dx), static_cast<const void*>(dwg),
-                          static_cast<const void*>(dwu)})
+    for (const void* p : {dh, x, wg, wu, static_cast<const void*>(dx), static_cast<const void*>(dwg), static_cast<const void*>(dwu)})
         if (!aligned(p, 2)) return EQUARX_ERR_ALIGN;
-    if (!aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    if (!aligned(g, kept) || !aligned(u, kept) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     TRY(check_overlap({matrix(dh, m, f, lddh, 2), matrix(x, m, k, ldx, 2), matrix(wg, f, k, ldwg, 2),
-                       matrix(wu, f, k, ldwu, 2), matrix(g, m, f, ldgu, 2), matrix(u, m, f, ldgu, 2)},
+                       matrix(wu, f, k, ldwu, 2), matrix(g, m, f, ldgu, kept), matrix(u, m, f, ldgu, kept)},
                       {matrix(dx, m, k, lddx, 2), matrix(dwg, f, k, lddwg, 2), matrix(dwu, f, k, lddwu, 2),
                        Span{workspace, m ? need : 0}}));
     if (m == 0) {       // sums over no tokens
@@ -782,11 +787,15 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
     e.rows = int(m);
     e.cols = int(f);
     e.act = act;
-    e.unit = std::min({unit_of(dh, lddh, 2), unit_of(g, ldgu, 2), unit_of(u, ldgu, 2)});
+    e.unit = std::min({unit_of(dh, lddh, 2), unit_of(g, ldgu, kept), unit_of(u, ldgu, kept)});
     const int threads = int(std::min<size_t>(512, up(ceil_div(f, 8 * kGradGroups), 32)));
-    TRY(launch(dtype == EQUARX_BF16 ? gate_grad_kernel<kBf16> : gate_grad_kernel<kFp16>, dim3(unsigned(m)), threads, 0, 1, e, stream));
+    const auto grad = dtype == EQUARX_BF16 ? (wide ? gate_grad_kernel<kBf16, true> : gate_grad_kernel<kBf16, false>)
+                                           : (wide ? gate_grad_kernel<kFp16, true> : gate_grad_kernel<kFp16, false>);
+    TRY(launch(grad, dim3(unsigned(m)), threads, 0, 1, e, stream));
     const float* const factor = dtype == EQUARX_FP16 ? e.factor : nullptr;
-    if (factor) TRY(launch(grad_range_kernel, dim3(unsigned(std::min<size_t>(m, sms))), 512, 0, 1, e, stream));
+    if (factor)
+        TRY(launch(wide ? grad_range_kernel<true> : grad_range_kernel<false>, dim3(unsigned(std::min<size_t>(m, sms))), 512, 0, 1, e,
+                   stream));
 
     // dx = dG Wg + dU Wu, whose reduction runs over f, twice, and dWg = dG^T x, dWu = dU^T x, whose runs over the
     // tokens.  Neither needs the other's result: where both take tiles they are one launch; else dx goes first and the

@@ -11,6 +11,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "tensor_ops.cuh"
 
 namespace equarx {
@@ -595,12 +597,13 @@ constexpr int kGradGroups = 2;        // groups of 8 elements of a thread, loade
 
 // One row by one CTA, divided by a power of two (`times`: its inverse); the largest finite magnitude that this
 // thread met, before that.
-template <int DT>
+template <int DT, bool WIDE>
 __device__ __forceinline__ float gate_grad_row(const GradArgs& p, size_t row, float times) {
+    using Kept = typename std::conditional<WIDE, float, uint16_t>::type;
     const int span = blockDim.x * 8;
     const uint16_t* const dh = static_cast<const uint16_t*>(p.dh) + row * p.ld_dh;
-    const uint16_t* const g = static_cast<const uint16_t*>(p.g) + row * p.ld_gu;
-    const uint16_t* const u = static_cast<const uint16_t*>(p.u) + row * p.ld_gu;
+    const Kept* const g = static_cast<const Kept*>(p.g) + row * p.ld_gu;
+    const Kept* const u = static_cast<const Kept*>(p.u) + row * p.ld_gu;
     auto load = [&](const uint16_t* src, int col) {
         if (p.unit >= 16 && col + 8 <= p.cols) return *reinterpret_cast<const uint4*>(src + col);
         if (p.unit >= 4 && col + 8 <= p.cols) {
@@ -611,6 +614,35 @@ __device__ __forceinline__ float gate_grad_row(const GradArgs& p, size_t row, fl
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = col + j < p.cols ? src[col + j] : 0;
         return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    };
+    // eight of g or u, as floats where they were kept in fp32
+    struct Eight {
+        uint4 w[WIDE ? 2 : 1];
+    };
+    auto load_kept = [&](const Kept* src, int col) {
+        Eight v;
+        if constexpr (!WIDE) {
+            v.w[0] = load(src, col);
+        } else if (p.unit >= 16 && col + 8 <= p.cols) {
+            v.w[0] = *reinterpret_cast<const uint4*>(src + col);
+            v.w[1] = *reinterpret_cast<const uint4*>(src + col + 4);
+        } else {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = col + j < p.cols ? __float_as_uint(src[col + j]) : 0;
+            v.w[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            v.w[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+        return v;
+    };
+    auto pair = [&](const Eight& v, int j) {
+        if constexpr (WIDE) {
+            const uint4& q = v.w[j / 2];
+            return j & 1 ? make_float2(__uint_as_float(q.z), __uint_as_float(q.w)) : make_float2(__uint_as_float(q.x), __uint_as_float(q.y));
+        } else {
+            const uint4& q = v.w[0];
+            return unpack2(j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w, DT);
+        }
     };
     float top = 0.0f;
     auto rounded = [&](float a, float b) {
@@ -623,25 +655,25 @@ __device__ __forceinline__ float gate_grad_row(const GradArgs& p, size_t row, fl
         }
     };
     for (int first = threadIdx.x * 8; first < p.cols; first += span * kGradGroups) {
-        uint4 a[kGradGroups], b[kGradGroups], c[kGradGroups];
+        uint4 a[kGradGroups];
+        Eight b[kGradGroups], c[kGradGroups];
 #pragma unroll
         for (int i = 0; i < kGradGroups; ++i) {
             const int col = first + i * span;
             if (col >= p.cols) continue;
             a[i] = load(dh, col);
-            b[i] = load(g, col);
-            c[i] = load(u, col);
+            b[i] = load_kept(g, col);
+            c[i] = load_kept(u, col);
         }
 #pragma unroll
         for (int i = 0; i < kGradGroups; ++i) {
             const int col = first + i * span;
             if (col >= p.cols) continue;
-            const uint32_t wa[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, wb[4] = {b[i].x, b[i].y, b[i].z, b[i].w},
-                           wc[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+            const uint32_t wa[4] = {a[i].x, a[i].y, a[i].z, a[i].w};
             uint32_t og[4], ou[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 fh = unpack2(wa[j], DT), fg = unpack2(wb[j], DT), fu = unpack2(wc[j], DT);
+                const float2 fh = unpack2(wa[j], DT), fg = pair(b[i], j), fu = pair(c[i], j);
                 float v0, v1, s0, s1;
                 act_grad(fg.x, p.act, v0, s0);
                 act_grad(fg.y, p.act, v1, s1);
@@ -664,13 +696,13 @@ __device__ __forceinline__ float block_max(float v, uint32_t (&shared)[16]) {
     return __uint_as_float(m);
 }
 
-// One CTA a row.
-template <int DT>
+// One CTA a row.  WIDE: g and u were kept in fp32.
+template <int DT, bool WIDE>
 __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ GradArgs p) {
     __shared__ uint32_t shared[16];
     grid_launch();
     grid_wait();
-    float top = gate_grad_row<DT>(p, blockIdx.x, 1.0f);
+    float top = gate_grad_row<DT, WIDE>(p, blockIdx.x, 1.0f);
     if constexpr (DT == kFp16) {
         top = block_max(top, shared);
         if (threadIdx.x == 0) p.row_top[blockIdx.x] = top;
@@ -683,6 +715,7 @@ __global__ void __launch_bounds__(512) gate_grad_kernel(const __grid_constant__ 
 // that brings it into [2^14, 2^15); the products' outputs are multiplied by it (*factor, else 1).  One for both,
 // because dx adds products with both.  A few CTAs that each find the largest of all rows.  Where all fit it costs 1 us
 // (backward pass of 2048 x 3840, 1920: 98.4 -> 99.5 us).
+template <bool WIDE>
 __global__ void __launch_bounds__(512) grad_range_kernel(const __grid_constant__ GradArgs p) {
     __shared__ uint32_t shared[16];
     grid_launch();
@@ -695,7 +728,7 @@ __global__ void __launch_bounds__(512) grad_range_kernel(const __grid_constant__
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.factor = __uint_as_float(uint32_t(127 + max(e, -100)) << 23);
     if (fits) return;
     const float times = __uint_as_float(uint32_t(127 - max(e, -100)) << 23);
-    for (int row = blockIdx.x; row < p.rows; row += gridDim.x) gate_grad_row<kFp16>(p, row, times);
+    for (int row = blockIdx.x; row < p.rows; row += gridDim.x) gate_grad_row<kFp16, WIDE>(p, row, times);
 }
 
 // 16-bit words to rows whose stride is a multiple of 16 bytes, up to three matrices in a launch

@@ -85,13 +85,16 @@ Matrix matrix(const at::Tensor& t, const char* what) {
     // any stride, in or out of the library's range, is reported for a single row, which has no next one
     return {t, t.data_ptr(), size_t(r), size_t(c), size_t(r > 1 ? ld : (c + 15) / 16 * 16)};
 }
-// a matrix that has to be rows x cols, of the type and on the device of `like`
-Matrix matrix(const at::Tensor& t, const char* what, size_t rows, size_t cols, const at::Tensor& like) {
+// a matrix that has to be rows x cols, of a type and on the device of `like`
+Matrix matrix(const at::Tensor& t, const char* what, size_t rows, size_t cols, at::ScalarType type, const at::Tensor& like) {
     const Matrix m = matrix(t, what);
-    TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols && t.scalar_type() == like.scalar_type() && t.device() == like.device(),
-                      what, " is ", t.sizes(), " ", t.scalar_type(), " on ", t.device(), ", expected [", rows, ", ", cols, "] ",
-                      like.scalar_type(), " on ", like.device());
+    TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols && t.scalar_type() == type && t.device() == like.device(), what, " is ",
+                      t.sizes(), " ", t.scalar_type(), " on ", t.device(), ", expected [", rows, ", ", cols, "] ", type, " on ",
+                      like.device());
     return m;
+}
+Matrix matrix(const at::Tensor& t, const char* what, size_t rows, size_t cols, const at::Tensor& like) {
+    return matrix(t, what, rows, cols, like.scalar_type(), like);
 }
 
 // The library knows nothing of autograd, so an output would come back cut off from what made it.
@@ -257,24 +260,26 @@ PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// gated_forward(x, wg, wu, act, save); None, and nothing is done, where autograd wants gradients
+// gated_forward(x, wg, wu, act, save, g and u in fp32); None, and nothing is done, where autograd wants gradients
 PyObject* gated_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    arguments(n, 5);
+    arguments(n, 6);
     const Matrix x = matrix(tensor(a[0], "x"), "x");
     const at::Tensor& tg = tensor(a[1], "wg");
     const size_t f = tg.dim() ? size_t(tg.size(0)) : 0;
     const Matrix wg = matrix(tg, "wg", f, x.cols, x.t), wu = matrix(tensor(a[2], "wu"), "wu", f, x.cols, x.t);
-    const int act = enumeration(a[3]), save = PyObject_IsTrue(a[4]), dtype = dtype_code(x.t.scalar_type(), "x");
-    if (save < 0) throw python_error();
+    const int act = enumeration(a[3]), save = PyObject_IsTrue(a[4]), wide = PyObject_IsTrue(a[5]),
+              dtype = dtype_code(x.t.scalar_type(), "x") | (wide ? EQUARX_KEPT_FP32 : 0);
+    if (save < 0 || wide < 0) throw python_error();
     const bool grad[] = {wants_gradient(x.t, "x"), wants_gradient(wg.t, "wg"), wants_gradient(wu.t, "wu")};
     if (grad[0] || grad[1] || grad[2]) Py_RETURN_NONE;
     const at::Device device = x.t.device();
     const at::Tensor h = empty(x.rows, f, x.t.scalar_type(), device);
     at::Tensor g, u;
     if (save) {
-        g = empty(x.rows, f, x.t.scalar_type(), device);
-        u = empty(x.rows, f, x.t.scalar_type(), device);
+        const at::ScalarType kept = wide ? at::kFloat : x.t.scalar_type();
+        g = empty(x.rows, f, kept, device);
+        u = empty(x.rows, f, kept, device);
     }
     const size_t need = entry.gated_forward_workspace_bytes(x.rows, f, x.cols, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld);
     const at::Tensor ws = bytes(need, device);
@@ -294,10 +299,13 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& tg = tensor(a[2], "wg");
     const size_t m = x.rows, k = x.cols, f = tg.dim() ? size_t(tg.size(0)) : 0;
     const Matrix wg = matrix(tg, "wg", f, k, x.t), wu = matrix(tensor(a[3], "wu"), "wu", f, k, x.t);
-    const Matrix dh = matrix(tensor(a[0], "dh"), "dh", m, f, x.t), g = matrix(tensor(a[4], "g"), "g", m, f, x.t),
-                 u = matrix(tensor(a[5], "u"), "u", m, f, x.t);
+    const at::Tensor& kept = tensor(a[4], "g");
+    const bool wide = kept.scalar_type() == at::kFloat;
+    const at::ScalarType type = wide ? at::kFloat : x.t.scalar_type();
+    const Matrix dh = matrix(tensor(a[0], "dh"), "dh", m, f, x.t), g = matrix(kept, "g", m, f, type, x.t),
+                 u = matrix(tensor(a[5], "u"), "u", m, f, type, x.t);
     TORCH_CHECK_VALUE(g.ld == u.ld, "g and u have different row strides");
-    const int act = enumeration(a[6]), dtype = dtype_code(x.t.scalar_type(), "x");
+    const int act = enumeration(a[6]), dtype = dtype_code(x.t.scalar_type(), "x") | (wide ? EQUARX_KEPT_FP32 : 0);
     const at::Device device = x.t.device();
     const at::Tensor dx = empty(m, k, x.t.scalar_type(), device), dwg = empty(f, k, x.t.scalar_type(), device),
                      dwu = empty(f, k, x.t.scalar_type(), device);

@@ -110,15 +110,19 @@ def fp4_gated(x, wg, wu, act=ACT_GELU_TANH):
 
 def gated_forward(x, wg, wu, act=ACT_GELU_TANH, save=False):
     """h = act(x wg^T) * (x wu^T) for x [tokens, k], wg and wu [f, k], all bfloat16 or all float16.
-    With save: (h, g, u), where g and u are the two projections that gated_backward needs."""
-    result = _native.gated_forward(x, wg, wu, act, save)
+    With save: (h, g, u), where g and u are the two projections that gated_backward needs, of x's type, or with
+    save=torch.float32 in fp32, for gradients with less rounding and twice the memory of g and u."""
+    wide = save is torch.float32
+    if isinstance(save, torch.dtype) and not wide and save is not x.dtype:
+        raise ValueError(f"g and u are kept in x's type or in torch.float32, not in {save}")
+    result = _native.gated_forward(x, wg, wu, act, save, wide)
     if result is None:                                  # gradients are wanted
         return _Gated.apply(x, wg, wu, act, save)
     return _or_raise(result, "equarx_gated_forward")
 
 
 def gated_backward(dh, x, wg, wu, g, u, act=ACT_GELU_TANH):
-    """(dx, dwg, dwu) of gated_forward from dh [tokens, f] and the g and u it saved."""
+    """(dx, dwg, dwu) of gated_forward from dh [tokens, f] and the g and u it saved, in either type."""
     return _or_raise(_native.gated_backward(dh, x, wg, wu, g, u, act), "equarx_gated_backward")
 
 
@@ -127,7 +131,7 @@ class _Gated(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, wg, wu, act, save):
-        h, g, u = gated_forward(x, wg, wu, act, save=True)
+        h, g, u = gated_forward(x, wg, wu, act, save or True)
         ctx.save_for_backward(x, wg, wu, g, u)
         ctx.act = act
         if not save:

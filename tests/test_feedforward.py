@@ -134,6 +134,23 @@ def test_gated_forward_and_backward_refuse_bad_arguments():
     assert eq.last_cuda_error() == 0
 
 
+def test_projections_in_fp32_are_checked_as_such():
+    fwd = dict(x=A, ldx=64, wg=A + GB, ldwg=64, wu=A + 2 * GB, ldwu=64, dtype=eq.FP16 | eq.KEPT_FP32, m=4, f=8, k=64, act=1,
+               h=A + 3 * GB, ldh=8, g=A + 4 * GB, u=A + 5 * GB, ldgu=8, workspace=0, workspace_bytes=0)
+    need = eq.gated_backward_workspace_bytes(4, 8, 64, A, 64, A, 64, A, 64)
+    bwd = dict(dh=A, lddh=8, x=A + GB, ldx=64, wg=A + 2 * GB, ldwg=64, wu=A + 3 * GB, ldwu=64, g=A + 4 * GB, u=A + 5 * GB,
+               ldgu=8, dtype=eq.BF16 | eq.KEPT_FP32, m=4, f=8, k=64, act=0, dx=A + 6 * GB, lddx=64, dwg=A + 7 * GB, lddwg=64,
+               dwu=A + 8 * GB, lddwu=64, workspace=A + 9 * GB, workspace_bytes=need)
+    for call, args in ((eq.gated_forward, fwd), (eq.gated_backward, bwd)):
+        for key in ("g", "u"):
+            assert status_of(call, **{**args, key: args[key] + 2}) == binding.ERR_ALIGN
+        for bad in (eq.FP32 | eq.KEPT_FP32, 2 * eq.KEPT_FP32, -1):
+            assert status_of(call, **{**args, "dtype": bad}) == binding.ERR_FORMAT
+    assert status_of(eq.gated_forward, **{**fwd, "u": fwd["g"] + 112}) == binding.ERR_ALIAS      # g is 128 bytes long
+    assert status_of(eq.gated_backward, **{**bwd, "dx": bwd["g"] + 112}) == binding.ERR_ALIAS
+    assert eq.last_cuda_error() == 0
+
+
 def side_by_side():
     def forward(g, u, ldgu, h=A + 3 * GB, ldh=8, m=4):
         return status_of(eq.gated_forward, x=A, ldx=64, wg=A + GB, ldwg=64, wu=A + 2 * GB, ldwu=64, dtype=eq.FP16, m=m, f=8, k=64,
@@ -527,6 +544,75 @@ def test_gradients_against_differences(act, m, f, k):
         numeric = (loss(*plus) - loss(*minus)) / (2 * step)
         tol = ((ref.rounded(v, e, dtype) + extra) * direction.abs()).sum() + 1e-5 * numeric.abs() + 1e-6
         assert abs(float((got.double() * direction).sum() - numeric)) <= float(tol), i
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("m,f,k", TRAIN + [(4100, 1300, 200)])
+def test_projections_kept_in_fp32(dtype, act, m, f, k):
+    pad = (0, 8, 3)[(m + f) % 3]
+    x = normal(m, k, m + f, dtype, 1.0, pad)
+    wg, wu = normal(f, k, f + 1, dtype, 2 * k ** -0.5, pad), normal(f, k, f + 2, dtype, k ** -0.5, (0, 5)[k % 2])
+    dh = normal(m, f, m + 3, dtype, 1.0, pad)
+    h, g, u = ff.gated_forward(x, wg, wu, act, save=torch.float32)
+    assert g.dtype == u.dtype == torch.float32 and torch.equal(ff.gated_forward(x, wg, wu, act), h)
+    xd, wgd, wud, dhd = (t.double() for t in (x, wg, wu, dh))
+    (gv, eg), (uv, eu) = ref.product(xd, wgd), ref.product(xd, wud)
+    ref.assert_within(g, gv, ref.rounded(gv, eg, torch.float32), "g")
+    ref.assert_within(u, uv, ref.rounded(uv, eu, torch.float32), "u")
+    grads = ff.gated_backward(dh, x, wg, wu, g, u, act)
+    want = backward_reference(dhd, xd, wgd, wud, g.double(), u.double(), act, ref.UNIT[dtype])
+    for name, got, (v, e) in zip(("dx", "dwg", "dwu"), grads, want):
+        assert got.dtype == dtype
+        ref.assert_within(got, v, ref.rounded(v, e, dtype), name)
+    # nearer to the gradients of the unrounded projections than with g and u kept in 16 bits
+    if min(m, f, k) > 60:
+        _, g16, u16 = ff.gated_forward(x, wg, wu, act, save=True)
+        off = lambda got, v: float((got.double() - v).norm() / v.norm())
+        exact = backward_reference(dhd, xd, wgd, wud, gv, uv, act, ref.UNIT[dtype])
+        for near, far, (v, _) in zip(grads, ff.gated_backward(dh, x, wg, wu, g16, u16, act), exact):
+            assert off(near, v) < off(far, v)
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("extra", [0, 3, 4])
+@pytest.mark.parametrize("m,f,k", [(3, 130, 72), (300, 264, 136)])
+def test_fp32_projections_in_wider_rows(m, f, k, extra):
+    """through the C ABI, g beside u in rows of any stride, the first at any element; the rest keeps its canary"""
+    dtype, stream = torch.bfloat16, torch.cuda.current_stream().cuda_stream
+    x, wg, wu, dh = normal(m, k, 1, dtype), normal(f, k, 2, dtype), normal(f, k, 3, dtype), normal(m, f, 4, dtype)
+    h0, g0, u0 = ff.gated_forward(x, wg, wu, save=torch.float32)
+    grads = ff.gated_backward(dh, x, wg, wu, g0, u0)
+    ld, kind = 2 * f + extra, eq.BF16 | eq.KEPT_FP32
+    store = torch.full(((m + 1) * ld + extra,), -77.0, device="cuda")
+    gu = store[extra:].as_strided((m, ld), (ld, 1))
+    at = lambda col: gu.data_ptr() + 4 * col
+    h = torch.empty_like(h0)
+    eq.gated_forward(x, k, wg, k, wu, k, kind, m, f, k, eq.ACT_GELU_TANH, h, f, at(0), at(f), ld, 0, 0, stream)
+    assert torch.equal(h, h0) and torch.equal(gu[:, :f], g0) and torch.equal(gu[:, f:2 * f], u0)
+    dx, dwg, dwu = torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)
+    nb = eq.gated_backward_workspace_bytes(m, f, k, x, k, wg, k, wu, k)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    eq.gated_backward(dh, f, x, k, wg, k, wu, k, at(0), at(f), ld, kind, m, f, k, eq.ACT_GELU_TANH, dx, k, dwg, k, dwu, k, ws, nb, stream)
+    for a, b in zip((dx, dwg, dwu), grads):
+        assert torch.equal(a, b)
+    gu[:, :2 * f] = -77.0
+    assert bool((store == -77.0).all())
+    # and through torch tensors that are views of it
+    eq.gated_forward(x, k, wg, k, wu, k, kind, m, f, k, eq.ACT_GELU_TANH, h, f, at(0), at(f), ld, 0, 0, stream)
+    for a, b in zip(ff.gated_backward(dh, x, wg, wu, gu[:, :f], gu[:, f:2 * f]), grads):
+        assert torch.equal(a, b)
+    with pytest.raises(ValueError):
+        ff.gated_backward(dh, x, wg, wu, g0, u0.to(dtype))
+    with pytest.raises(ValueError):
+        ff.gated_forward(x, wg, wu, save=torch.float16)
+    leaf = x.clone().requires_grad_()
+    out = ff.gated_forward(leaf, wg, wu, save=torch.float32)
+    out[0].backward(dh)
+    assert torch.equal(out[1], g0) and torch.equal(leaf.grad, grads[0])
+    ff.check()
 
 
 @gpu
