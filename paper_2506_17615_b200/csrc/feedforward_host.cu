@@ -867,9 +867,12 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
 
 int equarx_feedforward_check(void) {
     uint32_t seen = 0;
-    if (const char* polls = std::getenv("EQUARX_INJECT_TIMEOUT"))
+    cudaError_t e = cudaSuccess;
+    if (const char* polls = std::getenv("EQUARX_INJECT_TIMEOUT")) {
         give_up_kernel<<<1, 64>>>(uint32_t(std::min(std::max(std::atoi(polls), 1), int(tc::kWaitLimit))));
-    cudaError_t e = cudaDeviceSynchronize();
+        e = cudaGetLastError();
+    }
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&seen, tc::g_gave_up, sizeof(seen));
     const uint32_t zero = 0;
     if (e == cudaSuccess && seen) e = cudaMemcpyToSymbol(tc::g_gave_up, &zero, sizeof(zero));
