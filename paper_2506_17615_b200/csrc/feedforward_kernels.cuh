@@ -9,10 +9,9 @@
 //   pack_kernel       rows that TMA cannot read (a stride that is no multiple of 16 bytes) -> rows it can
 //   fp4_quantize_kernel, fp4_dequantize_kernel
 #pragma once
-#include <cuda_fp16.h>
-
 #include <type_traits>
 
+#include "elements.cuh"
 #include "tensor_ops.cuh"
 
 namespace equarx {
@@ -23,7 +22,6 @@ using namespace tc;
 enum Kind { kHalf = 0, kMx = 1, kNv = 2 };                 // 16-bit operands, 4-bit with either scale format
 // what a product kernel computes; the gradients are kGrads in tiles, kSum2 (dx) and kOut2 (dWg, dWu) transposed
 enum Mode { kPlain = 0, kGated = 1, kSum2 = 2, kOut2 = 3, kGrads = 4 };
-enum DType { kBf16 = 0, kFp16 = 1, kFp32 = 2 };
 enum Act { kSilu = 0, kGeluTanh = 1 };
 
 constexpr int kRowsM = 128;               // rows of a tile: lanes of tensor memory
@@ -34,28 +32,6 @@ constexpr int kChunkBytes = 64 * kRowBytes;   // MN-major operands: 64 elements 
 // scales of 128 rows for one stage: 512-byte tiles of 128 rows x 4 scales
 template <int KIND> constexpr int kScaleTiles = KIND == kNv ? 4 : KIND == kMx ? 2 : 0;
 template <int KIND> constexpr int kScaleBytes = 512 * kScaleTiles<KIND>;
-
-// ---------------------------------------------------------------- element types
-__device__ __forceinline__ uint32_t pack2(float lo, float hi, int dtype) {
-    uint32_t r;
-    if (dtype == kBf16)
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else
-        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ float2 unpack2(uint32_t w, int dtype) {
-    if (dtype == kBf16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-    __half2 h;
-    memcpy(&h, &w, 4);
-    return __half22float2(h);
-}
-__device__ __forceinline__ void store1(void* p, size_t i, float v, int dtype) {
-    if (dtype == kFp32)
-        static_cast<float*>(p)[i] = v;
-    else
-        static_cast<uint16_t*>(p)[i] = uint16_t(pack2(v, v, dtype));
-}
 
 // ---------------------------------------------------------------- activation
 // silu(g) = g sigma(g);  gelu_tanh(g) = g sigma(z), z = 2 sqrt(2/pi) (g + 0.044715 g^3), which is
@@ -806,42 +782,12 @@ __device__ __forceinline__ void decode8(uint32_t w, float* v) {
         v[2 * i + 1] = f.y;
     }
 }
-__device__ __forceinline__ uint32_t to_e4m3(float v) {
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
-    return r & 0xFF;
-}
-__device__ __forceinline__ float from_e4m3(uint32_t b) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(uint16_t(b)));
-    return unpack2(h, kFp16).x;
-}
-// 2^(byte - 127); 255 is NaN
-__device__ __forceinline__ float from_e8m0(uint32_t b) {
-    if (b == 255) return __uint_as_float(0x7FFFFFFFu);
-    return b ? __uint_as_float(b << 23) : __uint_as_float(0x00400000u);
-}
-
-constexpr uint32_t kInfBits = 0x7F800000u;
 constexpr int kRowChunks = 3;                    // groups of 16 elements that a thread holds in registers
 
 // 16 neighbouring elements as they are stored: 8 registers of 16-bit pairs or 16 floats
 template <int DT> struct Group {
     uint32_t w[DT == kFp32 ? 16 : 8];
 };
-
-// 256-bit accesses (sm_100): what is read once, or written and not read again here
-__device__ __forceinline__ void load_256(const void* p, uint32_t* w) {
-    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                 : "l"(p)
-                 : "memory");
-}
-__device__ __forceinline__ void store_256(void* p, const uint32_t* w) {
-    asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-}
 
 template <int DT>
 __device__ __forceinline__ void load_elements(const QuantArgs& p, size_t row, int col, Group<DT>& g) {
@@ -965,14 +911,6 @@ __device__ __forceinline__ void row_factors(uint32_t amax, float& up, float& g) 
         up = __fdiv_rn(448.0f, a);
     }
 }
-// two products with one instruction, each rounded as a single one is
-__device__ __forceinline__ void mul2(float& a, float& b, float c) {
-    uint64_t v, w;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
-    asm("mov.b64 %0, {%1, %1};" : "=l"(w) : "f"(c));
-    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(w));
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
-}
 __device__ __forceinline__ uint2 encode_values(float (&v)[16], float inv) {
 #pragma unroll
     for (int i = 0; i < 16; i += 2) mul2(v[i], v[i + 1], inv);
@@ -984,15 +922,6 @@ __device__ __forceinline__ uint2 encode_group(const Group<DT>& g, float inv) {
     group_values<DT>(g, v);
     return encode_values(v, inv);
 }
-// the four scale bytes of 4 neighbouring blocks as one word; a block is PER lanes
-template <int PER>
-__device__ __forceinline__ uint32_t gather_scales(uint32_t byte) {
-    uint32_t word = byte << (8 * (threadIdx.x / PER % 4));
-    word |= __shfl_xor_sync(0xFFFFFFFFu, word, PER);
-    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2 * PER);
-    return word;
-}
-
 // One CTA a row, one thread 16 neighbouring elements at a time.  A thread's three groups are loaded together
 // and stay in registers between the row's maximum and the rounding, so a row of up to 48 elements a thread
 // is read once; only longer rows (above 24576 elements) are read a second time for the NV form.  Two and four
