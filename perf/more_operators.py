@@ -259,10 +259,11 @@ def _run_plain(s):
 def _run_own(s):
     op = s["op"]
     if op == "norm":
-        y, total = s["nm"].add_rms_norm(s["x"], s["residual"], s["weight"], EPS, s["offset"])
         if not s["train"]:
+            y, total = s["nm"].add_rms_norm(s["x"], s["residual"], s["weight"], EPS, s["offset"])
             return {"sum": total, "y": y}
-        dx, dw = s["nm"].add_rms_norm_backward(s["dy"], s["dsum"], total, s["weight"], EPS, s["offset"])
+        y, total, factors = s["nm"].add_rms_norm(s["x"], s["residual"], s["weight"], EPS, s["offset"], save=True)
+        dx, dw = s["nm"].add_rms_norm_backward(s["dy"], s["dsum"], total, factors, s["weight"], s["offset"])
         return {"sum": total, "y": y, "dx": dx, "dw": dw}
     if op == "norm8":
         q, total = s["nm"].add_rms_norm_fp8(s["x"], s["residual"], s["weight"], EPS, s["offset"])
