@@ -77,7 +77,8 @@ enum equarx_status {
     EQUARX_ERR_FLAVOUR = 10,   /* flavour is not a combination of EQUARX_FLAVOUR_* bits  */
     EQUARX_ERR_FORMAT = 11,    /* an element type, 4-bit format or activation is not one of
                                   those the feed-forward calls list                      */
-    EQUARX_ERR_TIMEOUT = 12    /* equarx_feedforward_check: a kernel gave up a wait      */
+    EQUARX_ERR_TIMEOUT = 12,   /* equarx_feedforward_check: a kernel gave up a wait      */
+    EQUARX_ERR_VALUE = 13      /* eps is negative or not finite, or an offset not finite */
 };
 
 /*
@@ -416,7 +417,7 @@ int equarx_ring_allreduce(const void *const *in_bf16, void *const *out_bf16,
  * with its own slices of the weights, and the AllReduce sums the partials (in the
  * backward pass it sums dx).  These calls compute that block: with 16-bit weights
  * and their gradients, and, for serving, with weights and activations in
- * microscaled 4-bit floating point.  (The paper has no counterpart for them.)
+ * microscaled 4-bit or 8-bit floating point.  (The paper has no counterpart for them.)
  *
  * Conventions, in addition to those at the top of this file
  *   - Matrices are row-major: element (r, c) of a matrix with row stride ld is at
@@ -434,7 +435,7 @@ int equarx_ring_allreduce(const void *const *in_bf16, void *const *out_bf16,
  *   - Outputs must not overlap inputs, the workspace or one another.  Matrices with the
  *     same row stride may lie side by side in the rows of one buffer (g and u, or h beside
  *     x); with different strides they must be apart from first to last element.
- *   - Workspaces and 4-bit buffers are 16-byte aligned.
+ *   - Workspaces and 4-bit and 8-bit buffers are 16-byte aligned.
  *   - The result does not depend on timing: sums are taken in a fixed order.
  */
 #define EQUARX_BF16 0
@@ -514,6 +515,46 @@ int equarx_fp4_gated(const void *x, int dtype, size_t ldx,
                      void *workspace, size_t workspace_bytes, equarx_stream_t stream);
 
 /*
+ * Microscaled 8-bit floating point.  An element is E4M3 (largest value 448), rounded to
+ * nearest, ties to the even code, saturating; 32 neighbouring elements of a row share a
+ * power of two, e = max(floor(log2 amax) - 8, -127) stored as the byte e + 127;
+ * code = rn(v / 2^e), value = code * 2^e.  A quantized matrix of rows x cols is two
+ * buffers, both 16-byte aligned:
+ *   codes  : rows x ceil(cols/32)*32 bytes; codes past the last column are 0
+ *   scales : the scale of row r and block b is at byte
+ *            (r/128 * ceil(cols/128) + b/4) * 512 + (r%32) * 16 + (r%128/32) * 4 + b%4;
+ *            blocks past the last column have scale byte 0, rows past the last are not
+ *            written
+ * The products' rules are those of the 4-bit ones: summed in fp32, rounded once.  x may
+ * come from equarx_fp8_quantize or, normalised, from equarx_add_rms_norm_fp8.
+ */
+size_t equarx_fp8_codes_bytes(size_t rows, size_t cols);
+size_t equarx_fp8_scales_bytes(size_t rows, size_t cols);
+
+/* x (rows x cols; BF16, FP16 or FP32) -> the two buffers above. */
+int equarx_fp8_quantize(const void *x, int dtype, size_t rows, size_t cols, size_t ld,
+                        uint8_t *codes, uint8_t *scales, equarx_stream_t stream);
+
+/* The values that the codes stand for, rounded once to `dtype` (BF16, FP16 or FP32). */
+int equarx_fp8_dequantize(const uint8_t *codes, const uint8_t *scales, size_t rows, size_t cols,
+                          void *out, int dtype, size_t ld, equarx_stream_t stream);
+
+/* out = a b^T: a is m x k, b is n x k, out is m x n (BF16, FP16 or FP32). */
+int equarx_fp8_matmul(const uint8_t *a_codes, const uint8_t *a_scales,
+                      const uint8_t *b_codes, const uint8_t *b_scales,
+                      size_t m, size_t n, size_t k, void *out, int dtype, size_t ld, equarx_stream_t stream);
+
+/*
+ * h = act(x Wg^T) * (x Wu^T): x is m x k, both weights f x k, h m x f (BF16 or FP16); one
+ * kernel.
+ */
+int equarx_fp8_gated(const uint8_t *x_codes, const uint8_t *x_scales,
+                     const uint8_t *g_codes, const uint8_t *g_scales,
+                     const uint8_t *u_codes, const uint8_t *u_scales,
+                     size_t m, size_t f, size_t k, int act, void *h, int dtype, size_t ldh,
+                     equarx_stream_t stream);
+
+/*
  * h = act(x Wg^T) * (x Wu^T) over 16-bit weights, in one kernel: x is m x k, wg and wu
  * are f x k, h is m x f, all of one type (BF16 or FP16).  g and u, both m x f with row
  * stride ldgu, receive the projections x Wg^T and x Wu^T for the backward call; both
@@ -549,6 +590,70 @@ int equarx_gated_backward(const void *dh, size_t lddh, const void *x, size_t ldx
                           int dtype, size_t m, size_t f, size_t k, int act,
                           void *dx, size_t lddx, void *dwg, size_t lddwg, void *dwu, size_t lddwu,
                           void *workspace, size_t workspace_bytes, equarx_stream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Between an AllReduce and the next block: the residual stream and its norm.
+ *
+ *     sum = x + residual, rounded to their type (BF16 or FP16)
+ *     r = fl(1 / sqrt(mean(sum^2) + eps)) for each row, v = fl(fl(sum r) fl(offset + weight))
+ *     y = v rounded to the type of x, or v as microscaled 8-bit rows
+ * with fl a rounding to fp32; the squares are added in fp64, so that v, and with it the
+ * 8-bit codes, do not depend on an order of addition.  offset is 0, or 1 for weights that
+ * are stored as differences from 1.  The conventions of the feed-forward calls above hold
+ * here too (rows, strides, element alignment, zero rows); in addition
+ *   - weight has `cols` elements, of the matrices' type or FP32 (weight_dtype).
+ *   - residual and sum are both NULL where there is nothing to add: y is the norm of x.
+ *   - sum may be x or residual itself (the same pointer and row stride): the residual
+ *     stream is then updated in place.
+ *   - eps is finite and not negative, offset finite, else EQUARX_ERR_VALUE.
+ *   - factors, where it is not NULL, receives r of each row for the backward call.
+ */
+int equarx_add_rms_norm(const void *x, size_t ldx, const void *residual, size_t ldr,
+                        const void *weight, int dtype, int weight_dtype, size_t rows, size_t cols,
+                        double eps, float offset, void *sum, size_t lds, void *y, size_t ldy,
+                        float *factors, equarx_stream_t stream);
+
+/* The same with v as the codes and scales of a rows x cols matrix of equarx_fp8_quantize. */
+int equarx_add_rms_norm_fp8(const void *x, size_t ldx, const void *residual, size_t ldr,
+                            const void *weight, int dtype, int weight_dtype, size_t rows, size_t cols,
+                            double eps, float offset, void *sum, size_t lds,
+                            uint8_t *codes, uint8_t *scales, equarx_stream_t stream);
+
+/*
+ * Gradients of equarx_add_rms_norm from those of y and of sum (dsum, which may be NULL).
+ * With n = sum r and g = dy (offset + weight) of a row:
+ *     dx = dsum + r (g - n mean(g n)),   dweight = sum over rows of dy n.
+ * dx is the gradient of x and of the residual alike; dweight has the weight's type and may
+ * be NULL, and then no workspace is needed.  Sums are taken in fp32 in a fixed order.
+ */
+size_t equarx_add_rms_norm_backward_workspace_bytes(size_t rows, size_t cols);
+int equarx_add_rms_norm_backward(const void *dy, size_t lddy, const void *dsum, size_t ldds,
+                                 const void *sum, size_t lds, const float *factors,
+                                 const void *weight, int dtype, int weight_dtype, size_t rows, size_t cols,
+                                 float offset, void *dx, size_t lddx, void *dweight,
+                                 void *workspace, size_t workspace_bytes, equarx_stream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection.
+ *
+ *     out_t = y_t + scale_i (x_t A_i^T) B_i^T,   i = index[t]
+ * y (tokens x n) is the projection of x (tokens x k) with the weights that all requests
+ * share, a (adapters x rank x k) and b (adapters x n x rank), both dense, hold the adapters,
+ * scale (adapters floats) may be NULL: 1.  A token whose index is not in [0, adapters) has no
+ * adapter: out_t = y_t.  Indexes are read on the device; tokens of one request need not be
+ * neighbours, but are cheapest so.  All matrices are of one type (BF16 or FP16); sums are in
+ * fp32, x_t A_i^T enters the second product with 16 bits or more, out is rounded once.  What is
+ * not finite in one adapter or token reaches no token of another adapter.  rank is 1 to 128;
+ * adapters of lower rank are padded with zeros.  out may be y itself.  Under tensor
+ * parallelism with k split over the ranks, a rank passes its columns of A, and the AllReduce
+ * of the outputs adds the adapters' parts too.
+ */
+int equarx_add_adapters(const void *y, size_t ldy, const void *x, size_t ldx,
+                        const void *a, const void *b, const int32_t *index, const float *scale,
+                        int dtype, size_t tokens, size_t n, size_t k, size_t rank, size_t adapters,
+                        void *out, size_t ldo, equarx_stream_t stream);
 
 /*
  * The kernels of the feed-forward calls wait only for copies and products of their own

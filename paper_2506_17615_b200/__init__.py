@@ -3,7 +3,9 @@ per-hop dequantize / fp32 add / requantize and all-gather dequantize of a ring
 AllReduce, simulated on one GPU over N ranks.  The work is done by
 hand-written sm_100a kernels behind a C ABI (include/equarx.h); this package
 is the thin binding.  ``workloads`` holds the seeded synthetic inputs,
-``feedforward`` the layer whose partial sums the AllReduce reduces, for torch tensors.
+``feedforward`` the layer whose partial sums the AllReduce reduces, ``norm`` the residual
+stream between the two and ``adapters`` low-rank adapters beside a projection, for torch
+tensors.
 
 The CUDA library is loaded (and, if stale, built) on the first access to one of
 the binding's names, not on ``import``: ``workloads`` draws random tensors only and
@@ -29,6 +31,11 @@ _BINDING_NAMES = (
     "EquarxError",
     "LIB_PATH",
     "MAX_RANKS",
+    "add_adapters",
+    "add_rms_norm",
+    "add_rms_norm_backward",
+    "add_rms_norm_backward_workspace_bytes",
+    "add_rms_norm_fp8",
     "ag_dequant",
     "allreduce_sim",
     "allreduce_sim_bf16",
@@ -52,6 +59,12 @@ _BINDING_NAMES = (
     "fp4_matmul",
     "fp4_quantize",
     "fp4_scales_bytes",
+    "fp8_codes_bytes",
+    "fp8_dequantize",
+    "fp8_gated",
+    "fp8_matmul",
+    "fp8_quantize",
+    "fp8_scales_bytes",
     "gated_backward",
     "gated_backward_workspace_bytes",
     "gated_forward",
@@ -72,6 +85,6 @@ __all__ = list(_BINDING_NAMES) + ["binding", "workloads"]
 def __getattr__(name):
     if name in _BINDING_NAMES:
         return getattr(importlib.import_module(".binding", __name__), name)
-    if name in ("binding", "workloads", "ring", "feedforward", "block"):
+    if name in ("binding", "workloads", "ring", "feedforward", "norm", "adapters", "block"):
         return importlib.import_module("." + name, __name__)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

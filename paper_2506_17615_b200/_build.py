@@ -8,9 +8,11 @@ import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
-SOURCES = [os.path.join(_CSRC, name) for name in ("equarx_host.cu", "feedforward_host.cu")]
+SOURCES = [os.path.join(_CSRC, name) for name in ("equarx_host.cu", "feedforward_host.cu", "norm_host.cu",
+                                                    "adapter_host.cu")]
 DEPENDS = SOURCES + [os.path.join(_CSRC, name) for name in ("equarx_kernels.cuh", "equarx_internal.h", "tensor_ops.cuh",
-                                                            "feedforward_kernels.cuh", "elements.cuh", "host_common.h")] + \
+                                                            "feedforward_kernels.cuh", "elements.cuh", "host_common.h",
+                                                            "norm_kernels.cuh", "adapter_kernels.cuh")] + \
     [os.path.join(os.path.dirname(_HERE), "include", "equarx.h")]
 LIB = os.path.join(_HERE, "libequarx.so")
 TORCH_SOURCE = os.path.join(_CSRC, "feedforward_torch.cpp")

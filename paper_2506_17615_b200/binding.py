@@ -11,7 +11,7 @@ from . import _build
 
 MAX_RANKS = 64
 (OK, ERR_NULL, ERR_NRANKS, ERR_BLOCK, ERR_COUNT, ERR_ALIGN, ERR_WORKSPACE, ERR_ALIAS, ERR_CUDA, ERR_STATIC_LIMIT,
- ERR_FLAVOUR, ERR_FORMAT, ERR_TIMEOUT) = range(13)
+ ERR_FLAVOUR, ERR_FORMAT, ERR_TIMEOUT, ERR_VALUE) = range(14)
 FLAVOUR_SEMI_LOOP, FLAVOUR_QUANT_RS, FLAVOUR_QUANT_AG, FLAVOUR_E4M3, FLAVOUR_E5M2 = 1, 2, 4, 8, 16
 BF16, FP16, FP32 = range(3)
 FP4_MX, FP4_NV = range(2)
@@ -51,6 +51,17 @@ EXPORTS = (
     "equarx_gated_forward_workspace_bytes",
     "equarx_gated_backward",
     "equarx_gated_backward_workspace_bytes",
+    "equarx_fp8_codes_bytes",
+    "equarx_fp8_scales_bytes",
+    "equarx_fp8_quantize",
+    "equarx_fp8_dequantize",
+    "equarx_fp8_matmul",
+    "equarx_fp8_gated",
+    "equarx_add_rms_norm",
+    "equarx_add_rms_norm_fp8",
+    "equarx_add_rms_norm_backward",
+    "equarx_add_rms_norm_backward_workspace_bytes",
+    "equarx_add_adapters",
     "equarx_feedforward_check",
     "equarx_status_string",
     "equarx_last_cuda_error",
@@ -104,6 +115,20 @@ def _load():
     lib.equarx_gated_backward_workspace_bytes.argtypes = [sz, sz, sz, vp, sz, vp, sz, vp, sz]
     lib.equarx_gated_backward.argtypes = [vp, sz, vp, sz, vp, sz, vp, sz, vp, vp, sz, ci, sz, sz, sz, ci, vp, sz, vp, sz,
                                           vp, sz, vp, sz, vp]
+    cd, cf = ctypes.c_double, ctypes.c_float
+    lib.equarx_fp8_codes_bytes.argtypes = [sz, sz]
+    lib.equarx_fp8_scales_bytes.argtypes = [sz, sz]
+    lib.equarx_fp8_quantize.argtypes = [vp, ci, sz, sz, sz, vp, vp, vp]
+    lib.equarx_fp8_dequantize.argtypes = [vp, vp, sz, sz, vp, ci, sz, vp]
+    lib.equarx_fp8_matmul.argtypes = [vp] * 4 + [sz, sz, sz, vp, ci, sz, vp]
+    lib.equarx_fp8_gated.argtypes = [vp] * 6 + [sz, sz, sz, ci, vp, ci, sz, vp]
+    lib.equarx_add_rms_norm.argtypes = [vp, sz, vp, sz, vp, ci, ci, sz, sz, cd, cf, vp, sz, vp, sz, vp, vp]
+    lib.equarx_add_rms_norm_fp8.argtypes = [vp, sz, vp, sz, vp, ci, ci, sz, sz, cd, cf, vp, sz, vp, vp, vp]
+    lib.equarx_add_rms_norm_backward_workspace_bytes.argtypes = [sz, sz]
+    lib.equarx_add_rms_norm_backward.argtypes = [vp, sz, vp, sz, vp, sz, vp, vp, ci, ci, sz, sz, cf, vp, sz, vp, vp, sz, vp]
+    lib.equarx_add_adapters.argtypes = [vp, sz, vp, sz, vp, vp, vp, vp, ci, sz, sz, sz, sz, sz, vp, sz, vp]
+    for name in ("fp8_codes_bytes", "fp8_scales_bytes", "add_rms_norm_backward_workspace_bytes"):
+        getattr(lib, "equarx_" + name).restype = sz
     for name in ("fp4_codes_bytes", "fp4_scales_bytes", "fp4_linear_workspace_bytes", "gated_forward_workspace_bytes",
                  "gated_backward_workspace_bytes"):
         getattr(lib, "equarx_" + name).restype = sz
@@ -323,6 +348,67 @@ def gated_backward(dh, lddh, x, ldx, wg, ldwg, wu, ldwu, g, u, ldgu, dtype, m, f
                                      dtype, m, f, k, act, _ptr(dx), lddx, _ptr(dwg), lddwg, _ptr(dwu), lddwu,
                                      _ptr(workspace), workspace_bytes, _ptr(stream)),
            "equarx_gated_backward")
+
+
+def fp8_codes_bytes(rows, cols):
+    return lib.equarx_fp8_codes_bytes(rows, cols)
+
+
+def fp8_scales_bytes(rows, cols):
+    return lib.equarx_fp8_scales_bytes(rows, cols)
+
+
+def fp8_quantize(x, dtype, rows, cols, ld, codes, scales, stream=0):
+    _check(lib.equarx_fp8_quantize(_ptr(x), dtype, rows, cols, ld, _ptr(codes), _ptr(scales), _ptr(stream)), "equarx_fp8_quantize")
+
+
+def fp8_dequantize(codes, scales, rows, cols, out, dtype, ld, stream=0):
+    _check(lib.equarx_fp8_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), dtype, ld, _ptr(stream)),
+           "equarx_fp8_dequantize")
+
+
+def fp8_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, stream=0):
+    _check(lib.equarx_fp8_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), m, n, k, _ptr(out), dtype, ld,
+                                 _ptr(stream)),
+           "equarx_fp8_matmul")
+
+
+def fp8_gated(x_codes, x_scales, g_codes, g_scales, u_codes, u_scales, m, f, k, act, h, dtype, ldh, stream=0):
+    _check(lib.equarx_fp8_gated(_ptr(x_codes), _ptr(x_scales), _ptr(g_codes), _ptr(g_scales), _ptr(u_codes), _ptr(u_scales), m, f, k,
+                                act, _ptr(h), dtype, ldh, _ptr(stream)),
+           "equarx_fp8_gated")
+
+
+# ---- the residual stream and adapters (paper_2506_17615_b200.norm and .adapters wrap these for torch tensors)
+
+def add_rms_norm(x, ldx, residual, ldr, weight, dtype, weight_dtype, rows, cols, eps, offset, sum, lds, y, ldy, factors=0, stream=0):
+    _check(lib.equarx_add_rms_norm(_ptr(x), ldx, _ptr(residual), ldr, _ptr(weight), dtype, weight_dtype, rows, cols, eps, offset,
+                                   _ptr(sum), lds, _ptr(y), ldy, _ptr(factors), _ptr(stream)),
+           "equarx_add_rms_norm")
+
+
+def add_rms_norm_fp8(x, ldx, residual, ldr, weight, dtype, weight_dtype, rows, cols, eps, offset, sum, lds, codes, scales, stream=0):
+    _check(lib.equarx_add_rms_norm_fp8(_ptr(x), ldx, _ptr(residual), ldr, _ptr(weight), dtype, weight_dtype, rows, cols, eps, offset,
+                                       _ptr(sum), lds, _ptr(codes), _ptr(scales), _ptr(stream)),
+           "equarx_add_rms_norm_fp8")
+
+
+def add_rms_norm_backward_workspace_bytes(rows, cols):
+    return lib.equarx_add_rms_norm_backward_workspace_bytes(rows, cols)
+
+
+def add_rms_norm_backward(dy, lddy, dsum, ldds, sum, lds, factors, weight, dtype, weight_dtype, rows, cols, offset, dx, lddx, dweight,
+                          workspace, workspace_bytes, stream=0):
+    _check(lib.equarx_add_rms_norm_backward(_ptr(dy), lddy, _ptr(dsum), ldds, _ptr(sum), lds, _ptr(factors), _ptr(weight), dtype,
+                                            weight_dtype, rows, cols, offset, _ptr(dx), lddx, _ptr(dweight), _ptr(workspace),
+                                            workspace_bytes, _ptr(stream)),
+           "equarx_add_rms_norm_backward")
+
+
+def add_adapters(y, ldy, x, ldx, a, b, index, scale, dtype, tokens, n, k, rank, adapters, out, ldo, stream=0):
+    _check(lib.equarx_add_adapters(_ptr(y), ldy, _ptr(x), ldx, _ptr(a), _ptr(b), _ptr(index), _ptr(scale), dtype, tokens, n, k, rank,
+                                   adapters, _ptr(out), ldo, _ptr(stream)),
+           "equarx_add_adapters")
 
 
 def feedforward_check():

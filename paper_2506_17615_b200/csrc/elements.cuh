@@ -68,6 +68,42 @@ __device__ __forceinline__ uint32_t gather_scales(uint32_t byte) {
     return word;
 }
 
+// ---------------------------------------------------------------- microscaled 8-bit floating point
+// 32 neighbouring elements of a row share e = max(floor(log2 amax) - 8, -127), the power of two that brings the largest
+// into [256, 512); code = e4m3_rn(v / 2^e), above 448 it saturates.  Every step but the rounding is exact.  An element
+// that is not finite makes its block's scale NaN.  Scales lie as in 4 bits: the one of row r and block b at byte
+// (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of the 512-byte tile (r / 128, b / 4), which is one 128-byte stage of codes.
+__host__ __device__ inline size_t fp8_stages(size_t cols) { return (cols + 127) / 128; }
+__host__ __device__ inline size_t fp8_stride(size_t cols) { return (cols + 31) / 32 * 32; }
+__host__ __device__ inline size_t fp8_scale_offset(size_t row, size_t block, size_t stages) {
+    return (row / 128 * stages + block / 4) * 512 + (row % 32) * 16 + (row % 128 / 32) * 4 + block % 4;
+}
+// a block's scale and what its elements are multiplied by, from its largest magnitude as fp32 bits
+__device__ __forceinline__ void fp8_block_scale(uint32_t amax, uint32_t& byte, float& inv) {
+    const int e = max(int(amax >> 23) - 8, 0);             // the stored byte: exponent + 127
+    byte = amax >= kInfBits ? 255u : uint32_t(e);
+    inv = amax >= kInfBits ? 0.0f : __uint_as_float(uint32_t(254 - e) << 23);
+}
+// two codes, the first in the low byte
+__device__ __forceinline__ uint32_t encode_e4m3(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float2 decode_e4m3(uint32_t codes) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(uint16_t(codes)));
+    return unpack2(h, kFp16);
+}
+__device__ __forceinline__ uint4 encode_e4m3(float (&v)[16], float inv) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) mul2(v[i], v[i + 1], inv);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = encode_e4m3(v[4 * i], v[4 * i + 1]) | encode_e4m3(v[4 * i + 2], v[4 * i + 3]) << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // ---------------------------------------------------------------- wide accesses
 // 256-bit accesses (sm_100): what is read once, or written and not read again here
 __device__ __forceinline__ void load_256(const void* p, uint32_t* w) {

@@ -271,6 +271,7 @@ const char* equarx_status_string(int status) {
             return "EQUARX_ERR_STATIC_LIMIT: problem needs more than the 16 MiB built-in workspace";
         case EQUARX_ERR_FORMAT: return "EQUARX_ERR_FORMAT: unknown element type, 4-bit format or activation";
         case EQUARX_ERR_TIMEOUT: return "EQUARX_ERR_TIMEOUT: a feed-forward kernel gave up a wait; its output is incomplete";
+        case EQUARX_ERR_VALUE: return "EQUARX_ERR_VALUE: eps is negative or not finite, or offset is not finite";
         default: return "EQUARX: unknown status";
     }
 }

@@ -16,6 +16,9 @@ constexpr size_t kSplitSmem = 224 * 1024;      // dynamic; the kernel's own vari
 inline bool is_format(int f) { return f == EQUARX_FP4_MX || f == EQUARX_FP4_NV; }
 inline size_t codes_stride(size_t cols) { return ceil_div(cols, 32) * 16; }
 inline size_t fp4_stages(size_t cols) { return ceil_div(cols, 256); }
+// bytes of a row of codes, and stages of the reduction axis, of a product's coded operands
+template <int KIND> inline size_t coded_stride(size_t cols) { return KIND == kMx8 ? fp8_stride(cols) : codes_stride(cols); }
+template <int KIND> inline size_t coded_stages(size_t cols) { return KIND == kMx8 ? fp8_stages(cols) : fp4_stages(cols); }
 
 // Clusters of 1 .. 8 CTAs that run at one time when each CTA has an SM to itself: a cluster stays inside a
 // GPC, so this is less than the number of SMs divided by the size.
@@ -82,10 +85,11 @@ int make_map(CUtensorMap& map, const void* base, size_t elem, size_t inner, size
     return r == CUDA_SUCCESS ? EQUARX_OK : cuda_failure(cudaErrorInvalidValue);
 }
 
-// scales of a 4-bit matrix as rows of 128 bytes, those of one 128-row group and one stage together
-int scale_map(CUtensorMap& map, const uint8_t* scales, size_t rows, size_t cols, int format) {
-    const size_t box_rows = (format == EQUARX_FP4_MX ? kScaleBytes<kMx> : kScaleBytes<kNv>) / 128;
-    return make_map(map, scales, 1, 128, ceil_div(rows, 128) * fp4_stages(cols) * box_rows, 128, box_rows,
+// scales of a coded matrix as rows of 128 bytes, those of one 128-row group and one stage together
+template <int KIND>
+int scale_map(CUtensorMap& map, const uint8_t* scales, size_t rows, size_t cols) {
+    const size_t box_rows = kScaleBytes<KIND> / 128;
+    return make_map(map, scales, 1, 128, ceil_div(rows, 128) * coded_stages<KIND>(cols) * box_rows, 128, box_rows,
                     CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
@@ -93,7 +97,8 @@ inline Out out_rows(void* p, size_t ld, int dtype) {
     return Out{p, ld, dtype, unit_of(p, ld, size_of(dtype))};
 }
 
-// ---------------------------------------------------------------- 4-bit matrices
+// ---------------------------------------------------------------- 4- and 8-bit matrices
+// (8 bits: without row_scales)
 struct Fp4 {
     const uint8_t *codes, *scales;
     const float* row_scales;
@@ -114,6 +119,14 @@ inline Span scales_span(const Fp4& q, size_t rows, size_t cols, int format) {
 inline Span rows_span(const Fp4& q, size_t rows, int format) {
     return Span{format == EQUARX_FP4_NV ? q.row_scales : nullptr, rows * sizeof(float)};
 }
+
+inline size_t fp8_scale_bytes(size_t rows, size_t cols) { return ceil_div(rows, 128) * fp8_stages(cols) * kScaleBytes<kMx8>; }
+int check_fp8(const Fp4& q) {
+    if (!q.codes || !q.scales) return EQUARX_ERR_NULL;
+    return aligned(q.codes, 16) && aligned(q.scales, 16) ? EQUARX_OK : EQUARX_ERR_ALIGN;
+}
+inline Span fp8_codes_span(const Fp4& q, size_t rows, size_t cols) { return Span{q.codes, rows * fp8_stride(cols)}; }
+inline Span fp8_scales_span(const Fp4& q, size_t rows, size_t cols) { return Span{q.scales, fp8_scale_bytes(rows, cols)}; }
 
 // threads of a row's CTA: three groups of 16 elements each, a whole number of warps
 inline int row_threads(size_t cols) { return int(std::min<size_t>(512, up(ceil_div(cols, 16 * kRowChunks), 32))); }
@@ -271,24 +284,25 @@ int launch_split(SplitArgs& a, const SplitPlan& plan, size_t features, size_t to
 // weights of the transposed kernel
 template <int KIND, int MODE>
 int split_weights(SplitArgs& a, const Fp4* w, size_t n, size_t k) {
-    const size_t stride = codes_stride(k);
+    const size_t stride = coded_stride<KIND>(k);
     for (int i = 0; i < (MODE == kGated ? 2 : 1); ++i) {
         TRY(make_map(a.w[i], w[i].codes, 1, stride, n, stride, kRowsM));
         a.scales_w[i] = w[i].scales;
         a.row_w[i] = w[i].row_scales;
     }
-    a.stages = int(fp4_stages(k));
+    a.stages = int(coded_stages<KIND>(k));
     return EQUARX_OK;
 }
 
+// a product of coded matrices, with one or two weights
 template <int KIND, int MODE>
-int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, cudaStream_t stream) {
-    const size_t stride = codes_stride(k);
+int coded_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, cudaStream_t stream) {
+    const size_t stride = coded_stride<KIND>(k);
     int sms;
     TRY(current_device(sms));
-    const TilePlan tiles = plan_tiles(ceil_div(m, kTileM), n, fp4_stages(k), MODE == kGated, true, sms);
+    const TilePlan tiles = plan_tiles(ceil_div(m, kTileM), n, coded_stages<KIND>(k), MODE == kGated, true, sms);
     SplitPlan split;
-    TRY((plan_split<KIND, MODE, false>(split, n, m, int(fp4_stages(k)))));
+    TRY((plan_split<KIND, MODE, false>(split, n, m, int(coded_stages<KIND>(k)))));
     if (split.cost < tiles.cost) {
         SplitArgs a = {};
         TRY((split_weights<KIND, MODE>(a, w, n, k)));
@@ -301,17 +315,16 @@ int fp4_product(const Fp4& x, const Fp4* w, size_t m, size_t n, size_t k, int ac
     }
     TileArgs<MODE> a = {};
     Product& g = a.product[0];
-    const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
     TRY(make_map(g.a[0], x.codes, 1, stride, m, stride, kRowsM));
-    TRY(scale_map(a.scales_a, x.scales, m, k, format));
+    TRY(scale_map<KIND>(a.scales_a, x.scales, m, k));
     a.row_a = x.row_scales;
     for (int i = 0; i < (MODE == kGated ? 2 : 1); ++i) {
         TRY(make_map(g.b[i], w[i].codes, 1, stride, n, stride, tiles.bn / 2));
-        TRY(scale_map(a.scales_b[i], w[i].scales, n, k, format));
+        TRY(scale_map<KIND>(a.scales_b[i], w[i].scales, n, k));
         a.row_b[i] = w[i].row_scales;
     }
     g.out[0] = out;
-    g.stages = int(fp4_stages(k));
+    g.stages = int(coded_stages<KIND>(k));
     g.parts = 1;
     a.act = act;
     TRY(finish_product(g, tiles, m, n, MODE == kGated));
@@ -356,7 +369,7 @@ int quantized_product(const QuantArgs& x, const Fp4* w, size_t m, size_t n, size
     }
     const Fp4 q = carve(workspace, m, k, format);
     TRY(quantize(x.x, x.dtype, m, k, x.ld, format, q, stream));
-    return fp4_product<KIND, MODE>(q, w, m, n, k, act, out, stream);
+    return coded_product<KIND, MODE>(q, w, m, n, k, act, out, stream);
 }
 
 // ---------------------------------------------------------------- 16-bit operands
@@ -467,8 +480,8 @@ int equarx_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const flo
                        scales_span(b, n, k, format), rows_span(b, n, format)},
                       {matrix(out, m, n, ld, size_of(dtype))}));
     const Out o = out_rows(out, ld, dtype);
-    return format == EQUARX_FP4_MX ? fp4_product<kMx, kPlain>(a, &b, m, n, k, 0, o, stream)
-                                   : fp4_product<kNv, kPlain>(a, &b, m, n, k, 0, o, stream);
+    return format == EQUARX_FP4_MX ? coded_product<kMx, kPlain>(a, &b, m, n, k, 0, o, stream)
+                                   : coded_product<kNv, kPlain>(a, &b, m, n, k, 0, o, stream);
 }
 
 size_t equarx_fp4_linear_workspace_bytes(size_t m, size_t k, int format) {
@@ -517,6 +530,94 @@ int equarx_fp4_gated(const void* x, int dtype, size_t ldx, const uint8_t* g_code
     const Out o = out_rows(h, ldh, dtype);
     return format == EQUARX_FP4_MX ? quantized_product<kMx, kGated>(a, w, m, f, k, act, o, workspace, stream)
                                    : quantized_product<kNv, kGated>(a, w, m, f, k, act, o, workspace, stream);
+}
+
+size_t equarx_fp8_codes_bytes(size_t rows, size_t cols) {
+    return rows > kMaxDim || bad_dim(cols) ? 0 : rows * fp8_stride(cols);
+}
+
+size_t equarx_fp8_scales_bytes(size_t rows, size_t cols) {
+    return rows > kMaxDim || bad_dim(cols) ? 0 : fp8_scale_bytes(rows, cols);
+}
+
+int equarx_fp8_quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, uint8_t* codes, uint8_t* scales,
+                        equarx_stream_t stream) {
+    if (!is_float(dtype)) return EQUARX_ERR_FORMAT;
+    if (rows > kMaxDim || bad_dim(cols) || bad_ld(ld, cols)) return EQUARX_ERR_COUNT;
+    if (rows == 0) return EQUARX_OK;
+    const Fp4 q{codes, scales, nullptr};
+    if (!x) return EQUARX_ERR_NULL;
+    TRY(check_fp8(q));
+    if (!aligned(x, size_of(dtype))) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({matrix(x, rows, cols, ld, size_of(dtype))}, {fp8_codes_span(q, rows, cols), fp8_scales_span(q, rows, cols)}));
+    QuantArgs a = rows_to_quantize(x, dtype, rows, cols, ld);
+    a.codes = codes;
+    a.scales = scales;
+    const dim3 grid(a.rows);
+    const int threads = row_threads(cols);
+    const bool anywhere = a.unit < 16;
+    if (dtype == EQUARX_BF16)
+        return launch(anywhere ? fp8_quantize_kernel<kBf16, true> : fp8_quantize_kernel<kBf16, false>, grid, threads, 0, 1, a, stream);
+    if (dtype == EQUARX_FP16)
+        return launch(anywhere ? fp8_quantize_kernel<kFp16, true> : fp8_quantize_kernel<kFp16, false>, grid, threads, 0, 1, a, stream);
+    return launch(anywhere ? fp8_quantize_kernel<kFp32, true> : fp8_quantize_kernel<kFp32, false>, grid, threads, 0, 1, a, stream);
+}
+
+int equarx_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, size_t rows, size_t cols, void* out, int dtype, size_t ld,
+                          equarx_stream_t stream) {
+    if (!is_float(dtype)) return EQUARX_ERR_FORMAT;
+    if (rows > kMaxDim || bad_dim(cols) || bad_ld(ld, cols)) return EQUARX_ERR_COUNT;
+    if (rows == 0) return EQUARX_OK;
+    const Fp4 q{codes, scales, nullptr};
+    if (!out) return EQUARX_ERR_NULL;
+    TRY(check_fp8(q));
+    if (!aligned(out, size_of(dtype))) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({fp8_codes_span(q, rows, cols), fp8_scales_span(q, rows, cols)}, {matrix(out, rows, cols, ld, size_of(dtype))}));
+    DequantArgs a = {};
+    a.codes = codes;
+    a.scales = scales;
+    a.out = out;
+    a.ld = ld;
+    a.rows = int(rows);
+    a.cols = int(cols);
+    a.dtype = dtype;
+    a.unit = unit_of(out, ld, size_of(dtype));
+    // narrow stores: a quarter of a row's elements or pairs at a time
+    const int threads = a.unit < 16 ? row_threads(4 * cols) : row_threads(cols);
+    return launch(fp8_dequantize_kernel, dim3(a.rows), threads, 0, 1, a, stream);
+}
+
+int equarx_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, size_t m,
+                      size_t n, size_t k, void* out, int dtype, size_t ld, equarx_stream_t stream) {
+    if (!is_float(dtype)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(n) || bad_dim(k) || bad_ld(ld, n)) return EQUARX_ERR_COUNT;
+    if (m == 0) return EQUARX_OK;
+    const Fp4 a{a_codes, a_scales, nullptr}, b{b_codes, b_scales, nullptr};
+    if (!out) return EQUARX_ERR_NULL;
+    TRY(check_fp8(a));
+    TRY(check_fp8(b));
+    if (!aligned(out, size_of(dtype))) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({fp8_codes_span(a, m, k), fp8_scales_span(a, m, k), fp8_codes_span(b, n, k), fp8_scales_span(b, n, k)},
+                      {matrix(out, m, n, ld, size_of(dtype))}));
+    return coded_product<kMx8, kPlain>(a, &b, m, n, k, 0, out_rows(out, ld, dtype), stream);
+}
+
+int equarx_fp8_gated(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* g_codes, const uint8_t* g_scales,
+                     const uint8_t* u_codes, const uint8_t* u_scales, size_t m, size_t f, size_t k, int act, void* h, int dtype,
+                     size_t ldh, equarx_stream_t stream) {
+    if (!is_16bit(dtype) || !is_act(act)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(f) || bad_dim(k) || bad_ld(ldh, f)) return EQUARX_ERR_COUNT;
+    if (m == 0) return EQUARX_OK;
+    const Fp4 x{x_codes, x_scales, nullptr}, w[2] = {{g_codes, g_scales, nullptr}, {u_codes, u_scales, nullptr}};
+    if (!h) return EQUARX_ERR_NULL;
+    TRY(check_fp8(x));
+    TRY(check_fp8(w[0]));
+    TRY(check_fp8(w[1]));
+    if (!aligned(h, 2)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({fp8_codes_span(x, m, k), fp8_scales_span(x, m, k), fp8_codes_span(w[0], f, k), fp8_scales_span(w[0], f, k),
+                       fp8_codes_span(w[1], f, k), fp8_scales_span(w[1], f, k)},
+                      {matrix(h, m, f, ldh, 2)}));
+    return coded_product<kMx8, kGated>(x, w, m, f, k, act, out_rows(h, ldh, dtype), stream);
 }
 
 size_t equarx_gated_forward_workspace_bytes(size_t m, size_t f, size_t k, const void* x, size_t ldx, const void* wg, size_t ldwg,

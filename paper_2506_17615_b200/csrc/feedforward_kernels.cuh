@@ -1,13 +1,13 @@
 // Kernels of the tensor-parallel feed-forward block whose partial sums the AllReduce reduces:
-// products and gated products of 16-bit and of microscaled 4-bit operands, their gradients, and the
-// 4-bit quantiser.
+// products and gated products of 16-bit and of microscaled 4- and 8-bit operands, their gradients, and the
+// quantisers.
 //
 //   tile_kernel       persistent 256 x bn output tiles on the tensor cores of two SMs
 //   split_kernel      few tokens: weights on the 128-row side, the reduction split over a cluster
 //   gate_grad_kernel  gradients of the two projections from dh, g and u
 //   grad_range_kernel the same scaled, where fp16 cannot hold them
 //   pack_kernel       rows that TMA cannot read (a stride that is no multiple of 16 bytes) -> rows it can
-//   fp4_quantize_kernel, fp4_dequantize_kernel
+//   fp4_quantize_kernel, fp4_dequantize_kernel, fp8_quantize_kernel, fp8_dequantize_kernel
 #pragma once
 #include <type_traits>
 
@@ -19,18 +19,19 @@ namespace ff {
 
 using namespace tc;
 
-enum Kind { kHalf = 0, kMx = 1, kNv = 2 };                 // 16-bit operands, 4-bit with either scale format
+// 16-bit operands, 4-bit with either scale format, 8-bit
+enum Kind { kHalf = 0, kMx = 1, kNv = 2, kMx8 = 3 };
 // what a product kernel computes; the gradients are kGrads in tiles, kSum2 (dx) and kOut2 (dWg, dWu) transposed
 enum Mode { kPlain = 0, kGated = 1, kSum2 = 2, kOut2 = 3, kGrads = 4 };
 enum Act { kSilu = 0, kGeluTanh = 1 };
 
 constexpr int kRowsM = 128;               // rows of a tile: lanes of tensor memory
-constexpr int kRowBytes = 128;            // one stage of the reduction axis: 64 16-bit or 256 4-bit elements
+constexpr int kRowBytes = 128;            // one stage of the reduction axis: 64 16-bit, 128 8-bit or 256 4-bit elements
 constexpr int kTileBytes = kRowsM * kRowBytes;
 constexpr int kChunkBytes = 64 * kRowBytes;   // MN-major operands: 64 elements x 64 steps of the reduction
 
 // scales of 128 rows for one stage: 512-byte tiles of 128 rows x 4 scales
-template <int KIND> constexpr int kScaleTiles = KIND == kNv ? 4 : KIND == kMx ? 2 : 0;
+template <int KIND> constexpr int kScaleTiles = KIND == kNv ? 4 : KIND == kMx ? 2 : KIND == kMx8 ? 1 : 0;
 template <int KIND> constexpr int kScaleBytes = 512 * kScaleTiles<KIND>;
 
 // ---------------------------------------------------------------- activation
@@ -213,7 +214,8 @@ constexpr int kSmemSlack = 1024;          // 128-byte swizzle atoms start on mul
 constexpr int kStaging = kEpilogueWarps * 2 * kStageOut;
 template <int KIND> constexpr int kTileSmem = kPipe<KIND> * kStageBytes<KIND> + kStaging + kSmemSlack;
 // an SM has 227 KB; a kernel's own variables take up to 512 bytes, the column factors of NV 2048 more
-static_assert(kTileSmem<kHalf> + 512 <= 227 * 1024 && kTileSmem<kMx> + 512 <= 227 * 1024 && kTileSmem<kNv> + 2560 <= 227 * 1024);
+static_assert(kTileSmem<kHalf> + 512 <= 227 * 1024 && kTileSmem<kMx> + 512 <= 227 * 1024 && kTileSmem<kNv> + 2560 <= 227 * 1024 &&
+              kTileSmem<kMx8> + 512 <= 227 * 1024);
 
 // tile t in an order that walks `group` row tiles before the next column tile: the tiles that run at
 // one time share operands in L2
@@ -248,9 +250,9 @@ template <int KIND, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 1)
     tile_kernel(const __grid_constant__ TileArgs<MODE> p) {
     constexpr bool B_MN = MODE == kGrads;
-    constexpr bool FP4 = KIND != kHalf;
+    constexpr bool SCALED = KIND != kHalf;
     constexpr int PIPE = kPipe<KIND>, STAGE = kStageBytes<KIND>, SB = kScaleBytes<KIND>;
-    constexpr uint32_t kSecond = FP4 ? 192 : 256;       // first column of the second accumulator
+    constexpr uint32_t kSecond = SCALED ? 192 : 256;       // first column of the second accumulator
     constexpr uint32_t kScaleCol = 448;                 // scales of a, then of b
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[2 * PIPE + 5];
@@ -312,7 +314,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
             const int half = g.bn / 2;                     // columns of b in each CTA
             const int n0 = MODE == kGated ? nt * half : nt * g.bn + rank * half;
             uint32_t bytes = 2 * kTileBytes + 2 * (B_MN ? (half + 63) / 64 * kChunkBytes : half * kRowBytes);
-            if (FP4) {
+            if (SCALED) {
                 const int width = MODE == kGated ? half : g.bn;
                 const int groups_a = (g.m + 127) / 128, nb = min(width / 128, (g.n + 127) / 128 - nt * width / 128);
                 bytes += SB * (min(2, groups_a - mt * 2) + 2 * nb * (MODE == kGated ? 2 : 1));
@@ -323,7 +325,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                 const CUtensorMap* const mb = &g.b[MODE == kGated ? rank : part];
                 const bool a_mn = MODE == kGrads && g.a_mn;
                 int kc = 0;
-                for (int s = 0; s < g.stages; ++s, kc += FP4 ? kRowBytes : 64) {      // 4-bit codes travel as bytes
+                for (int s = 0; s < g.stages; ++s, kc += SCALED ? kRowBytes : 64) {      // 4-bit codes travel as bytes
                     if (!(ok = barrier_wait_warp(empty + 8 * slot, phase, &abort))) break;
                     const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, bar = counted + 8 * slot;
                     if (rank == 0) barrier_expect_warp(full + 8 * slot, bytes);
@@ -362,7 +364,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
             for (uint32_t i = issued > PIPE ? issued - PIPE : 0; i < issued; ++i)
                 barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
         __syncwarp();
-    } else if (FP4 && warp == kEpilogueWarps + 2) {
+    } else if (SCALED && warp == kEpilogueWarps + 2) {
         // ---------------------------------------------------- loads of the scales, counted with those
         const uint32_t counted = peer_addr(full, 0);
         uint32_t slot = 0, phase = 1;
@@ -401,12 +403,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                 const Product& g = p.product[MODE == kGrads && t >= first];
                 const int stages = g.stages * (MODE == kGrads ? g.parts : 1);
                 const bool a_mn = MODE == kGrads && g.a_mn;
-                const uint32_t idesc = FP4 ? 0 : desc_16bit(p.bf16, a_mn, B_MN, kTileM, g.bn);
+                const uint32_t idesc = SCALED ? 0 : desc_16bit(p.bf16, a_mn, B_MN, kTileM, g.bn);
                 for (int s = 0; s < stages; ++s) {
                     if (!(ok = barrier_wait_warp(full + 8 * slot, phase, &abort))) break;
                     fence_after();
                     const uint32_t sa = smem + slot * STAGE, sb = sa + kTileBytes, ss = sb + kTileBytes;
-                    if (FP4) {
+                    if (SCALED) {
 #pragma unroll
                         for (int j = 0; j < kScaleTiles<KIND>; ++j) {
                             copy_scales<2>(ta + 4 * j, ss + 512 * j);
@@ -417,7 +419,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                     if (s == 0) {
                         // 4 bits: the tile before has given up the columns that both accumulators use; 16 bits: the
                         // tile before that has given up this accumulator
-                        if (FP4) {
+                        if (SCALED) {
                             if (local && !(ok = barrier_wait_warp<true>(drained, (local - 1) & 1, &abort))) break;
                         } else {
                             if (local > 1 && !(ok = barrier_wait_warp<true>(drained + 8 * buf, (local / 2 - 1) & 1, &abort))) break;
@@ -430,7 +432,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                                                  : swizzled_desc(sa + 32 * kk, 16);
                         const uint32_t db = B_MN ? swizzled_desc(sb + 2048 * kk, kChunkBytes)
                                                  : swizzled_desc(sb + 32 * kk, 16);
-                        if constexpr (FP4) {
+                        if constexpr (KIND == kMx8) {
+                            mma_fp8<2>(d, da, db, desc_fp8(kTileM, g.bn, kk), ta, tb, s | kk);
+                        } else if constexpr (SCALED) {
                             const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
                             mma_fp4<2, KIND == kMx>(d, da, db, desc_fp4(KIND == kMx, kTileM, g.bn, which), ta + 4 * j,
                                                     tb + 8 * j, s | kk);
@@ -474,7 +478,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
             const int units = width / 32;                  // blocks of 32 output columns
             const int row0 = m0 + quarter * 32, n0 = nt * width;
             const uint32_t buf = local & 1, acc = tmem + buf * kSecond + (uint32_t(quarter * 32) << 16);
-            const uint32_t done = peer_addr(FP4 ? drained : drained + 8 * buf, 0);
+            const uint32_t done = peer_addr(SCALED ? drained : drained + 8 * buf, 0);
             float ra = 1.0f;
             const int steps = (units + 1) / 2;
             // the shared columns are the last of the first accumulator and the first of the second
@@ -495,7 +499,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
             if (!barrier_wait_warp(ready + 8 * buf, local / 2 & 1, &abort, limit)) break;
             fence_after();
 #pragma unroll
-            for (int i = 0; i < 4 / (FP4 ? SETS : 1); ++i) {
+            for (int i = 0; i < 4 / (SCALED ? SETS : 1); ++i) {
                 if (i >= steps) break;
                 __syncwarp();
                 const int u = unit_of_step(i);
@@ -506,7 +510,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
                     if (MODE == kGated) tmem_load32(acc + half + 32 * u, q);
                     tmem_wait_loads();
                 }
-                if (i == (FP4 ? 0 : steps - 1)) {
+                if (i == (SCALED ? 0 : steps - 1)) {
                     fence_before();
                     __syncwarp();
                     if (lane == 0) barrier_arrive_pair(done);
@@ -1113,6 +1117,117 @@ __global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_consta
     }
 }
 
+// ---------------------------------------------------------------- microscaled 8-bit floating point
+// One CTA a row, a thread three groups of 16 neighbouring elements at a time, loaded together; two threads are a block.
+// ANYWHERE as above.
+template <int DT, bool ANYWHERE>
+__global__ void __launch_bounds__(512) fp8_quantize_kernel(const __grid_constant__ QuantArgs p) {
+    const int tid = threadIdx.x, threads = blockDim.x;
+    const size_t row = blockIdx.x, stages = fp8_stages(p.cols), stride = fp8_stride(p.cols);
+    const int padded = int(stages * 128);
+    uint8_t* const codes = p.codes + row * stride;
+    uint8_t* const scales = p.scales + fp8_scale_offset(row, 0, stages);
+    grid_launch();
+    grid_wait();
+    for (int first = tid * 16; first - tid * 16 < padded; first += threads * 16 * kRowChunks) {
+        Group<DT> x[kRowChunks];
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + c * threads * 16;
+            if constexpr (ANYWHERE) load_shifted<DT>(p, row, col, x[c]);
+            else load_group<DT, false>(p, row, col, x[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + c * threads * 16;
+            uint32_t m = group_amax<DT>(x[c]), byte;
+            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+            float inv, v[16];
+            fp8_block_scale(m, byte, inv);
+            group_values<DT>(x[c], v);
+            const uint4 code = encode_e4m3(v, inv);
+            if (col < int(stride)) *reinterpret_cast<uint4*>(codes + col) = code;
+            const uint32_t word = gather_scales<2>(byte);
+            if (tid % 8 == 0 && col < padded) *reinterpret_cast<uint32_t*>(scales + size_t(col / 128) * 512) = word;
+        }
+    }
+}
+
+// value = code * scale in fp32, rounded once to the output type.  One CTA a row; a thread takes 16 neighbouring elements
+// where output rows start on multiples of 16 bytes, else (NARROW) two where they do on multiples of a pair, or one, the
+// next thread the next ones, so that a warp's stores are whole sectors anyway.
+template <int NARROW>
+__device__ __forceinline__ void fp8_dequantize_narrow(const DequantArgs& p, size_t row, const uint8_t* codes, const uint8_t* scales) {
+    for (int col = threadIdx.x * NARROW; col < p.cols; col += blockDim.x * NARROW) {
+        const float d = from_e8m0(scales[size_t(col / 128) * 512 + col / 32 % 4]);
+        const float2 v = decode_e4m3(NARROW == 2 ? *reinterpret_cast<const uint16_t*>(codes + col) : codes[col]);
+        const size_t at = row * p.ld + col;
+        const float a = __fmul_rn(v.x, d), b = __fmul_rn(v.y, d);
+        if (NARROW == 1 || col + 1 >= p.cols) store1(p.out, at, a, p.dtype);
+        else if (p.dtype == kFp32) *reinterpret_cast<float2*>(static_cast<float*>(p.out) + at) = make_float2(a, b);
+        else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at) = pack2(a, b, p.dtype);
+    }
+}
+__global__ void __launch_bounds__(512) fp8_dequantize_kernel(const __grid_constant__ DequantArgs p) {
+    const int tid = threadIdx.x, threads = blockDim.x;
+    const size_t row = blockIdx.x;
+    const uint8_t* const codes = p.codes + row * fp8_stride(p.cols);
+    const uint8_t* const scales = p.scales + fp8_scale_offset(row, 0, fp8_stages(p.cols));
+    grid_launch();
+    grid_wait();
+    if (p.unit < 16) {
+        if (p.unit >= (p.dtype == kFp32 ? 8 : 4)) fp8_dequantize_narrow<2>(p, row, codes, scales);
+        else fp8_dequantize_narrow<1>(p, row, codes, scales);
+        return;
+    }
+    for (int first = tid * 16; first < p.cols; first += threads * 16 * kRowChunks) {
+        uint4 w[kRowChunks];
+        uint32_t b[kRowChunks];
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + c * threads * 16;
+            if (col >= p.cols) continue;
+            w[c] = *reinterpret_cast<const uint4*>(codes + col);
+            b[c] = scales[size_t(col / 128) * 512 + col / 32 % 4];
+        }
+#pragma unroll
+        for (int c = 0; c < kRowChunks; ++c) {
+            const int col = first + c * threads * 16;
+            if (col >= p.cols) continue;
+            const float d = from_e8m0(b[c]);
+            const uint32_t word[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 f = decode_e4m3(word[j / 2] >> (j & 1) * 16);
+                v[2 * j] = __fmul_rn(f.x, d);
+                v[2 * j + 1] = __fmul_rn(f.y, d);
+            }
+            const size_t at = row * p.ld + col;
+            if (col + 16 > p.cols) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (col + j < p.cols) store1(p.out, at + j, v[j], p.dtype);
+            } else if (p.dtype == kFp32) {
+                float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.out) + at);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            } else {
+                uint32_t o[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = pack2(v[2 * j], v[2 * j + 1], p.dtype);
+                if (p.unit == 32) {
+                    store_256(static_cast<uint16_t*>(p.out) + at, o);
+                } else {
+                    uint4* q = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at);
+                    q[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                    q[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------- few tokens
 struct SplitArgs {
     CUtensorMap w[2], x[2];
@@ -1151,10 +1266,12 @@ __host__ __device__ constexpr int split_part_bytes(int nt, int ranks) {
 constexpr int kSmemOfSm = 228 * 1024, kSmemOfCta = 1024;      // of an SM; what every CTA costs beside its own
 constexpr int kLeastSplitSmem = split_stage_bytes<kHalf, kPlain>(16) + split_part_bytes<kPlain>(16, 1) + kSmemSlack;
 static_assert(split_stage_bytes<kMx, kPlain>(16) >= split_stage_bytes<kHalf, kPlain>(16) &&
+              split_stage_bytes<kMx8, kPlain>(16) >= split_stage_bytes<kHalf, kPlain>(16) &&
               split_part_bytes<kPlain>(16, 8) >= split_part_bytes<kPlain>(16, 1));
 static_assert(kTileSmem<kHalf> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
               kTileSmem<kMx> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
-              kTileSmem<kNv> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm);
+              kTileSmem<kNv> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
+              kTileSmem<kMx8> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm);
 
 // The output transposed: 128 features x nt tokens, so that a single token costs one narrow product over
 // each weight tile instead of a 256-row one, and the weights, which are all the bytes there are, are
@@ -1177,7 +1294,7 @@ static_assert(kTileSmem<kHalf> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
 // and a round trip of x.
 template <int KIND, int MODE, bool W_MN, bool X_MN, bool FUSED>
 __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_constant__ SplitArgs p) {
-    constexpr bool FP4 = KIND != kHalf, MX = KIND == kMx;
+    constexpr bool SCALED = KIND != kHalf, MX = KIND == kMx;
     constexpr int SB = kScaleBytes<KIND>, NW = MODE == kGated ? 2 : 1;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[2 * kSplitMaxPipe + 2];
@@ -1231,8 +1348,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         const int slot = it % p.pipe, s = s0 + it;
         const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb, bar = full + 8 * slot;
         const int second = MODE == kSum2 ? s >= p.stages : 0, ks = s - second * p.stages;
-        const int kc = FP4 ? ks * kRowBytes : ks * 64;
-        barrier_expect_warp(bar, NW * kTileBytes + (FUSED ? 0 : xb) + (FP4 ? (NW + (FUSED ? 0 : 1)) * SB : 0));
+        const int kc = SCALED ? ks * kRowBytes : ks * 64;
+        barrier_expect_warp(bar, NW * kTileBytes + (FUSED ? 0 : xb) + (SCALED ? (NW + (FUSED ? 0 : 1)) * SB : 0));
         for (int q = 0; q < NW; ++q) {
             const CUtensorMap* mw = &p.w[MODE == kSum2 ? second : q];
             if (W_MN) {
@@ -1241,7 +1358,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             } else {
                 tma_load_2d(sw + q * kTileBytes, mw, kc, f0, bar);
             }
-            if (FP4) bulk_load(ss + SB * q, p.scales_w[q] + (size_t(f0 / 128) * p.stages + ks) * SB, SB, bar);
+            if (SCALED) bulk_load(ss + SB * q, p.scales_w[q] + (size_t(f0 / 128) * p.stages + ks) * SB, SB, bar);
         }
         if (!FUSED) {
             if (X_MN) {
@@ -1249,7 +1366,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             } else {
                 tma_load_2d(sx, &p.x[second], kc, t0, bar);
             }
-            if (FP4) bulk_load(ss + SB * NW, p.scales_x + (size_t(t0 / 128) * p.stages + ks) * SB, SB, bar);
+            if (SCALED) bulk_load(ss + SB * NW, p.scales_x + (size_t(t0 / 128) * p.stages + ks) * SB, SB, bar);
         }
     };
     grid_begin(p.order);
@@ -1337,7 +1454,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             if (!(ok = barrier_wait_warp(full + 8 * slot, it / p.pipe & 1, &abort))) break;
             fence_after();
             const uint32_t sw = smem + slot * STAGE, sx = sw + NW * kTileBytes, ss = sx + xb;
-            if (FP4) {
+            if (SCALED) {
 #pragma unroll
                 for (int j = 0; j < kScaleTiles<KIND>; ++j) {
 #pragma unroll
@@ -1353,7 +1470,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
                 for (int q = 0; q < NW; ++q) {
                     const uint32_t a = sw + q * kTileBytes;
                     const uint32_t dw = W_MN ? swizzled_desc(a + 2048 * kk, kChunkBytes) : swizzled_desc(a + 32 * kk, 16);
-                    if constexpr (FP4) {
+                    if constexpr (KIND == kMx8) {
+                        mma_fp8<1>(tmem + q * p.nt, dw, dx, desc_fp8(128, p.nt, kk), tw + 4 * q, tx, it | kk);
+                    } else if constexpr (SCALED) {
                         const int j = KIND == kNv ? kk : kk / 2, which = KIND == kNv ? 0 : (kk & 1) * 2;
                         mma_fp4<1, MX>(tmem + q * p.nt, dw, dx, desc_fp4(MX, 128, p.nt, which),
                                        tw + (q * kScaleTiles<KIND> + j) * 4, tx + 4 * j, it | kk);

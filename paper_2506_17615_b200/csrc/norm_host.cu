@@ -1,0 +1,210 @@
+// C ABI of the residual addition with RMS norm (include/equarx.h): argument checks, launches.
+#include <cmath>
+
+#include "host_common.h"
+#include "norm_kernels.cuh"
+
+namespace {
+
+using namespace equarx;
+using namespace equarx::ff;
+using namespace equarx::host;
+
+inline bool is_weight(int dtype, int type) { return type == dtype || type == EQUARX_FP32; }
+inline bool bad_value(double eps, double offset) { return !(eps >= 0.0) || std::isinf(eps) || !std::isfinite(offset); }
+
+// elements of an access: rows that start on multiples of 16, 4 or 2 bytes
+struct Access {
+    int unit = 32;
+    void add(const void* p, size_t ld) {
+        if (p) unit = std::min(unit, unit_of(p, ld, 2));
+    }
+    // fp32 is read in words of 16 bytes or of 4
+    void add_weight(const void* p, bool fp32) {
+        if (!fp32) add(p, 0);
+        else if (!aligned(p, 16)) unit = std::min(unit, 4);
+    }
+    int width() const { return unit >= 16 ? 16 : unit >= 4 ? 2 : 1; }
+};
+
+inline int norm_threads(size_t cols) { return int(std::min<size_t>(kNormThreads, up(ceil_div(cols, 16), 32))); }
+
+// both are the same matrix: each element is read before it is written by the same thread
+inline bool same(const void* p, size_t ldp, const void* q, size_t ldq, size_t rows) { return p == q && (ldp == ldq || rows == 1); }
+
+template <bool EIGHT>
+int launch_norm(const NormArgs& a, int dtype, int width, size_t rows, cudaStream_t stream) {
+    const dim3 grid{unsigned(rows)};
+    const int threads = norm_threads(EIGHT ? fp8_stages(a.cols) * 128 : a.cols);
+    const auto kernel = dtype == EQUARX_BF16 ? (width == 16  ? norm_kernel<kBf16, 16, EIGHT>
+                                                : width == 2 ? norm_kernel<kBf16, 2, EIGHT>
+                                                             : norm_kernel<kBf16, 1, EIGHT>)
+                                             : (width == 16  ? norm_kernel<kFp16, 16, EIGHT>
+                                                : width == 2 ? norm_kernel<kFp16, 2, EIGHT>
+                                                             : norm_kernel<kFp16, 1, EIGHT>);
+    return launch(kernel, grid, threads, 0, 1, a, stream);
+}
+
+// what both outputs share
+void set_inputs(NormArgs& a, const void* x, size_t ldx, const void* residual, size_t ldr, const void* weight, int weight_dtype,
+                size_t cols, double eps, float offset, void* sum, size_t lds, Access& access) {
+    a.x = x;
+    a.residual = residual;
+    a.weight = weight;
+    a.sum = sum;
+    a.ldx = ldx;
+    a.ldr = ldr;
+    a.lds = lds;
+    a.inverse = 1.0 / double(cols);
+    a.eps = eps;
+    a.offset = offset;
+    a.cols = int(cols);
+    a.fp32 = weight_dtype == EQUARX_FP32;
+    access.add(x, ldx);
+    access.add(residual, ldr);
+    if (residual) access.add(sum, lds);
+    access.add_weight(weight, a.fp32);
+}
+
+int check_norm(const void* x, size_t ldx, const void* residual, size_t ldr, const void* weight, int dtype, int weight_dtype,
+               size_t rows, size_t cols, double eps, float offset, const void* sum, size_t lds) {
+    if (!is_16bit(dtype) || !is_weight(dtype, weight_dtype)) return EQUARX_ERR_FORMAT;
+    if (rows > kMaxDim || bad_dim(cols) || bad_ld(ldx, cols) || (residual && (bad_ld(ldr, cols) || bad_ld(lds, cols))))
+        return EQUARX_ERR_COUNT;
+    if (bad_value(eps, offset)) return EQUARX_ERR_VALUE;
+    if (rows == 0) return EQUARX_OK;
+    if (!x || !weight || (!residual) != (!sum)) return EQUARX_ERR_NULL;
+    if (!aligned(x, 2) || !aligned(residual, 2) || !aligned(sum, 2) || !aligned(weight, size_of(weight_dtype))) return EQUARX_ERR_ALIGN;
+    return EQUARX_OK;
+}
+// the sum against the inputs: it may be one of them
+int check_sum(const void* x, size_t ldx, const void* residual, size_t ldr, const void* weight, int weight_dtype, size_t rows,
+              size_t cols, const void* sum, size_t lds) {
+    if (!residual) return EQUARX_OK;
+    const Span s = matrix(sum, rows, cols, lds, 2);
+    if (!same(sum, lds, x, ldx, rows) && overlap(s, matrix(x, rows, cols, ldx, 2))) return EQUARX_ERR_ALIAS;
+    if (!same(sum, lds, residual, ldr, rows) && overlap(s, matrix(residual, rows, cols, ldr, 2))) return EQUARX_ERR_ALIAS;
+    return overlap(s, Span{weight, cols * size_of(weight_dtype)}) ? EQUARX_ERR_ALIAS : EQUARX_OK;
+}
+
+// CTAs of the backward pass, each with a part of the weight's gradient: three for each of 148 SMs, as many as fit at one
+// time, but not more than rows, nor so many that the parts of very long rows outgrow the matrices
+inline size_t norm_parts(size_t rows, size_t cols) {
+    return std::min({rows, size_t(444), std::max<size_t>(1, (size_t(1) << 28) / cols)});
+}
+
+}  // namespace
+
+extern "C" {
+
+int equarx_add_rms_norm(const void* x, size_t ldx, const void* residual, size_t ldr, const void* weight, int dtype,
+                        int weight_dtype, size_t rows, size_t cols, double eps, float offset, void* sum, size_t lds, void* y,
+                        size_t ldy, float* factors, equarx_stream_t stream) {
+    TRY(check_norm(x, ldx, residual, ldr, weight, dtype, weight_dtype, rows, cols, eps, offset, sum, lds));
+    if (bad_ld(ldy, cols)) return EQUARX_ERR_COUNT;
+    if (rows == 0) return EQUARX_OK;
+    if (!y) return EQUARX_ERR_NULL;
+    if (!aligned(y, 2) || !aligned(factors, 4)) return EQUARX_ERR_ALIGN;
+    TRY(check_sum(x, ldx, residual, ldr, weight, weight_dtype, rows, cols, sum, lds));
+    TRY(check_overlap({matrix(x, rows, cols, ldx, 2), matrix(residual, rows, cols, ldr, 2), matrix(sum, rows, cols, lds, 2),
+                       Span{weight, cols * size_of(weight_dtype)}},
+                      {matrix(y, rows, cols, ldy, 2), Span{factors, rows * sizeof(float)}}));
+    TRY(check_overlap({}, {matrix(sum, rows, cols, lds, 2), Span{factors, rows * sizeof(float)}}));
+    NormArgs a = {};
+    Access access;
+    set_inputs(a, x, ldx, residual, ldr, weight, weight_dtype, cols, eps, offset, sum, lds, access);
+    access.add(y, ldy);
+    a.y = y;
+    a.ldy = ldy;
+    a.factors = factors;
+    a.wide = access.unit >= 32;
+    return launch_norm<false>(a, dtype, access.width(), rows, stream);
+}
+
+int equarx_add_rms_norm_fp8(const void* x, size_t ldx, const void* residual, size_t ldr, const void* weight, int dtype,
+                            int weight_dtype, size_t rows, size_t cols, double eps, float offset, void* sum, size_t lds,
+                            uint8_t* codes, uint8_t* scales, equarx_stream_t stream) {
+    TRY(check_norm(x, ldx, residual, ldr, weight, dtype, weight_dtype, rows, cols, eps, offset, sum, lds));
+    if (rows == 0) return EQUARX_OK;
+    if (!codes || !scales) return EQUARX_ERR_NULL;
+    if (!aligned(codes, 16) || !aligned(scales, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_sum(x, ldx, residual, ldr, weight, weight_dtype, rows, cols, sum, lds));
+    TRY(check_overlap({matrix(x, rows, cols, ldx, 2), matrix(residual, rows, cols, ldr, 2), matrix(sum, rows, cols, lds, 2),
+                       Span{weight, cols * size_of(weight_dtype)}},
+                      {Span{codes, rows * fp8_stride(cols)}, Span{scales, equarx_fp8_scales_bytes(rows, cols)}}));
+    NormArgs a = {};
+    Access access;
+    set_inputs(a, x, ldx, residual, ldr, weight, weight_dtype, cols, eps, offset, sum, lds, access);
+    a.codes = codes;
+    a.scales = scales;
+    a.wide = access.unit >= 32;
+    return launch_norm<true>(a, dtype, access.width(), rows, stream);
+}
+
+size_t equarx_add_rms_norm_backward_workspace_bytes(size_t rows, size_t cols) {
+    return rows > kMaxDim || bad_dim(cols) ? 0 : norm_parts(rows, cols) * cols * sizeof(float);
+}
+
+int equarx_add_rms_norm_backward(const void* dy, size_t lddy, const void* dsum, size_t ldds, const void* sum, size_t lds,
+                                 const float* factors, const void* weight, int dtype, int weight_dtype, size_t rows, size_t cols,
+                                 float offset, void* dx, size_t lddx, void* dweight, void* workspace, size_t workspace_bytes,
+                                 equarx_stream_t stream) {
+    if (!is_16bit(dtype) || !is_weight(dtype, weight_dtype)) return EQUARX_ERR_FORMAT;
+    if (rows > kMaxDim || bad_dim(cols) || bad_ld(lddy, cols) || (dsum && bad_ld(ldds, cols)) || bad_ld(lds, cols) || bad_ld(lddx, cols))
+        return EQUARX_ERR_COUNT;
+    if (!std::isfinite(offset)) return EQUARX_ERR_VALUE;
+    const size_t size = size_of(weight_dtype), need = dweight ? norm_parts(rows, cols) * cols * sizeof(float) : 0;
+    if (rows && (!dy || !sum || !factors || !weight || !dx || (need && !workspace))) return EQUARX_ERR_NULL;
+    if (rows && workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
+    for (const void* p : {dy, dsum, sum, static_cast<const void*>(dx)})
+        if (!aligned(p, 2)) return EQUARX_ERR_ALIGN;
+    if (!aligned(factors, 4) || !aligned(weight, size) || !aligned(dweight, size) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    const Span ws{need ? workspace : nullptr, need}, dws{dweight, cols * size};
+    TRY(check_overlap({matrix(dy, rows, cols, lddy, 2), matrix(dsum, rows, cols, ldds, 2), matrix(sum, rows, cols, lds, 2),
+                       Span{factors, rows * sizeof(float)}, Span{weight, cols * size}},
+                      {matrix(dx, rows, cols, lddx, 2), dws, ws}));
+    if (rows == 0) {       // a sum over no rows
+        cudaError_t e = dweight ? launch_error_to_inject() : cudaSuccess;
+        if (e == cudaSuccess && dweight) e = cudaMemsetAsync(dweight, 0, cols * size, stream);
+        return e == cudaSuccess ? EQUARX_OK : cuda_failure(e);
+    }
+    NormGradArgs a = {};
+    Access access;
+    a.dy = dy;
+    a.dsum = dsum;
+    a.sum = sum;
+    a.factors = factors;
+    a.weight = weight;
+    a.dx = dx;
+    a.dw = dweight;
+    a.parts = dweight ? static_cast<float*>(workspace) : nullptr;
+    a.lddy = lddy;
+    a.ldds = ldds;
+    a.lds = lds;
+    a.lddx = lddx;
+    a.inverse = float(1.0 / double(cols));
+    a.offset = offset;
+    a.rows = int(rows);
+    a.cols = int(cols);
+    a.fp32 = weight_dtype == EQUARX_FP32;
+    a.count = int(norm_parts(rows, cols));
+    access.add(dy, lddy);
+    access.add(dsum, ldds);
+    access.add(sum, lds);
+    access.add(dx, lddx);
+    access.add_weight(weight, a.fp32);
+    a.wide = access.unit >= 32;
+    const int width = access.width();
+    const auto kernel = dtype == EQUARX_BF16 ? (width == 16  ? norm_grad_kernel<kBf16, 16>
+                                                : width == 2 ? norm_grad_kernel<kBf16, 2>
+                                                             : norm_grad_kernel<kBf16, 1>)
+                                             : (width == 16  ? norm_grad_kernel<kFp16, 16>
+                                                : width == 2 ? norm_grad_kernel<kFp16, 2>
+                                                             : norm_grad_kernel<kFp16, 1>);
+    TRY(launch(kernel, dim3(unsigned(a.count)), norm_threads(cols), 0, 1, a, stream));
+    if (!dweight) return EQUARX_OK;
+    return launch(dtype == EQUARX_BF16 ? norm_parts_kernel<kBf16> : norm_parts_kernel<kFp16>, dim3(unsigned(ceil_div(cols, 32))), 256, 0,
+                  1, a, stream);
+}
+
+}  // extern "C"

@@ -114,6 +114,11 @@ __device__ __forceinline__ void barrier_arrive_pair(uint32_t cluster_bar) {
 __device__ __forceinline__ void st_cluster_f32(uint32_t cluster_addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
 }
+__device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ void max_cluster_u32(uint32_t cluster_addr, uint32_t v) {
     asm volatile("red.shared::cluster.max.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
 }
@@ -274,6 +279,10 @@ __host__ __device__ constexpr uint32_t desc_16bit(bool bf16, bool a_mn, bool b_m
 __host__ __device__ constexpr uint32_t desc_fp4(bool e8m0, uint32_t m, uint32_t n, uint32_t which) {
     return (which << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (uint32_t(e8m0) << 23) | ((m >> 7) << 27) | (which << 29);
 }
+// block-scaled E4M3 operands with E8M0 scales; `which` selects the scale byte of a 32-bit cell, one for each 32 elements
+__host__ __device__ constexpr uint32_t desc_fp8(uint32_t m, uint32_t n, uint32_t which) {
+    return (which << 4) | ((n >> 3) << 17) | (1u << 23) | ((m >> 7) << 27) | (which << 29);
+}
 
 #define EQUARX_MMA_16BIT(GROUP)                                                                             \
     asm volatile("{\n .reg .pred elected, p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n" \
@@ -281,7 +290,7 @@ __host__ __device__ constexpr uint32_t desc_fp4(bool e8m0, uint32_t m, uint32_t 
                  " @elected tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d),     \
                  "r"(a), "r"(b), "r"(idesc), "r"(uint32_t(accumulate)), "n"(kSwizzledHigh)                  \
                  : "memory")
-#define EQUARX_MMA_FP4(GROUP, KIND)                                                                         \
+#define EQUARX_MMA_SCALED(GROUP, KIND)                                                                       \
     asm volatile("{\n .reg .pred elected, p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %7};\n mov.b64 b, {%2, %7};\n" \
                  " setp.ne.u32 p, %6, 0;\n elect.sync _|elected, 0xFFFFFFFF;\n"                             \
                  " @elected tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], a, b, %3, [%4], [%5], p;\n}" ::"r"(d), \
@@ -298,13 +307,20 @@ __device__ __forceinline__ void mma_16bit(uint32_t d, uint32_t a, uint32_t b, ui
 template <int CTAS, bool MX>
 __device__ __forceinline__ void mma_fp4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
                                         bool accumulate) {
-    if constexpr (CTAS == 1 && MX) EQUARX_MMA_FP4("1", "mxf4.block_scale.scale_vec::2X");
-    else if constexpr (CTAS == 1) EQUARX_MMA_FP4("1", "mxf4nvf4.block_scale.scale_vec::4X");
-    else if constexpr (MX) EQUARX_MMA_FP4("2", "mxf4.block_scale.scale_vec::2X");
-    else EQUARX_MMA_FP4("2", "mxf4nvf4.block_scale.scale_vec::4X");
+    if constexpr (CTAS == 1 && MX) EQUARX_MMA_SCALED("1", "mxf4.block_scale.scale_vec::2X");
+    else if constexpr (CTAS == 1) EQUARX_MMA_SCALED("1", "mxf4nvf4.block_scale.scale_vec::4X");
+    else if constexpr (MX) EQUARX_MMA_SCALED("2", "mxf4.block_scale.scale_vec::2X");
+    else EQUARX_MMA_SCALED("2", "mxf4nvf4.block_scale.scale_vec::4X");
+}
+// 32 elements of the reduction axis in 8 bits, with one E8M0 scale
+template <int CTAS>
+__device__ __forceinline__ void mma_fp8(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                        bool accumulate) {
+    if constexpr (CTAS == 1) EQUARX_MMA_SCALED("1", "mxf8f6f4.block_scale.scale_vec::1X");
+    else EQUARX_MMA_SCALED("2", "mxf8f6f4.block_scale.scale_vec::1X");
 }
 #undef EQUARX_MMA_16BIT
-#undef EQUARX_MMA_FP4
+#undef EQUARX_MMA_SCALED
 // one scale tile (128 rows x 4 scales) from shared to tensor memory, where each quarter of the lanes
 // gets its own copy, as the block-scaled product wants it; with two CTAs, in each of them
 template <int CTAS>

@@ -4,8 +4,8 @@
     partial = h Wd^T                    fp4_linear
 
 with 16-bit weights and their gradients (gated_forward, gated_backward), or with weights and
-activations in microscaled 4-bit floating point (fp4_quantize, fp4_dequantize, fp4_matmul, fp4_linear,
-fp4_gated).  Marshalling only, most of it in an extension module (csrc/feedforward_torch.cpp): outputs and
+activations in microscaled 4-bit or 8-bit floating point (fp4_ and fp8_ quantize, dequantize, matmul, linear,
+gated).  Marshalling only, most of it in an extension module (csrc/feedforward_torch.cpp): outputs and
 workspaces are allocated with torch on the current stream, the kernels run on it, and every argument check
 but those on shapes, strides, types and devices is the library's own (include/equarx.h has the formulas and
 layouts).  A failed call raises EquarxError, tensors that do not fit together raise ValueError; there is no
@@ -14,7 +14,7 @@ CPU path.
 Matrices are [rows, columns] with unit column stride; the row stride is free.
 
 gated_forward takes part in autograd: called with tensors that require gradients, its h is connected to them by
-gated_backward.  The 4-bit products have no gradients and refuse such an x (outside torch.no_grad()); a
+gated_backward.  The 4-bit and 8-bit products have no gradients and refuse such an x (outside torch.no_grad()); a
 quantized matrix is bytes, through which no gradient passes.  gated_backward's results have no gradients themselves.
 """
 import ctypes
@@ -31,7 +31,8 @@ _build.build_torch_module()
 _native = importlib.import_module("._feedforward", __package__)
 for _name in ("fp4_codes_bytes", "fp4_scales_bytes", "fp4_quantize", "fp4_dequantize", "fp4_matmul", "fp4_linear_workspace_bytes",
               "fp4_linear", "fp4_gated", "gated_forward_workspace_bytes", "gated_forward", "gated_backward_workspace_bytes",
-              "gated_backward"):
+              "gated_backward", "fp8_codes_bytes", "fp8_scales_bytes", "fp8_quantize", "fp8_dequantize", "fp8_matmul", "fp8_gated",
+              "add_rms_norm", "add_rms_norm_fp8", "add_rms_norm_backward_workspace_bytes", "add_rms_norm_backward", "add_adapters"):
     _native.bind(_name, ctypes.cast(getattr(binding.lib, "equarx_" + _name), ctypes.c_void_p).value)
 
 
@@ -61,6 +62,26 @@ class Fp4Matrix:
             return None
         first = _native.layout(self.rows, self.cols, self.format)[0]
         return self.data[first:first + 4 * self.rows].view(torch.float32)
+
+
+class Fp8Matrix:
+    """A rows x cols matrix in microscaled 8-bit floating point: one buffer that holds scales and, from a multiple of
+    256 bytes on, codes."""
+    __slots__ = ("data", "rows", "cols")
+
+    def __init__(self, data, rows, cols):
+        self.data, self.rows, self.cols = data, rows, cols
+
+    @property
+    def codes(self):
+        """uint8 [rows, ceil(cols/32)*32], E4M3"""
+        first, end = _native.layout8(self.rows, self.cols)
+        return self.data[first:end].view(self.rows, (self.cols + 31) // 32 * 32)
+
+    @property
+    def scales(self):
+        """uint8, in the tiled order of include/equarx.h"""
+        return self.data[:binding.fp8_scales_bytes(self.rows, self.cols)]
 
 
 def _or_raise(result, where):
@@ -106,6 +127,38 @@ def fp4_gated(x, wg, wu, act=ACT_GELU_TANH):
     if wg.rows != wu.rows or wg.cols != wu.cols or wg.format != wu.format:
         raise ValueError("the two weights differ in shape or format")
     return _or_raise(_native.gated(x, wg.data, wu.data, wg.rows, wg.cols, wg.format, act), "equarx_fp4_gated")
+
+
+def fp8_quantize(x):
+    """x [rows, cols], bfloat16, float16 or float32 -> Fp8Matrix."""
+    data = _or_raise(_native.quantize8(x), "equarx_fp8_quantize")
+    rows, cols = x.shape
+    return Fp8Matrix(data, rows, cols)
+
+
+def fp8_dequantize(q, dtype=torch.bfloat16):
+    """The values that q's codes stand for, rounded once to dtype."""
+    return _or_raise(_native.dequantize8(q.data, q.rows, q.cols, _code(dtype)), "equarx_fp8_dequantize")
+
+
+def fp8_matmul(a, b, dtype=torch.bfloat16):
+    """a b^T of two Fp8Matrix: [a.rows, b.rows]."""
+    if a.cols != b.cols:
+        raise ValueError("the operands differ in columns")
+    return _or_raise(_native.matmul8(a.data, a.rows, b.data, b.rows, a.cols, _code(dtype)), "equarx_fp8_matmul")
+
+
+def fp8_linear(x, w):
+    """x w^T: x [tokens, k] in 16 bits is quantized in the call, w is an Fp8Matrix [n, k]."""
+    return _or_raise(_native.linear8(x, w.data, w.rows, w.cols), "equarx_fp8_matmul")
+
+
+def fp8_gated(x, wg, wu, act=ACT_GELU_TANH, dtype=torch.bfloat16):
+    """act(x wg^T) * (x wu^T) in dtype: x an Fp8Matrix [tokens, k] (of norm.add_rms_norm_fp8 or fp8_quantize), wg and wu
+    Fp8Matrix [f, k]."""
+    if wg.rows != wu.rows or wg.cols != wu.cols or x.cols != wg.cols:
+        raise ValueError("the weights differ in shape, or x from them in columns")
+    return _or_raise(_native.gated8(x.data, x.rows, wg.data, wu.data, wg.rows, wg.cols, act, _code(dtype)), "equarx_fp8_gated")
 
 
 def gated_forward(x, wg, wu, act=ACT_GELU_TANH, save=False):

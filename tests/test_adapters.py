@@ -1,0 +1,245 @@
+"""Low-rank adapters of many requests: refusals (no GPU), and the kernel against 64-bit references.
+
+Bounds.  x A^T is a sum of k products in fp32, its value enters the second product with 16 bits at least (off by 2^-17 of itself;
+fp16: with 22, after a power of two), which is a sum of rank products in fp32, twice (high and low halves); the scale and the
+final addition are one fp32 rounding each, and the result is rounded to 16 bits once.
+"""
+import pytest
+import torch
+
+import ff_reference as ref
+import paper_2506_17615_b200 as eq
+from paper_2506_17615_b200 import adapters as ad
+from paper_2506_17615_b200 import binding
+from paper_2506_17615_b200 import feedforward as ff
+from test_feedforward import A, GB, normal, status_of
+
+gpu = pytest.mark.gpu
+TYPES = [torch.bfloat16, torch.float16]
+
+
+def call_args():
+    return dict(y=A, ldy=64, x=A + GB, ldx=32, a=A + 2 * GB, b=A + 3 * GB, index=A + 4 * GB, scale=A + 5 * GB, dtype=eq.BF16, tokens=4, n=64,
+                k=32, rank=8, adapters=3, out=A + 6 * GB, ldo=64)
+
+
+def test_refuses_bad_arguments():
+    f, a = eq.add_adapters, call_args()
+    for key in ("y", "x", "a", "b", "index", "out"):
+        assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
+    for key in ("y", "x", "a", "b", "index", "scale", "out"):
+        assert status_of(f, **{**a, key: a[key] + 1}) == binding.ERR_ALIGN
+    for bad in (eq.FP32, -1):
+        assert status_of(f, **{**a, "dtype": bad}) == binding.ERR_FORMAT
+    for key, bad in (("n", 0), ("k", 0), ("rank", 0), ("rank", 129), ("tokens", GB + 1), ("adapters", GB + 1), ("ldy", 63), ("ldx", 31),
+                     ("ldo", 63)):
+        assert status_of(f, **{**a, key: bad}) == binding.ERR_COUNT
+    for bad in (A + 2, A + GB, A + 2 * GB, A + 3 * GB, A + 4 * GB, A + 5 * GB):
+        assert status_of(f, **{**a, "out": bad}) == binding.ERR_ALIAS
+    assert status_of(f, **{**a, "out": A, "ldo": 72}) == binding.ERR_ALIAS
+    assert status_of(f, **{**a, "tokens": 0, "y": 0}) == 0
+    assert eq.last_cuda_error() == 0
+
+
+def test_what_the_extension_module_refuses():
+    y, a = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(1, 2, 8, dtype=torch.bfloat16)
+    for call in (lambda: ad.add_adapters(y, y, a, a, torch.zeros(4, dtype=torch.int32)), lambda: ad.add_adapters(None, y, a, a, None),
+                 lambda: ad.add_adapters(y[0], y, a, a, y)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+
+
+def inputs(tokens, n, k, rank, count, seed, dtype, pad=0):
+    y, x = normal(tokens, n, seed, dtype, 1.0, pad), normal(tokens, k, seed + 1, dtype, 1.0, pad)
+    a = normal(count * rank, k, seed + 2, dtype, k ** -0.5).contiguous().view(count, rank, k)
+    b = normal(count * n, rank, seed + 3, dtype, rank ** -0.5).contiguous().view(count, n, rank)
+    scale = torch.rand(count, generator=torch.Generator().manual_seed(seed)).add(0.5).cuda()
+    return y, x, a, b, scale
+
+
+def patterns(tokens, count, seed):
+    """indexes of requests one after the other, of tokens of all requests mixed, and of none"""
+    gen = torch.Generator().manual_seed(seed)
+    mixed = torch.randint(-1, count, (tokens,), generator=gen)
+    mixed[tokens // 2] = count + 5                                  # no adapter either
+    return [(torch.arange(tokens) * (count + 1) // tokens - 1).int().cuda(), mixed.int().cuda(), torch.full((tokens,), -1).int().cuda()]
+
+
+def check(out, y, x, a, b, index, scale):
+    dtype, value, bound = y.dtype, y.double().clone(), torch.zeros_like(y, dtype=torch.float64)
+    for i in range(a.shape[0]):
+        rows = (index == i).nonzero()[:, 0]
+        c = 1.0 if scale is None else float(scale[i])
+        s, es = ref.product(x[rows].double(), a[i].double())
+        es = es + (2.0 ** -17 if dtype == torch.bfloat16 else 2.0 ** -21) * s.abs() + 2.0 ** -24 * s.abs()
+        d, ed = ref.product(s, b[i].double())
+        value[rows] += c * d
+        bound[rows] = c * (2 * ed + es @ b[i].double().abs().T) + 2.0 ** -23 * (value[rows].abs() + c * d.abs())
+    ref.assert_within(out, value, ref.rounded(value, bound, dtype), "out")
+    bare = (index < 0) | (index >= a.shape[0])
+    assert torch.equal(out[bare], y[bare])
+
+
+SIZES = [(1, 1, 1, 1, 1), (1, 64, 64, 16, 1), (1, 5376, 2688, 16, 3), (2, 33, 40, 8, 2), (3, 130, 72, 5, 3), (16, 128, 256, 16, 4),
+         (17, 257, 129, 24, 5), (64, 520, 264, 16, 64), (64, 1000, 1000, 64, 9), (100, 96, 3000, 32, 4), (300, 513, 777, 128, 3),
+         (601, 264, 136, 64, 7), (1200, 136, 520, 16, 2), (2500, 300, 96, 40, 30), (5000, 40, 40, 100, 6), (700, 64, 64, 1, 700)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,n,k,rank,count", SIZES)
+def test_matches_the_definition(dtype, tokens, n, k, rank, count):
+    pad = (0, 8, 3)[(tokens + n) % 3]
+    y, x, a, b, scale = inputs(tokens, n, k, rank, count, tokens + n, dtype, pad)
+    for i, index in enumerate(patterns(tokens, count, tokens)):
+        c = scale if i != 1 else None
+        out = ad.add_adapters(y, x, a, b, index, c)
+        check(out, y, x, a, b, index, c)
+        assert torch.equal(ad.add_adapters(y, x, a, b, index, c), out), "not deterministic"
+        again = y.clone(memory_format=torch.contiguous_format)
+        assert ad.add_adapters(again, x, a, b, index, c, out=again) is again and torch.equal(again, out)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [1, 20, 400])
+def test_not_finite_values_stay_with_their_adapter(dtype, tokens):
+    y, x, a, b, scale = inputs(tokens, 136, 72, 16, 4, 1, dtype)
+    index = (torch.arange(tokens) % 4).int().cuda()
+    clean = ad.add_adapters(y, x, a, b, index, scale)
+    for bad in (float("nan"), float("inf")):
+        a2, b2 = a.clone(), b.clone()
+        a2[1, 3, 5], b2[2, 7, 0] = bad, bad
+        out = ad.add_adapters(y, x, a2, b2, index, scale)
+        rows = (index != 1) & (index != 2)
+        assert torch.equal(out[rows], clean[rows])
+        assert not bool(out[index == 1].isfinite().any())
+        two = index == 2
+        assert not bool(out[two][:, 7].isfinite().any())
+        others = [c for c in range(136) if c != 7]
+        assert torch.equal(out[two][:, others], clean[two][:, others])
+        x2 = x.clone()
+        x2[tokens // 2, 9] = bad
+        out = ad.add_adapters(y, x2, a, b, index, scale)
+        keep = torch.arange(tokens, device="cuda") != tokens // 2
+        assert torch.equal(out[keep], clean[keep]) and not bool(out[tokens // 2].isfinite().any())
+        y2 = y.clone()
+        y2[0, 3] = bad
+        out = ad.add_adapters(y2, x, a, b, index, scale)
+        assert not bool(out[0, 3].isfinite()) and torch.equal(out[1:], clean[1:]) and torch.equal(out[0, 4:], clean[0, 4:])
+
+
+@gpu
+@pytest.mark.parametrize("large", [True, False])
+def test_products_beyond_the_range_of_fp16(large):
+    """x A^T above 65504 or among fp16's subnormal numbers, with outputs inside its range"""
+    y, x, a, b, _ = inputs(40, 64, 96, 16, 3, 1, torch.float16)
+    a, b = (a * 2000, b * 2.0 ** -12) if large else (a * 2.0 ** -9, b * 2.0 ** 3)
+    x = x * 200 if large else x * 2.0 ** -10
+    index = (torch.arange(40) % 4 - 1).int().cuda()
+    s = x.double() @ a.double()[0].T
+    assert float(s.abs().max()) > 70000 if large else float(s.abs().max()) < 2.0 ** -15
+    out = ad.add_adapters(y * 0, x, a, b, index)
+    check(out, y * 0, x, a, b, index, None)
+
+
+@gpu
+@pytest.mark.parametrize("offset", [1, 2, 4, 8])
+@pytest.mark.parametrize("tokens", [3, 150])
+def test_views_that_start_anywhere(tokens, offset):
+    """through the C ABI; the rest of the output's buffer keeps its canary"""
+    dtype, stream, n, k, rank = torch.bfloat16, torch.cuda.current_stream().cuda_stream, 72, 40, 8
+    y, x, a, b, scale = inputs(tokens, n, k, rank, 3, 1, dtype)
+    index = patterns(tokens, 3, 2)[1]
+    want = ad.add_adapters(y, x, a, b, index, scale)
+
+    def place(t, ld):
+        store = torch.full((offset + t.shape[0] * ld + 16,), -77.0, device="cuda", dtype=dtype)
+        view = store[offset:].as_strided(t.shape, (ld, 1))
+        return store, view.copy_(t)
+
+    flat = lambda t: torch.empty(t.numel() + offset, device="cuda", dtype=dtype)[offset:].copy_(t.reshape(-1))
+    for extra in (0, 1, 8):
+        (_, vy), (_, vx), (so, vo) = place(y, n + extra), place(x, k + extra), place(y * 0, n + extra)
+        eq.add_adapters(vy, n + extra, vx, k + extra, flat(a), flat(b), index, scale, eq.BF16, tokens, n, k, rank, 3, vo, n + extra, stream)
+        assert torch.equal(vo, want)
+        vo.fill_(-77.0)
+        assert bool((so == -77.0).all())
+        eq.add_adapters(vy, n + extra, vx, k + extra, a, b, index, scale, eq.BF16, tokens, n, k, rank, 3, vy, n + extra, stream)
+        assert torch.equal(vy, want)
+
+
+@gpu
+def test_offsets_beyond_32_bits():
+    dtype, ld = torch.bfloat16, 1 << 26
+    y, x, a, b, scale = inputs(70, 96, 64, 16, 5, 1, dtype)
+    index = patterns(70, 5, 3)[1]
+    want = ad.add_adapters(y, x, a, b, index, scale)
+    store = torch.empty(69 * ld + 4096, dtype=dtype, device="cuda")
+    fy, fx, fo = (store.as_strided((70, w), (ld, 1), at) for w, at in ((96, 0), (64, 1024), (96, 2048)))
+    fy.copy_(y), fx.copy_(x)
+    assert torch.equal(ad.add_adapters(fy, fx, a, b, index, scale), want)
+    assert torch.equal(ad.add_adapters(fy, fx, a, b, index, scale, out=fo), want)
+    # adapters whose last one lies 2^32 elements after the first
+    del store, fy, fx, fo
+    count = 66000
+    big = torch.empty(count, 16, 4096, dtype=dtype, device="cuda")
+    xx, bb = normal(3, 4096, 5, dtype), normal(count * 8, 16, 6, dtype).view(count, 8, 16)
+    last = normal(16, 4096, 7, dtype, 2.0 ** -6)
+    big[-1], big[7] = last, last
+    bb[7] = bb[-1]
+    yy = normal(3, 8, 8, dtype)
+    at = lambda i: torch.full((3,), i, dtype=torch.int32, device="cuda")
+    assert torch.equal(ad.add_adapters(yy, xx, big, bb, at(count - 1)), ad.add_adapters(yy, xx, big, bb, at(7)))
+
+
+@gpu
+def test_no_tokens_no_adapters_streams_graphs():
+    dtype = torch.bfloat16
+    y, x, a, b, scale = inputs(100, 96, 64, 16, 5, 1, dtype)
+    index = patterns(100, 5, 3)[1]
+    assert ad.add_adapters(y[:0], x[:0], a, b, index[:0]).shape == (0, 96)
+    assert torch.equal(ad.add_adapters(y, x, a[:0], b[:0], index), y)
+    want = ad.add_adapters(y, x, a, b, index, scale)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [ad.add_adapters(y * 1, x, a, b, index, scale) for _ in range(3)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(t, want) for t in got)
+    w = ff.fp4_quantize(normal(96, 64, 9, dtype))
+    base = ff.fp4_linear(x, w)
+    both = ad.add_adapters(base, x, a, b, index, scale)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ff.fp4_linear(x, w)
+        ad.add_adapters(out, x, a, b, index, scale, out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, both)
+
+
+@gpu
+def test_what_is_refused_on_the_gpu(monkeypatch):
+    dtype = torch.bfloat16
+    y, x, a, b, scale = inputs(6, 96, 64, 16, 5, 1, dtype)
+    index = patterns(6, 5, 3)[0]
+    for bad in ((y, x[:5], a, b, index), (y, x, a[:, :, :63], b, index), (y, x, a.half(), b, index), (y, x, a, b[:4], index),
+                (y, x, a, b[:, :, :8], index), (y, x, a, b, index.long()), (y, x, a, b, index[:5]), (y, x, a, b, index, scale[:4]),
+                (y, x, a, b, index, scale.half()), (y, x, a, b, index, scale, x), (y.float(), x, a, b, index)):
+        with pytest.raises(ValueError):
+            ad.add_adapters(*bad)
+    with pytest.raises(eq.EquarxError):
+        ad.add_adapters(y, x, a, b, index, scale, y.as_strided((6, 96), (64, 1)))
+    for i in range(4):
+        args = [y, x, a, b]
+        args[i] = args[i].clone().requires_grad_()
+        with pytest.raises(ValueError, match="no_grad"):
+            ad.add_adapters(*args, index)
+        with torch.no_grad():
+            ad.add_adapters(*args, index)
+    monkeypatch.setenv("EQUARX_INJECT_LAUNCH_ERROR", "719")
+    with pytest.raises(eq.EquarxError) as err:
+        ad.add_adapters(y, x, a, b, index)
+    assert err.value.status == binding.ERR_CUDA and eq.last_cuda_error() == 719
