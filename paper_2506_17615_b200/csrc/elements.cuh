@@ -59,6 +59,39 @@ __device__ __forceinline__ void mul2(float& a, float& b, float c) {
     asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(w));
     asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
 }
+// pairs of fp32 with one instruction, each rounded as a single one is.  (A product that feeds an addition may be contracted.)
+__device__ __forceinline__ uint64_t pair_bits(float2 a) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a.x), "f"(a.y));
+    return v;
+}
+__device__ __forceinline__ float2 pair_of(uint64_t v) {
+    float2 a;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x), "=f"(a.y) : "l"(v));
+    return a;
+}
+__device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(v);
+}
+__device__ __forceinline__ float2 mul_pair(float2 a, float2 b) {
+    uint64_t v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(v);
+}
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+    return pair_of(v);
+}
+__device__ __forceinline__ float2 twice(float a) { return make_float2(a, a); }
+// the largest magnitude of three; NaN wins
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
 // the four scale bytes of 4 neighbouring blocks as one word; a block is PER lanes
 template <int PER>
 __device__ __forceinline__ uint32_t gather_scales(uint32_t byte) {

@@ -66,7 +66,7 @@ inline size_t size_of(int dtype) { return dtype == EQUARX_FP32 ? 4 : 2; }
 
 // ---------------------------------------------------------------- device facts, constant for the process
 // (kept in arrays of a fixed size: nothing here may throw into a C caller)
-constexpr int kMaxDevices = 64, kMaxKernels = 64;
+constexpr int kMaxDevices = 64, kMaxKernels = 128;
 
 struct DeviceFacts {
     int sms = 0;                 // 0: not looked up yet
@@ -96,7 +96,8 @@ inline int current_device(int& sms) {
 
 // ---------------------------------------------------------------- launches
 // kernels that need more than 48 KB of shared memory ask for it once per device
-inline cudaError_t allow_smem(const void* kernel) {
+// (`all`: of the SM's L1, as much as can be is shared memory, for kernels that want several CTAs on an SM)
+inline cudaError_t allow_smem(const void* kernel, bool all) {
     struct Entry {
         const void* kernel;
         uint64_t devices;
@@ -116,6 +117,8 @@ inline cudaError_t allow_smem(const void* kernel) {
     e = cudaFuncGetAttributes(&fa, kernel);
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kBigSmem - fa.sharedSizeBytes));
+    if (e == cudaSuccess && all)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e == cudaSuccess && i < kMaxKernels) {
         seen[i].kernel = kernel;
         seen[i].devices |= bit;
@@ -126,7 +129,7 @@ inline cudaError_t allow_smem(const void* kernel) {
 
 template <typename Args>
 int launch(void (*kernel)(Args), dim3 grid, int threads, size_t smem, unsigned cluster, const Args& args,
-           cudaStream_t stream) {
+           cudaStream_t stream, bool all_shared = false) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
@@ -147,7 +150,8 @@ int launch(void (*kernel)(Args), dim3 grid, int threads, size_t smem, unsigned c
     cfg.attrs = attr;
     cfg.numAttrs = n;
     cudaError_t e = launch_error_to_inject();
-    if (e == cudaSuccess && smem > 48 * 1024) e = allow_smem(reinterpret_cast<const void*>(kernel));
+    // (48 KB hold what a kernel declares, too)
+    if (e == cudaSuccess && smem > 32 * 1024) e = allow_smem(reinterpret_cast<const void*>(kernel), all_shared);
     if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, args);
     return e == cudaSuccess ? EQUARX_OK : cuda_failure(e);
 }

@@ -24,30 +24,62 @@ struct Access {
         if (!fp32) add(p, 0);
         else if (!aligned(p, 16)) unit = std::min(unit, 4);
     }
-    int width() const { return unit >= 16 ? 16 : unit >= 4 ? 2 : 1; }
+    int width() const { return unit >= 16 ? 8 : unit >= 4 ? 2 : 1; }
 };
 
-inline int norm_threads(size_t cols) { return int(std::min<size_t>(kNormThreads, up(ceil_div(cols, 16), 32))); }
+// Groups of 8 columns for each thread: as few threads as hold a row, up to 256 of them, since each thread's part in the
+// row's reduction costs as much as 8 columns do.  0: a row that no CTA holds.
+inline int norm_groups(size_t cols) { return cols > size_t(kNormOnce) ? 0 : int(ceil_div(cols, kNormColumns)); }
+inline int norm_threads(size_t cols) {
+    const int groups = norm_groups(cols);
+    return groups ? int(up(ceil_div(cols, 8 * groups), 32)) : kNormThreads;
+}
 
 // both are the same matrix: each element is read before it is written by the same thread
 inline bool same(const void* p, size_t ldp, const void* q, size_t ldq, size_t rows) { return p == q && (ldp == ldq || rows == 1); }
 
+template <int DT, int W, bool EIGHT>
+int launch_norm(const NormArgs& a, cudaStream_t stream) {
+    const size_t end = EIGHT ? fp8_stages(a.cols) * 128 : a.cols;
+    const int threads = int(std::min<size_t>(kRowThreads, up(ceil_div(end, 8), 32)));
+    return launch(end > size_t(kRowThreads) * 8 ? norm_kernel<DT, W, EIGHT, true> : norm_kernel<DT, W, EIGHT, false>, dim3(unsigned(a.rows)),
+                  threads, 0, 1, a, stream);
+}
 template <bool EIGHT>
-int launch_norm(const NormArgs& a, int dtype, int width, size_t rows, cudaStream_t stream) {
-    const dim3 grid{unsigned(rows)};
-    const int threads = norm_threads(EIGHT ? fp8_stages(a.cols) * 128 : a.cols);
-    const auto kernel = dtype == EQUARX_BF16 ? (width == 16  ? norm_kernel<kBf16, 16, EIGHT>
-                                                : width == 2 ? norm_kernel<kBf16, 2, EIGHT>
-                                                             : norm_kernel<kBf16, 1, EIGHT>)
-                                             : (width == 16  ? norm_kernel<kFp16, 16, EIGHT>
-                                                : width == 2 ? norm_kernel<kFp16, 2, EIGHT>
-                                                             : norm_kernel<kFp16, 1, EIGHT>);
-    return launch(kernel, grid, threads, 0, 1, a, stream);
+int launch_norm(const NormArgs& a, int dtype, int width, cudaStream_t stream) {
+    if (dtype == EQUARX_BF16)
+        return width == 8   ? launch_norm<kBf16, 8, EIGHT>(a, stream)
+               : width == 2 ? launch_norm<kBf16, 2, EIGHT>(a, stream)
+                            : launch_norm<kBf16, 1, EIGHT>(a, stream);
+    return width == 8   ? launch_norm<kFp16, 8, EIGHT>(a, stream)
+           : width == 2 ? launch_norm<kFp16, 2, EIGHT>(a, stream)
+                        : launch_norm<kFp16, 1, EIGHT>(a, stream);
+}
+
+template <int DT, int W, int G>
+int launch_grad(const NormGradArgs& a, int threads, cudaStream_t stream) {
+    return launch(norm_grad_kernel<DT, W, G>, dim3(unsigned(a.count)), threads, W == 8 ? size_t(kNormStages) * 3 * 16 * G * threads : 0, 1,
+                  a, stream, true);
+}
+template <int DT, int W>
+int launch_grad(const NormGradArgs& a, cudaStream_t stream) {
+    const int threads = norm_threads(a.cols);
+    switch (norm_groups(a.cols)) {
+        case 1: return launch_grad<DT, W, 1>(a, threads, stream);
+        case 2: return launch_grad<DT, W, 2>(a, threads, stream);
+        case 3: return launch_grad<DT, W, 3>(a, threads, stream);
+        case 4: return launch_grad<DT, W, 4>(a, threads, stream);
+        default: return launch_grad<DT, W, 0>(a, threads, stream);
+    }
+}
+template <int DT>
+int launch_grad(const NormGradArgs& a, int width, cudaStream_t stream) {
+    return width == 8 ? launch_grad<DT, 8>(a, stream) : width == 2 ? launch_grad<DT, 2>(a, stream) : launch_grad<DT, 1>(a, stream);
 }
 
 // what both outputs share
 void set_inputs(NormArgs& a, const void* x, size_t ldx, const void* residual, size_t ldr, const void* weight, int weight_dtype,
-                size_t cols, double eps, float offset, void* sum, size_t lds, Access& access) {
+                size_t rows, size_t cols, double eps, float offset, void* sum, size_t lds, Access& access) {
     a.x = x;
     a.residual = residual;
     a.weight = weight;
@@ -58,6 +90,7 @@ void set_inputs(NormArgs& a, const void* x, size_t ldx, const void* residual, si
     a.inverse = 1.0 / double(cols);
     a.eps = eps;
     a.offset = offset;
+    a.rows = int(rows);
     a.cols = int(cols);
     a.fp32 = weight_dtype == EQUARX_FP32;
     access.add(x, ldx);
@@ -87,10 +120,11 @@ int check_sum(const void* x, size_t ldx, const void* residual, size_t ldr, const
     return overlap(s, Span{weight, cols * size_of(weight_dtype)}) ? EQUARX_ERR_ALIAS : EQUARX_OK;
 }
 
-// CTAs of the backward pass, each with a part of the weight's gradient: three for each of 148 SMs, as many as fit at one
-// time, but not more than rows, nor so many that the parts of very long rows outgrow the matrices
+// CTAs of the backward pass, each with a part of the weight's gradient: two for each of 148 SMs (more where rows are
+// short), two rows at least for each, and not so many that the parts of very long rows outgrow the matrices
 inline size_t norm_parts(size_t rows, size_t cols) {
-    return std::min({rows, size_t(444), std::max<size_t>(1, (size_t(1) << 28) / cols)});
+    const size_t most = 148 * std::max<size_t>(2, std::min<size_t>(8, 512 / norm_threads(cols)));
+    return std::min({ceil_div(rows, 2), most, std::max<size_t>(1, (size_t(1) << 28) / cols)});
 }
 
 }  // namespace
@@ -112,13 +146,12 @@ int equarx_add_rms_norm(const void* x, size_t ldx, const void* residual, size_t 
     TRY(check_overlap({}, {matrix(sum, rows, cols, lds, 2), Span{factors, rows * sizeof(float)}}));
     NormArgs a = {};
     Access access;
-    set_inputs(a, x, ldx, residual, ldr, weight, weight_dtype, cols, eps, offset, sum, lds, access);
+    set_inputs(a, x, ldx, residual, ldr, weight, weight_dtype, rows, cols, eps, offset, sum, lds, access);
     access.add(y, ldy);
     a.y = y;
     a.ldy = ldy;
     a.factors = factors;
-    a.wide = access.unit >= 32;
-    return launch_norm<false>(a, dtype, access.width(), rows, stream);
+    return launch_norm<false>(a, dtype, access.width(), stream);
 }
 
 int equarx_add_rms_norm_fp8(const void* x, size_t ldx, const void* residual, size_t ldr, const void* weight, int dtype,
@@ -134,11 +167,10 @@ int equarx_add_rms_norm_fp8(const void* x, size_t ldx, const void* residual, siz
                       {Span{codes, rows * fp8_stride(cols)}, Span{scales, equarx_fp8_scales_bytes(rows, cols)}}));
     NormArgs a = {};
     Access access;
-    set_inputs(a, x, ldx, residual, ldr, weight, weight_dtype, cols, eps, offset, sum, lds, access);
+    set_inputs(a, x, ldx, residual, ldr, weight, weight_dtype, rows, cols, eps, offset, sum, lds, access);
     a.codes = codes;
     a.scales = scales;
-    a.wide = access.unit >= 32;
-    return launch_norm<true>(a, dtype, access.width(), rows, stream);
+    return launch_norm<true>(a, dtype, access.width(), stream);
 }
 
 size_t equarx_add_rms_norm_backward_workspace_bytes(size_t rows, size_t cols) {
@@ -193,17 +225,9 @@ int equarx_add_rms_norm_backward(const void* dy, size_t lddy, const void* dsum, 
     access.add(sum, lds);
     access.add(dx, lddx);
     access.add_weight(weight, a.fp32);
-    a.wide = access.unit >= 32;
-    const int width = access.width();
-    const auto kernel = dtype == EQUARX_BF16 ? (width == 16  ? norm_grad_kernel<kBf16, 16>
-                                                : width == 2 ? norm_grad_kernel<kBf16, 2>
-                                                             : norm_grad_kernel<kBf16, 1>)
-                                             : (width == 16  ? norm_grad_kernel<kFp16, 16>
-                                                : width == 2 ? norm_grad_kernel<kFp16, 2>
-                                                             : norm_grad_kernel<kFp16, 1>);
-    TRY(launch(kernel, dim3(unsigned(a.count)), norm_threads(cols), 0, 1, a, stream));
+    TRY(dtype == EQUARX_BF16 ? launch_grad<kBf16>(a, access.width(), stream) : launch_grad<kFp16>(a, access.width(), stream));
     if (!dweight) return EQUARX_OK;
-    return launch(dtype == EQUARX_BF16 ? norm_parts_kernel<kBf16> : norm_parts_kernel<kFp16>, dim3(unsigned(ceil_div(cols, 32))), 256, 0,
+    return launch(dtype == EQUARX_BF16 ? norm_parts_kernel<kBf16> : norm_parts_kernel<kFp16>, dim3(unsigned(ceil_div(cols, 32))), 1024, 0,
                   1, a, stream);
 }
 

@@ -12,52 +12,49 @@ namespace ff {
 
 using namespace tc;
 
-constexpr int kNormThreads = 1024;         // at most; a thread holds 16 elements
+constexpr int kNormThreads = 256;          // at most
+constexpr int kNormColumns = kNormThreads * 8;
+constexpr int kNormGroups = 4;             // groups of 8 elements that a thread holds, at most
+constexpr int kNormOnce = kNormGroups * kNormColumns;        // columns that a CTA holds in registers
+constexpr int kNormStages = 3;             // rows in shared memory, where rows are copied ahead
 
-// Sixteen elements of a row in a thread's registers.  W = 16: neighbours, for rows that start on multiples of 16 bytes.
-// W = 2 or 1: pairs or single elements, the next thread the next ones, for rows that start on multiples of 4 or 2 bytes: a
-// warp's accesses are then whole sectors all the same (with 16 neighbours each access would touch 32 sectors).
+constexpr int kRowThreads = 1024;          // of the forward pass, at most
+
+// Eight elements of a row in a thread's registers, pairs of neighbours.  W = 8: all neighbours, for rows that start on
+// multiples of 16 bytes.  W = 2 or 1: pairs or single elements, the next thread the next ones, for rows that start on multiples of 4
+// or 2 bytes: a warp's accesses are then whole sectors all the same.
 template <int W>
 __device__ __forceinline__ int column_of(int first, int e) {
-    if (W == 16) return first + int(threadIdx.x) * 16 + e;
+    if (W == 8) return first + int(threadIdx.x) * 8 + e;
     return first + (e / W * int(blockDim.x) + int(threadIdx.x)) * W + e % W;
 }
-// as pairs of 16-bit words; zero past the last column.  `wide`: rows start on multiples of 32 bytes
+// as pairs of 16-bit words; zero past the last column
 template <int W>
-__device__ __forceinline__ void load_row(const void* row, int first, int cols, bool wide, uint32_t (&v)[8]) {
+__device__ __forceinline__ void load_row(const void* row, int first, int cols, uint32_t (&v)[4]) {
     const uint16_t* const q = static_cast<const uint16_t*>(row);
     const int col = column_of<W>(first, 0);
-    if (W == 16 && col + 16 <= cols) {
-        if (wide) {
-            load_256(q + col, v);
-        } else {
-            const uint4 a = reinterpret_cast<const uint4*>(q + col)[0], b = reinterpret_cast<const uint4*>(q + col)[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        }
+    if (W == 8 && col + 8 <= cols) {
+        const uint4 a = *reinterpret_cast<const uint4*>(q + col);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const int c0 = column_of<W>(first, 2 * i), c1 = column_of<W>(first, 2 * i + 1);
         if (W == 2 && c1 < cols) v[i] = *reinterpret_cast<const uint32_t*>(q + c0);
         else v[i] = (c0 < cols ? q[c0] : 0) | uint32_t(c1 < cols ? q[c1] : 0) << 16;
     }
 }
 template <int W>
-__device__ __forceinline__ void store_row(void* row, int first, int cols, bool wide, const uint32_t (&v)[8]) {
+__device__ __forceinline__ void store_row(void* row, int first, int cols, const uint32_t (&v)[4]) {
     uint16_t* const q = static_cast<uint16_t*>(row);
     const int col = column_of<W>(first, 0);
-    if (W == 16 && col + 16 <= cols) {
-        if (wide) {
-            store_256(q + col, v);
-        } else {
-            reinterpret_cast<uint4*>(q + col)[0] = make_uint4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<uint4*>(q + col)[1] = make_uint4(v[4], v[5], v[6], v[7]);
-        }
+    if (W == 8 && col + 8 <= cols) {
+        *reinterpret_cast<uint4*>(q + col) = make_uint4(v[0], v[1], v[2], v[3]);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const int c0 = column_of<W>(first, 2 * i), c1 = column_of<W>(first, 2 * i + 1);
         if (W == 2 && c1 < cols) {
             *reinterpret_cast<uint32_t*>(q + c0) = v[i];
@@ -67,38 +64,30 @@ __device__ __forceinline__ void store_row(void* row, int first, int cols, bool w
         }
     }
 }
-// the weight, 16 bits or fp32, as it is stored
-struct Weights {
-    uint32_t w[16];
-};
-template <int W>
-__device__ __forceinline__ void load_weights(const void* weight, bool fp32, int first, int cols, bool wide, Weights& v) {
+// offset + weight, the weight in 16 bits or fp32
+template <int DT, int W>
+__device__ __forceinline__ void load_weights(const void* weight, bool fp32, float offset, int first, int cols, float2 (&v)[4]) {
     if (!fp32) {
-        uint32_t h[8];
-        load_row<W>(weight, first, cols, wide, h);
+        uint32_t h[4];
+        load_row<W>(weight, first, cols, h);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v.w[i] = h[i];
-        return;
-    }
-    const uint32_t* const q = static_cast<const uint32_t*>(weight);
-    const int col = column_of<W>(first, 0);
-    if (W == 16 && col + 16 <= cols) {
+        for (int i = 0; i < 4; ++i) v[i] = unpack2(h[i], DT);
+    } else {
+        const float* const q = static_cast<const float*>(weight);
+        const int col = column_of<W>(first, 0);
+        if (W == 8 && col + 8 <= cols) {
+            const float4 a = reinterpret_cast<const float4*>(q + col)[0], b = reinterpret_cast<const float4*>(q + col)[1];
+            v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w); v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 a = reinterpret_cast<const uint4*>(q + col)[i];
-            v.w[4 * i] = a.x; v.w[4 * i + 1] = a.y; v.w[4 * i + 2] = a.z; v.w[4 * i + 3] = a.w;
+            for (int i = 0; i < 4; ++i) {
+                const int c0 = column_of<W>(first, 2 * i), c1 = column_of<W>(first, 2 * i + 1);
+                v[i] = make_float2(c0 < cols ? q[c0] : 0.0f, c1 < cols ? q[c1] : 0.0f);
+            }
         }
-        return;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v.w[i] = column_of<W>(first, i) < cols ? q[column_of<W>(first, i)] : 0;
-}
-template <int DT>
-__device__ __forceinline__ float2 weight_pair(const Weights& v, bool fp32, int i, float offset) {
-    float2 f;
-    if (fp32) f = make_float2(__uint_as_float(v.w[2 * i]), __uint_as_float(v.w[2 * i + 1]));
-    else f = unpack2(v.w[i], DT);
-    return make_float2(__fadd_rn(offset, f.x), __fadd_rn(offset, f.y));
+    for (int i = 0; i < 4; ++i) v[i] = add_pair(v[i], twice(offset));
 }
 
 // the sum of all threads' values in an order that does not depend on timing; every thread gets it.  `shared` is not
@@ -117,6 +106,15 @@ __device__ __forceinline__ T block_sum(T v, T* shared) {
     return v;
 }
 
+// 1 / sqrt(m), in fp64 to about 2^-52: one step of third order from an fp32 start, r (1 + e/2 + 3 e^2/8) with e = 1 - m r^2
+// below 2^-21; the general function (twice the time) where fp32 does not reach.
+__device__ __forceinline__ double inverse_root(double m) {
+    const uint32_t exponent = uint32_t(__double2hiint(m)) >> 20;       // with the sign
+    if (exponent - (1023u - 100u) > 200u) return rsqrt(m);
+    const double r = double(rsqrtf(float(m))), e = fma(-m * r, r, 1.0);
+    return fma(r * e, fma(0.375, e, 0.5), r);
+}
+
 // ---------------------------------------------------------------- forward
 struct NormArgs {
     const void *x, *residual, *weight;     // residual may be null: the sum is x then, and is not written
@@ -126,111 +124,133 @@ struct NormArgs {
     size_t ldx, ldr, lds, ldy;
     double inverse, eps;                   // 1 / columns
     float offset;
-    int cols, wide, fp32;                  // wide: all rows start on multiples of 32 bytes; fp32: the weight's type
+    int rows, cols, fp32;                  // fp32: the weight's type
 };
+
+// the codes and scales of eight elements of a row, from column `first` on; scales end at column `end`
+template <int W>
+__device__ __forceinline__ void store_fp8(const NormArgs& p, uint8_t* codes, uint8_t* scales, int first, int end, float2 (&v)[4]) {
+    const int stride = int(fp8_stride(p.cols));
+    // 0 past the last column, also where r is not finite
+    if (column_of<W>(first, 7) >= p.cols) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (column_of<W>(first, 2 * i) >= p.cols) v[i].x = 0.0f;
+            if (column_of<W>(first, 2 * i + 1) >= p.cols) v[i].y = 0.0f;
+        }
+    }
+    if constexpr (W == 8) {
+        const int col = column_of<W>(first, 0);
+        uint32_t m = __float_as_uint(max_abs(max_abs(max_abs(v[0].x, v[0].y, v[1].x), v[1].y, v[2].x),
+                                             max_abs(v[2].y, v[3].x, v[3].y), 0.0f)), byte;
+        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+        float inv;
+        fp8_block_scale(m, byte, inv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = mul_pair(v[i], twice(inv));
+        if (col < stride)
+            *reinterpret_cast<uint2*>(codes + col) = make_uint2(encode_e4m3(v[0].x, v[0].y) | encode_e4m3(v[1].x, v[1].y) << 16,
+                                                                encode_e4m3(v[2].x, v[2].y) | encode_e4m3(v[3].x, v[3].y) << 16);
+        const uint32_t word = gather_scales<4>(byte);
+        if (threadIdx.x % 16 == 0 && col < end) *reinterpret_cast<uint32_t*>(scales + size_t(col / 128) * 512) = word;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e += W) {
+            const int col = column_of<W>(first, e);
+            const float a = e & 1 ? v[e / 2].y : v[e / 2].x, b = W == 2 ? v[e / 2].y : 0.0f;
+            uint32_t m = __float_as_uint(max_abs(a, b, 0.0f)), byte;
+            float inv;
+#pragma unroll
+            for (int d = 16 / W; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            fp8_block_scale(m, byte, inv);
+            const uint32_t code = encode_e4m3(__fmul_rn(a, inv), __fmul_rn(b, inv));
+            if (col < stride) {
+                if (W == 2) *reinterpret_cast<uint16_t*>(codes + col) = uint16_t(code);
+                else codes[col] = uint8_t(code);
+            }
+            if (col % 32 == 0 && col < end) scales[size_t(col / 128) * 512 + col / 32 % 4] = uint8_t(byte);
+        }
+    }
+}
 
 // sum = rn16(x + residual), r = 1 / sqrt(mean(sum^2) + eps), v = (sum r) (offset + weight), each step rounded to fp32.  The
 // squares are added in fp64: rows of thousands of elements then give an r that does not depend on the order of addition
 // (but where it lies within 2^-45 of a border), and with r the 8-bit codes are those of the definition, bit for bit.
 //
-// One CTA a row, 16 elements a thread, kept in registers between the row's sum and its scaling: each input is read once. Rows
-// of more than 16384 elements read their sum again.
-template <int DT, int W, bool EIGHT>
-__global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constant__ NormArgs p) {
-    __shared__ double shared[32];
-    const int threads = blockDim.x, span = threads * 16;
-    const size_t row = blockIdx.x, stages = fp8_stages(p.cols), stride = fp8_stride(p.cols);
-    const int end = EIGHT ? int(stages * 128) : p.cols;
+// One CTA a row, 8 elements a thread, kept in registers between the row's sum and its scaling: each input is read once.
+// LONG: rows of more than 8192 elements read their sum again.
+template <int DT, int W, bool EIGHT, bool LONG>
+__global__ void __launch_bounds__(kRowThreads) norm_kernel(const __grid_constant__ NormArgs p) {
+    __shared__ double parts[32];
+    __shared__ float root;
+    const int span = blockDim.x * 8, warps = blockDim.x / 32, lane = threadIdx.x & 31;
+    const size_t row = blockIdx.x;
+    const int end = EIGHT ? int(fp8_stages(p.cols) * 128) : p.cols;
+    const bool add = p.residual != nullptr;
     const uint16_t* const x = static_cast<const uint16_t*>(p.x) + row * p.ldx;
-    const uint16_t* const residual = static_cast<const uint16_t*>(p.residual) + (p.residual ? row * p.ldr : 0);
-    uint16_t* const sum = static_cast<uint16_t*>(p.sum) + (p.residual ? row * p.lds : 0);
-    const bool once = span >= end;
+    const uint16_t* const residual = static_cast<const uint16_t*>(p.residual) + row * p.ldr;
+    uint16_t* const sum = static_cast<uint16_t*>(p.sum) + row * p.lds;
     grid_launch();
     grid_wait();
 
-    uint32_t h[8];
-    Weights w;
-    double squares = 0.0;
-    for (int first = 0; first < p.cols; first += span) {
-        load_row<W>(x, first, p.cols, p.wide, h);
-        if (p.residual) {
-            uint32_t b[8];
-            load_row<W>(residual, first, p.cols, p.wide, b);
-            if (once) load_weights<W>(p.weight, p.fp32, first, p.cols, p.wide, w);
+    uint32_t h[4];
+    float2 w[4];
+    double even = 0.0, odd = 0.0;
+    for (int first = 0; first < (LONG ? p.cols : 1); first += span) {
+        uint32_t b[4];
+        load_row<W>(x, first, p.cols, h);
+        if (add) load_row<W>(residual, first, p.cols, b);
+        if (!LONG) load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w);
+        if (add) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 f = unpack2(h[i], DT), g = unpack2(b[i], DT);
-                h[i] = pack2(__fadd_rn(f.x, g.x), __fadd_rn(f.y, g.y), DT);
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = add_pair(unpack2(h[i], DT), unpack2(b[i], DT));
+                h[i] = pack2(f.x, f.y, DT);
             }
-            store_row<W>(sum, first, p.cols, p.wide, h);
-        } else if (once) {
-            load_weights<W>(p.weight, p.fp32, first, p.cols, p.wide, w);
+            store_row<W>(sum, first, p.cols, h);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const float2 f = unpack2(h[i], DT);
-            squares = fma(double(f.x), double(f.x), squares);
-            squares = fma(double(f.y), double(f.y), squares);
+            even = fma(double(f.x), double(f.x), even);
+            odd = fma(double(f.y), double(f.y), odd);
         }
     }
-    squares = block_sum(squares, shared);
-    const float r = float(rsqrt(fma(squares, p.inverse, p.eps)));
-    if (!EIGHT && p.factors && threadIdx.x == 0) p.factors[row] = r;
+    even += odd;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) even += __shfl_xor_sync(0xFFFFFFFFu, even, d);
+    if (lane == 0) parts[threadIdx.x >> 5] = even;
+    __syncthreads();
+    if (threadIdx.x < 32) {                                // one warp, so that the others' instructions go to elements
+        even = lane < warps ? parts[lane] : 0.0;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) even += __shfl_xor_sync(0xFFFFFFFFu, even, d);
+        if (lane == 0) {
+            root = float(inverse_root(fma(even, p.inverse, p.eps)));
+            if (!EIGHT && p.factors) p.factors[row] = root;
+        }
+    }
+    __syncthreads();
+    const float r = root;
 
-    for (int first = 0; first < end; first += span) {
-        if (!once) {
-            load_row<W>(p.residual ? sum : x, first, p.cols, p.wide, h);
-            load_weights<W>(p.weight, p.fp32, first, p.cols, p.wide, w);
+    uint8_t* const codes = p.codes + row * fp8_stride(p.cols);
+    uint8_t* const scales = p.scales + fp8_scale_offset(row, 0, fp8_stages(p.cols));
+    for (int first = 0; first < (LONG ? end : 1); first += span) {
+        if (LONG) {
+            load_row<W>(add ? sum : x, first, p.cols, h);
+            load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w);
         }
-        float v[16];
+        float2 v[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 f = unpack2(h[i], DT), s = weight_pair<DT>(w, p.fp32, i, p.offset);
-            v[2 * i] = __fmul_rn(__fmul_rn(f.x, r), s.x);
-            v[2 * i + 1] = __fmul_rn(__fmul_rn(f.y, r), s.y);
-        }
-        if constexpr (!EIGHT) {
-            uint32_t out[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = pack2(v[2 * i], v[2 * i + 1], DT);
-            store_row<W>(static_cast<uint16_t*>(p.y) + row * p.ldy, first, p.cols, p.wide, out);
+        for (int i = 0; i < 4; ++i) v[i] = mul_pair(mul_pair(unpack2(h[i], DT), twice(r)), w[i]);
+        if constexpr (EIGHT) {
+            store_fp8<W>(p, codes, scales, first, end, v);
         } else {
-            // 0 past the last column, also where r is not finite
+            uint32_t out[4];
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (column_of<W>(first, e) >= p.cols) v[e] = 0.0f;
-            uint8_t* const codes = p.codes + row * stride;
-            uint8_t* const scales = p.scales + fp8_scale_offset(row, 0, stages);
-            if constexpr (W == 16) {
-                uint32_t m = 0, byte;
-                float inv;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-                fp8_block_scale(m, byte, inv);
-                const uint4 code = encode_e4m3(v, inv);
-                const int col = column_of<W>(first, 0);
-                if (col < int(stride)) *reinterpret_cast<uint4*>(codes + col) = code;
-                const uint32_t word = gather_scales<2>(byte);
-                if (threadIdx.x % 8 == 0 && col < end) *reinterpret_cast<uint32_t*>(scales + size_t(col / 128) * 512) = word;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; e += W) {
-                    uint32_t m = __float_as_uint(v[e]) & 0x7FFFFFFFu, byte;
-                    if (W == 2) m = max(m, __float_as_uint(v[e + 1]) & 0x7FFFFFFFu);
-#pragma unroll
-                    for (int d = 16 / W; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-                    float inv;
-                    fp8_block_scale(m, byte, inv);
-                    const int col = column_of<W>(first, e);
-                    const uint32_t code = encode_e4m3(__fmul_rn(v[e], inv), W == 2 ? __fmul_rn(v[e + 1], inv) : 0.0f);
-                    if (col < int(stride)) {
-                        if (W == 2) *reinterpret_cast<uint16_t*>(codes + col) = uint16_t(code);
-                        else codes[col] = uint8_t(code);
-                    }
-                    if (col % 32 == 0 && col < end) scales[size_t(col / 128) * 512 + col / 32 % 4] = uint8_t(byte);
-                }
-            }
+            for (int i = 0; i < 4; ++i) out[i] = pack2(v[i].x, v[i].y, DT);
+            store_row<W>(static_cast<uint16_t*>(p.y) + row * p.ldy, first, p.cols, out);
         }
     }
 }
@@ -244,107 +264,164 @@ struct NormGradArgs {
     void* dw;
     size_t lddy, ldds, lds, lddx;
     float inverse, offset;
-    int rows, cols, wide, fp32, count;     // count: parts
+    int rows, cols, fp32, count;           // count: parts
 };
 
-// n = sum r, g = dy (offset + weight):  dx = dsum + r (g - n mean(g n)), dweight = sum over rows of dy n.
-// A CTA takes every gridDim-th row, a thread the same 16 columns of each, whose weight gradients it adds up in registers
-// (rows of more than 16384 elements: in its part in memory).
-template <int DT, int W>
-__global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
+// n = sum r, g = dy (offset + weight):  dx = dsum + r g - (r mean(g n)) n, dweight = sum over rows of dy n.
+// A CTA takes every gridDim-th row, a thread the same columns of each, whose weight gradients it adds up in registers (G = 0:
+// in its part in memory).  W = 8: the next rows are copied ahead, as above.
+template <int DT, int W, int G>
+__global__ void __launch_bounds__(kNormThreads, G == 4 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
+    constexpr bool STAGED = W == 8 && G > 0;
+    constexpr int N = G ? G : 1;
+    extern __shared__ __align__(16) uint8_t staged[];
     __shared__ float shared[2][32];
-    const int span = blockDim.x * 16;
-    const bool once = span >= p.cols;
+    const int span = blockDim.x * 8;
+    const bool add = p.dsum != nullptr;
     float* const part = p.parts ? p.parts + size_t(blockIdx.x) * p.cols : nullptr;
     grid_launch();
     grid_wait();
-    uint32_t dy[8], ds[8], h[8];
-    Weights w;
-    float acc[16] = {};
-    if (once) load_weights<W>(p.weight, p.fp32, 0, p.cols, p.wide, w);
-    int turn = 0;
-    for (size_t row = blockIdx.x; row < size_t(p.rows); row += gridDim.x, turn ^= 1) {
-        const uint16_t* const qy = static_cast<const uint16_t*>(p.dy) + row * p.lddy;
-        const uint16_t* const qs = static_cast<const uint16_t*>(p.dsum) + (p.dsum ? row * p.ldds : 0);
-        const uint16_t* const qh = static_cast<const uint16_t*>(p.sum) + row * p.lds;
-        const float r = p.factors[row];
-        float b = 0.0f;
-        for (int first = 0; first < p.cols; first += span) {
-            load_row<W>(qy, first, p.cols, p.wide, dy);
-            load_row<W>(qh, first, p.cols, p.wide, h);
-            if (once) {
-                if (p.dsum) load_row<W>(qs, first, p.cols, p.wide, ds);
-            } else {
-                load_weights<W>(p.weight, p.fp32, first, p.cols, p.wide, w);
-            }
+    float2 w[N][4], acc[N][4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                // past the last column dy and h are 0
-                const float2 fh = unpack2(h[i], DT), fy = unpack2(dy[i], DT), s = weight_pair<DT>(w, p.fp32, i, p.offset);
-                b = fmaf(fy.x * s.x, fh.x * r, b);
-                b = fmaf(fy.y * s.y, fh.y * r, b);
+    for (int g = 0; g < N; ++g) {
+        if (G) load_weights<DT, W>(p.weight, p.fp32, p.offset, g * span, p.cols, w[g]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[g][i] = make_float2(0.0f, 0.0f);
+    }
+    const uint32_t mine = smem_addr(staged) + threadIdx.x * 16;
+    const int per = blockDim.x * 16, per_stage = 3 * N * per;
+    auto fetch = [&](size_t row, uint32_t to) {
+        if (row < size_t(p.rows)) {
+            const uint16_t* const dy = static_cast<const uint16_t*>(p.dy) + row * p.lddy;
+            const uint16_t* const h = static_cast<const uint16_t*>(p.sum) + row * p.lds;
+            const uint16_t* const ds = static_cast<const uint16_t*>(p.dsum) + row * p.ldds;
+#pragma unroll
+            for (int g = 0; g < N; ++g) {
+                const int col = column_of<8>(g * span, 0), bytes = min(16, (p.cols - col) * 2);
+                if (bytes <= 0) continue;
+                copy_async_16(to + 3 * g * per, dy + col, bytes);
+                copy_async_16(to + (3 * g + 1) * per, h + col, bytes);
+                if (add) copy_async_16(to + (3 * g + 2) * per, ds + col, bytes);
             }
         }
-        // two buffers: a thread writes one again only after the barrier of the row between
-        const float c = block_sum(b, shared[turn]) * p.inverse;
-        for (int first = 0; first < p.cols; first += span) {
-            if (!once) {
-                load_row<W>(qy, first, p.cols, p.wide, dy);
-                load_row<W>(qh, first, p.cols, p.wide, h);
-                if (p.dsum) load_row<W>(qs, first, p.cols, p.wide, ds);
-                load_weights<W>(p.weight, p.fp32, first, p.cols, p.wide, w);
-            }
-            uint32_t out[8];
-            float v[16];
+        copy_async_commit();
+    };
+    if (STAGED)
+        for (int i = 0; i < kNormStages - 1; ++i) fetch(blockIdx.x + size_t(i) * gridDim.x, mine + i * per_stage);
+
+    int turn = 0, stage = 0;
+    float next = p.factors[blockIdx.x];
+    for (size_t row = blockIdx.x; row < size_t(p.rows); row += gridDim.x, turn ^= 1) {
+        const float r = next;
+        if (row + gridDim.x < size_t(p.rows)) next = p.factors[row + gridDim.x];
+        const uint16_t* const qy = static_cast<const uint16_t*>(p.dy) + row * p.lddy;
+        const uint16_t* const qh = static_cast<const uint16_t*>(p.sum) + row * p.lds;
+        const uint16_t* const qs = static_cast<const uint16_t*>(p.dsum) + (add ? row * p.ldds : 0);
+        uint32_t dy[N][4], h[N][4];
+        float2 b = make_float2(0.0f, 0.0f);
+        const uint32_t from = mine + stage * per_stage;
+        if (STAGED) {
+            copy_async_wait<kNormStages - 2>();
+            fetch(row + size_t(kNormStages - 1) * gridDim.x, mine + (stage ? stage - 1 : kNormStages - 1) * per_stage);
+            stage = stage == kNormStages - 1 ? 0 : stage + 1;
+        }
+        auto take = [&](int first, int g) {
+            if constexpr (STAGED) {
+                if (column_of<W>(first, 0) < p.cols) {
+                    ld_shared_v4(from + 3 * g * per, dy[g]);
+                    ld_shared_v4(from + (3 * g + 1) * per, h[g]);
+                } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 fh = unpack2(h[i], DT), fy = unpack2(dy[i], DT), s = weight_pair<DT>(w, p.fp32, i, p.offset);
-                const float2 fs = p.dsum ? unpack2(ds[i], DT) : make_float2(0.0f, 0.0f);
-                const float nx = fh.x * r, ny = fh.y * r;
-                out[i] = pack2(fmaf(r, fmaf(-c, nx, fy.x * s.x), fs.x), fmaf(r, fmaf(-c, ny, fy.y * s.y), fs.y), DT);
-                v[2 * i] = fy.x * nx;
-                v[2 * i + 1] = fy.y * ny;
-            }
-            store_row<W>(static_cast<uint16_t*>(p.dx) + row * p.lddx, first, p.cols, p.wide, out);
-            if (once) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[e] += v[e];
-            } else if (part) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int col = column_of<W>(first, e);
-                    if (col < p.cols) part[col] = row == blockIdx.x ? v[e] : part[col] + v[e];
+                    for (int i = 0; i < 4; ++i) dy[g][i] = h[g][i] = 0;
                 }
+            } else {
+                load_row<W>(qy, first, p.cols, dy[g]);
+                load_row<W>(qh, first, p.cols, h[g]);
+            }
+            // past the last column dy and h are 0
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                b = fma_pair(mul_pair(unpack2(dy[g][i], DT), w[g][i]), mul_pair(unpack2(h[g][i], DT), twice(r)), b);
+        };
+        if (G) {
+#pragma unroll
+            for (int g = 0; g < N; ++g) take(g * span, g);
+        } else {
+            for (int first = 0; first < p.cols; first += span) {
+                load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0]);
+                take(first, 0);
+            }
+        }
+        const float c = block_sum(b.x + b.y, shared[turn]) * p.inverse * r;
+        auto give = [&](int first, int g) {
+            uint32_t ds[4], dx[4];
+            if (add) {
+                if constexpr (STAGED) ld_shared_v4(from + (3 * g + 2) * per, ds);      // past the last column nothing is written
+                else load_row<W>(qs, first, p.cols, ds);
+            }
+            float2 dw[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 y = unpack2(dy[g][i], DT), n = mul_pair(unpack2(h[g][i], DT), twice(r));
+                float2 d = add ? unpack2(ds[i], DT) : make_float2(0.0f, 0.0f);
+                d = fma_pair(twice(-c), n, fma_pair(twice(r), mul_pair(y, w[g][i]), d));
+                dx[i] = pack2(d.x, d.y, DT);
+                if (G) acc[g][i] = fma_pair(y, n, acc[g][i]);
+                else dw[i] = mul_pair(y, n);
+            }
+            store_row<W>(static_cast<uint16_t*>(p.dx) + row * p.lddx, first, p.cols, dx);
+            if (!G && part) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = column_of<W>(first, e);
+                    const float v = e & 1 ? dw[e / 2].y : dw[e / 2].x;
+                    if (at < p.cols) part[at] = row == blockIdx.x ? v : part[at] + v;
+                }
+            }
+        };
+        if (G) {
+#pragma unroll
+            for (int g = 0; g < N; ++g) give(g * span, g);
+        } else {
+            for (int first = 0; first < p.cols; first += span) {
+                load_row<W>(qy, first, p.cols, dy[0]);
+                load_row<W>(qh, first, p.cols, h[0]);
+                load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0]);
+                give(first, 0);
             }
         }
     }
-    if (once && part) {
+    if (G && part) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int col = column_of<W>(0, e);
-            if (col < p.cols) part[col] = acc[e];
-        }
+        for (int g = 0; g < N; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int at = column_of<W>(g * span, e);
+                if (at < p.cols) part[at] = e & 1 ? acc[g][e / 2].y : acc[g][e / 2].x;
+            }
     }
 }
 
-// the parts of 32 columns, 8 threads a column, in a fixed order
+// the parts of 32 columns, 32 threads a column, in a fixed order
 template <int DT>
-__global__ void __launch_bounds__(256) norm_parts_kernel(const __grid_constant__ NormGradArgs p) {
-    __shared__ float shared[8][32];
+__global__ void __launch_bounds__(1024) norm_parts_kernel(const __grid_constant__ NormGradArgs p) {
+    __shared__ float shared[32][33];
     const int lane = threadIdx.x & 31, which = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     grid_launch();
     grid_wait();
     float v = 0.0f;
     if (col < p.cols) {
-#pragma unroll 8
-        for (int i = which; i < p.count; i += 8) v += __ldcg(p.parts + size_t(i) * p.cols + col);
+#pragma unroll 4
+        for (int i = which; i < p.count; i += 32) v += __ldcg(p.parts + size_t(i) * p.cols + col);
     }
     shared[which][lane] = v;
     __syncthreads();
-    if (which || col >= p.cols) return;
+    // a warp takes a column
+    v = shared[lane][which];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += shared[i][lane];
-    store1(p.dw, col, v, p.fp32 ? int(kFp32) : DT);
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    const int mine = blockIdx.x * 32 + which;
+    if (lane == 0 && mine < p.cols) store1(p.dw, mine, v, p.fp32 ? int(kFp32) : DT);
 }
 
 }  // namespace ff
