@@ -27,12 +27,12 @@ struct Access {
     int width() const { return unit >= 16 ? 8 : unit >= 4 ? 2 : 1; }
 };
 
-// Groups of 8 columns for each thread: as few threads as hold a row, up to 256 of them, since each thread's part in the
-// row's reduction costs as much as 8 columns do.  0: a row that no CTA holds.
-inline int norm_groups(size_t cols) { return cols > size_t(kNormOnce) ? 0 : int(ceil_div(cols, kNormColumns)); }
-inline int norm_threads(size_t cols) {
-    const int groups = norm_groups(cols);
-    return groups ? int(up(ceil_div(cols, 8 * groups), 32)) : kNormThreads;
+// Groups of 8 columns for each thread of the backward pass: as few threads as hold a row, up to 224 of them, since each
+// thread's part in the row's reduction costs as much as 8 columns do.  0: a row that no CTA holds.
+inline int grad_groups(size_t cols) { return cols > size_t(kGradGroups * kGradColumns) ? 0 : int(ceil_div(cols, kGradColumns)); }
+inline int grad_threads(size_t cols) {
+    const int groups = grad_groups(cols);
+    return groups ? int(up(ceil_div(cols, 8 * groups), 32)) : kGradThreads;
 }
 
 // both are the same matrix: each element is read before it is written by the same thread
@@ -40,7 +40,7 @@ inline bool same(const void* p, size_t ldp, const void* q, size_t ldq, size_t ro
 
 template <int DT, int W, bool EIGHT>
 int launch_norm(const NormArgs& a, cudaStream_t stream) {
-    const size_t end = EIGHT ? fp8_stages(a.cols) * 128 : a.cols;
+    const size_t end = EIGHT ? size_t(a.stages) * 128 : a.cols;
     const int threads = int(std::min<size_t>(kRowThreads, up(ceil_div(end, 8), 32)));
     return launch(end > size_t(kRowThreads) * 8 ? norm_kernel<DT, W, EIGHT, true> : norm_kernel<DT, W, EIGHT, false>, dim3(unsigned(a.rows)),
                   threads, 0, 1, a, stream);
@@ -58,17 +58,18 @@ int launch_norm(const NormArgs& a, int dtype, int width, cudaStream_t stream) {
 
 template <int DT, int W, int G>
 int launch_grad(const NormGradArgs& a, int threads, cudaStream_t stream) {
-    return launch(norm_grad_kernel<DT, W, G>, dim3(unsigned(a.count)), threads, W == 8 ? size_t(kNormStages) * 3 * 16 * G * threads : 0, 1,
+    return launch(norm_grad_kernel<DT, W, G>, dim3(unsigned(a.count)), threads, W == 8 ? size_t(kGradStages) * 3 * 16 * G * threads : 0, 1,
                   a, stream, true);
 }
 template <int DT, int W>
 int launch_grad(const NormGradArgs& a, cudaStream_t stream) {
-    const int threads = norm_threads(a.cols);
-    switch (norm_groups(a.cols)) {
+    const int threads = grad_threads(a.cols);
+    switch (grad_groups(a.cols)) {
         case 1: return launch_grad<DT, W, 1>(a, threads, stream);
         case 2: return launch_grad<DT, W, 2>(a, threads, stream);
         case 3: return launch_grad<DT, W, 3>(a, threads, stream);
         case 4: return launch_grad<DT, W, 4>(a, threads, stream);
+        case 5: return launch_grad<DT, W, 5>(a, threads, stream);
         default: return launch_grad<DT, W, 0>(a, threads, stream);
     }
 }
@@ -120,10 +121,10 @@ int check_sum(const void* x, size_t ldx, const void* residual, size_t ldr, const
     return overlap(s, Span{weight, cols * size_of(weight_dtype)}) ? EQUARX_ERR_ALIAS : EQUARX_OK;
 }
 
-// CTAs of the backward pass, each with a part of the weight's gradient: two for each of 148 SMs (more where rows are
-// short), two rows at least for each, and not so many that the parts of very long rows outgrow the matrices
+// CTAs of the backward pass, each with a part of the weight's gradient: as many as run at one time on 148 SMs (three on each,
+// more where rows are short), two rows at least for each, and not so many that the parts of very long rows outgrow the matrices
 inline size_t norm_parts(size_t rows, size_t cols) {
-    const size_t most = 148 * std::max<size_t>(2, std::min<size_t>(8, 512 / norm_threads(cols)));
+    const size_t most = 148 * std::max<size_t>(1, std::min<size_t>(8, (grad_groups(cols) > 3 ? 1 : 3) * kGradThreads / grad_threads(cols)));
     return std::min({ceil_div(rows, 2), most, std::max<size_t>(1, (size_t(1) << 28) / cols)});
 }
 
@@ -170,6 +171,7 @@ int equarx_add_rms_norm_fp8(const void* x, size_t ldx, const void* residual, siz
     set_inputs(a, x, ldx, residual, ldr, weight, weight_dtype, rows, cols, eps, offset, sum, lds, access);
     a.codes = codes;
     a.scales = scales;
+    a.stages = int(fp8_stages(cols));
     return launch_norm<true>(a, dtype, access.width(), stream);
 }
 

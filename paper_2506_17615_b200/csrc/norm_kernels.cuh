@@ -12,12 +12,10 @@ namespace ff {
 
 using namespace tc;
 
-constexpr int kNormThreads = 256;          // at most
-constexpr int kNormColumns = kNormThreads * 8;
-constexpr int kNormGroups = 4;             // groups of 8 elements that a thread holds, at most
-constexpr int kNormOnce = kNormGroups * kNormColumns;        // columns that a CTA holds in registers
-constexpr int kNormStages = 3;             // rows in shared memory, where rows are copied ahead
-
+constexpr int kGradThreads = 224;          // of the backward pass, at most
+constexpr int kGradColumns = kGradThreads * 8;
+constexpr int kGradGroups = 5;             // groups of 8 columns for each of its threads, at most
+constexpr int kGradStages = 2;             // its rows in shared memory
 constexpr int kRowThreads = 1024;          // of the forward pass, at most
 
 // Eight elements of a row in a thread's registers, pairs of neighbours.  W = 8: all neighbours, for rows that start on
@@ -125,12 +123,15 @@ struct NormArgs {
     double inverse, eps;                   // 1 / columns
     float offset;
     int rows, cols, fp32;                  // fp32: the weight's type
+    int stages;                            // EIGHT: of 128 columns
 };
 
 // the codes and scales of eight elements of a row, from column `first` on; scales end at column `end`
 template <int W>
-__device__ __forceinline__ void store_fp8(const NormArgs& p, uint8_t* codes, uint8_t* scales, int first, int end, float2 (&v)[4]) {
-    const int stride = int(fp8_stride(p.cols));
+__device__ __forceinline__ void store_fp8(const NormArgs& p, size_t row, int first, int end, float2 (&v)[4]) {
+    const int stride = (p.cols + 31) & ~31;
+    uint8_t* const codes = p.codes + row * uint32_t(stride);
+    auto scales = [&] { return p.scales + fp8_scale_offset(row, 0, p.stages); };
     // 0 past the last column, also where r is not finite
     if (column_of<W>(first, 7) >= p.cols) {
 #pragma unroll
@@ -153,7 +154,7 @@ __device__ __forceinline__ void store_fp8(const NormArgs& p, uint8_t* codes, uin
             *reinterpret_cast<uint2*>(codes + col) = make_uint2(encode_e4m3(v[0].x, v[0].y) | encode_e4m3(v[1].x, v[1].y) << 16,
                                                                 encode_e4m3(v[2].x, v[2].y) | encode_e4m3(v[3].x, v[3].y) << 16);
         const uint32_t word = gather_scales<4>(byte);
-        if (threadIdx.x % 16 == 0 && col < end) *reinterpret_cast<uint32_t*>(scales + size_t(col / 128) * 512) = word;
+        if (threadIdx.x % 16 == 0 && col < end) *reinterpret_cast<uint32_t*>(scales() + (col / 128) * size_t(512)) = word;
     } else {
 #pragma unroll
         for (int e = 0; e < 8; e += W) {
@@ -169,7 +170,7 @@ __device__ __forceinline__ void store_fp8(const NormArgs& p, uint8_t* codes, uin
                 if (W == 2) *reinterpret_cast<uint16_t*>(codes + col) = uint16_t(code);
                 else codes[col] = uint8_t(code);
             }
-            if (col % 32 == 0 && col < end) scales[size_t(col / 128) * 512 + col / 32 % 4] = uint8_t(byte);
+            if (col % 32 == 0 && col < end) scales()[(col / 128) * size_t(512) + col / 32 % 4] = uint8_t(byte);
         }
     }
 }
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(kRowThreads) norm_kernel(const __grid_constant
     __shared__ float root;
     const int span = blockDim.x * 8, warps = blockDim.x / 32, lane = threadIdx.x & 31;
     const size_t row = blockIdx.x;
-    const int end = EIGHT ? int(fp8_stages(p.cols) * 128) : p.cols;
+    const int end = EIGHT ? p.stages * 128 : p.cols;
     const bool add = p.residual != nullptr;
     const uint16_t* const x = static_cast<const uint16_t*>(p.x) + row * p.ldx;
     const uint16_t* const residual = static_cast<const uint16_t*>(p.residual) + row * p.ldr;
@@ -234,8 +235,6 @@ __global__ void __launch_bounds__(kRowThreads) norm_kernel(const __grid_constant
     __syncthreads();
     const float r = root;
 
-    uint8_t* const codes = p.codes + row * fp8_stride(p.cols);
-    uint8_t* const scales = p.scales + fp8_scale_offset(row, 0, fp8_stages(p.cols));
     for (int first = 0; first < (LONG ? end : 1); first += span) {
         if (LONG) {
             load_row<W>(add ? sum : x, first, p.cols, h);
@@ -245,7 +244,7 @@ __global__ void __launch_bounds__(kRowThreads) norm_kernel(const __grid_constant
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = mul_pair(mul_pair(unpack2(h[i], DT), twice(r)), w[i]);
         if constexpr (EIGHT) {
-            store_fp8<W>(p, codes, scales, first, end, v);
+            store_fp8<W>(p, row, first, end, v);
         } else {
             uint32_t out[4];
 #pragma unroll
@@ -268,14 +267,16 @@ struct NormGradArgs {
 };
 
 // n = sum r, g = dy (offset + weight):  dx = dsum + r g - (r mean(g n)) n, dweight = sum over rows of dy n.
-// A CTA takes every gridDim-th row, a thread the same columns of each, whose weight gradients it adds up in registers (G = 0:
-// in its part in memory).  W = 8: the next rows are copied ahead, as above.
+// A CTA takes every gridDim-th row, a thread the same G groups of 8 columns of each, whose weight gradients it adds up in
+// registers.  W = 8: a row is copied to shared memory while the one before it is worked on; a thread copies and reads its own
+// elements, so no barrier is needed for them, and reads them twice, so that registers hold weights and sums only.  G = 0: rows that
+// this does not hold; sums in the CTA's part in memory.
 template <int DT, int W, int G>
-__global__ void __launch_bounds__(kNormThreads, G == 4 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
+__global__ void __launch_bounds__(kGradThreads, G > 3 ? 1 : 3) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
     constexpr bool STAGED = W == 8 && G > 0;
     constexpr int N = G ? G : 1;
     extern __shared__ __align__(16) uint8_t staged[];
-    __shared__ float shared[2][32];
+    __shared__ float shared[2][32];        // a thread writes one again only after the barrier of the row between
     const int span = blockDim.x * 8;
     const bool add = p.dsum != nullptr;
     float* const part = p.parts ? p.parts + size_t(blockIdx.x) * p.cols : nullptr;
@@ -307,62 +308,56 @@ __global__ void __launch_bounds__(kNormThreads, G == 4 ? 1 : 2) norm_grad_kernel
         copy_async_commit();
     };
     if (STAGED)
-        for (int i = 0; i < kNormStages - 1; ++i) fetch(blockIdx.x + size_t(i) * gridDim.x, mine + i * per_stage);
+        for (int i = 0; i < kGradStages; ++i) fetch(blockIdx.x + size_t(i) * gridDim.x, mine + i * per_stage);
 
     int turn = 0, stage = 0;
     float next = p.factors[blockIdx.x];
     for (size_t row = blockIdx.x; row < size_t(p.rows); row += gridDim.x, turn ^= 1) {
         const float r = next;
         if (row + gridDim.x < size_t(p.rows)) next = p.factors[row + gridDim.x];
-        const uint16_t* const qy = static_cast<const uint16_t*>(p.dy) + row * p.lddy;
-        const uint16_t* const qh = static_cast<const uint16_t*>(p.sum) + row * p.lds;
-        const uint16_t* const qs = static_cast<const uint16_t*>(p.dsum) + (add ? row * p.ldds : 0);
-        uint32_t dy[N][4], h[N][4];
-        float2 b = make_float2(0.0f, 0.0f);
         const uint32_t from = mine + stage * per_stage;
-        if (STAGED) {
-            copy_async_wait<kNormStages - 2>();
-            fetch(row + size_t(kNormStages - 1) * gridDim.x, mine + (stage ? stage - 1 : kNormStages - 1) * per_stage);
-            stage = stage == kNormStages - 1 ? 0 : stage + 1;
-        }
-        auto take = [&](int first, int g) {
+        if (STAGED) copy_async_wait<kGradStages - 1>();
+        // eight elements of dy, sum and dsum; past the last column the first two are 0
+        auto load = [&](int first, int g, uint32_t (&dy)[4], uint32_t (&h)[4], uint32_t* ds) {
             if constexpr (STAGED) {
                 if (column_of<W>(first, 0) < p.cols) {
-                    ld_shared_v4(from + 3 * g * per, dy[g]);
-                    ld_shared_v4(from + (3 * g + 1) * per, h[g]);
+                    ld_shared_v4(from + 3 * g * per, dy);
+                    ld_shared_v4(from + (3 * g + 1) * per, h);
+                    if (ds && add) ld_shared_v4(from + (3 * g + 2) * per, *reinterpret_cast<uint32_t(*)[4]>(ds));
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dy[g][i] = h[g][i] = 0;
+                    for (int i = 0; i < 4; ++i) dy[i] = h[i] = 0;
                 }
             } else {
-                load_row<W>(qy, first, p.cols, dy[g]);
-                load_row<W>(qh, first, p.cols, h[g]);
+                load_row<W>(static_cast<const uint16_t*>(p.dy) + row * p.lddy, first, p.cols, dy);
+                load_row<W>(static_cast<const uint16_t*>(p.sum) + row * p.lds, first, p.cols, h);
+                if (ds && add)
+                    load_row<W>(static_cast<const uint16_t*>(p.dsum) + row * p.ldds, first, p.cols, *reinterpret_cast<uint32_t(*)[4]>(ds));
             }
-            // past the last column dy and h are 0
+            if (!G) load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0]);
+        };
+        float2 b = make_float2(0.0f, 0.0f);
+        auto take = [&](int first, int g) {
+            uint32_t dy[4], h[4];
+            load(first, g, dy, h, nullptr);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                b = fma_pair(mul_pair(unpack2(dy[g][i], DT), w[g][i]), mul_pair(unpack2(h[g][i], DT), twice(r)), b);
+                b = fma_pair(mul_pair(unpack2(dy[i], DT), w[g][i]), mul_pair(unpack2(h[i], DT), twice(r)), b);
         };
         if (G) {
 #pragma unroll
             for (int g = 0; g < N; ++g) take(g * span, g);
         } else {
-            for (int first = 0; first < p.cols; first += span) {
-                load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0]);
-                take(first, 0);
-            }
+            for (int first = 0; first < p.cols; first += span) take(first, 0);
         }
         const float c = block_sum(b.x + b.y, shared[turn]) * p.inverse * r;
         auto give = [&](int first, int g) {
-            uint32_t ds[4], dx[4];
-            if (add) {
-                if constexpr (STAGED) ld_shared_v4(from + (3 * g + 2) * per, ds);      // past the last column nothing is written
-                else load_row<W>(qs, first, p.cols, ds);
-            }
+            uint32_t dy[4], h[4], ds[4], dx[4];
+            load(first, g, dy, h, ds);
             float2 dw[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 y = unpack2(dy[g][i], DT), n = mul_pair(unpack2(h[g][i], DT), twice(r));
+                const float2 y = unpack2(dy[i], DT), n = mul_pair(unpack2(h[i], DT), twice(r));
                 float2 d = add ? unpack2(ds[i], DT) : make_float2(0.0f, 0.0f);
                 d = fma_pair(twice(-c), n, fma_pair(twice(r), mul_pair(y, w[g][i]), d));
                 dx[i] = pack2(d.x, d.y, DT);
@@ -383,12 +378,11 @@ __global__ void __launch_bounds__(kNormThreads, G == 4 ? 1 : 2) norm_grad_kernel
 #pragma unroll
             for (int g = 0; g < N; ++g) give(g * span, g);
         } else {
-            for (int first = 0; first < p.cols; first += span) {
-                load_row<W>(qy, first, p.cols, dy[0]);
-                load_row<W>(qh, first, p.cols, h[0]);
-                load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0]);
-                give(first, 0);
-            }
+            for (int first = 0; first < p.cols; first += span) give(first, 0);
+        }
+        if (STAGED) {
+            fetch(row + size_t(kGradStages) * gridDim.x, from);
+            stage = stage == kGradStages - 1 ? 0 : stage + 1;
         }
     }
     if (G && part) {
