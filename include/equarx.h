@@ -648,12 +648,14 @@ int equarx_add_rms_norm_backward(const void *dy, size_t lddy, const void *dsum, 
  * not finite in one adapter or token reaches no token of another adapter.  rank is 1 to 128;
  * adapters of lower rank are padded with zeros.  out may be y itself.  Under tensor
  * parallelism with k split over the ranks, a rank passes its columns of A, and the AllReduce
- * of the outputs adds the adapters' parts too.
+ * of the outputs adds the adapters' parts too.  For a few tokens the workspace is 0 bytes.
  */
+size_t equarx_add_adapters_workspace_bytes(size_t tokens, size_t rank);
 int equarx_add_adapters(const void *y, size_t ldy, const void *x, size_t ldx,
                         const void *a, const void *b, const int32_t *index, const float *scale,
                         int dtype, size_t tokens, size_t n, size_t k, size_t rank, size_t adapters,
-                        void *out, size_t ldo, equarx_stream_t stream);
+                        void *out, size_t ldo, void *workspace, size_t workspace_bytes,
+                        equarx_stream_t stream);
 
 /*
  * The kernels of the feed-forward calls wait only for copies and products of their own

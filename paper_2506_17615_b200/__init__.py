@@ -32,6 +32,7 @@ _BINDING_NAMES = (
     "LIB_PATH",
     "MAX_RANKS",
     "add_adapters",
+    "add_adapters_workspace_bytes",
     "add_rms_norm",
     "add_rms_norm_backward",
     "add_rms_norm_backward_workspace_bytes",

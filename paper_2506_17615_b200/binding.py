@@ -62,6 +62,7 @@ EXPORTS = (
     "equarx_add_rms_norm_backward",
     "equarx_add_rms_norm_backward_workspace_bytes",
     "equarx_add_adapters",
+    "equarx_add_adapters_workspace_bytes",
     "equarx_feedforward_check",
     "equarx_status_string",
     "equarx_last_cuda_error",
@@ -126,8 +127,9 @@ def _load():
     lib.equarx_add_rms_norm_fp8.argtypes = [vp, sz, vp, sz, vp, ci, ci, sz, sz, cd, cf, vp, sz, vp, vp, vp]
     lib.equarx_add_rms_norm_backward_workspace_bytes.argtypes = [sz, sz]
     lib.equarx_add_rms_norm_backward.argtypes = [vp, sz, vp, sz, vp, sz, vp, vp, ci, ci, sz, sz, cf, vp, sz, vp, vp, sz, vp]
-    lib.equarx_add_adapters.argtypes = [vp, sz, vp, sz, vp, vp, vp, vp, ci, sz, sz, sz, sz, sz, vp, sz, vp]
-    for name in ("fp8_codes_bytes", "fp8_scales_bytes", "add_rms_norm_backward_workspace_bytes"):
+    lib.equarx_add_adapters_workspace_bytes.argtypes = [sz, sz]
+    lib.equarx_add_adapters.argtypes = [vp, sz, vp, sz, vp, vp, vp, vp, ci, sz, sz, sz, sz, sz, vp, sz, vp, sz, vp]
+    for name in ("fp8_codes_bytes", "fp8_scales_bytes", "add_rms_norm_backward_workspace_bytes", "add_adapters_workspace_bytes"):
         getattr(lib, "equarx_" + name).restype = sz
     for name in ("fp4_codes_bytes", "fp4_scales_bytes", "fp4_linear_workspace_bytes", "gated_forward_workspace_bytes",
                  "gated_backward_workspace_bytes"):
@@ -405,9 +407,13 @@ def add_rms_norm_backward(dy, lddy, dsum, ldds, sum, lds, factors, weight, dtype
            "equarx_add_rms_norm_backward")
 
 
-def add_adapters(y, ldy, x, ldx, a, b, index, scale, dtype, tokens, n, k, rank, adapters, out, ldo, stream=0):
+def add_adapters_workspace_bytes(tokens, rank):
+    return lib.equarx_add_adapters_workspace_bytes(tokens, rank)
+
+
+def add_adapters(y, ldy, x, ldx, a, b, index, scale, dtype, tokens, n, k, rank, adapters, out, ldo, workspace, workspace_bytes, stream=0):
     _check(lib.equarx_add_adapters(_ptr(y), ldy, _ptr(x), ldx, _ptr(a), _ptr(b), _ptr(index), _ptr(scale), dtype, tokens, n, k, rank,
-                                   adapters, _ptr(out), ldo, _ptr(stream)),
+                                   adapters, _ptr(out), ldo, _ptr(workspace), workspace_bytes, _ptr(stream)),
            "equarx_add_adapters")
 
 

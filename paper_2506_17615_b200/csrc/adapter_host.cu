@@ -10,53 +10,74 @@ using namespace equarx::host;
 
 constexpr size_t kMaxRank = 128;
 
-// Tokens of a cluster and CTAs of it.
-void plan(AdapterArgs& a, int sms) {
-    a.ctas = 4;
-    a.tile = 1;
-    while (a.tile < kAdapterTokens && ceil_div(a.tokens, a.tile) > size_t(sms)) a.tile *= 2;
-    if (a.tile == 1 && a.tokens * 8 <= 2 * sms) a.ctas = 8;
+// Tokens up to which each has a cluster of its own.
+constexpr size_t kTokenForm = 96;
+
+inline size_t padded_rank(size_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+// a token's S, high and low
+inline size_t sums_bytes(size_t tokens, size_t rank) { return up(tokens * padded_rank(rank) * 4, 256); }
+inline size_t adapter_workspace(size_t tokens, size_t rank) {
+    return tokens <= kTokenForm ? 0 : sums_bytes(tokens, rank) + up(tokens * sizeof(float), 256);
 }
 
+template <int DT, int RT, bool VEC>
+int launch_adapters(AdapterArgs& a, int sms, cudaStream_t stream) {
+    if (size_t(a.tokens) <= kTokenForm) {
+        a.ctas = a.tokens * 8 <= 2 * sms ? 8 : 4;
+        return launch(adapter_token_kernel<DT, RT, VEC>, dim3(unsigned(a.tokens) * a.ctas), kAdapterThreads, 0, unsigned(a.ctas), a, stream);
+    }
+    // two CTAs run on an SM: where there are few tiles, up to eight share one
+    const size_t tiles = ceil_div(a.tokens, kDownTokens);
+    a.ctas = 1;
+    while (a.ctas < 8 && tiles * a.ctas * 2 <= size_t(2 * sms)) a.ctas *= 2;
+    TRY(launch(adapter_down_kernel<DT, RT, VEC>, dim3(unsigned(tiles * a.ctas)), kAdapterThreads, 0, unsigned(a.ctas), a, stream));
+    const size_t up_tiles = ceil_div(a.tokens, kUpTokens), all = ceil_div(a.n, 32);
+    // about eight CTAs for each SM, and eight blocks of features at least for each
+    const size_t parts = std::max<size_t>(1, std::min(ceil_div(size_t(8 * sms), up_tiles), all / 8));
+    a.blocks = int(ceil_div(all, parts));
+    return launch(adapter_up_kernel<DT, RT, VEC>, dim3(unsigned(up_tiles), unsigned(ceil_div(all, a.blocks))), 32 * kUpWarps, 0, 1, a, stream);
+}
 template <int DT, int RT>
-int launch_rank(AdapterArgs& a, bool vec, cudaStream_t stream) {
-    const int groups = int(ceil_div(a.tile, 8 * kAdapterGroups<RT>));
-    a.split = kAdapterWarps / (groups > 2 ? 4 : groups);
-    const dim3 grid(unsigned(ceil_div(a.tokens, a.tile) * a.ctas));
-    const size_t smem = adapter_smem<RT>(a.tile, a.split);
-    return launch(vec ? adapters_kernel<DT, RT, true> : adapters_kernel<DT, RT, false>, grid, kAdapterThreads, smem, unsigned(a.ctas), a,
-                  stream);
+int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
+    return vec ? launch_adapters<DT, RT, true>(a, sms, stream) : launch_adapters<DT, RT, false>(a, sms, stream);
 }
 template <int DT>
-int launch_type(AdapterArgs& a, bool vec, cudaStream_t stream) {
-    if (a.rank <= 16) return launch_rank<DT, 1>(a, vec, stream);
-    if (a.rank <= 32) return launch_rank<DT, 2>(a, vec, stream);
-    if (a.rank <= 64) return launch_rank<DT, 4>(a, vec, stream);
-    return launch_rank<DT, 8>(a, vec, stream);
+int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
+    if (a.rank <= 16) return launch_adapters<DT, 1>(a, vec, sms, stream);
+    if (a.rank <= 32) return launch_adapters<DT, 2>(a, vec, sms, stream);
+    if (a.rank <= 64) return launch_adapters<DT, 4>(a, vec, sms, stream);
+    return launch_adapters<DT, 8>(a, vec, sms, stream);
 }
 
 }  // namespace
 
 extern "C" {
 
+size_t equarx_add_adapters_workspace_bytes(size_t tokens, size_t rank) {
+    return tokens > kMaxDim || rank == 0 || rank > kMaxRank ? 0 : adapter_workspace(tokens, rank);
+}
+
 int equarx_add_adapters(const void* y, size_t ldy, const void* x, size_t ldx, const void* a, const void* b, const int32_t* index,
                         const float* scale, int dtype, size_t tokens, size_t n, size_t k, size_t rank, size_t adapters, void* out,
-                        size_t ldo, equarx_stream_t stream) {
+                        size_t ldo, void* workspace, size_t workspace_bytes, equarx_stream_t stream) {
     if (!is_16bit(dtype)) return EQUARX_ERR_FORMAT;
     if (tokens > kMaxDim || bad_dim(n) || bad_dim(k) || rank == 0 || rank > kMaxRank || adapters > kMaxDim || bad_ld(ldy, n) ||
         bad_ld(ldx, k) || bad_ld(ldo, n))
         return EQUARX_ERR_COUNT;
     if (tokens == 0) return EQUARX_OK;
-    if (!y || !x || !index || !out || (adapters && (!a || !b))) return EQUARX_ERR_NULL;
+    const size_t need = adapter_workspace(tokens, rank);
+    if (!y || !x || !index || !out || (adapters && (!a || !b)) || (need && !workspace)) return EQUARX_ERR_NULL;
+    if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
     for (const void* p : {y, x, a, b, static_cast<const void*>(out)})
         if (!aligned(p, 2)) return EQUARX_ERR_ALIGN;
-    if (!aligned(index, 4) || !aligned(scale, 4)) return EQUARX_ERR_ALIGN;
+    if (!aligned(index, 4) || !aligned(scale, 4) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
     const Span o = matrix(out, tokens, n, ldo, 2);
     // out may be y: each element is read before the same thread writes it
-    if (!(out == y && (ldo == ldy || tokens == 1)) && overlap(o, matrix(y, tokens, n, ldy, 2))) return EQUARX_ERR_ALIAS;
+    const Span ys = matrix(y, tokens, n, ldy, 2), ws{need ? workspace : nullptr, need};
+    if ((!(out == y && (ldo == ldy || tokens == 1)) && overlap(o, ys)) || overlap(ws, ys)) return EQUARX_ERR_ALIAS;
     TRY(check_overlap({matrix(x, tokens, k, ldx, 2), Span{a, adapters * rank * k * 2}, Span{b, adapters * rank * n * 2},
                        Span{index, tokens * 4}, Span{scale, adapters * 4}},
-                      {o}));
+                      {o, ws}));
     AdapterArgs p = {};
     p.y = y;
     p.x = x;
@@ -65,6 +86,8 @@ int equarx_add_adapters(const void* y, size_t ldy, const void* x, size_t ldx, co
     p.index = index;
     p.scale = scale;
     p.out = out;
+    p.s = static_cast<uint16_t*>(workspace);
+    p.back = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sums_bytes(tokens, rank));
     p.ldy = ldy;
     p.ldx = ldx;
     p.ldo = ldo;
@@ -75,10 +98,9 @@ int equarx_add_adapters(const void* y, size_t ldy, const void* x, size_t ldx, co
     p.adapters = int(adapters);
     int sms;
     TRY(current_device(sms));
-    plan(p, sms);
     bool vec = k % 8 == 0 && n % 8 == 0 && rank % 8 == 0 && aligned(a, 16) && aligned(b, 16);
     vec = vec && unit_of(y, ldy, 2) >= 16 && unit_of(x, ldx, 2) >= 16 && unit_of(out, ldo, 2) >= 16;
-    return dtype == EQUARX_BF16 ? launch_type<kBf16>(p, vec, stream) : launch_type<kFp16>(p, vec, stream);
+    return dtype == EQUARX_BF16 ? launch_adapters<kBf16>(p, vec, sms, stream) : launch_adapters<kFp16>(p, vec, sms, stream);
 }
 
 }  // extern "C"

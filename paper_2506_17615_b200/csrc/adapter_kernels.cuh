@@ -1,4 +1,8 @@
 // Low-rank adapters of many requests beside a shared projection.
+//
+//   adapter_token_kernel   few tokens: a cluster each, dot products in fp32
+//   adapter_down_kernel    many tokens: S = x A^T, split into high and low halves of 16 bits
+//   adapter_up_kernel      and out = y + S B^T
 #pragma once
 #include "elements.cuh"
 #include "tensor_ops.cuh"
@@ -14,26 +18,139 @@ struct AdapterArgs {
     const int* index;
     const float* scale;               // c, or null: 1
     void* out;
+    uint16_t* s;                      // many tokens: [tokens][high, low][ranks]
+    float* back;                      // and what a token's S has been divided by
     size_t ldy, ldx, ldo;
     int tokens, k, n, rank, adapters;
-    int tile;                         // tokens of a cluster, at most 64
-    int split;                        // ways in which the warps of a CTA split its part of k; they split the tokens 8 / split ways
-    int ctas;                         // of a cluster
+    int ctas;                         // of a cluster, which split k (and, for few tokens, n)
+    int blocks;                       // of 32 features, that a CTA of the second product takes
 };
-constexpr int kAdapterWarps = 8, kAdapterThreads = 32 * kAdapterWarps, kAdapterTokens = 64;
+constexpr int kAdapterWarps = 8, kAdapterThreads = 32 * kAdapterWarps;
+// ranks are padded to 16 RT, RT = 1, 2, 4 or 8
 
-// ranks are padded to 16 RT
-template <int RT> constexpr int kAdapterGroups = RT <= 2 ? 8 : RT == 4 ? 4 : 2;      // groups of 8 tokens that a warp holds sums of
-template <int RT> constexpr int kPackedStride = 16 * RT + 4;                          // of a token, in 16-bit elements
-// shared memory: the warps' sums (later the packed ones, high and low halves), the CTA's sums
-template <int RT>
-__host__ __device__ constexpr int adapter_sums(int tile) { return tile * 16 * RT * 4; }
-template <int RT>
-__host__ __device__ constexpr int adapter_smem(int tile, int split) {
-    const int warps = split * adapter_sums<RT>(tile), packed = 2 * ((tile + 15) / 16 * 16) * kPackedStride<RT> * 2;
-    return (warps > packed ? warps : packed) + adapter_sums<RT>(tile);
+// eight neighbouring elements of a row from `col` on, as pairs; zero past `cols`.  VEC: rows start on multiples of 16 bytes and
+// have a multiple of 8 elements
+template <bool VEC>
+__device__ __forceinline__ void load_eight(const uint16_t* row, int col, int cols, uint32_t* v) {
+    if (VEC) {
+        const uint4 q = col < cols ? *reinterpret_cast<const uint4*>(row + col) : make_uint4(0, 0, 0, 0);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = (col + 2 * i < cols ? row[col + 2 * i] : 0) | uint32_t(col + 2 * i + 1 < cols ? row[col + 2 * i + 1] : 0) << 16;
+    }
+}
+// the adapter of a token, -1: none
+__device__ __forceinline__ int adapter_of(const AdapterArgs& p, int token) {
+    const int i = p.index[token];
+    return i >= 0 && i < p.adapters ? i : -1;
+}
+template <int DT>
+__device__ __forceinline__ float dot_eight(const uint32_t* a, const float2* b, float v) {
+    float2 w = make_float2(v, 0.0f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w = fma_pair(unpack2(a[i], DT), b[i], w);
+    return w.x + w.y;
 }
 
+// ---------------------------------------------------------------- few tokens
+// One cluster for a token: its CTAs split k for S, whose parts they exchange through distributed shared memory, and then n.  Every
+// CTA has asked for its first rows of B before it waits for S.  A lane takes 8 columns of a row of A at a time, RT lanes share a row
+// of B, 16 ranks each: all reads are of neighbouring bytes.  Everything is summed in fp32.  Bound by the chain of start,
+// index, loads, exchange and store.
+template <int DT, int RT, bool VEC>
+__global__ void __launch_bounds__(kAdapterThreads) adapter_token_kernel(const __grid_constant__ AdapterArgs p) {
+    constexpr int ROWS = 2 * RT;                     // of A, for each warp
+    constexpr int AHEAD = 4;                         // parts of B's rows, for each thread
+    __shared__ __align__(16) float mine[16 * RT], total[16 * RT];
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, rank = int(cluster_rank());
+    const size_t token = blockIdx.x / p.ctas;
+    grid_launch();
+    grid_wait();
+    const int d = adapter_of(p, int(token));
+    const uint16_t* const x = static_cast<const uint16_t*>(p.x) + token * p.ldx;
+    const uint16_t* const y = static_cast<const uint16_t*>(p.y) + token * p.ldy;
+    uint16_t* const out = static_cast<uint16_t*>(p.out) + token * p.ldo;
+    const int f0 = int(int64_t(p.n) * rank / p.ctas), f1 = int(int64_t(p.n) * (rank + 1) / p.ctas);
+    if (d < 0) {                                     // all CTAs of the cluster alike
+        for (int f = f0 + tid; f < f1; f += kAdapterThreads) out[f] = y[f];
+        return;
+    }
+    const uint16_t* const a = static_cast<const uint16_t*>(p.a) + size_t(d) * p.rank * p.k;
+    const uint16_t* const b = static_cast<const uint16_t*>(p.b) + size_t(d) * p.n * p.rank;
+
+    // features f0 + tid / RT, and every kAdapterThreads / RT further; ranks 16 (tid % RT) on
+    constexpr int STEP = kAdapterThreads / RT;
+    const int part = tid % RT * 16, mf = f0 + tid / RT;
+    auto load_b = [&](int f, uint32_t (&v)[8]) {
+        const bool in = f < f1;
+        load_eight<VEC>(b + size_t(f) * p.rank, in ? part : p.rank, p.rank, v);
+        load_eight<VEC>(b + size_t(f) * p.rank, in ? part + 8 : p.rank, p.rank, v + 4);
+    };
+    uint32_t ahead[AHEAD][8];
+    uint16_t old[AHEAD];
+    auto load_ahead = [&](int f) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            load_b(f + i * STEP, ahead[i]);
+            old[i] = f + i * STEP < f1 ? y[f + i * STEP] : uint16_t(0);
+        }
+    };
+    load_ahead(mf);
+
+    const int chunks = (p.k + 7) / 8, c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
+    float acc[ROWS] = {};
+#pragma unroll 2
+    for (int c = c0 + lane; c < c1; c += 32) {
+        uint32_t v[4];
+        float2 f[4];
+        load_eight<VEC>(x, c * 8, p.k, v);
+        uint32_t w[ROWS][4];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int r = warp + i * kAdapterWarps;
+            load_eight<VEC>(a + size_t(r) * p.k, r < p.rank ? c * 8 : p.k, p.k, w[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = unpack2(v[i], DT);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) acc[i] = dot_eight<DT>(w[i], f, acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+        for (int s = 16; s; s >>= 1) acc[i] += __shfl_xor_sync(0xFFFFFFFFu, acc[i], s);
+        if (lane == 0) mine[warp + i * kAdapterWarps] = acc[i];
+    }
+    __syncwarp();
+    cluster_sync();
+    if (tid < 16 * RT) {
+        float v = 0.0f;
+        for (int q = 0; q < p.ctas; ++q) v += ld_cluster_f32(peer_addr(smem_addr(mine + tid), q));
+        total[tid] = tid < p.rank ? (p.scale ? v * p.scale[d] : v) : 0.0f;
+    }
+    __syncwarp();
+    cluster_arrive();                                // the others' sums have been read
+    __syncthreads();
+    float2 s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = *reinterpret_cast<const float2*>(total + part + 2 * i);
+    for (int f = mf; f - tid / RT < f1; f += AHEAD * STEP) {
+        if (f != mf) load_ahead(f);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            float v = dot_eight<DT>(ahead[i], s, 0.0f) + dot_eight<DT>(ahead[i] + 4, s + 4, 0.0f);
+#pragma unroll
+            for (int q = RT / 2; q; q >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, q);
+            if (tid % RT == 0 && f + i * STEP < f1) out[f + i * STEP] = uint16_t(pack2(unpack2(old[i], DT).x + v, 0.0f, DT));
+        }
+    }
+    __syncwarp();
+    cluster_wait();
+}
+
+// ---------------------------------------------------------------- many tokens
 template <int DT>
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (DT == kBf16)
@@ -45,178 +162,109 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
-// N (4 or 8) neighbouring elements of a row from `col` on, as pairs; zero past `cols`.  VEC: rows start on multiples of 16
-// bytes and have a multiple of 8 elements
-template <int N, bool VEC>
-__device__ __forceinline__ void load_few(const uint16_t* row, int col, int cols, uint32_t* v) {
-    if (VEC) {
-        if constexpr (N == 8) {
-            const uint4 q = col < cols ? __ldg(reinterpret_cast<const uint4*>(row + col)) : make_uint4(0, 0, 0, 0);
-            v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-        } else {
-            const uint2 q = col < cols ? __ldg(reinterpret_cast<const uint2*>(row + col)) : make_uint2(0, 0);
-            v[0] = q.x; v[1] = q.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i)
-            v[i] = (col + 2 * i < cols ? row[col + 2 * i] : 0) | uint32_t(col + 2 * i + 1 < cols ? row[col + 2 * i + 1] : 0) << 16;
-    }
+// Of up to 32 tokens, one in each lane: bit j is set where token j is the first with its adapter
+__device__ __forceinline__ uint32_t first_of_each(int d) {
+    const uint32_t alike = __match_any_sync(0xFFFFFFFFu, d);
+    return __ballot_sync(0xFFFFFFFFu, d >= 0 && __ffs(alike) == int(threadIdx.x & 31) + 1);
 }
 
-// the same 8 from a row that this kernel may also write
-template <bool VEC>
-__device__ __forceinline__ void load_eight(const uint16_t* row, int col, int cols, uint32_t (&v)[4]) {
-    if (VEC) {
-        if (col >= cols) return;
-        const uint4 q = *reinterpret_cast<const uint4*>(row + col);
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = (col + 2 * i < cols ? row[col + 2 * i] : 0) | uint32_t(col + 2 * i + 1 < cols ? row[col + 2 * i + 1] : 0) << 16;
-    }
-}
-template <bool VEC>
-__device__ __forceinline__ void store_eight(uint16_t* row, int col, int cols, const uint32_t (&v)[4]) {
-    if (VEC) {
-        if (col < cols) *reinterpret_cast<uint4*>(row + col) = make_uint4(v[0], v[1], v[2], v[3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < cols) row[col + i] = uint16_t(v[i / 2] >> (i & 1) * 16);
-    }
-}
-
-// One cluster for `tile` tokens, in two steps: S = x A^T with k split over its CTAs and their warps, then y + S B^T with the
-// output's features split over them.  So x, y and out pass once, a token's adapter is read by one cluster, and there is one
-// launch.  The reading bounds it: the tensor cores are used by mma.sync on fragments that come straight from memory (the
-// reduction axis is permuted alike for both operands, so that a thread's fragments are 16 neighbouring bytes), since a tile
-// of 16 to 64 output columns would not feed tcgen05 anyway.
+// Reading x and y bounds both products, so they use mma.sync on fragments that come straight from memory (the reduction axis is
+// permuted alike for both operands, so that a thread's fragments are 16 neighbouring bytes): with 16 to 128 columns there is no
+// reuse for tcgen05's operands in shared memory to pay for.
 //
-// A product runs once for each adapter that the tokens of a group have, with nothing in the other tokens' places, and only
-// this adapter's tokens take its result: what is not finite in one request's adapter does not reach another request.
+// A product runs once for each adapter that the tokens of a tile have, with nothing in the other tokens' places, and only this
+// adapter's tokens take its result: what is not finite in one request's adapter does not reach another request.
 //
 // S is rounded as the tensor cores want it, to two numbers of the 16-bit type, high and low, whose sum has 16 bits (bf16) or
 // 22: 2^-17 of S.  In fp16 a token's S is scaled by a power of two first, so that its range does not matter.
-template <int DT, int RT, bool VEC>
-__global__ void __launch_bounds__(kAdapterThreads) adapters_kernel(const __grid_constant__ AdapterArgs p) {
-    constexpr int R = 16 * RT, NT = kAdapterGroups<RT>, PS = kPackedStride<RT>;
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ int own[kAdapterTokens];              // each token's adapter, -1: none
-    __shared__ float back[kAdapterTokens];           // what a token's S has been divided by
-    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int rank = int(cluster_rank()), T = p.tile;
-    const int first = int(blockIdx.x / p.ctas) * T, count = min(T, p.tokens - first);
-    const int warps_bytes = adapter_smem<RT>(T, p.split) - adapter_sums<RT>(T);
-    float* const sums = reinterpret_cast<float*>(smem);                      // [split][T][R]
-    float* const mine = reinterpret_cast<float*>(smem + warps_bytes);        // [T][R]
-    uint16_t* const high = reinterpret_cast<uint16_t*>(smem);                // [T to 16][PS]
-    uint16_t* const low = high + (T + 15) / 16 * 16 * PS;
-    const uint16_t* const a = static_cast<const uint16_t*>(p.a);
-    const uint16_t* const b = static_cast<const uint16_t*>(p.b);
 
+// S of 32 tokens, transposed: 16 ranks x 8 tokens a product.  The CTA's warps split ranks above 32 between them, and k, and so do the
+// CTAs of a cluster where there are few tiles.
+constexpr int kDownTokens = 32;
+template <int RT> constexpr int kDownRanks = RT < 2 ? 1 : 2;                              // groups of 16 ranks of a warp
+template <int RT> constexpr int kDownSplit = kAdapterWarps * kDownRanks<RT> / RT;         // ways in which warps split k
+template <int DT, int RT, bool VEC>
+__global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const __grid_constant__ AdapterArgs p) {
+    constexpr int R = 16 * RT, RW = kDownRanks<RT>, SPLIT = kDownSplit<RT>, NT = kDownTokens / 8;
+    __shared__ float sums[SPLIT][kDownTokens][R];    // the first becomes the CTA's sums
+    __shared__ int own[kDownTokens];
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int rank = int(cluster_rank()), first = int(blockIdx.x / p.ctas) * kDownTokens, count = min(kDownTokens, p.tokens - first);
+    const uint16_t* const a = static_cast<const uint16_t*>(p.a);
     grid_launch();
     grid_wait();
-    if (tid < kAdapterTokens) {
-        const int i = tid < count ? p.index[first + tid] : -1;
-        own[tid] = i >= 0 && i < p.adapters ? i : -1;
-    }
+    if (tid < kDownTokens) own[tid] = tid < count ? adapter_of(p, first + tid) : -1;
     __syncthreads();
-    // Of `width` tokens from `at` on: bit j is set where token j is the first of its 32 with its adapter
-    auto leaders = [&](int at, int width) {
-        uint64_t bits = 0;
-        for (int base = 0; base < width; base += 32) {
-            const int d = base + lane < width ? own[at + base + lane] : -1;
-            const uint32_t alike = __match_any_sync(0xFFFFFFFFu, d);
-            bits |= uint64_t(__ballot_sync(0xFFFFFFFFu, d >= 0 && __ffs(alike) == lane + 1)) << base;
-        }
-        return bits;
-    };
 
-    // ---------------------------------------------------- S = x A^T, transposed: 16 ranks x 8 tokens a product
     const int chunks = (p.k + 31) / 32, c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
-    {
-        const int part = warp % p.split, at = warp / p.split * (NT * 8), width = min(NT * 8, kAdapterTokens - at);
-        if (at < count) {
-            const uint16_t* xrow[NT];
-            int adapter[NT];
+    const int part = warp % SPLIT, r0 = warp / SPLIT * (16 * RW);
+    const uint16_t* x[NT];
+    int adapter[NT];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const int token = at + i * 8 + g;
-                adapter[i] = own[token];
-                xrow[i] = static_cast<const uint16_t*>(p.x) + size_t(first + min(token, count - 1)) * p.ldx;
-            }
-            for (uint64_t left = leaders(at, width); left; left &= left - 1) {
-                const int d = own[at + __ffsll(left) - 1];
-                const uint16_t* const arow = a + size_t(d) * p.rank * p.k;
-                float acc[RT][NT][4] = {};
-                bool any[NT];
-#pragma unroll
-                for (int i = 0; i < NT; ++i) any[i] = __any_sync(0xFFFFFFFFu, adapter[i] == d);
+    for (int j = 0; j < NT; ++j) {
+        adapter[j] = own[j * 8 + g];
+        x[j] = static_cast<const uint16_t*>(p.x) + size_t(first + min(j * 8 + g, count - 1)) * p.ldx;
+    }
+    for (uint32_t left = first_of_each(own[lane]); left; left &= left - 1) {
+        const int d = own[__ffs(left) - 1];
+        const uint16_t* const arow = a + size_t(d) * p.rank * p.k;
+        float acc[RW][NT][4] = {};
 #pragma unroll 2
-                for (int c = c0 + part; c < c1; c += p.split) {
-                    const int col = c * 32 + 8 * t;
-                    uint32_t fx[NT][4], fa[RT][2][4];
+        for (int c = c0 + part; c < c1; c += SPLIT) {
+            const int col = c * 32 + 8 * t;
+            uint32_t fx[NT][4], fa[RW][2][4];
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        fx[i][0] = fx[i][1] = fx[i][2] = fx[i][3] = 0;
-                        if (adapter[i] == d) load_few<8, VEC>(xrow[i], col, p.k, fx[i]);
-                    }
+            for (int j = 0; j < NT; ++j) load_eight<VEC>(x[j], adapter[j] == d ? col : p.k, p.k, fx[j]);
 #pragma unroll
-                    for (int i = 0; i < RT; ++i)
+            for (int i = 0; i < RW; ++i)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const int r = i * 16 + half * 8 + g;
-                            fa[i][half][0] = fa[i][half][1] = fa[i][half][2] = fa[i][half][3] = 0;
-                            if (r < p.rank) load_few<8, VEC>(arow + size_t(r) * p.k, col, p.k, fa[i][half]);
-                        }
-#pragma unroll
-                    for (int i = 0; i < RT; ++i)
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            const uint32_t f[4] = {fa[i][0][2 * s], fa[i][1][2 * s], fa[i][0][2 * s + 1], fa[i][1][2 * s + 1]};
-#pragma unroll
-                            for (int j = 0; j < NT; ++j)
-                                if (any[j]) mma_16816<DT>(acc[i][j], f, fx[j][2 * s], fx[j][2 * s + 1]);
-                        }
+                for (int half = 0; half < 2; ++half) {
+                    const int r = r0 + i * 16 + half * 8 + g;
+                    load_eight<VEC>(arow + size_t(r) * p.k, r < p.rank ? col : p.k, p.k, fa[i][half]);
                 }
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+            for (int i = 0; i < RW; ++i)
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int token = at + j * 8 + 2 * t + q;
-                        if (token >= count || own[token] != d) continue;
-                        float* const to = sums + (size_t(part) * T + token) * R;
+                for (int s = 0; s < 2; ++s) {
+                    const uint32_t f[4] = {fa[i][0][2 * s], fa[i][1][2 * s], fa[i][0][2 * s + 1], fa[i][1][2 * s + 1]};
 #pragma unroll
-                        for (int i = 0; i < RT; ++i) {
-                            to[i * 16 + g] = acc[i][j][q];
-                            to[i * 16 + 8 + g] = acc[i][j][2 + q];
-                        }
-                    }
-            }
+                    for (int j = 0; j < NT; ++j) mma_16816<DT>(acc[i][j], f, fx[j][2 * s], fx[j][2 * s + 1]);
+                }
         }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int token = j * 8 + 2 * t + q;
+                if (own[token] != d) continue;
+#pragma unroll
+                for (int i = 0; i < RW; ++i) {
+                    sums[part][token][r0 + i * 16 + g] = acc[i][j][q];
+                    sums[part][token][r0 + i * 16 + 8 + g] = acc[i][j][2 + q];
+                }
+            }
     }
     __syncthreads();
-    for (int e = tid; e < count * R; e += kAdapterThreads) {
+    for (int e = tid; e < kDownTokens * R; e += kAdapterThreads) {
         float v = 0.0f;
         if (own[e / R] >= 0)
-            for (int i = 0; i < p.split; ++i) v += sums[i * T * R + e];
-        mine[e] = v;
+#pragma unroll
+            for (int i = 0; i < SPLIT; ++i) v += (&sums[i][0][0])[e];
+        (&sums[0][0][0])[e] = v;
     }
     cluster_sync();
-    // ---------------------------------------------------- the cluster's sums, scaled and packed
-    for (int token = warp; token < (T + 15) / 16 * 16; token += kAdapterWarps) {
-        const int i = token < count ? own[token] : -1;
+    // the cluster's sums of every ctas-th token, scaled and split
+    for (int token = rank + warp * p.ctas; token < count; token += kAdapterWarps * p.ctas) {
+        const int i = own[token];
+        if (i < 0) continue;
         constexpr int PER = (R + 31) / 32;
         float v[PER], top = 0.0f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int r = lane + 32 * j;
             v[j] = 0.0f;
-            if (i >= 0 && r < R) {
-                const uint32_t from = smem_addr(mine + token * R + r);
+            if (r < R) {
+                const uint32_t from = smem_addr(&sums[0][token][r]);
                 for (int q = 0; q < p.ctas; ++q) v[j] += ld_cluster_f32(peer_addr(from, q));
                 if (p.scale) v[j] *= p.scale[i];
             }
@@ -228,82 +276,121 @@ __global__ void __launch_bounds__(kAdapterThreads) adapters_kernel(const __grid_
             top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));
             const int e = top > 0.0f ? min(max(int(__float_as_uint(top) >> 23) - 127 - 14, -100), 100) : 0;
             times = __uint_as_float(uint32_t(127 - e) << 23);
-            if (lane == 0 && token < kAdapterTokens) back[token] = __uint_as_float(uint32_t(127 + e) << 23);
+            if (lane == 0) p.back[first + token] = __uint_as_float(uint32_t(127 + e) << 23);
         }
+        uint16_t* const to = p.s + size_t(first + token) * (2 * R);
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int r = lane + 32 * j;
             if (r >= R) continue;
             const float s = v[j] * times;
-            const uint32_t h = pack2(s, 0.0f, DT);
-            const float rest = s - unpack2(h, DT).x;
-            high[token * PS + r] = uint16_t(h);
+            const uint32_t high = pack2(s, 0.0f, DT);
+            const float rest = s - unpack2(high, DT).x;
+            to[r] = uint16_t(high);
             // nothing is left of what is not finite
-            low[token * PS + r] = fabsf(s) < __uint_as_float(kInfBits) ? uint16_t(pack2(rest, 0.0f, DT)) : uint16_t(0);
+            to[R + r] = fabsf(s) < __uint_as_float(kInfBits) ? uint16_t(pack2(rest, 0.0f, DT)) : uint16_t(0);
         }
     }
     __syncwarp();
-    cluster_arrive();                       // the others' sums have been read
-    __syncthreads();
+    cluster_sync();                                  // the others' sums have been read
+}
 
-    // ---------------------------------------------------- y + S B^T, 16 tokens x 32 features at a time
-    // Column c of the j-th of four products is feature 8 (c / 2) + 2 j + c % 2, so that a thread ends up with 8 neighbours.
-    const int blocks = (p.n + 31) / 32, b0 = int(int64_t(blocks) * rank / p.ctas), b1 = int(int64_t(blocks) * (rank + 1) / p.ctas);
-    for (int m0 = 0; m0 < count; m0 += 16) {
-        const uint64_t all = leaders(m0, 16);
-        const int d0 = own[m0 + g], d1 = own[m0 + g + 8];
-        const size_t r0 = size_t(first + m0 + g), r1 = r0 + 8;
-        const bool in0 = m0 + g < count, in1 = m0 + g + 8 < count;
-        const float back0 = DT == kFp16 ? back[m0 + g] : 1.0f, back1 = DT == kFp16 ? back[m0 + g + 8] : 1.0f;
-        for (int block = b0 + warp; block < b1; block += kAdapterWarps) {
-            const int f0 = block * 32 + 8 * t;
-            uint32_t y0[4] = {}, y1[4] = {};
-            if (in0) load_eight<VEC>(static_cast<const uint16_t*>(p.y) + r0 * p.ldy, f0, p.n, y0);
-            if (in1) load_eight<VEC>(static_cast<const uint16_t*>(p.y) + r1 * p.ldy, f0, p.n, y1);
-            for (uint64_t left = all; left; left &= left - 1) {
-                const int d = own[m0 + __ffsll(left) - 1];
-                const uint16_t* const brow = b + (size_t(d) * p.n + block * 32) * p.rank;
-                float acc[4][4] = {};
-                uint32_t fb[4][2 * RT];
+// out = y + S B^T.  A warp keeps S of 16 tokens in registers and takes 32 features at a time; the CTA's four warps read the same rows
+// of B.  Column c of the j-th of four products is feature 8 (c / 2) + 2 j + c % 2, so that a thread ends up with 8 neighbours.
+constexpr int kUpWarps = 4, kUpTokens = 16 * kUpWarps;
+template <bool VEC>
+__device__ __forceinline__ void store_eight(uint16_t* row, int col, int cols, const uint32_t (&v)[4]) {
+    if (VEC) {
+        if (col < cols) *reinterpret_cast<uint4*>(row + col) = make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int f = 8 * (g >> 1) + 2 * j + (g & 1);
+        for (int i = 0; i < 8; ++i)
+            if (col + i < cols) row[col + i] = uint16_t(v[i / 2] >> (i & 1) * 16);
+    }
+}
+template <int DT, int RT, bool VEC>
+__global__ void __launch_bounds__(32 * kUpWarps) adapter_up_kernel(const __grid_constant__ AdapterArgs p) {
+    constexpr int R = 16 * RT;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int first = int(blockIdx.x) * kUpTokens + uniform(threadIdx.x >> 5) * 16;
+    const uint16_t* const b = static_cast<const uint16_t*>(p.b);
+    grid_launch();
+    grid_wait();
+    if (first >= p.tokens) return;
+    const int d = first + (lane & 15) < p.tokens ? adapter_of(p, first + (lane & 15)) : -1;
+    const uint32_t leaders = first_of_each(lane < 16 ? d : -1);
+    const int d0 = __shfl_sync(0xFFFFFFFFu, d, g), d1 = __shfl_sync(0xFFFFFFFFu, d, g + 8);
+    const size_t t0 = first + g, t1 = t0 + 8;
+    const bool in0 = int(t0) < p.tokens, in1 = int(t1) < p.tokens;
+    // a thread's ranks are [4 RT t, 4 RT (t + 1)), four of them in each step of the product
+    uint2 high[2][RT], low[2][RT];
+    float back[2];
 #pragma unroll
-                    for (int i = 0; i < 2 * RT; ++i) fb[j][i] = 0;
-                    if (block * 32 + f >= p.n) continue;
-                    if constexpr (RT == 1) {
-                        load_few<4, VEC>(brow + size_t(f) * p.rank, 4 * t, p.rank, fb[j]);
+    for (int i = 0; i < 2; ++i) {
+        const bool has = (i ? d1 : d0) >= 0;
+        const size_t token = i ? t1 : t0;
+        const uint2* const s = reinterpret_cast<const uint2*>(p.s + token * (2 * R)) + t * RT;
+#pragma unroll
+        for (int j = 0; j < RT; ++j) {
+            high[i][j] = has ? __ldcg(s + j) : make_uint2(0, 0);
+            low[i][j] = has ? __ldcg(s + R / 4 + j) : make_uint2(0, 0);
+        }
+        back[i] = DT == kFp16 && has ? __ldcg(p.back + token) : 1.0f;
+    }
+    const uint16_t* const y0 = static_cast<const uint16_t*>(p.y) + t0 * p.ldy;
+    const uint16_t* const y1 = static_cast<const uint16_t*>(p.y) + t1 * p.ldy;
+    uint16_t* const o0 = static_cast<uint16_t*>(p.out) + t0 * p.ldo;
+    uint16_t* const o1 = static_cast<uint16_t*>(p.out) + t1 * p.ldo;
+    const int end = min(p.n, int(blockIdx.y + 1) * p.blocks * 32);
+    for (int f0 = int(blockIdx.y) * p.blocks * 32; f0 < end; f0 += 32) {
+        const int col = f0 + 8 * t;
+        uint32_t v0[4], v1[4];
+        load_eight<VEC>(y0, in0 ? col : p.n, p.n, v0);
+        load_eight<VEC>(y1, in1 ? col : p.n, p.n, v1);
+        for (uint32_t left = leaders; left; left &= left - 1) {
+            const int e = __shfl_sync(0xFFFFFFFFu, d, __ffs(left) - 1);
+            const uint16_t* const rows = b + (size_t(e) * p.n + f0) * p.rank;
+            float acc[4][4] = {};
+            uint32_t fb[4][2 * RT];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int f = 8 * (g >> 1) + 2 * j + (g & 1), limit = f0 + f < p.n ? p.rank : 0;
+                const uint16_t* const row = rows + size_t(f) * p.rank;
+                if constexpr (RT == 1) {
+                    if (VEC) {
+                        const uint2 q = 4 * t < limit ? *reinterpret_cast<const uint2*>(row + 4 * t) : make_uint2(0, 0);
+                        fb[j][0] = q.x; fb[j][1] = q.y;
                     } else {
 #pragma unroll
-                        for (int i = 0; i < RT / 2; ++i)
-                            load_few<8, VEC>(brow + size_t(f) * p.rank, 4 * RT * t + 8 * i, p.rank, fb[j] + 4 * i);
+                        for (int i = 0; i < 2; ++i)
+                            fb[j][i] = (4 * t + 2 * i < limit ? row[4 * t + 2 * i] : 0) |
+                                       uint32_t(4 * t + 2 * i + 1 < limit ? row[4 * t + 2 * i + 1] : 0) << 16;
                     }
-                }
+                } else {
 #pragma unroll
-                for (int s = 0; s < RT; ++s) {
-                    const int at = (m0 + g) * PS + 4 * RT * t + 4 * s;
-                    const uint2 h0 = *reinterpret_cast<const uint2*>(high + at), h1 = *reinterpret_cast<const uint2*>(high + at + 8 * PS);
-                    const uint2 l0 = *reinterpret_cast<const uint2*>(low + at), l1 = *reinterpret_cast<const uint2*>(low + at + 8 * PS);
-                    const uint32_t fh[4] = {h0.x, h1.x, h0.y, h1.y}, fl[4] = {l0.x, l1.x, l0.y, l1.y};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        mma_16816<DT>(acc[j], fh, fb[j][2 * s], fb[j][2 * s + 1]);
-                        mma_16816<DT>(acc[j], fl, fb[j][2 * s], fb[j][2 * s + 1]);
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 v0 = unpack2(y0[j], DT), v1 = unpack2(y1[j], DT);
-                    if (d0 == d) y0[j] = pack2(fmaf(acc[j][0], back0, v0.x), fmaf(acc[j][1], back0, v0.y), DT);
-                    if (d1 == d) y1[j] = pack2(fmaf(acc[j][2], back1, v1.x), fmaf(acc[j][3], back1, v1.y), DT);
+                    for (int i = 0; i < RT / 2; ++i) load_eight<VEC>(row, 4 * RT * t + 8 * i, limit, fb[j] + 4 * i);
                 }
             }
-            if (in0) store_eight<VEC>(static_cast<uint16_t*>(p.out) + r0 * p.ldo, f0, p.n, y0);
-            if (in1) store_eight<VEC>(static_cast<uint16_t*>(p.out) + r1 * p.ldo, f0, p.n, y1);
+#pragma unroll
+            for (int s = 0; s < RT; ++s) {
+                const uint32_t fh[4] = {high[0][s].x, high[1][s].x, high[0][s].y, high[1][s].y};
+                const uint32_t fl[4] = {low[0][s].x, low[1][s].x, low[0][s].y, low[1][s].y};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    mma_16816<DT>(acc[j], fh, fb[j][2 * s], fb[j][2 * s + 1]);
+                    mma_16816<DT>(acc[j], fl, fb[j][2 * s], fb[j][2 * s + 1]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 w0 = unpack2(v0[j], DT), w1 = unpack2(v1[j], DT);
+                if (d0 == e) v0[j] = pack2(fmaf(acc[j][0], back[0], w0.x), fmaf(acc[j][1], back[0], w0.y), DT);
+                if (d1 == e) v1[j] = pack2(fmaf(acc[j][2], back[1], w1.x), fmaf(acc[j][3], back[1], w1.y), DT);
+            }
         }
+        if (in0) store_eight<VEC>(o0, col, p.n, v0);
+        if (in1) store_eight<VEC>(o1, col, p.n, v1);
     }
-    __syncwarp();
-    cluster_wait();
 }
 
 }  // namespace ff

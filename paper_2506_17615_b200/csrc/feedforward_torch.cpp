@@ -42,6 +42,7 @@ namespace {
     X(add_rms_norm_backward_workspace_bytes) \
     X(add_rms_norm_backward)             \
     X(add_adapters)                      \
+    X(add_adapters_workspace_bytes)      \
     X(gated_forward_workspace_bytes)     \
     X(gated_forward)                     \
     X(gated_backward_workspace_bytes)    \
@@ -594,9 +595,11 @@ PyObject* add_adapters(PyObject*, PyObject* const* args, Py_ssize_t count) {
     const at::Tensor out = args[6] == Py_None ? empty(m, n, y.t.scalar_type(), device) : tensor(args[6], "out");
     const Matrix o = matrix(out, "out", m, n, y.t);
     no_gradient(out, "out", calls);
+    const size_t need = entry.add_adapters_workspace_bytes(m, rank);
+    const at::Tensor ws = bytes(need, device);
     const int status = call(device, [&](equarx_stream_t s) {
         return entry.add_adapters(y.p, y.ld, x.p, x.ld, ta.data_ptr(), tb.data_ptr(), static_cast<const int32_t*>(index.p), scale, dtype, m,
-                                  n, k, rank, adapters, o.p, o.ld, s);
+                                  n, k, rank, adapters, o.p, o.ld, address(ws), need, s);
     });
     return result(status, out);
     END_HANDLE_TH_ERRORS

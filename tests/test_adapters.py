@@ -20,7 +20,7 @@ TYPES = [torch.bfloat16, torch.float16]
 
 def call_args():
     return dict(y=A, ldy=64, x=A + GB, ldx=32, a=A + 2 * GB, b=A + 3 * GB, index=A + 4 * GB, scale=A + 5 * GB, dtype=eq.BF16, tokens=4, n=64,
-                k=32, rank=8, adapters=3, out=A + 6 * GB, ldo=64)
+                k=32, rank=8, adapters=3, out=A + 6 * GB, ldo=64, workspace=0, workspace_bytes=0)
 
 
 def test_refuses_bad_arguments():
@@ -38,6 +38,16 @@ def test_refuses_bad_arguments():
         assert status_of(f, **{**a, "out": bad}) == binding.ERR_ALIAS
     assert status_of(f, **{**a, "out": A, "ldo": 72}) == binding.ERR_ALIAS
     assert status_of(f, **{**a, "tokens": 0, "y": 0}) == 0
+    # many tokens go through a workspace
+    assert eq.add_adapters_workspace_bytes(4, 8) == 0 and eq.add_adapters_workspace_bytes(1000, 0) == 0
+    need = eq.add_adapters_workspace_bytes(1000, 17)
+    assert need >= 1000 * 32 * 4
+    many = {**a, "tokens": 1000, "rank": 17, "workspace": A + 7 * GB, "workspace_bytes": need}
+    assert status_of(f, **{**many, "workspace": 0}) == binding.ERR_NULL
+    assert status_of(f, **{**many, "workspace_bytes": need - 1}) == binding.ERR_WORKSPACE
+    assert status_of(f, **{**many, "workspace": A + 7 * GB + 8}) == binding.ERR_ALIGN
+    for bad in (A, A + GB, A + 3 * GB, A + 6 * GB):
+        assert status_of(f, **{**many, "workspace": bad}) == binding.ERR_ALIAS
     assert eq.last_cuda_error() == 0
 
 
@@ -159,13 +169,15 @@ def test_views_that_start_anywhere(tokens, offset):
         return store, view.copy_(t)
 
     flat = lambda t: torch.empty(t.numel() + offset, device="cuda", dtype=dtype)[offset:].copy_(t.reshape(-1))
+    nb = eq.add_adapters_workspace_bytes(tokens, rank)
+    ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
     for extra in (0, 1, 8):
         (_, vy), (_, vx), (so, vo) = place(y, n + extra), place(x, k + extra), place(y * 0, n + extra)
-        eq.add_adapters(vy, n + extra, vx, k + extra, flat(a), flat(b), index, scale, eq.BF16, tokens, n, k, rank, 3, vo, n + extra, stream)
+        eq.add_adapters(vy, n + extra, vx, k + extra, flat(a), flat(b), index, scale, eq.BF16, tokens, n, k, rank, 3, vo, n + extra, ws, nb, stream)
         assert torch.equal(vo, want)
         vo.fill_(-77.0)
         assert bool((so == -77.0).all())
-        eq.add_adapters(vy, n + extra, vx, k + extra, a, b, index, scale, eq.BF16, tokens, n, k, rank, 3, vy, n + extra, stream)
+        eq.add_adapters(vy, n + extra, vx, k + extra, a, b, index, scale, eq.BF16, tokens, n, k, rank, 3, vy, n + extra, ws, nb, stream)
         assert torch.equal(vy, want)
 
 
