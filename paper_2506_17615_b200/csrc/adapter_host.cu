@@ -30,12 +30,14 @@ int launch_adapters(AdapterArgs& a, int sms, cudaStream_t stream) {
     const size_t tiles = ceil_div(a.tokens, kDownTokens);
     a.ctas = 1;
     while (a.ctas < 8 && tiles * a.ctas * 2 <= size_t(2 * sms)) a.ctas *= 2;
-    TRY(launch(adapter_down_kernel<DT, RT, VEC>, dim3(unsigned(tiles * a.ctas)), kAdapterThreads, 0, unsigned(a.ctas), a, stream));
-    const size_t up_tiles = ceil_div(a.tokens, kUpTokens), all = ceil_div(a.n, 32);
-    // about eight CTAs for each SM, and eight blocks of features at least for each
-    const size_t parts = std::max<size_t>(1, std::min(ceil_div(size_t(8 * sms), up_tiles), all / 8));
+    TRY(launch(adapter_down_kernel<DT, RT, VEC>, dim3(unsigned(tiles * a.ctas)), kAdapterThreads, kDownSmem<RT>, unsigned(a.ctas), a, stream,
+               true));
+    // four CTAs run on an SM at one time; twice as many, so that a tile with two adapters holds up less
+    const size_t up_tiles = ceil_div(a.tokens, kUpTokens), all = ceil_div(a.n, kUpFeatures);
+    const size_t parts = std::max<size_t>(1, std::min(size_t(8 * sms) / up_tiles, ceil_div(all, 2)));
     a.blocks = int(ceil_div(all, parts));
-    return launch(adapter_up_kernel<DT, RT, VEC>, dim3(unsigned(up_tiles), unsigned(ceil_div(all, a.blocks))), 32 * kUpWarps, 0, 1, a, stream);
+    return launch(adapter_up_kernel<DT, RT, VEC>, dim3(unsigned(up_tiles), unsigned(ceil_div(all, a.blocks))), 32 * kUpWarps, kUpSmem<RT>, 1, a,
+                  stream, true);
 }
 template <int DT, int RT>
 int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {

@@ -23,7 +23,7 @@ struct AdapterArgs {
     size_t ldy, ldx, ldo;
     int tokens, k, n, rank, adapters;
     int ctas;                         // of a cluster, which split k (and, for few tokens, n)
-    int blocks;                       // of 32 features, that a CTA of the second product takes
+    int blocks;                       // of 64 features, that a CTA of the second product takes
 };
 constexpr int kAdapterWarps = 8, kAdapterThreads = 32 * kAdapterWarps;
 // ranks are padded to 16 RT, RT = 1, 2, 4 or 8
@@ -168,9 +168,9 @@ __device__ __forceinline__ uint32_t first_of_each(int d) {
     return __ballot_sync(0xFFFFFFFFu, d >= 0 && __ffs(alike) == int(threadIdx.x & 31) + 1);
 }
 
-// Reading x and y bounds both products, so they use mma.sync on fragments that come straight from memory (the reduction axis is
-// permuted alike for both operands, so that a thread's fragments are 16 neighbouring bytes): with 16 to 128 columns there is no
-// reuse for tcgen05's operands in shared memory to pay for.
+// Reading x and y bounds both products, so they use mma.sync (the reduction axis is permuted alike for both operands, so that a
+// thread's fragments are 16 neighbouring bytes): with 16 to 128 columns, and rows of several adapters in a tile, the
+// tensor cores' work is small beside the reading.
 //
 // A product runs once for each adapter that the tokens of a tile have, with nothing in the other tokens' places, and only this
 // adapter's tokens take its result: what is not finite in one request's adapter does not reach another request.
@@ -178,80 +178,124 @@ __device__ __forceinline__ uint32_t first_of_each(int d) {
 // S is rounded as the tensor cores want it, to two numbers of the 16-bit type, high and low, whose sum has 16 bits (bf16) or
 // 22: 2^-17 of S.  In fp16 a token's S is scaled by a power of two first, so that its range does not matter.
 
-// S of 32 tokens, transposed: 16 ranks x 8 tokens a product.  The CTA's warps split ranks above 32 between them, and k, and so do the
-// CTAs of a cluster where there are few tiles.
-constexpr int kDownTokens = 32;
-template <int RT> constexpr int kDownRanks = RT < 2 ? 1 : 2;                              // groups of 16 ranks of a warp
-template <int RT> constexpr int kDownSplit = kAdapterWarps * kDownRanks<RT> / RT;         // ways in which warps split k
+// The same 16 bytes in shared memory: copied while products run (VEC), else element by element
+template <bool VEC>
+__device__ __forceinline__ void stage_eight(uint32_t to, const uint16_t* row, int col, int cols) {
+    if (VEC) {
+        copy_async_16(to, row + (col < cols ? col : 0), col < cols ? 16 : 0);
+    } else {
+        uint32_t v[4];
+        load_eight<false>(row, col, cols, v);
+        st_shared_v4(to, v[0], v[1], v[2], v[3]);
+    }
+}
+
+// S of 32 tokens, transposed: 16 ranks x 8 tokens a product.  Chunks of x and A come through a ring in shared memory.  A warp has 16
+// ranks of S, the warps with the same ranks split a chunk, and the CTAs of a cluster split k where there are few tiles.  Rows
+// in shared memory are 64 bytes longer than a multiple of 128, so that two rows' 64 bytes meet no bank twice.
+constexpr int kDownTokens = 32, kDownStages = 3;
+template <int RT> constexpr int kDownChunk = RT == 1 ? 256 : 128;                         // columns
+template <int RT> constexpr int kDownRow = kDownChunk<RT> * 2 + 64;                       // bytes
+template <int RT> constexpr int kDownSplit = kAdapterWarps / RT;                          // warps with the same ranks
+template <int RT> constexpr int kDownStageBytes = (kDownTokens + 16 * RT) * kDownRow<RT>;
+template <int RT> constexpr int kDownSmem = kDownStages * kDownStageBytes<RT> + kDownSplit<RT> * kDownTokens * 16 * RT * 4;
 template <int DT, int RT, bool VEC>
 __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const __grid_constant__ AdapterArgs p) {
-    constexpr int R = 16 * RT, RW = kDownRanks<RT>, SPLIT = kDownSplit<RT>, NT = kDownTokens / 8;
-    __shared__ float sums[SPLIT][kDownTokens][R];    // the first becomes the CTA's sums
+    constexpr int R = 16 * RT, SPLIT = kDownSplit<RT>, NT = kDownTokens / 8, CHUNK = kDownChunk<RT>, ROW = kDownRow<RT>;
+    extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int own[kDownTokens];
+    const uint32_t ring = smem_addr(smem);
+    float* const sums = reinterpret_cast<float*>(smem + kDownStages * kDownStageBytes<RT>);      // [SPLIT][tokens][R]
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int rank = int(cluster_rank()), first = int(blockIdx.x / p.ctas) * kDownTokens, count = min(kDownTokens, p.tokens - first);
     const uint16_t* const a = static_cast<const uint16_t*>(p.a);
+    const uint16_t* const x = static_cast<const uint16_t*>(p.x) + size_t(first) * p.ldx;
     grid_launch();
     grid_wait();
     if (tid < kDownTokens) own[tid] = tid < count ? adapter_of(p, first + tid) : -1;
     __syncthreads();
 
-    const int chunks = (p.k + 31) / 32, c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
-    const int part = warp % SPLIT, r0 = warp / SPLIT * (16 * RW);
-    const uint16_t* x[NT];
+    const int chunks = (p.k + CHUNK - 1) / CHUNK;
+    const int c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
+    const int part = warp % SPLIT, r0 = warp / SPLIT * 16;
     int adapter[NT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        adapter[j] = own[j * 8 + g];
-        x[j] = static_cast<const uint16_t*>(p.x) + size_t(first + min(j * 8 + g, count - 1)) * p.ldx;
-    }
+    for (int j = 0; j < NT; ++j) adapter[j] = own[j * 8 + g];
     for (uint32_t left = first_of_each(own[lane]); left; left &= left - 1) {
         const int d = own[__ffs(left) - 1];
-        const uint16_t* const arow = a + size_t(d) * p.rank * p.k;
-        float acc[RW][NT][4] = {};
-#pragma unroll 2
-        for (int c = c0 + part; c < c1; c += SPLIT) {
-            const int col = c * 32 + 8 * t;
-            uint32_t fx[NT][4], fa[RW][2][4];
+        // a thread copies the same piece of every STEP-th row of x and A
+        constexpr int PIECES = CHUNK / 8, STEP = kAdapterThreads / PIECES, XS = kDownTokens / STEP, AS = (R + STEP - 1) / STEP;
+        const int row0 = tid / PIECES, piece = tid % PIECES;
+        const uint16_t* const rows = a + (size_t(d) * p.rank + row0) * p.k;
+        const uint16_t* xs[XS];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) load_eight<VEC>(x[j], adapter[j] == d ? col : p.k, p.k, fx[j]);
+        for (int i = 0; i < XS; ++i) xs[i] = x + size_t(min(row0 + i * STEP, count - 1)) * p.ldx;
+        int ahead = 0;
+        auto fetch = [&](int c) {
+            if (c < c1) {
+                const uint32_t to = ring + ahead * kDownStageBytes<RT> + row0 * ROW + piece * 16;
+                const int col = c * CHUNK + piece * 8;
 #pragma unroll
-            for (int i = 0; i < RW; ++i)
+                for (int i = 0; i < XS; ++i) stage_eight<VEC>(to + i * STEP * ROW, xs[i], col, p.k);
+                const uint16_t* from = rows;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int r = r0 + i * 16 + half * 8 + g;
-                    load_eight<VEC>(arow + size_t(r) * p.k, r < p.rank ? col : p.k, p.k, fa[i][half]);
+                for (int i = 0; i < AS; ++i, from += size_t(STEP) * p.k)
+                    if (R % STEP == 0 || row0 + i * STEP < R) {
+                        const bool in = row0 + i * STEP < p.rank;
+                        stage_eight<VEC>(to + (kDownTokens + i * STEP) * ROW, in ? from : a, in ? col : p.k, p.k);
+                    }
+            }
+            ahead = ahead == kDownStages - 1 ? 0 : ahead + 1;
+            copy_async_commit();
+        };
+        float acc[NT][4] = {};
+        for (int i = 0; i < kDownStages - 1; ++i) fetch(c0 + i);
+        int stage = 0;
+        for (int c = c0; c < c1; ++c) {
+            copy_async_wait<kDownStages - 2>();
+            __syncthreads();                               // this chunk is there, the one before it has been used
+            fetch(c + kDownStages - 1);
+            const uint32_t from = ring + stage * kDownStageBytes<RT>;
+            stage = stage == kDownStages - 1 ? 0 : stage + 1;
+#pragma unroll
+            for (int u = 0; u < CHUNK / 32 / SPLIT; ++u) {
+                const uint32_t at = (part + u * SPLIT) * 64 + t * 16;
+                uint32_t fx[NT][4], fa[2][4];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    ld_shared_v4(from + (j * 8 + g) * ROW + at, fx[j]);
+                    if (adapter[j] != d) fx[j][0] = fx[j][1] = fx[j][2] = fx[j][3] = 0;
                 }
 #pragma unroll
-            for (int i = 0; i < RW; ++i)
+                for (int half = 0; half < 2; ++half) ld_shared_v4(from + (kDownTokens + r0 + half * 8 + g) * ROW + at, fa[half]);
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    const uint32_t f[4] = {fa[i][0][2 * s], fa[i][1][2 * s], fa[i][0][2 * s + 1], fa[i][1][2 * s + 1]};
+                    const uint32_t f[4] = {fa[0][2 * s], fa[1][2 * s], fa[0][2 * s + 1], fa[1][2 * s + 1]};
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) mma_16816<DT>(acc[i][j], f, fx[j][2 * s], fx[j][2 * s + 1]);
+                    for (int j = 0; j < NT; ++j) mma_16816<DT>(acc[j], f, fx[j][2 * s], fx[j][2 * s + 1]);
                 }
+            }
         }
+        __syncthreads();                                   // the ring is free again
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int token = j * 8 + 2 * t + q;
                 if (own[token] != d) continue;
-#pragma unroll
-                for (int i = 0; i < RW; ++i) {
-                    sums[part][token][r0 + i * 16 + g] = acc[i][j][q];
-                    sums[part][token][r0 + i * 16 + 8 + g] = acc[i][j][2 + q];
-                }
+                sums[(part * kDownTokens + token) * R + r0 + g] = acc[j][q];
+                sums[(part * kDownTokens + token) * R + r0 + 8 + g] = acc[j][2 + q];
             }
     }
     __syncthreads();
-    for (int e = tid; e < kDownTokens * R; e += kAdapterThreads) {
-        float v = 0.0f;
-        if (own[e / R] >= 0)
+    if (SPLIT > 1)
+        for (int e = tid; e < kDownTokens * R; e += kAdapterThreads) {
+            if (own[e / R] < 0) continue;
+            float v = 0.0f;
 #pragma unroll
-            for (int i = 0; i < SPLIT; ++i) v += (&sums[i][0][0])[e];
-        (&sums[0][0][0])[e] = v;
-    }
+            for (int i = 0; i < SPLIT; ++i) v += sums[i * kDownTokens * R + e];
+            sums[e] = v;
+        }
     cluster_sync();
     // the cluster's sums of every ctas-th token, scaled and split
     for (int token = rank + warp * p.ctas; token < count; token += kAdapterWarps * p.ctas) {
@@ -264,7 +308,7 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
             const int r = lane + 32 * j;
             v[j] = 0.0f;
             if (r < R) {
-                const uint32_t from = smem_addr(&sums[0][token][r]);
+                const uint32_t from = smem_addr(sums + token * R + r);
                 for (int q = 0; q < p.ctas; ++q) v[j] += ld_cluster_f32(peer_addr(from, q));
                 if (p.scale) v[j] *= p.scale[i];
             }
@@ -295,9 +339,12 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
     cluster_sync();                                  // the others' sums have been read
 }
 
-// out = y + S B^T.  A warp keeps S of 16 tokens in registers and takes 32 features at a time; the CTA's four warps read the same rows
-// of B.  Column c of the j-th of four products is feature 8 (c / 2) + 2 j + c % 2, so that a thread ends up with 8 neighbours.
-constexpr int kUpWarps = 4, kUpTokens = 16 * kUpWarps;
+// out = y + S B^T for 64 tokens, 64 features at a time, whose rows of B come through a ring in shared memory; the next features' y
+// is on its way to registers meanwhile.  A warp keeps S of 16 tokens in registers.  Column c of the j-th of four products is
+// feature 8 (c / 2) + 2 j + c % 2, so that a thread ends up with 8 neighbours.
+constexpr int kUpWarps = 4, kUpTokens = 16 * kUpWarps, kUpFeatures = 64, kUpStages = 3;
+template <int RT> constexpr int kUpRow = 32 * RT + (RT >= 4 ? 16 : 0);                   // bytes of a row of B in shared memory
+template <int RT> constexpr int kUpSmem = kUpStages * kUpFeatures * kUpRow<RT>;
 template <bool VEC>
 __device__ __forceinline__ void store_eight(uint16_t* row, int col, int cols, const uint32_t (&v)[4]) {
     if (VEC) {
@@ -309,19 +356,32 @@ __device__ __forceinline__ void store_eight(uint16_t* row, int col, int cols, co
     }
 }
 template <int DT, int RT, bool VEC>
-__global__ void __launch_bounds__(32 * kUpWarps) adapter_up_kernel(const __grid_constant__ AdapterArgs p) {
-    constexpr int R = 16 * RT;
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int first = int(blockIdx.x) * kUpTokens + uniform(threadIdx.x >> 5) * 16;
+__global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_kernel(const __grid_constant__ AdapterArgs p) {
+    constexpr int R = 16 * RT, ROW = kUpRow<RT>;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int own[kUpTokens];
+    __shared__ uint32_t leaders[2];
+    const uint32_t ring = smem_addr(smem);
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int first = int(blockIdx.x) * kUpTokens;
     const uint16_t* const b = static_cast<const uint16_t*>(p.b);
     grid_launch();
     grid_wait();
-    if (first >= p.tokens) return;
-    const int d = first + (lane & 15) < p.tokens ? adapter_of(p, first + (lane & 15)) : -1;
-    const uint32_t leaders = first_of_each(lane < 16 ? d : -1);
-    const int d0 = __shfl_sync(0xFFFFFFFFu, d, g), d1 = __shfl_sync(0xFFFFFFFFu, d, g + 8);
-    const size_t t0 = first + g, t1 = t0 + 8;
-    const bool in0 = int(t0) < p.tokens, in1 = int(t1) < p.tokens;
+    if (tid < kUpTokens) own[tid] = first + tid < p.tokens ? adapter_of(p, first + tid) : -1;
+    __syncthreads();
+    if (tid < kUpTokens) {                           // the first token with each adapter
+        bool again = own[tid] < 0;
+        for (int i = 0; i < kUpTokens; ++i) again |= i < tid && own[i] == own[tid];
+        const uint32_t bits = __ballot_sync(0xFFFFFFFFu, !again);
+        if (lane == 0) leaders[warp] = bits;
+    }
+    __syncthreads();
+    const uint64_t list = leaders[0] | uint64_t(leaders[1]) << 32;
+    const int adapters = __popcll(list);
+
+    const int d0 = own[warp * 16 + g], d1 = own[warp * 16 + g + 8];
+    const size_t t0 = first + warp * 16 + g, t1 = t0 + 8;
+    const bool in0 = t0 < size_t(p.tokens), in1 = t1 < size_t(p.tokens);
     // a thread's ranks are [4 RT t, 4 RT (t + 1)), four of them in each step of the product
     uint2 high[2][RT], low[2][RT];
     float back[2];
@@ -341,55 +401,105 @@ __global__ void __launch_bounds__(32 * kUpWarps) adapter_up_kernel(const __grid_
     const uint16_t* const y1 = static_cast<const uint16_t*>(p.y) + t1 * p.ldy;
     uint16_t* const o0 = static_cast<uint16_t*>(p.out) + t0 * p.ldo;
     uint16_t* const o1 = static_cast<uint16_t*>(p.out) + t1 * p.ldo;
-    const int end = min(p.n, int(blockIdx.y + 1) * p.blocks * 32);
-    for (int f0 = int(blockIdx.y) * p.blocks * 32; f0 < end; f0 += 32) {
-        const int col = f0 + 8 * t;
-        uint32_t v0[4], v1[4];
-        load_eight<VEC>(y0, in0 ? col : p.n, p.n, v0);
-        load_eight<VEC>(y1, in1 ? col : p.n, p.n, v1);
-        for (uint32_t left = leaders; left; left &= left - 1) {
-            const int e = __shfl_sync(0xFFFFFFFFu, d, __ffs(left) - 1);
-            const uint16_t* const rows = b + (size_t(e) * p.n + f0) * p.rank;
-            float acc[4][4] = {};
-            uint32_t fb[4][2 * RT];
+
+    // units: blocks of features, and for each the adapters in turn
+    const int f0 = int(blockIdx.y) * p.blocks * kUpFeatures, f1 = min(p.n, f0 + p.blocks * kUpFeatures);
+    const int per = max(adapters, 1), units = (f1 - f0 + kUpFeatures - 1) / kUpFeatures * per;
+    int ahead = 0, ahead_f = f0, slot = 0, used = 0; // the unit that is copied next, its place and that of the one in use
+    uint64_t ahead_left = list;
+    auto fetch = [&] {
+        if (ahead < units && adapters) {
+            // a thread copies the same piece of every STEP-th row
+            constexpr int STEP = 32 * kUpWarps / (R / 8);
+            const int f = ahead_f + tid / (R / 8), r = tid % (R / 8) * 8;
+            const uint16_t* from = b + (size_t(own[__ffsll(ahead_left) - 1]) * p.n + f) * p.rank;
+            const uint32_t to = ring + slot * (kUpFeatures * ROW) + tid / (R / 8) * ROW + r * 2;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int f = 8 * (g >> 1) + 2 * j + (g & 1), limit = f0 + f < p.n ? p.rank : 0;
-                const uint16_t* const row = rows + size_t(f) * p.rank;
-                if constexpr (RT == 1) {
-                    if (VEC) {
-                        const uint2 q = 4 * t < limit ? *reinterpret_cast<const uint2*>(row + 4 * t) : make_uint2(0, 0);
-                        fb[j][0] = q.x; fb[j][1] = q.y;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            fb[j][i] = (4 * t + 2 * i < limit ? row[4 * t + 2 * i] : 0) |
-                                       uint32_t(4 * t + 2 * i + 1 < limit ? row[4 * t + 2 * i + 1] : 0) << 16;
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < RT / 2; ++i) load_eight<VEC>(row, 4 * RT * t + 8 * i, limit, fb[j] + 4 * i);
-                }
+            for (int i = 0; i < kUpFeatures / STEP; ++i, from += size_t(STEP) * p.rank) {
+                const bool in = f + i * STEP < p.n;
+                stage_eight<VEC>(to + i * STEP * ROW, in ? from : b, in ? r : p.rank, p.rank);
             }
-#pragma unroll
-            for (int s = 0; s < RT; ++s) {
-                const uint32_t fh[4] = {high[0][s].x, high[1][s].x, high[0][s].y, high[1][s].y};
-                const uint32_t fl[4] = {low[0][s].x, low[1][s].x, low[0][s].y, low[1][s].y};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    mma_16816<DT>(acc[j], fh, fb[j][2 * s], fb[j][2 * s + 1]);
-                    mma_16816<DT>(acc[j], fl, fb[j][2 * s], fb[j][2 * s + 1]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 w0 = unpack2(v0[j], DT), w1 = unpack2(v1[j], DT);
-                if (d0 == e) v0[j] = pack2(fmaf(acc[j][0], back[0], w0.x), fmaf(acc[j][1], back[0], w0.y), DT);
-                if (d1 == e) v1[j] = pack2(fmaf(acc[j][2], back[1], w1.x), fmaf(acc[j][3], back[1], w1.y), DT);
+            ahead_left &= ahead_left - 1;
+            if (!ahead_left) {
+                ahead_left = list;
+                ahead_f += kUpFeatures;
             }
         }
-        if (in0) store_eight<VEC>(o0, col, p.n, v0);
-        if (in1) store_eight<VEC>(o1, col, p.n, v1);
+        ++ahead;
+        slot = slot == kUpStages - 1 ? 0 : slot + 1;
+        copy_async_commit();
+    };
+    for (int i = 0; i < kUpStages - 1; ++i) fetch();
+    uint32_t v[2][2][4], next[2][2][4];              // y: two blocks of 32 features, two tokens
+    auto load_y = [&](int f) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int col = f + h * 32 + 8 * t;
+            load_eight<VEC>(y0, in0 ? col : p.n, p.n, next[h][0]);
+            load_eight<VEC>(y1, in1 ? col : p.n, p.n, next[h][1]);
+        }
+    };
+    load_y(f0);
+    uint64_t left = 0;
+    int f = f0 - kUpFeatures;
+    for (int unit = 0; unit < units; ++unit) {
+        if (!left) {                                 // the next features
+            left = list;
+            f += kUpFeatures;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[h][0][i] = next[h][0][i];
+                    v[h][1][i] = next[h][1][i];
+                }
+            if (f + kUpFeatures < f1) load_y(f + kUpFeatures);
+        }
+        copy_async_wait<kUpStages - 2>();
+        __syncthreads();
+        fetch();
+        used = unit ? (used == kUpStages - 1 ? 0 : used + 1) : 0;
+        if (left) {
+            const int d = own[__ffsll(left) - 1];
+            const uint32_t from = ring + used * (kUpFeatures * ROW) + 8 * RT * t;
+            if (__any_sync(0xFFFFFFFFu, d0 == d || d1 == d)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float acc[4][4] = {};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t fb[2 * RT];
+                        const uint32_t at = from + (h * 32 + 8 * (g >> 1) + 2 * j + (g & 1)) * ROW;
+                        if constexpr (RT == 1) ld_shared_v2(at, fb[0], fb[1]);
+                        else
+#pragma unroll
+                            for (int i = 0; i < RT / 2; ++i) ld_shared_v4(at + 16 * i, *reinterpret_cast<uint32_t(*)[4]>(fb + 4 * i));
+#pragma unroll
+                        for (int s = 0; s < RT; ++s) {
+                            const uint32_t fh[4] = {high[0][s].x, high[1][s].x, high[0][s].y, high[1][s].y};
+                            const uint32_t fl[4] = {low[0][s].x, low[1][s].x, low[0][s].y, low[1][s].y};
+                            mma_16816<DT>(acc[j], fh, fb[2 * s], fb[2 * s + 1]);
+                            mma_16816<DT>(acc[j], fl, fb[2 * s], fb[2 * s + 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 w0 = unpack2(v[h][0][j], DT), w1 = unpack2(v[h][1][j], DT);
+                        if (d0 == d) v[h][0][j] = pack2(fmaf(acc[j][0], back[0], w0.x), fmaf(acc[j][1], back[0], w0.y), DT);
+                        if (d1 == d) v[h][1][j] = pack2(fmaf(acc[j][2], back[1], w1.x), fmaf(acc[j][3], back[1], w1.y), DT);
+                    }
+                }
+            }
+            left &= left - 1;
+        }
+        if (!left) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int col = f + h * 32 + 8 * t;
+                if (in0) store_eight<VEC>(o0, col, p.n, v[h][0]);
+                if (in1) store_eight<VEC>(o1, col, p.n, v[h][1]);
+            }
+        }
     }
 }
 

@@ -151,7 +151,7 @@ int launch(void (*kernel)(Args), dim3 grid, int threads, size_t smem, unsigned c
     cfg.numAttrs = n;
     cudaError_t e = launch_error_to_inject();
     // (48 KB hold what a kernel declares, too)
-    if (e == cudaSuccess && smem > 32 * 1024) e = allow_smem(reinterpret_cast<const void*>(kernel), all_shared);
+    if (e == cudaSuccess && (smem > 32 * 1024 || all_shared)) e = allow_smem(reinterpret_cast<const void*>(kernel), all_shared);
     if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, args);
     return e == cudaSuccess ? EQUARX_OK : cuda_failure(e);
 }
