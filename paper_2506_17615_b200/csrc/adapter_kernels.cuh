@@ -339,12 +339,13 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
     cluster_sync();                                  // the others' sums have been read
 }
 
-// out = y + S B^T for 64 tokens, 64 features at a time, whose rows of B come through a ring in shared memory; the next features' y
-// is on its way to registers meanwhile.  A warp keeps S of 16 tokens in registers.  Column c of the j-th of four products is
+// out = y + S B^T for 64 tokens, 64 features at a time, whose rows of B and y come through rings in shared memory (of y a thread
+// copies and reads its own elements).  A warp keeps S of 16 tokens in registers.  Column c of the j-th of four products is
 // feature 8 (c / 2) + 2 j + c % 2, so that a thread ends up with 8 neighbours.
 constexpr int kUpWarps = 4, kUpTokens = 16 * kUpWarps, kUpFeatures = 64, kUpStages = 3;
 template <int RT> constexpr int kUpRow = 32 * RT + (RT >= 4 ? 16 : 0);                   // bytes of a row of B in shared memory
-template <int RT> constexpr int kUpSmem = kUpStages * kUpFeatures * kUpRow<RT>;
+constexpr int kUpY = kUpTokens * kUpFeatures * 2;                                        // bytes of y
+template <int RT> constexpr int kUpSmem = kUpStages * (kUpFeatures * kUpRow<RT> + kUpY);
 template <bool VEC>
 __device__ __forceinline__ void store_eight(uint16_t* row, int col, int cols, const uint32_t (&v)[4]) {
     if (VEC) {
@@ -407,7 +408,19 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
     const int per = max(adapters, 1), units = (f1 - f0 + kUpFeatures - 1) / kUpFeatures * per;
     int ahead = 0, ahead_f = f0, slot = 0, used = 0; // the unit that is copied next, its place and that of the one in use
     uint64_t ahead_left = list;
+    int y_slot = 0;                                  // of the features that are copied next; one block of them may have many units
+    const uint32_t y_ring = ring + kUpStages * kUpFeatures * ROW + tid * 16;
     auto fetch = [&] {
+        if (ahead < units && ahead_left == list) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int col = ahead_f + h * 32 + 8 * t;
+                stage_eight<VEC>(y_ring + y_slot * kUpY + h * (kUpY / 2), in0 ? y0 : b, in0 ? col : p.n, p.n);
+                stage_eight<VEC>(y_ring + y_slot * kUpY + h * (kUpY / 2) + kUpY / 4, in1 ? y1 : b, in1 ? col : p.n, p.n);
+            }
+            y_slot = y_slot == kUpStages - 1 ? 0 : y_slot + 1;
+            if (!adapters) ahead_f += kUpFeatures;
+        }
         if (ahead < units && adapters) {
             // a thread copies the same piece of every STEP-th row
             constexpr int STEP = 32 * kUpWarps / (R / 8);
@@ -430,33 +443,22 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
         copy_async_commit();
     };
     for (int i = 0; i < kUpStages - 1; ++i) fetch();
-    uint32_t v[2][2][4], next[2][2][4];              // y: two blocks of 32 features, two tokens
-    auto load_y = [&](int f) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int col = f + h * 32 + 8 * t;
-            load_eight<VEC>(y0, in0 ? col : p.n, p.n, next[h][0]);
-            load_eight<VEC>(y1, in1 ? col : p.n, p.n, next[h][1]);
-        }
-    };
-    load_y(f0);
+    uint32_t v[2][2][4];                             // y: two blocks of 32 features, two tokens
+    int y_used = 0;
     uint64_t left = 0;
     int f = f0 - kUpFeatures;
     for (int unit = 0; unit < units; ++unit) {
+        copy_async_wait<kUpStages - 2>();
+        __syncthreads();
         if (!left) {                                 // the next features
             left = list;
             f += kUpFeatures;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[h][0][i] = next[h][0][i];
-                    v[h][1][i] = next[h][1][i];
-                }
-            if (f + kUpFeatures < f1) load_y(f + kUpFeatures);
+                for (int i = 0; i < 2; ++i) ld_shared_v4(y_ring + y_used * kUpY + (2 * h + i) * (kUpY / 4), v[h][i]);
+            y_used = y_used == kUpStages - 1 ? 0 : y_used + 1;
         }
-        copy_async_wait<kUpStages - 2>();
-        __syncthreads();
         fetch();
         used = unit ? (used == kUpStages - 1 ? 0 : used + 1) : 0;
         if (left) {
