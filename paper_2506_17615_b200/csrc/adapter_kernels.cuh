@@ -172,8 +172,8 @@ __device__ __forceinline__ uint32_t first_of_each(int d) {
 // thread's fragments are 16 neighbouring bytes): with 16 to 128 columns, and rows of several adapters in a tile, the
 // tensor cores' work is small beside the reading.
 //
-// A product runs once for each adapter that the tokens of a tile have, with nothing in the other tokens' places, and only this
-// adapter's tokens take its result: what is not finite in one request's adapter does not reach another request.
+// A product runs once for each adapter that the tokens of a tile have, and only this adapter's tokens take their rows of its
+// result: what is not finite in one request's adapter does not reach another request.
 //
 // S is rounded as the tensor cores want it, to two numbers of the 16-bit type, high and low, whose sum has 16 bits (bf16) or
 // 22: 2^-17 of S.  In fp16 a token's S is scaled by a power of two first, so that its range does not matter.
@@ -218,9 +218,6 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
     const int chunks = (p.k + CHUNK - 1) / CHUNK;
     const int c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
     const int part = warp % SPLIT, r0 = warp / SPLIT * 16;
-    int adapter[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) adapter[j] = own[j * 8 + g];
     for (uint32_t left = first_of_each(own[lane]); left; left &= left - 1) {
         const int d = own[__ffs(left) - 1];
         // a thread copies the same piece of every STEP-th row of x and A
@@ -262,10 +259,7 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
                 const uint32_t at = (part + u * SPLIT) * 64 + t * 16;
                 uint32_t fx[NT][4], fa[2][4];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    ld_shared_v4(from + (j * 8 + g) * ROW + at, fx[j]);
-                    if (adapter[j] != d) fx[j][0] = fx[j][1] = fx[j][2] = fx[j][3] = 0;
-                }
+                for (int j = 0; j < NT; ++j) ld_shared_v4(from + (j * 8 + g) * ROW + at, fx[j]);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) ld_shared_v4(from + (kDownTokens + r0 + half * 8 + g) * ROW + at, fa[half]);
 #pragma unroll
@@ -343,6 +337,7 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
 // copies and reads its own elements).  A warp keeps S of 16 tokens in registers.  Column c of the j-th of four products is
 // feature 8 (c / 2) + 2 j + c % 2, so that a thread ends up with 8 neighbours.
 constexpr int kUpWarps = 4, kUpTokens = 16 * kUpWarps, kUpFeatures = 64, kUpStages = 3;
+constexpr int kUpAtOnce = 4;                     // products whose sums do not wait for one another
 template <int RT> constexpr int kUpRow = 32 * RT + (RT >= 4 ? 16 : 0);                   // bytes of a row of B in shared memory
 constexpr int kUpY = kUpTokens * kUpFeatures * 2;                                        // bytes of y
 template <int RT> constexpr int kUpSmem = kUpStages * (kUpFeatures * kUpRow<RT> + kUpY);
@@ -464,25 +459,40 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
         if (left) {
             const int d = own[__ffsll(left) - 1];
             const uint32_t from = ring + used * (kUpFeatures * ROW) + 8 * RT * t;
+            const bool whole = __all_sync(0xFFFFFFFFu, d0 == d && d1 == d);
             if (__any_sync(0xFFFFFFFFu, d0 == d || d1 == d)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     float acc[4][4] = {};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t fb[2 * RT];
-                        const uint32_t at = from + (h * 32 + 8 * (g >> 1) + 2 * j + (g & 1)) * ROW;
-                        if constexpr (RT == 1) ld_shared_v2(at, fb[0], fb[1]);
-                        else
+                    for (int j = 0; j < 4; j += kUpAtOnce) {
+                        uint32_t fb[kUpAtOnce][2 * RT];
 #pragma unroll
-                            for (int i = 0; i < RT / 2; ++i) ld_shared_v4(at + 16 * i, *reinterpret_cast<uint32_t(*)[4]>(fb + 4 * i));
+                        for (int i = 0; i < kUpAtOnce; ++i) {
+                            const uint32_t at = from + (h * 32 + 8 * (g >> 1) + 2 * (j + i) + (g & 1)) * ROW;
+                            if constexpr (RT == 1) ld_shared_v2(at, fb[i][0], fb[i][1]);
+                            else
+#pragma unroll
+                                for (int q = 0; q < RT / 2; ++q) ld_shared_v4(at + 16 * q, *reinterpret_cast<uint32_t(*)[4]>(fb[i] + 4 * q));
+                        }
 #pragma unroll
                         for (int s = 0; s < RT; ++s) {
                             const uint32_t fh[4] = {high[0][s].x, high[1][s].x, high[0][s].y, high[1][s].y};
                             const uint32_t fl[4] = {low[0][s].x, low[1][s].x, low[0][s].y, low[1][s].y};
-                            mma_16816<DT>(acc[j], fh, fb[2 * s], fb[2 * s + 1]);
-                            mma_16816<DT>(acc[j], fl, fb[2 * s], fb[2 * s + 1]);
+#pragma unroll
+                            for (int i = 0; i < kUpAtOnce; ++i) mma_16816<DT>(acc[j + i], fh, fb[i][2 * s], fb[i][2 * s + 1]);
+#pragma unroll
+                            for (int i = 0; i < kUpAtOnce; ++i) mma_16816<DT>(acc[j + i], fl, fb[i][2 * s], fb[i][2 * s + 1]);
                         }
+                    }
+                    if (whole) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 w0 = unpack2(v[h][0][j], DT), w1 = unpack2(v[h][1][j], DT);
+                            v[h][0][j] = pack2(fmaf(acc[j][0], back[0], w0.x), fmaf(acc[j][1], back[0], w0.y), DT);
+                            v[h][1][j] = pack2(fmaf(acc[j][2], back[1], w1.x), fmaf(acc[j][3], back[1], w1.y), DT);
+                        }
+                        continue;
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
