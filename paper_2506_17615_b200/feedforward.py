@@ -25,6 +25,8 @@ import torch
 from . import _build, binding
 from .binding import ACT_GELU_TANH, ACT_SILU, FP4_MX, FP4_NV, EquarxError  # noqa: F401  (part of this module's interface)
 
+FP8_MX = 2      # names the 8-bit form where a choice of forms is taken (block.Block); the fp4_ calls refuse it
+
 _DTYPES = {torch.bfloat16: binding.BF16, torch.float16: binding.FP16, torch.float32: binding.FP32}
 
 _build.build_torch_module()
