@@ -625,7 +625,7 @@ int equarx_add_rms_norm_fp8(const void *x, size_t ldx, const void *residual, siz
  * With n = sum r and g = dy (offset + weight) of a row:
  *     dx = dsum + r (g - n mean(g n)),   dweight = sum over rows of dy n.
  * dx is the gradient of x and of the residual alike; dweight has the weight's type and may
- * be NULL, and then no workspace is needed.  Sums are taken in fp32 in a fixed order.
+ * be NULL, and then, and for a few rows, no workspace is needed.  Sums are taken in fp32 in a fixed order.
  */
 size_t equarx_add_rms_norm_backward_workspace_bytes(size_t rows, size_t cols);
 int equarx_add_rms_norm_backward(const void *dy, size_t lddy, const void *dsum, size_t ldds,

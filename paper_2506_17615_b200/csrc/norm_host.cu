@@ -56,13 +56,16 @@ int launch_norm(const NormArgs& a, int dtype, int width, cudaStream_t stream) {
                         : launch_norm<kFp16, 1, EIGHT>(a, stream);
 }
 
-template <int DT, int W, int G>
+template <int DT, int W, int G, int MOST = kGradThreads>
 int launch_grad(const NormGradArgs& a, int threads, cudaStream_t stream) {
-    return launch(norm_grad_kernel<DT, W, G>, dim3(unsigned(a.count)), threads, W == 8 ? size_t(kGradStages) * 3 * 16 * G * threads : 0, 1,
-                  a, stream, true);
+    // the staged rows (12 bytes a column and more), or the sums in their place
+    const size_t smem = W == 8 ? size_t(kGradStages) * 3 * 16 * G * threads : a.together ? part_stride(a.cols) * sizeof(float) : 0;
+    return launch(norm_grad_kernel<DT, W, G, MOST>, dim3(unsigned(a.count)), threads, smem, unsigned(a.together), a, stream, true);
 }
 template <int DT, int W>
 int launch_grad(const NormGradArgs& a, cudaStream_t stream) {
+    if (a.cols > kGradColumns && a.cols <= kGradWide * 8 && a.rows <= 2 * a.count)
+        return launch_grad<DT, W, 1, kGradWide>(a, int(up(ceil_div(a.cols, 8), 32)), stream);
     const int threads = grad_threads(a.cols);
     switch (grad_groups(a.cols)) {
         case 1: return launch_grad<DT, W, 1>(a, threads, stream);
@@ -121,11 +124,19 @@ int check_sum(const void* x, size_t ldx, const void* residual, size_t ldr, const
     return overlap(s, Span{weight, cols * size_of(weight_dtype)}) ? EQUARX_ERR_ALIAS : EQUARX_OK;
 }
 
+// Rows up to which the CTAs of the backward pass are one cluster that adds the weight's gradient up itself.  Through Python, where a
+// launch takes the host 2 us, 16 rows of 3840 take 5.2 us against 7.5; 32 rows are four for each CTA, and 10.7 against 7.8.
+constexpr size_t kTogether = 16;
+inline bool together(size_t rows, size_t cols) { return rows <= kTogether && grad_groups(cols); }
+
 // CTAs of the backward pass, each with a part of the weight's gradient: as many as run at one time on 148 SMs (three on each,
 // more where rows are short), two rows at least for each, and not so many that the parts of very long rows outgrow the matrices
 inline size_t norm_parts(size_t rows, size_t cols) {
     const size_t most = 148 * std::max<size_t>(1, std::min<size_t>(8, (grad_groups(cols) > 3 ? 1 : 3) * kGradThreads / grad_threads(cols)));
-    return std::min({ceil_div(rows, 2), most, std::max<size_t>(1, (size_t(1) << 28) / cols)});
+    return std::min({ceil_div(rows, 2), together(rows, cols) ? 8 : most, std::max<size_t>(1, (size_t(1) << 28) / cols)});
+}
+inline size_t norm_workspace(size_t rows, size_t cols) {
+    return together(rows, cols) ? 0 : norm_parts(rows, cols) * part_stride(cols) * sizeof(float);
 }
 
 }  // namespace
@@ -176,7 +187,7 @@ int equarx_add_rms_norm_fp8(const void* x, size_t ldx, const void* residual, siz
 }
 
 size_t equarx_add_rms_norm_backward_workspace_bytes(size_t rows, size_t cols) {
-    return rows > kMaxDim || bad_dim(cols) ? 0 : norm_parts(rows, cols) * cols * sizeof(float);
+    return rows > kMaxDim || bad_dim(cols) ? 0 : norm_workspace(rows, cols);
 }
 
 int equarx_add_rms_norm_backward(const void* dy, size_t lddy, const void* dsum, size_t ldds, const void* sum, size_t lds,
@@ -187,7 +198,7 @@ int equarx_add_rms_norm_backward(const void* dy, size_t lddy, const void* dsum, 
     if (rows > kMaxDim || bad_dim(cols) || bad_ld(lddy, cols) || (dsum && bad_ld(ldds, cols)) || bad_ld(lds, cols) || bad_ld(lddx, cols))
         return EQUARX_ERR_COUNT;
     if (!std::isfinite(offset)) return EQUARX_ERR_VALUE;
-    const size_t size = size_of(weight_dtype), need = dweight ? norm_parts(rows, cols) * cols * sizeof(float) : 0;
+    const size_t size = size_of(weight_dtype), need = dweight ? norm_workspace(rows, cols) : 0;
     if (rows && (!dy || !sum || !factors || !weight || !dx || (need && !workspace))) return EQUARX_ERR_NULL;
     if (rows && workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
     for (const void* p : {dy, dsum, sum, static_cast<const void*>(dx)})
@@ -211,7 +222,8 @@ int equarx_add_rms_norm_backward(const void* dy, size_t lddy, const void* dsum, 
     a.weight = weight;
     a.dx = dx;
     a.dw = dweight;
-    a.parts = dweight ? static_cast<float*>(workspace) : nullptr;
+    a.parts = need ? static_cast<float*>(workspace) : nullptr;
+    a.together = dweight && together(rows, cols) ? int(norm_parts(rows, cols)) : 0;
     a.lddy = lddy;
     a.ldds = ldds;
     a.lds = lds;
@@ -228,9 +240,9 @@ int equarx_add_rms_norm_backward(const void* dy, size_t lddy, const void* dsum, 
     access.add(dx, lddx);
     access.add_weight(weight, a.fp32);
     TRY(dtype == EQUARX_BF16 ? launch_grad<kBf16>(a, access.width(), stream) : launch_grad<kFp16>(a, access.width(), stream));
-    if (!dweight) return EQUARX_OK;
-    return launch(dtype == EQUARX_BF16 ? norm_parts_kernel<kBf16> : norm_parts_kernel<kFp16>, dim3(unsigned(ceil_div(cols, 32))), 1024, 0,
-                  1, a, stream);
+    if (!need) return EQUARX_OK;
+    return launch(dtype == EQUARX_BF16 ? norm_parts_kernel<kBf16> : norm_parts_kernel<kFp16>, dim3(unsigned(ceil_div(cols, 32))),
+                  kPartsThreads, 0, 1, a, stream, true);
 }
 
 }  // extern "C"

@@ -16,6 +16,7 @@ constexpr int kGradThreads = 224;          // of the backward pass, at most
 constexpr int kGradColumns = kGradThreads * 8;
 constexpr int kGradGroups = 5;             // groups of 8 columns for each of its threads, at most
 constexpr int kGradStages = 2;             // its rows in shared memory
+constexpr int kGradWide = 1024;            // where each CTA has few rows, at most
 constexpr int kRowThreads = 1024;          // of the forward pass, at most
 
 // Eight elements of a row in a thread's registers, pairs of neighbours.  W = 8: all neighbours, for rows that start on
@@ -259,27 +260,32 @@ struct NormGradArgs {
     const void *dy, *dsum, *sum, *weight;  // dsum may be null
     const float* factors;                  // r of each row
     void* dx;
-    float* parts;                          // [CTAs][columns], null: no gradient of the weight
-    void* dw;
+    float* parts;                          // [CTAs][columns to 8], or null
+    void* dw;                              // null: no gradient of the weight
     size_t lddy, ldds, lds, lddx;
     float inverse, offset;
     int rows, cols, fp32, count;           // count: parts
+    int together;                          // the CTAs are one cluster, which adds their parts up itself
 };
+
+__host__ __device__ inline size_t part_stride(size_t cols) { return (cols + 7) & ~size_t(7); }
 
 // n = sum r, g = dy (offset + weight):  dx = dsum + r g - (r mean(g n)) n, dweight = sum over rows of dy n.
 // A CTA takes every gridDim-th row, a thread the same G groups of 8 columns of each, whose weight gradients it adds up in
 // registers.  W = 8: a row is copied to shared memory while the one before it is worked on; a thread copies and reads its own
-// elements, so no barrier is needed for them, and reads them twice, so that registers hold weights and sums only.  G = 0: rows that
-// this does not hold; sums in the CTA's part in memory.
-template <int DT, int W, int G>
-__global__ void __launch_bounds__(kGradThreads, G > 3 ? 1 : 3) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
+// elements, so no barrier is needed for them, and reads them twice, so that registers hold weights and sums only.  MOST = 1024: up
+// to 8192 columns with one group each, for CTAs of two rows, whose time is mostly the fetching of instructions.  G = 0: rows that
+// this does not hold; sums in the CTA's part in memory.  Few rows: the CTAs are a cluster and add their parts of the weight's
+// gradient up through distributed shared memory, which saves a launch.
+template <int DT, int W, int G, int MOST>
+__global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
     constexpr bool STAGED = W == 8 && G > 0;
     constexpr int N = G ? G : 1;
     extern __shared__ __align__(16) uint8_t staged[];
     __shared__ float shared[2][32];        // a thread writes one again only after the barrier of the row between
     const int span = blockDim.x * 8;
     const bool add = p.dsum != nullptr;
-    float* const part = p.parts ? p.parts + size_t(blockIdx.x) * p.cols : nullptr;
+    float* const part = p.parts ? p.parts + blockIdx.x * part_stride(p.cols) : nullptr;
     grid_launch();
     grid_wait();
     float2 w[N][4], acc[N][4];
@@ -385,37 +391,64 @@ __global__ void __launch_bounds__(kGradThreads, G > 3 ? 1 : 3) norm_grad_kernel(
             stage = stage == kGradStages - 1 ? 0 : stage + 1;
         }
     }
-    if (G && part) {
+    if (G && p.dw) {
+        float* const to = p.together ? reinterpret_cast<float*>(staged) : part;
+        __syncthreads();                                   // the rows in shared memory have been read
 #pragma unroll
-        for (int g = 0; g < N; ++g)
+        for (int g = 0; g < N; ++g) {
+            if constexpr (W == 8) {
+                if (column_of<W>(g * span, 0) < p.cols) {
+                    float4* const q = reinterpret_cast<float4*>(to + column_of<W>(g * span, 0));
+                    q[0] = make_float4(acc[g][0].x, acc[g][0].y, acc[g][1].x, acc[g][1].y);
+                    q[1] = make_float4(acc[g][2].x, acc[g][2].y, acc[g][3].x, acc[g][3].y);
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int at = column_of<W>(g * span, e);
-                if (at < p.cols) part[at] = e & 1 ? acc[g][e / 2].y : acc[g][e / 2].x;
+                for (int i = 0; i < 4; ++i) {
+                    const int at = column_of<W>(g * span, 2 * i), after = column_of<W>(g * span, 2 * i + 1);
+                    if (W == 2 && at < p.cols) *reinterpret_cast<float2*>(to + at) = acc[g][i];
+                    if (W == 1 && at < p.cols) to[at] = acc[g][i].x;
+                    if (W == 1 && after < p.cols) to[after] = acc[g][i].y;
+                }
             }
+        }
+        if (p.together) {
+            cluster_sync();
+            for (int col = blockIdx.x * blockDim.x + threadIdx.x; col < p.cols; col += gridDim.x * blockDim.x) {
+                float v = 0.0f;
+                for (int q = 0; q < p.together; ++q) v += ld_cluster_f32(peer_addr(smem_addr(staged) + col * 4, q));
+                store1(p.dw, col, v, p.fp32 ? int(kFp32) : DT);
+            }
+            __syncwarp();
+            cluster_sync();                                // the others' parts have been read
+        }
     }
 }
 
-// the parts of 32 columns, 32 threads a column, in a fixed order
+// The parts of 32 columns, a lane each, split among the warps and added in a fixed order.  Large CTAs: 256 threads are room enough
+// beside the launch before, and what waits there costs the launch after (backward pass of 8192 x 5376, one after the other: 108 us,
+// with 1024 threads 75).
+constexpr int kPartsThreads = 1024;
 template <int DT>
-__global__ void __launch_bounds__(1024) norm_parts_kernel(const __grid_constant__ NormGradArgs p) {
-    __shared__ float shared[32][33];
-    const int lane = threadIdx.x & 31, which = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+__global__ void __launch_bounds__(kPartsThreads) norm_parts_kernel(const __grid_constant__ NormGradArgs p) {
+    constexpr int WARPS = kPartsThreads / 32;
+    __shared__ float shared[WARPS][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     grid_launch();
     grid_wait();
     float v = 0.0f;
     if (col < p.cols) {
+        const size_t stride = part_stride(p.cols);
+        const float* q = p.parts + warp * stride + col;
 #pragma unroll 4
-        for (int i = which; i < p.count; i += 32) v += __ldcg(p.parts + size_t(i) * p.cols + col);
+        for (int i = warp; i < p.count; i += WARPS, q += WARPS * stride) v += __ldcg(q);
     }
-    shared[which][lane] = v;
+    shared[warp][lane] = v;
     __syncthreads();
-    // a warp takes a column
-    v = shared[lane][which];
+    if (warp || col >= p.cols) return;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-    const int mine = blockIdx.x * 32 + which;
-    if (lane == 0 && mine < p.cols) store1(p.dw, mine, v, p.fp32 ? int(kFp32) : DT);
+    for (int i = 1; i < WARPS; ++i) v += shared[i][lane];
+    store1(p.dw, col, v, p.fp32 ? int(kFp32) : DT);
 }
 
 }  // namespace ff

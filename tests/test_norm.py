@@ -6,7 +6,7 @@ fp32 numbers: one row in 2^20.)
 
 Bounds of the gradients, relative to the sums of magnitudes: n, g and their product take 4 roundings to fp32; a row's sum
 passes 4 pairs of columns for each 1792 columns of the row, and 11 steps of a tree.  A sum over rows passes fewer
-additions than there are rows, and 8 more.
+additions than there are rows, and 10 more.
 """
 import pytest
 import torch
@@ -59,10 +59,11 @@ def test_forward_refuses_bad_arguments():
 
 
 def test_backward_refuses_bad_arguments():
-    need = eq.add_rms_norm_backward_workspace_bytes(4, 64)
-    assert need == 2 * 64 * 4 and eq.add_rms_norm_backward_workspace_bytes(4, 0) == 0
+    need = eq.add_rms_norm_backward_workspace_bytes(40, 64)
+    assert need == 20 * 64 * 4 and eq.add_rms_norm_backward_workspace_bytes(40, 0) == 0
+    assert eq.add_rms_norm_backward_workspace_bytes(4, 64) == 0                  # a few rows need none
     a = dict(dy=A, lddy=64, dsum=A + GB, ldds=64, sum=A + 2 * GB, lds=64, factors=A + 3 * GB, weight=A + 4 * GB, dtype=eq.FP16,
-             weight_dtype=eq.FP16, rows=4, cols=64, offset=1.0, dx=A + 5 * GB, lddx=64, dweight=A + 6 * GB, workspace=A + 7 * GB,
+             weight_dtype=eq.FP16, rows=40, cols=64, offset=1.0, dx=A + 5 * GB, lddx=64, dweight=A + 6 * GB, workspace=A + 7 * GB,
              workspace_bytes=need)
     f = eq.add_rms_norm_backward
     for key in ("dy", "sum", "factors", "weight", "dx", "workspace"):
@@ -221,12 +222,12 @@ def gradients(dy, dsum, total, w, eps, offset):
     ec = steps * EPS * (g * n).abs().mean(1, keepdim=True)
     # dx = dsum + r g - c n takes two more roundings, of dsum + r g (no more than |dx| + |c n|) and of dx
     ex = r * (6 * EPS * (g.abs() + (n * (g * n).mean(1, keepdim=True)).abs()) + n.abs() * ec) + 2 * EPS * dx.abs()
-    return (dx, ex), ((dy * n).sum(0), (rows + 8 + 4) * EPS * (dy * n).abs().sum(0))
+    return (dx, ex), ((dy * n).sum(0), (rows + 10 + 4) * EPS * (dy * n).abs().sum(0))
 
 
 @gpu
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,cols,pad", SHAPES + [(1000, 64, 0), (5000, 40, 0), (450, 16400, 0), (450, 17001, 0)])
+@pytest.mark.parametrize("rows,cols,pad", SHAPES + [(2, 842, 0), (16, 5376, 0), (17, 1001, 3), (16, 8960, 0), (33, 40, 0), (7, 20001, 0), (1000, 64, 0), (5000, 40, 0), (450, 16400, 0), (450, 17001, 0)])
 def test_gradients(dtype, rows, cols, pad):
     for wtype, offset in ((dtype, 1.0), (torch.float32, 0.0)):
         x, residual, w = inputs(rows, cols, rows + cols, dtype, wtype, offset, pad)
@@ -283,7 +284,7 @@ def test_backward_of_views_that_start_anywhere(rows, cols, offset):
     vy.copy_(dy), vd.copy_(dsum), vs.copy_(s)
     dw = torch.full((cols + offset + 8,), -77.0, device="cuda", dtype=dtype)
     nb = eq.add_rms_norm_backward_workspace_bytes(rows, cols)
-    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
     eq.add_rms_norm_backward(vy, ld, vd, ld, vs, ld, factors, w, eq.BF16, eq.BF16, rows, cols, 0.0, vx, ld, dw[offset:], ws, nb, stream)
     ref.assert_within(vx, want[0][0], ref.rounded(*want[0], dtype), "dx")
     ref.assert_within(dw[offset:offset + cols], want[1][0], ref.rounded(*want[1], dtype), "dw")
