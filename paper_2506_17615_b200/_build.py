@@ -12,7 +12,8 @@ SOURCES = [os.path.join(_CSRC, name) for name in ("equarx_host.cu", "feedforward
                                                     "adapter_host.cu")]
 DEPENDS = SOURCES + [os.path.join(_CSRC, name) for name in ("equarx_kernels.cuh", "equarx_internal.h", "tensor_ops.cuh",
                                                             "feedforward_kernels.cuh", "elements.cuh", "host_common.h",
-                                                            "norm_kernels.cuh", "adapter_kernels.cuh")] + \
+                                                            "norm_kernels.cuh", "adapter_kernels.cuh",
+                                                            "adapter_tiles.cuh", "host_maps.h")] + \
     [os.path.join(os.path.dirname(_HERE), "include", "equarx.h")]
 LIB = os.path.join(_HERE, "libequarx.so")
 TORCH_SOURCE = os.path.join(_CSRC, "feedforward_torch.cpp")

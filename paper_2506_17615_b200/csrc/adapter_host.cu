@@ -1,6 +1,6 @@
 // C ABI of the low-rank adapters (include/equarx.h): argument checks, launches.
-#include "adapter_kernels.cuh"
-#include "host_common.h"
+#include "adapter_tiles.cuh"
+#include "host_maps.h"
 
 namespace {
 
@@ -20,28 +20,60 @@ inline size_t adapter_workspace(size_t tokens, size_t rank) {
     return tokens <= kTokenForm ? 0 : sums_bytes(tokens, rank) + up(tokens * sizeof(float), 256);
 }
 
-template <int DT, int RT, bool VEC>
-int launch_adapters(AdapterArgs& a, int sms, cudaStream_t stream) {
+// Whole waves of CTAs, each with its share of `work` steps and what starting costs, `start` steps: the number of CTAs for each tile
+// that takes least.  `most`: CTAs that run at one time.
+size_t share(size_t tiles, size_t work, size_t start, size_t most, size_t limit, bool powers) {
+    size_t best = 1, least = ~size_t(0);
+    for (size_t c = 1; c <= std::min(limit, work); powers ? c *= 2 : ++c) {
+        const size_t cost = ceil_div(tiles * c, most) * (ceil_div(work, c) + start);
+        if (cost < least) {
+            least = cost;
+            best = c;
+        }
+    }
+    return best;
+}
+
+template <int DT, int RT>
+int launch_tiles(AdapterArgs& a, int sms, cudaStream_t stream) {
+    constexpr size_t R = 16 * RT;
+    const size_t tiles = ceil_div(a.tokens, kTileTokens), blocks = ceil_div(a.n, kUpBlock);
+    AdapterMaps m = {};
+    TRY(make_map(m.x, a.x, 2, a.k, a.tokens, a.ldx * 2, kTileTokens));
+    TRY(make_map(m.a, a.a, 2, a.k, size_t(a.adapters) * a.rank, size_t(a.k) * 2, R));
+    TRY(make_map(m.high, a.s, 2, R, a.tokens, R * 4, kTileTokens));
+    TRY(make_map(m.low, a.s + R, 2, R, a.tokens, R * 4, kTileTokens));
+    TRY(make_map(m.b, a.b, 2, a.rank, size_t(a.adapters) * a.n, size_t(a.rank) * 2, kUpBlock));
+    TRY(make_map(m.y, a.y, 2, a.n, a.tokens, a.ldy * 2, kTileTokens));
+    TRY(make_map(m.out, a.out, 2, a.n, a.tokens, a.ldo * 2, 32));
+    // a CTA's start and the exchange of sums take as long as six chunks of 64 columns, the start of the second product as three blocks
+    a.ctas = int(share(tiles, ceil_div(a.k, 64), 6, sms * (RT == 8 ? 1 : 2), 8, true));
+    a.blocks = int(ceil_div(blocks, share(tiles, blocks, 3, sms, ceil_div(2 * sms, tiles), false)));
+    m.p = a;
+    TRY(launch(adapter_down_tiles<DT, RT>, dim3(unsigned(tiles * a.ctas)), kAdapterTileThreads, kDownTileSmem<RT>, unsigned(a.ctas), m, stream, true));
+    return launch(adapter_up_tiles<DT, RT>, dim3(unsigned(tiles), unsigned(ceil_div(blocks, a.blocks))), kAdapterTileThreads, kUpTileSmem<RT>, 1,
+                  m, stream, true);
+}
+
+template <int DT, int RT>
+int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
     if (size_t(a.tokens) <= kTokenForm) {
         a.ctas = a.tokens * 8 <= 2 * sms ? 8 : 4;
-        return launch(adapter_token_kernel<DT, RT, VEC>, dim3(unsigned(a.tokens) * a.ctas), kAdapterThreads, 0, unsigned(a.ctas), a, stream);
+        return launch(vec ? adapter_token_kernel<DT, RT, true> : adapter_token_kernel<DT, RT, false>, dim3(unsigned(a.tokens) * a.ctas),
+                      kAdapterThreads, 0, unsigned(a.ctas), a, stream);
     }
+    if (a.tiles) return launch_tiles<DT, RT>(a, sms, stream);
     // two CTAs run on an SM: where there are few tiles, up to eight share one
     const size_t tiles = ceil_div(a.tokens, kDownTokens);
     a.ctas = 1;
     while (a.ctas < 8 && tiles * a.ctas * 2 <= size_t(2 * sms)) a.ctas *= 2;
-    TRY(launch(adapter_down_kernel<DT, RT, VEC>, dim3(unsigned(tiles * a.ctas)), kAdapterThreads, kDownSmem<RT>, unsigned(a.ctas), a, stream,
-               true));
+    TRY(launch(adapter_down_kernel<DT, RT>, dim3(unsigned(tiles * a.ctas)), kAdapterThreads, kDownSmem<RT>, unsigned(a.ctas), a, stream, true));
     // four CTAs run on an SM at one time; twice as many, so that a tile with two adapters holds up less
     const size_t up_tiles = ceil_div(a.tokens, kUpTokens), all = ceil_div(a.n, kUpFeatures);
     const size_t parts = std::max<size_t>(1, std::min(size_t(8 * sms) / up_tiles, ceil_div(all, 2)));
     a.blocks = int(ceil_div(all, parts));
-    return launch(adapter_up_kernel<DT, RT, VEC>, dim3(unsigned(up_tiles), unsigned(ceil_div(all, a.blocks))), 32 * kUpWarps, kUpSmem<RT>, 1, a,
-                  stream, true);
-}
-template <int DT, int RT>
-int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
-    return vec ? launch_adapters<DT, RT, true>(a, sms, stream) : launch_adapters<DT, RT, false>(a, sms, stream);
+    return launch(adapter_up_kernel<DT, RT>, dim3(unsigned(up_tiles), unsigned(ceil_div(all, a.blocks))), 32 * kUpWarps, kUpSmem<RT>, 1, a, stream,
+                  true);
 }
 template <int DT>
 int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
@@ -52,6 +84,15 @@ int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
 }
 
 }  // namespace
+
+namespace equarx {
+cudaError_t adapters_gave_up(uint32_t& seen) {
+    const uint32_t zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(&seen, tc::g_gave_up, sizeof(seen));
+    if (e == cudaSuccess && seen) e = cudaMemcpyToSymbol(tc::g_gave_up, &zero, sizeof(zero));
+    return e;
+}
+}  // namespace equarx
 
 extern "C" {
 
@@ -100,8 +141,10 @@ int equarx_add_adapters(const void* y, size_t ldy, const void* x, size_t ldx, co
     p.adapters = int(adapters);
     int sms;
     TRY(current_device(sms));
-    bool vec = k % 8 == 0 && n % 8 == 0 && rank % 8 == 0 && aligned(a, 16) && aligned(b, 16);
-    vec = vec && unit_of(y, ldy, 2) >= 16 && unit_of(x, ldx, 2) >= 16 && unit_of(out, ldo, 2) >= 16;
+    // rows that start on multiples of 16 bytes; TMA counts the rows of all adapters together
+    const bool vec = k % 8 == 0 && rank % 8 == 0 && aligned(a, 16) && aligned(b, 16) && unit_of(x, ldx, 2) >= 16;
+    p.tiles = vec && unit_of(y, ldy, 2) >= 16 && unit_of(out, ldo, 2) >= 16 && adapters && adapters * rank <= size_t(INT32_MAX) &&
+              adapters * n <= size_t(INT32_MAX);
     return dtype == EQUARX_BF16 ? launch_adapters<kBf16>(p, vec, sms, stream) : launch_adapters<kFp16>(p, vec, sms, stream);
 }
 

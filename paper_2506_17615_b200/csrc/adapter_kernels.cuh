@@ -23,7 +23,8 @@ struct AdapterArgs {
     size_t ldy, ldx, ldo;
     int tokens, k, n, rank, adapters;
     int ctas;                         // of a cluster, which split k (and, for few tokens, n)
-    int blocks;                       // of 64 features, that a CTA of the second product takes
+    int tiles;                        // many tokens: through TMA
+    int blocks;                       // of features, that a CTA of the second product takes
 };
 constexpr int kAdapterWarps = 8, kAdapterThreads = 32 * kAdapterWarps;
 // ranks are padded to 16 RT, RT = 1, 2, 4 or 8
@@ -178,16 +179,45 @@ __device__ __forceinline__ uint32_t first_of_each(int d) {
 // S is rounded as the tensor cores want it, to two numbers of the 16-bit type, high and low, whose sum has 16 bits (bf16) or
 // 22: 2^-17 of S.  In fp16 a token's S is scaled by a power of two first, so that its range does not matter.
 
-// The same 16 bytes in shared memory: copied while products run (VEC), else element by element
-template <bool VEC>
-__device__ __forceinline__ void stage_eight(uint32_t to, const uint16_t* row, int col, int cols) {
-    if (VEC) {
-        copy_async_16(to, row + (col < cols ? col : 0), col < cols ? 16 : 0);
-    } else {
-        uint32_t v[4];
-        load_eight<false>(row, col, cols, v);
-        st_shared_v4(to, v[0], v[1], v[2], v[3]);
+// A token's S, a warp's lanes 32 ranks apart: scaled, split and stored
+template <int DT, int R>
+__device__ __forceinline__ void store_sums(const AdapterArgs& p, int token, int adapter, float (&v)[(R + 31) / 32]) {
+    constexpr int PER = (R + 31) / 32;
+    const int lane = threadIdx.x & 31;
+    const float c = p.scale ? p.scale[adapter] : 1.0f;
+    float top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        v[j] *= c;
+        if (fabsf(v[j]) < __uint_as_float(kInfBits)) top = fmaxf(top, fabsf(v[j]));
     }
+    float times = 1.0f;
+    if constexpr (DT == kFp16) {
+        // the largest finite one goes to [2^14, 2^15)
+        top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));
+        const int e = top > 0.0f ? min(max(int(__float_as_uint(top) >> 23) - 127 - 14, -100), 100) : 0;
+        times = __uint_as_float(uint32_t(127 - e) << 23);
+        if (lane == 0) p.back[token] = __uint_as_float(uint32_t(127 + e) << 23);
+    }
+    uint16_t* const to = p.s + size_t(token) * (2 * R);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int r = lane + 32 * j;
+        if (r >= R) continue;
+        const float s = v[j] * times;
+        const uint32_t high = pack2(s, 0.0f, DT);
+        const float rest = s - unpack2(high, DT).x;
+        to[r] = uint16_t(high);
+        // nothing is left of what is not finite
+        to[R + r] = fabsf(s) < __uint_as_float(kInfBits) ? uint16_t(pack2(rest, 0.0f, DT)) : uint16_t(0);
+    }
+}
+
+// The same into shared memory
+__device__ __forceinline__ void stage_eight(uint32_t to, const uint16_t* row, int col, int cols) {
+    uint32_t v[4];
+    load_eight<false>(row, col, cols, v);
+    st_shared_v4(to, v[0], v[1], v[2], v[3]);
 }
 
 // S of 32 tokens, transposed: 16 ranks x 8 tokens a product.  Chunks of x and A come through a ring in shared memory.  A warp has 16
@@ -199,7 +229,7 @@ template <int RT> constexpr int kDownRow = kDownChunk<RT> * 2 + 64;             
 template <int RT> constexpr int kDownSplit = kAdapterWarps / RT;                          // warps with the same ranks
 template <int RT> constexpr int kDownStageBytes = (kDownTokens + 16 * RT) * kDownRow<RT>;
 template <int RT> constexpr int kDownSmem = kDownStages * kDownStageBytes<RT> + kDownSplit<RT> * kDownTokens * 16 * RT * 4;
-template <int DT, int RT, bool VEC>
+template <int DT, int RT>
 __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const __grid_constant__ AdapterArgs p) {
     constexpr int R = 16 * RT, SPLIT = kDownSplit<RT>, NT = kDownTokens / 8, CHUNK = kDownChunk<RT>, ROW = kDownRow<RT>;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -233,23 +263,21 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
                 const uint32_t to = ring + ahead * kDownStageBytes<RT> + row0 * ROW + piece * 16;
                 const int col = c * CHUNK + piece * 8;
 #pragma unroll
-                for (int i = 0; i < XS; ++i) stage_eight<VEC>(to + i * STEP * ROW, xs[i], col, p.k);
+                for (int i = 0; i < XS; ++i) stage_eight(to + i * STEP * ROW, xs[i], col, p.k);
                 const uint16_t* from = rows;
 #pragma unroll
                 for (int i = 0; i < AS; ++i, from += size_t(STEP) * p.k)
                     if (R % STEP == 0 || row0 + i * STEP < R) {
                         const bool in = row0 + i * STEP < p.rank;
-                        stage_eight<VEC>(to + (kDownTokens + i * STEP) * ROW, in ? from : a, in ? col : p.k, p.k);
+                        stage_eight(to + (kDownTokens + i * STEP) * ROW, in ? from : a, in ? col : p.k, p.k);
                     }
             }
             ahead = ahead == kDownStages - 1 ? 0 : ahead + 1;
-            copy_async_commit();
         };
         float acc[NT][4] = {};
         for (int i = 0; i < kDownStages - 1; ++i) fetch(c0 + i);
         int stage = 0;
         for (int c = c0; c < c1; ++c) {
-            copy_async_wait<kDownStages - 2>();
             __syncthreads();                               // this chunk is there, the one before it has been used
             fetch(c + kDownStages - 1);
             const uint32_t from = ring + stage * kDownStageBytes<RT>;
@@ -296,38 +324,16 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
         const int i = own[token];
         if (i < 0) continue;
         constexpr int PER = (R + 31) / 32;
-        float v[PER], top = 0.0f;
+        float v[PER];
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int r = lane + 32 * j;
             v[j] = 0.0f;
-            if (r < R) {
-                const uint32_t from = smem_addr(sums + token * R + r);
-                for (int q = 0; q < p.ctas; ++q) v[j] += ld_cluster_f32(peer_addr(from, q));
-                if (p.scale) v[j] *= p.scale[i];
-            }
-            if (fabsf(v[j]) < __uint_as_float(kInfBits)) top = fmaxf(top, fabsf(v[j]));
-        }
-        float times = 1.0f;
-        if constexpr (DT == kFp16) {
-            // the largest finite one goes to [2^14, 2^15)
-            top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));
-            const int e = top > 0.0f ? min(max(int(__float_as_uint(top) >> 23) - 127 - 14, -100), 100) : 0;
-            times = __uint_as_float(uint32_t(127 - e) << 23);
-            if (lane == 0) p.back[first + token] = __uint_as_float(uint32_t(127 + e) << 23);
-        }
-        uint16_t* const to = p.s + size_t(first + token) * (2 * R);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int r = lane + 32 * j;
             if (r >= R) continue;
-            const float s = v[j] * times;
-            const uint32_t high = pack2(s, 0.0f, DT);
-            const float rest = s - unpack2(high, DT).x;
-            to[r] = uint16_t(high);
-            // nothing is left of what is not finite
-            to[R + r] = fabsf(s) < __uint_as_float(kInfBits) ? uint16_t(pack2(rest, 0.0f, DT)) : uint16_t(0);
+            const uint32_t from = smem_addr(sums + token * R + r);
+            for (int q = 0; q < p.ctas; ++q) v[j] += ld_cluster_f32(peer_addr(from, q));
         }
+        store_sums<DT, R>(p, first + token, i, v);
     }
     __syncwarp();
     cluster_sync();                                  // the others' sums have been read
@@ -341,17 +347,12 @@ constexpr int kUpAtOnce = 4;                     // products whose sums do not w
 template <int RT> constexpr int kUpRow = 32 * RT + (RT >= 4 ? 16 : 0);                   // bytes of a row of B in shared memory
 constexpr int kUpY = kUpTokens * kUpFeatures * 2;                                        // bytes of y
 template <int RT> constexpr int kUpSmem = kUpStages * (kUpFeatures * kUpRow<RT> + kUpY);
-template <bool VEC>
 __device__ __forceinline__ void store_eight(uint16_t* row, int col, int cols, const uint32_t (&v)[4]) {
-    if (VEC) {
-        if (col < cols) *reinterpret_cast<uint4*>(row + col) = make_uint4(v[0], v[1], v[2], v[3]);
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (col + i < cols) row[col + i] = uint16_t(v[i / 2] >> (i & 1) * 16);
-    }
+    for (int i = 0; i < 8; ++i)
+        if (col + i < cols) row[col + i] = uint16_t(v[i / 2] >> (i & 1) * 16);
 }
-template <int DT, int RT, bool VEC>
+template <int DT, int RT>
 __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_kernel(const __grid_constant__ AdapterArgs p) {
     constexpr int R = 16 * RT, ROW = kUpRow<RT>;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -410,8 +411,8 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int col = ahead_f + h * 32 + 8 * t;
-                stage_eight<VEC>(y_ring + y_slot * kUpY + h * (kUpY / 2), in0 ? y0 : b, in0 ? col : p.n, p.n);
-                stage_eight<VEC>(y_ring + y_slot * kUpY + h * (kUpY / 2) + kUpY / 4, in1 ? y1 : b, in1 ? col : p.n, p.n);
+                stage_eight(y_ring + y_slot * kUpY + h * (kUpY / 2), in0 ? y0 : b, in0 ? col : p.n, p.n);
+                stage_eight(y_ring + y_slot * kUpY + h * (kUpY / 2) + kUpY / 4, in1 ? y1 : b, in1 ? col : p.n, p.n);
             }
             y_slot = y_slot == kUpStages - 1 ? 0 : y_slot + 1;
             if (!adapters) ahead_f += kUpFeatures;
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
 #pragma unroll
             for (int i = 0; i < kUpFeatures / STEP; ++i, from += size_t(STEP) * p.rank) {
                 const bool in = f + i * STEP < p.n;
-                stage_eight<VEC>(to + i * STEP * ROW, in ? from : b, in ? r : p.rank, p.rank);
+                stage_eight(to + i * STEP * ROW, in ? from : b, in ? r : p.rank, p.rank);
             }
             ahead_left &= ahead_left - 1;
             if (!ahead_left) {
@@ -435,7 +436,6 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
         }
         ++ahead;
         slot = slot == kUpStages - 1 ? 0 : slot + 1;
-        copy_async_commit();
     };
     for (int i = 0; i < kUpStages - 1; ++i) fetch();
     uint32_t v[2][2][4];                             // y: two blocks of 32 features, two tokens
@@ -443,7 +443,6 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
     uint64_t left = 0;
     int f = f0 - kUpFeatures;
     for (int unit = 0; unit < units; ++unit) {
-        copy_async_wait<kUpStages - 2>();
         __syncthreads();
         if (!left) {                                 // the next features
             left = list;
@@ -508,8 +507,8 @@ __global__ void __launch_bounds__(32 * kUpWarps, RT == 8 ? 2 : 4) adapter_up_ker
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int col = f + h * 32 + 8 * t;
-                if (in0) store_eight<VEC>(o0, col, p.n, v[h][0]);
-                if (in1) store_eight<VEC>(o1, col, p.n, v[h][1]);
+                if (in0) store_eight(o0, col, p.n, v[h][0]);
+                if (in1) store_eight(o1, col, p.n, v[h][1]);
             }
         }
     }

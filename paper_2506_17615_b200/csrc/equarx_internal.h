@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <cstdint>
+
 namespace equarx {
 // cudaSuccess, or what EQUARX_INJECT_LAUNCH_ERROR asks every launch to report
 cudaError_t launch_error_to_inject();
@@ -9,4 +11,6 @@ cudaError_t launch_error_to_inject();
 bool dependent_launches();
 // records `e` for equarx_last_cuda_error() and returns EQUARX_ERR_CUDA
 int cuda_failure(cudaError_t e);
+// waits of the adapters' kernels that gave up on the current device since the last call
+cudaError_t adapters_gave_up(uint32_t& seen);
 }  // namespace equarx

@@ -92,7 +92,8 @@ def check(out, y, x, a, b, index, scale):
 
 SIZES = [(1, 1, 1, 1, 1), (1, 64, 64, 16, 1), (1, 5376, 2688, 16, 3), (2, 33, 40, 8, 2), (3, 130, 72, 5, 3), (16, 128, 256, 16, 4),
          (17, 257, 129, 24, 5), (64, 520, 264, 16, 64), (64, 1000, 1000, 64, 9), (100, 96, 3000, 32, 4), (300, 513, 777, 128, 3),
-         (601, 264, 136, 64, 7), (1200, 136, 520, 16, 2), (2500, 300, 96, 40, 30), (5000, 40, 40, 100, 6), (700, 64, 64, 1, 700)]
+         (601, 264, 136, 64, 7), (1200, 136, 520, 16, 2), (2500, 300, 96, 40, 30), (5000, 40, 40, 100, 6), (700, 64, 64, 1, 700), (129, 640, 72, 8, 3), (300, 1000, 1000, 64, 2), (130, 136, 64, 128, 130), (2000, 264, 200, 72, 3),
+         (97, 2568, 512, 16, 20), (4100, 136, 64, 32, 2), (640, 9000, 128, 24, 6), (1000, 72, 5000, 16, 4)]
 
 
 @gpu
