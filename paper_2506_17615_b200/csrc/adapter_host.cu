@@ -50,8 +50,8 @@ int launch_tiles(AdapterArgs& a, int sms, cudaStream_t stream) {
     a.ctas = int(share(tiles, ceil_div(a.k, 64), 6, sms * (RT == 8 ? 1 : 2), 8, true));
     a.blocks = int(ceil_div(blocks, share(tiles, blocks, 3, sms, ceil_div(2 * sms, tiles), false)));
     m.p = a;
-    TRY(launch(adapter_down_tiles<DT, RT>, dim3(unsigned(tiles * a.ctas)), kAdapterTileThreads, kDownTileSmem<RT>, unsigned(a.ctas), m, stream, true));
-    return launch(adapter_up_tiles<DT, RT>, dim3(unsigned(tiles), unsigned(ceil_div(blocks, a.blocks))), kAdapterTileThreads, kUpTileSmem<RT>, 1,
+    TRY(launch(adapter_down_tiles<DT, RT>, dim3(unsigned(tiles * a.ctas)), kDownThreads, kDownTileSmem<RT>, unsigned(a.ctas), m, stream, true));
+    return launch(adapter_up_tiles<DT, RT>, dim3(unsigned(tiles), unsigned(ceil_div(blocks, a.blocks))), kUpThreads, kUpTileSmem<RT>, 1,
                   m, stream, true);
 }
 

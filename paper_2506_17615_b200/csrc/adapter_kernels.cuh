@@ -61,7 +61,7 @@ __device__ __forceinline__ float dot_eight(const uint32_t* a, const float2* b, f
 // of B, 16 ranks each: all reads are of neighbouring bytes.  Everything is summed in fp32.  Bound by the chain of start,
 // index, loads, exchange and store.
 template <int DT, int RT, bool VEC>
-__global__ void __launch_bounds__(kAdapterThreads) adapter_token_kernel(const __grid_constant__ AdapterArgs p) {
+__global__ void __launch_bounds__(kAdapterThreads, RT < 4 ? 3 : 2) adapter_token_kernel(const __grid_constant__ AdapterArgs p) {
     constexpr int ROWS = 2 * RT;                     // of A, for each warp
     constexpr int AHEAD = 4;                         // parts of B's rows, for each thread
     __shared__ __align__(16) float mine[16 * RT], total[16 * RT];
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kAdapterThreads) adapter_token_kernel(const __
 
     const int chunks = (p.k + 7) / 8, c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
     float acc[ROWS] = {};
-#pragma unroll 2
+#pragma unroll(RT < 4 ? 2 : 1)
     for (int c = c0 + lane; c < c1; c += 32) {
         uint32_t v[4];
         float2 f[4];
@@ -179,6 +179,19 @@ __device__ __forceinline__ uint32_t first_of_each(int d) {
 // S is rounded as the tensor cores want it, to two numbers of the 16-bit type, high and low, whose sum has 16 bits (bf16) or
 // 22: 2^-17 of S.  In fp16 a token's S is scaled by a power of two first, so that its range does not matter.
 
+// fp16: what a token's S is multiplied by, so that its largest finite magnitude goes to [2^14, 2^15), and what by afterwards
+__device__ __forceinline__ void range_of(float top, float& times, float& back) {
+    const int e = top > 0.0f ? min(max(int(__float_as_uint(top) >> 23) - 127 - 14, -100), 100) : 0;
+    times = __uint_as_float(uint32_t(127 - e) << 23);
+    back = __uint_as_float(uint32_t(127 + e) << 23);
+}
+// two values as high and low halves; nothing is left of what is not finite
+template <int DT>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t& high, uint32_t& low) {
+    high = pack2(a, b, DT);
+    const float2 h = unpack2(high, DT);
+    low = pack2(fabsf(a) < __uint_as_float(kInfBits) ? a - h.x : 0.0f, fabsf(b) < __uint_as_float(kInfBits) ? b - h.y : 0.0f, DT);
+}
 // A token's S, a warp's lanes 32 ranks apart: scaled, split and stored
 template <int DT, int R>
 __device__ __forceinline__ void store_sums(const AdapterArgs& p, int token, int adapter, float (&v)[(R + 31) / 32]) {
@@ -193,23 +206,20 @@ __device__ __forceinline__ void store_sums(const AdapterArgs& p, int token, int 
     }
     float times = 1.0f;
     if constexpr (DT == kFp16) {
-        // the largest finite one goes to [2^14, 2^15)
         top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));
-        const int e = top > 0.0f ? min(max(int(__float_as_uint(top) >> 23) - 127 - 14, -100), 100) : 0;
-        times = __uint_as_float(uint32_t(127 - e) << 23);
-        if (lane == 0) p.back[token] = __uint_as_float(uint32_t(127 + e) << 23);
+        float back;
+        range_of(top, times, back);
+        if (lane == 0) p.back[token] = back;
     }
     uint16_t* const to = p.s + size_t(token) * (2 * R);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const int r = lane + 32 * j;
         if (r >= R) continue;
-        const float s = v[j] * times;
-        const uint32_t high = pack2(s, 0.0f, DT);
-        const float rest = s - unpack2(high, DT).x;
+        uint32_t high, low;
+        split_pair<DT>(v[j] * times, 0.0f, high, low);
         to[r] = uint16_t(high);
-        // nothing is left of what is not finite
-        to[R + r] = fabsf(s) < __uint_as_float(kInfBits) ? uint16_t(pack2(rest, 0.0f, DT)) : uint16_t(0);
+        to[R + r] = uint16_t(low);
     }
 }
 

@@ -15,7 +15,7 @@ struct AdapterMaps {
     CUtensorMap x, a, high, low, b, y, out;     // boxes of 64 columns; of 128 rows, a: of 16 RT, out: of 32
     AdapterArgs p;
 };
-constexpr int kTileTokens = 128, kAdapterTileThreads = 192, kTileOutWarps = 4;
+constexpr int kTileTokens = 128, kDownWarps = 4, kDownThreads = 32 * (kDownWarps + 2);
 constexpr int kBoxBytes = kTileTokens * 128;    // 128 rows x 64 columns of 16 bits
 constexpr int kTileSlack = 1024;                // swizzled tiles start on multiples of 1024 bytes
 
@@ -26,8 +26,14 @@ struct TileAdapters {
     // by all threads; returns how many there are
     __device__ __forceinline__ int find(const AdapterArgs& p, int first) {
         const int t = threadIdx.x;
-        if (t < kTileTokens) own[t] = first + t < p.tokens ? adapter_of(p, first + t) : -1;
-        __syncthreads();
+        int d = 0;
+        if (t < kTileTokens) own[t] = d = first + t < p.tokens ? adapter_of(p, first + t) : -1;
+        const int one = first < p.tokens ? adapter_of(p, first) : -1;
+        if (__syncthreads_and(t >= kTileTokens || d == one)) {             // one request's tokens
+            if (t == 0) list[0] = one;
+            __syncthreads();
+            return one >= 0;
+        }
         bool lead = false;
         if (t < kTileTokens) {
             bool again = own[t] < 0;
@@ -61,7 +67,7 @@ template <int RT> constexpr int kDownTileSmem = kDownPipe<RT> * kDownTileStage<R
 static_assert(kDownTileSmem<8> + 4096 <= 227 * 1024 && 2 * (kDownTileSmem<4> + 4096) <= 227 * 1024);
 
 template <int DT, int RT>
-__global__ void __launch_bounds__(kAdapterTileThreads, RT == 8 ? 1 : 2) adapter_down_tiles(const __grid_constant__ AdapterMaps m) {
+__global__ void __launch_bounds__(kDownThreads, RT == 8 ? 1 : 2) adapter_down_tiles(const __grid_constant__ AdapterMaps m) {
     constexpr int R = 16 * RT, PIPE = kDownPipe<RT>, STAGE = kDownTileStage<RT>, PITCH = kDownPitch<RT>;
     constexpr uint32_t COLS = R < 32 ? 32 : R;
     const AdapterArgs& p = m.p;
@@ -81,7 +87,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, RT == 8 ? 1 : 2) adapter_
             barrier_init(empty + 8 * i, 1);
         }
         barrier_init(ready, 1);
-        barrier_init(drained, kTileOutWarps);
+        barrier_init(drained, kDownWarps);
         barrier_init(drain, 1);
         abort = 0;
         fence_barrier_init();
@@ -90,7 +96,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, RT == 8 ? 1 : 2) adapter_
     grid_wait();
     const int adapters = uniform(tile.find(p, first));
     // only now: no launch before this one can still want tensor memory
-    if (warp == 5) {
+    if (warp == kDownWarps + 1) {
         tmem_alloc<1>(smem_addr(&tmem_slot), COLS);
         fence_before();
     }
@@ -100,7 +106,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, RT == 8 ? 1 : 2) adapter_
     // every CTA has chunks: a cluster has no more CTAs than there are
     const int chunks = (p.k + 63) / 64, c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
 
-    if (warp == 4) {
+    if (warp == kDownWarps) {
         bool ok = true;
         int it = 0;
         for (int i = 0; i < adapters && ok; ++i) {
@@ -119,7 +125,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, RT == 8 ? 1 : 2) adapter_
         if (gave_up_warp(&abort))
             for (int i = max(it - PIPE, 0); i < it; ++i) barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
         __syncwarp();
-    } else if (warp == 5) {
+    } else if (warp == kDownWarps + 1) {
         bool ok = true;
         int it = 0;
         for (int i = 0; i < adapters && ok; ++i) {
@@ -171,28 +177,53 @@ __global__ void __launch_bounds__(kAdapterTileThreads, RT == 8 ? 1 : 2) adapter_
     }
     fence_before();
     __syncthreads();
-    if (warp == 5) {
+    if (warp == kDownWarps + 1) {
         fence_after();
         tmem_free<1>(tmem, COLS);
     }
     __syncwarp();
     cluster_sync();
-    // the cluster's sums of every ctas-th token, scaled and split
-    for (int token = rank + warp * p.ctas; token < count; token += kAdapterTileThreads / 32 * p.ctas) {
-        const int i = tile.own[token];
-        if (i < 0) continue;
-        constexpr int PER = (R + 31) / 32;
-        float v[PER];
+    // The cluster's sums of every ctas-th token, scaled, split and stored.  A lane has four ranks; all CTAs' parts are asked for
+    // before the first is added.
+    constexpr int LANES = R / 4, AT_ONCE = 32 / LANES;
+    for (int base = warp * AT_ONCE; base * p.ctas < kTileTokens; base += kDownThreads / 32 * AT_ONCE) {
+        const int token = (base + lane / LANES) * p.ctas + rank, r = lane % LANES * 4;
+        const int i = token < count ? tile.own[token] : -1;
+        float4 part[8];
+        const uint32_t from = smem_addr(sums + min(token, kTileTokens - 1) * PITCH + r);
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int r = lane + 32 * j;
-            v[j] = 0.0f;
-            if (r < p.rank) {              // past the adapter's own ranks lie the next one's
-                const uint32_t from = smem_addr(sums + token * PITCH + r);
-                for (int q = 0; q < p.ctas; ++q) v[j] += ld_cluster_f32(peer_addr(from, q));
+        for (int q = 0; q < 8; ++q)
+            if (q < p.ctas) part[q] = ld_cluster_f32x4(peer_addr(from, q));
+        float v[4] = {};
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < p.ctas) {
+                v[0] += part[q].x; v[1] += part[q].y; v[2] += part[q].z; v[3] += part[q].w;
             }
+        const float c = p.scale && i >= 0 ? p.scale[i] : 1.0f;
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = i >= 0 && r + j < p.rank ? v[j] * c : 0.0f;     // past the adapter's own ranks lie the next one's
+            if (fabsf(v[j]) < __uint_as_float(kInfBits)) top = fmaxf(top, fabsf(v[j]));
         }
-        store_sums<DT, R>(p, first + token, i, v);
+        float times = 1.0f;
+        if constexpr (DT == kFp16) {
+#pragma unroll
+            for (int s = LANES / 2; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+            float back;
+            range_of(top, times, back);
+            if (i >= 0 && r == 0) p.back[first + token] = back;
+        }
+        if (i < 0) continue;
+        uint32_t high[2], low[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            split_pair<DT>(v[2 * j] * times, v[2 * j + 1] * times, high[j], low[j]);
+        }
+        uint16_t* const to = p.s + size_t(first + token) * (2 * R) + r;
+        *reinterpret_cast<uint2*>(to) = make_uint2(high[0], high[1]);
+        *reinterpret_cast<uint2*>(to + R) = make_uint2(low[0], low[1]);
     }
     __syncwarp();
     cluster_sync();                        // the others' sums have been read
@@ -203,13 +234,14 @@ __global__ void __launch_bounds__(kAdapterTileThreads, RT == 8 ? 1 : 2) adapter_
 // there.  High and low halves of S are two products with the same rows of B, added up in tensor memory, where two accumulators let the
 // next products run meanwhile.
 constexpr int kUpBlock = 128, kUpOut = 2 * kBoxBytes;                            // features; bytes of y
+constexpr int kUpOutWarps = 8, kUpThreads = 32 * (kUpOutWarps + 2);              // 32 tokens x 64 features each
 template <int RT> constexpr int kRankBoxes = RT == 8 ? 2 : 1;                    // of 64 ranks
 template <int RT> constexpr int kUpRing = RT == 8 ? 2 : 3;
 template <int RT> constexpr int kUpTileSmem = 2 * kRankBoxes<RT> * kBoxBytes + kUpRing<RT> * (kRankBoxes<RT> * kBoxBytes + kUpOut) + kTileSlack;
 static_assert(kUpTileSmem<4> + 4096 <= 227 * 1024 && kUpTileSmem<8> + 4096 <= 227 * 1024);
 
 template <int DT, int RT>
-__global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const __grid_constant__ AdapterMaps m) {
+__global__ void __launch_bounds__(kUpThreads, 1) adapter_up_tiles(const __grid_constant__ AdapterMaps m) {
     constexpr int BOXES = kRankBoxes<RT>, RING = kUpRing<RT>, B_BYTES = BOXES * kBoxBytes;
     const AdapterArgs& p = m.p;
     extern __shared__ uint8_t smem_raw[];
@@ -229,12 +261,12 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
             barrier_init(b_full + 8 * i, 1);
             barrier_init(b_empty + 8 * i, 1);
             barrier_init(y_full + 8 * i, 1);
-            barrier_init(y_empty + 8 * i, kTileOutWarps);
+            barrier_init(y_empty + 8 * i, kUpOutWarps);
         }
         barrier_init(s_full, 1);
         for (int i = 0; i < 2; ++i) {
             barrier_init(ready + 8 * i, 1);
-            barrier_init(drained + 8 * i, kTileOutWarps);
+            barrier_init(drained + 8 * i, kUpOutWarps);
         }
         barrier_init(drain, 1);
         abort = 0;
@@ -243,7 +275,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
     grid_launch();
     grid_wait();
     const int adapters = uniform(tile.find(p, first));
-    if (warp == 5) {
+    if (warp == kUpOutWarps + 1) {
         tmem_alloc<1>(smem_addr(&tmem_slot), 2 * kUpBlock);
         fence_before();
     }
@@ -251,7 +283,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
     fence_after();
     const uint32_t tmem = uniform(tmem_slot);
 
-    if (warp == 4) {
+    if (warp == kUpOutWarps) {
         bool ok = true;
         int unit = 0, block = 0;
         if (adapters) {
@@ -282,7 +314,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
             for (int i = max(block - RING, 0); i < block; ++i) barrier_drain(y_full + 8 * (i % RING), i / RING & 1);
         }
         __syncwarp();
-    } else if (warp == 5) {
+    } else if (warp == kUpOutWarps + 1) {
         const int units = blocks * adapters;
         bool ok = units == 0 || barrier_wait_warp(s_full, 0, &abort);
         for (int unit = 0; unit < units && ok; ++unit) {
@@ -308,13 +340,13 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
         }
         __syncwarp();
     } else {
-        const int row = warp * 32 + lane, mine = tile.own[row];
+        const int rows = warp % 4 * 32, row = rows + lane, half = warp / 4, mine = tile.own[row];
         const float back = DT == kFp16 && mine >= 0 ? __ldcg(p.back + first + row) : 1.0f;
         bool ok = true;
         int unit = 0;
         for (int block = 0; block < blocks && ok; ++block) {
             const int slot = block % RING, f = f0 + block * kUpBlock;
-            const uint32_t y = y_at + slot * kUpOut + row * 128;
+            const uint32_t y = y_at + slot * kUpOut + half * kBoxBytes + row * 128;
             if (!(ok = barrier_wait_warp(y_full + 8 * slot, block / RING & 1, &abort))) break;
             for (int i = 0; i < adapters; ++i, ++unit) {
                 const int buf = unit & 1;
@@ -323,15 +355,15 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
                 const bool take = tile.list[i] == mine;
                 if (__any_sync(0xFFFFFFFFu, take)) {
 #pragma unroll
-                    for (int c = 0; c < kUpBlock; c += 32) {
+                    for (int c = 0; c < 64; c += 32) {
                         uint32_t v[32];
                         __syncwarp();
-                        tmem_load32(tmem + buf * kUpBlock + (uint32_t(warp * 32) << 16) + c, v);
+                        tmem_load32(tmem + buf * kUpBlock + half * 64 + (uint32_t(rows) << 16) + c, v);
                         tmem_wait_loads();
                         if (!take) continue;
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {      // pieces of 8 columns
-                            const uint32_t at = y + c / 64 * kBoxBytes + (((c % 64 / 8 + q) ^ (row & 7)) << 4);
+                            const uint32_t at = y + (((c / 8 + q) ^ (row & 7)) << 4);
                             uint32_t w[4];
                             ld_shared_v4(at, w);
 #pragma unroll
@@ -353,11 +385,9 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
             fence_async_shared();
             __syncwarp();
             if (lane == 0) {
-                const uint32_t from = y_at + slot * kUpOut + warp * 32 * 128;
-                if (first + warp * 32 < p.tokens)
-                    for (int h = 0; h < 2 && f + h * 64 < p.n; ++h) tma_store_2d(&m.out, from + h * kBoxBytes, f + h * 64, first + warp * 32);
-                // the block before this one has left (only the last block may have one store instead of two)
-                tma_store_wait_read<2>();
+                if (first + rows < p.tokens && f + half * 64 < p.n)
+                    tma_store_2d(&m.out, y_at + slot * kUpOut + half * kBoxBytes + rows * 128, f + half * 64, first + rows);
+                tma_store_wait_read<1>();                  // the block before this one has left
                 if (block) barrier_arrive(y_empty + 8 * ((block - 1) % RING));
             }
             __syncwarp();
@@ -367,7 +397,7 @@ __global__ void __launch_bounds__(kAdapterTileThreads, 1) adapter_up_tiles(const
     }
     fence_before();
     __syncthreads();
-    if (warp == 5) {
+    if (warp == kUpOutWarps + 1) {
         fence_after();
         tmem_free<1>(tmem, 2 * kUpBlock);
     }
