@@ -650,7 +650,7 @@ int equarx_add_rms_norm_backward(const void *dy, size_t lddy, const void *dsum, 
  * parallelism with k split over the ranks, a rank passes its columns of A, and the AllReduce
  * of the outputs adds the adapters' parts too.  For a few tokens the workspace is 0 bytes.
  */
-size_t equarx_add_adapters_workspace_bytes(size_t tokens, size_t rank);
+size_t equarx_add_adapters_workspace_bytes(size_t tokens, size_t n, size_t k, size_t rank, size_t adapters);
 int equarx_add_adapters(const void *y, size_t ldy, const void *x, size_t ldx,
                         const void *a, const void *b, const int32_t *index, const float *scale,
                         int dtype, size_t tokens, size_t n, size_t k, size_t rank, size_t adapters,

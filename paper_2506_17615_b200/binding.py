@@ -127,7 +127,7 @@ def _load():
     lib.equarx_add_rms_norm_fp8.argtypes = [vp, sz, vp, sz, vp, ci, ci, sz, sz, cd, cf, vp, sz, vp, vp, vp]
     lib.equarx_add_rms_norm_backward_workspace_bytes.argtypes = [sz, sz]
     lib.equarx_add_rms_norm_backward.argtypes = [vp, sz, vp, sz, vp, sz, vp, vp, ci, ci, sz, sz, cf, vp, sz, vp, vp, sz, vp]
-    lib.equarx_add_adapters_workspace_bytes.argtypes = [sz, sz]
+    lib.equarx_add_adapters_workspace_bytes.argtypes = [sz] * 5
     lib.equarx_add_adapters.argtypes = [vp, sz, vp, sz, vp, vp, vp, vp, ci, sz, sz, sz, sz, sz, vp, sz, vp, sz, vp]
     for name in ("fp8_codes_bytes", "fp8_scales_bytes", "add_rms_norm_backward_workspace_bytes", "add_adapters_workspace_bytes"):
         getattr(lib, "equarx_" + name).restype = sz
@@ -407,8 +407,8 @@ def add_rms_norm_backward(dy, lddy, dsum, ldds, sum, lds, factors, weight, dtype
            "equarx_add_rms_norm_backward")
 
 
-def add_adapters_workspace_bytes(tokens, rank):
-    return lib.equarx_add_adapters_workspace_bytes(tokens, rank)
+def add_adapters_workspace_bytes(tokens, n, k, rank, adapters):
+    return lib.equarx_add_adapters_workspace_bytes(tokens, n, k, rank, adapters)
 
 
 def add_adapters(y, ldy, x, ldx, a, b, index, scale, dtype, tokens, n, k, rank, adapters, out, ldo, workspace, workspace_bytes, stream=0):

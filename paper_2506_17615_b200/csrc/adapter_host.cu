@@ -10,14 +10,33 @@ using namespace equarx::host;
 
 constexpr size_t kMaxRank = 128;
 
-// Tokens up to which each has a cluster of its own.
-constexpr size_t kTokenForm = 96;
-
 inline size_t padded_rank(size_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+
+// Whether each token gets a cluster of its own, which reads the token's adapter again for each token, or tiles of tokens are
+// multiplied with each adapter that they have.  Only the device knows how many that are.  us, 2688 -> 5376, few requests one after the
+// other / 16 mixed / a request for each token:
+//                     rank 16: tokens           tiles                rank 64: tokens           tiles
+//     64 tokens       7 / 7 / 8                 11 / 32 / 115        12 / 14 / 18              12 / 38 / 169
+//     128             10 / 10 / 14              11 / 32 / 287        20 / 23 / 29              11 / 41 / 326
+//     256             14 / 15 / 21              12 / 33 / 289        34 / 38 / 50              12 / 45 / 327
+//     512             15 / 26 / 40              11 / 44 / 356        34 / 74 / 97              12 / 55 / 407
+// So up to 80 MB of adapters read tokens have their own.  Up to eight times as many they have it where there are adapters for every
+// second token at least: with that many loaded, tokens are likely those of many requests, a batch of single tokens.
+inline bool token_form(size_t tokens, size_t n, size_t k, size_t rank, size_t adapters) {
+    const double bytes = 2.0 * double(tokens) * double(rank) * double(n + k);
+    return bytes <= 80e6 || (tokens <= 2 * adapters && bytes <= 640e6);
+}
+// CTAs of a token's cluster: with them all, two for each SM at most, and 32 KB of adapter at least for each
+inline int token_ctas(size_t tokens, size_t n, size_t k, size_t rank, size_t sms) {
+    int c = 1;
+    while (c < 8 && tokens * c * 2 <= 2 * sms && rank * (n + k) * 2 >= size_t(c) * 2 * 32768 * 7 / 8) c *= 2;
+    return c;
+}
+
 // a token's S, high and low
 inline size_t sums_bytes(size_t tokens, size_t rank) { return up(tokens * padded_rank(rank) * 4, 256); }
-inline size_t adapter_workspace(size_t tokens, size_t rank) {
-    return tokens <= kTokenForm ? 0 : sums_bytes(tokens, rank) + up(tokens * sizeof(float), 256);
+inline size_t adapter_workspace(size_t tokens, size_t n, size_t k, size_t rank, size_t adapters) {
+    return token_form(tokens, n, k, rank, adapters) ? 0 : sums_bytes(tokens, rank) + up(tokens * sizeof(float), 256);
 }
 
 // Whole waves of CTAs, each with its share of `work` steps and what starting costs, `start` steps: the number of CTAs for each tile
@@ -57,8 +76,8 @@ int launch_tiles(AdapterArgs& a, int sms, cudaStream_t stream) {
 
 template <int DT, int RT>
 int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
-    if (size_t(a.tokens) <= kTokenForm) {
-        a.ctas = a.tokens * 8 <= 2 * sms ? 8 : 4;
+    if (token_form(a.tokens, a.n, a.k, a.rank, a.adapters)) {
+        a.ctas = token_ctas(a.tokens, a.n, a.k, a.rank, sms);
         return launch(vec ? adapter_token_kernel<DT, RT, true> : adapter_token_kernel<DT, RT, false>, dim3(unsigned(a.tokens) * a.ctas),
                       kAdapterThreads, 0, unsigned(a.ctas), a, stream);
     }
@@ -96,8 +115,9 @@ cudaError_t adapters_gave_up(uint32_t& seen) {
 
 extern "C" {
 
-size_t equarx_add_adapters_workspace_bytes(size_t tokens, size_t rank) {
-    return tokens > kMaxDim || rank == 0 || rank > kMaxRank ? 0 : adapter_workspace(tokens, rank);
+size_t equarx_add_adapters_workspace_bytes(size_t tokens, size_t n, size_t k, size_t rank, size_t adapters) {
+    if (tokens > kMaxDim || bad_dim(n) || bad_dim(k) || rank == 0 || rank > kMaxRank || adapters > kMaxDim) return 0;
+    return adapter_workspace(tokens, n, k, rank, adapters);
 }
 
 int equarx_add_adapters(const void* y, size_t ldy, const void* x, size_t ldx, const void* a, const void* b, const int32_t* index,
@@ -108,7 +128,7 @@ int equarx_add_adapters(const void* y, size_t ldy, const void* x, size_t ldx, co
         bad_ld(ldx, k) || bad_ld(ldo, n))
         return EQUARX_ERR_COUNT;
     if (tokens == 0) return EQUARX_OK;
-    const size_t need = adapter_workspace(tokens, rank);
+    const size_t need = adapter_workspace(tokens, n, k, rank, adapters);
     if (!y || !x || !index || !out || (adapters && (!a || !b)) || (need && !workspace)) return EQUARX_ERR_NULL;
     if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
     for (const void* p : {y, x, a, b, static_cast<const void*>(out)})

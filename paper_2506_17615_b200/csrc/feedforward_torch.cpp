@@ -595,7 +595,7 @@ PyObject* add_adapters(PyObject*, PyObject* const* args, Py_ssize_t count) {
     const at::Tensor out = args[6] == Py_None ? empty(m, n, y.t.scalar_type(), device) : tensor(args[6], "out");
     const Matrix o = matrix(out, "out", m, n, y.t);
     no_gradient(out, "out", calls);
-    const size_t need = entry.add_adapters_workspace_bytes(m, rank);
+    const size_t need = entry.add_adapters_workspace_bytes(m, n, k, rank, adapters);
     const at::Tensor ws = bytes(need, device);
     const int status = call(device, [&](equarx_stream_t s) {
         return entry.add_adapters(y.p, y.ld, x.p, x.ld, ta.data_ptr(), tb.data_ptr(), static_cast<const int32_t*>(index.p), scale, dtype, m,

@@ -39,10 +39,10 @@ def test_refuses_bad_arguments():
     assert status_of(f, **{**a, "out": A, "ldo": 72}) == binding.ERR_ALIAS
     assert status_of(f, **{**a, "tokens": 0, "y": 0}) == 0
     # many tokens go through a workspace
-    assert eq.add_adapters_workspace_bytes(4, 8) == 0 and eq.add_adapters_workspace_bytes(1000, 0) == 0
-    need = eq.add_adapters_workspace_bytes(1000, 17)
-    assert need >= 1000 * 32 * 4
-    many = {**a, "tokens": 1000, "rank": 17, "workspace": A + 7 * GB, "workspace_bytes": need}
+    assert eq.add_adapters_workspace_bytes(4, 64, 32, 8, 3) == 0 and eq.add_adapters_workspace_bytes(10 ** 6, 64, 32, 0, 3) == 0
+    need = eq.add_adapters_workspace_bytes(10 ** 5, 64, 32, 17, 3)
+    assert need >= 10 ** 5 * 32 * 4
+    many = {**a, "tokens": 10 ** 5, "rank": 17, "workspace": A + 7 * GB, "workspace_bytes": need}
     assert status_of(f, **{**many, "workspace": 0}) == binding.ERR_NULL
     assert status_of(f, **{**many, "workspace_bytes": need - 1}) == binding.ERR_WORKSPACE
     assert status_of(f, **{**many, "workspace": A + 7 * GB + 8}) == binding.ERR_ALIGN
@@ -90,10 +90,14 @@ def check(out, y, x, a, b, index, scale):
     assert torch.equal(out[bare], y[bare])
 
 
+# a cluster for each token
 SIZES = [(1, 1, 1, 1, 1), (1, 64, 64, 16, 1), (1, 5376, 2688, 16, 3), (2, 33, 40, 8, 2), (3, 130, 72, 5, 3), (16, 128, 256, 16, 4),
          (17, 257, 129, 24, 5), (64, 520, 264, 16, 64), (64, 1000, 1000, 64, 9), (100, 96, 3000, 32, 4), (300, 513, 777, 128, 3),
-         (601, 264, 136, 64, 7), (1200, 136, 520, 16, 2), (2500, 300, 96, 40, 30), (5000, 40, 40, 100, 6), (700, 64, 64, 1, 700), (129, 640, 72, 8, 3), (300, 1000, 1000, 64, 2), (130, 136, 64, 128, 130), (2000, 264, 200, 72, 3),
-         (97, 2568, 512, 16, 20), (4100, 136, 64, 32, 2), (640, 9000, 128, 24, 6), (1000, 72, 5000, 16, 4)]
+         (601, 264, 136, 64, 7), (700, 64, 64, 1, 700), (40, 2001, 700, 100, 40), (9, 520, 3000, 128, 2)]
+# tiles of tokens, of rows that TMA reads and of others
+SIZES += [(1500, 5376, 520, 16, 2), (8192, 640, 72, 8, 3), (5000, 1000, 1000, 64, 2), (3000, 1360, 640, 128, 30), (2000, 2640, 1000, 72, 3),
+          (2500, 1001, 777, 16, 4), (4100, 600, 201, 40, 5), (1300, 1032, 777, 100, 3), (1030, 3000, 1000, 32, 300), (2049, 2568, 512, 24, 20),
+          (70000, 72, 136, 5, 6), (1111, 2500, 2600, 31, 2), (900, 9000, 128, 16, 3)]
 
 
 @gpu
@@ -113,9 +117,11 @@ def test_matches_the_definition(dtype, tokens, n, k, rank, count):
 
 @gpu
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("tokens", [1, 20, 400])
+@pytest.mark.parametrize("tokens", [1, 20, 400, 2001])
 def test_not_finite_values_stay_with_their_adapter(dtype, tokens):
-    y, x, a, b, scale = inputs(tokens, 136, 72, 16, 4, 1, dtype)
+    k = 72 if tokens < 1000 else 2600                               # tiles of tokens
+    y, x, a, b, scale = inputs(tokens, 136, k, 16, 4, 1, dtype)
+    assert (eq.add_adapters_workspace_bytes(tokens, 136, k, 16, 4) > 0) == (tokens > 1000)
     index = (torch.arange(tokens) % 4).int().cuda()
     clean = ad.add_adapters(y, x, a, b, index, scale)
     for bad in (float("nan"), float("inf")):
@@ -142,12 +148,13 @@ def test_not_finite_values_stay_with_their_adapter(dtype, tokens):
 
 @gpu
 @pytest.mark.parametrize("large", [True, False])
-def test_products_beyond_the_range_of_fp16(large):
+@pytest.mark.parametrize("tokens,n", [(40, 64), (12000, 200), (12000, 201)])
+def test_products_beyond_the_range_of_fp16(large, tokens, n):
     """x A^T above 65504 or among fp16's subnormal numbers, with outputs inside its range"""
-    y, x, a, b, _ = inputs(40, 64, 96, 16, 3, 1, torch.float16)
+    y, x, a, b, _ = inputs(tokens, n, 96, 16, 3, 1, torch.float16)
     a, b = (a * 2000, b * 2.0 ** -12) if large else (a * 2.0 ** -9, b * 2.0 ** 3)
     x = x * 200 if large else x * 2.0 ** -10
-    index = (torch.arange(40) % 4 - 1).int().cuda()
+    index = (torch.arange(tokens) % 4 - 1).int().cuda()
     s = x.double() @ a.double()[0].T
     assert float(s.abs().max()) > 70000 if large else float(s.abs().max()) < 2.0 ** -15
     out = ad.add_adapters(y * 0, x, a, b, index)
@@ -156,13 +163,20 @@ def test_products_beyond_the_range_of_fp16(large):
 
 @gpu
 @pytest.mark.parametrize("offset", [1, 2, 4, 8])
-@pytest.mark.parametrize("tokens", [3, 150])
+@pytest.mark.parametrize("tokens", [3, 150, 50001])
 def test_views_that_start_anywhere(tokens, offset):
-    """through the C ABI; the rest of the output's buffer keeps its canary"""
+    """through the C ABI; the rest of the output's buffer keeps its canary.  A cluster for each token gives the bits of aligned
+    rows; tiles of rows that TMA cannot read add in another order, which the bound of all results allows"""
     dtype, stream, n, k, rank = torch.bfloat16, torch.cuda.current_stream().cuda_stream, 72, 40, 8
     y, x, a, b, scale = inputs(tokens, n, k, rank, 3, 1, dtype)
     index = patterns(tokens, 3, 2)[1]
     want = ad.add_adapters(y, x, a, b, index, scale)
+
+    def assert_same(out):
+        if tokens < 1000:
+            assert torch.equal(out, want)
+        else:
+            check(out, y, x, a, b, index, scale)
 
     def place(t, ld):
         store = torch.full((offset + t.shape[0] * ld + 16,), -77.0, device="cuda", dtype=dtype)
@@ -170,16 +184,16 @@ def test_views_that_start_anywhere(tokens, offset):
         return store, view.copy_(t)
 
     flat = lambda t: torch.empty(t.numel() + offset, device="cuda", dtype=dtype)[offset:].copy_(t.reshape(-1))
-    nb = eq.add_adapters_workspace_bytes(tokens, rank)
+    nb = eq.add_adapters_workspace_bytes(tokens, n, k, rank, 3)
     ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
     for extra in (0, 1, 8):
         (_, vy), (_, vx), (so, vo) = place(y, n + extra), place(x, k + extra), place(y * 0, n + extra)
         eq.add_adapters(vy, n + extra, vx, k + extra, flat(a), flat(b), index, scale, eq.BF16, tokens, n, k, rank, 3, vo, n + extra, ws, nb, stream)
-        assert torch.equal(vo, want)
+        assert_same(vo)
         vo.fill_(-77.0)
         assert bool((so == -77.0).all())
         eq.add_adapters(vy, n + extra, vx, k + extra, a, b, index, scale, eq.BF16, tokens, n, k, rank, 3, vy, n + extra, ws, nb, stream)
-        assert torch.equal(vy, want)
+        assert_same(vy)
 
 
 @gpu
@@ -204,6 +218,13 @@ def test_offsets_beyond_32_bits():
     yy = normal(3, 8, 8, dtype)
     at = lambda i: torch.full((3,), i, dtype=torch.int32, device="cuda")
     assert torch.equal(ad.add_adapters(yy, xx, big, bb, at(count - 1)), ad.add_adapters(yy, xx, big, bb, at(7)))
+    # the same through tiles: the adapters that follow one another end at that one
+    xx, yy = normal(3000, 4096, 5, dtype), normal(3000, 8, 8, dtype)
+    few = big[-3:]
+    index = (torch.arange(3000) % 3).int().cuda()
+    want = ad.add_adapters(yy, xx, few.contiguous(), bb[-3:].contiguous(), index)
+    assert eq.add_adapters_workspace_bytes(3000, 8, 4096, 16, 3) > 0
+    assert torch.equal(ad.add_adapters(yy, xx, few, bb[-3:], index), want)
 
 
 @gpu
@@ -220,6 +241,10 @@ def test_no_tokens_no_adapters_streams_graphs():
         got = [ad.add_adapters(y * 1, x, a, b, index, scale) for _ in range(3)]
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(t, want) for t in got)
+    many = inputs(3000, 520, 512, 32, 3, 5, dtype)                  # tiles of tokens
+    mixed = patterns(3000, 3, 6)[1]
+    tiles = ad.add_adapters(*many[:4], mixed, many[4])
+    assert torch.equal(ad.add_adapters(many[0], many[1], many[2][:0], many[3][:0], mixed), many[0])
     w = ff.fp4_quantize(normal(96, 64, 9, dtype))
     base = ff.fp4_linear(x, w)
     both = ad.add_adapters(base, x, a, b, index, scale)
@@ -227,10 +252,12 @@ def test_no_tokens_no_adapters_streams_graphs():
     with torch.cuda.graph(graph):
         out = ff.fp4_linear(x, w)
         ad.add_adapters(out, x, a, b, index, scale, out=out)
+        out2 = ad.add_adapters(*many[:4], mixed, many[4])
     for _ in range(3):
-        out.zero_()
+        out.zero_(), out2.zero_()
         graph.replay()
-        assert torch.equal(out, both)
+        assert torch.equal(out, both) and torch.equal(out2, tiles)
+    ff.check()
 
 
 @gpu
