@@ -658,8 +658,8 @@ int equarx_add_adapters(const void *y, size_t ldy, const void *x, size_t ldx,
                         equarx_stream_t stream);
 
 /*
- * The kernels of the feed-forward calls wait only for copies and products of their own
- * blocks, and each wait has a limit of about a second (more for a reduction of very
+ * The kernels of the feed-forward calls and of equarx_add_adapters wait only for copies and
+ * products of their own blocks, and each wait has a limit of about a second (more for a reduction of very
  * many columns or tokens): a kernel whose wait ran out leaves and its output is
  * incomplete.  This call synchronises the current device and returns
  * EQUARX_ERR_TIMEOUT if that has happened on it since the last check, else EQUARX_OK.

@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside a shared projection.
 //
 //   adapter_token_kernel   few tokens: a cluster each, dot products in fp32
-//   adapter_down_kernel    many tokens: S = x A^T, split into high and low halves of 16 bits
+//   adapter_down_kernel    many tokens, rows that TMA cannot read: S = x A^T, split into high and low halves of 16 bits
 //   adapter_up_kernel      and out = y + S B^T
 #pragma once
 #include "elements.cuh"
@@ -59,7 +59,8 @@ __device__ __forceinline__ float dot_eight(const uint32_t* a, const float2* b, f
 // One cluster for a token: its CTAs split k for S, whose parts they exchange through distributed shared memory, and then n.  Every
 // CTA has asked for its first rows of B before it waits for S.  A lane takes 8 columns of a row of A at a time, RT lanes share a row
 // of B, 16 ranks each: all reads are of neighbouring bytes.  Everything is summed in fp32.  Bound by the chain of start,
-// index, loads, exchange and store.
+// index, loads, exchange and store: 2688 -> 5376, rank 16, 4.3 us for one token, 7.7 for 64 with an adapter each (18 MB, 2.4 TB/s;
+// of rank 64 17.6 us, 3.9 TB/s).  Products of tiles of tokens by mma.sync in one launch took 7.4 and 12.9.
 template <int DT, int RT, bool VEC>
 __global__ void __launch_bounds__(kAdapterThreads, RT < 4 ? 3 : 2) adapter_token_kernel(const __grid_constant__ AdapterArgs p) {
     constexpr int ROWS = 2 * RT;                     // of A, for each warp
@@ -169,9 +170,9 @@ __device__ __forceinline__ uint32_t first_of_each(int d) {
     return __ballot_sync(0xFFFFFFFFu, d >= 0 && __ffs(alike) == int(threadIdx.x & 31) + 1);
 }
 
-// Reading x and y bounds both products, so they use mma.sync (the reduction axis is permuted alike for both operands, so that a
-// thread's fragments are 16 neighbouring bytes): with 16 to 128 columns, and rows of several adapters in a tile, the
-// tensor cores' work is small beside the reading.
+// The form for rows that do not start on multiples of 16 bytes, whose elements are read one by one: that bounds it, so it uses
+// mma.sync (the reduction axis is permuted alike for both operands, so that a thread's fragments are 16 neighbouring bytes).  4000
+// tokens, 1777 -> 3001, rank 64: 127 us, where rows that TMA reads take 27.
 //
 // A product runs once for each adapter that the tokens of a tile have, and only this adapter's tokens take their rows of its
 // result: what is not finite in one request's adapter does not reach another request.
@@ -230,7 +231,7 @@ __device__ __forceinline__ void stage_eight(uint32_t to, const uint16_t* row, in
     st_shared_v4(to, v[0], v[1], v[2], v[3]);
 }
 
-// S of 32 tokens, transposed: 16 ranks x 8 tokens a product.  Chunks of x and A come through a ring in shared memory.  A warp has 16
+// S of 32 tokens, transposed: 16 ranks x 8 tokens a product.  Chunks of x and A go through a ring in shared memory.  A warp has 16
 // ranks of S, the warps with the same ranks split a chunk, and the CTAs of a cluster split k where there are few tiles.  Rows
 // in shared memory are 64 bytes longer than a multiple of 128, so that two rows' 64 bytes meet no bank twice.
 constexpr int kDownTokens = 32, kDownStages = 3;
@@ -349,8 +350,8 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
     cluster_sync();                                  // the others' sums have been read
 }
 
-// out = y + S B^T for 64 tokens, 64 features at a time, whose rows of B and y come through rings in shared memory (of y a thread
-// copies and reads its own elements).  A warp keeps S of 16 tokens in registers.  Column c of the j-th of four products is
+// out = y + S B^T for 64 tokens, 64 features at a time, whose rows of B and y go through rings in shared memory (of y a thread
+// writes and reads its own elements).  A warp keeps S of 16 tokens in registers.  Column c of the j-th of four products is
 // feature 8 (c / 2) + 2 j + c % 2, so that a thread ends up with 8 neighbours.
 constexpr int kUpWarps = 4, kUpTokens = 16 * kUpWarps, kUpFeatures = 64, kUpStages = 3;
 constexpr int kUpAtOnce = 4;                     // products whose sums do not wait for one another

@@ -245,7 +245,7 @@ __device__ __forceinline__ void tile_at(const Product& p, int t, int& mt, int& n
 // cycles, bound by the power cap (1.3 - 1.6 GHz); single CTAs of 128 x 256 took 442.  4 bits, 8192 x 2688 x 5376, MX 50 us,
 // 4.7 PFLOP/s, NV 60: a tile's 11 stages do not hide the 900 cycles between its last product and the next
 // tile's first, nor NV's scale copies; longer reductions reach 5.4 and 5.1 PFLOP/s (5376), bound by the loads of a
-// stage (36 and 38 KB a CTA in 500 cycles).
+// stage (36 and 38 KB a CTA in 500 cycles).  8 bits, gated 8192 x 5376 x 2688: 164 us, 2.9 PFLOP/s, tensor cores active 90 %.
 template <int KIND, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 1)
     tile_kernel(const __grid_constant__ TileArgs<MODE> p) {
@@ -1119,7 +1119,7 @@ __global__ void __launch_bounds__(512) fp4_dequantize_kernel(const __grid_consta
 
 // ---------------------------------------------------------------- microscaled 8-bit floating point
 // One CTA a row, a thread three groups of 16 neighbouring elements at a time, loaded together; two threads are a block.
-// ANYWHERE as above.
+// ANYWHERE as above.  8192 x 5376: 22 us, 6.1 TB/s; bound by DRAM.
 template <int DT, bool ANYWHERE>
 __global__ void __launch_bounds__(512) fp8_quantize_kernel(const __grid_constant__ QuantArgs p) {
     const int tid = threadIdx.x, threads = blockDim.x;
@@ -1155,7 +1155,7 @@ __global__ void __launch_bounds__(512) fp8_quantize_kernel(const __grid_constant
 
 // value = code * scale in fp32, rounded once to the output type.  One CTA a row; a thread takes 16 neighbouring elements
 // where output rows start on multiples of 16 bytes, else (NARROW) two where they do on multiples of a pair, or one, the
-// next thread the next ones, so that a warp's stores are whole sectors anyway.
+// next thread the next ones, so that a warp's stores are whole sectors anyway.  8192 x 5376: 21 us, 6.3 TB/s.
 template <int NARROW>
 __device__ __forceinline__ void fp8_dequantize_narrow(const DequantArgs& p, size_t row, const uint8_t* codes, const uint8_t* scales) {
     for (int col = threadIdx.x * NARROW; col < p.cols; col += blockDim.x * NARROW) {

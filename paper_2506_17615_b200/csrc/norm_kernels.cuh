@@ -182,6 +182,11 @@ __device__ __forceinline__ void store_fp8(const NormArgs& p, size_t row, int fir
 //
 // One CTA a row, 8 elements a thread, kept in registers between the row's sum and its scaling: each input is read once.
 // LONG: rows of more than 8192 elements read their sum again.
+//
+// Bound by DRAM, 16 bits, and by instruction issue beside it, 8 bits (67 % of the slots).  8192 x 5376: 57 us for 352 MB, 6.2 TB/s, and 57
+// us for 310 MB, 5.4 TB/s.  Other forms of 8192 x 5376, 16 / 8 bits: 16 elements a thread 62 / 67 us; every warp with the second half of
+// the row's sum 59 / 67; CTAs that stay, with the next rows copied ahead, 60 / 77, with 24 elements a thread 67 / 64; a warp a row
+// 66 / 74, a warp a row with rows copied ahead 85 / 95 (too few warps to issue what a row needs).
 template <int DT, int W, bool EIGHT, bool LONG>
 __global__ void __launch_bounds__(kRowThreads) norm_kernel(const __grid_constant__ NormArgs p) {
     __shared__ double parts[32];
@@ -277,6 +282,10 @@ __host__ __device__ inline size_t part_stride(size_t cols) { return (cols + 7) &
 // to 8192 columns with one group each, for CTAs of two rows, whose time is mostly the fetching of instructions.  G = 0: rows that
 // this does not hold; sums in the CTA's part in memory.  Few rows: the CTAs are a cluster and add their parts of the weight's
 // gradient up through distributed shared memory, which saves a launch.
+//
+// 8192 x 5376: 68 us for 352 MB, 5.2 TB/s, and 7 us for the sum of 444 parts; bound by the wait for the row's sum and by what can be
+// copied ahead beside it (21 warps an SM, 45 % of the issue slots).  One group of 16 columns a thread without copies ahead took 260 us
+// (registers spilled), 8 columns a thread with 21 warps for a row 93, two CTAs of three groups with three rows ahead 75.
 template <int DT, int W, int G, int MOST>
 __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
     constexpr bool STAGED = W == 8 && G > 0;

@@ -10,7 +10,8 @@ weights stored as differences from 1.  A failed call raises EquarxError, tensors
 ValueError; there is no CPU path.
 
 add_rms_norm takes part in autograd.  Its 8-bit form has no gradients and refuses inputs that ask for one (outside
-torch.no_grad()); add_rms_norm_backward's results have no gradients themselves.
+torch.no_grad()); add_rms_norm_backward's results have no gradients themselves.  A backward pass that is recorded in a CUDA graph
+calls add_rms_norm_backward; autograd's own recording needs what torch asks for there (no graph of the same leaves from outside).
 """
 import torch
 
