@@ -60,7 +60,7 @@ __device__ __forceinline__ float dot_eight(const uint32_t* a, const float2* b, f
 // CTA has asked for its first rows of B before it waits for S.  A lane takes 8 columns of a row of A at a time, RT lanes share a row
 // of B, 16 ranks each: all reads are of neighbouring bytes.  Everything is summed in fp32.  Bound by the chain of start,
 // index, loads, exchange and store: 2688 -> 5376, rank 16, 4.3 us for one token, 7.7 for 64 with an adapter each (18 MB, 2.4 TB/s;
-// of rank 64 17.6 us, 3.9 TB/s).  Products of tiles of tokens by mma.sync in one launch took 7.4 and 12.9.
+// of rank 64 17.6 us, 3.8 TB/s).  Products of tiles of tokens by mma.sync in one launch took 7.4 and 12.9.
 template <int DT, int RT, bool VEC>
 __global__ void __launch_bounds__(kAdapterThreads, RT < 4 ? 3 : 2) adapter_token_kernel(const __grid_constant__ AdapterArgs p) {
     constexpr int ROWS = 2 * RT;                     // of A, for each warp

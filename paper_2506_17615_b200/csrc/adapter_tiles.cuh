@@ -62,8 +62,8 @@ struct TileAdapters {
 
 // ---------------------------------------------------------------- S = x A^T
 // 128 tokens x 16 RT ranks; the CTAs of a cluster split k and add their parts up in rank order through distributed shared memory.
-// 8192 tokens, 2688 columns, rank 64: 12 us of the 7 that reading x takes; the rest is the start (index, adapters of the tile) and the
-// exchange.
+// 8192 tokens, 2688 columns, rank 64: 19 us from a cold cache, where reading x takes 7; the rest is the start (index, adapters of the
+// tile), the wait for copies and the exchange.
 template <int RT> constexpr int kDownPipe = RT == 8 ? 4 : 3;
 template <int RT> constexpr int kDownTileStage = kBoxBytes + 16 * RT * 128;
 template <int RT> constexpr int kDownPitch = 16 * RT + 4;                        // floats of a token's sums
@@ -236,9 +236,9 @@ __global__ void __launch_bounds__(kDownThreads, RT == 8 ? 1 : 2) adapter_down_ti
 // ---------------------------------------------------------------- out = y + S B^T
 // 128 tokens, 128 features at a time.  S stays in shared memory; B and y come through rings, y is added to where it lies and leaves from
 // there.  High and low halves of S are two products with the same rows of B, added up in tensor memory, where two accumulators let the
-// next products run meanwhile.  8192 tokens, 5376 features, rank 64: 38 us for 176 MB; copying y alone through this takes 35, a plain copy
-// 28 (128 of 148 SMs have a tile's half; rows of 256 bytes far apart).  Five blocks of y under way instead of three, with a loading
-// warp of their own, changed nothing; four output warps instead of eight took 43.
+// next products run meanwhile.  8192 tokens, 5376 features, rank 64: 43 us for 176 MB from a cold cache; both launches take 57, without any
+// adapter to apply 39, and a plain copy of y 28.  Five blocks of y under way instead of three, with a loading warp of their own, changed
+// nothing.
 constexpr int kUpBlock = 128, kUpOut = 2 * kBoxBytes;                            // features; bytes of y
 constexpr int kUpOutWarps = 8, kUpThreads = 32 * (kUpOutWarps + 2);              // 32 tokens x 64 features each
 template <int RT> constexpr int kRankBoxes = RT == 8 ? 2 : 1;                    // of 64 ranks

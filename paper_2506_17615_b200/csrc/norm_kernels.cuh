@@ -183,10 +183,10 @@ __device__ __forceinline__ void store_fp8(const NormArgs& p, size_t row, int fir
 // One CTA a row, 8 elements a thread, kept in registers between the row's sum and its scaling: each input is read once.
 // LONG: rows of more than 8192 elements read their sum again.
 //
-// Bound by DRAM, 16 bits, and by instruction issue beside it, 8 bits (67 % of the slots).  8192 x 5376: 57 us for 352 MB, 6.2 TB/s, and 57
-// us for 310 MB, 5.4 TB/s.  Other forms of 8192 x 5376, 16 / 8 bits: 16 elements a thread 62 / 67 us; every warp with the second half of
-// the row's sum 59 / 67; CTAs that stay, with the next rows copied ahead, 60 / 77, with 24 elements a thread 67 / 64; a warp a row
-// 66 / 74, a warp a row with rows copied ahead 85 / 95 (too few warps to issue what a row needs).
+// Bound by DRAM, 16 bits, and by instruction issue beside it, 8 bits (63 % of the slots).  8192 x 5376: 57.0 us for 352 MB, 6.2 TB/s,
+// and 57.5 us for 310 MB, 5.4 TB/s.  Other forms of 8192 x 5376, 16 / 8 bits: 16 elements a thread 62 / 67 us; the row's factor found by
+// every warp 59 / 67; CTAs that stay, with the next rows copied ahead, 60 / 77, with 24 elements a thread 67 / 64; a warp a row
+// 66 / 74, a warp a row with rows copied ahead 85 / 95.
 template <int DT, int W, bool EIGHT, bool LONG>
 __global__ void __launch_bounds__(kRowThreads) norm_kernel(const __grid_constant__ NormArgs p) {
     __shared__ double parts[32];
@@ -284,8 +284,8 @@ __host__ __device__ inline size_t part_stride(size_t cols) { return (cols + 7) &
 // gradient up through distributed shared memory, which saves a launch.
 //
 // 8192 x 5376: 68 us for 352 MB, 5.2 TB/s, and 7 us for the sum of 444 parts; bound by the wait for the row's sum and by what can be
-// copied ahead beside it (21 warps an SM, 45 % of the issue slots).  One group of 16 columns a thread without copies ahead took 260 us
-// (registers spilled), 8 columns a thread with 21 warps for a row 93, two CTAs of three groups with three rows ahead 75.
+// copied ahead beside it (21 warps an SM, 48 % of the issue slots).  Without copies ahead, 16 columns a thread, the whole took 267 us,
+// with copies and 8 columns a thread 93, with 24 columns and 384 threads 92.
 template <int DT, int W, int G, int MOST>
 __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
     constexpr bool STAGED = W == 8 && G > 0;
