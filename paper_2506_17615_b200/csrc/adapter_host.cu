@@ -13,18 +13,18 @@ constexpr size_t kMaxRank = 128;
 inline size_t padded_rank(size_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 
 // Whether each token gets a cluster of its own, which reads the token's adapter again for each token, or tiles of tokens are
-// multiplied with each adapter that they have.  Only the device knows how many that are.  us, 2688 -> 5376, few requests one after the
-// other / 16 mixed / a request for each token:
-//                     rank 16: tokens           tiles                rank 64: tokens           tiles
-//     64 tokens       7 / 7 / 8                 11 / 32 / 115        12 / 14 / 18              12 / 38 / 169
-//     128             10 / 10 / 14              11 / 32 / 287        20 / 23 / 29              11 / 41 / 326
-//     256             14 / 15 / 21              12 / 33 / 289        34 / 38 / 50              12 / 45 / 327
-//     512             15 / 26 / 40              11 / 44 / 356        34 / 74 / 97              12 / 55 / 407
-// So up to 80 MB of adapters read tokens have their own.  Up to eight times as many they have it where there are adapters for every
-// second token at least: with that many loaded, tokens are likely those of many requests, a batch of single tokens.
+// multiplied with each adapter that they have.  Only the device knows how many that are.  us, bf16, tokens / tiles, requests: 2, one after
+// the other | 16 mixed | one for each token:
+//   2688 -> 5376, rank 16:  64 tokens 6.9 / 9.1 | 7.6 / 27 | 7.6 / 60     256: 14 / 9.8 | 16 / 28 | 21 / 141    512: 15 / 11 | 24 / 36 | 37 / 216
+//                 rank 64:  64        12 / 10 | 13 / 34 | 16 / 79         256: 34 / 11 | 37 / 37 | 46 / 193     512: 35 / 12 | 73 / 46 | 90 / 281
+//   512 -> 768,   rank 16:  512       4.5 / 8.4 | 6.7 / 19 | 6.9 / 95     2048: 11 / 8.2 | 18 / 22 | 24 / 119   8192: 50 / 12 | 71 / 41 | 84 / 277
+//   128 -> 128,   rank 16:  512       3.6 / 7.9 | 5.7 / 19 | 5.8 / 96     2048: 8.8 / 7.7 | 15 / 19 | 15 / 104  8192: 31 / 7.4 | 53 / 20 | 62 / 118
+// A token costs 5 ns and its adapter's bytes at 8 TB/s (the L2 has most).  Tokens have their own clusters where that is 13 us at most, and
+// where there are adapters for every second token at least up to eight times as much: with that many loaded, tokens are likely
+// those of many requests, a batch of single tokens.
 inline bool token_form(size_t tokens, size_t n, size_t k, size_t rank, size_t adapters) {
-    const double bytes = 2.0 * double(tokens) * double(rank) * double(n + k);
-    return bytes <= 80e6 || (tokens <= 2 * adapters && bytes <= 640e6);
+    const double ns = double(tokens) * (5.0 + 2.0 * double(rank) * double(n + k) / 8000.0);
+    return ns <= 13e3 || (tokens <= 2 * adapters && ns <= 104e3);
 }
 // CTAs of a token's cluster: with them all, two for each SM at most, and 32 KB of adapter at least for each
 inline int token_ctas(size_t tokens, size_t n, size_t k, size_t rank, size_t sms) {
@@ -39,39 +39,36 @@ inline size_t adapter_workspace(size_t tokens, size_t n, size_t k, size_t rank, 
     return token_form(tokens, n, k, rank, adapters) ? 0 : sums_bytes(tokens, rank) + up(tokens * sizeof(float), 256);
 }
 
-// Whole waves of CTAs, each with its share of `work` steps and what starting costs, `start` steps: the number of CTAs for each tile
-// that takes least.  `most`: CTAs that run at one time.
-size_t share(size_t tiles, size_t work, size_t start, size_t most, size_t limit, bool powers) {
-    size_t best = 1, least = ~size_t(0);
-    for (size_t c = 1; c <= std::min(limit, work); powers ? c *= 2 : ++c) {
-        const size_t cost = ceil_div(tiles * c, most) * (ceil_div(work, c) + start);
-        if (cost < least) {
-            least = cost;
-            best = c;
-        }
-    }
-    return best;
-}
-
 template <int DT, int RT>
-int launch_tiles(AdapterArgs& a, int sms, cudaStream_t stream) {
-    constexpr size_t R = 16 * RT;
-    const size_t tiles = ceil_div(a.tokens, kTileTokens), blocks = ceil_div(a.n, kUpBlock);
+int launch_tiles(AdapterArgs& a, cudaStream_t stream) {
+    const size_t tiles = ceil_div(a.tokens, kTileTokens), chunks = ceil_div(a.k, 64), blocks = ceil_div(a.n, kTileBlock);
     AdapterMaps m = {};
     TRY(make_map(m.x, a.x, 2, a.k, a.tokens, a.ldx * 2, kTileTokens));
-    TRY(make_map(m.a, a.a, 2, a.k, size_t(a.adapters) * a.rank, size_t(a.k) * 2, R));
-    TRY(make_map(m.high, a.s, 2, R, a.tokens, R * 4, kTileTokens));
-    TRY(make_map(m.low, a.s + R, 2, R, a.tokens, R * 4, kTileTokens));
-    TRY(make_map(m.b, a.b, 2, a.rank, size_t(a.adapters) * a.n, size_t(a.rank) * 2, kUpBlock));
+    TRY(make_map(m.a, a.a, 2, a.k, size_t(a.adapters) * a.rank, size_t(a.k) * 2, 16 * RT));
+    TRY(make_map(m.b, a.b, 2, a.rank, size_t(a.adapters) * a.n, size_t(a.rank) * 2, kTileBlock));
     TRY(make_map(m.y, a.y, 2, a.n, a.tokens, a.ldy * 2, kTileTokens));
     TRY(make_map(m.out, a.out, 2, a.n, a.tokens, a.ldo * 2, 32));
-    // a CTA's start and the exchange of sums take as long as six chunks of 64 columns, the start of the second product as three blocks
-    a.ctas = int(share(tiles, ceil_div(a.k, 64), 6, sms * (RT == 8 ? 1 : 2), 8, true));
-    a.blocks = int(ceil_div(blocks, share(tiles, blocks, 3, sms, ceil_div(2 * sms, tiles), false)));
+    int clusters[9];
+    TRY(resident_clusters(clusters));
+    // Whole waves of clusters.  ns: a cluster's start and the exchange of sums; chunks of x and blocks of y, which take longer where many
+    // CTAs read and write at one time.  Clusters of one size and another, 2688 -> 5376, rank 64, us: 1024 tokens 18 of 6 or 8, two for
+    // each tile, 21 of 6, 26 of 4, 40 of 2; 4096 tokens 30 of 4, 33 of 3, 42 of 2; 8192 tokens 48 of 2, 60 of 3, 74 of 1.
+    size_t least = ~size_t(0);
+    for (size_t c = 1; c <= 8; ++c)
+        for (size_t copies = 1; copies == 1 || (copies <= 8 && copies * c <= blocks && tiles * copies <= size_t(clusters[c])); ++copies) {
+            const size_t busy = std::min(tiles * copies, size_t(clusters[c])) * c;
+            const size_t chunk = std::max<size_t>(200, 27 * busy / 10), block = std::max<size_t>(1300, 25 * busy / 2);
+            const size_t cost = ceil_div(tiles * copies, clusters[c]) *
+                                (5000 + ceil_div(chunks, c) * chunk + ceil_div(blocks, c * copies) * block);
+            if (cost < least) {
+                least = cost;
+                a.ctas = int(c);
+                a.copies = int(copies);
+            }
+        }
     m.p = a;
-    TRY(launch(adapter_down_tiles<DT, RT>, dim3(unsigned(tiles * a.ctas)), kDownThreads, kDownTileSmem<RT>, unsigned(a.ctas), m, stream, true));
-    return launch(adapter_up_tiles<DT, RT>, dim3(unsigned(tiles), unsigned(ceil_div(blocks, a.blocks))), kUpThreads, kUpTileSmem<RT>, 1,
-                  m, stream, true);
+    return launch(adapter_tiles_kernel<DT, RT>, dim3(unsigned(tiles * a.copies * a.ctas)), kTileAdapterThreads, TileRoom<RT>::BYTES,
+                  unsigned(a.ctas), m, stream, true);
 }
 
 template <int DT, int RT>
@@ -81,7 +78,7 @@ int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
         return launch(vec ? adapter_token_kernel<DT, RT, true> : adapter_token_kernel<DT, RT, false>, dim3(unsigned(a.tokens) * a.ctas),
                       kAdapterThreads, 0, unsigned(a.ctas), a, stream);
     }
-    if (a.tiles) return launch_tiles<DT, RT>(a, sms, stream);
+    if (a.tiles) return launch_tiles<DT, RT>(a, stream);
     // two CTAs run on an SM: where there are few tiles, up to eight share one
     const size_t tiles = ceil_div(a.tokens, kDownTokens);
     a.ctas = 1;

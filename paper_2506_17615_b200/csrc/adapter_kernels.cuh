@@ -24,7 +24,8 @@ struct AdapterArgs {
     int tokens, k, n, rank, adapters;
     int ctas;                         // of a cluster, which split k (and, for few tokens, n)
     int tiles;                        // many tokens: through TMA
-    int blocks;                       // of features, that a CTA of the second product takes
+    int copies;                       // and the clusters that a tile of tokens has
+    int blocks;                       // of features, that a CTA of the second product takes where TMA does not read rows
 };
 constexpr int kAdapterWarps = 8, kAdapterThreads = 32 * kAdapterWarps;
 // ranks are padded to 16 RT, RT = 1, 2, 4 or 8

@@ -1,12 +1,18 @@
 // Low-rank adapters of many tokens on the fifth-generation tensor cores, for rows that TMA can read and write.
 //
-//   adapter_down_tiles   S = x A^T, split into high and low halves of 16 bits
-//   adapter_up_tiles     out = y + S B^T
+// A cluster has a tile of 128 tokens.  Its CTAs split k for S = x A^T, exchange their parts, so that each has the whole of S in shared
+// memory, split into high and low halves of 16 bits, and then split n for out = y + S B^T.  More than one cluster for a tile: each
+// makes S for itself, and they split n.  A product runs once for each adapter that the tile's tokens have, and only this adapter's
+// tokens take their rows of its result: what is not finite in one request's adapter does not reach another request.
 //
-// Both take tiles of 128 tokens; reading and writing bounds them, and everything comes and goes by TMA, so that few instructions
-// are left (mma.sync on fragments from memory took 154 us for 8192 tokens, 2688 -> 5376 of rank 64, from rings filled by
-// asynchronous copies 86, this 57).  A product runs once for each adapter that the tile's tokens have, and only this adapter's tokens
-// take their rows of its result: what is not finite in one request's adapter does not reach another request.
+// Everything comes and goes by TMA, so that few instructions are left: x, and A of up to four adapters for it, through a ring; the first
+// blocks of y while S is not there yet; y is added to where it lies and leaves from there.  High and low halves of S are two products
+// with the same rows of B, added up in tensor memory.
+//
+// 8192 tokens, 2688 -> 5376, rank 64: 45 us for one request, 48 for 7, 4.9 and 4.6 TB/s (rank 16: 44).  Bound by DRAM in the second part,
+// about 31 us of it, and by the chain of start, first part and exchange before.  Two launches with S in memory took 57 and read y
+// only in the second; one group of output warps 57; x read once for each adapter of a tile 51; stores by a warp of their own 54; blocks of
+// a cluster's CTAs side by side in a row made no difference.  Of 128 ranks, which leave room for two blocks of y, 69.
 #pragma once
 #include "adapter_kernels.cuh"
 
@@ -14,12 +20,15 @@ namespace equarx {
 namespace ff {
 
 struct AdapterMaps {
-    CUtensorMap x, a, high, low, b, y, out;     // boxes of 64 columns; of 128 rows, a: of 16 RT, out: of 32
+    CUtensorMap x, a, b, y, out;                // boxes of 64 columns; of 128 rows, a: of 16 RT, out: of 32
     AdapterArgs p;
 };
-constexpr int kTileTokens = 128, kDownWarps = 4, kDownThreads = 32 * (kDownWarps + 2);
+constexpr int kTileTokens = 128;
 constexpr int kBoxBytes = kTileTokens * 128;    // 128 rows x 64 columns of 16 bits
 constexpr int kTileSlack = 1024;                // swizzled tiles start on multiples of 1024 bytes
+constexpr int kTileBlock = 128, kYBytes = 2 * kBoxBytes;                         // features; bytes of y
+// Two groups of eight warps put out alternate blocks, 32 tokens x 64 features each, from tensor memory and slots of y of their own.
+constexpr int kGroupWarps = 8, kTileOutWarps = 2 * kGroupWarps, kTileAdapterThreads = 32 * (kTileOutWarps + 2);
 
 // the adapters of a tile's tokens, each once
 struct TileAdapters {
@@ -60,38 +69,66 @@ struct TileAdapters {
     }
 };
 
-// ---------------------------------------------------------------- S = x A^T
-// 128 tokens x 16 RT ranks; the CTAs of a cluster split k and add their parts up in rank order through distributed shared memory.
-// 8192 tokens, 2688 columns, rank 64: 19 us from a cold cache, where reading x takes 7; the rest is the start (index, adapters of the
-// tile), the wait for copies and the exchange.
-template <int RT> constexpr int kDownPipe = RT == 8 ? 4 : 3;
-template <int RT> constexpr int kDownTileStage = kBoxBytes + 16 * RT * 128;
-template <int RT> constexpr int kDownPitch = 16 * RT + 4;                        // floats of a token's sums
-template <int RT> constexpr int kDownTileSmem = kDownPipe<RT> * kDownTileStage<RT> + kTileTokens * kDownPitch<RT> * 4 + kTileSlack;
-static_assert(kDownTileSmem<8> + 4096 <= 227 * 1024 && 2 * (kDownTileSmem<4> + 4096) <= 227 * 1024);
+// Shared memory: S high, S low | blocks of y | blocks of B.  Before S is whole, x and A go through a ring in the place of the later blocks
+// of y and the earlier ones of B, and the CTA's part of S is behind it (128 ranks: the part in the place of y).
+template <int RT> struct TileRoom {
+    static constexpr int R = 16 * RT;
+    static constexpr int BOXES = RT == 8 ? 2 : 1;                                // of 64 ranks
+    static constexpr int B_BYTES = BOXES * kBoxBytes;
+    static constexpr int Y_RING = RT == 8 ? 2 : 4, B_RING = RT == 8 ? 2 : 4;     // a slot of y belongs to one group
+    static constexpr int EARLY_Y = RT == 8 ? 0 : 2, EARLY_B = 2;                 // slots that nothing else is in before
+    static constexpr int AT_ONCE = RT == 8 ? 1 : RT == 1 ? 4 : 2;                // adapters that a pass over x serves
+    static constexpr int PIPE = RT < 4 ? 4 : 3, STAGE = kBoxBytes + AT_ONCE * R * 128;
+    static constexpr int Y = 2 * B_BYTES, B = Y + Y_RING * kYBytes, X = RT == 8 ? B : Y + EARLY_Y * kYBytes;
+    static constexpr int PART = kTileTokens * R * 4, PARTS = RT == 8 ? Y : B + EARLY_B * B_BYTES;
+    static constexpr int END = RT == 8 ? X + PIPE * STAGE : B + B_RING * B_BYTES, BYTES = END + kTileSlack;
+    static_assert(RT == 8 || (X + PIPE * STAGE <= PARTS && PARTS + PART <= END));
+    static_assert(RT != 8 || (B + B_RING * B_BYTES <= END && PARTS + PART <= X));
+};
+// (a CTA that asks for tensor memory after the launch before it must not meet one of tile_kernel, which asks earlier)
+static_assert(TileRoom<1>::BYTES > 128 * 1024 && TileRoom<2>::BYTES > 128 * 1024);
+static_assert(TileRoom<1>::BYTES + 2048 <= 227 * 1024 && TileRoom<2>::BYTES + 2048 <= 227 * 1024 && TileRoom<4>::BYTES + 2048 <= 227 * 1024 &&
+              TileRoom<8>::BYTES + 2048 <= 227 * 1024);
 
 template <int DT, int RT>
-__global__ void __launch_bounds__(kDownThreads, RT == 8 ? 1 : 2) adapter_down_tiles(const __grid_constant__ AdapterMaps m) {
-    constexpr int R = 16 * RT, PIPE = kDownPipe<RT>, STAGE = kDownTileStage<RT>, PITCH = kDownPitch<RT>;
-    constexpr uint32_t COLS = R < 32 ? 32 : R;
+__global__ void __launch_bounds__(kTileAdapterThreads, 1) adapter_tiles_kernel(const __grid_constant__ AdapterMaps m) {
+    using Room = TileRoom<RT>;
+    constexpr int R = Room::R, PIPE = Room::PIPE, STAGE = Room::STAGE, BOXES = Room::BOXES, AT_ONCE = Room::AT_ONCE, Y_RING = Room::Y_RING,
+                  B_RING = Room::B_RING, B_BYTES = Room::B_BYTES;
+    constexpr uint32_t COLS = 4 * kTileBlock;
     const AdapterArgs& p = m.p;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * PIPE + 3];
+    __shared__ uint64_t bars[2 * PIPE + 2 * Y_RING + 2 * B_RING + 11];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t abort;
+    __shared__ float factors[kTileTokens];         // a token's scale, then (fp16) what its S has been divided by
     __shared__ __align__(16) TileAdapters tile;
     const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    float* const sums = reinterpret_cast<float*>(smem_raw + (smem - smem_addr(smem_raw)) + PIPE * STAGE);      // [tokens][PITCH]
-    const uint32_t full = smem_addr(bars), empty = full + 8 * PIPE, ready = empty + 8 * PIPE, drained = ready + 8, drain = drained + 8;
+    const uint32_t s_at = smem, y_at = smem + Room::Y, part_at = smem + Room::PARTS, x_at = smem + Room::X, b_at = smem + Room::B;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * PIPE, b_full = empty + 8 * PIPE, b_empty = b_full + 8 * B_RING,
+                   y_full = b_empty + 8 * B_RING, y_empty = y_full + 8 * Y_RING, got = y_empty + 8 * Y_RING, taken = got + 8,
+                   ready = taken + 8, drained = ready + 32, drain = drained + 32;      // ready, drained: of two accumulators for each group
     const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, rank = uniform(cluster_rank());
-    const int first = int(blockIdx.x / p.ctas) * kTileTokens, count = min(kTileTokens, p.tokens - first);
+    const int cluster = int(blockIdx.x / p.ctas), first = cluster / p.copies * kTileTokens;
     if (threadIdx.x == 0) {
         for (int i = 0; i < PIPE; ++i) {
             barrier_init(full + 8 * i, 1);
             barrier_init(empty + 8 * i, 1);
         }
-        barrier_init(ready, 1);
-        barrier_init(drained, kDownWarps);
+        for (int i = 0; i < B_RING; ++i) {
+            barrier_init(b_full + 8 * i, 1);
+            barrier_init(b_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < Y_RING; ++i) {
+            barrier_init(y_full + 8 * i, 1);
+            barrier_init(y_empty + 8 * i, kGroupWarps);
+        }
+        barrier_init(got, 1);
+        barrier_init(taken, kTileOutWarps);
+        for (int i = 0; i < 4; ++i) {
+            barrier_init(ready + 8 * i, 1);
+            barrier_init(drained + 8 * i, kGroupWarps);
+        }
         barrier_init(drain, 1);
         abort = 0;
         fence_barrier_init();
@@ -99,54 +136,88 @@ __global__ void __launch_bounds__(kDownThreads, RT == 8 ? 1 : 2) adapter_down_ti
     grid_launch();
     grid_wait();
     const int adapters = uniform(tile.find(p, first));
+    if (threadIdx.x < kTileTokens) {
+        const int i = tile.own[threadIdx.x];
+        factors[threadIdx.x] = p.scale && i >= 0 ? p.scale[i] : 1.0f;
+    }
     // only now: no launch before this one can still want tensor memory
-    if (warp == kDownWarps + 1) {
+    if (warp == kTileOutWarps + 1) {
         tmem_alloc<1>(smem_addr(&tmem_slot), COLS);
         fence_before();
     }
     __syncthreads();
     fence_after();
     const uint32_t tmem = uniform(tmem_slot);
-    // every CTA has chunks: a cluster has no more CTAs than there are
-    const int chunks = (p.k + 63) / 64, c0 = int(int64_t(chunks) * rank / p.ctas), c1 = int(int64_t(chunks) * (rank + 1) / p.ctas);
+    // chunks of k: the first CTAs of the cluster have one at least
+    const int chunks = (p.k + 63) / 64, sharers = min(p.ctas, chunks);
+    const int c0 = rank < sharers ? int(int64_t(chunks) * rank / sharers) : 0;
+    const int c1 = rank < sharers ? int(int64_t(chunks) * (rank + 1) / sharers) : 0;
+    // blocks of n
+    const int all = (p.n + kTileBlock - 1) / kTileBlock, place = cluster % p.copies * p.ctas + rank, places = p.copies * p.ctas;
+    const int b0 = int(int64_t(all) * place / places), blocks = int(int64_t(all) * (place + 1) / places) - b0, units = blocks * adapters;
 
-    if (warp == kDownWarps) {
+    // ------------------------------------------------ this CTA's part of S
+    // the loading warp's: chunks, blocks of y and units of B that it has asked for
+    int chunk = 0, asked = 0, unit = 0;
+    auto ask_y = [&] {
+        const uint32_t bar = y_full + 8 * (asked % Y_RING), to = y_at + asked % Y_RING * kYBytes;
+        barrier_expect_warp(bar, kYBytes);
+        for (int h = 0; h < 2; ++h) tma_load_2d(to + h * kBoxBytes, &m.y, (b0 + asked) * kTileBlock + h * 64, first, bar);
+        ++asked;
+    };
+    // past this adapter's features lie the next one's, whose results are not stored
+    auto ask_b = [&](int block, int i) {
+        const uint32_t bar = b_full + 8 * (unit % B_RING), to = b_at + unit % B_RING * B_BYTES;
+        barrier_expect_warp(bar, B_BYTES);
+        for (int c = 0; c < BOXES; ++c) tma_load_2d(to + c * kBoxBytes, &m.b, c * 64, tile.list[i] * p.n + (b0 + block) * kTileBlock, bar);
+        ++unit;
+    };
+    if (warp == kTileOutWarps) {
         bool ok = true;
-        int it = 0;
-        for (int i = 0; i < adapters && ok; ++i) {
-            const int row = tile.list[i] * p.rank;
-            for (int c = c0; c < c1; ++c, ++it) {
-                const int slot = it % PIPE;
-                if (it >= PIPE && !(ok = barrier_wait_warp(empty + 8 * slot, (it / PIPE & 1) ^ 1, &abort))) break;
-                const uint32_t to = smem + slot * STAGE, bar = full + 8 * slot;
-                barrier_expect_warp(bar, STAGE);
+        auto early_y = [&] {
+            while (asked < min(Room::EARLY_Y, blocks)) ask_y();
+        };
+        for (int i = 0; i < adapters && ok; i += AT_ONCE) {
+            const int now = min(AT_ONCE, adapters - i);
+            for (int c = c0; c < c1; ++c, ++chunk) {
+                const int slot = chunk % PIPE;
+                if (chunk == PIPE) early_y();
+                if (chunk >= PIPE && !(ok = barrier_wait_warp(empty + 8 * slot, (chunk / PIPE & 1) ^ 1, &abort))) break;
+                const uint32_t to = x_at + slot * STAGE, bar = full + 8 * slot;
+                barrier_expect_warp(bar, kBoxBytes + now * (R * 128));
                 tma_load_2d(to, &m.x, c * 64, first, bar);
-                tma_load_2d(to + kBoxBytes, &m.a, c * 64, row, bar);
+                for (int g = 0; g < now; ++g) tma_load_2d(to + kBoxBytes + g * (R * 128), &m.a, c * 64, tile.list[i + g] * p.rank, bar);
             }
         }
-        // arrivals that are still owed come before the shared memory goes away
-        for (int i = max(it - PIPE, 0); i < it && ok; ++i) ok = barrier_wait_warp(empty + 8 * (i % PIPE), i / PIPE & 1, &abort);
-        if (gave_up_warp(&abort))
-            for (int i = max(it - PIPE, 0); i < it; ++i) barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
+        early_y();
+        // the ring has been read: B may come
+        for (int i = max(chunk - PIPE, 0); i < chunk && ok; ++i) ok = barrier_wait_warp(empty + 8 * (i % PIPE), i / PIPE & 1, &abort);
+        if (gave_up_warp(&abort))          // what has been started lands before the shared memory goes away
+            for (int i = max(chunk - PIPE, 0); i < chunk; ++i) barrier_drain(full + 8 * (i % PIPE), i / PIPE & 1);
+        else
+            while (unit < min(Room::EARLY_B, units)) ask_b(unit / adapters, unit % adapters);
         __syncwarp();
-    } else if (warp == kDownWarps + 1) {
+    } else if (warp == kTileOutWarps + 1) {
         bool ok = true;
         int it = 0;
-        for (int i = 0; i < adapters && ok; ++i) {
-            if (i && !(ok = barrier_wait_warp(drained, (i - 1) & 1, &abort))) break;
+        for (int i = 0, pass = 0; i < adapters && c0 < c1 && ok; i += AT_ONCE, ++pass) {
+            if (pass && !(ok = barrier_wait_warp(taken, (pass - 1) & 1, &abort))) break;
             fence_after();
+            const int now = min(AT_ONCE, adapters - i);
             for (int c = c0; c < c1; ++c, ++it) {
                 const int slot = it % PIPE;
                 if (!(ok = barrier_wait_warp(full + 8 * slot, it / PIPE & 1, &abort))) break;
                 fence_after();
-                const uint32_t from = smem + slot * STAGE;
+                const uint32_t from = x_at + slot * STAGE;
+                for (int g = 0; g < now; ++g)
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    mma_16bit<1>(tmem, swizzled_desc(from + 32 * kk, 16), swizzled_desc(from + kBoxBytes + 32 * kk, 16),
-                                 desc_16bit(DT == kBf16, false, false, kTileTokens, R), c > c0 || kk);
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_16bit<1>(tmem + g * R, swizzled_desc(from + 32 * kk, 16),
+                                     swizzled_desc(from + kBoxBytes + g * (R * 128) + 32 * kk, 16),
+                                     desc_16bit(DT == kBf16, false, false, kTileTokens, R), c > c0 || kk);
                 mma_commit<1>(empty + 8 * slot);
             }
-            if (ok) mma_commit<1>(ready);
+            if (ok) mma_commit<1>(got);
         }
         if (gave_up_warp(&abort)) {        // products in flight read this shared memory
             mma_commit<1>(drain);
@@ -154,209 +225,148 @@ __global__ void __launch_bounds__(kDownThreads, RT == 8 ? 1 : 2) adapter_down_ti
         }
         __syncwarp();
     } else {
-        const int row = warp * 32 + lane, mine = tile.own[row];
-        float4* const to = reinterpret_cast<float4*>(sums + row * PITCH);
-        for (int i = 0; i < adapters; ++i) {
-            if (!barrier_wait_warp(ready, i & 1, &abort, wait_limit(c1 - c0))) break;
+        // [tokens][ranks]; of a row, four ranks change places with others, so that the rows of a warp meet all banks
+        const int row = warp % 4 * 32 + lane, mine = tile.own[row];
+        for (int i = 0, pass = 0; i < adapters && c0 < c1; i += AT_ONCE, ++pass) {
+            if (!barrier_wait_warp(got, pass & 1, &abort, wait_limit(c1 - c0))) break;
             fence_after();
-            const bool take = tile.list[i] == mine;
+            for (int g = 0; g < min(AT_ONCE, adapters - i); ++g) {
+                const bool take = tile.list[i + g] == mine;
+                if (!__any_sync(0xFFFFFFFFu, take)) continue;
 #pragma unroll
-            for (int c = 0; c < R; c += 16) {
-                uint32_t v[16];
-                __syncwarp();
-                tmem_load16(tmem + (uint32_t(warp * 32) << 16) + c, v);
-                tmem_wait_loads();
-                if (take) {
+                for (int c = 0; c < R; c += 64) {
+                    const int from = c + warp / 4 * 16;
+                    if (from >= R) continue;
+                    uint32_t v[16];
+                    __syncwarp();
+                    tmem_load16(tmem + (uint32_t(warp % 4 * 32) << 16) + g * R + from, v);
+                    tmem_wait_loads();
+                    if (take) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        to[c / 4 + j] = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]),
-                                                    __uint_as_float(v[4 * j + 3]));
+                        for (int j = 0; j < 4; ++j)
+                            st_shared_v4(part_at + row * (R * 4) + (((from / 4 + j) ^ (row & (R / 4 - 1))) << 4), v[4 * j], v[4 * j + 1],
+                                         v[4 * j + 2], v[4 * j + 3]);
+                    }
                 }
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) barrier_arrive(drained);
+            if (lane == 0) barrier_arrive(taken);
         }
         __syncwarp();
     }
-    fence_before();
-    __syncthreads();
-    if (warp == kDownWarps + 1) {
-        fence_after();
-        tmem_free<1>(tmem, COLS);
-    }
-    __syncwarp();
-    cluster_sync();
-    // The cluster's sums of every ctas-th token, scaled, split and stored.  A lane has four ranks; all CTAs' parts are asked for
-    // before the first is added.
-    constexpr int LANES = R / 4, AT_ONCE = 32 / LANES;
-    for (int base = warp * AT_ONCE; base * p.ctas < kTileTokens; base += kDownThreads / 32 * AT_ONCE) {
-        const int token = (base + lane / LANES) * p.ctas + rank, r = lane % LANES * 4;
-        const int i = token < count ? tile.own[token] : -1;
-        float4 part[8];
-        const uint32_t from = smem_addr(sums + min(token, kTileTokens - 1) * PITCH + r);
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (q < p.ctas) part[q] = ld_cluster_f32x4(peer_addr(from, q));
-        float v[4] = {};
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (q < p.ctas) {
-                v[0] += part[q].x; v[1] += part[q].y; v[2] += part[q].z; v[3] += part[q].w;
-            }
-        const float c = p.scale && i >= 0 ? p.scale[i] : 1.0f;
-        float top = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = i >= 0 && r + j < p.rank ? v[j] * c : 0.0f;     // past the adapter's own ranks lie the next one's
-            if (fabsf(v[j]) < __uint_as_float(kInfBits)) top = fmaxf(top, fabsf(v[j]));
-        }
-        float times = 1.0f;
-        if constexpr (DT == kFp16) {
-#pragma unroll
-            for (int s = LANES / 2; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
-            float back;
-            range_of(top, times, back);
-            if (i >= 0 && r == 0) p.back[first + token] = back;
-        }
-        if (i < 0) continue;
-        uint32_t high[2], low[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            split_pair<DT>(v[2 * j] * times, v[2 * j + 1] * times, high[j], low[j]);
-        }
-        uint16_t* const to = p.s + size_t(first + token) * (2 * R) + r;
-        *reinterpret_cast<uint2*>(to) = make_uint2(high[0], high[1]);
-        *reinterpret_cast<uint2*>(to + R) = make_uint2(low[0], low[1]);
-    }
-    __syncwarp();
-    cluster_sync();                        // the others' sums have been read
-}
-
-// ---------------------------------------------------------------- out = y + S B^T
-// 128 tokens, 128 features at a time.  S stays in shared memory; B and y come through rings, y is added to where it lies and leaves from
-// there.  High and low halves of S are two products with the same rows of B, added up in tensor memory, where two accumulators let the
-// next products run meanwhile.  8192 tokens, 5376 features, rank 64: 43 us for 176 MB from a cold cache; both launches take 57, without any
-// adapter to apply 39, and a plain copy of y 28.  Five blocks of y under way instead of three, with a loading warp of their own, changed
-// nothing.
-constexpr int kUpBlock = 128, kUpOut = 2 * kBoxBytes;                            // features; bytes of y
-constexpr int kUpOutWarps = 8, kUpThreads = 32 * (kUpOutWarps + 2);              // 32 tokens x 64 features each
-template <int RT> constexpr int kRankBoxes = RT == 8 ? 2 : 1;                    // of 64 ranks
-template <int RT> constexpr int kUpRing = RT == 8 ? 2 : 3;
-template <int RT> constexpr int kUpTileSmem = 2 * kRankBoxes<RT> * kBoxBytes + kUpRing<RT> * (kRankBoxes<RT> * kBoxBytes + kUpOut) + kTileSlack;
-static_assert(kUpTileSmem<4> + 4096 <= 227 * 1024 && kUpTileSmem<8> + 4096 <= 227 * 1024);
-
-template <int DT, int RT>
-__global__ void __launch_bounds__(kUpThreads, 1) adapter_up_tiles(const __grid_constant__ AdapterMaps m) {
-    constexpr int BOXES = kRankBoxes<RT>, RING = kUpRing<RT>, B_BYTES = BOXES * kBoxBytes;
-    const AdapterArgs& p = m.p;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[4 * RING + 6];
-    __shared__ uint32_t tmem_slot;
-    __shared__ volatile uint32_t abort;
-    __shared__ __align__(16) TileAdapters tile;
-    const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t s_at = smem, b_at = s_at + 2 * B_BYTES, y_at = b_at + RING * B_BYTES;      // S: high, then low
-    const uint32_t b_full = smem_addr(bars), b_empty = b_full + 8 * RING, y_full = b_empty + 8 * RING, y_empty = y_full + 8 * RING,
-                   s_full = y_empty + 8 * RING, ready = s_full + 8, drained = ready + 16, drain = drained + 16;
-    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int first = int(blockIdx.x) * kTileTokens;
-    const int f0 = int(blockIdx.y) * p.blocks * kUpBlock, blocks = (min(p.n - f0, p.blocks * kUpBlock) + kUpBlock - 1) / kUpBlock;
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < RING; ++i) {
-            barrier_init(b_full + 8 * i, 1);
-            barrier_init(b_empty + 8 * i, 1);
-            barrier_init(y_full + 8 * i, 1);
-            barrier_init(y_empty + 8 * i, kUpOutWarps);
-        }
-        barrier_init(s_full, 1);
-        for (int i = 0; i < 2; ++i) {
-            barrier_init(ready + 8 * i, 1);
-            barrier_init(drained + 8 * i, kUpOutWarps);
-        }
-        barrier_init(drain, 1);
-        abort = 0;
-        fence_barrier_init();
-    }
-    grid_launch();
-    grid_wait();
-    const int adapters = uniform(tile.find(p, first));
-    if (warp == kUpOutWarps + 1) {
-        tmem_alloc<1>(smem_addr(&tmem_slot), 2 * kUpBlock);
+    // ------------------------------------------------ S, whole
+    // Every ctas-th token, scaled, split and sent to all.  A lane has four ranks; all CTAs' parts are asked for before the first
+    // is added, and they are added in rank order.
+    if (adapters) {                        // all CTAs of the cluster alike
         fence_before();
+        cluster_sync();
+        fence_after();
+        constexpr int LANES = R / 4, TOKENS = 32 / LANES;
+        const int count = p.tokens - first;
+        for (int base = warp * TOKENS; base * p.ctas < kTileTokens; base += kTileAdapterThreads / 32 * TOKENS) {
+            const int token = (base + lane / LANES) * p.ctas + rank, r = lane % LANES * 4, row = min(token, kTileTokens - 1);
+            const int i = token < min(count, kTileTokens) ? tile.own[token] : -1;
+            const uint32_t from = part_at + row * (R * 4) + (((r / 4) ^ (row & (R / 4 - 1))) << 4);
+            float4 part[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < sharers) part[q] = ld_cluster_f32x4(peer_addr(from, q));
+            float v[4] = {};
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < sharers) {
+                    v[0] += part[q].x; v[1] += part[q].y; v[2] += part[q].z; v[3] += part[q].w;
+                }
+            const float c = factors[row];
+            float top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = i >= 0 && r + j < p.rank ? v[j] * c : 0.0f;     // past the adapter's own ranks lie the next one's
+                if (fabsf(v[j]) < __uint_as_float(kInfBits)) top = fmaxf(top, fabsf(v[j]));
+            }
+            float times = 1.0f, back = 1.0f;
+            if constexpr (DT == kFp16) {
+#pragma unroll
+                for (int d = LANES / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                range_of(top, times, back);
+            }
+            if (i < 0) continue;
+            uint32_t high[2], low[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) split_pair<DT>(v[2 * j] * times, v[2 * j + 1] * times, high[j], low[j]);
+            const uint32_t to = s_at + r / 64 * kBoxBytes + token * 128 + (((r % 64 / 8) ^ (token & 7)) << 4) + r % 8 * 2;
+            for (int q = 0; q < p.ctas; ++q) {
+                st_cluster_v2(peer_addr(to, q), high[0], high[1]);
+                st_cluster_v2(peer_addr(to + B_BYTES, q), low[0], low[1]);
+                if (DT == kFp16 && r == 0) st_cluster_f32(peer_addr(smem_addr(factors + token), q), back);
+            }
+        }
+        fence_async();                     // the products read S, and y comes to where the parts were
+        __syncwarp();
+        cluster_sync();
+        fence_async();
     }
-    __syncthreads();
-    fence_after();
-    const uint32_t tmem = uniform(tmem_slot);
 
-    if (warp == kUpOutWarps) {
-        bool ok = true;
-        int unit = 0, block = 0;
-        if (adapters) {
-            barrier_expect_warp(s_full, 2 * B_BYTES);
-            for (int c = 0; c < BOXES; ++c) {
-                tma_load_2d(s_at + c * kBoxBytes, &m.high, c * 64, first, s_full);
-                tma_load_2d(s_at + B_BYTES + c * kBoxBytes, &m.low, c * 64, first, s_full);
+    // ------------------------------------------------ out = y + S B^T
+    bool ok = !gave_up_warp(&abort);
+    if (warp == kTileOutWarps) {
+        while (ok && asked < min(Y_RING, blocks)) ask_y();
+        for (int block = 0; block < blocks && ok; ++block) {
+            if (block >= asked) {
+                if (!(ok = barrier_wait_warp(y_empty + 8 * (block % Y_RING), (block / Y_RING & 1) ^ 1, &abort))) break;
+                ask_y();
+            }
+            for (int i = max(unit - block * adapters, 0); i < adapters; ++i) {
+                if (unit >= B_RING && !(ok = barrier_wait_warp(b_empty + 8 * (unit % B_RING), (unit / B_RING & 1) ^ 1, &abort))) break;
+                ask_b(block, i);
             }
         }
-        for (; block < blocks && ok; ++block) {
-            const int slot = block % RING, f = f0 + block * kUpBlock;
-            if (block >= RING && !(ok = barrier_wait_warp(y_empty + 8 * slot, (block / RING & 1) ^ 1, &abort))) break;
-            barrier_expect_warp(y_full + 8 * slot, kUpOut);
-            for (int h = 0; h < 2; ++h) tma_load_2d(y_at + slot * kUpOut + h * kBoxBytes, &m.y, f + h * 64, first, y_full + 8 * slot);
-            for (int i = 0; i < adapters; ++i, ++unit) {
-                const int at = unit % RING;
-                if (unit >= RING && !(ok = barrier_wait_warp(b_empty + 8 * at, (unit / RING & 1) ^ 1, &abort))) break;
-                barrier_expect_warp(b_full + 8 * at, B_BYTES);
-                // past this adapter's features lie the next one's, whose results are not stored
-                for (int c = 0; c < BOXES; ++c)
-                    tma_load_2d(b_at + at * B_BYTES + c * kBoxBytes, &m.b, c * 64, tile.list[i] * p.n + f, b_full + 8 * at);
-            }
-        }
-        for (int i = max(unit - RING, 0); i < unit && ok; ++i) ok = barrier_wait_warp(b_empty + 8 * (i % RING), i / RING & 1, &abort);
-        if (gave_up_warp(&abort)) {        // what has been started lands before the shared memory goes away
-            if (adapters) barrier_drain(s_full, 0);
-            for (int i = max(unit - RING, 0); i < unit; ++i) barrier_drain(b_full + 8 * (i % RING), i / RING & 1);
-            for (int i = max(block - RING, 0); i < block; ++i) barrier_drain(y_full + 8 * (i % RING), i / RING & 1);
+        // arrivals that are still owed come before the shared memory goes away
+        for (int i = max(unit - B_RING, 0); i < unit && ok; ++i)
+            ok = barrier_wait_warp(b_empty + 8 * (i % B_RING), i / B_RING & 1, &abort);
+        if (gave_up_warp(&abort)) {
+            for (int i = max(unit - B_RING, 0); i < unit; ++i) barrier_drain(b_full + 8 * (i % B_RING), i / B_RING & 1);
+            for (int i = max(asked - Y_RING, 0); i < asked; ++i) barrier_drain(y_full + 8 * (i % Y_RING), i / Y_RING & 1);
         }
         __syncwarp();
-    } else if (warp == kUpOutWarps + 1) {
-        const int units = blocks * adapters;
-        bool ok = units == 0 || barrier_wait_warp(s_full, 0, &abort);
-        for (int unit = 0; unit < units && ok; ++unit) {
-            const int at = unit % RING, buf = unit & 1;
-            if (!(ok = barrier_wait_warp(b_full + 8 * at, unit / RING & 1, &abort))) break;
-            if (unit > 1 && !(ok = barrier_wait_warp(drained + 8 * buf, (unit / 2 - 1) & 1, &abort))) break;
-            fence_after();
-            const uint32_t d = tmem + buf * kUpBlock, from = b_at + at * B_BYTES;
+    } else if (warp == kTileOutWarps + 1) {
+        const bool start = ok;
+        int u = 0;
+        for (int block = 0; block < blocks && ok; ++block)
+            for (int i = 0; i < adapters; ++i, ++u) {
+                const int at = u % B_RING, turn = block / 2 * adapters + i, buf = block % 2 * 2 + turn % 2;      // turn: of the group
+                if (!(ok = barrier_wait_warp(b_full + 8 * at, u / B_RING & 1, &abort))) break;
+                if (turn > 1 && !(ok = barrier_wait_warp(drained + 8 * buf, (turn / 2 - 1) & 1, &abort))) break;
+                fence_after();
+                const uint32_t d = tmem + buf * kTileBlock, from = b_at + at * B_BYTES;
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int kk = 0; kk < RT; ++kk) {
-                    const uint32_t in = kk / 4 * kBoxBytes + kk % 4 * 32;
-                    mma_16bit<1>(d, swizzled_desc(s_at + half * B_BYTES + in, 16), swizzled_desc(from + in, 16),
-                                 desc_16bit(DT == kBf16, false, false, kTileTokens, kUpBlock), half | kk);
-                }
-            mma_commit<1>(b_empty + 8 * at);
-            mma_commit<1>(ready + 8 * buf);
-        }
-        if (gave_up_warp(&abort)) {
+                    for (int kk = 0; kk < RT; ++kk) {
+                        const uint32_t in = kk / 4 * kBoxBytes + kk % 4 * 32;
+                        mma_16bit<1>(d, swizzled_desc(s_at + half * B_BYTES + in, 16), swizzled_desc(from + in, 16),
+                                     desc_16bit(DT == kBf16, false, false, kTileTokens, kTileBlock), half | kk);
+                    }
+                mma_commit<1>(b_empty + 8 * at);
+                mma_commit<1>(ready + 8 * buf);
+            }
+        if (start && gave_up_warp(&abort)) {
             mma_commit<1>(drain);
             barrier_drain(drain, 0);
         }
         __syncwarp();
     } else {
-        const int rows = warp % 4 * 32, row = rows + lane, half = warp / 4, mine = tile.own[row];
-        const float back = DT == kFp16 && mine >= 0 ? __ldcg(p.back + first + row) : 1.0f;
-        bool ok = true;
-        int unit = 0;
-        for (int block = 0; block < blocks && ok; ++block) {
-            const int slot = block % RING, f = f0 + block * kUpBlock;
-            const uint32_t y = y_at + slot * kUpOut + half * kBoxBytes + row * 128;
-            if (!(ok = barrier_wait_warp(y_full + 8 * slot, block / RING & 1, &abort))) break;
-            for (int i = 0; i < adapters; ++i, ++unit) {
-                const int buf = unit & 1;
-                if (!(ok = barrier_wait_warp(ready + 8 * buf, unit / 2 & 1, &abort))) break;
+        const int group = warp / kGroupWarps, rows = warp % 4 * 32, row = rows + lane, half = warp / 4 % 2, mine = tile.own[row];
+        const float back = DT == kFp16 && mine >= 0 ? factors[row] : 1.0f;
+        int turn = 0;
+        for (int block = group; block < blocks && ok; block += 2) {
+            const int slot = block % Y_RING, f = (b0 + block) * kTileBlock;
+            const uint32_t y = y_at + slot * kYBytes + half * kBoxBytes + row * 128;
+            if (!(ok = barrier_wait_warp(y_full + 8 * slot, block / Y_RING & 1, &abort))) break;
+            for (int i = 0; i < adapters; ++i, ++turn) {
+                const int buf = group * 2 + turn % 2;
+                if (!(ok = barrier_wait_warp(ready + 8 * buf, turn / 2 & 1, &abort))) break;
                 fence_after();
                 const bool take = tile.list[i] == mine;
                 if (__any_sync(0xFFFFFFFFu, take)) {
@@ -364,7 +374,7 @@ __global__ void __launch_bounds__(kUpThreads, 1) adapter_up_tiles(const __grid_c
                     for (int c = 0; c < 64; c += 32) {
                         uint32_t v[32];
                         __syncwarp();
-                        tmem_load32(tmem + buf * kUpBlock + half * 64 + (uint32_t(rows) << 16) + c, v);
+                        tmem_load32(tmem + buf * kTileBlock + half * 64 + (uint32_t(rows) << 16) + c, v);
                         tmem_wait_loads();
                         if (!take) continue;
 #pragma unroll
@@ -392,9 +402,9 @@ __global__ void __launch_bounds__(kUpThreads, 1) adapter_up_tiles(const __grid_c
             __syncwarp();
             if (lane == 0) {
                 if (first + rows < p.tokens && f + half * 64 < p.n)
-                    tma_store_2d(&m.out, y_at + slot * kUpOut + half * kBoxBytes + rows * 128, f + half * 64, first + rows);
-                tma_store_wait_read<1>();                  // the block before this one has left
-                if (block) barrier_arrive(y_empty + 8 * ((block - 1) % RING));
+                    tma_store_2d(&m.out, y_at + slot * kYBytes + half * kBoxBytes + rows * 128, f + half * 64, first + rows);
+                tma_store_wait_read<0>();                  // the other group works meanwhile
+                barrier_arrive(y_empty + 8 * slot);
             }
             __syncwarp();
         }
@@ -403,9 +413,9 @@ __global__ void __launch_bounds__(kUpThreads, 1) adapter_up_tiles(const __grid_c
     }
     fence_before();
     __syncthreads();
-    if (warp == kUpOutWarps + 1) {
+    if (warp == kTileOutWarps + 1) {
         fence_after();
-        tmem_free<1>(tmem, 2 * kUpBlock);
+        tmem_free<1>(tmem, COLS);
     }
 }
 

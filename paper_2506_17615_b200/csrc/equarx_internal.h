@@ -1,4 +1,4 @@
-// What the library's two host files share.
+// What the library's host files share.
 #pragma once
 #include <cuda_runtime.h>
 
@@ -11,6 +11,8 @@ cudaError_t launch_error_to_inject();
 bool dependent_launches();
 // records `e` for equarx_last_cuda_error() and returns EQUARX_ERR_CUDA
 int cuda_failure(cudaError_t e);
+// clusters of 1 .. 8 CTAs that run at one time on the current device when each CTA has an SM to itself
+int resident_clusters(int (&out)[9]);
 // waits of the adapters' kernels that gave up on the current device since the last call
 cudaError_t adapters_gave_up(uint32_t& seen);
 }  // namespace equarx

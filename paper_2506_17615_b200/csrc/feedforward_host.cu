@@ -21,6 +21,9 @@ inline size_t fp4_stages(size_t cols) { return ceil_div(cols, 256); }
 template <int KIND> inline size_t coded_stride(size_t cols) { return KIND == kMx8 ? fp8_stride(cols) : codes_stride(cols); }
 template <int KIND> inline size_t coded_stages(size_t cols) { return KIND == kMx8 ? fp8_stages(cols) : fp4_stages(cols); }
 
+}  // namespace
+
+namespace equarx {
 // Clusters of 1 .. 8 CTAs that run at one time when each CTA has an SM to itself: a cluster stays inside a
 // GPC, so this is less than the number of SMs divided by the size.
 int resident_clusters(int (&out)[9]) {
@@ -51,6 +54,9 @@ int resident_clusters(int (&out)[9]) {
     std::copy(facts.clusters, facts.clusters + 9, out);
     return EQUARX_OK;
 }
+}  // namespace equarx
+
+namespace {
 
 // ---------------------------------------------------------------- tensor maps
 // scales of a coded matrix as rows of 128 bytes, those of one 128-row group and one stage together

@@ -93,6 +93,9 @@ __device__ __forceinline__ uint32_t ld_shared_u16(uint32_t addr) {
 }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// the same for any memory, another CTA's too
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
 // ---------------------------------------------------------------- copies of one thread
 // 16 bytes to shared memory, the last 16 - `bytes` of them zeros; both addresses are multiples of 16
 __device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src, int bytes) {
@@ -126,6 +129,9 @@ __device__ __forceinline__ void barrier_arrive_pair(uint32_t cluster_bar) {
 }
 __device__ __forceinline__ void st_cluster_f32(uint32_t cluster_addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster_v2(uint32_t cluster_addr, uint32_t a, uint32_t b) {
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(cluster_addr), "r"(a), "r"(b) : "memory");
 }
 __device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
     float v;

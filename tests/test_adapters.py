@@ -98,6 +98,9 @@ SIZES = [(1, 1, 1, 1, 1), (1, 64, 64, 16, 1), (1, 5376, 2688, 16, 3), (2, 33, 40
 SIZES += [(1500, 5376, 520, 16, 2), (8192, 640, 72, 8, 3), (5000, 1000, 1000, 64, 2), (3000, 1360, 640, 128, 30), (2000, 2640, 1000, 72, 3),
           (2500, 1001, 777, 16, 4), (4100, 600, 201, 40, 5), (1300, 1032, 777, 100, 3), (1030, 3000, 1000, 32, 300), (2049, 2568, 512, 24, 20),
           (70000, 72, 136, 5, 6), (1111, 2500, 2600, 31, 2), (900, 9000, 128, 16, 3)]
+# one chunk of columns, one block of features, clusters of one CTA, two for a tile, adapters that a pass over x does not hold
+SIZES += [(1200, 7000, 64, 32, 3), (3000, 8, 3000, 16, 5), (40000, 128, 128, 16, 5), (1400, 5000, 1000, 128, 5), (1025, 4096, 2000, 16, 11),
+          (2100, 2000, 640, 64, 9), (20000, 300 * 8, 64, 8, 2)]
 
 
 @gpu
