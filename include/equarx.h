@@ -545,6 +545,17 @@ int equarx_fp8_matmul(const uint8_t *a_codes, const uint8_t *a_scales,
                       size_t m, size_t n, size_t k, void *out, int dtype, size_t ld, equarx_stream_t stream);
 
 /*
+ * out = x w^T, x (m x k, BF16 or FP16) quantized by this call, w (n x k) before:
+ * equarx_fp8_quantize followed by equarx_fp8_matmul.  out has x's type.  For a few tokens
+ * the product quantizes x itself and the workspace is 0 bytes.
+ */
+size_t equarx_fp8_linear_workspace_bytes(size_t m, size_t k);
+int equarx_fp8_linear(const void *x, int dtype, size_t ldx,
+                      const uint8_t *w_codes, const uint8_t *w_scales,
+                      size_t m, size_t n, size_t k, void *out, size_t ld,
+                      void *workspace, size_t workspace_bytes, equarx_stream_t stream);
+
+/*
  * h = act(x Wg^T) * (x Wu^T): x is m x k, both weights f x k, h m x f (BF16 or FP16); one
  * kernel.
  */

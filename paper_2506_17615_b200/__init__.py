@@ -63,6 +63,8 @@ _BINDING_NAMES = (
     "fp8_codes_bytes",
     "fp8_dequantize",
     "fp8_gated",
+    "fp8_linear",
+    "fp8_linear_workspace_bytes",
     "fp8_matmul",
     "fp8_quantize",
     "fp8_scales_bytes",

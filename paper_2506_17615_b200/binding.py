@@ -56,6 +56,8 @@ EXPORTS = (
     "equarx_fp8_quantize",
     "equarx_fp8_dequantize",
     "equarx_fp8_matmul",
+    "equarx_fp8_linear",
+    "equarx_fp8_linear_workspace_bytes",
     "equarx_fp8_gated",
     "equarx_add_rms_norm",
     "equarx_add_rms_norm_fp8",
@@ -122,6 +124,8 @@ def _load():
     lib.equarx_fp8_quantize.argtypes = [vp, ci, sz, sz, sz, vp, vp, vp]
     lib.equarx_fp8_dequantize.argtypes = [vp, vp, sz, sz, vp, ci, sz, vp]
     lib.equarx_fp8_matmul.argtypes = [vp] * 4 + [sz, sz, sz, vp, ci, sz, vp]
+    lib.equarx_fp8_linear_workspace_bytes.argtypes = [sz, sz]
+    lib.equarx_fp8_linear.argtypes = [vp, ci, sz, vp, vp, sz, sz, sz, vp, sz, vp, sz, vp]
     lib.equarx_fp8_gated.argtypes = [vp] * 6 + [sz, sz, sz, ci, vp, ci, sz, vp]
     lib.equarx_add_rms_norm.argtypes = [vp, sz, vp, sz, vp, ci, ci, sz, sz, cd, cf, vp, sz, vp, sz, vp, vp]
     lib.equarx_add_rms_norm_fp8.argtypes = [vp, sz, vp, sz, vp, ci, ci, sz, sz, cd, cf, vp, sz, vp, vp, vp]
@@ -129,7 +133,8 @@ def _load():
     lib.equarx_add_rms_norm_backward.argtypes = [vp, sz, vp, sz, vp, sz, vp, vp, ci, ci, sz, sz, cf, vp, sz, vp, vp, sz, vp]
     lib.equarx_add_adapters_workspace_bytes.argtypes = [sz] * 5
     lib.equarx_add_adapters.argtypes = [vp, sz, vp, sz, vp, vp, vp, vp, ci, sz, sz, sz, sz, sz, vp, sz, vp, sz, vp]
-    for name in ("fp8_codes_bytes", "fp8_scales_bytes", "add_rms_norm_backward_workspace_bytes", "add_adapters_workspace_bytes"):
+    for name in ("fp8_codes_bytes", "fp8_scales_bytes", "fp8_linear_workspace_bytes", "add_rms_norm_backward_workspace_bytes",
+                 "add_adapters_workspace_bytes"):
         getattr(lib, "equarx_" + name).restype = sz
     for name in ("fp4_codes_bytes", "fp4_scales_bytes", "fp4_linear_workspace_bytes", "gated_forward_workspace_bytes",
                  "gated_backward_workspace_bytes"):
@@ -373,6 +378,16 @@ def fp8_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, st
     _check(lib.equarx_fp8_matmul(_ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), m, n, k, _ptr(out), dtype, ld,
                                  _ptr(stream)),
            "equarx_fp8_matmul")
+
+
+def fp8_linear_workspace_bytes(m, k):
+    return lib.equarx_fp8_linear_workspace_bytes(m, k)
+
+
+def fp8_linear(x, dtype, ldx, w_codes, w_scales, m, n, k, out, ld, workspace, workspace_bytes, stream=0):
+    _check(lib.equarx_fp8_linear(_ptr(x), dtype, ldx, _ptr(w_codes), _ptr(w_scales), m, n, k, _ptr(out), ld, _ptr(workspace),
+                                 workspace_bytes, _ptr(stream)),
+           "equarx_fp8_linear")
 
 
 def fp8_gated(x_codes, x_scales, g_codes, g_scales, u_codes, u_scales, m, f, k, act, h, dtype, ldh, stream=0):

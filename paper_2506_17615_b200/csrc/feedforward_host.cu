@@ -151,8 +151,12 @@ int quantize(const void* x, int dtype, size_t rows, size_t cols, size_t ld, int 
 //                 graph    8.6 / 7.8              10.3 / 9.7              5.7 / 5.3
 // MX wins up to 8 tokens everywhere.  NV's row maxima go round the cluster first: up to 2 tokens it wins as calls, and in
 // a graph for the gated block, where a single product loses 0.2 to 0.7 us.
-constexpr size_t kFusedMxTokens = 8, kFusedNvTokens = 2;
-static_assert(kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, "the fused form takes one tile of tokens");
+// 8 bits, 1 token  calls   7.9 / 9.2              -                       4.5 / 7.5
+//                  graph   7.5 / 8.2              -                       3.7 / 4.5
+//         8        graph   7.7 / 8.3              -                       3.6 / 4.8
+//         16       graph   9.5 / 8.5              -                       3.8 / 4.9
+constexpr size_t kFusedMxTokens = 8, kFusedNvTokens = 2, kFusedFp8Tokens = 8;
+static_assert(kFusedFp8Tokens <= kFusedTokens && kFusedMxTokens <= kFusedTokens && kFusedNvTokens <= kFusedTokens, "the fused form takes one tile of tokens");
 
 // Columns of a tile, and what the launch is expected to take in cycles of an SM.  The pairs of SMs work
 // through whole rounds of tiles.  A stage takes a pair 1.3 cycles for each of the (256 + bn) rows of 128 bytes
@@ -326,21 +330,34 @@ inline size_t product_workspace(size_t m, size_t k, int format) {
     return quantizes_itself(m, format) ? 0 : carved_bytes(m, k, format);
 }
 
+// the same in 8 bits
+Fp4 carve8(void* ws, size_t rows, size_t cols) {
+    uint8_t* const p = static_cast<uint8_t*>(ws);
+    return Fp4{p + up(equarx_fp8_scales_bytes(rows, cols), 256), p, nullptr};
+}
+inline size_t carved8_bytes(size_t rows, size_t cols) {
+    return up(equarx_fp8_scales_bytes(rows, cols), 256) + up(rows * fp8_stride(cols), 256);
+}
+
+// a product that quantizes x (16 bits) itself
+template <int KIND, int MODE>
+int itself_quantized(const QuantArgs& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, cudaStream_t stream) {
+    SplitArgs a = {};
+    SplitPlan split;
+    TRY((plan_split<KIND, MODE, false>(split, n, m, int(coded_stages<KIND>(k)))));
+    TRY((split_weights<KIND, MODE>(a, w, n, k)));
+    a.raw = x;
+    a.out[0] = out;
+    a.act = act;
+    return launch_split<KIND, MODE, false, false, true>(a, split, n, m, stream);
+}
+
 // x (16 bits) quantized and multiplied with one or two weights
 template <int KIND, int MODE>
 int quantized_product(const QuantArgs& x, const Fp4* w, size_t m, size_t n, size_t k, int act, const Out& out, void* workspace,
                       cudaStream_t stream) {
     const int format = KIND == kMx ? EQUARX_FP4_MX : EQUARX_FP4_NV;
-    if (quantizes_itself(m, format)) {
-        SplitArgs a = {};
-        SplitPlan split;
-        TRY((plan_split<KIND, MODE, false>(split, n, m, int(fp4_stages(k)))));
-        TRY((split_weights<KIND, MODE>(a, w, n, k)));
-        a.raw = x;
-        a.out[0] = out;
-        a.act = act;
-        return launch_split<KIND, MODE, false, false, true>(a, split, n, m, stream);
-    }
+    if (quantizes_itself(m, format)) return itself_quantized<KIND, MODE>(x, w, m, n, k, act, out, stream);
     const Fp4 q = carve(workspace, m, k, format);
     TRY(quantize(x.x, x.dtype, m, k, x.ld, format, q, stream));
     return coded_product<KIND, MODE>(q, w, m, n, k, act, out, stream);
@@ -574,6 +591,31 @@ int equarx_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uin
     TRY(check_overlap({fp8_codes_span(a, m, k), fp8_scales_span(a, m, k), fp8_codes_span(b, n, k), fp8_scales_span(b, n, k)},
                       {matrix(out, m, n, ld, size_of(dtype))}));
     return coded_product<kMx8, kPlain>(a, &b, m, n, k, 0, out_rows(out, ld, dtype), stream);
+}
+
+size_t equarx_fp8_linear_workspace_bytes(size_t m, size_t k) {
+    return m > kMaxDim || bad_dim(k) || m <= kFusedFp8Tokens ? 0 : carved8_bytes(m, k);
+}
+
+int equarx_fp8_linear(const void* x, int dtype, size_t ldx, const uint8_t* w_codes, const uint8_t* w_scales, size_t m, size_t n, size_t k,
+                      void* out, size_t ld, void* workspace, size_t workspace_bytes, equarx_stream_t stream) {
+    if (!is_16bit(dtype)) return EQUARX_ERR_FORMAT;
+    if (m > kMaxDim || bad_dim(n) || bad_dim(k) || bad_ld(ldx, k) || bad_ld(ld, n)) return EQUARX_ERR_COUNT;
+    if (m == 0) return EQUARX_OK;
+    const Fp4 w{w_codes, w_scales, nullptr};
+    const size_t need = equarx_fp8_linear_workspace_bytes(m, k);
+    if (!x || !out || (need && !workspace)) return EQUARX_ERR_NULL;
+    TRY(check_fp8(w));
+    if (workspace_bytes < need) return EQUARX_ERR_WORKSPACE;
+    if (!aligned(x, 2) || !aligned(out, 2) || !aligned(workspace, 16)) return EQUARX_ERR_ALIGN;
+    TRY(check_overlap({matrix(x, m, k, ldx, 2), fp8_codes_span(w, n, k), fp8_scales_span(w, n, k)},
+                      {matrix(out, m, n, ld, 2), Span{workspace, need}}));
+    const QuantArgs a = rows_to_quantize(x, dtype, m, k, ldx);
+    const Out o = out_rows(out, ld, dtype);
+    if (m <= kFusedFp8Tokens) return itself_quantized<kMx8, kPlain>(a, &w, m, n, k, 0, o, stream);
+    const Fp4 q = carve8(workspace, m, k);
+    TRY(equarx_fp8_quantize(x, dtype, m, k, ldx, const_cast<uint8_t*>(q.codes), const_cast<uint8_t*>(q.scales), stream));
+    return coded_product<kMx8, kPlain>(q, &w, m, n, k, 0, o, stream);
 }
 
 int equarx_fp8_gated(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* g_codes, const uint8_t* g_scales,

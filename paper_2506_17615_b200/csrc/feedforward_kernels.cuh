@@ -1289,12 +1289,12 @@ static_assert(kTileSmem<kHalf> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
 // reduction axis (W_MN and X_MN), features = columns of x and "tokens" = rows of a weight, the second half
 // of grid.y being the second output.
 //
-// FUSED (4-bit, at most 16 tokens): x comes in 16 bits; the warps that write the output later quantize
+// FUSED (4 and 8 bits, at most 16 tokens): x comes in 16 bits; the warps that write the output later quantize
 // the stages of x first, straight into the swizzled rows that the products read, which saves a launch
 // and a round trip of x.
 template <int KIND, int MODE, bool W_MN, bool X_MN, bool FUSED>
 __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_constant__ SplitArgs p) {
-    constexpr bool SCALED = KIND != kHalf, MX = KIND == kMx;
+    constexpr bool SCALED = KIND != kHalf, MX = KIND == kMx, NV = KIND == kNv;
     constexpr int SB = kScaleBytes<KIND>, NW = MODE == kGated ? 2 : 1;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[2 * kSplitMaxPipe + 2];
@@ -1374,13 +1374,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
     if (warp == 4) {
         for (int it = 0; it < early; ++it) load_stage(it);
     }
-    // FUSED.  A unit is one token's part of one stage: 16 groups of 16 elements, half a warp.  The first four
+    // FUSED.  A unit is one token's part of one stage: 16 groups of 16 elements, half a warp, or, 8 bits, 8 groups.  The first four
     // warps take the units in the order of the stages, the next one's loads under way.  One body for both
     // 16-bit types and no unrolling: what runs a few times costs mostly the fetching of its instructions.
-    const int j = lane & 15;
+    constexpr int LANES = KIND == kMx8 ? 8 : 16, AT_ONCE = 32 / LANES;
+    const int j = lane % LANES;
     auto for_units = [&](auto&& body) {
         const int n = s1 - s0;
-        int it = 0, t = warp * 2 + (lane >> 4);
+        int it = 0, t = warp * AT_ONCE + lane / LANES;
         auto settle = [&] {
             while (t >= p.tokens && it < n) {
                 t -= p.tokens;
@@ -1389,14 +1390,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         };
         settle();
         Group<kBf16> next = {};                          // the bits of either type
-        if (it < n) load_group<kBf16, true>(p.raw, t, (s0 + it) * 256 + j * 16, next);
+        if (it < n) load_group<kBf16, true>(p.raw, t, ((s0 + it) * LANES + j) * 16, next);
 #pragma unroll 1
         while (__any_sync(0xFFFFFFFFu, it < n)) {
             const Group<kBf16> g = next;
             const int at = it, row = t;
-            t += 8;
+            t += 4 * AT_ONCE;
             settle();
-            if (it < n) load_group<kBf16, true>(p.raw, t, (s0 + it) * 256 + j * 16, next);
+            if (it < n) load_group<kBf16, true>(p.raw, t, ((s0 + it) * LANES + j) * 16, next);
             float v[16];
             uint32_t m = 0;
 #pragma unroll
@@ -1409,7 +1410,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             body(at, row, at < n, v, m);
         }
     };
-    if constexpr (FUSED && !MX) {
+    if constexpr (FUSED && NV) {
         // The rows' maxima: the cluster's CTAs have the whole of each row between them, and each tells all.
         __syncthreads();
         cluster_wait();                                 // every CTA of the cluster has started
@@ -1496,21 +1497,27 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
             const int slot = at % p.pipe;
             float up = 0.0f, factor = 0.0f, inv;
             uint32_t byte;
-            if (MX) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-            if (!MX && in) row_factors(row_max[row], up, factor);
-            block_scale<MX>(m, up, factor, byte, inv);
-            const uint2 code = encode_values(v, inv);
-            // the halves of the warp may wait for different stages, and go on together
+            if (!NV) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+            if (NV && in) row_factors(row_max[row], up, factor);
+            if constexpr (KIND == kMx8) fp8_block_scale(m, byte, inv);
+            else block_scale<MX>(m, up, factor, byte, inv);
+            auto codes = [&] {
+                if constexpr (KIND == kMx8) return encode_e4m3(v, inv);
+                else return encode_values(v, inv);
+            };
+            const auto code = codes();
+            // the parts of the warp may wait for different stages, and go on together
             bool vacant = ok;
             if (ok && in && at >= p.pipe) vacant = barrier_wait(empty + 8 * slot, (at / p.pipe & 1) ^ 1, &abort, kWaitLimit);
             ok = __all_sync(0xFFFFFFFFu, vacant);
             if (in && ok) {
                 uint8_t* const sx = smem_ptr + slot * STAGE + NW * kTileBytes;
                 uint8_t* const ss = sx + xb + SB * NW;
-                // byte 8 j of the row's 128: 16-byte pieces are swizzled by the row
-                *reinterpret_cast<uint2*>(sx + row * 128 + (((j >> 1) ^ (row & 7)) << 4) + (j & 1) * 8) = code;
-                const int block = MX ? j >> 1 : j;
-                if (!MX || !(j & 1)) ss[(block >> 2) * 512 + row * 16 + (block & 3)] = uint8_t(byte);
+                // byte 8 j, or 16 j, of the row's 128: 16-byte pieces are swizzled by the row
+                if constexpr (KIND == kMx8) *reinterpret_cast<uint4*>(sx + row * 128 + ((j ^ (row & 7)) << 4)) = code;
+                else *reinterpret_cast<uint2*>(sx + row * 128 + (((j >> 1) ^ (row & 7)) << 4) + (j & 1) * 8) = code;
+                const int block = NV ? j : j >> 1;
+                if (NV || !(j & 1)) ss[(block >> 2) * 512 + row * 16 + (block & 3)] = uint8_t(byte);
                 fence_async_shared();
             }
             __syncwarp();
@@ -1527,7 +1534,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) split_kernel(const __grid_co
         fence_after();
     }
     if (p.reuse) cluster_arrive();                      // this CTA's loads and products are done
-    if constexpr (!FUSED || MX) cluster_wait();         // the others' memory may be written
+    if constexpr (!FUSED || !NV) cluster_wait();        // the others' memory may be written
     if (warp < 4 && good) {
         const uint32_t row = warp * 32 + lane;
         for (int q = 0; q < NW; ++q) {

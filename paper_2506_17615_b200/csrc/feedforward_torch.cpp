@@ -36,6 +36,8 @@ namespace {
     X(fp8_quantize)                      \
     X(fp8_dequantize)                    \
     X(fp8_matmul)                        \
+    X(fp8_linear_workspace_bytes)        \
+    X(fp8_linear)                        \
     X(fp8_gated)                         \
     X(add_rms_norm)                      \
     X(add_rms_norm_fp8)                  \
@@ -411,7 +413,7 @@ PyObject* gated8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// linear8(x, buffer w, rows of w, cols): x quantized first, into a buffer of its own
+// linear8(x, buffer w, rows of w, cols): x quantized in the call
 PyObject* linear8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     arguments(n, 4);
@@ -424,12 +426,11 @@ PyObject* linear8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     no_gradient(x.t, "x", kEight);
     const at::Device device = x.t.device();
     const Fp8 w = parts8(dw, rows, k, device);
-    const at::Tensor out = empty(x.rows, rows, x.t.scalar_type(), device), ws = empty8(x.rows, k, device);
-    const Fp8 q = parts8(ws, x.rows, k, device);
+    const at::Tensor out = empty(x.rows, rows, x.t.scalar_type(), device);
+    const size_t need = entry.fp8_linear_workspace_bytes(x.rows, k);
+    const at::Tensor ws = bytes(need, device);
     return result(call(device, [&](equarx_stream_t s) {
-        const int status = entry.fp8_quantize(x.p, dtype, x.rows, k, x.ld, q.codes, q.scales, s);
-        return status ? status
-                      : entry.fp8_matmul(q.codes, q.scales, w.codes, w.scales, x.rows, rows, k, out.data_ptr(), dtype, rows, s);
+        return entry.fp8_linear(x.p, dtype, x.ld, w.codes, w.scales, x.rows, rows, k, out.data_ptr(), rows, address(ws), need, s);
     }), out);
     END_HANDLE_TH_ERRORS
 }

@@ -34,7 +34,7 @@ _native = importlib.import_module("._feedforward", __package__)
 for _name in ("fp4_codes_bytes", "fp4_scales_bytes", "fp4_quantize", "fp4_dequantize", "fp4_matmul", "fp4_linear_workspace_bytes",
               "fp4_linear", "fp4_gated", "gated_forward_workspace_bytes", "gated_forward", "gated_backward_workspace_bytes",
               "gated_backward", "fp8_codes_bytes", "fp8_scales_bytes", "fp8_quantize", "fp8_dequantize", "fp8_matmul", "fp8_gated",
-              "add_rms_norm", "add_rms_norm_fp8", "add_rms_norm_backward_workspace_bytes", "add_rms_norm_backward", "add_adapters",
+              "fp8_linear_workspace_bytes", "fp8_linear", "add_rms_norm", "add_rms_norm_fp8", "add_rms_norm_backward_workspace_bytes", "add_rms_norm_backward", "add_adapters",
               "add_adapters_workspace_bytes"):
     _native.bind(_name, ctypes.cast(getattr(binding.lib, "equarx_" + _name), ctypes.c_void_p).value)
 
@@ -153,7 +153,7 @@ def fp8_matmul(a, b, dtype=torch.bfloat16):
 
 def fp8_linear(x, w):
     """x w^T: x [tokens, k] in 16 bits is quantized in the call, w is an Fp8Matrix [n, k]."""
-    return _or_raise(_native.linear8(x, w.data, w.rows, w.cols), "equarx_fp8_matmul")
+    return _or_raise(_native.linear8(x, w.data, w.rows, w.cols), "equarx_fp8_linear")
 
 
 def fp8_gated(x, wg, wu, act=ACT_GELU_TANH, dtype=torch.bfloat16):

@@ -50,6 +50,25 @@ def test_products_refuse_bad_arguments():
     assert eq.last_cuda_error() == 0
 
 
+def test_linear_refuses_bad_arguments():
+    need = eq.fp8_linear_workspace_bytes(40, 64)
+    assert need == 512 + 40 * 64 and eq.fp8_linear_workspace_bytes(1, 64) == 0 and eq.fp8_linear_workspace_bytes(40, 0) == 0
+    f = eq.fp8_linear
+    a = dict(x=A, dtype=eq.FP16, ldx=64, w_codes=A + GB, w_scales=A + 2 * GB, m=40, n=8, k=64, out=A + 3 * GB, ld=8, workspace=A + 4 * GB,
+             workspace_bytes=need)
+    for key, off in (("x", 1), ("out", 1), ("w_codes", 8), ("w_scales", 8), ("workspace", 8)):
+        assert status_of(f, **{**a, key: 0}) == binding.ERR_NULL
+        assert status_of(f, **{**a, key: a[key] + off}) == binding.ERR_ALIGN
+    for key, bad in (("n", 0), ("k", 0), ("ld", 7), ("ldx", 63), ("m", GB + 1)):
+        assert status_of(f, **{**a, key: bad}) == binding.ERR_COUNT
+    assert status_of(f, **{**a, "dtype": eq.FP32}) == binding.ERR_FORMAT
+    assert status_of(f, **{**a, "workspace_bytes": need - 1}) == binding.ERR_WORKSPACE
+    for key, bad in (("out", A + 32), ("out", A + GB + 32), ("workspace", A), ("workspace", A + GB), ("workspace", A + 3 * GB)):
+        assert status_of(f, **{**a, key: bad}) == binding.ERR_ALIAS
+    assert status_of(f, **{**a, "m": 0, "x": 0}) == 0
+    assert eq.last_cuda_error() == 0
+
+
 def test_sizes_of_the_buffers():
     assert eq.fp8_codes_bytes(3, 33) == 3 * 64 and eq.fp8_scales_bytes(1, 1) == 512
     assert eq.fp8_scales_bytes(129, 129) == 2 * 2 * 512
@@ -201,6 +220,22 @@ def test_products(m, n, k):
         assert torch.equal(ff.fp8_matmul(xq, wq, dtype), y)
         y32 = ff.fp8_matmul(xq, wq, torch.float32)
         ref.assert_within(y32, value, ref.rounded(value, bound, torch.float32), "matmul, fp32")
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n,k", [(1, 1), (130, 129), (257, 1000), (2688, 128), (1000, 5376), (512, 2697)])
+def test_linear_of_few_tokens(n, k, dtype):
+    """the same bits as two calls, for rows that start anywhere, and with what is not finite"""
+    w = ff.fp8_quantize(normal(n, k, n + k, dtype, k ** -0.5))
+    for m in (1, 2, 3, 5, 7, 8, 9, 16, 17):
+        for shift in (0, 1, 2, 8):
+            store = normal(m, k + shift + 24, m + k, dtype, 1.0)
+            x = store[:, shift:shift + k]
+            x[m // 2, k // 2] = (float("nan"), float("inf"), -0.0, 60000.0)[(m + shift) % 4]
+            got, want = ff.fp8_linear(x, w), ff.fp8_matmul(ff.fp8_quantize(x), w, dtype)
+            assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0))
     ff.check()
 
 
