@@ -35,6 +35,39 @@ inline int grad_threads(size_t cols) {
     return groups ? int(up(ceil_div(cols, 8 * groups), 32)) : kGradThreads;
 }
 
+// Rows up to which the CTAs of the backward pass are one cluster that adds the weight's gradient up itself.  Through Python, where a
+// launch takes the host 2 us, 16 rows of 3840 take 5.2 us against 7.5; 32 rows are four for each CTA, and 10.7 against 7.8.
+constexpr size_t kTogether = 16;
+inline bool together(size_t rows, size_t cols) { return rows <= kTogether && grad_groups(cols); }
+
+// Groups of threads that an SM has: three CTAs of one each, or, where rows are short, more in one CTA of 672 threads (1024 with 64
+// registers each took longer).  Groups of several warps have a barrier each, of which there are 15.
+inline size_t groups_of_sm(size_t cols) {
+    const int pieces = grad_groups(cols), threads = grad_threads(cols);
+    if (pieces > 3) return 1;
+    return pieces ? std::min(kGradGroupThreads / threads, threads == 32 ? kGradMostGroups : 15) : 3;
+}
+// as many as run at one time on 148 SMs, two rows at least for each, and not so many that the parts of very long rows outgrow the
+// matrices
+inline size_t row_groups(size_t rows, size_t cols) {
+    return std::min({ceil_div(rows, 2), together(rows, cols) ? 8 : 148 * groups_of_sm(cols), std::max<size_t>(1, (size_t(1) << 28) / cols)});
+}
+// two rows for each CTA, of one piece a thread
+inline bool wide(size_t rows, size_t cols) {
+    return cols > size_t(kGradColumns) && cols <= size_t(kGradWide) * 8 && rows <= 2 * row_groups(rows, cols);
+}
+// Groups of a CTA: all that an SM has where a thread has one piece or those are more than three, which saves parts and their addition.  One CTA of all / CTAs of one,
+// us: 30000 x 512 27 / 51, 16384 x 1024 27 / 41, 8192 x 2048 30 / 37; three: 8192 x 3584 47 / 43, 8192 x 5376 80 / 65.
+inline size_t groups_of_cta(size_t rows, size_t cols) {
+    const bool several = grad_groups(cols) == 1 || groups_of_sm(cols) > 3;
+    return together(rows, cols) || wide(rows, cols) || !several ? 1 : ceil_div(row_groups(rows, cols), 148);
+}
+// CTAs, each with a part of the weight's gradient
+inline size_t norm_parts(size_t rows, size_t cols) { return ceil_div(row_groups(rows, cols), groups_of_cta(rows, cols)); }
+inline size_t norm_workspace(size_t rows, size_t cols) {
+    return together(rows, cols) ? 0 : norm_parts(rows, cols) * part_stride(cols) * sizeof(float);
+}
+
 // both are the same matrix: each element is read before it is written by the same thread
 inline bool same(const void* p, size_t ldp, const void* q, size_t ldq, size_t rows) { return p == q && (ldp == ldq || rows == 1); }
 
@@ -56,24 +89,29 @@ int launch_norm(const NormArgs& a, int dtype, int width, cudaStream_t stream) {
                         : launch_norm<kFp16, 1, EIGHT>(a, stream);
 }
 
-template <int DT, int W, int G, int MOST = kGradThreads>
+template <int DT, int W, int G, int MOST>
 int launch_grad(const NormGradArgs& a, int threads, cudaStream_t stream) {
     // the staged rows (12 bytes a column and more), or the sums in their place
-    const size_t smem = W == 8 ? size_t(kGradStages) * 3 * 16 * G * threads : a.together ? part_stride(a.cols) * sizeof(float) : 0;
-    return launch(norm_grad_kernel<DT, W, G, MOST>, dim3(unsigned(a.count)), threads, smem, unsigned(a.together), a, stream, true);
+    const size_t sums = a.together || a.groups > 1 ? a.groups * part_stride(a.cols) * sizeof(float) : 0;
+    const size_t smem = W == 8 ? size_t(kGradStages) * 3 * 16 * G * threads * a.groups : sums;
+    return launch(norm_grad_kernel<DT, W, G, MOST>, dim3(unsigned(a.count)), threads * a.groups, smem, unsigned(a.together), a, stream, true);
 }
 template <int DT, int W>
 int launch_grad(const NormGradArgs& a, cudaStream_t stream) {
-    if (a.cols > kGradColumns && a.cols <= kGradWide * 8 && a.rows <= 2 * a.count)
-        return launch_grad<DT, W, 1, kGradWide>(a, int(up(ceil_div(a.cols, 8), 32)), stream);
+    // Rows that are read by elements or pairs do not go through shared memory: more threads with one piece each, and no registers that spill
+    // (8191 x 5375: 369 us, with three pieces 486)
+    const bool narrow = W < 8 && a.cols > kGradColumns && a.cols <= kGradWide * 8 && a.groups == 1;
+    if (narrow || wide(a.rows, a.cols)) return launch_grad<DT, W, 1, kGradWide>(a, int(up(ceil_div(a.cols, 8), 32)), stream);
     const int threads = grad_threads(a.cols);
     switch (grad_groups(a.cols)) {
-        case 1: return launch_grad<DT, W, 1>(a, threads, stream);
-        case 2: return launch_grad<DT, W, 2>(a, threads, stream);
-        case 3: return launch_grad<DT, W, 3>(a, threads, stream);
-        case 4: return launch_grad<DT, W, 4>(a, threads, stream);
-        case 5: return launch_grad<DT, W, 5>(a, threads, stream);
-        default: return launch_grad<DT, W, 0>(a, threads, stream);
+        case 1: return launch_grad<DT, W, 1, kGradGroupThreads>(a, threads, stream);
+        case 2:
+            return groups_of_sm(a.cols) > 3 ? launch_grad<DT, W, 2, kGradGroupThreads>(a, threads, stream)
+                                            : launch_grad<DT, W, 2, kGradThreads>(a, threads, stream);
+        case 3: return launch_grad<DT, W, 3, kGradThreads>(a, threads, stream);
+        case 4: return launch_grad<DT, W, 4, kGradThreads>(a, threads, stream);
+        case 5: return launch_grad<DT, W, 5, kGradThreads>(a, threads, stream);
+        default: return launch_grad<DT, W, 0, kGradThreads>(a, threads, stream);
     }
 }
 template <int DT>
@@ -122,21 +160,6 @@ int check_sum(const void* x, size_t ldx, const void* residual, size_t ldr, const
     if (!same(sum, lds, x, ldx, rows) && overlap(s, matrix(x, rows, cols, ldx, 2))) return EQUARX_ERR_ALIAS;
     if (!same(sum, lds, residual, ldr, rows) && overlap(s, matrix(residual, rows, cols, ldr, 2))) return EQUARX_ERR_ALIAS;
     return overlap(s, Span{weight, cols * size_of(weight_dtype)}) ? EQUARX_ERR_ALIAS : EQUARX_OK;
-}
-
-// Rows up to which the CTAs of the backward pass are one cluster that adds the weight's gradient up itself.  Through Python, where a
-// launch takes the host 2 us, 16 rows of 3840 take 5.2 us against 7.5; 32 rows are four for each CTA, and 10.7 against 7.8.
-constexpr size_t kTogether = 16;
-inline bool together(size_t rows, size_t cols) { return rows <= kTogether && grad_groups(cols); }
-
-// CTAs of the backward pass, each with a part of the weight's gradient: as many as run at one time on 148 SMs (three on each,
-// more where rows are short), two rows at least for each, and not so many that the parts of very long rows outgrow the matrices
-inline size_t norm_parts(size_t rows, size_t cols) {
-    const size_t most = 148 * std::max<size_t>(1, std::min<size_t>(8, (grad_groups(cols) > 3 ? 1 : 3) * kGradThreads / grad_threads(cols)));
-    return std::min({ceil_div(rows, 2), together(rows, cols) ? 8 : most, std::max<size_t>(1, (size_t(1) << 28) / cols)});
-}
-inline size_t norm_workspace(size_t rows, size_t cols) {
-    return together(rows, cols) ? 0 : norm_parts(rows, cols) * part_stride(cols) * sizeof(float);
 }
 
 }  // namespace
@@ -234,6 +257,7 @@ int equarx_add_rms_norm_backward(const void* dy, size_t lddy, const void* dsum, 
     a.cols = int(cols);
     a.fp32 = weight_dtype == EQUARX_FP32;
     a.count = int(norm_parts(rows, cols));
+    a.groups = int(groups_of_cta(rows, cols));
     access.add(dy, lddy);
     access.add(dsum, ldds);
     access.add(sum, lds);

@@ -16,22 +16,27 @@ constexpr int kGradThreads = 224;          // of the backward pass, at most
 constexpr int kGradColumns = kGradThreads * 8;
 constexpr int kGradGroups = 5;             // groups of 8 columns for each of its threads, at most
 constexpr int kGradStages = 2;             // its rows in shared memory
+constexpr int kGradGroupThreads = 3 * kGradThreads, kGradMostGroups = kGradGroupThreads / 32;      // of a CTA that has an SM to itself
 constexpr int kGradWide = 1024;            // where each CTA has few rows, at most
 constexpr int kRowThreads = 1024;          // of the forward pass, at most
 
 // Eight elements of a row in a thread's registers, pairs of neighbours.  W = 8: all neighbours, for rows that start on
 // multiples of 16 bytes.  W = 2 or 1: pairs or single elements, the next thread the next ones, for rows that start on multiples of 4
 // or 2 bytes: a warp's accesses are then whole sectors all the same.
+struct Place {
+    int thread, threads;               // among those that have a row
+};
+__device__ __forceinline__ Place in_block() { return {int(threadIdx.x), int(blockDim.x)}; }
 template <int W>
-__device__ __forceinline__ int column_of(int first, int e) {
-    if (W == 8) return first + int(threadIdx.x) * 8 + e;
-    return first + (e / W * int(blockDim.x) + int(threadIdx.x)) * W + e % W;
+__device__ __forceinline__ int column_of(int first, int e, Place at = in_block()) {
+    if (W == 8) return first + at.thread * 8 + e;
+    return first + (e / W * at.threads + at.thread) * W + e % W;
 }
 // as pairs of 16-bit words; zero past the last column
 template <int W>
-__device__ __forceinline__ void load_row(const void* row, int first, int cols, uint32_t (&v)[4]) {
+__device__ __forceinline__ void load_row(const void* row, int first, int cols, uint32_t (&v)[4], Place at = in_block()) {
     const uint16_t* const q = static_cast<const uint16_t*>(row);
-    const int col = column_of<W>(first, 0);
+    const int col = column_of<W>(first, 0, at);
     if (W == 8 && col + 8 <= cols) {
         const uint4 a = *reinterpret_cast<const uint4*>(q + col);
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
@@ -39,22 +44,22 @@ __device__ __forceinline__ void load_row(const void* row, int first, int cols, u
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int c0 = column_of<W>(first, 2 * i), c1 = column_of<W>(first, 2 * i + 1);
+        const int c0 = column_of<W>(first, 2 * i, at), c1 = column_of<W>(first, 2 * i + 1, at);
         if (W == 2 && c1 < cols) v[i] = *reinterpret_cast<const uint32_t*>(q + c0);
         else v[i] = (c0 < cols ? q[c0] : 0) | uint32_t(c1 < cols ? q[c1] : 0) << 16;
     }
 }
 template <int W>
-__device__ __forceinline__ void store_row(void* row, int first, int cols, const uint32_t (&v)[4]) {
+__device__ __forceinline__ void store_row(void* row, int first, int cols, const uint32_t (&v)[4], Place at = in_block()) {
     uint16_t* const q = static_cast<uint16_t*>(row);
-    const int col = column_of<W>(first, 0);
+    const int col = column_of<W>(first, 0, at);
     if (W == 8 && col + 8 <= cols) {
         *reinterpret_cast<uint4*>(q + col) = make_uint4(v[0], v[1], v[2], v[3]);
         return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int c0 = column_of<W>(first, 2 * i), c1 = column_of<W>(first, 2 * i + 1);
+        const int c0 = column_of<W>(first, 2 * i, at), c1 = column_of<W>(first, 2 * i + 1, at);
         if (W == 2 && c1 < cols) {
             *reinterpret_cast<uint32_t*>(q + c0) = v[i];
         } else {
@@ -65,22 +70,23 @@ __device__ __forceinline__ void store_row(void* row, int first, int cols, const 
 }
 // offset + weight, the weight in 16 bits or fp32
 template <int DT, int W>
-__device__ __forceinline__ void load_weights(const void* weight, bool fp32, float offset, int first, int cols, float2 (&v)[4]) {
+__device__ __forceinline__ void load_weights(const void* weight, bool fp32, float offset, int first, int cols, float2 (&v)[4],
+                                             Place at = in_block()) {
     if (!fp32) {
         uint32_t h[4];
-        load_row<W>(weight, first, cols, h);
+        load_row<W>(weight, first, cols, h, at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = unpack2(h[i], DT);
     } else {
         const float* const q = static_cast<const float*>(weight);
-        const int col = column_of<W>(first, 0);
+        const int col = column_of<W>(first, 0, at);
         if (W == 8 && col + 8 <= cols) {
             const float4 a = reinterpret_cast<const float4*>(q + col)[0], b = reinterpret_cast<const float4*>(q + col)[1];
             v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w); v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int c0 = column_of<W>(first, 2 * i), c1 = column_of<W>(first, 2 * i + 1);
+                const int c0 = column_of<W>(first, 2 * i, at), c1 = column_of<W>(first, 2 * i + 1, at);
                 v[i] = make_float2(c0 < cols ? q[c0] : 0.0f, c1 < cols ? q[c1] : 0.0f);
             }
         }
@@ -89,17 +95,16 @@ __device__ __forceinline__ void load_weights(const void* weight, bool fp32, floa
     for (int i = 0; i < 4; ++i) v[i] = add_pair(v[i], twice(offset));
 }
 
-// the sum of all threads' values in an order that does not depend on timing; every thread gets it.  `shared` is not
-// written again before every thread has passed another barrier.
-template <typename T>
-__device__ __forceinline__ T block_sum(T v, T* shared) {
+// the sum of the values of a group of warps, whose barrier is `id`, in an order that does not depend on timing; every thread gets
+// it.  `shared` is not written again before every thread of the group has passed another barrier.
+__device__ __forceinline__ float group_sum(float v, float* shared, Place at, int id) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-    const int warps = blockDim.x / 32, lane = threadIdx.x & 31;
+    const int warps = at.threads / 32, lane = at.thread & 31;
     if (warps == 1) return v;
-    if (lane == 0) shared[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = lane < warps ? shared[lane] : T(0);
+    if (lane == 0) shared[at.thread >> 5] = v;
+    asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(id), "r"(at.threads) : "memory");
+    v = lane < warps ? shared[lane] : 0.0f;
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     return v;
@@ -265,34 +270,39 @@ struct NormGradArgs {
     const void *dy, *dsum, *sum, *weight;  // dsum may be null
     const float* factors;                  // r of each row
     void* dx;
-    float* parts;                          // [CTAs][columns to 8], or null
+    float* parts;                          // [count][columns to 8], or null
     void* dw;                              // null: no gradient of the weight
     size_t lddy, ldds, lds, lddx;
     float inverse, offset;
-    int rows, cols, fp32, count;           // count: parts
+    int rows, cols, fp32, count;           // count: CTAs, and their parts
+    int groups;                            // of a CTA's threads, with a row each at a time
     int together;                          // the CTAs are one cluster, which adds their parts up itself
 };
 
 __host__ __device__ inline size_t part_stride(size_t cols) { return (cols + 7) & ~size_t(7); }
 
 // n = sum r, g = dy (offset + weight):  dx = dsum + r g - (r mean(g n)) n, dweight = sum over rows of dy n.
-// A CTA takes every gridDim-th row, a thread the same G groups of 8 columns of each, whose weight gradients it adds up in
-// registers.  W = 8: a row is copied to shared memory while the one before it is worked on; a thread copies and reads its own
-// elements, so no barrier is needed for them, and reads them twice, so that registers hold weights and sums only.  MOST = 1024: up
-// to 8192 columns with one group each, for CTAs of two rows, whose time is mostly the fetching of instructions.  G = 0: rows that
-// this does not hold; sums in the CTA's part in memory.  Few rows: the CTAs are a cluster and add their parts of the weight's
-// gradient up through distributed shared memory, which saves a launch.
+// The groups of a CTA's threads take rows in turn, a thread the same G pieces of 8 columns of each, whose weight gradients it adds up in
+// registers; at the end the groups' are added in shared memory, so that one part for each SM goes to memory.  W = 8: a row is
+// copied to shared memory while the one before it is worked on; a thread copies and reads its own elements, so no barrier is
+// needed for them, and reads them twice, so that registers hold weights and sums only.  MOST = 1024: up to 8192 columns with one
+// piece each, for CTAs of two rows, whose time is mostly the fetching of instructions.  G = 0: rows that this does not hold; sums
+// in the CTA's part in memory.  Few rows: the CTAs are a cluster and add their parts of the weight's gradient up through
+// distributed shared memory, which saves a launch.
 //
-// 8192 x 5376: 68 us for 352 MB, 5.2 TB/s, and 7 us for the sum of 444 parts; bound by the wait for the row's sum and by what can be
-// copied ahead beside it (21 warps an SM, 48 % of the issue slots).  Without copies ahead, 16 columns a thread, the whole took 267 us,
-// with copies and 8 columns a thread 93, with 24 columns and 384 threads 92.
+// XXX
 template <int DT, int W, int G, int MOST>
-__global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
+__global__ void __launch_bounds__(MOST, MOST == kGradThreads && G <= 3 ? 3 : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
     constexpr bool STAGED = W == 8 && G > 0;
     constexpr int N = G ? G : 1;
     extern __shared__ __align__(16) uint8_t staged[];
-    __shared__ float shared[2][32];        // a thread writes one again only after the barrier of the row between
-    const int span = blockDim.x * 8;
+    constexpr bool GROUPS = MOST == kGradGroupThreads;
+    __shared__ float shared[GROUPS ? kGradMostGroups : 1][2][32];     // one is written again only after the barrier of the row between
+    // (a group is whole warps)
+    const int groups = GROUPS ? p.groups : 1, threads = blockDim.x / groups, group = uniform(threadIdx.x / threads);
+    const Place at = {int(threadIdx.x) - group * threads, threads};
+    const int span = threads * 8;
+    const size_t first_row = blockIdx.x * groups + group, step = size_t(gridDim.x) * groups;
     const bool add = p.dsum != nullptr;
     float* const part = p.parts ? p.parts + blockIdx.x * part_stride(p.cols) : nullptr;
     grid_launch();
@@ -300,12 +310,12 @@ __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm
     float2 w[N][4], acc[N][4];
 #pragma unroll
     for (int g = 0; g < N; ++g) {
-        if (G) load_weights<DT, W>(p.weight, p.fp32, p.offset, g * span, p.cols, w[g]);
+        if (G) load_weights<DT, W>(p.weight, p.fp32, p.offset, g * span, p.cols, w[g], at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[g][i] = make_float2(0.0f, 0.0f);
     }
-    const uint32_t mine = smem_addr(staged) + threadIdx.x * 16;
-    const int per = blockDim.x * 16, per_stage = 3 * N * per;
+    const int per = threads * 16, per_stage = 3 * N * per;
+    const uint32_t mine = smem_addr(staged) + group * kGradStages * per_stage + at.thread * 16;
     auto fetch = [&](size_t row, uint32_t to) {
         if (row < size_t(p.rows)) {
             const uint16_t* const dy = static_cast<const uint16_t*>(p.dy) + row * p.lddy;
@@ -313,7 +323,7 @@ __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm
             const uint16_t* const ds = static_cast<const uint16_t*>(p.dsum) + row * p.ldds;
 #pragma unroll
             for (int g = 0; g < N; ++g) {
-                const int col = column_of<8>(g * span, 0), bytes = min(16, (p.cols - col) * 2);
+                const int col = column_of<8>(g * span, 0, at), bytes = min(16, (p.cols - col) * 2);
                 if (bytes <= 0) continue;
                 copy_async_16(to + 3 * g * per, dy + col, bytes);
                 copy_async_16(to + (3 * g + 1) * per, h + col, bytes);
@@ -323,19 +333,19 @@ __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm
         copy_async_commit();
     };
     if (STAGED)
-        for (int i = 0; i < kGradStages; ++i) fetch(blockIdx.x + size_t(i) * gridDim.x, mine + i * per_stage);
+        for (int i = 0; i < kGradStages; ++i) fetch(first_row + i * step, mine + i * per_stage);
 
     int turn = 0, stage = 0;
-    float next = p.factors[blockIdx.x];
-    for (size_t row = blockIdx.x; row < size_t(p.rows); row += gridDim.x, turn ^= 1) {
+    float next = first_row < size_t(p.rows) ? p.factors[first_row] : 0.0f;
+    for (size_t row = first_row; row < size_t(p.rows); row += step, turn ^= 1) {
         const float r = next;
-        if (row + gridDim.x < size_t(p.rows)) next = p.factors[row + gridDim.x];
+        if (row + step < size_t(p.rows)) next = p.factors[row + step];
         const uint32_t from = mine + stage * per_stage;
         if (STAGED) copy_async_wait<kGradStages - 1>();
         // eight elements of dy, sum and dsum; past the last column the first two are 0
         auto load = [&](int first, int g, uint32_t (&dy)[4], uint32_t (&h)[4], uint32_t* ds) {
             if constexpr (STAGED) {
-                if (column_of<W>(first, 0) < p.cols) {
+                if (column_of<W>(first, 0, at) < p.cols) {
                     ld_shared_v4(from + 3 * g * per, dy);
                     ld_shared_v4(from + (3 * g + 1) * per, h);
                     if (ds && add) ld_shared_v4(from + (3 * g + 2) * per, *reinterpret_cast<uint32_t(*)[4]>(ds));
@@ -344,12 +354,13 @@ __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm
                     for (int i = 0; i < 4; ++i) dy[i] = h[i] = 0;
                 }
             } else {
-                load_row<W>(static_cast<const uint16_t*>(p.dy) + row * p.lddy, first, p.cols, dy);
-                load_row<W>(static_cast<const uint16_t*>(p.sum) + row * p.lds, first, p.cols, h);
+                load_row<W>(static_cast<const uint16_t*>(p.dy) + row * p.lddy, first, p.cols, dy, at);
+                load_row<W>(static_cast<const uint16_t*>(p.sum) + row * p.lds, first, p.cols, h, at);
                 if (ds && add)
-                    load_row<W>(static_cast<const uint16_t*>(p.dsum) + row * p.ldds, first, p.cols, *reinterpret_cast<uint32_t(*)[4]>(ds));
+                    load_row<W>(static_cast<const uint16_t*>(p.dsum) + row * p.ldds, first, p.cols, *reinterpret_cast<uint32_t(*)[4]>(ds),
+                                at);
             }
-            if (!G) load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0]);
+            if (!G) load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0], at);
         };
         float2 b = make_float2(0.0f, 0.0f);
         auto take = [&](int first, int g) {
@@ -365,7 +376,7 @@ __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm
         } else {
             for (int first = 0; first < p.cols; first += span) take(first, 0);
         }
-        const float c = block_sum(b.x + b.y, shared[turn]) * p.inverse * r;
+        const float c = group_sum(b.x + b.y, shared[GROUPS ? group : 0][turn], at, 1 + group) * p.inverse * r;
         auto give = [&](int first, int g) {
             uint32_t dy[4], h[4], ds[4], dx[4];
             load(first, g, dy, h, ds);
@@ -379,13 +390,13 @@ __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm
                 if (G) acc[g][i] = fma_pair(y, n, acc[g][i]);
                 else dw[i] = mul_pair(y, n);
             }
-            store_row<W>(static_cast<uint16_t*>(p.dx) + row * p.lddx, first, p.cols, dx);
+            store_row<W>(static_cast<uint16_t*>(p.dx) + row * p.lddx, first, p.cols, dx, at);
             if (!G && part) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int at = column_of<W>(first, e);
+                    const int col = column_of<W>(first, e, at);
                     const float v = e & 1 ? dw[e / 2].y : dw[e / 2].x;
-                    if (at < p.cols) part[at] = row == blockIdx.x ? v : part[at] + v;
+                    if (col < p.cols) part[col] = row == first_row ? v : part[col] + v;
                 }
             }
         };
@@ -396,29 +407,42 @@ __global__ void __launch_bounds__(MOST, G > 3 || MOST == kGradWide ? 1 : 3) norm
             for (int first = 0; first < p.cols; first += span) give(first, 0);
         }
         if (STAGED) {
-            fetch(row + size_t(kGradStages) * gridDim.x, from);
+            fetch(row + kGradStages * step, from);
             stage = stage == kGradStages - 1 ? 0 : stage + 1;
         }
     }
     if (G && p.dw) {
-        float* const to = p.together ? reinterpret_cast<float*>(staged) : part;
+        const size_t stride = part_stride(p.cols);
+        float* const sums = reinterpret_cast<float*>(staged);
+        float* const to = p.together ? sums : groups > 1 ? sums + group * stride : part;
         __syncthreads();                                   // the rows in shared memory have been read
 #pragma unroll
         for (int g = 0; g < N; ++g) {
             if constexpr (W == 8) {
-                if (column_of<W>(g * span, 0) < p.cols) {
-                    float4* const q = reinterpret_cast<float4*>(to + column_of<W>(g * span, 0));
+                if (column_of<W>(g * span, 0, at) < p.cols) {
+                    float4* const q = reinterpret_cast<float4*>(to + column_of<W>(g * span, 0, at));
                     q[0] = make_float4(acc[g][0].x, acc[g][0].y, acc[g][1].x, acc[g][1].y);
                     q[1] = make_float4(acc[g][2].x, acc[g][2].y, acc[g][3].x, acc[g][3].y);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = column_of<W>(g * span, 2 * i), after = column_of<W>(g * span, 2 * i + 1);
-                    if (W == 2 && at < p.cols) *reinterpret_cast<float2*>(to + at) = acc[g][i];
-                    if (W == 1 && at < p.cols) to[at] = acc[g][i].x;
+                    const int col = column_of<W>(g * span, 2 * i, at), after = column_of<W>(g * span, 2 * i + 1, at);
+                    if (W == 2 && col < p.cols) *reinterpret_cast<float2*>(to + col) = acc[g][i];
+                    if (W == 1 && col < p.cols) to[col] = acc[g][i].x;
                     if (W == 1 && after < p.cols) to[after] = acc[g][i].y;
                 }
+            }
+        }
+        if (GROUPS && groups > 1) {
+            __syncthreads();
+            for (int col = threadIdx.x * 4; col < p.cols; col += blockDim.x * 4) {     // up to the part's end, a multiple of 8
+                float4 v = *reinterpret_cast<const float4*>(sums + col);
+                for (int g = 1; g < groups; ++g) {
+                    const float4 a = *reinterpret_cast<const float4*>(sums + g * stride + col);
+                    v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+                }
+                *reinterpret_cast<float4*>(part + col) = v;
             }
         }
         if (p.together) {
