@@ -42,6 +42,21 @@ __device__ __forceinline__ void load_row(const void* row, int first, int cols, u
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
         return;
     }
+    if (W < 8 && column_of<W>(first, 7, at) < cols) {      // one test for all, so that the loads go out together
+        uint16_t h[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            if (W == 2) {
+                v[e / 2] = *reinterpret_cast<const uint32_t*>(q + column_of<W>(first, e, at));
+            } else {
+                h[e] = q[column_of<W>(first, e, at)];
+                h[e + 1] = q[column_of<W>(first, e + 1, at)];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4 && W == 1; ++i) v[i] = h[2 * i] | uint32_t(h[2 * i + 1]) << 16;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int c0 = column_of<W>(first, 2 * i, at), c1 = column_of<W>(first, 2 * i + 1, at);
@@ -55,6 +70,18 @@ __device__ __forceinline__ void store_row(void* row, int first, int cols, const 
     const int col = column_of<W>(first, 0, at);
     if (W == 8 && col + 8 <= cols) {
         *reinterpret_cast<uint4*>(q + col) = make_uint4(v[0], v[1], v[2], v[3]);
+        return;
+    }
+    if (W < 8 && column_of<W>(first, 7, at) < cols) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            if (W == 2) {
+                *reinterpret_cast<uint32_t*>(q + column_of<W>(first, e, at)) = v[e / 2];
+            } else {
+                q[column_of<W>(first, e, at)] = uint16_t(v[e / 2]);
+                q[column_of<W>(first, e + 1, at)] = uint16_t(v[e / 2] >> 16);
+            }
+        }
         return;
     }
 #pragma unroll
@@ -83,6 +110,9 @@ __device__ __forceinline__ void load_weights(const void* weight, bool fp32, floa
         if (W == 8 && col + 8 <= cols) {
             const float4 a = reinterpret_cast<const float4*>(q + col)[0], b = reinterpret_cast<const float4*>(q + col)[1];
             v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w); v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
+        } else if (W < 8 && column_of<W>(first, 7, at) < cols) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = make_float2(q[column_of<W>(first, 2 * i, at)], q[column_of<W>(first, 2 * i + 1, at)]);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
