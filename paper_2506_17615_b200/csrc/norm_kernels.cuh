@@ -323,7 +323,7 @@ __host__ __device__ inline size_t part_stride(size_t cols) { return (cols + 7) &
 // XXX
 template <int DT, int W, int G, int MOST>
 __global__ void __launch_bounds__(MOST, MOST == kGradThreads && G <= 3 ? 3 : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs p) {
-    constexpr bool STAGED = W == 8 && G > 0;
+    constexpr bool STAGED = W == 8 && G > 0, HELD = W < 8 && G == 1;      // HELD: in registers from one use to the next
     constexpr int N = G ? G : 1;
     extern __shared__ __align__(16) uint8_t staged[];
     constexpr bool GROUPS = MOST == kGradGroupThreads;
@@ -393,9 +393,16 @@ __global__ void __launch_bounds__(MOST, MOST == kGradThreads && G <= 3 ? 3 : 1) 
             if (!G) load_weights<DT, W>(p.weight, p.fp32, p.offset, first, p.cols, w[0], at);
         };
         float2 b = make_float2(0.0f, 0.0f);
+        uint32_t held[3][4];
+        if (HELD) load(0, 0, held[0], held[1], held[2]);
         auto take = [&](int first, int g) {
             uint32_t dy[4], h[4];
-            load(first, g, dy, h, nullptr);
+            if (!HELD) load(first, g, dy, h, nullptr);
+#pragma unroll
+            for (int i = 0; i < 4 && HELD; ++i) {
+                dy[i] = held[0][i];
+                h[i] = held[1][i];
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 b = fma_pair(mul_pair(unpack2(dy[i], DT), w[g][i]), mul_pair(unpack2(h[i], DT), twice(r)), b);
@@ -409,7 +416,13 @@ __global__ void __launch_bounds__(MOST, MOST == kGradThreads && G <= 3 ? 3 : 1) 
         const float c = group_sum(b.x + b.y, shared[GROUPS ? group : 0][turn], at, 1 + group) * p.inverse * r;
         auto give = [&](int first, int g) {
             uint32_t dy[4], h[4], ds[4], dx[4];
-            load(first, g, dy, h, ds);
+            if (!HELD) load(first, g, dy, h, ds);
+#pragma unroll
+            for (int i = 0; i < 4 && HELD; ++i) {
+                dy[i] = held[0][i];
+                h[i] = held[1][i];
+                ds[i] = held[2][i];
+            }
             float2 dw[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
