@@ -244,6 +244,33 @@ def test_gradients(dtype, rows, cols, pad):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,shift", [(9001, 256, 0), (2999, 40, 1), (7000, 33, 0), (1777, 848, 0), (1301, 1792, 0), (1201, 1250, 2), (1999, 2048, 0),
+                                             (1500, 2048, 1), (1333, 3584, 0), (1000, 3581, 0), (1200, 5374, 0), (1000, 5375, 0), (600, 8191, 0),
+                                             (600, 8192, 2), (300, 8200, 0)])
+def test_gradients_of_many_rows(dtype, rows, cols, shift):
+    """several rows at a time in a CTA, and rows that are read by pairs or elements, within their memory; dx does not ask for dweight"""
+    code, stream = eq.BF16 if dtype == torch.bfloat16 else eq.FP16, torch.cuda.current_stream().cuda_stream
+    x, residual, w = inputs(rows, cols, rows + cols, dtype, dtype, 0.0)
+    dy, dsum = normal(rows, cols + 8, 7, dtype)[:, shift:shift + cols], normal(rows, cols, 8, dtype)
+    _, s, factors = norm.add_rms_norm(x, residual, w, save=True)
+    nb = eq.add_rms_norm_backward_workspace_bytes(rows, cols)
+    store, ws = torch.full((rows * cols + 16,), -77.0, device="cuda", dtype=dtype), torch.full((nb + 512,), 77, device="cuda", dtype=torch.uint8)
+    dx, dw = store[8:8 + rows * cols].view(rows, cols), torch.full((cols + 16,), -77.0, device="cuda", dtype=dtype)
+    for extra in (dsum, None):
+        eq.add_rms_norm_backward(dy, cols + 8, extra, cols, s, cols, factors, w, code, code, rows, cols, 0.0, dx, cols, dw[8:], ws[256:], nb,
+                                 stream)
+        (vx, ex), (vw, ew) = gradients(dy, extra, s, w, 1e-6, 0.0)
+        ref.assert_within(dx, vx, ref.rounded(vx, ex, dtype), "dx")
+        ref.assert_within(dw[8:8 + cols], vw, ref.rounded(vw, ew, dtype), "dw")
+        bits = dx.clone()
+        eq.add_rms_norm_backward(dy, cols + 8, extra, cols, s, cols, factors, w, code, code, rows, cols, 0.0, dx, cols, 0, 0, 0, stream)
+        assert torch.equal(dx, bits)
+    for t, n, fill in ((store, 8, -77.0), (dw, 8, -77.0), (ws, 256, 77)):
+        assert bool((t[:n] == fill).all()) and bool((t[-n:] == fill).all())
+
+
+@gpu
 @pytest.mark.parametrize("rows,cols", [(4, 40), (60, 300)])
 def test_gradients_against_differences(rows, cols):
     """<gradient, v> against a central difference of the 64-bit formula along v; the difference's own error is O(step^2)"""
