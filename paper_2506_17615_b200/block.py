@@ -192,7 +192,7 @@ def main(argv=None):
         "ranks": a.ranks, "tokens": a.tokens, "hidden": a.hidden, "width": a.width, "format": a.format,
         "serve_rel_error": round(rel(y, y_ref), 4), "train_dx_rel_error": round(rel(dx, dx_ref), 4),
         "serve_layer_rel_error": round(rel(out, out_ref), 4), "train_layer_rel_error": round(rel(dstream, dstream_ref), 4),
-        "us": {"partials_4bit_all_ranks": round(device_us(lambda: block.partials(x), a.steps), 1),
+        "us": {f"partials_{8 if block.eight else 4}bit_all_ranks": round(device_us(lambda: block.partials(x), a.steps), 1),
                "allreduce": round(device_us(lambda: block.allreduce(parts), a.steps), 1),
                "train_all_ranks": round(device_us(lambda: block.train(x, dy), a.steps), 1),
                "serve_layer": round(device_us(lambda: block.serve_layer(x, residual, index), a.steps), 1),
