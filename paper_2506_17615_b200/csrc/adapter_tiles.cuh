@@ -12,7 +12,9 @@
 // 8192 tokens, 2688 -> 5376, rank 64: 45 us for one request, 48 for 7, 4.9 and 4.6 TB/s (rank 16: 44).  Bound by DRAM in the second part,
 // about 31 us of it, and by the chain of start, first part and exchange before.  Two launches with S in memory took 57 and read y
 // only in the second; one group of output warps 57; x read once for each adapter of a tile 51; stores by a warp of their own 54; blocks of
-// a cluster's CTAs side by side in a row made no difference.  Of 128 ranks, which leave room for two blocks of y, 69.
+// a cluster's CTAs side by side in a row made no difference.  Results held in registers until all adapters of a tile are done, so that y
+// is written once: 54, and 512 tokens of 16 requests mixed, rank 16, 31 instead of 35; a form for each 55 and 41, for want of registers.
+// Of 128 ranks, which leave room for two blocks of y, 69.
 #pragma once
 #include "adapter_kernels.cuh"
 
