@@ -87,8 +87,11 @@ template <int RT> struct TileRoom {
     static_assert(RT == 8 || (X + PIPE * STAGE <= PARTS && PARTS + PART <= END));
     static_assert(RT != 8 || (B + B_RING * B_BYTES <= END && PARTS + PART <= X));
 };
-// (a CTA that asks for tensor memory after the launch before it must not meet one of tile_kernel, which asks earlier)
-static_assert(TileRoom<1>::BYTES > 128 * 1024 && TileRoom<2>::BYTES > 128 * 1024);
+// A CTA here waits for its cluster while it has tensor memory, and asks for it after the launch before, where a CTA of tile_kernel asks
+// earlier.  So that none of them waits in a circle, no other CTA that wants tensor memory, 24 KB of shared memory at least, fits on
+// the same SM of 228 KB.
+template <int RT> constexpr bool kAlone = TileRoom<RT>::BYTES + 24 * 1024 > 228 * 1024;
+static_assert(kAlone<1> && kAlone<2> && kAlone<4> && kAlone<8>);
 static_assert(TileRoom<1>::BYTES + 2048 <= 227 * 1024 && TileRoom<2>::BYTES + 2048 <= 227 * 1024 && TileRoom<4>::BYTES + 2048 <= 227 * 1024 &&
               TileRoom<8>::BYTES + 2048 <= 227 * 1024);
 

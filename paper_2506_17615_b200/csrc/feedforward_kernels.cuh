@@ -1268,6 +1268,7 @@ constexpr int kLeastSplitSmem = split_stage_bytes<kHalf, kPlain>(16) + split_par
 static_assert(split_stage_bytes<kMx, kPlain>(16) >= split_stage_bytes<kHalf, kPlain>(16) &&
               split_stage_bytes<kMx8, kPlain>(16) >= split_stage_bytes<kHalf, kPlain>(16) &&
               split_part_bytes<kPlain>(16, 8) >= split_part_bytes<kPlain>(16, 1));
+static_assert(kLeastSplitSmem >= 24 * 1024);       // what the adapters' kernel counts on
 static_assert(kTileSmem<kHalf> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
               kTileSmem<kMx> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
               kTileSmem<kNv> + kLeastSplitSmem + 2 * kSmemOfCta > kSmemOfSm &&
