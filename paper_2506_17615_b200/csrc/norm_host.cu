@@ -41,10 +41,12 @@ constexpr size_t kTogether = 16;
 inline bool together(size_t rows, size_t cols) { return rows <= kTogether && grad_groups(cols); }
 
 // Groups of threads that an SM has: three CTAs of one each, or, where rows are short, more in one CTA of 672 threads (1024 with 64
-// registers each took longer).  Groups of several warps have a barrier each, of which there are 15.
+// registers each took longer).  Groups of several warps have a barrier each, of which there are 15.  Three pieces a thread are for CTAs
+// of one group, three an SM: their kernel takes no more threads than one group has (four an SM: 8192 x 3840 65 us, three 57).
 inline size_t groups_of_sm(size_t cols) {
     const int pieces = grad_groups(cols), threads = grad_threads(cols);
     if (pieces > 3) return 1;
+    if (pieces == 3) return 3;
     return pieces ? std::min(kGradGroupThreads / threads, threads == 32 ? kGradMostGroups : 15) : 3;
 }
 // as many as run at one time on 148 SMs, two rows at least for each, and not so many that the parts of very long rows outgrow the

@@ -271,6 +271,23 @@ def test_gradients_of_many_rows(dtype, rows, cols, shift):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", [(1185, 3840, 0), (8192, 3840, 0), (1200, 3585, 0), (1700, 3592, 8), (2000, 3714, 2), (1500, 3839, 1),
+                                           (1185, 3841, 0), (1185, 3584, 0), (1185, 2688, 0), (1185, 2689, 0), (1184, 3840, 0), (888, 3840, 0), (889, 3840, 0)])
+def test_gradients_of_long_batches(dtype, rows, cols, pad):
+    """sizes at whose borders the form of the launch changes: how many groups an SM has, and whether one CTA has them all"""
+    x, residual, w = inputs(rows, cols, rows + cols, dtype, dtype, 1.0, pad)
+    dy, dsum = normal(rows, cols, 7, dtype, 1.0, pad), normal(rows, cols, 8, dtype)
+    _, s, factors = norm.add_rms_norm(x, residual, w, 1e-6, 1.0, save=True)
+    got = norm.add_rms_norm_backward(dy, dsum, s, factors, w, 1.0)
+    (dx, ex), (dw, ew) = gradients(dy, dsum, s, w, 1e-6, 1.0)
+    ref.assert_within(got[0], dx, ref.rounded(dx, ex, dtype), "dx")
+    ref.assert_within(got[1], dw, ref.rounded(dw, ew, dtype), "dw")
+    again = norm.add_rms_norm_backward(dy, dsum, s, factors, w, 1.0)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1]), "not deterministic"
+
+
+@gpu
 @pytest.mark.parametrize("rows,cols", [(4, 40), (60, 300)])
 def test_gradients_against_differences(rows, cols):
     """<gradient, v> against a central difference of the 64-bit formula along v; the difference's own error is O(step^2)"""
