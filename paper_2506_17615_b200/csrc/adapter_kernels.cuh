@@ -350,6 +350,7 @@ __global__ void __launch_bounds__(kAdapterThreads, 2) adapter_down_kernel(const 
             if (r >= R) continue;
             const uint32_t from = smem_addr(sums + token * R + r);
             for (int q = 0; q < p.ctas; ++q) v[j] += ld_cluster_f32(peer_addr(from, q));
+            if (r >= p.rank) v[j] = 0.0f;            // zeros times x are NaN where x is infinite
         }
         store_sums<DT, R>(p, first + token, i, v);
     }

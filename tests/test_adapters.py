@@ -164,6 +164,31 @@ def test_products_beyond_the_range_of_fp16(large, tokens, n):
     check(out, y * 0, x, a, b, index, None)
 
 
+# a cluster for each token, tiles of rows that TMA reads, tiles of others
+FORMS = [(4, 136, 72), (3000, 1360, 640), (3000, 1001, 777)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rank", [1, 5, 8, 33, 72, 100])
+@pytest.mark.parametrize("tokens,n,k", FORMS)
+def test_infinite_values_in_adapters_whose_ranks_are_padded(dtype, rank, tokens, n, k):
+    """what fills the ranks up multiplies no infinity: with positive adapters an infinite element of x gives the definition's infinities,
+    and no NaN"""
+    y, x, a, b, _ = inputs(tokens, n, k, rank, 3, 1, dtype)
+    a, b = a.abs() + 0.01, b.abs() + 0.01
+    assert (eq.add_adapters_workspace_bytes(tokens, n, k, rank, 3) > 0) == (tokens > 1000)
+    index = (torch.arange(tokens) % 4 - 1).int().cuda()
+    clean = ad.add_adapters(y, x, a, b, index)
+    for sign in (1.0, -1.0):
+        x2 = x.clone()
+        x2[2, 9] = sign * float("inf")
+        out = ad.add_adapters(y, x2, a, b, index)
+        assert bool((out[2] == sign * float("inf")).all())
+        keep = torch.arange(tokens, device="cuda") != 2
+        assert torch.equal(out[keep], clean[keep])
+
+
 @gpu
 @pytest.mark.parametrize("offset", [1, 2, 4, 8])
 @pytest.mark.parametrize("tokens", [3, 150, 50001])
