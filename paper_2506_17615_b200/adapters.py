@@ -14,5 +14,6 @@ def add_adapters(y, x, a, b, index, scale=None, out=None):
     """y[t] + scale[i] (x[t] a[i]^T) b[i]^T with i = index[t], and y[t] where index[t] is no adapter (negative, say).
 
     y [tokens, n] and x [tokens, k], both bfloat16 or both float16; a [adapters, rank, k] and b [adapters, n, rank], dense, rank
-    at most 128; index int32 [tokens]; scale float32 [adapters], None: 1.  out may be y."""
+    at most 128; index int32 [tokens]; scale float32 [adapters], None: 1.  out may be y; writing to it advances its version, as torch's own
+    calls in place do."""
     return _or_raise(_native.add_adapters(y, x, a, b, index, scale, out), "equarx_add_adapters")

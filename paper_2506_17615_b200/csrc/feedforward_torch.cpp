@@ -11,6 +11,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/AutogradState.h>
+#include <c10/core/InferenceMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -596,12 +597,15 @@ PyObject* add_adapters(PyObject*, PyObject* const* args, Py_ssize_t count) {
     const at::Tensor out = args[6] == Py_None ? empty(m, n, y.t.scalar_type(), device) : tensor(args[6], "out");
     const Matrix o = matrix(out, "out", m, n, y.t);
     no_gradient(out, "out", calls);
+    TORCH_CHECK(!out.is_inference() || c10::InferenceMode::is_enabled(), "out is an inference tensor: it is written in inference mode only");
     const size_t need = entry.add_adapters_workspace_bytes(m, n, k, rank, adapters);
     const at::Tensor ws = bytes(need, device);
     const int status = call(device, [&](equarx_stream_t s) {
         return entry.add_adapters(y.p, y.ld, x.p, x.ld, ta.data_ptr(), tb.data_ptr(), static_cast<const int32_t*>(index.p), scale, dtype, m,
                                   n, k, rank, adapters, o.p, o.ld, address(ws), need, s);
     });
+    // what autograd has saved of a caller's tensor is not what it was, whatever the gradient mode is now
+    if (!status && args[6] != Py_None) out.unsafeGetTensorImpl()->bump_version();
     return result(status, out);
     END_HANDLE_TH_ERRORS
 }

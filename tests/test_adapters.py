@@ -190,6 +190,39 @@ def test_infinite_values_in_adapters_whose_ranks_are_padded(dtype, rank, tokens,
 
 
 @gpu
+def test_a_result_in_place_is_one_to_torch():
+    """writing into a tensor advances its version: what an operation has saved of it is not used afterwards"""
+    dtype = torch.bfloat16
+    y, x, a, b, scale = inputs(6, 96, 64, 16, 5, 1, dtype)
+    index = patterns(6, 5, 3)[0]
+    w = torch.ones(96, dtype=dtype, device="cuda").requires_grad_()
+    for target in (y, y.clone().requires_grad_()):
+        z = (target * w).sum()
+        before = target._version
+        with torch.no_grad():
+            assert ad.add_adapters(target, x, a, b, index, scale, out=target) is target
+        assert target._version == before + 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            z.backward()
+    # a view's version is its base's, and nothing else's is touched
+    base = torch.empty(6, 192, dtype=dtype, device="cuda")
+    versions = base._version, y._version, x._version
+    out = ad.add_adapters(y, x, a, b, index, scale, out=base[:, 96:])
+    assert (base._version, y._version, x._version) == (versions[0] + 1, *versions[1:]) and out._version == base._version
+    before = base._version
+    ad.add_adapters(y, x, a, b, index, scale)
+    with pytest.raises(eq.EquarxError):
+        ad.add_adapters(base[:, :96], x, a, b, index, scale, out=base[:, 8:104])
+    assert base._version == before                                   # nothing has been written
+    # tensors of inference mode have no version, and torch's rule for them holds
+    with torch.inference_mode():
+        t = torch.zeros(6, 96, dtype=dtype, device="cuda")
+        assert torch.equal(ad.add_adapters(y, x, a, b, index, scale, out=t), ad.add_adapters(y, x, a, b, index, scale))
+    with pytest.raises(RuntimeError, match="inference"):
+        ad.add_adapters(y, x, a, b, index, scale, out=t)
+
+
+@gpu
 @pytest.mark.parametrize("offset", [1, 2, 4, 8])
 @pytest.mark.parametrize("tokens", [3, 150, 50001])
 def test_views_that_start_anywhere(tokens, offset):
