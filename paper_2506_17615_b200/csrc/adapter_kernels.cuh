@@ -189,14 +189,19 @@ __device__ __forceinline__ uint32_t first_of_each(int d) {
 
 // fp16: what a token's S is multiplied by, so that its largest finite magnitude goes to [2^14, 2^15), and what by afterwards
 __device__ __forceinline__ void range_of(float top, float& times, float& back) {
-    const int e = top > 0.0f ? min(max(int(__float_as_uint(top) >> 23) - 127 - 14, -100), 100) : 0;
+    const int e = top > 0.0f ? max(int(__float_as_uint(top) >> 23) - 127 - 14, -100) : 0;       // up to 113
     times = __uint_as_float(uint32_t(127 - e) << 23);
     back = __uint_as_float(uint32_t(127 + e) << 23);
 }
-// two values as high and low halves; nothing is left of what is not finite
+// Two values as high and low halves; nothing is left of what is not finite.  bf16: fp32 ends a little later, and what would be rounded
+// to infinity has the largest finite number as its high half (fp16: 2^15 is inside the range).
 template <int DT>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t& high, uint32_t& low) {
     high = pack2(a, b, DT);
+    if constexpr (DT == kBf16) {
+        if ((high & 0x7FFFu) == 0x7F80u && fabsf(a) < __uint_as_float(kInfBits)) high -= 1;
+        if ((high & 0x7FFF0000u) == 0x7F800000u && fabsf(b) < __uint_as_float(kInfBits)) high -= 0x10000u;
+    }
     const float2 h = unpack2(high, DT);
     low = pack2(fabsf(a) < __uint_as_float(kInfBits) ? a - h.x : 0.0f, fabsf(b) < __uint_as_float(kInfBits) ? b - h.y : 0.0f, DT);
 }

@@ -190,6 +190,32 @@ def test_infinite_values_in_adapters_whose_ranks_are_padded(dtype, rank, tokens,
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,n,k", FORMS)
+def test_sums_at_the_end_of_the_range_of_fp32(dtype, tokens, n, k):
+    """a finite S that the 16-bit type's range does not hold, or only after a large power of two: S is the scale itself, and what B
+    multiplies it with is 0 or brings it back.  2^-17 of S holds here too: below fp32's end at most 2^-8 of S is left beside the type's
+    largest number, and that rounds to 8 bits."""
+    top = 3.4e38 if dtype == torch.bfloat16 else 2.0 ** 127
+    y, _, _, _, _ = inputs(tokens, n, k, 8, 1, 1, dtype)
+    x, a, b = (torch.zeros(s, dtype=dtype, device="cuda") for s in ((tokens, k), (2, 8, k), (2, n, 8)))
+    x[:, 0], a[:, 0, 0] = 1.0, 1.0
+    small = 2.0 ** -100 if dtype == torch.bfloat16 else 2.0 ** -24
+    b[:, 1::2, 0] = small                                            # every other feature
+    scale = torch.tensor([top, -top], device="cuda")
+    index = (torch.arange(tokens) % 3 - 1).int().cuda()
+    out = ad.add_adapters(y, x, a, b, index, scale)
+    c = torch.where(index < 0, 0.0, scale[index.clamp(min=0).long()]).double()
+    part = c[:, None] * b[0, :, 0].double()[None, :]
+    want = y.double() + part
+    if dtype == torch.float16:                                       # beyond it, or nothing
+        assert torch.equal(out, want.to(dtype))
+    else:
+        ref.assert_within(out, want, ref.rounded(want, (2.0 ** -17 + 2.0 ** -23) * part.abs() + 2.0 ** -23 * want.abs(), dtype), "out")
+    assert torch.equal(out[:, 0::2], y[:, 0::2]) and torch.equal(out[index < 0], y[index < 0])
+
+
+@gpu
 def test_a_result_in_place_is_one_to_torch():
     """writing into a tensor advances its version: what an operation has saved of it is not used afterwards"""
     dtype = torch.bfloat16
