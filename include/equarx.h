@@ -675,7 +675,8 @@ int equarx_add_adapters(const void *y, size_t ldy, const void *x, size_t ldx,
  * incomplete.  This call synchronises the current device and returns
  * EQUARX_ERR_TIMEOUT if that has happened on it since the last check, else EQUARX_OK.
  * For tests, EQUARX_INJECT_TIMEOUT=<polls> in the environment makes it run a kernel
- * first whose wait runs out after so many polls.
+ * first whose wait runs out after so many polls, and EQUARX_INJECT_TIMEOUT_ADAPTERS=<polls>
+ * one whose wait counts as one of equarx_add_adapters.
  */
 int equarx_feedforward_check(void);
 

@@ -102,6 +102,10 @@ int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
 }  // namespace
 
 namespace equarx {
+cudaError_t adapters_give_up(uint32_t polls) {
+    tc::give_up_kernel<tc::kAdapterWaits><<<1, 64>>>(polls);
+    return cudaGetLastError();
+}
 cudaError_t adapters_gave_up(uint32_t& seen) {
     const uint32_t zero = 0;
     cudaError_t e = cudaMemcpyFromSymbol(&seen, tc::g_gave_up, sizeof(seen));

@@ -842,10 +842,16 @@ int equarx_gated_backward(const void* dh, size_t lddh, const void* x, size_t ldx
 int equarx_feedforward_check(void) {
     uint32_t seen = 0;
     cudaError_t e = cudaSuccess;
-    if (const char* polls = std::getenv("EQUARX_INJECT_TIMEOUT")) {
-        give_up_kernel<<<1, 64>>>(uint32_t(std::min(std::max(std::atoi(polls), 1), int(tc::kWaitLimit))));
+    auto asked = [](const char* name) -> uint32_t {
+        const char* const polls = std::getenv(name);
+        return polls ? uint32_t(std::min(std::max(std::atoi(polls), 1), int(tc::kWaitLimit))) : 0;
+    };
+    if (const uint32_t polls = asked("EQUARX_INJECT_TIMEOUT")) {
+        tc::give_up_kernel<tc::kFeedForwardWaits><<<1, 64>>>(polls);
         e = cudaGetLastError();
     }
+    if (const uint32_t polls = asked("EQUARX_INJECT_TIMEOUT_ADAPTERS"))
+        if (e == cudaSuccess) e = equarx::adapters_give_up(polls);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&seen, tc::g_gave_up, sizeof(seen));
     const uint32_t zero = 0;

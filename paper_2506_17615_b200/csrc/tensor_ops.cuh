@@ -372,5 +372,23 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
                      : "memory");
 }
 
+// ---------------------------------------------------------------- a wait that runs out
+// For tests of what the host is told: one warp waits `polls` times on a barrier on which nobody arrives, and a second
+// one, with the full limit, leaves because the first has given up.  Each source file with waits has a count, and by its number a kernel of
+// this name, of its own.
+enum GiveUpSource { kFeedForwardWaits = 0, kAdapterWaits = 1 };
+template <int SOURCE>
+__global__ void __launch_bounds__(64) give_up_kernel(uint32_t polls) {
+    __shared__ uint64_t bar;
+    __shared__ volatile uint32_t abort;
+    const uint32_t never = smem_addr(&bar);
+    if (threadIdx.x == 0) {
+        barrier_init(never, 1);
+        abort = 0;
+    }
+    __syncthreads();
+    barrier_wait_warp(never, 0, &abort, threadIdx.x < 32 ? polls : kWaitLimit);
+}
+
 }  // namespace tc
 }  // namespace equarx

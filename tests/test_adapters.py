@@ -370,3 +370,23 @@ def test_what_is_refused_on_the_gpu(monkeypatch):
     with pytest.raises(eq.EquarxError) as err:
         ad.add_adapters(y, x, a, b, index)
     assert err.value.status == binding.ERR_CUDA and eq.last_cuda_error() == 719
+
+
+@gpu
+def test_a_wait_of_the_adapters_that_runs_out_is_reported_once(monkeypatch):
+    """their waits have a count of their own, which the check reads too; the context stays usable"""
+    dtype = torch.bfloat16
+    y, x, a, b, scale = inputs(3000, 520, 512, 32, 3, 5, dtype)     # tiles of tokens, whose kernel waits
+    index = patterns(3000, 3, 6)[0]
+    want = ad.add_adapters(y, x, a, b, index, scale)
+    ff.check()
+    for names in (["EQUARX_INJECT_TIMEOUT_ADAPTERS"], ["EQUARX_INJECT_TIMEOUT_ADAPTERS", "EQUARX_INJECT_TIMEOUT"]):
+        for name in names:
+            monkeypatch.setenv(name, "50")                          # 0.2 ms
+        with pytest.raises(eq.EquarxError) as err:
+            ff.check()
+        assert err.value.status == binding.ERR_TIMEOUT
+        for name in names:
+            monkeypatch.delenv(name)
+        ff.check()
+    assert torch.equal(ad.add_adapters(y, x, a, b, index, scale), want)
