@@ -109,9 +109,9 @@ __device__ __forceinline__ void store_staged(const CUtensorMap* map, uint32_t bu
     if (lane == 0) tma_store_2d(map, buf, col0, row0);
 }
 
-// To any other output.  16-bit: neighbouring lanes write a row's neighbouring columns, in units of 8, 4 or
-// 2 bytes as base and row stride allow; each lane writing its own row would touch every sector many times.
-// fp32: each lane writes its own row.
+// To any other output, and the last columns of one whose width is no multiple of 16 bytes.  16-bit: neighbouring lanes write a row's
+// neighbouring columns, in units of 8, 4 or 2 bytes as base and row stride allow; each lane writing its own row would touch every
+// sector many times.  fp32: each lane writes its own row.
 __device__ __forceinline__ void store_direct(const Out& o, uint32_t buf, int row0, int col0, int rows, int cols,
                                              const float (&v)[32]) {
     const uint32_t lane = threadIdx.x & 31;
@@ -184,7 +184,7 @@ __device__ __forceinline__ void scale_columns(float (&v)[32], float row, const f
 // One product: out = a b^T, by tiles of 256 x bn.
 struct Product {
     CUtensorMap a[2], b[2];
-    CUtensorMap store[3];                 // 16-bit outputs with aligned rows: blocks of 32 x 32
+    CUtensorMap store[3];                 // 16-bit outputs with aligned rows: blocks of 32 x 32, inside the columns or ending with them
     Out out[3];                           // gated: h, g, u; two outputs: one each
     int m, n;                             // rows and columns of an output
     int stages;                           // of the reduction axis, in each part
@@ -464,7 +464,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads<KIND>, 
         const uint32_t staging = smem + PIPE * STAGE + warp * 2 * kStageOut;
         auto store = [&](const Product& g, int i, int row0, int col0, float (&v)[32]) {
             if (row0 >= g.m || col0 >= g.n) return;
-            if (g.out[i].unit >= 16 && g.out[i].dtype != kFp32) {
+            // TMA ends a row with a whole piece of 16 bytes, zeros past the last column: there may be another matrix
+            const bool ragged = col0 + 32 > g.n && g.n % 8;
+            if (g.out[i].unit >= 16 && g.out[i].dtype != kFp32 && !ragged) {
                 store_staged(&g.store[i], staging + flip, row0, col0, g.out[i].dtype, v);
                 flip ^= kStageOut;
             } else {

@@ -847,6 +847,65 @@ def test_outputs_side_by_side_in_one_buffer(m, f, k):
     ff.check()
 
 
+def padded(rows, cols, dtype, beside=8):
+    """(buffer, row stride, view): rows that TMA writes, whose last columns fill no 16 bytes, and what lies beside them"""
+    ld = (cols + 7) // 8 * 8 + beside
+    store = torch.full((rows, ld), -77.0, dtype=dtype, device="cuda")
+    return store, ld, store[:, :cols]
+
+
+def assert_beside(store, cols):
+    assert bool((store[:, cols:] == -77.0).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("beside", [0, 8])
+@pytest.mark.parametrize("m,f,k", [(3, 33, 75), (300, 130, 101), (261, 5, 67), (1500, 541, 259), (2100, 1663, 126)])
+def test_what_lies_beside_an_output_stays(dtype, beside, m, f, k):
+    """through the C ABI: the bits of dense outputs, and nothing past an output's last column, whose row goes on to a multiple of 16 bytes"""
+    code, stream = {torch.bfloat16: eq.BF16, torch.float16: eq.FP16}[dtype], torch.cuda.current_stream().cuda_stream
+    x, wg, wu, dh = normal(m, k, 1, dtype), normal(f, k, 2, dtype, 0.1), normal(f, k, 3, dtype, 0.1), normal(m, f, 4, dtype)
+    for fmt in FORMATS:
+        q, w = ff.fp4_quantize(x, fmt), ff.fp4_quantize(wg, fmt)
+        store, ld, view = padded(m, f, dtype, beside)
+        eq.fp4_matmul(q.codes, q.scales, q.row_scales, w.codes, w.scales, w.row_scales, m, f, k, fmt, view, code, ld, stream)
+        assert torch.equal(view, ff.fp4_matmul(q, w, dtype))
+        assert_beside(store, f)
+        nb = eq.fp4_linear_workspace_bytes(m, k, fmt)
+        ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
+        store, ld, view = padded(m, f, dtype, beside)
+        eq.fp4_gated(x, code, k, w.codes, w.scales, w.row_scales, w.codes, w.scales, w.row_scales, m, f, k, fmt, eq.ACT_SILU, view, ld, ws, nb,
+                     stream)
+        assert torch.equal(view, ff.fp4_gated(x, w, w, eq.ACT_SILU))
+        assert_beside(store, f)
+    h, g, u = ff.gated_forward(x, wg, wu, save=True)
+    grads = ff.gated_backward(dh, x, wg, wu, g, u)
+    (sh, ldh, vh), (sg, ldg, vg), (su, _, vu) = (padded(m, f, dtype, beside) for _ in range(3))
+    nb = eq.gated_forward_workspace_bytes(m, f, k, x, k, wg, k, wu, k)
+    ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
+    eq.gated_forward(x, k, wg, k, wu, k, code, m, f, k, eq.ACT_GELU_TANH, vh, ldh, vg, vu, ldg, ws, nb, stream)
+    for store, view, want in ((sh, vh, h), (sg, vg, g), (su, vu, u)):
+        assert torch.equal(view, want)
+        assert_beside(store, f)
+    nb = eq.gated_backward_workspace_bytes(m, f, k, x, k, wg, k, wu, k)
+    ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
+    outs = [padded(rows, k, dtype, beside) for rows in (m, f, f)]
+    (sx, ldx, vx), (swg, ldw, vwg), (swu, _, vwu) = outs
+    eq.gated_backward(dh, f, x, k, wg, k, wu, k, g, u, f, code, m, f, k, eq.ACT_GELU_TANH, vx, ldx, vwg, ldw, vwu, ldw, ws, nb, stream)
+    for (store, _, view), want in zip(outs, grads):
+        assert torch.equal(view, want)
+        assert_beside(store, k)
+    # the matrix that begins right after another's last column
+    row = torch.zeros(m, (2 * f + 7) // 8 * 8, dtype=dtype, device="cuda")
+    at = lambda col: row.data_ptr() + 2 * col
+    nb = eq.gated_forward_workspace_bytes(m, f, k, x, k, wg, k, wu, k)
+    ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
+    eq.gated_forward(x, k, wg, k, wu, k, code, m, f, k, eq.ACT_GELU_TANH, h, f, at(0), at(f), row.shape[1], ws, nb, stream)
+    assert torch.equal(row[:, :f], g) and torch.equal(row[:, f:2 * f], u)
+    ff.check()
+
+
 @gpu
 @pytest.mark.parametrize("offset", [1, 2, 4, 7])
 @pytest.mark.parametrize("m,f,k", [(5, 40, 72), (200, 136, 264)])

@@ -7,7 +7,7 @@ import ff_reference as ref
 import paper_2506_17615_b200 as eq
 from paper_2506_17615_b200 import binding
 from paper_2506_17615_b200 import feedforward as ff
-from test_feedforward import A, ACTS, GB, MANY, SIZES, hard_rows, normal, status_of
+from test_feedforward import A, ACTS, GB, MANY, SIZES, assert_beside, hard_rows, normal, padded, status_of
 
 gpu = pytest.mark.gpu
 CODE = {torch.bfloat16: eq.BF16, torch.float16: eq.FP16, torch.float32: eq.FP32}
@@ -334,4 +334,27 @@ def test_launch_errors_come_back(monkeypatch):
         assert err.value.status == binding.ERR_CUDA and eq.last_cuda_error() == 719
     monkeypatch.delenv("EQUARX_INJECT_LAUNCH_ERROR")
     ff.fp8_linear(x, q)
+    ff.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("beside", [0, 8])
+@pytest.mark.parametrize("m,n,k", [(3, 33, 75), (300, 130, 101), (261, 5, 67), (1500, 541, 259), (2100, 1663, 126)])
+def test_what_lies_beside_an_output_stays(dtype, beside, m, n, k):
+    """through the C ABI: the bits of dense outputs, and nothing past an output's last column, whose row goes on to a multiple of 16 bytes"""
+    stream = torch.cuda.current_stream().cuda_stream
+    x, w = normal(m, k, 1, dtype), ff.fp8_quantize(normal(n, k, 2, dtype, 0.1))
+    q = ff.fp8_quantize(x)
+    nb = eq.fp8_linear_workspace_bytes(m, k)
+    ws = torch.empty(max(nb, 16), dtype=torch.uint8, device="cuda")
+    for call, want in (
+            (lambda v, ld: eq.fp8_matmul(q.codes, q.scales, w.codes, w.scales, m, n, k, v, CODE[dtype], ld, stream), ff.fp8_matmul(q, w, dtype)),
+            (lambda v, ld: eq.fp8_linear(x, CODE[dtype], k, w.codes, w.scales, m, n, k, v, ld, ws, nb, stream), ff.fp8_linear(x, w)),
+            (lambda v, ld: eq.fp8_gated(q.codes, q.scales, w.codes, w.scales, w.codes, w.scales, m, n, k, eq.ACT_SILU, v, CODE[dtype], ld, stream),
+             ff.fp8_gated(q, w, w, eq.ACT_SILU, dtype))):
+        store, ld, view = padded(m, n, dtype, beside)
+        call(view, ld)
+        assert torch.equal(view, want)
+        assert_beside(store, n)
     ff.check()
