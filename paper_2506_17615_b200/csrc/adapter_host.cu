@@ -47,7 +47,7 @@ int launch_tiles(AdapterArgs& a, cudaStream_t stream) {
     TRY(make_map(m.a, a.a, 2, a.k, size_t(a.adapters) * a.rank, size_t(a.k) * 2, 16 * RT));
     TRY(make_map(m.b, a.b, 2, a.rank, size_t(a.adapters) * a.n, size_t(a.rank) * 2, kTileBlock));
     TRY(make_map(m.y, a.y, 2, a.n, a.tokens, a.ldy * 2, kTileTokens));
-    TRY(make_map(m.out, a.out, 2, a.n, a.tokens, a.ldo * 2, 32));
+    TRY(make_map(m.out, a.out, 2, std::max(8, a.n & ~7), a.tokens, a.ldo * 2, 32));      // of less than 8 columns nothing is stored
     int clusters[9];
     TRY(resident_clusters(clusters));
     // Whole waves of clusters.  ns: a cluster's start and the exchange of sums; chunks of x and blocks of y, which take longer where many

@@ -22,7 +22,7 @@ namespace equarx {
 namespace ff {
 
 struct AdapterMaps {
-    CUtensorMap x, a, b, y, out;                // boxes of 64 columns; of 128 rows, a: of 16 RT, out: of 32
+    CUtensorMap x, a, b, y, out;                // boxes of 64 columns; of 128 rows, a: of 16 RT, out: of 32 (columns to a multiple of 8)
     AdapterArgs p;
 };
 constexpr int kTileTokens = 128;
@@ -364,6 +364,7 @@ __global__ void __launch_bounds__(kTileAdapterThreads, 1) adapter_tiles_kernel(c
     } else {
         const int group = warp / kGroupWarps, rows = warp % 4 * 32, row = rows + lane, half = warp / 4 % 2, mine = tile.own[row];
         const float back = DT == kFp16 && mine >= 0 ? factors[row] : 1.0f;
+        const int pieces = p.n & ~7;
         int turn = 0;
         for (int block = group; block < blocks && ok; block += 2) {
             const int slot = block % Y_RING, f = (b0 + block) * kTileBlock;
@@ -403,10 +404,16 @@ __global__ void __launch_bounds__(kTileAdapterThreads, 1) adapter_tiles_kernel(c
                 if (lane == 0) barrier_arrive(drained + 8 * buf);
             }
             if (!ok) break;
+            // TMA writes whole pieces of 16 bytes (it would fill the last one with zeros); a lane writes what is left of its row
+            if (f + half * 64 + 64 > pieces && first + row < p.tokens) {
+                uint16_t* const out = static_cast<uint16_t*>(p.out) + size_t(first + row) * p.ldo;
+                for (int c = max(pieces - f - half * 64, 0); c < min(64, p.n - f - half * 64); ++c)
+                    out[f + half * 64 + c] = uint16_t(ld_shared_u16(y + (((c / 8) ^ (row & 7)) << 4) + c % 8 * 2));
+            }
             fence_async_shared();
             __syncwarp();
             if (lane == 0) {
-                if (first + rows < p.tokens && f + half * 64 < p.n)
+                if (first + rows < p.tokens && f + half * 64 < pieces)
                     tma_store_2d(&m.out, y_at + slot * kYBytes + half * kBoxBytes + rows * 128, f + half * 64, first + rows);
                 tma_store_wait_read<0>();                  // the other group works meanwhile
                 barrier_arrive(y_empty + 8 * slot);

@@ -12,7 +12,7 @@ import paper_2506_17615_b200 as eq
 from paper_2506_17615_b200 import adapters as ad
 from paper_2506_17615_b200 import binding
 from paper_2506_17615_b200 import feedforward as ff
-from test_feedforward import A, GB, normal, status_of
+from test_feedforward import A, GB, assert_beside, normal, padded, status_of
 
 gpu = pytest.mark.gpu
 TYPES = [torch.bfloat16, torch.float16]
@@ -281,6 +281,24 @@ def test_views_that_start_anywhere(tokens, offset):
         assert bool((so == -77.0).all())
         eq.add_adapters(vy, n + extra, vx, k + extra, a, b, index, scale, eq.BF16, tokens, n, k, rank, 3, vy, n + extra, ws, nb, stream)
         assert_same(vy)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("beside", [0, 8])
+@pytest.mark.parametrize("tokens,n,k,rank,count", [(9, 33, 72, 16, 3), (3000, 1001, 640, 64, 2), (2500, 541, 1000, 8, 5), (5000, 5, 648, 16, 3),
+                                                   (3001, 131, 64, 128, 2), (4000, 190, 777, 16, 2), (20001, 63, 136, 32, 9)])
+def test_what_lies_beside_an_output_stays(dtype, beside, tokens, n, k, rank, count):
+    """outputs that are columns of a wider tensor, of a width that fills no 16 bytes, apart from y and in its place"""
+    y, x, a, b, scale = inputs(tokens, n, k, rank, count, 1, dtype)
+    for index in patterns(tokens, count, tokens):
+        store, _, view = padded(tokens, n, dtype, beside)
+        wide, _, same = padded(tokens, n, dtype, beside)
+        same.copy_(y)
+        assert ad.add_adapters(same, x, a, b, index, scale, out=view) is view
+        check(view, y, x, a, b, index, scale)
+        assert torch.equal(ad.add_adapters(same, x, a, b, index, scale, out=same), view)
+        assert_beside(store, n), assert_beside(wide, n)
 
 
 @gpu
