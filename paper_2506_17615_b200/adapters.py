@@ -3,6 +3,9 @@
     y = fp4_linear(x, w)                                 the projection that all requests share
     y = add_adapters(y, x, a, b, index, scale, out=y)    and each token's own adapter
 
+They are added to a projection that exists as a tensor, such as the down projection.  The gated block multiplies gate and up inside
+one kernel and gives out neither before the activation, so adapters of those two do not go through it.
+
 Marshalling only; include/equarx.h has the arithmetic.  A failed call raises EquarxError, tensors that do not fit together
 raise ValueError; there is no CPU path.  For serving: there are no gradients, and tensors that ask for one are refused
 (outside torch.no_grad()).

@@ -21,7 +21,9 @@ inline size_t padded_rank(size_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 3
 //   128 -> 128,   rank 16:  512       3.6 / 7.9 | 5.7 / 19 | 5.8 / 96     2048: 8.8 / 7.7 | 15 / 19 | 15 / 104  8192: 31 / 7.4 | 53 / 20 | 62 / 118
 // A token costs 5 ns and its adapter's bytes at 8 TB/s (the L2 has most).  Tokens have their own clusters where that is 13 us at most, and
 // where there are adapters for every second token at least up to eight times as much: with that many loaded, tokens are likely
-// those of many requests, a batch of single tokens.
+// those of many requests, a batch of single tokens.  That is a guess, wrong both ways (2688 -> 5376, us, this rule / the other form): 512
+// tokens of one request with 256 adapters loaded, rank 64, 66 / 12, rank 16, 22 / 11; 512 tokens of 64 requests mixed, rank 64, 159 / 93 at
+// most (what as many different adapters take), rank 16, 124 / 29 at most.
 inline bool token_form(size_t tokens, size_t n, size_t k, size_t rank, size_t adapters) {
     const double ns = double(tokens) * (5.0 + 2.0 * double(rank) * double(n + k) / 8000.0);
     return ns <= 13e3 || (tokens <= 2 * adapters && ns <= 104e3);
@@ -79,12 +81,12 @@ int launch_adapters(AdapterArgs& a, bool vec, int sms, cudaStream_t stream) {
                       kAdapterThreads, 0, unsigned(a.ctas), a, stream);
     }
     if (a.tiles) return launch_tiles<DT, RT>(a, stream);
-    // two CTAs run on an SM: where there are few tiles, up to eight share one
+    // two CTAs run on an SM (of more than 64 ranks one, for their shared memory): where there are few tiles, up to eight share one
     const size_t tiles = ceil_div(a.tokens, kDownTokens);
     a.ctas = 1;
     while (a.ctas < 8 && tiles * a.ctas * 2 <= size_t(2 * sms)) a.ctas *= 2;
     TRY(launch(adapter_down_kernel<DT, RT>, dim3(unsigned(tiles * a.ctas)), kAdapterThreads, kDownSmem<RT>, unsigned(a.ctas), a, stream, true));
-    // four CTAs run on an SM at one time; twice as many, so that a tile with two adapters holds up less
+    // four CTAs run on an SM at one time (of more than 64 ranks two); twice as many, so that a tile with two adapters holds up less
     const size_t up_tiles = ceil_div(a.tokens, kUpTokens), all = ceil_div(a.n, kUpFeatures);
     const size_t parts = std::max<size_t>(1, std::min(size_t(8 * sms) / up_tiles, ceil_div(all, 2)));
     a.blocks = int(ceil_div(all, parts));

@@ -101,7 +101,7 @@ int launch_grad(const NormGradArgs& a, int threads, cudaStream_t stream) {
 template <int DT, int W>
 int launch_grad(const NormGradArgs& a, cudaStream_t stream) {
     // Rows that are read by elements or pairs do not go through shared memory: more threads with one piece each, and no registers that spill
-    // (8191 x 5375: 369 us, with three pieces 486)
+    // (8191 x 3839: 156 us, with three pieces 215; 8191 x 5375: 224 and 228; by pairs 8191 x 3838: 96 and 126, 8191 x 5374: 145 and 137)
     const bool narrow = W < 8 && a.cols > kGradColumns && a.cols <= kGradWide * 8 && a.groups == 1;
     if (narrow || wide(a.rows, a.cols)) return launch_grad<DT, W, 1, kGradWide>(a, int(up(ceil_div(a.cols, 8), 32)), stream);
     const int threads = grad_threads(a.cols);
